@@ -291,6 +291,42 @@ moevie_status moevie_moe_backward(const moevie_layer* layer, const void* x, cons
                                   float* dW3, float* dWs1, float* dWs2, float* dWs3, void* ws,
                                   size_t ws_bytes, void* stream);
 
+/* Newton-Schulz orthogonalisation of a stack of N matrices U [rows, cols] (the update of the
+ * Muon optimiser).  With X0 = U / |U|_F (X0 = 0 for U = 0) and, per step, coefficients
+ * (a, b, c) = coef[3 i .. 3 i + 2]:
+ *     A = X X^T,   X <- a X + (b A + c A^2) X,
+ * which moves every singular value s of X0 to the odd quintic a s + b s^3 + c s^5 of itself
+ * and keeps the singular vectors.  (For rows > cols it is formed from X^T X; the result is
+ * the same.)  Each matrix of the stack is treated by itself; one that holds an infinity or a
+ * NaN gives NaN and leaves the others alone.
+ *   U: fp32 (u_bf16 = 0) or bf16 (u_bf16 = 1), row stride ld_u >= cols and matrix stride
+ *   stride_u elements; any alignment of rows (16-byte aligned rows are read faster).
+ *   O: bf16, row stride ld_o >= cols, matrix stride stride_o.  O does not overlap U.
+ * Arithmetic: fp16 tensor-core operands (scaled), fp32 accumulation, X carried in 22 bits:
+ * the result is within 2e-3 (2-norm) of the formula's, before its rounding to bf16.
+ * coef: HOST memory, steps x 3 floats, finite; 1 <= steps <= 32.  Sizes: rows and cols in
+ * [1, 8192], 0 <= N <= 65535, else MOEVIE_ERR_UNSUPPORTED; N == 0 launches nothing.  ws:
+ * moevie_orthogonalize_workspace_size bytes, set up with moevie_workspace_init. */
+moevie_status moevie_orthogonalize_workspace_size(int64_t N, int64_t rows, int64_t cols, size_t* bytes);
+moevie_status moevie_orthogonalize(const void* U, int u_bf16, int64_t ld_u, int64_t stride_u, int64_t N,
+                                   int64_t rows, int64_t cols, const float* coef, int steps, void* O,
+                                   int64_t ld_o, int64_t stride_o, void* ws, size_t ws_bytes, void* stream);
+
+/* One Muon step on a stack of N weight matrices W [rows, cols] (e.g. W1 of all experts with
+ * dW1 of moevie_moe_backward), all in place:
+ *     M <- momentum M + G,     U = G + momentum M (nesterov) or M,
+ *     O = the Newton-Schulz orthogonalisation of U (as moevie_orthogonalize),
+ *     W <- (1 - lr weight_decay) W - lr scale O,      W_bf16 = bf16(W).
+ * W, M, G: fp32, W_bf16: bf16 or NULL; all four have row stride ld (a multiple of 8,
+ * >= cols) and matrix stride `stride` (a multiple of 8, >= rows ld), 16-byte aligned: the
+ * layout of W1 and of dW1.  Pad columns are neither read nor written.  A zero U (an expert
+ * that got no token, without momentum) only decays its weights.  Workspace, coef, steps and
+ * sizes as for moevie_orthogonalize. */
+moevie_status moevie_muon_update(float* W, void* W_bf16, float* M, const float* G, int64_t N, int64_t rows,
+                                 int64_t cols, int64_t ld, int64_t stride, float lr, float momentum,
+                                 int nesterov, float weight_decay, float scale, const float* coef, int steps,
+                                 void* ws, size_t ws_bytes, void* stream);
+
 /* Synchronise `stream`, then read the workspace's device status into *out
  * (MOEVIE_OK when no device-side error was recorded).  `detail` (host, may be
  * NULL) receives 4 ints: code, site, and two values describing the failure. */

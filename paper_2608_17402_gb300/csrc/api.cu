@@ -1,6 +1,7 @@
 // api.cu -- extern "C" entry points of the MoE-ViE layer library (moevie.h,
 // moevie_testing.h): argument checks, workspace carving and launch order.
 // Nothing here allocates, frees or synchronises on the layer path.
+#include <math.h>
 #include <stdint.h>
 #include <string.h>
 
@@ -962,6 +963,95 @@ moevie_status moevie_moe_forward_host(const moevie_layer* layer, const void* x_h
     MV_TRY(cudaEventRecord(p->done, p->out));
     MV_TRY(cudaStreamWaitEvent(s, p->done, 0));
     return MOEVIE_OK;
+}
+
+static moevie_status check_ns(int64_t N, int64_t rows, int64_t cols) {
+    if (N < 0 || rows < 1 || cols < 1) return MOEVIE_ERR_INVALID_ARG;
+    if (N > NS_MAX_COUNT || rows > NS_MAX_DIM || cols > NS_MAX_DIM) return MOEVIE_ERR_UNSUPPORTED;
+    return MOEVIE_OK;
+}
+
+static moevie_status check_coef(const float* coef, int steps) {
+    if (!coef || steps < 1) return MOEVIE_ERR_INVALID_ARG;
+    if (steps > NS_MAX_STEPS) return MOEVIE_ERR_UNSUPPORTED;
+    for (int i = 0; i < 3 * steps; ++i)
+        if (!(fabsf(coef[i]) <= 3.0e38f)) return MOEVIE_ERR_INVALID_ARG;
+    return MOEVIE_OK;
+}
+
+moevie_status moevie_orthogonalize_workspace_size(int64_t N, int64_t rows, int64_t cols, size_t* bytes) {
+    if (!bytes) return MOEVIE_ERR_INVALID_ARG;
+    const moevie_status c = check_ns(N, rows, cols);
+    if (c != MOEVIE_OK) return c;
+    *bytes = ns_workspace_bytes(N, rows, cols);
+    return MOEVIE_OK;
+}
+
+moevie_status moevie_orthogonalize(const void* U, int u_bf16, int64_t ld_u, int64_t stride_u, int64_t N,
+                                   int64_t rows, int64_t cols, const float* coef, int steps, void* O,
+                                   int64_t ld_o, int64_t stride_o, void* ws, size_t ws_bytes, void* stream) {
+    moevie_status c = check_ns(N, rows, cols);
+    if (c == MOEVIE_OK) c = check_coef(coef, steps);
+    if (c != MOEVIE_OK) return c;
+    if (N == 0) return MOEVIE_OK;
+    if (!U || !O || !ws || !a16(ws) || (u_bf16 != 0 && u_bf16 != 1)) return MOEVIE_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(U) % (u_bf16 ? 2 : 4) || reinterpret_cast<uintptr_t>(O) % 2)
+        return MOEVIE_ERR_INVALID_ARG;
+    if (ld_u < cols || ld_o < cols || ld_u >= (int64_t(1) << 31) || ld_o >= (int64_t(1) << 31))
+        return MOEVIE_ERR_INVALID_ARG;
+    if (N > 1 && (stride_u < 0 || stride_o < (rows - 1) * ld_o + cols)) return MOEVIE_ERR_INVALID_ARG;
+    if (ws_bytes < ns_workspace_bytes(N, rows, cols)) return MOEVIE_ERR_WORKSPACE;
+    NsCall q = {};
+    q.N = (int)N;
+    q.r = (int)rows;
+    q.c = (int)cols;
+    q.U = U;
+    q.u_bf16 = u_bf16;
+    q.ld_u = ld_u;
+    q.st_u = N > 1 ? stride_u : 0;   // one matrix: its stride is not used
+    q.O = static_cast<__nv_bfloat16*>(O);
+    q.ld_o = ld_o;
+    q.st_o = N > 1 ? stride_o : 0;
+    q.coef = coef;
+    q.steps = steps;
+    return cuda_status(launch_newton_schulz(q, static_cast<uint8_t*>(ws), num_sms(), WAIT_LIMIT_NS,
+                                            static_cast<cudaStream_t>(stream)));
+}
+
+moevie_status moevie_muon_update(float* W, void* W_bf16, float* M, const float* G, int64_t N, int64_t rows,
+                                 int64_t cols, int64_t ld, int64_t stride, float lr, float momentum,
+                                 int nesterov, float weight_decay, float scale, const float* coef, int steps,
+                                 void* ws, size_t ws_bytes, void* stream) {
+    moevie_status c = check_ns(N, rows, cols);
+    if (c == MOEVIE_OK) c = check_coef(coef, steps);
+    if (c != MOEVIE_OK) return c;
+    if (nesterov != 0 && nesterov != 1) return MOEVIE_ERR_INVALID_ARG;
+    for (const float v : {lr, momentum, weight_decay, scale})
+        if (!(fabsf(v) <= 3.0e38f)) return MOEVIE_ERR_INVALID_ARG;
+    if (N == 0) return MOEVIE_OK;
+    if (!W || !M || !G || !ws) return MOEVIE_ERR_INVALID_ARG;
+    if (!a16(W) || !a16(W_bf16) || !a16(M) || !a16(G) || !a16(ws)) return MOEVIE_ERR_INVALID_ARG;
+    if (ld < cols || ld >= (int64_t(1) << 31) || (N > 1 && stride < rows * ld)) return MOEVIE_ERR_INVALID_ARG;
+    if (ld % 8 != 0 || (N > 1 && stride % 8 != 0)) return MOEVIE_ERR_UNSUPPORTED;
+    if (ws_bytes < ns_workspace_bytes(N, rows, cols)) return MOEVIE_ERR_WORKSPACE;
+    NsCall q = {};
+    q.N = (int)N;
+    q.r = (int)rows;
+    q.c = (int)cols;
+    q.U = G;
+    q.ld_u = ld;
+    q.st_u = N > 1 ? stride : 0;
+    q.M = M;
+    q.momentum = momentum;
+    q.nesterov = nesterov;
+    q.W = W;
+    q.Wb = static_cast<__nv_bfloat16*>(W_bf16);
+    q.decay = 1.0f - lr * weight_decay;
+    q.rate = lr * scale;
+    q.coef = coef;
+    q.steps = steps;
+    return cuda_status(launch_newton_schulz(q, static_cast<uint8_t*>(ws), num_sms(), WAIT_LIMIT_NS,
+                                            static_cast<cudaStream_t>(stream)));
 }
 
 moevie_status moevie_get_device_status(const void* ws, void* stream, moevie_status* out,

@@ -42,6 +42,11 @@ enum Site : int {
     SITE_BIAS_COUNTS = 21,
     SITE_TIMEOUT_PROBE = 30,
     SITE_PERMUTE_BARRIER = 31,
+    SITE_NS_WAIT_EMPTY = 40,
+    SITE_NS_WAIT_FULL = 41,
+    SITE_NS_WAIT_TFULL = 42,
+    SITE_NS_WAIT_TEMPTY = 43,
+    SITE_NS_DRAIN = 44,
 };
 
 __device__ __forceinline__ void report(DevStatus* st, int code, int site, int a, int b) {

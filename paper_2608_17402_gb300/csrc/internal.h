@@ -343,6 +343,33 @@ cudaError_t launch_bwd_router(const int32_t* idx, const float* sig, const float*
 cudaError_t launch_bwd_copy(const float* src, int64_t ld_src, float* dst, int64_t rows, int64_t cols,
                             cudaStream_t s);
 
+// --------------------------------- Newton-Schulz orthogonalisation, optimiser step
+
+constexpr int64_t NS_MAX_DIM = 8192;    // rows and columns of a matrix
+constexpr int64_t NS_MAX_COUNT = 65535; // matrices of a stack
+constexpr int NS_MAX_STEPS = 32;
+
+// A stack of N matrices [r, c] (muon.cu).  U: the update, or with M the gradient; O: the
+// orthogonalised update, or with W the weights it is applied to.
+struct NsCall {
+    int N, r, c;
+    const void* U;            // fp32, or bf16 with u_bf16: row stride ld_u, matrix stride st_u
+    int u_bf16;
+    int64_t ld_u, st_u;
+    float* M;                 // momentum (fp32, laid out as U) or NULL
+    float momentum;
+    int nesterov;
+    __nv_bfloat16* O;         // row stride ld_o, matrix stride st_o; NULL with W
+    int64_t ld_o, st_o;
+    float* W;                 // fp32 weights laid out as U, and their bf16 copy (or NULL)
+    __nv_bfloat16* Wb;
+    float decay, rate;        // W <- decay W - rate O
+    const float* coef;        // host, [steps][3]
+    int steps;
+};
+size_t ns_workspace_bytes(int64_t N, int64_t r, int64_t c);
+cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t limit_ns, cudaStream_t s);
+
 // ---------------------------------------- permute without a caller workspace
 
 // moevie_permute_static keeps its scratch in one fixed device array (in permute.cu):

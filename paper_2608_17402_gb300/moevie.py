@@ -28,6 +28,7 @@ C_ENTRY_POINTS = ("moevie_status_string", "moevie_version", "moevie_workspace_si
                   "moevie_shared_expert", "moevie_combine", "moevie_moe_forward", "moevie_moe_forward_host",
                   "moevie_get_device_status", "moevie_launch_count", "moevie_shared_groups",
                   "moevie_update_bias", "moevie_backward_workspace_size", "moevie_moe_backward",
+                  "moevie_orthogonalize_workspace_size", "moevie_orthogonalize", "moevie_muon_update",
                   "moevie_test_route_logits",
                   "moevie_test_fallback_count", "moevie_test_expert_hidden",
                   "moevie_test_moe_forward_events", "moevie_test_wait_timeout")
@@ -81,6 +82,11 @@ def load():
         "moevie_update_bias": ([P, I64, F, ctypes.c_int, P, P, SZ, P], ctypes.c_int),
         "moevie_backward_workspace_size": ([I64] * 6 + [ctypes.c_int, P], ctypes.c_int),
         "moevie_moe_backward": ([P, P, P, I64, P, P, P, P, P, P, P, P, P, P, SZ, P], ctypes.c_int),
+        "moevie_orthogonalize_workspace_size": ([I64] * 3 + [P], ctypes.c_int),
+        "moevie_orthogonalize": ([P, ctypes.c_int, I64, I64, I64, I64, I64, P, ctypes.c_int, P, I64, I64, P, SZ, P],
+                                 ctypes.c_int),
+        "moevie_muon_update": ([P] * 4 + [I64] * 5 + [F, F, ctypes.c_int, F, F, P, ctypes.c_int, P, SZ, P],
+                               ctypes.c_int),
         "moevie_test_route_logits": ([P, P, I64, I64, I64, P, P, SZ, P], ctypes.c_int),
         "moevie_test_fallback_count": ([P, P, P], ctypes.c_int),
         "moevie_test_expert_hidden": ([P, P, P, P, I64, I64, I64, I64, I64, P, P, SZ, P],
@@ -415,6 +421,83 @@ def moevie_moe_backward(layer: LayerWeights, x, dy, idx, ws: "BackwardWorkspace"
         if name in out:
             out[name] = out[name][..., :w]
     return out
+
+
+# ------------------------------------------- orthogonalised updates (Muon)
+
+NS_COEF = (3.4445, -4.7750, 2.0315)   # quintic with slope 3.4 at 0 and values near 1 on (0.1, 1)
+
+
+def moevie_orthogonalize_workspace_size(N, rows, cols) -> int:
+    out = ctypes.c_size_t(0)
+    _call("moevie_orthogonalize_workspace_size", N, rows, cols, ctypes.byref(out))
+    return out.value
+
+
+class OrthoWorkspace(Workspace):
+    """Caller-owned device scratch of moevie_orthogonalize and moevie_muon_update for stacks
+    of up to ``N`` matrices of this size."""
+
+    def __init__(self, N, rows, cols, device="cuda", stream=None):
+        self.dims = (N, rows, cols)
+        self.nbytes = moevie_orthogonalize_workspace_size(N, rows, cols)
+        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        moevie_workspace_init(self, stream)
+
+
+def _coef(coef, steps):
+    """``coef``: one (a, b, c) for every step, or one per step."""
+    rows = list(coef) if isinstance(coef[0], (tuple, list)) else [coef] * steps
+    if len(rows) != steps or any(len(r) != 3 for r in rows):
+        raise ValueError(f"coef: expected (a, b, c) or {steps} of them")
+    return (ctypes.c_float * (3 * steps))(*(float(v) for r in rows for v in r))
+
+
+def _stack(t, dtypes, name):
+    """A CUDA tensor [N, r, c] or [r, c] with consecutive columns -> (N, r, c, row stride, matrix stride)."""
+    if not (t.is_cuda and t.dtype in dtypes and t.dim() in (2, 3) and (t.shape[-1] <= 1 or t.stride(-1) == 1)):
+        raise ValueError(f"{name}: expected a CUDA tensor [N, rows, cols] or [rows, cols] of {dtypes} with "
+                         f"consecutive columns, got {t.dtype} on {t.device} with shape {tuple(t.shape)} and "
+                         f"strides {t.stride()}")
+    r, c = t.shape[-2:]
+    N = t.shape[0] if t.dim() == 3 else 1
+    ld = t.stride(-2) if r > 1 else max(c, t.stride(-2))
+    return N, r, c, ld, t.stride(0) if N > 1 and t.dim() == 3 else r * ld
+
+
+def moevie_orthogonalize(U, ws: OrthoWorkspace, coef=NS_COEF, steps=5, out=None, stream=None):
+    """Newton-Schulz orthogonalisation of U [N, rows, cols] (or one matrix [rows, cols]), fp32
+    or bf16, each matrix by itself; returns bf16 of U's shape (``out`` when given)."""
+    N, r, c, ld, st = _stack(U, (torch.float32, torch.bfloat16), "U")
+    O = out if out is not None else torch.empty(U.shape, dtype=torch.bfloat16, device=U.device)
+    if O.shape != U.shape:
+        raise ValueError(f"out: expected shape {tuple(U.shape)}, got {tuple(O.shape)}")
+    _, _, _, ldo, sto = _stack(O, (torch.bfloat16,), "out")
+    _call("moevie_orthogonalize", _p(U), int(U.dtype == torch.bfloat16), ld, st, N, r, c, _coef(coef, steps),
+          steps, _p(O), ldo, sto, ws.ptr, ws.nbytes, _stream(stream))
+    return O
+
+
+def moevie_muon_update(W, M, G, ws: OrthoWorkspace, lr, momentum=0.95, weight_decay=0.0, nesterov=True,
+                       scale=None, W_bf16=None, coef=NS_COEF, steps=5, stream=None):
+    """One Muon step, in place on W, M and (when given) the bf16 copy W_bf16 of W.  W, M, G:
+    fp32 [N, rows, cols] (or [rows, cols]) whose rows are row_ld(cols) apart, as W1 and dW1 are
+    (moevie_pad_rows).  ``scale`` multiplies the orthogonalised update (default
+    0.2 sqrt(max(rows, cols)), about the size of an Adam update)."""
+    for name, t, dt in (("W", W, torch.float32), ("M", M, torch.float32), ("G", G, torch.float32),
+                        ("W_bf16", W_bf16, torch.bfloat16)):
+        if t is None and name == "W_bf16":
+            continue
+        if t.dim() not in (2, 3) or t.shape != W.shape:
+            raise ValueError(f"{name}: expected [N, rows, cols] or [rows, cols] as W, got {tuple(t.shape)}")
+        _want_rows(t, dt, name)
+    r, c = W.shape[-2:]
+    N = W.shape[0] if W.dim() == 3 else 1
+    s = 0.2 * max(r, c) ** 0.5 if scale is None else scale
+    _call("moevie_muon_update", _p(W), _p(W_bf16), _p(M), _p(G), N, r, c, row_ld(c), r * row_ld(c), float(lr),
+          float(momentum), int(bool(nesterov)), float(weight_decay), float(s), _coef(coef, steps), steps, ws.ptr,
+          ws.nbytes, _stream(stream))
+    return W
 
 
 def moevie_launch_count() -> int:

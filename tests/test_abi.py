@@ -269,3 +269,43 @@ def test_header_is_plain_c(lib, tmp_path):
     out = subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()
     rc, want = _ws_size(lib, 512, 768, 16, 2, 768, 0)
     assert out == ["0", str(want)] and rc == 0
+
+
+def test_muon_entry_points_validate_before_launch(lib):
+    """moevie_orthogonalize and moevie_muon_update check sizes, strides, pointers, coefficients
+    and the workspace before anything is enqueued."""
+    P = ctypes.c_void_p
+    fake = P(0x1000)
+    coef = (ctypes.c_float * 6)(3.4445, -4.7750, 2.0315, 1.5, -0.5, 0.0)
+
+    def size(*dims):
+        out = ctypes.c_size_t(0)
+        return lib.moevie_orthogonalize_workspace_size(*dims, ctypes.byref(out)), out.value
+    rc, a = size(4, 64, 96)
+    rc2, b = size(8, 64, 96)
+    assert rc == rc2 == 0 and 0 < a < b
+    assert size(-1, 4, 4)[0] == 1 and size(1, 0, 4)[0] == 1
+    assert size(1, 8193, 4)[0] == 2 and size(1, 4, 8193)[0] == 2 and size(65536, 4, 4)[0] == 2
+
+    def ortho(U=fake, bf16=0, ld_u=96, st_u=64 * 96, N=4, r=64, c=96, co=coef, steps=2, O=fake, ld_o=96,
+              st_o=64 * 96, ws=fake, nbytes=1 << 30):
+        return lib.moevie_orthogonalize(U, bf16, ld_u, st_u, N, r, c, co, steps, O, ld_o, st_o, ws, nbytes, None)
+    assert ortho(N=0, U=None, O=None, ws=None, nbytes=0) == 0
+    assert ortho(U=None) == ortho(O=None) == ortho(ws=None) == ortho(co=None) == 1
+    assert ortho(steps=0) == 1 and ortho(steps=33) == 2
+    assert ortho(bf16=2) == 1 and ortho(U=P(0x1002)) == 1 and ortho(U=P(0x1001), bf16=1) == 1
+    assert ortho(ld_u=95) == 1 and ortho(ld_o=95) == 1 and ortho(st_o=64 * 96 - 1) == 1 and ortho(st_u=-8) == 1
+    assert ortho(ws=P(0x1008)) == 1 and ortho(nbytes=a - 1) == 3
+    bad = (ctypes.c_float * 6)(3.4, float("nan"), 2.0, 1.5, -0.5, 0.0)
+    assert ortho(co=bad) == 1
+
+    def muon(W=fake, Wb=fake, M=fake, G=fake, N=4, r=64, c=96, ld=96, st=64 * 96, lr=0.1, steps=2, nest=1,
+             ws=fake, nbytes=1 << 30):
+        return lib.moevie_muon_update(W, Wb, M, G, N, r, c, ld, st, lr, 0.9, nest, 0.0, 1.0, coef, steps, ws,
+                                      nbytes, None)
+    assert muon(N=0, W=None, Wb=None, M=None, G=None, ws=None, nbytes=0) == 0
+    assert muon(W=None) == muon(M=None) == muon(G=None) == muon(ws=None) == 1
+    assert muon(W=P(0x1008)) == muon(Wb=P(0x1004)) == 1
+    assert muon(ld=95) == 1 and muon(ld=100) == 1 and muon(ld=100, st=6400) == 2 and muon(c=90, ld=92, st=64 * 92) == 2
+    assert muon(lr=float("inf")) == 1 and muon(nest=2) == 1 and muon(steps=0) == 1
+    assert muon(nbytes=a - 1) == 3
