@@ -291,6 +291,24 @@ moevie_status moevie_moe_backward(const moevie_layer* layer, const void* x, cons
                                   float* dW3, float* dWs1, float* dWs2, float* dWs3, void* ws,
                                   size_t ws_bytes, void* stream);
 
+/* The whole layer for a few tokens (1 <= T <= MOEVIE_FEW_MAX_TOKENS): the function of
+ * moevie_moe_forward, for callers that run the layer token by token or on small batches, where
+ * its time is that of reading the router and the selected experts once.  GELU or SwiGLU
+ * experts, with or without a shared expert, the layer's weights as for moevie_moe_forward.
+ * idx [T, k] (ascending ids per token) and gate [T, k] are optional outputs (NULL: not
+ * returned).  The selection is that of exact arithmetic up to the rounding of a 64-bit sum
+ * (products of bf16 and fp32 are exact in 64 bits; keys in 64 bits; ties to the lowest id; a
+ * key that is NaN comes after every number).  Hidden activations keep more than bf16's bits, so
+ * y is as precise as 32-bit arithmetic rounded once to bf16.  Each token's y depends on that
+ * token alone, and results do not depend on timing.
+ * Sizes: those of moevie_moe_forward, k <= 32 and d, h, h_s <= 65535; T == 0 launches nothing.
+ * ws: moevie_few_workspace_size(T_max, ...) bytes, set up with moevie_workspace_init. */
+#define MOEVIE_FEW_MAX_TOKENS 64
+moevie_status moevie_few_workspace_size(int64_t T_max, int64_t d, int64_t E, int64_t k, int64_t h,
+                                        int64_t h_s, size_t* bytes);
+moevie_status moevie_moe_few(const moevie_layer* layer, const void* x, int64_t T, void* y, int32_t* idx,
+                             float* gate, void* ws, size_t ws_bytes, void* stream);
+
 /* Newton-Schulz orthogonalisation of a stack of N matrices U [rows, cols] (the update of the
  * Muon optimiser).  With X0 = U / |U|_F (X0 = 0 for U = 0) and, per step, coefficients
  * (a, b, c) = coef[3 i .. 3 i + 2]:

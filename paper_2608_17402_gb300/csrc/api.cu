@@ -965,6 +965,66 @@ moevie_status moevie_moe_forward_host(const moevie_layer* layer, const void* x_h
     return MOEVIE_OK;
 }
 
+static moevie_status check_few_sizes(int64_t T, int64_t d, int64_t E, int64_t k, int64_t h, int64_t hs) {
+    const moevie_status c = check_sizes(T, d, E, k, h, hs);
+    if (c != MOEVIE_OK) return c;
+    if (h < 1) return MOEVIE_ERR_INVALID_ARG;
+    if (T > MOEVIE_FEW_MAX_TOKENS || k > 32 || d > 65535 || h > 65535 || hs > 65535) return MOEVIE_ERR_UNSUPPORTED;
+    return MOEVIE_OK;
+}
+
+moevie_status moevie_few_workspace_size(int64_t T_max, int64_t d, int64_t E, int64_t k, int64_t h,
+                                        int64_t h_s, size_t* bytes) {
+    if (!bytes) return MOEVIE_ERR_INVALID_ARG;
+    const moevie_status c = check_few_sizes(T_max, d, E, k, h, h_s);
+    if (c != MOEVIE_OK) return c;
+    *bytes = few_workspace_bytes(T_max, d, E, k, h, h_s);
+    return MOEVIE_OK;
+}
+
+moevie_status moevie_moe_few(const moevie_layer* Lr, const void* x, int64_t T, void* y, int32_t* idx,
+                             float* gate, void* ws, size_t ws_bytes, void* stream) {
+    if (!Lr) return MOEVIE_ERR_INVALID_ARG;
+    const moevie_status c = check_few_sizes(T, Lr->d, Lr->E, Lr->k, Lr->h, Lr->h_s);
+    if (c != MOEVIE_OK) return c;
+    if (T == 0) return MOEVIE_OK;
+    const bool swiglu = Lr->W3 != nullptr, shared = Lr->h_s > 0;
+    if (!x || !y || !ws || !Lr->W_r || !Lr->b || !Lr->W1 || !Lr->W2) return MOEVIE_ERR_INVALID_ARG;
+    if (shared && (!Lr->Ws1 || !Lr->Ws2 || (swiglu && !Lr->Ws3))) return MOEVIE_ERR_INVALID_ARG;
+    if (!a16(x) || !a16(y) || !a16(ws) || !a16(Lr->W_r) || !a16(Lr->b) || !a16(Lr->W1) || !a16(Lr->W2) ||
+        !a16(Lr->W3) || !a16(idx) || !a16(gate))
+        return MOEVIE_ERR_INVALID_ARG;
+    if (shared && (!a16(Lr->Ws1) || !a16(Lr->Ws2) || (swiglu && !a16(Lr->Ws3)))) return MOEVIE_ERR_INVALID_ARG;
+    if (ws_bytes < few_workspace_bytes(T, Lr->d, Lr->E, Lr->k, Lr->h, Lr->h_s)) return MOEVIE_ERR_WORKSPACE;
+    typedef const __nv_bfloat16* BP;
+    FewArgs a = {};
+    a.x = static_cast<BP>(x);
+    a.W_r = Lr->W_r;
+    a.b = Lr->b;
+    a.W1 = static_cast<BP>(Lr->W1);
+    a.W2 = static_cast<BP>(Lr->W2);
+    a.W3 = static_cast<BP>(Lr->W3);
+    if (shared) {
+        a.Ws1 = static_cast<BP>(Lr->Ws1);
+        a.Ws2 = static_cast<BP>(Lr->Ws2);
+        a.Ws3 = swiglu ? static_cast<BP>(Lr->Ws3) : nullptr;
+    }
+    a.T = (int)T;
+    a.d = (int)Lr->d;
+    a.E = (int)Lr->E;
+    a.k = (int)Lr->k;
+    a.h = (int)Lr->h;
+    a.hs = (int)Lr->h_s;
+    a.hp = row_ld(Lr->h);
+    a.hsp = row_ld(Lr->h_s);
+    a.lambda = Lr->lambda;
+    a.idx = idx;
+    a.gate = gate;
+    a.y = static_cast<__nv_bfloat16*>(y);
+    return cuda_status(launch_few(a, static_cast<uint8_t*>(ws), num_sms(), WAIT_LIMIT_NS,
+                                  static_cast<cudaStream_t>(stream)));
+}
+
 static moevie_status check_ns(int64_t N, int64_t rows, int64_t cols) {
     if (N < 0 || rows < 1 || cols < 1) return MOEVIE_ERR_INVALID_ARG;
     if (N > NS_MAX_COUNT || rows > NS_MAX_DIM || cols > NS_MAX_DIM) return MOEVIE_ERR_UNSUPPORTED;

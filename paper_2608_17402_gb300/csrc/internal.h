@@ -343,6 +343,25 @@ cudaError_t launch_bwd_router(const int32_t* idx, const float* sig, const float*
 cudaError_t launch_bwd_copy(const float* src, int64_t ld_src, float* dst, int64_t rows, int64_t cols,
                             cudaStream_t s);
 
+// ------------------------------------------------ the layer for a few tokens
+
+// Arguments of the few-token layer (few.cu); the workspace pointers are filled in by launch_few.
+struct FewArgs {
+    const __nv_bfloat16* x;
+    const float *W_r, *b;
+    const __nv_bfloat16 *W1, *W2, *W3, *Ws1, *Ws2, *Ws3;   // W3, Ws3: NULL for GELU experts
+    int T, d, E, k, h, hs;
+    int64_t hp, hsp;          // row strides of W1 / W3 and of Ws1 / Ws3
+    float lambda;
+    int32_t* idx;             // outputs; NULL: kept in the workspace
+    float* gate;
+    __nv_bfloat16* y;
+    float *hid, *hid_s;
+    DevStatus* status;
+};
+size_t few_workspace_bytes(int64_t T, int64_t d, int64_t E, int64_t k, int64_t h, int64_t hs);
+cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaStream_t s);
+
 // --------------------------------- Newton-Schulz orthogonalisation, optimiser step
 
 constexpr int64_t NS_MAX_DIM = 8192;    // rows and columns of a matrix

@@ -28,6 +28,7 @@ C_ENTRY_POINTS = ("moevie_status_string", "moevie_version", "moevie_workspace_si
                   "moevie_shared_expert", "moevie_combine", "moevie_moe_forward", "moevie_moe_forward_host",
                   "moevie_get_device_status", "moevie_launch_count", "moevie_shared_groups",
                   "moevie_update_bias", "moevie_backward_workspace_size", "moevie_moe_backward",
+                  "moevie_few_workspace_size", "moevie_moe_few",
                   "moevie_orthogonalize_workspace_size", "moevie_orthogonalize", "moevie_muon_update",
                   "moevie_test_route_logits",
                   "moevie_test_fallback_count", "moevie_test_expert_hidden",
@@ -82,6 +83,8 @@ def load():
         "moevie_update_bias": ([P, I64, F, ctypes.c_int, P, P, SZ, P], ctypes.c_int),
         "moevie_backward_workspace_size": ([I64] * 6 + [ctypes.c_int, P], ctypes.c_int),
         "moevie_moe_backward": ([P, P, P, I64, P, P, P, P, P, P, P, P, P, P, SZ, P], ctypes.c_int),
+        "moevie_few_workspace_size": ([I64] * 6 + [P], ctypes.c_int),
+        "moevie_moe_few": ([P, P, I64, P, P, P, P, SZ, P], ctypes.c_int),
         "moevie_orthogonalize_workspace_size": ([I64] * 3 + [P], ctypes.c_int),
         "moevie_orthogonalize": ([P, ctypes.c_int, I64, I64, I64, I64, I64, P, ctypes.c_int, P, I64, I64, P, SZ, P],
                                  ctypes.c_int),
@@ -421,6 +424,47 @@ def moevie_moe_backward(layer: LayerWeights, x, dy, idx, ws: "BackwardWorkspace"
         if name in out:
             out[name] = out[name][..., :w]
     return out
+
+
+# ------------------------------------------------ the layer for a few tokens
+
+FEW_MAX_TOKENS = 64   # MOEVIE_FEW_MAX_TOKENS
+
+
+def moevie_few_workspace_size(T_max, d, E, k, h, h_s=0) -> int:
+    out = ctypes.c_size_t(0)
+    _call("moevie_few_workspace_size", T_max, d, E, k, h, h_s, ctypes.byref(out))
+    return out.value
+
+
+class FewWorkspace(Workspace):
+    """Caller-owned device scratch of moevie_moe_few (up to ``T_max`` <= 64 tokens)."""
+
+    def __init__(self, T_max, d, E, k, h, h_s=0, device="cuda", stream=None):
+        self.dims = (T_max, d, E, k, h, h_s)
+        self.nbytes = moevie_few_workspace_size(T_max, d, E, k, h, h_s)
+        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        moevie_workspace_init(self, stream)
+
+
+def moevie_moe_few(layer: LayerWeights, x, ws: FewWorkspace, y=None, routing=False, stream=None):
+    """The layer forward for up to 64 tokens x bf16 [T, d]; returns y bf16 [T, d], with
+    ``routing=True`` (y, idx int32 [T, k], gate fp32 [T, k])."""
+    _want(x, torch.bfloat16, "x")
+    T, d = x.shape
+    k = layer.k
+    if d != layer.W_r.shape[0]:
+        raise ValueError(f"x: expected [T, {layer.W_r.shape[0]}], got {tuple(x.shape)}")
+    dev = x.device
+    y = _want(y, torch.bfloat16, "y") if y is not None else torch.empty((T, d), dtype=torch.bfloat16, device=dev)
+    if y.shape != x.shape:
+        raise ValueError(f"y: expected {tuple(x.shape)}, got {tuple(y.shape)}")
+    idx = torch.empty((T, k), dtype=torch.int32, device=dev) if routing else None
+    gate = torch.empty((T, k), dtype=torch.float32, device=dev) if routing else None
+    L = layer.c_struct()
+    _call("moevie_moe_few", ctypes.byref(L), _p(x), T, _p(y), _p(idx), _p(gate), ws.ptr, ws.nbytes,
+          _stream(stream))
+    return (y, idx, gate) if routing else y
 
 
 # ------------------------------------------- orthogonalised updates (Muon)

@@ -309,3 +309,35 @@ def test_muon_entry_points_validate_before_launch(lib):
     assert muon(ld=95) == 1 and muon(ld=100) == 1 and muon(ld=100, st=6400) == 2 and muon(c=90, ld=92, st=64 * 92) == 2
     assert muon(lr=float("inf")) == 1 and muon(nest=2) == 1 and muon(steps=0) == 1
     assert muon(nbytes=a - 1) == 3
+
+
+def test_few_token_entry_point_validates_before_launch(lib):
+    from paper_2608_17402_gb300.moevie import _Layer
+    P = ctypes.c_void_p
+    fake = 0x1000
+
+    def size(*dims):
+        out = ctypes.c_size_t(0)
+        return lib.moevie_few_workspace_size(*dims, ctypes.byref(out)), out.value
+    prev = 0
+    for T in range(0, 65):
+        rc, n = size(T, 1664, 256, 8, 416, 416)
+        assert rc == 0 and n >= prev, T
+        prev = n
+    assert size(65, 64, 8, 2, 32, 0)[0] == 2 and size(8, 64, 64, 33, 32, 0)[0] == 2
+    assert size(8, 60, 8, 2, 32, 0)[0] == 2 and size(8, 64, 8, 2, 70000, 0)[0] == 2
+    assert size(-1, 64, 8, 2, 32, 0)[0] == 1 and size(8, 64, 8, 2, 0, 0)[0] == 1
+
+    def few(layer, T=4, x=fake, y=fake, idx=fake, gate=fake, ws=fake, nbytes=1 << 30):
+        return lib.moevie_moe_few(ctypes.byref(layer) if layer else None, P(x), T, P(y), P(idx), P(gate), P(ws),
+                                  nbytes, None)
+    L = _Layer(16, 8, 2, 32, 0, fake, fake, fake, fake, 0, 0, 1.0)
+    assert few(None) == 1
+    assert few(L, T=0, x=0, y=0, ws=0, nbytes=0) == 0
+    assert few(L, nbytes=16) == 3
+    assert few(L, T=65) == 2
+    assert few(L, x=0) == few(L, y=0) == few(L, ws=0) == 1
+    assert few(L, x=fake + 8) == few(L, y=fake + 2) == few(L, idx=fake + 4) == few(L, gate=fake + 4) == 1
+    assert few(_Layer(16, 8, 2, 32, 32, fake, fake, fake, fake, fake, 0, 1.0)) == 1          # shared, no Ws2
+    assert few(_Layer(16, 8, 2, 32, 32, fake, fake, fake, fake, fake, fake, 1.0, fake, 0)) == 1   # no Ws3
+    assert few(_Layer(16, 8, 2, 32, 0, fake, fake, fake + 4, fake, 0, 0, 1.0)) == 1          # misaligned W1
