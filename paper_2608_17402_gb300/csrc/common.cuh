@@ -47,6 +47,13 @@ enum Site : int {
     SITE_NS_WAIT_TFULL = 42,
     SITE_NS_WAIT_TEMPTY = 43,
     SITE_NS_DRAIN = 44,
+    SITE_FEW_WAIT_EMPTY = 50,
+    SITE_FEW_WAIT_FULL = 51,
+    SITE_FEW_WAIT_TFULL = 52,
+    SITE_FEW_WAIT_TEMPTY = 53,
+    SITE_FEW_WAIT_UP = 54,
+    SITE_FEW_BARRIER = 55,
+    SITE_FEW_DRAIN = 56,
 };
 
 __device__ __forceinline__ void report(DevStatus* st, int code, int site, int a, int b) {

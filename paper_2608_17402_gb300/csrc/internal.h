@@ -298,6 +298,9 @@ bool make_rows_tmap(CUtensorMap* tm, const void* base, int64_t cols, int64_t row
 // stride g_ld elements, multiples of 8), box {64, box_n, 1}.
 bool make_kmajor_tmap(CUtensorMap* tm, const void* base, int64_t K, int64_t N, int64_t G, int64_t k_ld,
                       int64_t g_ld, int box_n);
+// The 2-D row tensor map of A[rows][cols] bf16 (row stride ld elements) with one-row boxes
+// of 64 columns, for row gathers.
+bool make_gather_tmap(CUtensorMap* tm, const void* base, int64_t cols, int64_t rows, int64_t ld);
 // Picks BN (multiple of 32, <= 256) and the number of N tiles for width N.
 void choose_bn(int N, int* BN, int* n_ntiles);
 cudaError_t launch_grouped_gemm(const GemmArgs& a, int grid, cudaStream_t s);
@@ -345,7 +348,8 @@ cudaError_t launch_bwd_copy(const float* src, int64_t ld_src, float* dst, int64_
 
 // ------------------------------------------------ the layer for a few tokens
 
-// Arguments of the few-token layer (few.cu); the workspace pointers are filled in by launch_few.
+// Arguments of the few-token layer (few.cu).  The caller fills in the first block; launch_few
+// the rest.
 struct FewArgs {
     const __nv_bfloat16* x;
     const float *W_r, *b;
@@ -356,8 +360,25 @@ struct FewArgs {
     int32_t* idx;             // outputs; NULL: kept in the workspace
     float* gate;
     __nv_bfloat16* y;
-    float *hid, *hid_s;
+
+    CUtensorMap tW1, tW3, tW2, tS1, tS3, tS2;   // weights, 3-D {N, K, E}, boxes 64 x 64
+    CUtensorMap tX;                             // token rows, one-row boxes (gather)
+    CUtensorMap tH, tHs;                        // hidden rows, 3-D {h, rows, 2}, boxes 64 x 16
+    float *part, *wsq;        // router: partial logits [rt_parts][T][E], sums of squares [rt_parts][E]
+    int32_t *done_up, *up_cnt, *y_cnt;          // counters, n_counters in a row from done_up
+    int n_counters;
+    float* up_part;           // partial up-projections [item][1 or 2][nb][128]
+    __nv_bfloat16 *H, *Hs;    // hidden rows, hi then lo: [2][T k][ldh], [2][T][ldhs]
+    float* y_part;            // partial outputs [P2][T k][d], [P2s][T][d]
+    int ldh, ldhs, na_max;    // na_max: bound on the experts with tokens
+    int nb;                   // token columns of a tile at most (T rounded up to 16)
+    int nt, nt_s, ntd;        // 128-column tiles of h, h_s and d
+    int nkb_d, nkb_h, nkb_hs; // 64-row blocks of K
+    int acc_cols, tmem_cols;
+    int rt_eb, rt_parts, rt_dch;   // router: blocks of 8 experts, parts of d and their length
+    float rt_err;             // logit error bound over |x| |W_r[:, e]|
     DevStatus* status;
+    uint64_t limit_ns;
 };
 size_t few_workspace_bytes(int64_t T, int64_t d, int64_t E, int64_t k, int64_t h, int64_t hs);
 cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaStream_t s);
