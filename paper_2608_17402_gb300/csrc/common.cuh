@@ -24,7 +24,9 @@ struct DevStatus {
     int fb_count;    // router: tokens re-decided with exact logits in the last call
     int bar_count;   // grid barrier of a cooperative launch: arrivals so far (0 between barriers)
     int bar_gen;     //   and the barrier's generation (bumped by the last arrival)
-    int pad[57];
+    int pad0;
+    unsigned long long few_arrivals;   // grid barriers of the few-token kernel: CTAs arrived so far
+    int pad[54];
 };
 static_assert(sizeof(DevStatus) == 256, "status block is 256 bytes");
 
@@ -119,6 +121,16 @@ __device__ __forceinline__ uint64_t globaltimer_ns() {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
     return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+
+// True in one lane of a converged warp.  A role that a single thread plays branches on this
+// rather than on a lane number: the compiler then knows that the branch has one active thread
+// and issues tcgen05.mma and TMA instructions from uniform registers directly, instead of
+// looping over possibly active lanes (measured: 25 instead of 61 cycles per TMA instruction).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0;
 }
 
 // --------------------------------------------------------------- mbarrier
@@ -388,6 +400,40 @@ __device__ __forceinline__ float rcp_approx(float x) {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+
+// GELU(u) = u/2 (1 + erf(u / sqrt 2)) = max(u, 0) - |u|/2 erfc(|u| / sqrt 2), the
+// second form free of the cancellation of 1 + erf for u < 0.  erfc from Abramowitz &
+// Stegun 7.1.28: erfc(z) = (1 + a1 z + a2 z^2 + ... + a6 z^6)^-16 for z >= 0, with
+// |error| <= 3e-7 (one reciprocal and no exponential; the sixteenth power by four
+// squarings, which overflow to +inf, and so to erfc = 0, only where erfc is far
+// below fp32 resolution).  Evaluated in fp32 the GELU error stays below 1e-6 in
+// absolute value; the hidden activation is then rounded to bf16 (2^-9 relative).
+// Two values at a time with the packed fp32x2 instructions.
+__device__ __forceinline__ void erfc_as2(float a0, float a1, float& q0, float& q1) {   // a0, a1 >= 0
+    const uint64_t z = f2_mul(f2_pack(a0, a1), f2_pack(0.70710678118654752f, 0.70710678118654752f));
+    uint64_t P = f2_fma(z, f2_pack(0.0000430638f, 0.0000430638f), f2_pack(0.0002765672f, 0.0002765672f));
+    P = f2_fma(P, z, f2_pack(0.0001520143f, 0.0001520143f));
+    P = f2_fma(P, z, f2_pack(0.0092705272f, 0.0092705272f));
+    P = f2_fma(P, z, f2_pack(0.0422820123f, 0.0422820123f));
+    P = f2_fma(P, z, f2_pack(0.0705230784f, 0.0705230784f));
+    P = f2_fma(P, z, f2_pack(1.0f, 1.0f));
+    P = f2_mul(P, P);
+    P = f2_mul(P, P);
+    P = f2_mul(P, P);
+    P = f2_mul(P, P);
+    float p0, p1;
+    f2_unpack(P, p0, p1);
+    q0 = rcp_approx(p0);
+    q1 = rcp_approx(p1);
+}
+
+__device__ __forceinline__ void gelu_erf2(float& u0, float& u1) {
+    float q0, q1;
+    erfc_as2(fabsf(u0), fabsf(u1), q0, q1);
+    const uint64_t r = f2_fma(f2_mul(f2_pack(fabsf(u0), fabsf(u1)), f2_pack(-0.5f, -0.5f)), f2_pack(q0, q1),
+                              f2_pack(fmaxf(u0, 0.0f), fmaxf(u1, 0.0f)));
+    f2_unpack(r, u0, u1);
 }
 
 __device__ __forceinline__ void unpack_bf16x8(const uint4& u, float (&v)[8]) {

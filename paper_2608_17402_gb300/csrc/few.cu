@@ -12,18 +12,18 @@
 //      whose margin exceeds the key errors is the exact one.  Otherwise the experts near the
 //      boundary get 64-bit logits and keys.  Up to FEW_SEL_WARPS tokens every CTA selects for
 //      itself (no second barrier); above, the CTAs share the tokens out and meet again.
-//   3. Expert products on tcgen05 with the weights as the M operand: D[128 columns of W, tokens]
-//      = W^T . x^T.  W tiles go from HBM to shared memory by TMA as they lie (MN-major, 128-byte
-//      swizzle) and no thread touches them again; the tokens of the expert (TMA row gather) are
-//      the N operand, 16 to 64 columns, so the tensor cores do in passing what would otherwise
-//      cost an unpack and an FMA per weight and token.  Items (expert, 128 columns, part of K)
-//      are dealt to the CTAs round-robin, K split so that they come out even.
-//   4. Up items: the last of an item's K parts to finish adds them in order, applies the
-//      activation and stores it as two bf16 pieces (hi + lo, 16 bits) so that y is rounded to
-//      bf16 once.  Down items wait for their expert's up items (a counter), while their weights
-//      are already on the way: the weight loads run ahead of the wait by the whole ring.
+//   3. Expert products on tcgen05 with the weights as the M operand: D[columns of W, tokens] =
+//      W^T . x^T.  W tiles (64 or 128 columns, 64 rows of K at a time) go from HBM to shared
+//      memory by TMA as they lie (MN-major, 128-byte swizzle) and no thread touches them again;
+//      the tokens of the expert (TMA row gather) are the N operand, 16 to 64 columns, so the
+//      tensor cores do in passing what would otherwise cost an unpack and an FMA per weight and
+//      token.  Items (expert, columns) are dealt to the CTAs round-robin.
+//   4. Up items apply the activation and store it as two bf16 pieces (hi + lo, 16 bits) so that y
+//      is rounded to bf16 once.  Down items (expert, columns, part of K) wait for their expert's up
+//      items (a counter), while their weights are already on the way: the weight loads run ahead
+//      of the wait by the whole ring.
 //   5. Down items leave fp32 partial rows; whoever completes the last contribution to a token's
-//      128 columns of y adds them up in slot order (no float atomics: results do not depend on
+//      columns of y adds them up in slot order (no float atomics: results do not depend on
 //      timing).
 //
 // Waits between CTAs rely on co-residency (cooperative launch) and on the item order: every
@@ -37,7 +37,7 @@ namespace mv {
 
 namespace {
 
-constexpr int FEW_EPI_WARPS = 8;      // two per TMEM lane quadrant, alternate groups of 8 tokens
+constexpr int FEW_EPI_WARPS = 8;      // two groups of four (one warp per TMEM lane quadrant)
 constexpr int FEW_WARP_W = 8;         // weight loads
 constexpr int FEW_WARP_MMA = 9;
 constexpr int FEW_WARP_B = 10;        // token / hidden loads
@@ -46,15 +46,26 @@ constexpr int FEW_THREADS = FEW_WARPS * 32;
 constexpr int FEW_SEL_WARPS = 8;      // tokens that every CTA selects for itself
 constexpr int FEW_TILE_BYTES = 128 * 64 * 2;   // 128 columns x 64 K rows of a weight matrix
 constexpr int FEW_RT_K = 512;         // rows of W_r staged at a time
-constexpr int FEW_RT_XLD = FEW_RT_K + 4;       // float row strides of the staged x and W_r^T
-constexpr int FEW_RT_WLD = FEW_RT_K + 16;      //   (bank-conflict-free 16-byte reads)
-constexpr int FEW_SMEM_MAX = 232448 - 256;   // 227 KB less the kernel's static variables
-constexpr int FEW_BAR_BYTES = 512;
-// Splits of K: at most FEW_MAX_P parts of an up item (FEW_MAX_PART items in all when split, the
-// size of the partial buffer), FEW_MAX_P2 of a routed and FEW_MAX_P2S of a shared down item.
-constexpr int FEW_MAX_P = 8, FEW_MAX_PART = 640, FEW_MAX_P2 = 4, FEW_MAX_P2S = 8;
+constexpr int FEW_RT_XLD = FEW_RT_K + 16;      // row strides of the staged x (bf16; rows 16-byte
+constexpr int FEW_RT_WLD = FEW_RT_K + 4;       //   aligned) and W_r^T (fp32)
+constexpr int FEW_SMEM_MAX = 232448 - 3072;   // 227 KB less the kernel's static variables
+constexpr int FEW_BAR_BYTES = 512, FEW_FLAG_BYTES = 576;
+// Parts of K at most: of a routed and of a shared down item.
+constexpr int FEW_MAX_P2 = 4, FEW_MAX_P2S = 8;
 
-__device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ int up16(int v) { return (v + 15) & ~15; }
+// Barrier of one epilogue group's 128 threads.
+__device__ __forceinline__ void epi_sync(int group) { asm volatile("bar.sync %0, 128;" ::"r"(group + 1) : "memory"); }
+// Counter updates that publish what the group wrote before its barrier, and (acq_rel) order
+// later reads after the other contributors' writes.
+__device__ __forceinline__ void add_release(int32_t* p, int v) {
+    asm volatile("red.add.release.gpu.global.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+__device__ __forceinline__ int add_acq_rel(int32_t* p, int v) {
+    int old;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
+    return old;
+}
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 __device__ __forceinline__ int ld_acquire(const int32_t* p) {
     int v;
@@ -70,79 +81,114 @@ __device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[
         : "memory");
 }
 
-__device__ __forceinline__ float act_gelu(float u) { return 0.5f * u * (1.0f + erff(u * 0.70710678118654752f)); }
-__device__ __forceinline__ float act_silu(float u) { return u / (1.0f + expf(-u)); }
+// Grid barrier on a counter that only grows (64 bits; every launch adds the same multiple of the
+// grid's size): one atomic per CTA and no reset, so its cost is two trips to L2.  Gives up
+// after the time limit (false, recorded).
+__device__ bool few_barrier(DevStatus* st, uint64_t limit_ns) {
+    __shared__ int s_ok;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        unsigned long long ticket, now;
+        asm volatile("atom.add.acq_rel.gpu.global.u64 %0, [%1], 1;" : "=l"(ticket) : "l"(&st->few_arrivals) : "memory");
+        const unsigned long long want = (ticket / gridDim.x + 1) * gridDim.x;
+        const uint64_t t0 = globaltimer_ns();
+        int ok = 1;
+        for (uint32_t i = 1;; ++i) {
+            asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(now) : "l"(&st->few_arrivals) : "memory");
+            if (now >= want) break;
+            if ((i & 63u) == 0u && globaltimer_ns() - t0 > limit_ns) {
+                ok = 0;
+                report(st, MOEVIE_ERR_TIMEOUT, SITE_FEW_BARRIER, (int)blockIdx.x, (int)(want - now));
+                break;
+            }
+        }
+        s_ok = ok;
+    }
+    __syncthreads();
+    return s_ok != 0;
+}
 
 // ------------------------------------------------------------- 1. logits
 
-// part[ds][t][e] and wsq[ds][e] of this CTA's blocks of 8 experts x parts of d.  smem: staged
-// x [8 TG][FEW_RT_XLD], W_r^T [8][FEW_RT_WLD], then the per-warp sums.
-__device__ void few_logits(const FewArgs& p, float* smem) {
+// part[ds][t][e] and wsq[ds][e] of this CTA's blocks of 8 experts x parts of d.  Up to
+// FEW_RT_K rows at a time are staged by cp.async, all copies in flight at once: x as bf16
+// [8 TG][FEW_RT_XLD], W_r^T as fp32 [8][FEW_RT_WLD].  A warp sums 8 tokens (group g) over its
+// share kp of K; lane (ep, ks): experts ep and ep + 4, four K of every 32.
+__device__ void few_logits(const FewArgs& p, uint8_t* smem) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int TG = (p.T + 7) / 8, KP = FEW_WARPS / TG;
-    float* xs = smem;
-    float* ws = xs + 8 * TG * FEW_RT_XLD;
+    float* ws = reinterpret_cast<float*>(smem);
     float* red = ws + 8 * FEW_RT_WLD;      // [KP][8 TG][8]
     float* redq = red + FEW_WARPS * 64;    // [KP][8]
-    const int g = warp % TG, kp = warp / TG, e8 = lane >> 2, ks = lane & 3;
+    __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(redq + FEW_WARPS * 8);
+    const int g = warp % TG, kp = warp / TG, ep = lane >> 3, ks = lane & 7;
     for (int item = blockIdx.x; item < p.rt_eb * p.rt_parts; item += gridDim.x) {
         const int e0 = item % p.rt_eb * 8, ds = item / p.rt_eb;
         const int d0 = ds * p.rt_dch, d1 = min(p.d, d0 + p.rt_dch);
-        float acc2[8] = {}, sq = 0.f;
+        float tot[2][8] = {}, sq[2] = {};
         for (int k0 = d0; k0 < d1; k0 += FEW_RT_K) {
-            const int kc = min(FEW_RT_K, d1 - k0), kcp = (kc + 15) & ~15;
+            const int kc = min(FEW_RT_K, d1 - k0), kcp = (kc + 31) & ~31;
             for (int q = threadIdx.x; q < kcp * 8; q += FEW_THREADS) {
                 const int r = q >> 3, e = q & 7;
-                ws[e * FEW_RT_WLD + r] =
-                    (r < kc && e0 + e < p.E) ? __ldg(p.W_r + (int64_t)(k0 + r) * p.E + e0 + e) : 0.f;
+                const bool in = r < kc && e0 + e < p.E;
+                const float* src = p.W_r + (in ? (int64_t)(k0 + r) * p.E + e0 + e : 0);
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(
+                                 smem_u32(ws + e * FEW_RT_WLD + r)), "l"(src), "r"(in ? 4u : 0u)
+                             : "memory");
             }
-            const int n8 = kcp / 8;   // kc is a multiple of 8, as d and the parts are
-            for (int q = threadIdx.x; q < p.T * n8; q += FEW_THREADS) {
-                const int t = q / n8, c = (q - t * n8) * 8;
-                float v[8] = {};
-                if (c < kc) unpack_bf16x8(__ldg(reinterpret_cast<const uint4*>(p.x + (int64_t)t * p.d + k0 + c)), v);
-                float4* o = reinterpret_cast<float4*>(xs + t * FEW_RT_XLD + c);
-                o[0] = make_float4(v[0], v[1], v[2], v[3]);
-                o[1] = make_float4(v[4], v[5], v[6], v[7]);
-            }
+            for (int t = warp; t < p.T; t += FEW_WARPS)
+                for (int c = lane * 8; c < kcp; c += 256)   // kc is a multiple of 8, as d and the parts are
+                    cp_async16(smem_u32(xs + t * FEW_RT_XLD + c), c < kc ? p.x + (int64_t)t * p.d + k0 + c : p.x,
+                               c < kc ? 16u : 0u);
+            cp_async_wait_all();
             __syncthreads();
             if (kp < KP) {
-                float acc[8] = {};
-                const int nit = kcp / 16;
+                float acc[2][8] = {};
                 int n = 0;
-                for (int it = kp; it < nit; it += KP) {
-                    const int k = it * 16 + ks * 4;
-                    const float4 w = *reinterpret_cast<const float4*>(ws + e8 * FEW_RT_WLD + k);
-                    sq = fmaf(w.x, w.x, fmaf(w.y, w.y, fmaf(w.z, w.z, fmaf(w.w, w.w, sq))));
+                for (int it = kp; it < kcp / 32; it += KP) {
+                    const int k = it * 32 + ks * 4;
+                    const float4 w0 = *reinterpret_cast<const float4*>(ws + ep * FEW_RT_WLD + k);
+                    const float4 w1 = *reinterpret_cast<const float4*>(ws + (ep + 4) * FEW_RT_WLD + k);
+                    sq[0] = fmaf(w0.x, w0.x, fmaf(w0.y, w0.y, fmaf(w0.z, w0.z, fmaf(w0.w, w0.w, sq[0]))));
+                    sq[1] = fmaf(w1.x, w1.x, fmaf(w1.y, w1.y, fmaf(w1.z, w1.z, fmaf(w1.w, w1.w, sq[1]))));
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {   // (rows past T hold no token: their sums are dropped)
-                        const float4 x = *reinterpret_cast<const float4*>(xs + (8 * g + i) * FEW_RT_XLD + k);
-                        acc[i] = fmaf(x.w, w.w, fmaf(x.z, w.z, fmaf(x.y, w.y, fmaf(x.x, w.x, acc[i]))));
+                        const uint2 xx = *reinterpret_cast<const uint2*>(xs + (8 * g + i) * FEW_RT_XLD + k);
+                        const float x0 = __uint_as_float(xx.x << 16), x1 = __uint_as_float(xx.x & 0xffff0000u);
+                        const float x2 = __uint_as_float(xx.y << 16), x3 = __uint_as_float(xx.y & 0xffff0000u);
+                        acc[0][i] = fmaf(x3, w0.w, fmaf(x2, w0.z, fmaf(x1, w0.y, fmaf(x0, w0.x, acc[0][i]))));
+                        acc[1][i] = fmaf(x3, w1.w, fmaf(x2, w1.z, fmaf(x1, w1.y, fmaf(x0, w1.x, acc[1][i]))));
                     }
-                    if ((++n & 3) == 0) {   // short chains: 16 products, then their sums
+                    if (++n & 1) continue;   // short chains: 8 products, then their sums
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            acc2[i] += acc[i];
-                            acc[i] = 0.f;
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            tot[u][i] += acc[u][i];
+                            acc[u][i] = 0.f;
                         }
-                    }
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc2[i] += acc[i];
+                for (int i = 0; i < 8; ++i) {
+                    tot[0][i] += acc[0][i];
+                    tot[1][i] += acc[1][i];
+                }
             }
             __syncthreads();
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            acc2[i] += __shfl_xor_sync(0xffffffffu, acc2[i], 1);
-            acc2[i] += __shfl_xor_sync(0xffffffffu, acc2[i], 2);
-        }
-        sq += __shfl_xor_sync(0xffffffffu, sq, 1);
-        sq += __shfl_xor_sync(0xffffffffu, sq, 2);
-        if (kp < KP && ks == 0) {
+        for (int u = 0; u < 2; ++u) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) red[(kp * 8 * TG + 8 * g + i) * 8 + e8] = acc2[i];
-            if (g == 0) redq[kp * 8 + e8] = sq;
+            for (int o = 1; o < 8; o <<= 1) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) tot[u][i] += __shfl_xor_sync(0xffffffffu, tot[u][i], o);
+                sq[u] += __shfl_xor_sync(0xffffffffu, sq[u], o);
+            }
+            if (kp < KP && ks == 0) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) red[(kp * 8 * TG + 8 * g + i) * 8 + ep + 4 * u] = tot[u][i];
+                if (g == 0) redq[kp * 8 + ep + 4 * u] = sq[u];
+            }
         }
         __syncthreads();
         for (int q = threadIdx.x; q < (p.T + 1) * 8; q += FEW_THREADS) {
@@ -169,164 +215,204 @@ __device__ __forceinline__ uint32_t key_order(float f) {
     const uint32_t u = __float_as_uint(f + 0.0f);   // -0 -> +0
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
-__device__ __forceinline__ float warp_min(float v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = fminf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
-}
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
-}
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
-// x_t . W_r[:, e] in 64 bits, by one warp (every lane gets the sum).
-__device__ double few_exact_logit(const FewArgs& p, int t, int e) {
-    const int lane = threadIdx.x & 31;
-    double s = 0.0;
-#pragma unroll 4
-    for (int i = lane; i < p.d; i += 32)
-        s = fma((double)__bfloat162float(p.x[(int64_t)t * p.d + i]), (double)__ldg(p.W_r + (int64_t)i * p.E + e), s);
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+// Sum of up to 8 values `stride` floats apart, all loads in flight at once, added in order.
+__device__ __forceinline__ float sum_parts(const float* q, int64_t stride, int n) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? __ldcg(q + j * stride) : 0.f;
+    float s = v[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) s += v[j];
     return s;
 }
 
-// Selection and gates of token t by one warp.  buf: 24 bytes per expert (E rounded up to 32).
-// Lane l holds experts l, l + 32, ...; bit q of its masks stands for expert 32 q + l.
-__device__ void few_select(const FewArgs& p, int t, uint8_t* buf, int32_t* out_idx, float* out_gate) {
-    const int lane = threadIdx.x & 31, NQ = (p.E + 31) / 32, Ep = NQ * 32;
-    double* kd = reinterpret_cast<double*>(buf);
-    float* key = reinterpret_cast<float*>(kd + Ep);
-    float* lg = key + Ep;
-    float* er = lg + Ep;
-    const __nv_bfloat16* x = p.x + (int64_t)t * p.d;
-    float x2 = 0.f;
-    for (int c = lane; c < p.d / 8; c += 32) {
+// |x_t|, by one warp.
+__device__ __forceinline__ float few_norm(const FewArgs& p, int t) {
+    const uint4* x = reinterpret_cast<const uint4*>(p.x + (int64_t)t * p.d);
+    float s = 0.f;
+#pragma unroll 4
+    for (int c = threadIdx.x & 31; c < p.d / 8; c += 32) {
         float v[8];
-        unpack_bf16x8(__ldg(reinterpret_cast<const uint4*>(x) + c), v);
+        unpack_bf16x8(__ldg(x + c), v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x2 = fmaf(v[i], v[i], x2);
+        for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
     }
-    const float xn = sqrtf(warp_sum(x2)) * p.rt_err;
-    uint32_t have = 0, sel = 0;
-    for (int q = 0; q < NQ; ++q) {
-        const int e = q * 32 + lane;
-        if (e >= p.E) break;
-        have |= 1u << q;
-        float s = 0.f, w2 = 0.f;
-        for (int j = 0; j < p.rt_parts; ++j) {
-            s += __ldcg(p.part + ((int64_t)j * p.T + t) * p.E + e);
-            w2 += __ldcg(p.wsq + j * p.E + e);
-        }
-        const float v = 1.0f / (1.0f + expf(-s)) + __ldg(p.b + e);
-        lg[e] = s;
-        key[e] = v;
-        // a quarter of the logit's error (the sigmoid's largest slope) and the fp32 evaluation
-        er[e] = 0.25f * xn * sqrtf(w2) + 1e-6f * (1.0f + fabsf(v));
+    return sqrtf(warp_sum(s));
+}
+
+// Bytes of shared memory per expert (E rounded up to 32) that one token's selection takes:
+// 64-bit key, order of the fp32 key, logit, key half-width, list of experts to decide exactly.
+constexpr int FEW_SEL_BYTES = 24;
+
+// The float that key_order maps to u (NaN for 1).
+__device__ __forceinline__ float key_value(uint32_t u) {
+    return __uint_as_float((u & 0x80000000u) ? u ^ 0x80000000u : ~u);
+}
+
+// Selection and gates of the CTA's tokens t0, t0 + step, ... (n <= FEW_SEL_WARPS of them), by all
+// threads.  xn: |x_t| of each.  buf: FEW_SEL_BYTES per expert and token.  A thread takes
+// (token, expert) pairs, a warp 32 consecutive experts of one token; the selected are those
+// with fewer than k experts ahead of them (larger key, or the same and a lower id), counted
+// directly: no round waits for another.
+__device__ void few_select(const FewArgs& p, int t0, int step, int n, const float* xn, uint8_t* buf,
+                           int32_t* out_idx, float* out_gate) {
+    __shared__ uint32_t s_lo[FEW_SEL_WARPS], s_hi[FEW_SEL_WARPS], s_sel[FEW_SEL_WARPS][32];
+    __shared__ int n_cand[FEW_SEL_WARPS];
+    __shared__ float s_sig[FEW_SEL_WARPS][32];
+    __shared__ double part64[FEW_WARPS][4];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, NQ = (p.E + 31) / 32, Ep = NQ * 32;
+    auto base = [&](int w) { return buf + (size_t)w * Ep * FEW_SEL_BYTES; };
+    auto kd_of = [&](int w) { return reinterpret_cast<double*>(base(w)); };
+    auto ok_of = [&](int w) { return reinterpret_cast<uint32_t*>(base(w) + Ep * 8); };
+    auto lg_of = [&](int w) { return reinterpret_cast<float*>(base(w) + Ep * 12); };
+    auto er_of = [&](int w) { return reinterpret_cast<float*>(base(w) + Ep * 16); };
+    auto cand_of = [&](int w) { return reinterpret_cast<uint16_t*>(base(w) + Ep * 20); };
+    if (threadIdx.x < FEW_SEL_WARPS) {
+        s_lo[threadIdx.x] = 0xffffffffu;   // lowest lower bound of a selected key
+        s_hi[threadIdx.x] = 0u;            // highest upper bound of an unselected one
+        n_cand[threadIdx.x] = 0;
     }
-    auto lane_best = [&](uint32_t& bu, int& be) {
-        bu = 0u;
-        be = 0x7fffffff;
-        for (int q = 0; q < NQ; ++q)
-            if ((have & ~sel) >> q & 1u) {
-                const uint32_t u = key_order(key[q * 32 + lane]);
-                if (u > bu) {
-                    bu = u;
-                    be = q * 32 + lane;
-                }
-            }
-    };
-    uint32_t bu;
-    int be;
-    lane_best(bu, be);
-    for (int j = 0; j < p.k; ++j) {
-        const uint32_t mu = __reduce_max_sync(0xffffffffu, bu);
-        const int me = __reduce_min_sync(0xffffffffu, bu == mu ? be : 0x7fffffff);
-        if (me == be) {
-            sel |= 1u << (be >> 5);
-            lane_best(bu, be);
+    for (int q = warp; q < n * NQ; q += FEW_WARPS) {
+        const int w = q / NQ, e = (q - w * NQ) * 32 + lane;
+        uint32_t o = 0u;
+        if (e < p.E) {
+            const float s = sum_parts(p.part + (int64_t)(t0 + w * step) * p.E + e, (int64_t)p.T * p.E, p.rt_parts);
+            const float w2 = sum_parts(p.wsq + e, p.E, p.rt_parts);
+            const float v = __fdividef(1.0f, 1.0f + __expf(-s)) + __ldg(p.b + e);
+            o = key_order(v);
+            lg_of(w)[e] = s;
+            // Half-width of the key: a quarter (the sigmoid's largest slope) of the logit's error
+            // bound, and the fp32 evaluation (fast sigmoid: under 1e-6; the sum's rounding).
+            er_of(w)[e] = 0.25f * p.rt_err * xn[w] * sqrtf(w2) + 2e-6f + 2.4e-7f * fabsf(v);
         }
+        ok_of(w)[e] = o;
     }
-    if (p.k < p.E) {
-        float lo = INFINITY, hi = -INFINITY;   // lowest selected, highest unselected key bounds
-        for (int q = 0; q < NQ; ++q) {
-            if (!(have >> q & 1u)) continue;
-            const float v = key[q * 32 + lane], r = er[q * 32 + lane];
-            if (sel >> q & 1u) lo = (v - r == v - r) ? fminf(lo, v - r) : -INFINITY;
-            else hi = (v + r == v + r) ? fmaxf(hi, v + r) : INFINITY;
+    __syncthreads();
+    for (int q = warp; q < n * NQ; q += FEW_WARPS) {
+        const int w = q / NQ, e0 = (q - w * NQ) * 32, e = e0 + lane;
+        const uint4* all = reinterpret_cast<const uint4*>(ok_of(w));
+        const uint32_t o = ok_of(w)[e];
+        int ahead = 0;
+#pragma unroll 2
+        for (int j = 0; j < e0 / 4; ++j) {
+            const uint4 u = all[j];
+            ahead += (u.x >= o) + (u.y >= o) + (u.z >= o) + (u.w >= o);
         }
-        lo = warp_min(lo);
-        hi = warp_max(hi);
-        if (!(lo > hi)) {
-            // Surely in: the lower bound is above every unselected upper bound; surely out: the
-            // upper bound is below every selected lower bound.  The rest get exact keys.
-            uint32_t cand = 0;
-            for (int q = 0; q < NQ; ++q) {
-                if (!(have >> q & 1u)) continue;
-                const float v = key[q * 32 + lane], r = er[q * 32 + lane];
-                if ((sel >> q & 1u) ? !(v - r > hi) : !(v + r < lo)) cand |= 1u << q;
-            }
-            for (int q = 0; q < NQ; ++q) {
-                uint32_t who = __ballot_sync(0xffffffffu, cand >> q & 1u);
-                while (who) {
-                    const int l = __ffs(who) - 1;
-                    who &= who - 1;
-                    const double s = few_exact_logit(p, t, q * 32 + l);
-                    if (lane == l) kd[q * 32 + l] = 1.0 / (1.0 + exp(-s)) + (double)__ldg(p.b + q * 32 + l);
-                }
-            }
-            sel &= ~cand;
-            int need = p.k - (int)__reduce_add_sync(0xffffffffu, (unsigned)__popc(sel));
-            for (; need > 0; --need) {
-                double bv = 0.0;
-                int b = 0x7fffffff;
-                // better: a number before NaN, the larger key, the lower id
-                auto better = [](double v, int e, double w, int f) {
-                    if (f == 0x7fffffff) return e != 0x7fffffff;
-                    if (e == 0x7fffffff) return false;
-                    if (isnan(v) != isnan(w)) return (bool)isnan(w);
-                    return v > w || (!(w > v) && e < f);
-                };
-                for (int q = 0; q < NQ; ++q)
-                    if ((cand & ~sel) >> q & 1u) {
-                        const int e = q * 32 + lane;
-                        if (better(kd[e], e, bv, b)) {
-                            bv = kd[e];
-                            b = e;
-                        }
-                    }
-                const int mine = b;
-                for (int o = 16; o; o >>= 1) {
-                    const double ov = __shfl_xor_sync(0xffffffffu, bv, o);
-                    const int oe = __shfl_xor_sync(0xffffffffu, b, o);
-                    if (better(ov, oe, bv, b)) {
-                        bv = ov;
-                        b = oe;
-                    }
-                }
-                if (mine == b && b != 0x7fffffff) sel |= 1u << (b >> 5);
-            }
+#pragma unroll 2
+        for (int j = e0 / 4; j < e0 / 4 + 8; ++j) {
+            const uint4 u = all[j];
+            ahead += (u.x > o || (u.x == o && 4 * j < e)) + (u.y > o || (u.y == o && 4 * j + 1 < e)) +
+                     (u.z > o || (u.z == o && 4 * j + 2 < e)) + (u.w > o || (u.w == o && 4 * j + 3 < e));
+        }
+#pragma unroll 2
+        for (int j = e0 / 4 + 8; j < Ep / 4; ++j) {
+            const uint4 u = all[j];
+            ahead += (u.x > o) + (u.y > o) + (u.z > o) + (u.w > o);
+        }
+        const bool sel = e < p.E && ahead < p.k;
+        const uint32_t m = __ballot_sync(0xffffffffu, sel);
+        // bounds (a NaN lower bound counts as lowest, a NaN upper bound as highest)
+        uint32_t lo = 0xffffffffu, hi = 0u;
+        if (e < p.E) {
+            const float v = key_value(o), r = er_of(w)[e];
+            if (sel) lo = (v - r == v - r) ? key_order(v - r) : 0u;
+            else hi = (v + r == v + r) ? key_order(v + r) : 0xffffffffu;
+        }
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        if (lane == 0) {
+            s_sel[w][e0 / 32] = m;
+            atomicMin(&s_lo[w], lo);
+            atomicMax(&s_hi[w], hi);
         }
     }
-    float mys = 0.f;
-    for (int q = 0; q < NQ; ++q)
-        if (sel >> q & 1u) mys += 1.0f / (1.0f + expf(-lg[q * 32 + lane]));
-    const float sum = warp_sum(mys);
-    int base = 0;
-    for (int q = 0; q < NQ; ++q) {
-        const bool s = sel >> q & 1u;
-        const uint32_t m = __ballot_sync(0xffffffffu, s);
-        if (s) {
-            const int j = base + __popc(m & ((1u << lane) - 1u));
-            out_idx[j] = q * 32 + lane;
-            out_gate[j] = 1.0f / (1.0f + expf(-lg[q * 32 + lane])) / sum;
+    __syncthreads();
+    // Where the lowest selected key may not be above the highest unselected one: an expert whose
+    // lower bound is above every unselected upper bound is in, one whose upper bound is below
+    // every selected lower bound is out, the rest get exact keys.
+    for (int q = warp; q < n * NQ; q += FEW_WARPS) {
+        const int w = q / NQ, e0 = (q - w * NQ) * 32, e = e0 + lane;
+        if (s_lo[w] > s_hi[w] || e >= p.E) continue;
+        const float v = key_value(ok_of(w)[e]), r = er_of(w)[e];
+        const bool sel = s_sel[w][e0 / 32] >> lane & 1u;
+        const uint32_t lo = (v - r == v - r) ? key_order(v - r) : 0u;
+        const uint32_t hi = (v + r == v + r) ? key_order(v + r) : 0xffffffffu;
+        if (sel ? lo <= s_hi[w] : hi >= s_lo[w]) cand_of(w)[atomicAdd(&n_cand[w], 1)] = (uint16_t)e;
+    }
+    __syncthreads();
+    for (int w = 0; w < n; ++w) {
+        const int nc = n_cand[w];
+        if (nc == 0) continue;
+        // Exact logits, by all threads, four experts at a time: products of bf16 and fp32 are
+        // exact in 64 bits, summed in a fixed order.
+        const __nv_bfloat16* x = p.x + (int64_t)(t0 + w * step) * p.d;
+        for (int c0 = 0; c0 < nc; c0 += 4) {
+            double s[4] = {};
+            const float* col[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) col[j] = p.W_r + cand_of(w)[min(c0 + j, nc - 1)];
+#pragma unroll 4
+            for (int i = threadIdx.x; i < p.d; i += FEW_THREADS) {
+                const double xv = (double)__bfloat162float(x[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[j] = fma(xv, (double)__ldg(col[j] + (int64_t)i * p.E), s[j]);
+            }
+            for (int o = 16; o; o >>= 1)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
+            if (lane < 4) part64[warp][lane] = lane == 0 ? s[0] : lane == 1 ? s[1] : lane == 2 ? s[2] : s[3];
+            __syncthreads();
+            if (threadIdx.x < 4 && c0 + (int)threadIdx.x < nc) {
+                const int e = cand_of(w)[c0 + threadIdx.x];
+                double t = 0.0;
+                for (int j = 0; j < FEW_WARPS; ++j) t += part64[j][threadIdx.x];
+                kd_of(w)[e] = 1.0 / (1.0 + exp(-t)) + (double)__ldg(p.b + e);
+                atomicAnd(&s_sel[w][e / 32], ~(1u << (e & 31)));
+            }
+            __syncthreads();
         }
-        base += __popc(m);
+        // The places that the sure ones leave go to the largest exact keys (a number before NaN,
+        // the lower id of equals).
+        int need = p.k;
+        for (int q = 0; q < NQ; ++q) need -= __popc(s_sel[w][q]);
+        __syncthreads();
+        for (int c = threadIdx.x; c < nc; c += FEW_THREADS) {
+            const int e = cand_of(w)[c];
+            const double v = kd_of(w)[e];
+            int ahead = 0;
+            for (int j = 0; j < nc; ++j) {
+                const int f = cand_of(w)[j];
+                const double u = kd_of(w)[f];
+                ahead += isnan(v) != isnan(u) ? (isnan(v) ? 1 : 0) : (u > v || (!(v > u) && f < e)) ? 1 : 0;
+            }
+            if (ahead < need) atomicOr(&s_sel[w][e / 32], 1u << (e & 31));
+        }
+        __syncthreads();
+    }
+    // Places in ascending order of ids; the gates' sum in that order.
+    for (int q = warp; q < n * NQ; q += FEW_WARPS) {
+        const int w = q / NQ, qe = q - w * NQ;
+        const uint32_t m = s_sel[w][qe];
+        if (m == 0u) continue;
+        int j = __popc(m & ((1u << lane) - 1u));
+        for (int i = 0; i < qe; ++i) j += __popc(s_sel[w][i]);
+        if (m >> lane & 1u) {
+            out_idx[(t0 + w * step) * p.k + j] = qe * 32 + lane;
+            s_sig[w][j] = 1.0f / (1.0f + expf(-lg_of(w)[qe * 32 + lane]));
+        }
+    }
+    __syncthreads();
+    for (int q = threadIdx.x; q < n * p.k; q += FEW_THREADS) {
+        const int w = q / p.k, j = q - w * p.k;
+        float sum = 0.f;
+        for (int i = 0; i < p.k; ++i) sum += s_sig[w][i];
+        out_gate[(t0 + w * step) * p.k + j] = s_sig[w][j] / sum;
     }
 }
 
@@ -334,27 +420,27 @@ __device__ void few_select(const FewArgs& p, int t, uint8_t* buf, int32_t* out_i
 
 // Built by every CTA from the selection; kept in shared memory.
 struct FewPlan {
-    int n_act;             // experts with tokens
-    int P, P2, P2s;        // splits of K: up items, routed and shared down items
-    int n_up, n_items;     // items: up, then down
-    int n_shared_down;
+    int n_act;              // experts with tokens
+    int tw, nt, nt_s;       // up items: columns (64 or 128), tiles of h and of h_s
+    int tw2, ntd, P2, P2s;  // down items: columns, tiles of d, parts of K (routed, shared)
+    int n_up, n_shared_down, n_items;   // items: up, then down (shared first in each)
 };
 
 struct FewItem {
-    int up, shared, i, e;  // i: active expert index
-    int n0, kb0, kb1;
-    int tile, part;        // up: index of (expert, columns) and K part; down: K part
-    int cnt, row0;         // tokens of the expert, first row
+    int up, shared, i, e;   // i: active expert index
+    int n0, tw, kb0, kb1;
+    int part;               // down: K part
+    int cnt, row0;          // tokens of the expert, first row
 };
 
-struct FewLists {          // shared memory
+struct FewLists {           // shared memory
     FewPlan* plan;
-    uint16_t* act;         // [na] expert of active index i
-    uint16_t* off;         // [na] its first row
-    uint8_t* cnt;          // [na] its tokens
-    uint8_t* row_tok;      // [T k] token of a row
-    uint16_t* row_of;      // [T k] row of slot t k + j
-    float* gate;           // [T k]
+    uint16_t* act;          // [na] expert of active index i
+    uint16_t* off;          // [na] its first row
+    uint8_t* cnt;           // [na] its tokens
+    uint8_t* row_tok;       // [T k] token of a row
+    uint16_t* row_of;       // [T k] row of slot t k + j
+    float* gate;            // [T k]
 };
 
 __device__ __forceinline__ FewItem few_item(const FewArgs& p, const FewLists& L, int id) {
@@ -362,24 +448,23 @@ __device__ __forceinline__ FewItem few_item(const FewArgs& p, const FewLists& L,
     FewItem it;
     it.up = id < pl.n_up;
     if (it.up) {
-        it.tile = id / pl.P;
-        it.part = id - it.tile * pl.P;
-        it.shared = it.tile < p.nt_s;
-        const int q = it.tile - p.nt_s;
-        it.i = it.shared ? 0 : q / p.nt;
-        it.n0 = (it.shared ? it.tile : q - it.i * p.nt) * 128;
-        it.kb0 = it.part * p.nkb_d / pl.P;
-        it.kb1 = (it.part + 1) * p.nkb_d / pl.P;
+        it.shared = id < pl.nt_s;
+        const int q = id - pl.nt_s;
+        it.i = it.shared ? 0 : q / pl.nt;
+        it.tw = pl.tw;
+        it.n0 = (it.shared ? id : q - it.i * pl.nt) * pl.tw;
+        it.part = 0;
+        it.kb0 = 0;
+        it.kb1 = p.nkb_d;
     } else {
         int q = id - pl.n_up;
         it.shared = q < pl.n_shared_down;
         if (!it.shared) q -= pl.n_shared_down;
-        const int P = it.shared ? pl.P2s : pl.P2, nkb = it.shared ? p.nkb_hs : p.nkb_h;
-        it.part = q % P;
-        q /= P;
-        it.i = it.shared ? 0 : q / p.ntd;
-        it.n0 = (it.shared ? q : q - it.i * p.ntd) * 128;
-        it.tile = 0;
+        const int P = it.shared ? pl.P2s : pl.P2, nkb = it.shared ? p.nkb_hs : p.nkb_h, r = q / P;
+        it.part = q - r * P;
+        it.i = it.shared ? 0 : r / pl.ntd;
+        it.tw = pl.tw2;
+        it.n0 = (it.shared ? r : r - it.i * pl.ntd) * pl.tw2;
         it.kb0 = it.part * nkb / P;
         it.kb1 = (it.part + 1) * nkb / P;
     }
@@ -389,19 +474,19 @@ __device__ __forceinline__ FewItem few_item(const FewArgs& p, const FewLists& L,
     return it;
 }
 
-// Splits of K: the P for which ceil(items P / CTAs) rounds of ceil(nkb / P) blocks (and one
-// block's worth of start and finish) are shortest.
-__device__ int few_choose_split(int items, int nkb, int ctas, int most, int most_items) {
-    int best = 1, cost = 0x7fffffff;
-    for (int P = 1; P <= most && P <= nkb; ++P) {
-        if (P > 1 && items * P > most_items) break;
-        const int c = (items * P + ctas - 1) / ctas * ((nkb + P - 1) / P + 1);
-        if (c < cost) {
-            cost = c;
-            best = P;
-        }
-    }
-    return best;
+// Estimated time (ns) of `items` items of `blocks` K blocks of `kb` bytes: an SM takes a block
+// in kb / 70 GB/s at least, and c CTAs at work share 6600 GB/s (measured with tiles streamed by 8
+// to 152 SMs); the last, partial round of items runs at its own c; 400 ns an item besides.
+__device__ __forceinline__ float few_time(int items, int blocks, int kb, int ctas) {
+    const int rounds = items / ctas, rest = items - rounds * ctas;
+    const float one = (float)kb / 70.0f, all = (float)kb / 6600.0f;
+    return rounds * (blocks * fmaxf(one, all * ctas) + 400.0f) +
+           (rest > 0 ? blocks * fmaxf(one, all * rest) + 400.0f : 0.0f);
+}
+// The lane with the smallest time (the lowest of equals).
+__device__ __forceinline__ int few_fastest(float t) {
+    const uint32_t c = (uint32_t)fminf(t, 1.0e8f) * 32u + (threadIdx.x & 31);
+    return (int)(__reduce_min_sync(0xffffffffu, c) & 31u);
 }
 
 // Expert lists and the plan from the selection (idx, gate of all slots).  tmp: 10 bytes per
@@ -410,59 +495,107 @@ __device__ int few_choose_split(int items, int nkb, int ctas, int most, int most
 template <bool SHARED_SEL>
 __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx, const float* gate,
                          uint8_t* tmp) {
+    __shared__ int n_in[32], rows_in[32];   // of each 32 experts: how many have tokens, their rows
     unsigned long long* mask = reinterpret_cast<unsigned long long*>(tmp);   // tokens of each expert
     uint16_t* off = reinterpret_cast<uint16_t*>(mask + p.E);                 // first row of each expert
     auto load = [](const auto* q) { return SHARED_SEL ? *q : __ldcg(q); };
-    const int n = p.T * p.k;
+    const int n = p.T * p.k, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int e = threadIdx.x; e < p.E; e += FEW_THREADS) mask[e] = 0ull;
+    if (threadIdx.x < 32) n_in[threadIdx.x] = rows_in[threadIdx.x] = 0;
     __syncthreads();
-    for (int s = threadIdx.x; s < n; s += FEW_THREADS) atomicOr(&mask[load(idx + s)], 1ull << (s / p.k));
-    __syncthreads();
-    if (threadIdx.x < 32) {
-        const int lane = threadIdx.x;
-        int na = 0, rows = 0;
-        for (int e0 = 0; e0 < p.E; e0 += 32) {
-            const int e = e0 + lane;
-            const int c = e < p.E ? __popcll(mask[e]) : 0;
-            int sum = c;   // inclusive prefix over the lanes
+    constexpr int PER = (MOEVIE_FEW_MAX_TOKENS * 32 + FEW_THREADS - 1) / FEW_THREADS;   // slots of a thread
+    int my_e[PER];
+    float my_g[PER];
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, sum, o);
-                if (lane >= o) sum += v;
-            }
-            const uint32_t m = __ballot_sync(0xffffffffu, c > 0);
-            if (c > 0) {
-                const int i = na + __popc(m & ((1u << lane) - 1u));
-                L.act[i] = (uint16_t)e;
-                L.off[i] = (uint16_t)(rows + sum - c);
-                L.cnt[i] = (uint8_t)c;
-                off[e] = (uint16_t)(rows + sum - c);
-            }
-            na += __popc(m);
-            rows += __shfl_sync(0xffffffffu, sum, 31);
-        }
+    for (int i = 0; i < PER; ++i) {
+        const int s = threadIdx.x + i * FEW_THREADS;
+        if (s >= n) break;
+        my_e[i] = load(idx + s);
+        my_g[i] = load(gate + s);
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int s = threadIdx.x + i * FEW_THREADS;
+        if (s >= n) break;
+        atomicOr(&mask[my_e[i]], 1ull << (s / p.k));
+    }
+    __syncthreads();
+    for (int q = warp; q * 32 < p.E; q += FEW_WARPS) {
+        const int e = q * 32 + lane, c = e < p.E ? __popcll(mask[e]) : 0;
+        const uint32_t m = __ballot_sync(0xffffffffu, c > 0);
+        const int rows = (int)__reduce_add_sync(0xffffffffu, (unsigned)c);
         if (lane == 0) {
-            FewPlan& pl = *L.plan;
-            const int ctas = (int)gridDim.x;
-            pl.n_act = na;
-            const int tiles = na * p.nt + p.nt_s;
-            pl.P = few_choose_split(tiles, p.nkb_d, ctas, FEW_MAX_P, FEW_MAX_PART);
-            pl.P2 = few_choose_split(na * p.ntd + (p.hs > 0 ? p.ntd * ((p.nkb_hs + p.nkb_h - 1) / p.nkb_h) : 0),
-                                     p.nkb_h, ctas, FEW_MAX_P2, 0x7fffffff);
-            pl.P2s = 1;   // shared down items about as long as the routed ones
-            if (p.hs > 0) pl.P2s = min(min(FEW_MAX_P2S, p.nkb_hs), max(1, (p.nkb_hs * pl.P2 + p.nkb_h / 2) / p.nkb_h));
-            pl.n_up = tiles * pl.P;
-            pl.n_shared_down = p.hs > 0 ? p.ntd * pl.P2s : 0;
-            pl.n_items = pl.n_up + pl.n_shared_down + na * p.ntd * pl.P2;
+            n_in[q] = __popc(m);
+            rows_in[q] = rows;
         }
     }
     __syncthreads();
-    for (int s = threadIdx.x; s < n; s += FEW_THREADS) {
-        const int t = s / p.k, e = load(idx + s);
+    // inclusive prefixes over the groups of 32, in every warp
+    int na = n_in[lane], nrow = rows_in[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, na, o), v = __shfl_up_sync(0xffffffffu, nrow, o);
+        if (lane >= o) {
+            na += u;
+            nrow += v;
+        }
+    }
+    const int n_act = __shfl_sync(0xffffffffu, na, 31);
+    for (int q = warp; q * 32 < p.E; q += FEW_WARPS) {
+        const int e = q * 32 + lane, c = e < p.E ? __popcll(mask[e]) : 0;
+        int sum = c;   // inclusive prefix over the lanes
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        const uint32_t m = __ballot_sync(0xffffffffu, c > 0);
+        const int i = __shfl_sync(0xffffffffu, na, q) - n_in[q] + __popc(m & ((1u << lane) - 1u));
+        const int row = __shfl_sync(0xffffffffu, nrow, q) - rows_in[q] + sum - c;
+        if (c > 0) {
+            L.act[i] = (uint16_t)e;
+            L.off[i] = (uint16_t)row;
+            L.cnt[i] = (uint8_t)c;
+            off[e] = (uint16_t)row;
+        }
+    }
+    if (warp == FEW_WARPS - 1) {
+        // 64-column items where 128-column ones are too few to keep all SMs streaming; down items
+        // may also split K (their partial rows are joined anyway).
+        const int ctas = (int)gridDim.x, bn = up16((n + n_act - 1) / n_act) * 128, mats = p.W3 ? 2 : 1;
+        const int tw_l = 128 >> (lane & 1), tiles_l = n_act * ((p.h + tw_l - 1) / tw_l) + (p.hs + tw_l - 1) / tw_l;
+        const int up = few_fastest(lane < 2 ? few_time(tiles_l, p.nkb_d, mats * tw_l * 128 + bn, ctas) : 3.0e38f);
+        const int P_l = (lane >> 1) + 1, ntd_l = (p.d + tw_l - 1) / tw_l;
+        const int items_l = ntd_l * P_l * (n_act + (p.nkb_hs + p.nkb_h - 1) / p.nkb_h);
+        const int dn = few_fastest(P_l <= FEW_MAX_P2 && P_l <= p.nkb_h
+                                       ? few_time(items_l, (p.nkb_h + P_l - 1) / P_l, tw_l * 128 + 2 * bn, ctas)
+                                       : 3.0e38f);
+        if (lane == 0) {
+            FewPlan& pl = *L.plan;
+            pl.n_act = n_act;
+            pl.tw = 128 >> up;
+            pl.nt = (p.h + pl.tw - 1) / pl.tw;
+            pl.nt_s = (p.hs + pl.tw - 1) / pl.tw;
+            pl.tw2 = 128 >> (dn & 1);
+            pl.P2 = (dn >> 1) + 1;
+            pl.ntd = (p.d + pl.tw2 - 1) / pl.tw2;
+            // shared down items about as long as the routed ones
+            pl.P2s = p.hs > 0 ? min(min(FEW_MAX_P2S, p.nkb_hs), max(1, (p.nkb_hs * pl.P2 + p.nkb_h / 2) / p.nkb_h)) : 1;
+            pl.n_up = n_act * pl.nt + pl.nt_s;
+            pl.n_shared_down = p.hs > 0 ? pl.ntd * pl.P2s : 0;
+            pl.n_items = pl.n_up + pl.n_shared_down + n_act * pl.ntd * pl.P2;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int s = threadIdx.x + i * FEW_THREADS;
+        if (s >= n) break;
+        const int t = s / p.k, e = my_e[i];
         const int row = off[e] + __popcll(mask[e] & ((1ull << t) - 1ull));
         L.row_tok[row] = (uint8_t)t;
         L.row_of[s] = (uint16_t)row;
-        L.gate[s] = load(gate + s);
+        L.gate[s] = my_g[i];
     }
 }
 
@@ -470,15 +603,13 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
 
 struct FewSmem {
     uint32_t ring, full, empty, tfull, tempty, drain;
-    int stages, stage_bytes, b_off, lo_off;   // within a stage: B (hi) and B lo
+    int stages, stage_bytes, b_off;   // b_off: the N operand within a stage
 };
 
 __device__ __forceinline__ void few_abort(volatile int* flag, DevStatus* st, int site, int a) {
     *flag = 1;
     report(st, MOEVIE_ERR_TIMEOUT, site, (int)blockIdx.x, a);
 }
-
-__device__ __forceinline__ int up16(int v) { return (v + 15) & ~15; }
 
 // Weight tiles of every item; never waits for anything but a free stage.
 __device__ void few_load_w(const FewArgs& p, const FewSmem& sm, const FewLists& L, volatile int* abort_flag) {
@@ -496,14 +627,11 @@ __device__ void few_load_w(const FewArgs& p, const FewSmem& sm, const FewLists& 
                 return;
             }
             const uint32_t bar = sm.full + 8 * s, dst = sm.ring + s * sm.stage_bytes;
-            mbar_arrive_expect_tx(bar, two ? 2 * FEW_TILE_BYTES : FEW_TILE_BYTES);
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                tma_load_3d(dst + j * (FEW_TILE_BYTES / 2), a, bar, it.n0 + 64 * j, kb * 64, it.e);
-            if (two)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    tma_load_3d(dst + FEW_TILE_BYTES + j * (FEW_TILE_BYTES / 2), a3, bar, it.n0 + 64 * j, kb * 64, it.e);
+            mbar_arrive_expect_tx(bar, (two ? 2 : 1) * it.tw * 128);
+            for (int j = 0; j < it.tw; j += 64) {
+                tma_load_3d(dst + j * 128, a, bar, it.n0 + j, kb * 64, it.e);
+                if (two) tma_load_3d(dst + FEW_TILE_BYTES + j * 128, a3, bar, it.n0 + j, kb * 64, it.e);
+            }
             if (++s == sm.stages) {
                 s = 0;
                 ph ^= 1u;
@@ -512,50 +640,54 @@ __device__ void few_load_w(const FewArgs& p, const FewSmem& sm, const FewLists& 
     }
 }
 
-// The N operand: token rows (up) or the two pieces of the hidden rows (down), after the
-// expert's up items are done.  Rows past the expert's last token repeat its first (up) or hold
-// whatever follows (down): their columns of D are not read.
+// The N operand, by a whole warp (a lane per 4 gathered rows): token rows (up) or the two pieces of
+// the hidden rows (down: hi, then lo N rows further), after the expert's up items are done.
+// Rows past the expert's last token repeat its first (up) or hold whatever follows (down):
+// their columns of D are not read.
 __device__ void few_load_b(const FewArgs& p, const FewSmem& sm, const FewLists& L, volatile int* abort_flag) {
-    const int n_items = L.plan->n_items;
+    const int n_items = L.plan->n_items, lane = threadIdx.x & 31;
     int s = 0;
     uint32_t ph = 0;
     for (int id = blockIdx.x; id < n_items; id += gridDim.x) {
         const FewItem it = few_item(p, L, id);
         const int N = up16(it.cnt);
-        if (!it.up) {
-            const int32_t* c = p.done_up + (it.shared ? p.na_max : it.i);
-            const int want = it.shared ? p.nt_s : p.nt;
-            const uint64_t t0 = globaltimer_ns();
-            for (uint32_t i = 1; ld_acquire(c) < want; ++i)
-                if ((i & 63u) == 0u && (*abort_flag || globaltimer_ns() - t0 > p.limit_ns)) {
-                    few_abort(abort_flag, p.status, SITE_FEW_WAIT_UP, id);
-                    return;
-                }
+        int tok[4] = {};
+        if (it.up) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = 4 * lane + i < it.cnt ? 4 * lane + i : 0;
+                tok[i] = it.shared ? j : L.row_tok[it.row0 + j];
+            }
+        } else {
+            int ok = 1;
+            if (lane == 0) {
+                const int32_t* c = p.done_up + (it.shared ? p.na_max : it.i);
+                const int want = it.shared ? L.plan->nt_s : L.plan->nt;
+                const uint64_t t0 = globaltimer_ns();
+                for (uint32_t i = 1; ld_acquire(c) < want; ++i)
+                    if ((i & 63u) == 0u && (*abort_flag || globaltimer_ns() - t0 > p.limit_ns)) {
+                        few_abort(abort_flag, p.status, SITE_FEW_WAIT_UP, id);
+                        ok = 0;
+                        break;
+                    }
+            }
+            if (!__shfl_sync(0xffffffffu, ok, 0)) return;
             fence_proxy_async_all();   // the hidden rows were written by ordinary stores
         }
         for (int kb = it.kb0; kb < it.kb1; ++kb) {
-            if (!mbar_wait(sm.empty + 8 * s, ph ^ 1u, p.limit_ns, abort_flag)) {
-                few_abort(abort_flag, p.status, SITE_FEW_WAIT_EMPTY, -id);
-                return;
-            }
+            int ok = 1;
             const uint32_t bar = sm.full + 8 * s, dst = sm.ring + s * sm.stage_bytes + sm.b_off;
-            mbar_arrive_expect_tx(bar, (it.up ? 1 : 2) * N * 128);
+            if (lane == 0) {
+                ok = mbar_wait(sm.empty + 8 * s, ph ^ 1u, p.limit_ns, abort_flag);
+                if (ok) mbar_arrive_expect_tx(bar, (it.up ? 1 : 2) * N * 128);
+                else few_abort(abort_flag, p.status, SITE_FEW_WAIT_EMPTY, -id);
+            }
+            if (!__shfl_sync(0xffffffffu, ok, 0)) return;
             if (it.up) {
-                for (int r = 0; r < N; r += 4) {
-                    int tok[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int j = r + i < it.cnt ? r + i : 0;
-                        tok[i] = it.shared ? j : L.row_tok[it.row0 + j];
-                    }
-                    tma_gather4(dst + r * 128, &p.tX, bar, kb * 64, tok[0], tok[1], tok[2], tok[3]);
-                }
-            } else {
-                const CUtensorMap* h = it.shared ? &p.tHs : &p.tH;
-                for (int r = 0; r < N; r += 16) {
-                    tma_load_3d(dst + r * 128, h, bar, kb * 64, it.row0 + r, 0);
-                    tma_load_3d(dst + sm.lo_off + r * 128, h, bar, kb * 64, it.row0 + r, 1);
-                }
+                if (4 * lane < N) tma_gather4(dst + lane * 512, &p.tX, bar, kb * 64, tok[0], tok[1], tok[2], tok[3]);
+            } else if (8 * lane < N) {   // lanes 2 r, 2 r + 1: rows 16 r of hi and of lo
+                tma_load_3d(dst + (lane & 1) * N * 128 + (lane >> 1) * 2048, it.shared ? &p.tHs : &p.tH, bar, kb * 64,
+                            it.row0 + (lane >> 1) * 16, lane & 1);
             }
             if (++s == sm.stages) {
                 s = 0;
@@ -577,7 +709,8 @@ __device__ void few_mma(const FewArgs& p, const FewSmem& sm, const FewLists& L, 
     bool issued = false;
     for (int id = blockIdx.x; id < n_items; id += gridDim.x, ++n) {
         const FewItem it = few_item(p, L, id);
-        const uint32_t idesc = idesc_bf16_f32(128, up16(it.cnt), true, false);
+        // down: hi and lo pieces of the tokens side by side, added by the epilogue
+        const uint32_t idesc = idesc_bf16_f32(128, (it.up ? 1 : 2) * up16(it.cnt), true, false);
         const int acc = n & 1;
         const bool two = it.up && p.W3;
         if (!mbar_wait(sm.tempty + 8 * acc, ((uint32_t)(n >> 1) & 1u) ^ 1u, p.limit_ns, abort_flag)) {
@@ -601,8 +734,6 @@ __device__ void few_mma(const FewArgs& p, const FewSmem& sm, const FewLists& L, 
                 tc_mma_bf16(d, wd + q * (2048 >> 4), bd + q * (32 >> 4), idesc, add);
                 if (two)
                     tc_mma_bf16(d + p.nb, wd + (FEW_TILE_BYTES >> 4) + q * (2048 >> 4), bd + q * (32 >> 4), idesc, add);
-                else if (!it.up)
-                    tc_mma_bf16(d, wd + q * (2048 >> 4), bd + (uint64_t)(sm.lo_off >> 4) + q * (32 >> 4), idesc, 1u);
             }
             issued = true;
             tc_commit(sm.empty + 8 * s);
@@ -621,163 +752,140 @@ __device__ void few_mma(const FewArgs& p, const FewSmem& sm, const FewLists& L, 
     }
 }
 
-// hi and lo pieces of one hidden activation.
-__device__ __forceinline__ void store_hidden(const FewArgs& p, const FewItem& it, int j, int col, float a) {
-    const int ld = it.shared ? p.ldhs : p.ldh;
-    __nv_bfloat16* H = it.shared ? p.Hs : p.H;
-    const int64_t rows = it.shared ? p.T : (int64_t)p.T * p.k;
-    const int64_t at = (int64_t)(it.row0 + j) * ld + col;
-    const __nv_bfloat16 hi = __float2bfloat16_rn(a);
-    H[at] = hi;
-    H[rows * ld + at] = __float2bfloat16_rn(a - __bfloat162float(hi));
-}
-
-// Eight warps: warp w reads TMEM lanes 32 (w % 4) .. (its columns of W) and the token groups
-// of 8 w / 4, w / 4 + 2, ...  One thread waits and decides for all, so that the warps take
-// the same way through the barriers below.
+// Two groups of four warps take the CTA's items in turn (accumulator = group), so that the trips
+// to L2 of one item's bookkeeping overlap the next item's.  Warp w of a group reads TMEM lanes
+// 32 w .. (its columns of W) for all tokens.  One thread waits and decides for its group, so
+// that the warps take the same way through its barriers.
 __device__ void few_epilogue(const FewArgs& p, const FewSmem& sm, const FewLists& L, uint32_t tmem,
-                             volatile int* abort_flag, volatile int* flags) {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int quad = warp & 3, half = warp >> 2, c = quad * 32 + lane;
-    const int n_items = L.plan->n_items, P = L.plan->P;
-    const int mats = p.W3 ? 2 : 1;
+                             volatile int* abort_flag, volatile int* flags_all) {
+    const int group = threadIdx.x >> 7, tid = threadIdx.x & 127, warp = tid >> 5, lane = tid & 31;
+    const FewPlan pl = *L.plan;
+    volatile int* flags = flags_all + group * 65;
+    const bool two = p.W3 != nullptr;
+    const int64_t slots = (int64_t)p.T * p.k;
+    const uint32_t tb = tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)(group * p.acc_cols);
     int n = 0;
-    for (int id = blockIdx.x; id < n_items; id += gridDim.x, ++n) {
+    for (int id = blockIdx.x + group * gridDim.x; id < pl.n_items; id += 2 * gridDim.x, ++n) {
         const FewItem it = few_item(p, L, id);
-        const int acc = n & 1;
         if (tid == 0) {
-            const bool ok = mbar_wait(sm.tfull + 8 * acc, (uint32_t)(n >> 1) & 1u, p.limit_ns, abort_flag);
+            const bool ok = mbar_wait(sm.tfull + 8 * group, (uint32_t)n & 1u, p.limit_ns, abort_flag);
             if (!ok) few_abort(abort_flag, p.status, SITE_FEW_WAIT_TFULL, id);
             flags[64] = ok;
         }
-        epi_sync();
+        epi_sync(group);
         if (!flags[64]) return;
         tc_fence_after();
-        const uint32_t tb = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * p.acc_cols);
-        const int groups = (it.cnt + 7) / 8;
+        const int c = tid, N = up16(it.cnt);
+        const bool active = 32 * warp < it.tw;
         if (it.up) {
-            const int h = it.shared ? p.hs : p.h, col = it.n0 + c;
-            float* part = P > 1 ? p.up_part + (int64_t)(it.tile * P + it.part) * mats * p.nb * 128 : nullptr;
-            for (int g = half; g < groups; g += 2) {
+            const int col = it.n0 + c, h = it.shared ? p.hs : p.h, ld = it.shared ? p.ldhs : p.ldh;
+            const bool ok = c < it.tw && col < h;
+            __nv_bfloat16* hi = (it.shared ? p.Hs : p.H) + (int64_t)it.row0 * ld + col;
+            __nv_bfloat16* lo = hi + (it.shared ? (int64_t)p.T : slots) * ld;
+            for (int j0 = 0; j0 < it.cnt && active; j0 += 8) {
                 uint32_t u[8], v[8];
-                tmem_ld_32x32b_x8(tb + 8 * g, u);
-                if (mats == 2) tmem_ld_32x32b_x8(tb + p.nb + 8 * g, v);
+                tmem_ld_32x32b_x8(tb + j0, u);
+                if (two) tmem_ld_32x32b_x8(tb + p.nb + j0, v);
                 tmem_wait_ld();
+                float f[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int j = 8 * g + i;
-                    if (j >= it.cnt) break;
-                    if (part) {
-                        part[j * 128 + c] = __uint_as_float(u[i]);
-                        if (mats == 2) part[(p.nb + j) * 128 + c] = __uint_as_float(v[i]);
-                    } else if (col < h) {
-                        const float f = __uint_as_float(u[i]);
-                        store_hidden(p, it, j, col, mats == 2 ? act_silu(f) * __uint_as_float(v[i]) : act_gelu(f));
-                    }
+                for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(u[i]);
+                if (two) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        f[i] = __fdividef(f[i], 1.0f + __expf(-f[i])) * __uint_as_float(v[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) gelu_erf2(f[i], f[i + 1]);
                 }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (ok && j0 + i < it.cnt) {   // two bf16 pieces: 16 significant bits
+                        const __nv_bfloat16 a = __float2bfloat16_rn(f[i]);
+                        hi[(int64_t)(j0 + i) * ld] = a;
+                        lo[(int64_t)(j0 + i) * ld] = __float2bfloat16_rn(f[i] - __bfloat162float(a));
+                    }
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(sm.tempty + 8 * acc);
-            fence_proxy_async_all();
-            __threadfence();
-            epi_sync();
-            int32_t* done = p.done_up + (it.shared ? p.na_max : it.i);
-            if (!part) {
-                if (tid == 0) atomicAdd(done, 1);
-                continue;
-            }
-            if (tid == 0) flags[65] = atomicAdd(p.up_cnt + it.tile, 1) == P - 1;
-            epi_sync();
-            if (!flags[65]) continue;
-            __threadfence();   // the other parts' stores, before they are read
-            const float* all = p.up_part + (int64_t)it.tile * P * mats * p.nb * 128;
-            const int64_t step = (int64_t)mats * p.nb * 128;
-            for (int q = tid; q < it.cnt * 128; q += FEW_EPI_WARPS * 32) {
-                const int j = q >> 7, cc = q & 127;
-                if (it.n0 + cc >= h) continue;
-                float u = 0.f, v = 0.f;
-                for (int pp = 0; pp < P; ++pp) {
-                    u += __ldcg(all + pp * step + j * 128 + cc);
-                    if (mats == 2) v += __ldcg(all + pp * step + (p.nb + j) * 128 + cc);
-                }
-                store_hidden(p, it, j, it.n0 + cc, mats == 2 ? act_silu(u) * v : act_gelu(u));
-            }
-            fence_proxy_async_all();
-            __threadfence();
-            epi_sync();
-            if (tid == 0) atomicAdd(done, 1);
+            if (lane == 0) mbar_arrive(sm.tempty + 8 * group);
+            fence_proxy_async_all();   // the rows will be read by TMA
+            epi_sync(group);
+            if (tid == 0) add_release(p.done_up + (it.shared ? p.na_max : it.i), 1);
         } else {
-            const int64_t slots = (int64_t)p.T * p.k;
             // rows of the partial outputs: [P2][T k] routed, then [P2s][T] shared
-            float* yp = it.shared ? p.y_part + (int64_t)L.plan->P2 * slots * p.d + (int64_t)it.part * p.T * p.d
-                                  : p.y_part + ((int64_t)it.part * slots + it.row0) * p.d;
             const int col = it.n0 + c;
-            for (int g = half; g < groups; g += 2) {
-                uint32_t u[8];
-                tmem_ld_32x32b_x8(tb + 8 * g, u);
+            const bool ok = c < it.tw && col < p.d;
+            float* yp = p.y_part + (it.shared ? ((int64_t)pl.P2 * slots + (int64_t)it.part * p.T)
+                                              : ((int64_t)it.part * slots + it.row0)) * p.d + col;
+            for (int j0 = 0; j0 < it.cnt && active; j0 += 8) {
+                uint32_t u[8], v[8];
+                tmem_ld_32x32b_x8(tb + j0, u);
+                tmem_ld_32x32b_x8(tb + N + j0, v);
                 tmem_wait_ld();
-                if (col < p.d) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int j = 8 * g + i;
-                        if (j < it.cnt) yp[(int64_t)j * p.d + col] = __uint_as_float(u[i]);
-                    }
-                }
+                for (int i = 0; i < 8; ++i)
+                    if (ok && j0 + i < it.cnt)
+                        yp[(int64_t)(j0 + i) * p.d] = __uint_as_float(u[i]) + __uint_as_float(v[i]);
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(sm.tempty + 8 * acc);
-            __threadfence();
-            epi_sync();
-            const int dt = it.n0 / 128, want = p.k * L.plan->P2 + (p.hs > 0 ? L.plan->P2s : 0);
+            if (lane == 0) mbar_arrive(sm.tempty + 8 * group);
+            epi_sync(group);
+            const int dt = it.n0 / it.tw, want = p.k * pl.P2 + (p.hs > 0 ? pl.P2s : 0);
             if (tid < it.cnt) {
                 const int t = it.shared ? tid : L.row_tok[it.row0 + tid];
-                flags[tid] = atomicAdd(p.y_cnt + t * p.ntd + dt, 1) == want - 1 ? t : -1;
+                flags[tid] = add_acq_rel(p.y_cnt + t * pl.ntd + dt, 1) == want - 1 ? t : -1;
             }
-            epi_sync();
-            for (int j = warp; j < it.cnt; j += FEW_EPI_WARPS) {
+            epi_sync(group);
+            // Tokens that are now complete in these columns: slots in order, a slot's parts in
+            // order.  A lane holds the offset and the weight of one row; four columns each.
+            for (int j = warp; j < it.cnt; j += 4) {
                 const int t = flags[j];
                 if (t < 0) continue;
-                __threadfence();
-                const int cc = it.n0 + lane * 4;   // d is a multiple of 8: whole groups of 4
-                if (cc >= p.d) continue;
+                const int cc = it.n0 + lane * 4, nr = p.k * pl.P2, na = want;   // d is a multiple of 8
+                const bool in = lane * 4 < it.tw && cc < p.d;
                 float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int q = 0; q < p.k; ++q) {
-                    const float gt = L.gate[t * p.k + q];
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int pp = 0; pp < L.plan->P2; ++pp) {
-                        const float4 a = __ldcg(reinterpret_cast<const float4*>(
-                            p.y_part + ((int64_t)pp * slots + L.row_of[t * p.k + q]) * p.d + cc));
-                        o.x += a.x;
-                        o.y += a.y;
-                        o.z += a.z;
-                        o.w += a.w;
+                for (int r0 = 0; r0 < na; r0 += 32) {
+                    const int r = r0 + lane;
+                    int64_t row = 0;
+                    float g = 0.f;
+                    if (r < nr) {
+                        const int q = t * p.k + r / pl.P2;
+                        row = (int64_t)(r % pl.P2) * slots + L.row_of[q];
+                        g = L.gate[q];
+                    } else if (r < na) {
+                        row = (int64_t)pl.P2 * slots + (int64_t)(r - nr) * p.T + t;
+                        g = p.lambda;
                     }
-                    y.x = fmaf(gt, o.x, y.x);
-                    y.y = fmaf(gt, o.y, y.y);
-                    y.z = fmaf(gt, o.z, y.z);
-                    y.w = fmaf(gt, o.w, y.w);
-                }
-                if (p.hs > 0) {
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int pp = 0; pp < L.plan->P2s; ++pp) {
-                        const float4 a = __ldcg(reinterpret_cast<const float4*>(
-                            p.y_part + ((int64_t)L.plan->P2 * slots + (int64_t)pp * p.T + t) * p.d + cc));
-                        o.x += a.x;
-                        o.y += a.y;
-                        o.z += a.z;
-                        o.w += a.w;
+                    row = row * p.d + cc - lane * 4;
+                    for (int i0 = 0; i0 < 32 && r0 + i0 < na; i0 += 8) {
+                        float4 a[8];
+                        float gi[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {   // eight rows' loads in flight
+                            const int64_t at = __shfl_sync(0xffffffffu, row, i0 + i);
+                            gi[i] = __shfl_sync(0xffffffffu, g, i0 + i);
+                            a[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (in && r0 + i0 + i < na)
+                                a[i] = __ldcg(reinterpret_cast<const float4*>(p.y_part + at + lane * 4));
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (r0 + i0 + i >= na) break;
+                            y.x = fmaf(gi[i], a[i].x, y.x);
+                            y.y = fmaf(gi[i], a[i].y, y.y);
+                            y.z = fmaf(gi[i], a[i].z, y.z);
+                            y.w = fmaf(gi[i], a[i].w, y.w);
+                        }
                     }
-                    y.x = fmaf(p.lambda, o.x, y.x);
-                    y.y = fmaf(p.lambda, o.y, y.y);
-                    y.z = fmaf(p.lambda, o.z, y.z);
-                    y.w = fmaf(p.lambda, o.w, y.w);
                 }
-                uint2 u;
-                u.x = pack_bf16x2(y.x, y.y);
-                u.y = pack_bf16x2(y.z, y.w);
-                *reinterpret_cast<uint2*>(p.y + (int64_t)t * p.d + cc) = u;
+                if (in) {
+                    uint2 u;
+                    u.x = pack_bf16x2(y.x, y.y);
+                    u.y = pack_bf16x2(y.z, y.w);
+                    *reinterpret_cast<uint2*>(p.y + (int64_t)t * p.d + cc) = u;
+                }
             }
         }
     }
@@ -796,10 +904,10 @@ __host__ __device__ inline FewSizes few_sizes(int T, int k, int E, bool swiglu) 
     z.stage_bytes = (swiglu ? 2 : 1) * FEW_TILE_BYTES + 2 * nb * 128;
     // plan, gate, row_of, act, off, cnt, row_tok
     z.lists = 64 + ((4 * n + 2 * n + 4 * na + na + n + 15) & ~15);
-    const int left = FEW_SMEM_MAX - 1024 - FEW_BAR_BYTES - 320 - z.lists;
+    const int left = FEW_SMEM_MAX - 1024 - FEW_BAR_BYTES - FEW_FLAG_BYTES - z.lists;
     z.stages = left / z.stage_bytes;
     if (z.stages > 12) z.stages = 12;
-    z.total = 1024 + z.stages * z.stage_bytes + FEW_BAR_BYTES + 320 + z.lists;
+    z.total = 1024 + z.stages * z.stage_bytes + FEW_BAR_BYTES + FEW_FLAG_BYTES + z.lists;
     return z;
 }
 
@@ -810,10 +918,11 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     const FewSizes z = few_sizes(p.T, p.k, p.E, p.W3 != nullptr);
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + z.stages * z.stage_bytes);
     uint8_t* after = reinterpret_cast<uint8_t*>(bars) + FEW_BAR_BYTES;
-    volatile int* flags = reinterpret_cast<volatile int*>(after);            // 66 ints
-    volatile int* abort_flag = flags + 68;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(after) + 69;
-    uint8_t* at = after + 320;
+    volatile int* flags = reinterpret_cast<volatile int*>(after);            // 2 x 65 ints
+    volatile int* abort_flag = flags + 130;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(after) + 131;
+    float* xn = reinterpret_cast<float*>(after) + 132;                       // [FEW_SEL_WARPS]
+    uint8_t* at = after + FEW_FLAG_BYTES;
     const int n = p.T * p.k, na = n < p.E ? n : p.E;
     FewLists L;
     L.plan = reinterpret_cast<FewPlan*>(at);
@@ -828,7 +937,6 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     sm.stages = z.stages;
     sm.stage_bytes = z.stage_bytes;
     sm.b_off = z.stage_bytes - 2 * p.nb * 128;
-    sm.lo_off = p.nb * 128;
     sm.full = smem_u32(bars);
     sm.empty = sm.full + 8 * 12;
     sm.tfull = sm.empty + 8 * 12;
@@ -842,26 +950,42 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(sm.tfull + 8 * a, 1);
-            mbar_init(sm.tempty + 8 * a, FEW_EPI_WARPS);
+            mbar_init(sm.tempty + 8 * a, FEW_EPI_WARPS / 2);
         }
         mbar_init(sm.drain, 1);
         *abort_flag = 0;
         mbar_fence_init();
+        tma_prefetch_desc(&p.tW1);
+        tma_prefetch_desc(&p.tW2);
+        tma_prefetch_desc(&p.tX);
+        tma_prefetch_desc(&p.tH);
+        if (p.W3) tma_prefetch_desc(&p.tW3);
+        if (p.hs > 0) {
+            tma_prefetch_desc(&p.tS1);
+            tma_prefetch_desc(&p.tS2);
+            tma_prefetch_desc(&p.tHs);
+            if (p.W3) tma_prefetch_desc(&p.tS3);
+        }
     }
     pdl_wait();
     // counters of this call, used only after the grid barrier
     for (int i = blockIdx.x * FEW_THREADS + threadIdx.x; i < p.n_counters; i += gridDim.x * FEW_THREADS)
         p.done_up[i] = 0;
-    few_logits(p, reinterpret_cast<float*>(smem));
-    if (!grid_barrier(p.status, gridDim.x, p.limit_ns, SITE_FEW_BARRIER)) return;
-
-    const int sel_bytes = (p.E + 31) / 32 * 32 * 24, ring_bytes = z.stages * z.stage_bytes;
-    const int sel_warps = min(FEW_SEL_WARPS, ring_bytes / sel_bytes);
-    uint8_t* sel = smem + warp * sel_bytes;
-    if (p.T <= FEW_SEL_WARPS && p.T * sel_bytes + 8 * n <= ring_bytes) {   // every CTA selects
+    few_logits(p, smem);
+    const int sel_bytes = (p.E + 31) / 32 * 32 * FEW_SEL_BYTES, ring_bytes = z.stages * z.stage_bytes;
+    const bool everywhere = p.T <= FEW_SEL_WARPS && p.T * sel_bytes + 8 * n <= ring_bytes;
+    // tokens of this CTA: all, or every gridDim.x-th
+    const int t0 = everywhere ? 0 : blockIdx.x, step = everywhere ? 1 : (int)gridDim.x;
+    const int mine = everywhere ? p.T : (p.T - t0 + step - 1) / step;
+    if (warp < min(mine, FEW_SEL_WARPS)) {   // while the other CTAs arrive
+        const float v = few_norm(p, t0 + warp * step);
+        if ((threadIdx.x & 31) == 0) xn[warp] = v;
+    }
+    if (!few_barrier(p.status, p.limit_ns)) return;
+    if (everywhere) {
         int32_t* s_idx = reinterpret_cast<int32_t*>(smem + p.T * sel_bytes);
         float* s_gate = reinterpret_cast<float*>(s_idx + n);
-        if (warp < p.T) few_select(p, warp, sel, s_idx + warp * p.k, s_gate + warp * p.k);
+        few_select(p, 0, 1, mine, xn, smem, s_idx, s_gate);
         __syncthreads();
         if (blockIdx.x == 0)
             for (int i = threadIdx.x; i < n; i += FEW_THREADS) {
@@ -870,10 +994,16 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
             }
         few_plan<true>(p, L, s_idx, s_gate, smem);
     } else {
-        if (warp < sel_warps)
-            for (int t = blockIdx.x + (int)gridDim.x * warp; t < p.T; t += (int)gridDim.x * sel_warps)
-                few_select(p, t, sel, p.idx + t * p.k, p.gate + t * p.k);
-        if (!grid_barrier(p.status, gridDim.x, p.limit_ns, SITE_FEW_BARRIER)) return;
+        const int most = min(FEW_SEL_WARPS, ring_bytes / sel_bytes);   // (one batch, unless the GPU is tiny)
+        for (int i = 0; i < mine; i += most) {
+            if (i > 0) {
+                if (i + warp < mine && warp < most) xn[warp] = few_norm(p, t0 + (i + warp) * step);
+                __syncthreads();
+            }
+            few_select(p, t0 + i * step, step, min(most, mine - i), xn, smem, p.idx, p.gate);
+            __syncthreads();
+        }
+        if (!few_barrier(p.status, p.limit_ns)) return;
         few_plan<false>(p, L, p.idx, p.gate, smem);
     }
     __syncwarp();
@@ -888,11 +1018,14 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     const uint32_t tmem = *tmem_slot;
     if (warp < FEW_EPI_WARPS) {
         few_epilogue(p, sm, L, tmem, abort_flag, flags);
-    } else if ((threadIdx.x & 31) == 0) {
-        if (warp == FEW_WARP_W) few_load_w(p, sm, L, abort_flag);
-        else if (warp == FEW_WARP_MMA) few_mma(p, sm, L, tmem, abort_flag);
-        else if (warp == FEW_WARP_B) few_load_b(p, sm, L, abort_flag);
+    } else if (warp == FEW_WARP_W) {
+        if (elect_one()) few_load_w(p, sm, L, abort_flag);
+    } else if (warp == FEW_WARP_MMA) {
+        if (elect_one()) few_mma(p, sm, L, tmem, abort_flag);
+    } else if (warp == FEW_WARP_B) {
+        few_load_b(p, sm, L, abort_flag);
     }
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (warp == FEW_WARP_MMA) {
@@ -903,7 +1036,6 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
 
 inline size_t up256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 inline int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
-inline int64_t tiles128(int64_t v) { return (v + 127) / 128; }
 
 // Router split: parts of d for blocks of 8 experts.
 int few_rt_parts(int d, int E, int ctas) {
@@ -915,8 +1047,8 @@ int few_rt_parts(int d, int E, int ctas) {
 }
 
 struct FewLayout {
-    size_t idx, gate, part, wsq, counters, up_part, H, Hs, y_part, total;
-    int64_t n_done, n_up_cnt, n_y_cnt;
+    size_t idx, gate, part, wsq, counters, H, Hs, y_part, total;
+    int64_t n_done, n_y_cnt;
 };
 FewLayout few_layout(int64_t T, int64_t d, int64_t E, int64_t k, int64_t h, int64_t hs) {
     FewLayout L;
@@ -926,16 +1058,14 @@ FewLayout few_layout(int64_t T, int64_t d, int64_t E, int64_t k, int64_t h, int6
         o += up256(bytes);
         return at;
     };
-    const int64_t n = T * k, na = n < E ? n : E, nb = (T + 15) / 16 * 16;
+    const int64_t n = T * k, na = n < E ? n : E;
     L.idx = take(4 * n);
     L.gate = take(4 * n);
     L.part = take(4 * 8 * T * E);
     L.wsq = take(4 * 8 * E);
     L.n_done = na + 1;
-    L.n_up_cnt = na * tiles128(h) + tiles128(hs);
-    L.n_y_cnt = T * tiles128(d);
-    L.counters = take(4 * (L.n_done + L.n_up_cnt + L.n_y_cnt));
-    L.up_part = take((size_t)4 * FEW_MAX_PART * 2 * nb * 128);
+    L.n_y_cnt = T * ((d + 63) / 64);   // at most: 64-column items
+    L.counters = take(4 * (L.n_done + L.n_y_cnt));
     L.H = take(2 * 2 * n * up8(h));
     L.Hs = take(2 * 2 * T * up8(hs));
     L.y_part = take(4 * (FEW_MAX_P2 * n + (hs > 0 ? FEW_MAX_P2S * T : 0)) * d);
@@ -957,10 +1087,8 @@ cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaS
     a.part = reinterpret_cast<float*>(ws + L.part);
     a.wsq = reinterpret_cast<float*>(ws + L.wsq);
     a.done_up = reinterpret_cast<int32_t*>(ws + L.counters);
-    a.up_cnt = a.done_up + L.n_done;
-    a.y_cnt = a.up_cnt + L.n_up_cnt;
-    a.n_counters = (int)(L.n_done + L.n_up_cnt + L.n_y_cnt);
-    a.up_part = reinterpret_cast<float*>(ws + L.up_part);
+    a.y_cnt = a.done_up + L.n_done;
+    a.n_counters = (int)(L.n_done + L.n_y_cnt);
     a.H = reinterpret_cast<__nv_bfloat16*>(ws + L.H);
     a.Hs = reinterpret_cast<__nv_bfloat16*>(ws + L.Hs);
     a.y_part = reinterpret_cast<float*>(ws + L.y_part);
@@ -970,22 +1098,19 @@ cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaS
     a.ldhs = (int)up8(a.hs);
     a.na_max = n < a.E ? n : a.E;
     a.nb = (a.T + 15) / 16 * 16;
-    a.nt = (int)tiles128(a.h);
-    a.nt_s = (int)tiles128(a.hs);
-    a.ntd = (int)tiles128(a.d);
     a.nkb_d = (a.d + 63) / 64;
     a.nkb_h = (a.h + 63) / 64;
     a.nkb_hs = (a.hs + 63) / 64;
-    a.acc_cols = a.nb * (a.W3 ? 2 : 1);
+    a.acc_cols = 2 * a.nb;   // gate and up projections, or hi and lo pieces
     a.tmem_cols = 32;
     while (a.tmem_cols < 2 * a.acc_cols) a.tmem_cols *= 2;
     a.rt_eb = (a.E + 7) / 8;
     a.rt_parts = few_rt_parts(a.d, a.E, sms);
     a.rt_dch = (int)up8((a.d + a.rt_parts - 1) / a.rt_parts);
-    // length of the summation chains of a logit (few_logits): 16 products, their sums, the
-    // lanes, the warps, the parts; times 2^-24, with room for the second-order terms
-    const int kp = FEW_WARPS / ((a.T + 7) / 8);
-    const int chain = 16 + (a.rt_dch / (64 * kp) + a.rt_dch / FEW_RT_K + 2) + 2 + kp + a.rt_parts + 2;
+    // length of the summation chains of a logit (few_logits): 8 products, their sums (one more per
+    // staged block), the lanes, the warps, the parts; times 2^-24, with room for second order
+    const int kp = FEW_WARPS / ((a.T + 7) / 8), blocks = (a.rt_dch + FEW_RT_K - 1) / FEW_RT_K;
+    const int chain = 8 + (a.rt_dch / (64 * kp) + 2 * blocks) + 3 + kp + a.rt_parts;
     a.rt_err = 1.01f * (float)chain * 5.9604645e-8f;
 
     bool ok = make_weight_tmap_strided(&a.tW1, a.W1, a.h, a.d, a.E, a.hp, (int64_t)a.d * a.hp) &&

@@ -244,40 +244,6 @@ __device__ __forceinline__ Tile decode_tile(const GemmArgs& p, int64_t w) {
     return tile_finish(p, tile_load(p, w));
 }
 
-// GELU(u) = u/2 (1 + erf(u / sqrt 2)) = max(u, 0) - |u|/2 erfc(|u| / sqrt 2), the
-// second form free of the cancellation of 1 + erf for u < 0.  erfc from Abramowitz &
-// Stegun 7.1.28: erfc(z) = (1 + a1 z + a2 z^2 + ... + a6 z^6)^-16 for z >= 0, with
-// |error| <= 3e-7 (one reciprocal and no exponential; the sixteenth power by four
-// squarings, which overflow to +inf, and so to erfc = 0, only where erfc is far
-// below fp32 resolution).  Evaluated in fp32 the GELU error stays below 1e-6 in
-// absolute value; the hidden activation is then rounded to bf16 (2^-9 relative).
-// Two values at a time with the packed fp32x2 instructions.
-__device__ __forceinline__ void erfc_as2(float a0, float a1, float& q0, float& q1) {   // a0, a1 >= 0
-    const uint64_t z = f2_mul(f2_pack(a0, a1), f2_pack(0.70710678118654752f, 0.70710678118654752f));
-    uint64_t P = f2_fma(z, f2_pack(0.0000430638f, 0.0000430638f), f2_pack(0.0002765672f, 0.0002765672f));
-    P = f2_fma(P, z, f2_pack(0.0001520143f, 0.0001520143f));
-    P = f2_fma(P, z, f2_pack(0.0092705272f, 0.0092705272f));
-    P = f2_fma(P, z, f2_pack(0.0422820123f, 0.0422820123f));
-    P = f2_fma(P, z, f2_pack(0.0705230784f, 0.0705230784f));
-    P = f2_fma(P, z, f2_pack(1.0f, 1.0f));
-    P = f2_mul(P, P);
-    P = f2_mul(P, P);
-    P = f2_mul(P, P);
-    P = f2_mul(P, P);
-    float p0, p1;
-    f2_unpack(P, p0, p1);
-    q0 = rcp_approx(p0);
-    q1 = rcp_approx(p1);
-}
-
-__device__ __forceinline__ void gelu_erf2(float& u0, float& u1) {
-    float q0, q1;
-    erfc_as2(fabsf(u0), fabsf(u1), q0, q1);
-    const uint64_t r = f2_fma(f2_mul(f2_pack(fabsf(u0), fabsf(u1)), f2_pack(-0.5f, -0.5f)), f2_pack(q0, q1),
-                              f2_pack(fmaxf(u0, 0.0f), fmaxf(u1, 0.0f)));
-    f2_unpack(r, u0, u1);
-}
-
 // GELU'(u) = Phi(u) + u phi(u) (the derivative of the erf form) of two values, for the
 // training path: Phi(u) = erfc(-u / sqrt 2) / 2 from the erfc above (1 - q / 2 for
 // u >= 0, q / 2 below), phi(u) = exp(-u^2 / 2) / sqrt(2 pi) with CUDA's __expf.

@@ -365,14 +365,12 @@ struct FewArgs {
     CUtensorMap tX;                             // token rows, one-row boxes (gather)
     CUtensorMap tH, tHs;                        // hidden rows, 3-D {h, rows, 2}, boxes 64 x 16
     float *part, *wsq;        // router: partial logits [rt_parts][T][E], sums of squares [rt_parts][E]
-    int32_t *done_up, *up_cnt, *y_cnt;          // counters, n_counters in a row from done_up
+    int32_t *done_up, *y_cnt; // counters, n_counters in a row from done_up
     int n_counters;
-    float* up_part;           // partial up-projections [item][1 or 2][nb][128]
     __nv_bfloat16 *H, *Hs;    // hidden rows, hi then lo: [2][T k][ldh], [2][T][ldhs]
     float* y_part;            // partial outputs [P2][T k][d], [P2s][T][d]
     int ldh, ldhs, na_max;    // na_max: bound on the experts with tokens
     int nb;                   // token columns of a tile at most (T rounded up to 16)
-    int nt, nt_s, ntd;        // 128-column tiles of h, h_s and d
     int nkb_d, nkb_h, nkb_hs; // 64-row blocks of K
     int acc_cols, tmem_cols;
     int rt_eb, rt_parts, rt_dch;   // router: blocks of 8 experts, parts of d and their length
