@@ -15,7 +15,7 @@
 //   3. Expert products on tcgen05 with the weights as the M operand: D[columns of W, tokens] =
 //      W^T . x^T.  W tiles (64 or 128 columns, 64 rows of K at a time) go from HBM to shared
 //      memory by TMA as they lie (MN-major, 128-byte swizzle) and no thread touches them again;
-//      the tokens of the expert (TMA row gather) are the N operand, 16 to 64 columns, so the
+//      the tokens of the expert (TMA row gather) are the N operand, 16 or 32 columns, so the
 //      tensor cores do in passing what would otherwise cost an unpack and an FMA per weight and
 //      token.  Items (expert, columns) are dealt to the CTAs round-robin.
 //   4. Up items apply the activation and store it as two bf16 pieces (hi + lo, 16 bits) so that y
@@ -299,18 +299,19 @@ __device__ void few_select(const FewArgs& p, int t0, int step, int n, const floa
         const uint4* all = reinterpret_cast<const uint4*>(ok_of(w));
         const uint32_t o = ok_of(w)[e];
         int ahead = 0;
-#pragma unroll 2
+#pragma unroll 8
         for (int j = 0; j < e0 / 4; ++j) {
             const uint4 u = all[j];
             ahead += (u.x >= o) + (u.y >= o) + (u.z >= o) + (u.w >= o);
         }
-#pragma unroll 2
-        for (int j = e0 / 4; j < e0 / 4 + 8; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int j = e0 / 4 + i;
             const uint4 u = all[j];
             ahead += (u.x > o || (u.x == o && 4 * j < e)) + (u.y > o || (u.y == o && 4 * j + 1 < e)) +
                      (u.z > o || (u.z == o && 4 * j + 2 < e)) + (u.w > o || (u.w == o && 4 * j + 3 < e));
         }
-#pragma unroll 2
+#pragma unroll 8
         for (int j = e0 / 4 + 8; j < Ep / 4; ++j) {
             const uint4 u = all[j];
             ahead += (u.x > o) + (u.y > o) + (u.z > o) + (u.w > o);
@@ -418,24 +419,29 @@ __device__ void few_select(const FewArgs& p, int t0, int step, int n, const floa
 
 // ----------------------------------------------------- 3. work of a call
 
+// An entry is up to nb (16 or 32) tokens of one expert; most experts have one.  More tokens make
+// another entry, whose weights then come from L2: with larger N operands the ring would hold fewer
+// weights in flight for every expert.
+//
 // Built by every CTA from the selection; kept in shared memory.
 struct FewPlan {
-    int n_act;              // experts with tokens
+    int n_act;              // entries
     int tw, nt, nt_s;       // up items: columns (64 or 128), tiles of h and of h_s
     int tw2, ntd, P2, P2s;  // down items: columns, tiles of d, parts of K (routed, shared)
-    int n_up, n_shared_down, n_items;   // items: up, then down (shared first in each)
+    int n_up_shared, n_up, n_down_shared, n_items;   // items: up, then down (shared first in each)
 };
 
 struct FewItem {
-    int up, shared, i, e;   // i: active expert index
-    int n0, tw, kb0, kb1;
+    int up, shared, i;      // i: entry (routed), block of nb tokens (shared)
+    int e;
+    int n0, tw, kb0, kb1;   // columns; K blocks (up, SwiGLU: gate and up blocks alternate)
     int part;               // down: K part
-    int cnt, row0;          // tokens of the expert, first row
+    int cnt, row0;          // tokens, first row
 };
 
 struct FewLists {           // shared memory
     FewPlan* plan;
-    uint16_t* act;          // [na] expert of active index i
+    uint16_t* act;          // [na] expert of an entry
     uint16_t* off;          // [na] its first row
     uint8_t* cnt;           // [na] its tokens
     uint8_t* row_tok;       // [T k] token of a row
@@ -447,39 +453,41 @@ __device__ __forceinline__ FewItem few_item(const FewArgs& p, const FewLists& L,
     const FewPlan& pl = *L.plan;
     FewItem it;
     it.up = id < pl.n_up;
+    int q = it.up ? id : id - pl.n_up;
+    it.shared = q < (it.up ? pl.n_up_shared : pl.n_down_shared);
+    it.part = 0;
     if (it.up) {
-        it.shared = id < pl.nt_s;
-        const int q = id - pl.nt_s;
-        it.i = it.shared ? 0 : q / pl.nt;
         it.tw = pl.tw;
-        it.n0 = (it.shared ? id : q - it.i * pl.nt) * pl.tw;
-        it.part = 0;
         it.kb0 = 0;
-        it.kb1 = p.nkb_d;
+        it.kb1 = p.nkb_d * (p.W3 ? 2 : 1);
+        if (!it.shared) q -= pl.n_up_shared;
+        const int per = it.shared ? p.n_sh : pl.nt, r = q / per;   // shared: the blocks of a tile side by side
+        it.i = it.shared ? q - r * per : r;
+        it.n0 = (it.shared ? r : q - r * per) * pl.tw;
     } else {
-        int q = id - pl.n_up;
-        it.shared = q < pl.n_shared_down;
-        if (!it.shared) q -= pl.n_shared_down;
+        if (!it.shared) q -= pl.n_down_shared;
         const int P = it.shared ? pl.P2s : pl.P2, nkb = it.shared ? p.nkb_hs : p.nkb_h, r = q / P;
+        const int per = it.shared ? p.n_sh : pl.ntd, v = r / per;
         it.part = q - r * P;
-        it.i = it.shared ? 0 : r / pl.ntd;
+        it.i = it.shared ? r - v * per : v;
         it.tw = pl.tw2;
-        it.n0 = (it.shared ? r : r - it.i * pl.ntd) * pl.tw2;
+        it.n0 = (it.shared ? v : r - v * per) * pl.tw2;
         it.kb0 = it.part * nkb / P;
         it.kb1 = (it.part + 1) * nkb / P;
     }
     it.e = it.shared ? 0 : L.act[it.i];
-    it.cnt = it.shared ? p.T : L.cnt[it.i];
-    it.row0 = it.shared ? 0 : L.off[it.i];
+    it.row0 = it.shared ? it.i * p.nb : L.off[it.i];
+    it.cnt = it.shared ? min(p.nb, p.T - it.row0) : L.cnt[it.i];
     return it;
 }
 
 // Estimated time (ns) of `items` items of `blocks` K blocks of `kb` bytes: an SM takes a block
-// in kb / 70 GB/s at least, and c CTAs at work share 6600 GB/s (measured with tiles streamed by 8
-// to 152 SMs); the last, partial round of items runs at its own c; 400 ns an item besides.
+// in kb / 70 GB/s and 0.2 us (its waits and four MMAs) at least, and c CTAs at work share
+// 6600 GB/s (measured with tiles streamed by 8 to 152 SMs); the last, partial round of items runs
+// at its own c; 400 ns an item besides.
 __device__ __forceinline__ float few_time(int items, int blocks, int kb, int ctas) {
     const int rounds = items / ctas, rest = items - rounds * ctas;
-    const float one = (float)kb / 70.0f, all = (float)kb / 6600.0f;
+    const float one = fmaxf((float)kb / 70.0f, 200.0f), all = (float)kb / 6600.0f;
     return rounds * (blocks * fmaxf(one, all * ctas) + 400.0f) +
            (rest > 0 ? blocks * fmaxf(one, all * rest) + 400.0f : 0.0f);
 }
@@ -520,12 +528,13 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
         atomicOr(&mask[my_e[i]], 1ull << (s / p.k));
     }
     __syncthreads();
+    const int sh = p.nb == 16 ? 4 : 5;
     for (int q = warp; q * 32 < p.E; q += FEW_WARPS) {
         const int e = q * 32 + lane, c = e < p.E ? __popcll(mask[e]) : 0;
-        const uint32_t m = __ballot_sync(0xffffffffu, c > 0);
+        const int ent = (int)__reduce_add_sync(0xffffffffu, (unsigned)((c + p.nb - 1) >> sh));
         const int rows = (int)__reduce_add_sync(0xffffffffu, (unsigned)c);
         if (lane == 0) {
-            n_in[q] = __popc(m);
+            n_in[q] = ent;
             rows_in[q] = rows;
         }
     }
@@ -542,31 +551,31 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
     }
     const int n_act = __shfl_sync(0xffffffffu, na, 31);
     for (int q = warp; q * 32 < p.E; q += FEW_WARPS) {
-        const int e = q * 32 + lane, c = e < p.E ? __popcll(mask[e]) : 0;
-        int sum = c;   // inclusive prefix over the lanes
+        const int e = q * 32 + lane, c = e < p.E ? __popcll(mask[e]) : 0, ent = (c + p.nb - 1) >> sh;
+        int sum = c + (ent << 16);   // inclusive prefixes over the lanes: rows, entries
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += v;
         }
-        const uint32_t m = __ballot_sync(0xffffffffu, c > 0);
-        const int i = __shfl_sync(0xffffffffu, na, q) - n_in[q] + __popc(m & ((1u << lane) - 1u));
-        const int row = __shfl_sync(0xffffffffu, nrow, q) - rows_in[q] + sum - c;
-        if (c > 0) {
+        int i = __shfl_sync(0xffffffffu, na, q) - n_in[q] + (sum >> 16) - ent;
+        int row = __shfl_sync(0xffffffffu, nrow, q) - rows_in[q] + (sum & 0xffff) - c;
+        if (c > 0) off[e] = (uint16_t)row;
+        for (int left = c; left > 0; left -= p.nb, ++i, row += p.nb) {
             L.act[i] = (uint16_t)e;
             L.off[i] = (uint16_t)row;
-            L.cnt[i] = (uint8_t)c;
-            off[e] = (uint16_t)row;
+            L.cnt[i] = (uint8_t)min(left, p.nb);
         }
     }
     if (warp == FEW_WARPS - 1) {
         // 64-column items where 128-column ones are too few to keep all SMs streaming; down items
         // may also split K (their partial rows are joined anyway).
-        const int ctas = (int)gridDim.x, bn = up16((n + n_act - 1) / n_act) * 128, mats = p.W3 ? 2 : 1;
-        const int tw_l = 128 >> (lane & 1), tiles_l = n_act * ((p.h + tw_l - 1) / tw_l) + (p.hs + tw_l - 1) / tw_l;
-        const int up = few_fastest(lane < 2 ? few_time(tiles_l, p.nkb_d, mats * tw_l * 128 + bn, ctas) : 3.0e38f);
+        const int ctas = (int)gridDim.x, bn = up16(min((n + n_act - 1) / n_act, p.nb)) * 128, mats = p.W3 ? 2 : 1;
+        const int tw_l = 128 >> (lane & 1);
+        const int tiles_l = n_act * ((p.h + tw_l - 1) / tw_l) + p.n_sh * ((p.hs + tw_l - 1) / tw_l);
+        const int up = few_fastest(lane < 2 ? few_time(tiles_l, mats * p.nkb_d, tw_l * 128 + bn, ctas) : 3.0e38f);
         const int P_l = (lane >> 1) + 1, ntd_l = (p.d + tw_l - 1) / tw_l;
-        const int items_l = ntd_l * P_l * (n_act + (p.nkb_hs + p.nkb_h - 1) / p.nkb_h);
+        const int items_l = ntd_l * P_l * (n_act + p.n_sh * ((p.nkb_hs + p.nkb_h - 1) / p.nkb_h));
         const int dn = few_fastest(P_l <= FEW_MAX_P2 && P_l <= p.nkb_h
                                        ? few_time(items_l, (p.nkb_h + P_l - 1) / P_l, tw_l * 128 + 2 * bn, ctas)
                                        : 3.0e38f);
@@ -581,9 +590,10 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
             pl.ntd = (p.d + pl.tw2 - 1) / pl.tw2;
             // shared down items about as long as the routed ones
             pl.P2s = p.hs > 0 ? min(min(FEW_MAX_P2S, p.nkb_hs), max(1, (p.nkb_hs * pl.P2 + p.nkb_h / 2) / p.nkb_h)) : 1;
-            pl.n_up = n_act * pl.nt + pl.nt_s;
-            pl.n_shared_down = p.hs > 0 ? pl.ntd * pl.P2s : 0;
-            pl.n_items = pl.n_up + pl.n_shared_down + n_act * pl.ntd * pl.P2;
+            pl.n_up_shared = p.n_sh * pl.nt_s;
+            pl.n_up = n_act * pl.nt + pl.n_up_shared;
+            pl.n_down_shared = p.n_sh * pl.ntd * pl.P2s;
+            pl.n_items = pl.n_up + pl.n_down_shared + n_act * pl.ntd * pl.P2;
         }
     }
     __syncthreads();
@@ -603,7 +613,7 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
 
 struct FewSmem {
     uint32_t ring, full, empty, tfull, tempty, drain;
-    int stages, stage_bytes, b_off;   // b_off: the N operand within a stage
+    int stages, stage_bytes;   // a stage: weights (FEW_TILE_BYTES), then the N operand
 };
 
 __device__ __forceinline__ void few_abort(volatile int* flag, DevStatus* st, int site, int a) {
@@ -618,20 +628,20 @@ __device__ void few_load_w(const FewArgs& p, const FewSmem& sm, const FewLists& 
     uint32_t ph = 0;
     for (int id = blockIdx.x; id < n_items; id += gridDim.x) {
         const FewItem it = few_item(p, L, id);
-        const bool two = it.up && p.W3;
         const CUtensorMap* a = it.up ? (it.shared ? &p.tS1 : &p.tW1) : (it.shared ? &p.tS2 : &p.tW2);
         const CUtensorMap* a3 = it.shared ? &p.tS3 : &p.tW3;
+        const int two = it.up && p.W3;
         for (int kb = it.kb0; kb < it.kb1; ++kb) {
             if (!mbar_wait(sm.empty + 8 * s, ph ^ 1u, p.limit_ns, abort_flag)) {
                 few_abort(abort_flag, p.status, SITE_FEW_WAIT_EMPTY, id);
                 return;
             }
             const uint32_t bar = sm.full + 8 * s, dst = sm.ring + s * sm.stage_bytes;
-            mbar_arrive_expect_tx(bar, (two ? 2 : 1) * it.tw * 128);
-            for (int j = 0; j < it.tw; j += 64) {
-                tma_load_3d(dst + j * 128, a, bar, it.n0 + j, kb * 64, it.e);
-                if (two) tma_load_3d(dst + FEW_TILE_BYTES + j * 128, a3, bar, it.n0 + j, kb * 64, it.e);
-            }
+            mbar_arrive_expect_tx(bar, it.tw * 128);
+            const CUtensorMap* m = (two & kb) ? a3 : a;
+            const int k0 = (kb >> two) * 64;
+            tma_load_3d(dst, m, bar, it.n0, k0, it.e);
+            if (it.tw == 128) tma_load_3d(dst + FEW_TILE_BYTES / 2, m, bar, it.n0 + 64, k0, it.e);
             if (++s == sm.stages) {
                 s = 0;
                 ph ^= 1u;
@@ -640,54 +650,55 @@ __device__ void few_load_w(const FewArgs& p, const FewSmem& sm, const FewLists& 
     }
 }
 
-// The N operand, by a whole warp (a lane per 4 gathered rows): token rows (up) or the two pieces of
-// the hidden rows (down: hi, then lo N rows further), after the expert's up items are done.
-// Rows past the expert's last token repeat its first (up) or hold whatever follows (down):
-// their columns of D are not read.
+// The N operand: token rows (up) or the two pieces of the hidden rows (down: hi, then lo N rows
+// further), after the entry's up items are done.  Rows past the entry's last token repeat its
+// first (up) or hold whatever follows (down): their columns of D are not read.
 __device__ void few_load_b(const FewArgs& p, const FewSmem& sm, const FewLists& L, volatile int* abort_flag) {
-    const int n_items = L.plan->n_items, lane = threadIdx.x & 31;
+    const int n_items = L.plan->n_items;
     int s = 0;
     uint32_t ph = 0;
     for (int id = blockIdx.x; id < n_items; id += gridDim.x) {
         const FewItem it = few_item(p, L, id);
         const int N = up16(it.cnt);
-        int tok[4] = {};
+        int tok[32];
         if (it.up) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int j = 4 * lane + i < it.cnt ? 4 * lane + i : 0;
-                tok[i] = it.shared ? j : L.row_tok[it.row0 + j];
+            for (int i = 0; i < 32; ++i) {
+                const int j = i < it.cnt ? i : 0;
+                if (i < N) tok[i] = it.shared ? it.row0 + j : L.row_tok[it.row0 + j];
             }
         } else {
-            int ok = 1;
-            if (lane == 0) {
-                const int32_t* c = p.done_up + (it.shared ? p.na_max : it.i);
-                const int want = it.shared ? L.plan->nt_s : L.plan->nt;
-                const uint64_t t0 = globaltimer_ns();
-                for (uint32_t i = 1; ld_acquire(c) < want; ++i)
-                    if ((i & 63u) == 0u && (*abort_flag || globaltimer_ns() - t0 > p.limit_ns)) {
-                        few_abort(abort_flag, p.status, SITE_FEW_WAIT_UP, id);
-                        ok = 0;
-                        break;
-                    }
-            }
-            if (!__shfl_sync(0xffffffffu, ok, 0)) return;
+            const int32_t* c = p.done_up + (it.shared ? p.na_max + it.i : it.i);
+            const int want = it.shared ? L.plan->nt_s : L.plan->nt;
+            const uint64_t t0 = globaltimer_ns();
+            for (uint32_t i = 1; ld_acquire(c) < want; ++i)
+                if ((i & 63u) == 0u && (*abort_flag || globaltimer_ns() - t0 > p.limit_ns)) {
+                    few_abort(abort_flag, p.status, SITE_FEW_WAIT_UP, id);
+                    return;
+                }
             fence_proxy_async_all();   // the hidden rows were written by ordinary stores
         }
+        const int two = it.up && p.W3;
+        const CUtensorMap* h = it.shared ? &p.tHs : &p.tH;
         for (int kb = it.kb0; kb < it.kb1; ++kb) {
-            int ok = 1;
-            const uint32_t bar = sm.full + 8 * s, dst = sm.ring + s * sm.stage_bytes + sm.b_off;
-            if (lane == 0) {
-                ok = mbar_wait(sm.empty + 8 * s, ph ^ 1u, p.limit_ns, abort_flag);
-                if (ok) mbar_arrive_expect_tx(bar, (it.up ? 1 : 2) * N * 128);
-                else few_abort(abort_flag, p.status, SITE_FEW_WAIT_EMPTY, -id);
+            if (!mbar_wait(sm.empty + 8 * s, ph ^ 1u, p.limit_ns, abort_flag)) {
+                few_abort(abort_flag, p.status, SITE_FEW_WAIT_EMPTY, -id);
+                return;
             }
-            if (!__shfl_sync(0xffffffffu, ok, 0)) return;
+            const uint32_t bar = sm.full + 8 * s, dst = sm.ring + s * sm.stage_bytes + FEW_TILE_BYTES;
+            mbar_arrive_expect_tx(bar, (it.up ? 1 : 2) * N * 128);
+            const int k0 = (kb >> two) * 64;
             if (it.up) {
-                if (4 * lane < N) tma_gather4(dst + lane * 512, &p.tX, bar, kb * 64, tok[0], tok[1], tok[2], tok[3]);
-            } else if (8 * lane < N) {   // lanes 2 r, 2 r + 1: rows 16 r of hi and of lo
-                tma_load_3d(dst + (lane & 1) * N * 128 + (lane >> 1) * 2048, it.shared ? &p.tHs : &p.tH, bar, kb * 64,
-                            it.row0 + (lane >> 1) * 16, lane & 1);
+#pragma unroll
+                for (int r = 0; r < 32; r += 4)
+                    if (r < N) tma_gather4(dst + r * 128, &p.tX, bar, k0, tok[r], tok[r + 1], tok[r + 2], tok[r + 3]);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 32; r += 16)
+                    if (r < N) {
+                        tma_load_3d(dst + r * 128, h, bar, k0, it.row0 + r, 0);
+                        tma_load_3d(dst + (N + r) * 128, h, bar, k0, it.row0 + r, 1);
+                    }
             }
             if (++s == sm.stages) {
                 s = 0;
@@ -703,7 +714,7 @@ __device__ void few_mma(const FewArgs& p, const FewSmem& sm, const FewLists& L, 
     // weights MN-major: 64-column atoms 8192 bytes apart, K slices of 16 rows 2048 bytes apart;
     // tokens K-major: K slices 32 bytes apart
     const uint64_t wd0 = smem_desc_sw128(sm.ring, 8192, 1024);
-    const uint64_t bd0 = smem_desc_sw128(sm.ring + sm.b_off, 16, 1024);
+    const uint64_t bd0 = smem_desc_sw128(sm.ring + FEW_TILE_BYTES, 16, 1024);
     int s = 0, n = 0;
     uint32_t ph = 0;
     bool issued = false;
@@ -712,7 +723,7 @@ __device__ void few_mma(const FewArgs& p, const FewSmem& sm, const FewLists& L, 
         // down: hi and lo pieces of the tokens side by side, added by the epilogue
         const uint32_t idesc = idesc_bf16_f32(128, (it.up ? 1 : 2) * up16(it.cnt), true, false);
         const int acc = n & 1;
-        const bool two = it.up && p.W3;
+        const int two = it.up && p.W3;   // gate blocks into columns 0 .., up blocks into nb ..
         if (!mbar_wait(sm.tempty + 8 * acc, ((uint32_t)(n >> 1) & 1u) ^ 1u, p.limit_ns, abort_flag)) {
             few_abort(abort_flag, p.status, SITE_FEW_WAIT_TEMPTY, id);
             break;
@@ -730,10 +741,8 @@ __device__ void few_mma(const FewArgs& p, const FewSmem& sm, const FewLists& L, 
             const uint64_t bd = bd0 + (uint64_t)((s * sm.stage_bytes) >> 4);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint32_t add = (kb != it.kb0 || q != 0) ? 1u : 0u;
-                tc_mma_bf16(d, wd + q * (2048 >> 4), bd + q * (32 >> 4), idesc, add);
-                if (two)
-                    tc_mma_bf16(d + p.nb, wd + (FEW_TILE_BYTES >> 4) + q * (2048 >> 4), bd + q * (32 >> 4), idesc, add);
+                tc_mma_bf16(d + ((two & kb) ? p.nb : 0), wd + q * (2048 >> 4), bd + q * (32 >> 4), idesc,
+                            (kb > it.kb0 + two || q != 0) ? 1u : 0u);
             }
             issued = true;
             tc_commit(sm.empty + 8 * s);
@@ -811,13 +820,13 @@ __device__ void few_epilogue(const FewArgs& p, const FewSmem& sm, const FewLists
             if (lane == 0) mbar_arrive(sm.tempty + 8 * group);
             fence_proxy_async_all();   // the rows will be read by TMA
             epi_sync(group);
-            if (tid == 0) add_release(p.done_up + (it.shared ? p.na_max : it.i), 1);
+            if (tid == 0) add_release(p.done_up + (it.shared ? p.na_max + it.i : it.i), 1);
         } else {
             // rows of the partial outputs: [P2][T k] routed, then [P2s][T] shared
             const int col = it.n0 + c;
             const bool ok = c < it.tw && col < p.d;
-            float* yp = p.y_part + (it.shared ? ((int64_t)pl.P2 * slots + (int64_t)it.part * p.T)
-                                              : ((int64_t)it.part * slots + it.row0)) * p.d + col;
+            float* yp = p.y_part + (it.shared ? (int64_t)pl.P2 * slots + (int64_t)it.part * p.T : (int64_t)it.part * slots) * p.d +
+                        (int64_t)it.row0 * p.d + col;
             for (int j0 = 0; j0 < it.cnt && active; j0 += 8) {
                 uint32_t u[8], v[8];
                 tmem_ld_32x32b_x8(tb + j0, u);
@@ -834,7 +843,7 @@ __device__ void few_epilogue(const FewArgs& p, const FewSmem& sm, const FewLists
             epi_sync(group);
             const int dt = it.n0 / it.tw, want = p.k * pl.P2 + (p.hs > 0 ? pl.P2s : 0);
             if (tid < it.cnt) {
-                const int t = it.shared ? tid : L.row_tok[it.row0 + tid];
+                const int t = it.shared ? it.row0 + tid : L.row_tok[it.row0 + tid];
                 flags[tid] = add_acq_rel(p.y_cnt + t * pl.ntd + dt, 1) == want - 1 ? t : -1;
             }
             epi_sync(group);
@@ -898,10 +907,15 @@ __device__ void few_epilogue(const FewArgs& p, const FewSmem& sm, const FewLists
 struct FewSizes {
     int stage_bytes, stages, lists, total;
 };
-__host__ __device__ inline FewSizes few_sizes(int T, int k, int E, bool swiglu) {
+__host__ __device__ inline int few_nb(int T) { return T <= 16 ? 16 : 32; }
+__host__ __device__ inline int few_entries(int T, int k, int E) {   // at most
+    const int n = T * k;
+    return (n < E ? n : E) + n / few_nb(T);
+}
+__host__ __device__ inline FewSizes few_sizes(int T, int k, int E) {
     FewSizes z;
-    const int nb = (T + 15) / 16 * 16, n = T * k, na = n < E ? n : E;
-    z.stage_bytes = (swiglu ? 2 : 1) * FEW_TILE_BYTES + 2 * nb * 128;
+    const int n = T * k, na = few_entries(T, k, E);
+    z.stage_bytes = FEW_TILE_BYTES + 2 * few_nb(T) * 128;
     // plan, gate, row_of, act, off, cnt, row_tok
     z.lists = 64 + ((4 * n + 2 * n + 4 * na + na + n + 15) & ~15);
     const int left = FEW_SMEM_MAX - 1024 - FEW_BAR_BYTES - FEW_FLAG_BYTES - z.lists;
@@ -915,7 +929,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     extern __shared__ uint8_t few_smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(few_smem_raw) + 1023) &
                                                ~static_cast<uintptr_t>(1023));
-    const FewSizes z = few_sizes(p.T, p.k, p.E, p.W3 != nullptr);
+    const FewSizes z = few_sizes(p.T, p.k, p.E);
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + z.stages * z.stage_bytes);
     uint8_t* after = reinterpret_cast<uint8_t*>(bars) + FEW_BAR_BYTES;
     volatile int* flags = reinterpret_cast<volatile int*>(after);            // 2 x 65 ints
@@ -923,7 +937,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(after) + 131;
     float* xn = reinterpret_cast<float*>(after) + 132;                       // [FEW_SEL_WARPS]
     uint8_t* at = after + FEW_FLAG_BYTES;
-    const int n = p.T * p.k, na = n < p.E ? n : p.E;
+    const int n = p.T * p.k, na = p.na_max;
     FewLists L;
     L.plan = reinterpret_cast<FewPlan*>(at);
     L.gate = reinterpret_cast<float*>(at + 64);
@@ -936,7 +950,6 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     sm.ring = smem_u32(smem);
     sm.stages = z.stages;
     sm.stage_bytes = z.stage_bytes;
-    sm.b_off = z.stage_bytes - 2 * p.nb * 128;
     sm.full = smem_u32(bars);
     sm.empty = sm.full + 8 * 12;
     sm.tfull = sm.empty + 8 * 12;
@@ -1023,7 +1036,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     } else if (warp == FEW_WARP_MMA) {
         if (elect_one()) few_mma(p, sm, L, tmem, abort_flag);
     } else if (warp == FEW_WARP_B) {
-        few_load_b(p, sm, L, abort_flag);
+        if (elect_one()) few_load_b(p, sm, L, abort_flag);
     }
     __syncwarp();
     tc_fence_before();
@@ -1058,12 +1071,12 @@ FewLayout few_layout(int64_t T, int64_t d, int64_t E, int64_t k, int64_t h, int6
         o += up256(bytes);
         return at;
     };
-    const int64_t n = T * k, na = n < E ? n : E;
+    const int64_t n = T * k, na = few_entries((int)T, (int)k, (int)E);
     L.idx = take(4 * n);
     L.gate = take(4 * n);
     L.part = take(4 * 8 * T * E);
     L.wsq = take(4 * 8 * E);
-    L.n_done = na + 1;
+    L.n_done = na + (T + few_nb((int)T) - 1) / few_nb((int)T);
     L.n_y_cnt = T * ((d + 63) / 64);   // at most: 64-column items
     L.counters = take(4 * (L.n_done + L.n_y_cnt));
     L.H = take(2 * 2 * n * up8(h));
@@ -1096,8 +1109,9 @@ cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaS
     a.limit_ns = limit_ns;
     a.ldh = (int)up8(a.h);
     a.ldhs = (int)up8(a.hs);
-    a.na_max = n < a.E ? n : a.E;
-    a.nb = (a.T + 15) / 16 * 16;
+    a.na_max = few_entries(a.T, a.k, a.E);
+    a.nb = few_nb(a.T);
+    a.n_sh = a.hs > 0 ? (a.T + a.nb - 1) / a.nb : 0;
     a.nkb_d = (a.d + 63) / 64;
     a.nkb_h = (a.h + 63) / 64;
     a.nkb_hs = (a.hs + 63) / 64;
@@ -1133,7 +1147,7 @@ cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaS
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
-    const FewSizes z = few_sizes(a.T, a.k, a.E, a.W3 != nullptr);
+    const FewSizes z = few_sizes(a.T, a.k, a.E);
     const cudaError_t e = launch_pdl_coop(few_kernel, dim3((unsigned)sms), dim3(FEW_THREADS), z.total, s, a);
     count_launches(1);
     return e != cudaSuccess ? e : cudaGetLastError();

@@ -369,8 +369,8 @@ struct FewArgs {
     int n_counters;
     __nv_bfloat16 *H, *Hs;    // hidden rows, hi then lo: [2][T k][ldh], [2][T][ldhs]
     float* y_part;            // partial outputs [P2][T k][d], [P2s][T][d]
-    int ldh, ldhs, na_max;    // na_max: bound on the experts with tokens
-    int nb;                   // token columns of a tile at most (T rounded up to 16)
+    int ldh, ldhs, na_max;    // na_max: bound on the entries (experts with tokens, in blocks of nb)
+    int nb, n_sh;             // token columns of a tile at most; blocks of nb tokens of the shared expert
     int nkb_d, nkb_h, nkb_hs; // 64-row blocks of K
     int acc_cols, tmem_cols;
     int rt_eb, rt_parts, rt_dch;   // router: blocks of 8 experts, parts of d and their length
