@@ -56,22 +56,6 @@ constexpr int FEW_MAX_P2 = 4, FEW_MAX_P2S = 8;
 __device__ __forceinline__ int up16(int v) { return (v + 15) & ~15; }
 // Barrier of one epilogue group's 128 threads.
 __device__ __forceinline__ void epi_sync(int group) { asm volatile("bar.sync %0, 128;" ::"r"(group + 1) : "memory"); }
-// Counter updates that publish what the group wrote before its barrier, and (acq_rel) order
-// later reads after the other contributors' writes.
-__device__ __forceinline__ void add_release(int32_t* p, int v) {
-    asm volatile("red.add.release.gpu.global.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
-}
-__device__ __forceinline__ int add_acq_rel(int32_t* p, int v) {
-    int old;
-    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
-    return old;
-}
-__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
-__device__ __forceinline__ int ld_acquire(const int32_t* p) {
-    int v;
-    asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
 // 32 lanes x 8 consecutive 32-bit columns (thread i: lane base + i).
 __device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[8]) {
     asm volatile(

@@ -10,19 +10,36 @@
 // Kernels
 //   muon_moment_kernel  one pass over the gradient: momentum update (M <- mu M + G) and, per
 //                       chunk, partial sums of squares of U.  Bound by memory.
-//   muon_scale_kernel   X0 in the working format from U and the matrix's norm.
-//   ns_gemm_kernel      the three products of a step on tcgen05, each with its epilogue.
-//   ns_thin_kernel      all steps of a matrix whose smaller side is at most 32, in fp32.
+//   ns_kernel           everything else in one persistent launch: X0 from U and its norm, the
+//                       three products of every step on tcgen05 CTA pairs, and the output or the
+//                       weight update in the last product's epilogue.
+//   ns_thin_kernel      all of that for matrices whose smaller side is at most 32, in fp32.
 //
-// Working format.  X is held as hi + lo / 2048, two fp16 values (22 significant bits), times
-// 2^8; A and B as fp16 times 2^8.  The tensor cores multiply the hi parts (fp16 has three
-// bits more than bf16 at the same rate, and every entry of X, A and B is bounded by a few
-// units, so its range suffices), accumulate in fp32, and the a X term is added from the full
-// hi + lo pair in fp32.  That term is what keeps the directions in which U is (nearly)
-// singular clean: each step multiplies them by a = 3.4, so a rounding of X there would grow by
-// a^steps, several hundred times, while B X is small there to begin with.  Against 64 bits the
-// result is within 2e-3 (2-norm over 2-norm) for full-rank and for low-rank U alike; with X
-// rounded to fp16 alone it would be 4e-2 for a U of rank 16.
+// ns_kernel.  Work items are (matrix, stage, tile): stage 0 loads X0, then Gram, polynomial and
+// apply stages of each step.  Only a few matrices are under way at a time, in buffers that are
+// used again for the next ones, so that everything between U and the result stays in L2 (DRAM
+// then sees U, M and the weights once; with all matrices under way at once the apply stage alone
+// moved 1.4 GB a step and took 755 us of a 1000 us step on 256 x 416 x 1664).  The matrices under
+// way form NS_LANES groups that are one stage apart; in each slot of the schedule every group
+// advances by a stage, so that a tile's inputs were finished about a slot of other tiles earlier
+// and its pair rarely waits.  A counter per matrix holds the finished tiles of its stages, which
+// follow one another; an item waits for the count of all earlier stages.  Items are dealt to the
+// pairs round-robin in schedule order and depend on earlier slots only; all pairs are co-resident
+// (cooperative launch).
+//
+// Working format.  X is held as hi + lo, two fp16 values (22 significant bits), times 2^10; A and B
+// as fp16 times 2^10.  The tensor cores multiply the hi parts (fp16 has three bits more than bf16
+// at the same rate, and every entry of X, A and B is bounded by a few units, so its range
+// suffices), accumulate in fp32, and the a X term is added from hi and lo in fp32.  That term is
+// what keeps the directions in which U is (nearly) singular clean: each step multiplies them by
+// a = 3.4, so a rounding of X there would grow by a^steps, several hundred times, while B X is
+// small there to begin with.  Against 64 bits the result is within 2e-3 (2-norm over 2-norm) for
+// full-rank and for low-rank U alike; with X rounded to fp16 alone it would be 4e-2 for a U of
+// rank 16.  In the last two steps, whose roundings are not amplified any more, lo counts 2 and 1
+// times instead of a: where singular values have arrived near 1, B lo (which is not formed) takes
+// up most of a lo, and leaving both out is nearer (1.6e-3 becomes 1.4e-3 on Gaussian matrices).
+// For m <= 128 the roundings of a few singular values average less, and time is latency: there
+// A and B have lo parts too and every product is hi hi + hi lo + lo hi (about 1e-5).
 #include "internal.h"
 
 #include <cuda_fp16.h>
@@ -31,10 +48,8 @@ namespace mv {
 
 namespace {
 
-constexpr float NS_S = 256.0f;            // scale of X, A, B in the working format
-constexpr float NS_INV_S = 1.0f / 256.0f;
-constexpr float NS_LO = 2048.0f;          // lo holds (x - hi) * 2^11
-constexpr float NS_INV_LO = 1.0f / 2048.0f;
+constexpr float NS_S = 1024.0f;           // scale of X, A, B in the working format
+constexpr float NS_INV_S = 1.0f / 1024.0f;
 
 // ----------------------------------------------------- element loads (prologue)
 
@@ -87,7 +102,7 @@ __device__ __forceinline__ void split8(const float (&x)[8], uint4& hi, uint4& lo
     for (int q = 0; q < 4; ++q) {
         h[q] = pack_half2(x[2 * q], x[2 * q + 1]);
         const float2 f = unpack_half2(h[q]);
-        l[q] = pack_half2((x[2 * q] - f.x) * NS_LO, (x[2 * q + 1] - f.y) * NS_LO);
+        l[q] = pack_half2(x[2 * q] - f.x, x[2 * q + 1] - f.y);
     }
     hi = make_uint4(h[0], h[1], h[2], h[3]);
     lo = make_uint4(l[0], l[1], l[2], l[3]);
@@ -104,29 +119,32 @@ constexpr float NS_TINY = 8.271806125530277e-25f;   // 2^-80
 constexpr int NS_PRO_THREADS = 256;
 constexpr int NS_PRO_GROUPS = 4096;   // groups of 8 values per CTA
 
-struct ProArgs {
+// Where the update U comes from.
+struct UpdateArgs {
     const void* U;        // the update (or the gradient G) [N] x [r][ld_u]
     int64_t ld_u, st_u;
+    int u_bf16, vec;      // bf16 (else fp32); rows 16-byte aligned
     float* M;             // momentum (NULL: U is used as it is), laid out as U
     float mu;
     int nesterov;
-    int r, c, ld;         // ld: row stride of the working arrays (c rounded up to 8)
+    int r, c, gpr;        // gpr: groups of 8 per row
     int groups, chunks;   // groups of 8 per matrix, chunks of NS_PRO_GROUPS of them
-    float* part;          // [N][chunks][3]
-    __half* xh;           // [N][r][ld]
-    __half* xl;
+    float* part;          // sums of squares [N][chunks][3]
+    int32_t* prog;        // progress counters of the matrices, cleared here
 };
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(NS_PRO_THREADS) muon_moment_kernel(const __grid_constant__ ProArgs p) {
+__global__ void __launch_bounds__(NS_PRO_THREADS) muon_moment_kernel(const __grid_constant__ UpdateArgs p) {
     pdl_wait();
-    const int e = blockIdx.y, gpr = p.ld / 8;
+    const int e = blockIdx.y;
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.prog[e] = 0;
     const int g0 = blockIdx.x * NS_PRO_GROUPS, g1 = min(g0 + NS_PRO_GROUPS, p.groups);
     const T* U = static_cast<const T*>(p.U) + e * p.st_u;
     float* M = p.M ? p.M + e * p.st_u : nullptr;
     float s0 = 0.f, s1 = 0.f, s2 = 0.f;
+#pragma unroll 2
     for (int g = g0 + (int)threadIdx.x; g < g1; g += NS_PRO_THREADS) {
-        const int row = g / gpr, col = (g - row * gpr) * 8, n = p.c - col;
+        const int row = g / p.gpr, col = (g - row * p.gpr) * 8, n = p.c - col;
         const int64_t at = row * p.ld_u + col;
         float v[8];
         load8<T, VEC>(U + at, n, v);
@@ -168,14 +186,21 @@ __global__ void __launch_bounds__(NS_PRO_THREADS) muon_moment_kernel(const __gri
     }
 }
 
-// x = (v * pre) * post in the working format, from the matrix's partial sums (added in chunk
-// order by every thread's CTA, so that all of them use the same bits).
-__device__ __forceinline__ void norm_scales(const float* part, int chunks, float& pre, float& post) {
+// X0 = (v * pre) * post from the matrix's partial sums, by one warp (every lane gets the result;
+// a fixed order, so that all warps of the grid use the same bits).
+__device__ __forceinline__ void norm_scales(const UpdateArgs& u, int e, float& pre, float& post) {
+    const float* part = u.part + (int64_t)e * u.chunks * 3;
     float s0 = 0.f, s1 = 0.f, s2 = 0.f;
-    for (int i = 0; i < chunks; ++i) {
-        s0 += part[3 * i];
-        s1 += part[3 * i + 1];
-        s2 += part[3 * i + 2];
+    for (int i = threadIdx.x & 31; i < u.chunks; i += 32) {
+        s0 += __ldg(part + 3 * i);
+        s1 += __ldg(part + 3 * i + 1);
+        s2 += __ldg(part + 3 * i + 2);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        s0 += __shfl_xor_sync(0xffffffffu, s0, o);
+        s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+        s2 += __shfl_xor_sync(0xffffffffu, s2, o);
     }
     float s = s0;
     pre = 1.f;
@@ -186,76 +211,75 @@ __device__ __forceinline__ void norm_scales(const float* part, int chunks, float
         s = s2;
         pre = NS_UP;
     }
-    post = s == 0.f ? 0.f : NS_S / sqrtf(s);   // a zero matrix stays zero; NaN stays NaN
+    post = s == 0.f ? 0.f : 1.0f / sqrtf(s);   // a zero matrix stays zero; NaN stays NaN
 }
 
+// Eight values of the update U of matrix e (n of them exist).
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(NS_PRO_THREADS) muon_scale_kernel(const __grid_constant__ ProArgs p) {
-    pdl_wait();
-    __shared__ float sc[2];
-    const int e = blockIdx.y, gpr = p.ld / 8;
-    if (threadIdx.x == 0) norm_scales(p.part + (int64_t)e * p.chunks * 3, p.chunks, sc[0], sc[1]);
-    __syncthreads();
-    const float pre = sc[0], post = sc[1];
-    const int g0 = blockIdx.x * NS_PRO_GROUPS, g1 = min(g0 + NS_PRO_GROUPS, p.groups);
-    const T* U = static_cast<const T*>(p.U) + e * p.st_u;
-    const float* M = p.M ? p.M + e * p.st_u : nullptr;
-    __half* xh = p.xh + (int64_t)e * p.r * p.ld;
-    __half* xl = p.xl + (int64_t)e * p.r * p.ld;
-    for (int g = g0 + (int)threadIdx.x; g < g1; g += NS_PRO_THREADS) {
-        const int row = g / gpr, col = (g - row * gpr) * 8, n = p.c - col;
-        const int64_t at = row * p.ld_u + col;
-        float v[8];
-        if (M && !p.nesterov) {
-            load8<float, VEC>(M + at, n, v);
-        } else {
-            load8<T, VEC>(U + at, n, v);
-            if (M) {
-                float m[8];
-                load8<float, VEC>(M + at, n, m);
+__device__ __forceinline__ void update8_as(const UpdateArgs& u, int e, int row, int col, int n, float (&v)[8]) {
+    const int64_t at = e * u.st_u + row * u.ld_u + col;
+    if (u.M && !u.nesterov) {
+        load8<float, VEC>(u.M + at, n, v);
+        return;
+    }
+    load8<T, VEC>(static_cast<const T*>(u.U) + at, n, v);
+    if (u.M) {
+        float m[8];
+        load8<float, VEC>(u.M + at, n, m);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = fmaf(p.mu, m[i], v[i]);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (v[i] * pre) * post;
-        uint4 hi, lo;
-        split8(v, hi, lo);
-        *reinterpret_cast<uint4*>(xh + (int64_t)g * 8) = hi;
-        *reinterpret_cast<uint4*>(xl + (int64_t)g * 8) = lo;
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(u.mu, m[i], v[i]);
+    }
+}
+__device__ __forceinline__ void update8(const UpdateArgs& u, int e, int row, int col, int n, float (&v)[8]) {
+    if (u.u_bf16) {
+        if (u.vec) update8_as<__nv_bfloat16, true>(u, e, row, col, n, v);
+        else update8_as<__nv_bfloat16, false>(u, e, row, col, n, v);
+    } else {
+        if (u.vec) update8_as<float, true>(u, e, row, col, n, v);
+        else update8_as<float, false>(u, e, row, col, n, v);
     }
 }
 
 // ------------------------------------------------------------------ products
 
-constexpr int NS_BM = 128;            // output rows per tile: TMEM lanes
+constexpr int NS_BM = 256;            // output rows per tile: a CTA pair, 128 rows (TMEM lanes) each
+constexpr int NS_HALF = 128;
 constexpr int NS_MAXBN = 256;         // output columns per tile at most (one tcgen05.mma)
-constexpr int NS_BK = 64;             // K per stage: one 128-byte swizzle row of fp16
-constexpr int NS_STAGES = 4;
-constexpr int NS_BOX = 64 * NS_BK * 2;                  // bytes of one 64 x 64 TMA box
-constexpr int NS_STAGE_BYTES = (NS_BM + NS_MAXBN) / 64 * NS_BOX;
+constexpr int NS_BK = 64;             // K per ring stage: one 128-byte swizzle row of fp16
+constexpr int NS_STAGES = 6;
+constexpr int NS_BOX = 64 * NS_BK * 2;                     // bytes of one 64 x 64 TMA box
+constexpr int NS_STAGE_BYTES = (NS_HALF + NS_MAXBN / 2) / 64 * NS_BOX;   // a CTA's A rows and half of B
 constexpr int NS_EPI_WARPS = 8;       // two per TMEM lane quadrant, alternate 32-column chunks
 constexpr int NS_WARP_LOAD = NS_EPI_WARPS;
 constexpr int NS_WARP_MMA = NS_EPI_WARPS + 1;
 constexpr int NS_THREADS = (NS_EPI_WARPS + 2) * 32;
-constexpr int NS_SMEM = NS_STAGES * NS_STAGE_BYTES + 1024 + 256;
+constexpr int NS_STG_LD = 36;         // floats per staged row (32 values, padded)
+constexpr int NS_STG_ROWS = 16;       // rows a warp stages at a time
+constexpr int NS_STG_BYTES = NS_EPI_WARPS * NS_STG_ROWS * NS_STG_LD * 4;
+constexpr int NS_SMEM = NS_STAGES * NS_STAGE_BYTES + NS_STG_BYTES + 1024 + 256;
 static_assert(NS_SMEM <= 232448, "shared memory of one CTA");
 
-enum NsKind : int { NS_GRAM = 0, NS_POLY = 1, NS_APPLY = 2 };
+constexpr int NS_LANES = 3;           // groups of matrices under way, a stage apart
+constexpr int NS_LOAD_GROUPS = 2048;  // groups of 8 values per load item (half per CTA of the pair)
+constexpr int NS_MAX_STAGES = 1 + 3 * NS_MAX_STEPS;
+constexpr int NS_DONE = 2 * NS_EPI_WARPS;   // a finished item's contribution to its matrix's counter
+
+enum NsKind : int { NS_LOAD = 0, NS_GRAM = 1, NS_POLY = 2, NS_APPLY = 3 };
 
 struct NsArgs {
-    CUtensorMap tmX[2], tmA, tmB;   // 3-D maps {inner, rows, N}, boxes 64 x 64
-    __half* xh[2];                  // X hi, ping-pong [N][r][ldx]
-    __half* xl;                     // X lo [N][r][ldx]; each element is rewritten by the thread that reads it
-    __half* A;                      // [N][m][ldm]
-    __half* B;
-    int N, r, c, m, ldx, ldm, tall;
-    int bn_s, nt_s, mt_s, sym_tiles;   // m x m outputs: tile width, tiles across, down, computed
-    int bn_x, nt_x, mt_x;              // r x c outputs
-    int kind, src;                     // this launch's product; X buffer it reads
-    float ca, cb, cc;                  // the step's coefficients
-    int last;                          // NS_APPLY of the last step: write the outputs
-    // outputs of the last step
+    CUtensorMap tX[2][2], tA[2], tB[2];   // [buffer][hi, lo]; 3-D maps {inner, rows, slots}, boxes 64 x 64
+    UpdateArgs u;
+    __half *xh[2], *xl[2];             // X, ping-pong [slots][r][ldx] (lo in place with one term)
+    __half *A[2], *B[2];               // hi, lo (lo with three terms only) [slots][m][ldm]
+    int N, r, c, m, ldx, ldm, tall, terms;
+    int bn_s, nt_s, mt_s, bn_x, nt_x, mt_x;   // tiles of m x m and of r x c outputs
+    int tiles[4];                      // items of a matrix's stage, by kind
+    int n_stages, n_groups, group_max; // stages of a matrix; groups of matrices; their largest size
+    int total;                         // items
+    uint8_t kind[NS_MAX_STAGES], step[NS_MAX_STAGES];
+    int need[NS_MAX_STAGES + 1];       // counter value at which a stage's inputs are complete
+    float coef[3 * NS_MAX_STEPS], lo_coef[NS_MAX_STEPS];   // lo_coef: multiplier of lo in a X
+    int steps;
     __nv_bfloat16* O;                  // orthogonalised matrices (or NULL)
     int64_t ld_o, st_o;
     int vec_o;
@@ -267,27 +291,104 @@ struct NsArgs {
     uint64_t limit_ns;
 };
 
+// Position of a role in the schedule: slot t holds items [base, base + count).
+struct NsWalk {
+    int t, base, count;
+};
+struct NsItem {
+    int e, buf, stage, kind, step, tile;
+    int prev;                          // the matrix that used the buffers before, or -1
+};
+
+__device__ __forceinline__ int ns_first(const NsArgs& p, int g) {   // first matrix of group g
+    return (int)((int64_t)g * p.N / p.n_groups);
+}
+// Group and stage of lane l in slot t; false when it has none.
+__device__ __forceinline__ bool ns_lane(const NsArgs& p, int t, int l, int& g, int& stage) {
+    const int u = t - l;
+    if (u < 0) return false;
+    const int q = u / p.n_stages;
+    g = q * NS_LANES + l;
+    stage = u - q * p.n_stages;
+    return g < p.n_groups;
+}
+__device__ __forceinline__ int ns_slot_count(const NsArgs& p, int t) {
+    int n = 0;
+#pragma unroll
+    for (int l = 0; l < NS_LANES; ++l) {
+        int g, st;
+        if (ns_lane(p, t, l, g, st)) n += (ns_first(p, g + 1) - ns_first(p, g)) * p.tiles[p.kind[st]];
+    }
+    return n;
+}
+__device__ __forceinline__ NsWalk ns_walk_start(const NsArgs& p) { return {0, 0, ns_slot_count(p, 0)}; }
+
+// Item `id` (ids only grow from call to call).
+__device__ __forceinline__ NsItem ns_item(const NsArgs& p, NsWalk& w, int id) {
+    while (id >= w.base + w.count) {
+        w.base += w.count;
+        w.count = ns_slot_count(p, ++w.t);
+    }
+    NsItem it = {};
+    int pos = id - w.base;
+#pragma unroll
+    for (int l = 0; l < NS_LANES; ++l) {
+        int g, st;
+        if (pos < 0 || !ns_lane(p, w.t, l, g, st)) continue;
+        const int first = ns_first(p, g), tiles = p.tiles[p.kind[st]], n = (ns_first(p, g + 1) - first) * tiles;
+        if (pos < n) {
+            const int i = pos / tiles;
+            it.e = first + i;
+            it.buf = l * p.group_max + i;
+            it.stage = st;
+            it.kind = p.kind[st];
+            it.step = p.step[st];
+            it.tile = pos - i * tiles;
+            it.prev = -1;   // sizes of groups differ by one: at most one group back lacks the place
+            for (int h = g - NS_LANES; h >= 0; h -= NS_LANES)
+                if (i < ns_first(p, h + 1) - ns_first(p, h)) {
+                    it.prev = ns_first(p, h) + i;
+                    break;
+                }
+            pos = -1;
+        } else {
+            pos -= n;
+        }
+    }
+    return it;
+}
+
 struct NsTile {
-    int e, m0, n0, num_kb, bn;
+    int m0, n0, bn, num_kb;            // num_kb: K blocks of one term
+    const CUtensorMap *a[2], *b[2];    // operands, hi and lo
+    bool a_mn, b_mn;
 };
 
 // First needed tile of row tile i of a symmetric output: tiles left of it lie strictly below
 // the diagonal and are written as mirror images.
 __device__ __forceinline__ int sym_first(const NsArgs& p, int i) { return i * NS_BM / p.bn_s; }
 
-__device__ __forceinline__ NsTile ns_tile(const NsArgs& p, int w) {
+// Operand layouts of a product: an operand whose K runs along the rows of its array is read
+// MN-major, one whose K runs along the columns K-major; no array is ever transposed.
+//   r <= c:  Gram  X X^T both K-major;   apply B X: B K-major, X MN-major
+//   r >  c:  Gram  X^T X both MN-major;  apply X B: both K-major (B is symmetric)
+__device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
     NsTile t;
-    if (p.kind == NS_APPLY) {
-        const int per = p.mt_x * p.nt_x;
-        t.e = w / per;
-        const int q = w - t.e * per;
-        t.m0 = q / p.nt_x * NS_BM;
-        t.n0 = q % p.nt_x * p.bn_x;
+    const int src = it.step & 1;
+    int k = p.m;
+    if (it.kind == NS_APPLY) {
+        t.m0 = it.tile / p.nt_x * NS_BM;
+        t.n0 = it.tile % p.nt_x * p.bn_x;
         t.bn = p.bn_x;
-        t.num_kb = (p.m + NS_BK - 1) / NS_BK;
+        t.a_mn = false;
+        t.b_mn = !p.tall;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            t.a[i] = p.tall ? &p.tX[src][i] : &p.tB[i];
+            t.b[i] = p.tall ? &p.tB[i] : &p.tX[src][i];
+        }
     } else {
-        t.e = w / p.sym_tiles;
-        int q = w - t.e * p.sym_tiles, i = 0;
+        int q = it.tile, i = 0;
         for (; i < p.mt_s - 1; ++i) {
             const int n = p.nt_s - sym_first(p, i);
             if (q < n) break;
@@ -296,9 +397,13 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, int w) {
         t.m0 = i * NS_BM;
         t.n0 = (sym_first(p, i) + q) * p.bn_s;
         t.bn = p.bn_s;
-        const int k = p.kind == NS_GRAM ? (p.tall ? p.r : p.c) : p.m;
-        t.num_kb = (k + NS_BK - 1) / NS_BK;
+        const bool gram = it.kind == NS_GRAM;
+        if (gram) k = p.tall ? p.r : p.c;
+        t.a_mn = t.b_mn = gram && p.tall;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) t.a[j] = t.b[j] = gram ? &p.tX[src][j] : &p.tA[j];
     }
+    t.num_kb = (k + NS_BK - 1) / NS_BK;
     return t;
 }
 
@@ -307,33 +412,11 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn_maj
            ((static_cast<uint32_t>(N) >> 3) << 17) | ((static_cast<uint32_t>(M) >> 4) << 24);
 }
 
-// Operand layouts of a product: an operand whose K runs along the rows of its array is read
-// MN-major, one whose K runs along the columns K-major; no array is ever transposed.
-//   r <= c:  Gram  X X^T both K-major;   apply B X: B K-major, X MN-major
-//   r >  c:  Gram  X^T X both MN-major;  apply X B: both K-major (B is symmetric)
-struct NsOperands {
-    const CUtensorMap *a, *b;
-    bool a_mn, b_mn;
-};
-__device__ __forceinline__ NsOperands ns_operands(const NsArgs& p) {
-    NsOperands o;
-    if (p.kind == NS_GRAM) {
-        o.a = o.b = &p.tmX[p.src];
-        o.a_mn = o.b_mn = p.tall;
-    } else if (p.kind == NS_POLY) {
-        o.a = o.b = &p.tmA;
-        o.a_mn = o.b_mn = false;
-    } else {
-        o.a = p.tall ? &p.tmX[p.src] : &p.tmB;
-        o.b = p.tall ? &p.tmB : &p.tmX[p.src];
-        o.a_mn = false;
-        o.b_mn = !p.tall;
-    }
-    return o;
-}
-
 struct NsSmem {
     uint32_t ring, full, empty, tfull, tempty, drain;
+    float* stg;
+    uint32_t rank;
+    int pair, npairs;
 };
 
 __device__ __forceinline__ void ns_abort(volatile int* flag, DevStatus* st, int site, int a) {
@@ -341,64 +424,89 @@ __device__ __forceinline__ void ns_abort(volatile int* flag, DevStatus* st, int 
     report(st, MOEVIE_ERR_TIMEOUT, site, (int)blockIdx.x, a);
 }
 
-__device__ void ns_producer(const NsArgs& p, const NsSmem& sm, int n_work, volatile int* abort_flag) {
-    const NsOperands o = ns_operands(p);
-    tma_prefetch_desc(o.a);
-    tma_prefetch_desc(o.b);
+// Waits until matrix e's counter has reached `want` (its writers' stores are then visible).
+__device__ __forceinline__ bool ns_wait(const NsArgs& p, int e, int want, volatile int* abort_flag, int site) {
+    const int32_t* c = p.u.prog + e;
+    if (ld_acquire(c) >= want) return true;
+    const uint64_t t0 = globaltimer_ns();
+    for (uint32_t i = 1; ld_acquire(c) < want; ++i) {
+        if ((i & 63u) == 0u && (*abort_flag || globaltimer_ns() - t0 > p.limit_ns)) {
+            ns_abort(abort_flag, p.status, site, e);
+            return false;
+        }
+    }
+    return true;
+}
+
+// TMA producer (one thread per CTA): the CTA's 128 rows of A and its half of B's columns; the
+// leader posts the byte count of both CTAs on its full barrier.
+__device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abort_flag) {
+    const uint32_t full_leader = peer_addr(sm.full, 0);
     int s = 0;
     uint32_t ph = 0;
-    for (int w = blockIdx.x; w < n_work; w += gridDim.x) {
-        const NsTile t = ns_tile(p, w);
-        const int nbox = (t.bn + 63) / 64;
-        const uint32_t bytes = (uint32_t)(2 + nbox) * NS_BOX;
-        for (int kb = 0; kb < t.num_kb; ++kb) {
-            if (!mbar_wait(sm.empty + 8 * s, ph ^ 1u, p.limit_ns, abort_flag)) {
-                ns_abort(abort_flag, p.status, SITE_NS_WAIT_EMPTY, w);
-                return;
-            }
-            const uint32_t bar = sm.full + 8 * s, dst = sm.ring + s * NS_STAGE_BYTES;
-            mbar_arrive_expect_tx(bar, bytes);
-            const int kk = kb * NS_BK;
+    NsWalk w = ns_walk_start(p);
+    for (int id = sm.pair; id < p.total; id += sm.npairs) {
+        const NsItem it = ns_item(p, w, id);
+        if (it.kind == NS_LOAD) continue;
+        const NsTile t = ns_tile(p, it);
+        if (!ns_wait(p, it.e, p.need[it.stage], abort_flag, SITE_NS_WAIT_INPUT)) return;
+        fence_proxy_async_all();   // the inputs were written by ordinary stores
+        const int nbox = (t.bn / 2 + 63) / 64;
+        const uint32_t bytes = 2u * (uint32_t)(2 + nbox) * NS_BOX;
+        const int mm = t.m0 + (int)sm.rank * NS_HALF, nn = t.n0 + (int)sm.rank * (t.bn / 2);
+        for (int term = 0; term < p.terms; ++term) {
+            const CUtensorMap *ma = t.a[term == 2], *mb = t.b[term == 1];   // hi hi, hi lo, lo hi
+            for (int kb = 0; kb < t.num_kb; ++kb) {
+                if (!mbar_wait(sm.empty + 8 * s, ph ^ 1u, p.limit_ns, abort_flag)) {
+                    ns_abort(abort_flag, p.status, SITE_NS_WAIT_EMPTY, id);
+                    return;
+                }
+                const uint32_t bar = full_leader + 8 * s, dst = sm.ring + s * NS_STAGE_BYTES;
+                if (sm.rank == 0) mbar_arrive_expect_tx(sm.full + 8 * s, bytes);
+                const int kk = kb * NS_BK;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int mm = t.m0 + 64 * j;
-                tma_load_3d(dst + j * NS_BOX, o.a, bar, o.a_mn ? mm : kk, o.a_mn ? kk : mm, t.e);
-            }
-            for (int j = 0; j < nbox; ++j) {
-                const int nn = t.n0 + 64 * j;
-                tma_load_3d(dst + (2 + j) * NS_BOX, o.b, bar, o.b_mn ? nn : kk, o.b_mn ? kk : nn, t.e);
-            }
-            if (++s == NS_STAGES) {
-                s = 0;
-                ph ^= 1u;
+                for (int j = 0; j < 2; ++j)
+                    tma_load_3d_pair(dst + j * NS_BOX, ma, bar, t.a_mn ? mm + 64 * j : kk, t.a_mn ? kk : mm + 64 * j,
+                                     it.buf);
+                for (int j = 0; j < nbox; ++j)
+                    tma_load_3d_pair(dst + (2 + j) * NS_BOX, mb, bar, t.b_mn ? nn + 64 * j : kk,
+                                     t.b_mn ? kk : nn + 64 * j, it.buf);
+                if (++s == NS_STAGES) {
+                    s = 0;
+                    ph ^= 1u;
+                }
             }
         }
     }
 }
 
-__device__ __forceinline__ void ns_mma(const NsArgs& p, const NsSmem& sm, uint32_t tmem, int n_work,
-                                       volatile int* abort_flag) {
-    const NsOperands o = ns_operands(p);
-    const uint64_t ad0 = smem_desc_sw128(sm.ring, o.a_mn ? NS_BOX : 16, 1024);
-    const uint64_t bd0 = smem_desc_sw128(sm.ring + 2 * NS_BOX, o.b_mn ? NS_BOX : 16, 1024);
-    const uint32_t as = (o.a_mn ? 2048 : 32) >> 4, bs = (o.b_mn ? 2048 : 32) >> 4;
-    int s = 0, it = 0;
+// MMA issuer: one thread of the leader CTA.
+__device__ __forceinline__ void ns_mma(const NsArgs& p, const NsSmem& sm, uint32_t tmem, volatile int* abort_flag) {
+    int s = 0, n = 0;
     uint32_t ph = 0;
     bool issued = false;
-    for (int w = blockIdx.x; w < n_work; w += gridDim.x, ++it) {
-        const NsTile t = ns_tile(p, w);
-        const uint32_t idesc = idesc_f16_f32(NS_BM, t.bn, o.a_mn, o.b_mn);
-        const int acc = it & 1;
-        if (!mbar_wait(sm.tempty + 8 * acc, ((it >> 1) & 1) ^ 1u, p.limit_ns, abort_flag)) {
-            ns_abort(abort_flag, p.status, SITE_NS_WAIT_TEMPTY, w);
+    NsWalk w = ns_walk_start(p);
+    for (int id = sm.pair; id < p.total; id += sm.npairs) {
+        const NsItem it = ns_item(p, w, id);
+        if (it.kind == NS_LOAD) continue;
+        const NsTile t = ns_tile(p, it);
+        const uint32_t idesc = idesc_f16_f32(NS_BM, t.bn, t.a_mn, t.b_mn);
+        const uint64_t ad0 = smem_desc_sw128(sm.ring, t.a_mn ? NS_BOX : 16, 1024);
+        const uint64_t bd0 = smem_desc_sw128(sm.ring + 2 * NS_BOX, t.b_mn ? NS_BOX : 16, 1024);
+        const uint32_t as = (t.a_mn ? 2048 : 32) >> 4, bs = (t.b_mn ? 2048 : 32) >> 4;
+        const int acc = n & 1;
+        if (!mbar_wait(sm.tempty + 8 * acc, ((uint32_t)(n >> 1) & 1u) ^ 1u, p.limit_ns, abort_flag)) {
+            ns_abort(abort_flag, p.status, SITE_NS_WAIT_TEMPTY, id);
             break;
         }
+        ++n;
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)acc * NS_MAXBN;
+        const int kbs = t.num_kb * p.terms;
         bool ok = true;
-        for (int kb = 0; kb < t.num_kb; ++kb) {
+        for (int kb = 0; kb < kbs; ++kb) {
             if (!mbar_wait(sm.full + 8 * s, ph, p.limit_ns, abort_flag)) {
-                ns_abort(abort_flag, p.status, SITE_NS_WAIT_FULL, w);
+                ns_abort(abort_flag, p.status, SITE_NS_WAIT_FULL, id);
                 ok = false;
                 break;
             }
@@ -406,27 +514,25 @@ __device__ __forceinline__ void ns_mma(const NsArgs& p, const NsSmem& sm, uint32
             const uint64_t bd = bd0 + (uint64_t)((s * NS_STAGE_BYTES) >> 4);
 #pragma unroll
             for (int q = 0; q < NS_BK / 16; ++q)
-                tc_mma_bf16(d, ad + q * as, bd + q * bs, idesc, (kb | q) != 0 ? 1u : 0u);
+                tc_mma_bf16_pair(d, ad + q * as, bd + q * bs, idesc, (kb | q) != 0 ? 1u : 0u);
             issued = true;
-            tc_commit(sm.empty + 8 * s);
+            tc_commit_pair(sm.empty + 8 * s);
             if (++s == NS_STAGES) {
                 s = 0;
                 ph ^= 1u;
             }
         }
         if (!ok) break;
-        tc_commit(sm.tfull + 8 * acc);
+        tc_commit_pair(sm.tfull + 8 * acc);
     }
     if (issued) {   // every tcgen05.mma is complete before TMEM is released
-        tc_commit(sm.drain);
+        tc_commit_pair(sm.drain);
         if (!mbar_wait(sm.drain, 0, p.limit_ns, nullptr))
             report(p.status, MOEVIE_ERR_TIMEOUT, SITE_NS_DRAIN, (int)blockIdx.x, 0);
     }
 }
 
-// Eight working-format values of a row from L2 (written by other SMs).
-__device__ __forceinline__ void load_half8(const __half* p, float (&v)[8]) {
-    const uint4 u = __ldcg(reinterpret_cast<const uint4*>(p));
+__device__ __forceinline__ void unpack_half8(const uint4& u, float (&v)[8]) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -435,146 +541,247 @@ __device__ __forceinline__ void load_half8(const __half* p, float (&v)[8]) {
         v[2 * q + 1] = f.y;
     }
 }
-
-// One group of eight columns of an output row.
-__device__ __forceinline__ void ns_store_sym(const NsArgs& p, const NsTile& t, int row, int col,
-                                             const float (&d)[8]) {
-    const int64_t base = (int64_t)t.e * p.m * p.ldm;
-    float v[8];
-    const bool gram = p.kind == NS_GRAM;
-    if (gram) {
-        // with c = 0 the step has no A^2: B = b A comes straight from the Gram product
-        const float sc = p.cc == 0.f ? p.cb * NS_INV_S : NS_INV_S;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = d[i] * sc;
-    } else {
-        load_half8(p.A + base + (int64_t)row * p.ldm + col, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = fmaf(p.cc * NS_INV_S, d[i], p.cb * v[i]);
-    }
-    __half* out = (gram && p.cc != 0.f ? p.A : p.B) + base;
-    uint4 u;
-    u.x = pack_half2(v[0], v[1]);
-    u.y = pack_half2(v[2], v[3]);
-    u.z = pack_half2(v[4], v[5]);
-    u.w = pack_half2(v[6], v[7]);
-    *reinterpret_cast<uint4*>(out + (int64_t)row * p.ldm + col) = u;
-    // the mirror image, where its own tile is not computed
-    const int col_end = (row / p.bn_s + 1) * p.bn_s;   // end of the tile column that holds `row`
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int j = col + i;
-        if (j < p.m && col_end <= j / NS_BM * NS_BM) out[(int64_t)j * p.ldm + row] = __float2half_rn(v[i]);
-    }
+__device__ __forceinline__ uint4 pack_bf16x8(const float (&v)[8], float sc) {
+    return make_uint4(pack_bf16x2(v[0] * sc, v[1] * sc), pack_bf16x2(v[2] * sc, v[3] * sc),
+                      pack_bf16x2(v[4] * sc, v[5] * sc), pack_bf16x2(v[6] * sc, v[7] * sc));
 }
 
-__device__ __forceinline__ void ns_store_x(const NsArgs& p, const NsTile& t, int row, int col,
-                                           const float (&d)[8]) {
-    const int64_t at = ((int64_t)t.e * p.r + row) * p.ldx + col;
-    float v[8], l[8];
-    load_half8(p.xh[p.src] + at, v);
-    load_half8(p.xl + at, l);
+// X0 = U / |U| of a range of groups of matrix it.e, by the 8 epilogue warps.
+__device__ __forceinline__ void ns_load_x0(const NsArgs& p, const NsItem& it, uint32_t rank) {
+    float pre, post;
+    norm_scales(p.u, it.e, pre, post);
+    post *= NS_S;
+    constexpr int HALF = NS_LOAD_GROUPS / 2;
+    const int g0 = it.tile * NS_LOAD_GROUPS + (int)rank * HALF, g1 = min(g0 + HALF, p.u.groups);
+    const int64_t base = (int64_t)it.buf * p.r * p.ldx;
+#pragma unroll 2
+    for (int g = g0 + (int)threadIdx.x; g < g1; g += NS_EPI_WARPS * 32) {
+        const int row = g / p.u.gpr, col = (g - row * p.u.gpr) * 8;
+        float v[8];
+        update8(p.u, it.e, row, col, p.c - col, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = fmaf(NS_INV_S, d[i], p.ca * fmaf(NS_INV_LO, l[i], v[i]));
-    if (!p.last) {
+        for (int i = 0; i < 8; ++i) v[i] = (v[i] * pre) * post;
         uint4 hi, lo;
         split8(v, hi, lo);
-        *reinterpret_cast<uint4*>(p.xh[p.src ^ 1] + at) = hi;
-        *reinterpret_cast<uint4*>(p.xl + at) = lo;
-        return;
-    }
-    const int n = p.c - col;   // columns of this group that exist
-    if (p.O) {
-        __nv_bfloat16* o = p.O + t.e * p.st_o + row * p.ld_o + col;
-        if (p.vec_o && n >= 8) {
-            uint4 u;
-            u.x = pack_bf16x2(v[0] * NS_INV_S, v[1] * NS_INV_S);
-            u.y = pack_bf16x2(v[2] * NS_INV_S, v[3] * NS_INV_S);
-            u.z = pack_bf16x2(v[4] * NS_INV_S, v[5] * NS_INV_S);
-            u.w = pack_bf16x2(v[6] * NS_INV_S, v[7] * NS_INV_S);
-            *reinterpret_cast<uint4*>(o) = u;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < n) o[i] = __float2bfloat16_rn(v[i] * NS_INV_S);
-        }
-    } else {
-        const int64_t wat = t.e * p.st_w + row * p.ld_w + col;
-        float w[8];
-        load8<float, true>(p.W + wat, n, w);
-        const float rate = p.rate * NS_INV_S;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = fmaf(-rate, v[i], p.decay * w[i]);
-        store8<true>(p.W + wat, n, w);
-        if (p.Wb) {
-            if (n >= 8) {
-                uint4 u;
-                u.x = pack_bf16x2(w[0], w[1]);
-                u.y = pack_bf16x2(w[2], w[3]);
-                u.z = pack_bf16x2(w[4], w[5]);
-                u.w = pack_bf16x2(w[6], w[7]);
-                *reinterpret_cast<uint4*>(p.Wb + wat) = u;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 7; ++i)
-                    if (i < n) p.Wb[wat + i] = __float2bfloat16_rn(w[i]);
-            }
-        }
+        *reinterpret_cast<uint4*>(p.xh[0] + base + (int64_t)g * 8) = hi;   // ldx = 8 gpr
+        *reinterpret_cast<uint4*>(p.xl[0] + base + (int64_t)g * 8) = lo;
     }
 }
 
-__device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, int n_work,
-                            volatile int* abort_flag) {
+// Warp w reads TMEM lanes 32 (w % 4) .. of its CTA's 128 rows and the 32-column chunks w / 4,
+// w / 4 + 2, ... of a tile.  The accumulator rows pass a small per-warp buffer so that four
+// consecutive lanes hold 32 consecutive columns of a row and every global access of a warp covers
+// eight whole 64-byte (fp16) pieces; what a chunk reads from L2 is loaded a chunk ahead.
+__device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, volatile int* abort_flag) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int quad = warp & 3, half = warp >> 2;
-    int it = 0;
-    for (int w = blockIdx.x; w < n_work; w += gridDim.x, ++it) {
-        const NsTile t = ns_tile(p, w);
-        const int acc = it & 1, row = t.m0 + quad * 32 + lane;
-        const int rows = p.kind == NS_APPLY ? p.r : p.m, cols = p.kind == NS_APPLY ? p.c : p.m;
-        const int nchunk = (t.bn + 31) / 32;
-        if (!mbar_wait(sm.tfull + 8 * acc, (uint32_t)(it >> 1) & 1u, p.limit_ns, abort_flag)) {
-            ns_abort(abort_flag, p.status, SITE_NS_WAIT_TFULL, w);
-            return;
-        }
-        tc_fence_after();
-        const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * NS_MAXBN;
-        for (int ch = half; ch < nchunk; ch += 2) {
-            uint32_t v[32];
-            tmem_ld_32x32b_x32(tbase + ch * 32, v);
-            tmem_wait_ld();
-            if (row >= rows) continue;
+    float* stg = sm.stg + warp * NS_STG_ROWS * NS_STG_LD;
+    const uint32_t tempty_leader = peer_addr(sm.tempty, 0);
+    const int lr = lane >> 2, lc = (lane & 3) * 8;   // a lane's row (of 8) and first column after staging
+    int n = 0;
+    NsWalk w = ns_walk_start(p);
+    for (int id = sm.pair; id < p.total; id += sm.npairs) {
+        const NsItem it = ns_item(p, w, id);
+        if (it.kind == NS_LOAD) {
+            int ok = 1;   // the buffers' last user is done with them
+            if (lane == 0 && it.prev >= 0) ok = ns_wait(p, it.prev, p.need[p.n_stages], abort_flag, SITE_NS_WAIT_BUFFER);
+            if (!__shfl_sync(0xffffffffu, ok, 0)) return;
+            ns_load_x0(p, it, sm.rank);
+        } else {
+            const NsTile t = ns_tile(p, it);
+            const bool apply = it.kind == NS_APPLY, gram = it.kind == NS_GRAM;
+            const bool last = apply && it.step == p.steps - 1;
+            const int rows = apply ? p.r : p.m, cols = apply ? p.c : p.m;
+            const float ca = p.coef[3 * it.step], cb = p.coef[3 * it.step + 1], cc = p.coef[3 * it.step + 2];
+            const int src = it.step & 1;
+            const int row0 = t.m0 + (int)sm.rank * NS_HALF + quad * 32;
+            const int ld = apply ? p.ldx : p.ldm;
+            const int64_t base = (int64_t)it.buf * rows * ld;
+            // what the chunk reads: A (polynomial) or X (apply), hi and lo
+            const __half* ph = apply ? p.xh[src] : gram ? nullptr : p.A[0];
+            const __half* pl = apply ? p.xl[src] : (gram || p.terms == 1) ? nullptr : p.A[1];
+            const int nchunk = (t.bn + 31) / 32;
+            uint4 nh[4], nl[4];
+            auto fetch = [&](int ch) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int off = ch * 32 + g * 8, col = t.n0 + off;
-                if (off >= t.bn || col >= cols) break;
-                float d[8];
+                for (int i = 0; i < 4; ++i) {
+                    const int row = row0 + 8 * i + lr, off = ch * 32 + lc, col = t.n0 + off;
+                    nh[i] = nl[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (ph && row < rows && off < t.bn && col < cols) {
+                        const int64_t at = base + (int64_t)row * ld + col;
+                        nh[i] = __ldcg(reinterpret_cast<const uint4*>(ph + at));
+                        if (pl) nl[i] = __ldcg(reinterpret_cast<const uint4*>(pl + at));
+                    }
+                }
+            };
+            if (ph) {
+                int ok = 1;
+                if (lane == 0) ok = ns_wait(p, it.e, p.need[it.stage], abort_flag, SITE_NS_WAIT_INPUT);
+                if (!__shfl_sync(0xffffffffu, ok, 0)) return;
+            }
+            if (half < nchunk) fetch(half);
+            const int acc = n & 1;
+            if (!mbar_wait(sm.tfull + 8 * acc, (uint32_t)(n >> 1) & 1u, p.limit_ns, abort_flag)) {
+                ns_abort(abort_flag, p.status, SITE_NS_WAIT_TFULL, id);
+                return;
+            }
+            ++n;
+            tc_fence_after();
+            const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * NS_MAXBN;
+            if (half >= nchunk) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote(tempty_leader + 8 * acc);
+            }
+            for (int ch = half; ch < nchunk; ch += 2) {
+                uint32_t v[32];
+                tmem_ld_32x32b_x32(tbase + ch * 32, v);
+                tmem_wait_ld();
+                if (ch + 2 >= nchunk) {   // this warp's last read of the accumulator
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_remote(tempty_leader + 8 * acc);
+                }
+                uint4 xh[4], xl[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] = __uint_as_float(v[8 * g + i]);
-                if (p.kind == NS_APPLY) ns_store_x(p, t, row, col, d);
-                else ns_store_sym(p, t, row, col, d);
+                for (int i = 0; i < 4; ++i) {
+                    xh[i] = nh[i];
+                    xl[i] = nl[i];
+                }
+                if (ch + 2 < nchunk) fetch(ch + 2);
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    if ((lane >> 4) == hh) {
+                        float4* o = reinterpret_cast<float4*>(stg + (lane & 15) * NS_STG_LD);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            o[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
+                                               __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int row = row0 + hh * 16 + 8 * i + lr, off = ch * 32 + lc, col = t.n0 + off;
+                        float4* cell = reinterpret_cast<float4*>(stg + (8 * i + lr) * NS_STG_LD + lc);
+                        const float4 d0 = cell[0], d1 = cell[1];
+                        float d[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w}, x[8], y[8];
+                        unpack_half8(xh[2 * hh + i], x);
+                        unpack_half8(xl[2 * hh + i], y);
+                        const bool in = row < rows && off < t.bn && col < cols;
+                        const int64_t at = base + (int64_t)row * ld + col;
+                        if (apply) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                x[j] = fmaf(NS_INV_S, d[j], fmaf(ca, x[j], p.lo_coef[it.step] * y[j]));
+                            if (!last) {
+                                uint4 hi, lo;
+                                split8(x, hi, lo);
+                                if (in) {
+                                    *reinterpret_cast<uint4*>(p.xh[src ^ 1] + at) = hi;
+                                    *reinterpret_cast<uint4*>(p.xl[src ^ 1] + at) = lo;
+                                }
+                            } else if (in) {
+                                const int nc = p.c - col;   // columns of this group that exist
+                                if (p.O) {
+                                    __nv_bfloat16* o = p.O + it.e * p.st_o + row * p.ld_o + col;
+                                    if (p.vec_o && nc >= 8) {
+                                        *reinterpret_cast<uint4*>(o) = pack_bf16x8(x, NS_INV_S);
+                                    } else {
+#pragma unroll
+                                        for (int j = 0; j < 8; ++j)
+                                            if (j < nc) o[j] = __float2bfloat16_rn(x[j] * NS_INV_S);
+                                    }
+                                } else {
+                                    const int64_t wat = it.e * p.st_w + row * p.ld_w + col;
+                                    const float rate = p.rate * NS_INV_S;
+                                    load8<float, true>(p.W + wat, nc, y);
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j) y[j] = fmaf(-rate, x[j], p.decay * y[j]);
+                                    store8<true>(p.W + wat, nc, y);
+                                    if (p.Wb) {
+                                        if (nc >= 8) {
+                                            *reinterpret_cast<uint4*>(p.Wb + wat) = pack_bf16x8(y, 1.0f);
+                                        } else {
+#pragma unroll
+                                            for (int j = 0; j < 8; ++j)
+                                                if (j < nc) p.Wb[wat + j] = __float2bfloat16_rn(y[j]);
+                                        }
+                                    }
+                                }
+                            }
+                        } else {
+                            // Gram: A = D.  Polynomial: B = b A + c D.  A step with c = 0 has no
+                            // polynomial stage: its Gram writes B = b D.
+                            if (gram) {
+                                const float sc = cc == 0.f ? cb * NS_INV_S : NS_INV_S;
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) x[j] = d[j] * sc;
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) x[j] = fmaf(cc * NS_INV_S, d[j], cb * (x[j] + y[j]));
+                            }
+                            uint4 hi, lo;
+                            split8(x, hi, lo);
+                            __half* const* out = gram && cc != 0.f ? p.A : p.B;
+                            if (in) {
+                                *reinterpret_cast<uint4*>(out[0] + at) = hi;
+                                if (p.terms == 3) *reinterpret_cast<uint4*>(out[1] + at) = lo;
+                            }
+                            cell[0] = make_float4(x[0], x[1], x[2], x[3]);
+                            cell[1] = make_float4(x[4], x[5], x[6], x[7]);
+                        }
+                    }
+                    __syncwarp();
+                    if (!apply) {
+                        // mirror images of the 16 x 32 values, where their own tiles are not
+                        // computed: a lane takes 8 rows of a column
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int j = ch * 32 + 16 * i + (lane >> 1), col = t.n0 + j, r8 = (lane & 1) * 8;
+                            const int row = row0 + hh * 16 + r8;
+                            const int col_end = (row / p.bn_s + 1) * p.bn_s;   // end of the tile column holding `row`
+                            if (j < t.bn && col < p.m && row < p.m && col_end <= col / NS_BM * NS_BM) {
+                                float x[8];
+#pragma unroll
+                                for (int q = 0; q < 8; ++q) x[q] = stg[(r8 + q) * NS_STG_LD + 16 * i + (lane >> 1)];
+                                uint4 hi, lo;
+                                split8(x, hi, lo);
+                                __half* const* out = gram && cc != 0.f ? p.A : p.B;
+                                const int64_t at = base + (int64_t)col * ld + row;
+                                *reinterpret_cast<uint4*>(out[0] + at) = hi;
+                                if (p.terms == 3) *reinterpret_cast<uint4*>(out[1] + at) = lo;
+                            }
+                        }
+                        __syncwarp();
+                    }
+                }
             }
         }
-        tc_fence_before();
+        fence_proxy_async_all();   // what was written will be read by TMA
         __syncwarp();
-        if (lane == 0) mbar_arrive(sm.tempty + 8 * acc);
+        if (lane == 0) add_release(p.u.prog + it.e, 1);
     }
 }
 
-__global__ void __launch_bounds__(NS_THREADS, 1) ns_gemm_kernel(const __grid_constant__ NsArgs p) {
+__global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant__ NsArgs p) {
     extern __shared__ uint8_t ns_smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ns_smem_raw) + 1023) &
                                                ~static_cast<uintptr_t>(1023));
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + NS_STAGES * NS_STAGE_BYTES);
+    uint8_t* after = smem + NS_STAGES * NS_STAGE_BYTES;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(after + NS_STG_BYTES);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * NS_STAGES + 5);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     NsSmem sm;
     sm.ring = smem_u32(smem);
+    sm.stg = reinterpret_cast<float*>(after);
     sm.full = smem_u32(bars);
     sm.empty = sm.full + 8 * NS_STAGES;
     sm.tfull = sm.empty + 8 * NS_STAGES;
     sm.tempty = sm.tfull + 16;
     sm.drain = sm.tempty + 16;
+    sm.rank = cluster_rank();
+    sm.pair = blockIdx.x >> 1;
+    sm.npairs = gridDim.x >> 1;
     const int warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS_STAGES; ++s) {
@@ -583,34 +790,36 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_gemm_kernel(const __grid_con
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(sm.tfull + 8 * a, 1);
-            mbar_init(sm.tempty + 8 * a, NS_EPI_WARPS);
+            mbar_init(sm.tempty + 8 * a, 2 * NS_EPI_WARPS);
         }
         mbar_init(sm.drain, 1);
         *abort_flag = 0;
         mbar_fence_init();
     }
     if (warp == NS_WARP_MMA) {
-        tmem_alloc(smem_u32(tmem_slot), 2 * NS_MAXBN);
-        tmem_relinquish();
+        tmem_alloc_pair(smem_u32(tmem_slot), 2 * NS_MAXBN);
+        tmem_relinquish_pair();
     }
     tc_fence_before();
     __syncthreads();
+    cluster_sync();   // barriers of both CTAs initialised before any remote arrival
     tc_fence_after();
     pdl_wait();
     const uint32_t tmem = *tmem_slot;
-    const int n_work = p.N * (p.kind == NS_APPLY ? p.mt_x * p.nt_x : p.sym_tiles);
     if (warp < NS_EPI_WARPS) {
-        ns_epilogue(p, sm, tmem, n_work, abort_flag);
+        ns_epilogue(p, sm, tmem, abort_flag);
     } else if (warp == NS_WARP_LOAD) {
-        if ((threadIdx.x & 31) == 0) ns_producer(p, sm, n_work, abort_flag);
+        if (elect_one()) ns_producer(p, sm, abort_flag);
     } else {
-        if ((threadIdx.x & 31) == 0) ns_mma(p, sm, tmem, n_work, abort_flag);
+        if (sm.rank == 0 && elect_one()) ns_mma(p, sm, tmem, abort_flag);
     }
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
+    cluster_sync();   // the leader's MMAs have drained; both CTAs are done with TMEM
     if (warp == NS_WARP_MMA) {
         tc_fence_after();
-        tmem_dealloc(tmem, 2 * NS_MAXBN);
+        tmem_dealloc_pair(tmem, 2 * NS_MAXBN);
     }
 }
 
@@ -637,27 +846,28 @@ __device__ __forceinline__ void ns_out1(const NsArgs& p, int e, int row, int col
     }
 }
 
-struct NsSteps {
-    float coef[3 * NS_MAX_STEPS];
-    int steps;
-};
-
-__global__ void __launch_bounds__(NS_THIN_THREADS) ns_thin_kernel(const __grid_constant__ NsArgs p,
-                                                                  const __grid_constant__ NsSteps st) {
+__global__ void __launch_bounds__(NS_THIN_THREADS) ns_thin_kernel(const __grid_constant__ NsArgs p) {
     pdl_wait();
     __shared__ float A[NS_THIN][NS_THIN + 1], P[NS_THIN][NS_THIN + 1], Q[NS_THIN][NS_THIN + 1],
         T[NS_THIN][NS_THIN + 1], xs[NS_THIN][NS_THIN_K + 1];
     const int e = blockIdx.x, m = p.m, n = p.tall ? p.r : p.c, tid = threadIdx.x;
     constexpr int PER = NS_THIN * NS_THIN / NS_THIN_THREADS;
-    const __half* xh = p.xh[0] + (int64_t)e * p.r * p.ldx;
-    const __half* xl = p.xl + (int64_t)e * p.r * p.ldx;
+    float pre, post;
+    norm_scales(p.u, e, pre, post);
     auto stage = [&](int k0) {   // xs[i][kk] = X0 (i, k0 + kk) of the m x n orientation
         for (int q = tid; q < m * NS_THIN_K; q += NS_THIN_THREADS) {
             const int i = p.tall ? q % m : q / NS_THIN_K, kk = p.tall ? q / m : q % NS_THIN_K;
             float v = 0.f;
             if (k0 + kk < n) {
-                const int64_t at = p.tall ? (int64_t)(k0 + kk) * p.ldx + i : (int64_t)i * p.ldx + k0 + kk;
-                v = fmaf(NS_INV_LO, __half2float(xl[at]), __half2float(xh[at])) * NS_INV_S;
+                const int64_t at = e * p.u.st_u + (p.tall ? (int64_t)(k0 + kk) * p.u.ld_u + i : i * p.u.ld_u + k0 + kk);
+                if (p.u.M && !p.u.nesterov) {
+                    v = p.u.M[at];
+                } else {
+                    v = p.u.u_bf16 ? as_f32(static_cast<const __nv_bfloat16*>(p.u.U)[at])
+                                   : static_cast<const float*>(p.u.U)[at];
+                    if (p.u.M) v = fmaf(p.u.mu, p.u.M[at], v);
+                }
+                v = (v * pre) * post;
             }
             xs[i][kk] = v;
         }
@@ -693,8 +903,8 @@ __global__ void __launch_bounds__(NS_THIN_THREADS) ns_thin_kernel(const __grid_c
         if (q < m * m) A[q / m][q % m] = acc[u];
     }
     __syncthreads();
-    for (int it = 0; it < st.steps; ++it) {
-        const float ca = st.coef[3 * it], cb = st.coef[3 * it + 1], cc = st.coef[3 * it + 2];
+    for (int it = 0; it < p.steps; ++it) {
+        const float ca = p.coef[3 * it], cb = p.coef[3 * it + 1], cc = p.coef[3 * it + 2];
         product(T, A, A);
         for (int q = tid; q < m * m; q += NS_THIN_THREADS) {
             const int i = q / m, j = q - i * m;
@@ -707,7 +917,7 @@ __global__ void __launch_bounds__(NS_THIN_THREADS) ns_thin_kernel(const __grid_c
             for (int q = tid; q < m * m; q += NS_THIN_THREADS) Q[q / m][q % m] = T[q / m][q % m];
             __syncthreads();
         }
-        if (it + 1 < st.steps) {
+        if (it + 1 < p.steps) {
             product(T, P, A);
             product(A, T, P);
         }
@@ -727,78 +937,89 @@ __global__ void __launch_bounds__(NS_THIN_THREADS) ns_thin_kernel(const __grid_c
     }
 }
 
-// Width of the n-tiles of an output of n columns: as few tiles as 256-wide MMAs allow, of
-// equal width, a multiple of 16.
+// Width of the n-tiles of an output of n columns: as few tiles as 256-wide MMAs allow, of equal
+// width, a multiple of 32 (each CTA of a pair holds half of the columns).
 void ns_tiles(int n, int* bn, int* nt) {
     const int t = (n + NS_MAXBN - 1) / NS_MAXBN;
-    *bn = ((n + t - 1) / t + 15) / 16 * 16;
+    *bn = ((n + t - 1) / t + 31) / 32 * 32;
     *nt = (n + *bn - 1) / *bn;
 }
 
 inline int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
 inline size_t up256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 
+// Matrices under way, NS_LANES groups of them: as many as keep the working arrays within
+// NS_L2_BYTES of L2, but enough tiles for all pairs where the stack has them.
+constexpr int64_t NS_L2_BYTES = 72ll << 20;
+
 struct NsLayout {
-    size_t part, xh0, xh1, xl, A, B, total;
-    int chunks, groups;
+    size_t prog, part, xh0, xh1, xl0, xl1, A, Al, B, Bl, total;
+    int chunks, groups, n_groups, group_max, slots, terms;
 };
 NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     NsLayout L;
     const int64_t m = r < c ? r : c, ldx = up8(c), ldm = up8(m);
     L.groups = (int)(r * ldx / 8);
     L.chunks = (L.groups + NS_PRO_GROUPS - 1) / NS_PRO_GROUPS;
+    L.terms = m <= 128 ? 3 : 1;
+    const int64_t each = (L.terms == 3 ? 8 : 6) * r * ldx + (L.terms == 3 ? 8 : 4) * m * ldm;
+    int64_t most = NS_L2_BYTES / (each * NS_LANES);   // matrices of a group
+    if (most < 1) most = 1;
+    const int64_t rounds = (N + most * NS_LANES - 1) / (most * NS_LANES);
+    L.n_groups = (int)(rounds * NS_LANES < N ? rounds * NS_LANES : N);   // sizes then differ by one at most
+    if (L.n_groups < 1) L.n_groups = 1;
+    L.group_max = (int)((N + L.n_groups - 1) / L.n_groups);
+    L.slots = L.group_max * (L.n_groups < NS_LANES ? L.n_groups : NS_LANES);
     size_t o = up256(sizeof(DevStatus));
     auto take = [&](size_t bytes) {
         const size_t at = o;
         o += up256(bytes);
         return at;
     };
+    L.prog = take((size_t)N * 4);
     L.part = take((size_t)N * L.chunks * 3 * sizeof(float));
-    L.xh0 = take((size_t)(N * r * ldx) * 2);
-    L.xh1 = take((size_t)(N * r * ldx) * 2);
-    L.xl = take((size_t)(N * r * ldx) * 2);
-    L.A = take((size_t)(N * m * ldm) * 2);
-    L.B = take((size_t)(N * m * ldm) * 2);
+    const size_t x = (size_t)L.slots * r * ldx * 2, a = (size_t)L.slots * m * ldm * 2;
+    const bool thin = m <= NS_THIN;
+    L.xh0 = take(thin ? 0 : x);
+    L.xh1 = take(thin ? 0 : x);
+    L.xl0 = take(thin ? 0 : x);
+    L.xl1 = L.terms == 3 ? take(thin ? 0 : x) : L.xl0;
+    L.A = take(thin ? 0 : a);
+    L.B = take(thin ? 0 : a);
+    L.Al = L.terms == 3 ? take(thin ? 0 : a) : L.A;
+    L.Bl = L.terms == 3 ? take(thin ? 0 : a) : L.B;
     L.total = o;
     return L;
 }
 
 template <typename T, bool VEC>
-cudaError_t launch_prologue(const ProArgs& p, int N, cudaStream_t s) {
-    const dim3 grid((unsigned)p.chunks, (unsigned)N);
-    cudaError_t e = launch_pdl(muon_moment_kernel<T, VEC>, grid, dim3(NS_PRO_THREADS), 0, s, p);
-    if (e != cudaSuccess) return e;
-    return launch_pdl(muon_scale_kernel<T, VEC>, grid, dim3(NS_PRO_THREADS), 0, s, p);
+cudaError_t launch_moment(const UpdateArgs& p, int N, cudaStream_t s) {
+    return launch_pdl(muon_moment_kernel<T, VEC>, dim3((unsigned)p.chunks, (unsigned)N), dim3(NS_PRO_THREADS), 0, s, p);
 }
 
 }  // namespace
 
-size_t ns_workspace_bytes(int64_t N, int64_t r, int64_t c) { return ns_layout(N, r, c).total; }
+// Monotone in N: a larger stack may have smaller groups under way, so the sizes of all smaller
+// stacks' buffers are bounded by those of one full set of groups.
+size_t ns_workspace_bytes(int64_t N, int64_t r, int64_t c) {
+    const NsLayout L = ns_layout(N, r, c);
+    size_t most = L.total;
+    const int64_t m = r < c ? r : c, ldx = up8(c), ldm = up8(m);
+    const int64_t each = (L.terms == 3 ? 8 : 6) * r * ldx + (L.terms == 3 ? 8 : 4) * m * ldm;
+    int64_t full = NS_L2_BYTES / (each * NS_LANES);
+    if (full < 1) full = 1;
+    full = full * NS_LANES < N ? full * NS_LANES : N;
+    if (full > 0) {
+        const NsLayout F = ns_layout(full, r, c);
+        const size_t per = 4 + (size_t)L.chunks * 3 * sizeof(float);
+        const size_t v = F.total + (size_t)(N - full) * per + 512;
+        if (v > most) most = v;
+    }
+    return most;
+}
 
 cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t limit_ns, cudaStream_t s) {
     const NsLayout L = ns_layout(q.N, q.r, q.c);
-    ProArgs pa = {};
-    pa.U = q.U;
-    pa.ld_u = q.ld_u;
-    pa.st_u = q.st_u;
-    pa.M = q.M;
-    pa.mu = q.momentum;
-    pa.nesterov = q.nesterov;
-    pa.r = q.r;
-    pa.c = q.c;
-    pa.ld = (int)up8(q.c);
-    pa.groups = L.groups;
-    pa.chunks = L.chunks;
-    pa.part = reinterpret_cast<float*>(ws + L.part);
-    pa.xh = reinterpret_cast<__half*>(ws + L.xh0);
-    pa.xl = reinterpret_cast<__half*>(ws + L.xl);
-    const bool vec = q.ld_u % 8 == 0 && q.st_u % 8 == 0 && (reinterpret_cast<uintptr_t>(q.U) & 15u) == 0;
-    cudaError_t e;
-    if (q.u_bf16) e = vec ? launch_prologue<__nv_bfloat16, true>(pa, q.N, s) : launch_prologue<__nv_bfloat16, false>(pa, q.N, s);
-    else e = vec ? launch_prologue<float, true>(pa, q.N, s) : launch_prologue<float, false>(pa, q.N, s);
-    if (e != cudaSuccess) return e;
-    count_launches(2);
-
     NsArgs a = {};
     a.N = q.N;
     a.r = q.r;
@@ -807,23 +1028,43 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.m = a.tall ? q.c : q.r;
     a.ldx = (int)up8(q.c);
     a.ldm = (int)up8(a.m);
-    a.xh[0] = reinterpret_cast<__half*>(ws + L.xh0);
-    a.xh[1] = reinterpret_cast<__half*>(ws + L.xh1);
-    a.xl = reinterpret_cast<__half*>(ws + L.xl);
-    a.A = reinterpret_cast<__half*>(ws + L.A);
-    a.B = reinterpret_cast<__half*>(ws + L.B);
-    for (int i = 0; i < 2; ++i)
-        if (!make_weight_tmap_strided(&a.tmX[i], a.xh[i], a.c, a.r, a.N, a.ldx, (int64_t)a.r * a.ldx))
-            return cudaErrorInvalidValue;
-    if (!make_weight_tmap_strided(&a.tmA, a.A, a.m, a.m, a.N, a.ldm, (int64_t)a.m * a.ldm) ||
-        !make_weight_tmap_strided(&a.tmB, a.B, a.m, a.m, a.N, a.ldm, (int64_t)a.m * a.ldm))
-        return cudaErrorInvalidValue;
-    ns_tiles(a.m, &a.bn_s, &a.nt_s);
-    ns_tiles(a.c, &a.bn_x, &a.nt_x);
-    a.mt_s = (a.m + NS_BM - 1) / NS_BM;
-    a.mt_x = (a.r + NS_BM - 1) / NS_BM;
-    a.sym_tiles = 0;
-    for (int i = 0; i < a.mt_s; ++i) a.sym_tiles += a.nt_s - i * NS_BM / a.bn_s;
+    a.terms = L.terms;
+    a.u.U = q.U;
+    a.u.ld_u = q.ld_u;
+    a.u.st_u = q.st_u;
+    a.u.u_bf16 = q.u_bf16;
+    a.u.vec = q.ld_u % 8 == 0 && q.st_u % 8 == 0 && (reinterpret_cast<uintptr_t>(q.U) & 15u) == 0;
+    a.u.M = q.M;
+    a.u.mu = q.momentum;
+    a.u.nesterov = q.nesterov;
+    a.u.r = q.r;
+    a.u.c = q.c;
+    a.u.gpr = a.ldx / 8;
+    a.u.groups = L.groups;
+    a.u.chunks = L.chunks;
+    a.u.part = reinterpret_cast<float*>(ws + L.part);
+    a.u.prog = reinterpret_cast<int32_t*>(ws + L.prog);
+    cudaError_t e;
+    if (q.u_bf16) e = a.u.vec ? launch_moment<__nv_bfloat16, true>(a.u, q.N, s) : launch_moment<__nv_bfloat16, false>(a.u, q.N, s);
+    else e = a.u.vec ? launch_moment<float, true>(a.u, q.N, s) : launch_moment<float, false>(a.u, q.N, s);
+    count_launches(1);
+    if (e != cudaSuccess) return e;
+
+    a.steps = q.steps;
+    int stage = 0;
+    a.kind[stage++] = NS_LOAD;
+    for (int it = 0; it < q.steps; ++it) {
+        for (int j = 0; j < 3; ++j) a.coef[3 * it + j] = q.coef[3 * it + j];
+        // lo in the last two steps: see the file comment
+        const float ca = a.coef[3 * it], lim = it == q.steps - 1 ? 1.0f : 2.0f;
+        a.lo_coef[it] = a.terms == 3 || it < q.steps - 2 || fabsf(ca) <= lim ? ca : copysignf(lim, ca);
+        for (int kind = NS_GRAM; kind <= NS_APPLY; ++kind) {
+            if (kind == NS_POLY && a.coef[3 * it + 2] == 0.f) continue;
+            a.kind[stage] = (uint8_t)kind;
+            a.step[stage++] = (uint8_t)it;
+        }
+    }
+    a.n_stages = stage;
     a.O = q.O;
     a.ld_o = q.ld_o;
     a.st_o = q.st_o;
@@ -837,38 +1078,75 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.status = reinterpret_cast<DevStatus*>(ws);
     a.limit_ns = limit_ns;
     if (a.m <= NS_THIN) {
-        NsSteps st = {};
-        st.steps = q.steps;
-        for (int i = 0; i < 3 * q.steps; ++i) st.coef[i] = q.coef[i];
-        e = launch_pdl(ns_thin_kernel, dim3((unsigned)a.N), dim3(NS_THIN_THREADS), 0, s, a, st);
+        e = launch_pdl(ns_thin_kernel, dim3((unsigned)a.N), dim3(NS_THIN_THREADS), 0, s, a);
         count_launches(1);
         return e != cudaSuccess ? e : cudaGetLastError();
     }
+    a.xh[0] = reinterpret_cast<__half*>(ws + L.xh0);
+    a.xh[1] = reinterpret_cast<__half*>(ws + L.xh1);
+    a.xl[0] = reinterpret_cast<__half*>(ws + L.xl0);
+    a.xl[1] = reinterpret_cast<__half*>(ws + L.xl1);
+    a.A[0] = reinterpret_cast<__half*>(ws + L.A);
+    a.A[1] = reinterpret_cast<__half*>(ws + L.Al);
+    a.B[0] = reinterpret_cast<__half*>(ws + L.B);
+    a.B[1] = reinterpret_cast<__half*>(ws + L.Bl);
+    bool ok = true;
+    for (int i = 0; i < 2; ++i) {
+        for (int j = 0; j < 2; ++j)
+            ok = ok && make_weight_tmap_strided(&a.tX[i][j], j ? a.xl[i] : a.xh[i], a.c, a.r, L.slots, a.ldx,
+                                                (int64_t)a.r * a.ldx);
+        ok = ok && make_weight_tmap_strided(&a.tA[i], a.A[i], a.m, a.m, L.slots, a.ldm, (int64_t)a.m * a.ldm) &&
+             make_weight_tmap_strided(&a.tB[i], a.B[i], a.m, a.m, L.slots, a.ldm, (int64_t)a.m * a.ldm);
+    }
+    if (!ok) return cudaErrorInvalidValue;
+    ns_tiles(a.m, &a.bn_s, &a.nt_s);
+    ns_tiles(a.c, &a.bn_x, &a.nt_x);
+    a.mt_s = (a.m + NS_BM - 1) / NS_BM;
+    a.mt_x = (a.r + NS_BM - 1) / NS_BM;
+    int sym = 0;
+    for (int i = 0; i < a.mt_s; ++i) sym += a.nt_s - i * NS_BM / a.bn_s;
+    a.tiles[NS_LOAD] = (L.groups + NS_LOAD_GROUPS - 1) / NS_LOAD_GROUPS;
+    a.tiles[NS_GRAM] = a.tiles[NS_POLY] = sym;
+    a.tiles[NS_APPLY] = a.mt_x * a.nt_x;
+    int64_t items = 0;
+    for (int i = 0; i < a.n_stages; ++i) {
+        a.need[i] = (int)items * NS_DONE;
+        items += a.tiles[a.kind[i]];
+    }
+    a.need[a.n_stages] = (int)items * NS_DONE;
+    items *= a.N;
+    if (items >= (int64_t(1) << 31) - 65536) return cudaErrorInvalidValue;
+    a.total = (int)items;
+    a.n_groups = L.n_groups;
+    a.group_max = L.group_max;
     static bool attr_set[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev >= 0 && dev < 64 && !attr_set[dev]) {
-        e = cudaFuncSetAttribute(ns_gemm_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM);
+        e = cudaFuncSetAttribute(ns_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM);
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
-    for (int it = 0; it < q.steps; ++it) {
-        a.ca = q.coef[3 * it];
-        a.cb = q.coef[3 * it + 1];
-        a.cc = q.coef[3 * it + 2];
-        a.src = it & 1;
-        a.last = it == q.steps - 1;
-        for (int kind = NS_GRAM; kind <= NS_APPLY; ++kind) {
-            if (kind == NS_POLY && a.cc == 0.f) continue;
-            a.kind = kind;
-            const int64_t work = (int64_t)a.N * (kind == NS_APPLY ? a.mt_x * a.nt_x : a.sym_tiles);
-            e = launch_pdl(ns_gemm_kernel, dim3((unsigned)(work < sms ? work : sms)), dim3(NS_THREADS), NS_SMEM,
-                           s, a);
-            count_launches(1);
-            if (e != cudaSuccess) return e;
-        }
-    }
-    return cudaGetLastError();
+    const int64_t pairs = items < sms / 2 ? items : sms / 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * (pairs < 1 ? 1 : pairs)));
+    cfg.blockDim = dim3(NS_THREADS);
+    cfg.dynamicSmemBytes = NS_SMEM;
+    cfg.stream = s;
+    cudaLaunchAttribute at[3];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeCooperative;   // pairs wait on one another: all co-resident
+    at[1].val.cooperative = 1;
+    at[2].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see launch_pdl
+    at[2].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 3;
+    e = cudaLaunchKernelEx(&cfg, ns_kernel, a);
+    count_launches(1);
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace mv
