@@ -10,15 +10,14 @@
 // Kernels
 //   muon_moment_kernel  one pass over the gradient: momentum update (M <- mu M + G) and, per
 //                       chunk, partial sums of squares of U.  Bound by memory.
-//   ns_kernel           everything else in one persistent launch: X0 from U and its norm, the
-//                       three products of every step on tcgen05 CTA pairs, and the output or the
-//                       weight update in the last product's epilogue.
+//   muon_scale_kernel   X0 in the working format from U and its norm.  Bound by memory.
+//   ns_kernel           the three products of every step on tcgen05 CTA pairs in one persistent
+//                       launch, with the output or the weight update in the last one's epilogue.
 //   ns_thin_kernel      all of that for matrices whose smaller side is at most 32, in fp32.
 //
-// ns_kernel.  Work items are (matrix, stage, tile): stage 0 loads X0, then Gram, polynomial and
-// apply stages of each step.  Only a few matrices are under way at a time, in buffers that are
-// used again for the next ones, so that everything between U and the result stays in L2 (DRAM
-// then sees U, M and the weights once; with all matrices under way at once the apply stage alone
+// ns_kernel.  Work items are (matrix, stage, tile): a Gram, a polynomial and an apply stage for
+// each step.  Only a few matrices are under way at a time, in buffers that are
+// used again for the next ones, so that everything between X0 and the result stays in L2 (with all matrices under way at once the apply stage alone
 // moved 1.4 GB a step and took 755 us of a 1000 us step on 256 x 416 x 1664).  The matrices under
 // way form NS_LANES groups that are one stage apart; in each slot of the schedule every group
 // advances by a stage, so that a tile's inputs were finished about a slot of other tiles earlier
@@ -240,41 +239,67 @@ __device__ __forceinline__ void update8(const UpdateArgs& u, int e, int row, int
     }
 }
 
+// X0 = U / |U| in the working format.
+__global__ void __launch_bounds__(NS_PRO_THREADS) muon_scale_kernel(const __grid_constant__ UpdateArgs u, __half* xh,
+                                                                    __half* xl) {
+    pdl_wait();
+    const int e = blockIdx.y;
+    float pre, post;
+    norm_scales(u, e, pre, post);
+    post *= NS_S;
+    const int g0 = blockIdx.x * NS_PRO_GROUPS, g1 = min(g0 + NS_PRO_GROUPS, u.groups);
+    const int64_t base = (int64_t)e * u.groups * 8;
+#pragma unroll 2
+    for (int g = g0 + (int)threadIdx.x; g < g1; g += NS_PRO_THREADS) {
+        const int row = g / u.gpr, col = (g - row * u.gpr) * 8;
+        float v[8];
+        update8(u, e, row, col, u.c - col, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (v[i] * pre) * post;
+        uint4 hi, lo;
+        split8(v, hi, lo);
+        *reinterpret_cast<uint4*>(xh + base + (int64_t)g * 8) = hi;
+        *reinterpret_cast<uint4*>(xl + base + (int64_t)g * 8) = lo;
+    }
+}
+
 // ------------------------------------------------------------------ products
 
 constexpr int NS_BM = 256;            // output rows per tile: a CTA pair, 128 rows (TMEM lanes) each
 constexpr int NS_HALF = 128;
 constexpr int NS_MAXBN = 256;         // output columns per tile at most (one tcgen05.mma)
 constexpr int NS_BK = 64;             // K per ring stage: one 128-byte swizzle row of fp16
-constexpr int NS_STAGES = 6;
+constexpr int NS_STAGES = 5;
 constexpr int NS_BOX = 64 * NS_BK * 2;                     // bytes of one 64 x 64 TMA box
 constexpr int NS_STAGE_BYTES = (NS_HALF + NS_MAXBN / 2) / 64 * NS_BOX;   // a CTA's A rows and half of B
-constexpr int NS_EPI_WARPS = 8;       // two per TMEM lane quadrant, alternate 32-column chunks
+constexpr int NS_EPI_WARPS = 8;       // two per TMEM lane quadrant, 16-column chunks in turn
+constexpr int NS_CH = NS_EPI_WARPS / 4;   // a warp takes every NS_CH-th chunk
 constexpr int NS_WARP_LOAD = NS_EPI_WARPS;
 constexpr int NS_WARP_MMA = NS_EPI_WARPS + 1;
 constexpr int NS_THREADS = (NS_EPI_WARPS + 2) * 32;
-constexpr int NS_STG_LD = 36;         // floats per staged row (32 values, padded)
-constexpr int NS_STG_ROWS = 16;       // rows a warp stages at a time
+constexpr int NS_STG_LD = 20;         // floats per staged row (16 values, padded)
+constexpr int NS_STG_ROWS = 32;       // a warp's rows
 constexpr int NS_STG_BYTES = NS_EPI_WARPS * NS_STG_ROWS * NS_STG_LD * 4;
 constexpr int NS_SMEM = NS_STAGES * NS_STAGE_BYTES + NS_STG_BYTES + 1024 + 256;
 static_assert(NS_SMEM <= 232448, "shared memory of one CTA");
 
 constexpr int NS_LANES = 3;           // groups of matrices under way, a stage apart
-constexpr int NS_LOAD_GROUPS = 2048;  // groups of 8 values per load item (half per CTA of the pair)
-constexpr int NS_MAX_STAGES = 1 + 3 * NS_MAX_STEPS;
+constexpr int NS_MAX_STAGES = 3 * NS_MAX_STEPS;
 constexpr int NS_DONE = 2 * NS_EPI_WARPS;   // a finished item's contribution to its matrix's counter
 
-enum NsKind : int { NS_LOAD = 0, NS_GRAM = 1, NS_POLY = 2, NS_APPLY = 3 };
+enum NsKind : int { NS_GRAM = 0, NS_POLY = 1, NS_APPLY = 2 };
 
 struct NsArgs {
-    CUtensorMap tX[2][2], tA[2], tB[2];   // [buffer][hi, lo]; 3-D maps {inner, rows, slots}, boxes 64 x 64
+    CUtensorMap tX[3][2], tA[2], tB[2];   // [X0, buffer 0, 1][hi, lo]; 3-D maps {inner, rows, matrices
+                                          //   (X0) or slots}, boxes 64 x 64
     UpdateArgs u;
-    __half *xh[2], *xl[2];             // X, ping-pong [slots][r][ldx] (lo in place with one term)
+    __half *xh[3], *xl[3];             // X0 [N][r][ldx]; X, ping-pong [slots][r][ldx] (lo in place with one term)
     __half *A[2], *B[2];               // hi, lo (lo with three terms only) [slots][m][ldm]
     int N, r, c, m, ldx, ldm, tall, terms;
     int bn_s, nt_s, mt_s, bn_x, nt_x, mt_x;   // tiles of m x m and of r x c outputs
-    int tiles[4];                      // items of a matrix's stage, by kind
+    int tiles[3];                      // items of a matrix's stage, by kind
     int n_stages, n_groups, group_max; // stages of a matrix; groups of matrices; their largest size
+    int base_size, big_groups;         // the first big_groups of them hold base_size + 1, the others base_size
     int total;                         // items
     uint8_t kind[NS_MAX_STAGES], step[NS_MAX_STAGES];
     int need[NS_MAX_STAGES + 1];       // counter value at which a stage's inputs are complete
@@ -291,76 +316,84 @@ struct NsArgs {
     uint64_t limit_ns;
 };
 
-// Position of a role in the schedule: slot t holds items [base, base + count).
+// Position of a role in the schedule: the slot that holds items [base, base + count), with the
+// group and the stage of each lane (a stage below 0: the lane has not started) and the lane's
+// items.
 struct NsWalk {
-    int t, base, count;
+    int base, count;
+    int g[NS_LANES], stage[NS_LANES], n[NS_LANES];
 };
 struct NsItem {
     int e, buf, stage, kind, step, tile;
     int prev;                          // the matrix that used the buffers before, or -1
 };
 
-__device__ __forceinline__ int ns_first(const NsArgs& p, int g) {   // first matrix of group g
-    return (int)((int64_t)g * p.N / p.n_groups);
-}
-// Group and stage of lane l in slot t; false when it has none.
-__device__ __forceinline__ bool ns_lane(const NsArgs& p, int t, int l, int& g, int& stage) {
-    const int u = t - l;
-    if (u < 0) return false;
-    const int q = u / p.n_stages;
-    g = q * NS_LANES + l;
-    stage = u - q * p.n_stages;
-    return g < p.n_groups;
-}
-__device__ __forceinline__ int ns_slot_count(const NsArgs& p, int t) {
-    int n = 0;
+// Groups hold base_size matrices, the first big_groups of them one more.
+__device__ __forceinline__ int ns_first(const NsArgs& p, int g) { return g * p.base_size + min(g, p.big_groups); }
+__device__ __forceinline__ int ns_size(const NsArgs& p, int g) { return p.base_size + (g < p.big_groups ? 1 : 0); }
+
+__device__ __forceinline__ void ns_count(const NsArgs& p, NsWalk& w) {
+    w.count = 0;
 #pragma unroll
     for (int l = 0; l < NS_LANES; ++l) {
-        int g, st;
-        if (ns_lane(p, t, l, g, st)) n += (ns_first(p, g + 1) - ns_first(p, g)) * p.tiles[p.kind[st]];
+        w.n[l] = w.stage[l] >= 0 && w.g[l] < p.n_groups ? ns_size(p, w.g[l]) * p.tiles[p.kind[w.stage[l]]] : 0;
+        w.count += w.n[l];
     }
-    return n;
 }
-__device__ __forceinline__ NsWalk ns_walk_start(const NsArgs& p) { return {0, 0, ns_slot_count(p, 0)}; }
+__device__ __forceinline__ NsWalk ns_walk_start(const NsArgs& p) {
+    NsWalk w;
+    w.base = 0;
+#pragma unroll
+    for (int l = 0; l < NS_LANES; ++l) {
+        w.g[l] = l;
+        w.stage[l] = -l;
+    }
+    ns_count(p, w);
+    return w;
+}
 
 // Item `id` (ids only grow from call to call).
 __device__ __forceinline__ NsItem ns_item(const NsArgs& p, NsWalk& w, int id) {
     while (id >= w.base + w.count) {
         w.base += w.count;
-        w.count = ns_slot_count(p, ++w.t);
-    }
-    NsItem it = {};
-    int pos = id - w.base;
 #pragma unroll
-    for (int l = 0; l < NS_LANES; ++l) {
-        int g, st;
-        if (pos < 0 || !ns_lane(p, w.t, l, g, st)) continue;
-        const int first = ns_first(p, g), tiles = p.tiles[p.kind[st]], n = (ns_first(p, g + 1) - first) * tiles;
-        if (pos < n) {
-            const int i = pos / tiles;
-            it.e = first + i;
-            it.buf = l * p.group_max + i;
-            it.stage = st;
-            it.kind = p.kind[st];
-            it.step = p.step[st];
-            it.tile = pos - i * tiles;
-            it.prev = -1;   // sizes of groups differ by one: at most one group back lacks the place
-            for (int h = g - NS_LANES; h >= 0; h -= NS_LANES)
-                if (i < ns_first(p, h + 1) - ns_first(p, h)) {
-                    it.prev = ns_first(p, h) + i;
-                    break;
-                }
-            pos = -1;
-        } else {
-            pos -= n;
-        }
+        for (int l = 0; l < NS_LANES; ++l)
+            if (++w.stage[l] == p.n_stages) {
+                w.stage[l] = 0;
+                w.g[l] += NS_LANES;
+            }
+        ns_count(p, w);
     }
+    int pos = id - w.base, l = 0, g = w.g[0], stage = w.stage[0];
+#pragma unroll
+    for (int i = 1; i < NS_LANES; ++i)
+        if (l == i - 1 && pos >= w.n[i - 1]) {
+            pos -= w.n[i - 1];
+            l = i;
+            g = w.g[i];
+            stage = w.stage[i];
+        }
+    NsItem it;
+    it.stage = stage;
+    it.kind = p.kind[stage];
+    it.step = p.step[stage];
+    const int tiles = p.tiles[it.kind], i = pos / tiles;
+    it.tile = pos - i * tiles;
+    it.e = ns_first(p, g) + i;
+    it.buf = l * p.group_max + i;
+    it.prev = -1;   // the group before on this lane; it has the place, as earlier groups are not smaller
+    if (g >= NS_LANES) it.prev = ns_first(p, g - NS_LANES) + i;
     return it;
 }
+
+// Where step s reads X (0: X0), and where it writes it (1 or 2).
+__device__ __forceinline__ int ns_src(int s) { return s == 0 ? 0 : 2 - (s & 1); }
+__device__ __forceinline__ int ns_dst(int s) { return 1 + (s & 1); }
 
 struct NsTile {
     int m0, n0, bn, num_kb;            // num_kb: K blocks of one term
     const CUtensorMap *a[2], *b[2];    // operands, hi and lo
+    int za, zb;                        // their matrix or slot
     bool a_mn, b_mn;
 };
 
@@ -374,7 +407,7 @@ __device__ __forceinline__ int sym_first(const NsArgs& p, int i) { return i * NS
 //   r >  c:  Gram  X^T X both MN-major;  apply X B: both K-major (B is symmetric)
 __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
     NsTile t;
-    const int src = it.step & 1;
+    const int src = ns_src(it.step);
     int k = p.m;
     if (it.kind == NS_APPLY) {
         t.m0 = it.tile / p.nt_x * NS_BM;
@@ -382,6 +415,8 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
         t.bn = p.bn_x;
         t.a_mn = false;
         t.b_mn = !p.tall;
+        t.za = p.tall && src == 0 ? it.e : it.buf;
+        t.zb = !p.tall && src == 0 ? it.e : it.buf;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             t.a[i] = p.tall ? &p.tX[src][i] : &p.tB[i];
@@ -400,6 +435,7 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
         const bool gram = it.kind == NS_GRAM;
         if (gram) k = p.tall ? p.r : p.c;
         t.a_mn = t.b_mn = gram && p.tall;
+        t.za = t.zb = gram && src == 0 ? it.e : it.buf;
 #pragma unroll
         for (int j = 0; j < 2; ++j) t.a[j] = t.b[j] = gram ? &p.tX[src][j] : &p.tA[j];
     }
@@ -430,7 +466,8 @@ __device__ __forceinline__ bool ns_wait(const NsArgs& p, int e, int want, volati
     if (ld_acquire(c) >= want) return true;
     const uint64_t t0 = globaltimer_ns();
     for (uint32_t i = 1; ld_acquire(c) < want; ++i) {
-        if ((i & 63u) == 0u && (*abort_flag || globaltimer_ns() - t0 > p.limit_ns)) {
+        __nanosleep(100);
+        if ((i & 15u) == 0u && (*abort_flag || globaltimer_ns() - t0 > p.limit_ns)) {
             ns_abort(abort_flag, p.status, site, e);
             return false;
         }
@@ -447,9 +484,11 @@ __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abo
     NsWalk w = ns_walk_start(p);
     for (int id = sm.pair; id < p.total; id += sm.npairs) {
         const NsItem it = ns_item(p, w, id);
-        if (it.kind == NS_LOAD) continue;
         const NsTile t = ns_tile(p, it);
-        if (!ns_wait(p, it.e, p.need[it.stage], abort_flag, SITE_NS_WAIT_INPUT)) return;
+        // the matrix's earlier stages; before its first, the last user of its buffers
+        if (it.stage > 0 ? !ns_wait(p, it.e, p.need[it.stage], abort_flag, SITE_NS_WAIT_INPUT)
+                         : it.prev >= 0 && !ns_wait(p, it.prev, p.need[p.n_stages], abort_flag, SITE_NS_WAIT_BUFFER))
+            return;
         fence_proxy_async_all();   // the inputs were written by ordinary stores
         const int nbox = (t.bn / 2 + 63) / 64;
         const uint32_t bytes = 2u * (uint32_t)(2 + nbox) * NS_BOX;
@@ -467,10 +506,10 @@ __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abo
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
                     tma_load_3d_pair(dst + j * NS_BOX, ma, bar, t.a_mn ? mm + 64 * j : kk, t.a_mn ? kk : mm + 64 * j,
-                                     it.buf);
+                                     t.za);
                 for (int j = 0; j < nbox; ++j)
                     tma_load_3d_pair(dst + (2 + j) * NS_BOX, mb, bar, t.b_mn ? nn + 64 * j : kk,
-                                     t.b_mn ? kk : nn + 64 * j, it.buf);
+                                     t.b_mn ? kk : nn + 64 * j, t.zb);
                 if (++s == NS_STAGES) {
                     s = 0;
                     ph ^= 1u;
@@ -488,7 +527,6 @@ __device__ __forceinline__ void ns_mma(const NsArgs& p, const NsSmem& sm, uint32
     NsWalk w = ns_walk_start(p);
     for (int id = sm.pair; id < p.total; id += sm.npairs) {
         const NsItem it = ns_item(p, w, id);
-        if (it.kind == NS_LOAD) continue;
         const NsTile t = ns_tile(p, it);
         const uint32_t idesc = idesc_f16_f32(NS_BM, t.bn, t.a_mn, t.b_mn);
         const uint64_t ad0 = smem_desc_sw128(sm.ring, t.a_mn ? NS_BOX : 16, 1024);
@@ -546,217 +584,194 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float (&v)[8], float sc) {
                       pack_bf16x2(v[4] * sc, v[5] * sc), pack_bf16x2(v[6] * sc, v[7] * sc));
 }
 
-// X0 = U / |U| of a range of groups of matrix it.e, by the 8 epilogue warps.
-__device__ __forceinline__ void ns_load_x0(const NsArgs& p, const NsItem& it, uint32_t rank) {
-    float pre, post;
-    norm_scales(p.u, it.e, pre, post);
-    post *= NS_S;
-    constexpr int HALF = NS_LOAD_GROUPS / 2;
-    const int g0 = it.tile * NS_LOAD_GROUPS + (int)rank * HALF, g1 = min(g0 + HALF, p.u.groups);
-    const int64_t base = (int64_t)it.buf * p.r * p.ldx;
-#pragma unroll 2
-    for (int g = g0 + (int)threadIdx.x; g < g1; g += NS_EPI_WARPS * 32) {
-        const int row = g / p.u.gpr, col = (g - row * p.u.gpr) * 8;
-        float v[8];
-        update8(p.u, it.e, row, col, p.c - col, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (v[i] * pre) * post;
-        uint4 hi, lo;
-        split8(v, hi, lo);
-        *reinterpret_cast<uint4*>(p.xh[0] + base + (int64_t)g * 8) = hi;   // ldx = 8 gpr
-        *reinterpret_cast<uint4*>(p.xl[0] + base + (int64_t)g * 8) = lo;
-    }
-}
+enum NsMode : int { NS_M_GRAM, NS_M_POLY, NS_M_X, NS_M_O, NS_M_W };
 
-// Warp w reads TMEM lanes 32 (w % 4) .. of its CTA's 128 rows and the 32-column chunks w / 4,
-// w / 4 + 2, ... of a tile.  The accumulator rows pass a small per-warp buffer so that four
-// consecutive lanes hold 32 consecutive columns of a row and every global access of a warp covers
-// eight whole 64-byte (fp16) pieces; what a chunk reads from L2 is loaded a chunk ahead.
-__device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, volatile int* abort_flag) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int quad = warp & 3, half = warp >> 2;
-    float* stg = sm.stg + warp * NS_STG_ROWS * NS_STG_LD;
-    const uint32_t tempty_leader = peer_addr(sm.tempty, 0);
-    const int lr = lane >> 2, lc = (lane & 3) * 8;   // a lane's row (of 8) and first column after staging
-    int n = 0;
-    NsWalk w = ns_walk_start(p);
-    for (int id = sm.pair; id < p.total; id += sm.npairs) {
-        const NsItem it = ns_item(p, w, id);
-        if (it.kind == NS_LOAD) {
-            int ok = 1;   // the buffers' last user is done with them
-            if (lane == 0 && it.prev >= 0) ok = ns_wait(p, it.prev, p.need[p.n_stages], abort_flag, SITE_NS_WAIT_BUFFER);
-            if (!__shfl_sync(0xffffffffu, ok, 0)) return;
-            ns_load_x0(p, it, sm.rank);
-        } else {
-            const NsTile t = ns_tile(p, it);
-            const bool apply = it.kind == NS_APPLY, gram = it.kind == NS_GRAM;
-            const bool last = apply && it.step == p.steps - 1;
-            const int rows = apply ? p.r : p.m, cols = apply ? p.c : p.m;
-            const float ca = p.coef[3 * it.step], cb = p.coef[3 * it.step + 1], cc = p.coef[3 * it.step + 2];
-            const int src = it.step & 1;
-            const int row0 = t.m0 + (int)sm.rank * NS_HALF + quad * 32;
-            const int ld = apply ? p.ldx : p.ldm;
-            const int64_t base = (int64_t)it.buf * rows * ld;
-            // what the chunk reads: A (polynomial) or X (apply), hi and lo
-            const __half* ph = apply ? p.xh[src] : gram ? nullptr : p.A[0];
-            const __half* pl = apply ? p.xl[src] : (gram || p.terms == 1) ? nullptr : p.A[1];
-            const int nchunk = (t.bn + 31) / 32;
-            uint4 nh[4], nl[4];
-            auto fetch = [&](int ch) {
+// One tile of one warp: TMEM lanes 32 (w % 4) .. of the CTA's 128 rows, the 16-column chunks
+// w / 4, w / 4 + 2, ...  The accumulator rows pass a per-warp buffer so that two consecutive lanes
+// hold 16 consecutive columns of a row and every global access of a warp covers sixteen whole
+// 32-byte (fp16) sectors; what a chunk reads from L2 is loaded a chunk ahead.  One instance per
+// MODE, so that each loop holds only the code that its tiles run:
+//   GRAM: A = D (a step with c = 0 has no polynomial stage: B = b D);  POLY: B = b A + c D;
+//   X: X = a X + D in the working format;  O, W: the same of the last step, to the outputs.
+template <int MODE>
+__device__ __forceinline__ bool ns_epi_tile(const NsArgs& p, const NsSmem& sm, const NsItem& it, const NsTile& t,
+                                            float* stg, uint32_t tmem, int n, volatile int* abort_flag) {
+    constexpr bool APPLY = MODE >= NS_M_X;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = warp & 3, first = warp >> 2;
+    const int lr = lane >> 1, lc = (lane & 1) * 8;   // a lane's row (of 16) and first column after staging
+    const int rows = APPLY ? p.r : p.m, cols = APPLY ? p.c : p.m, ld = APPLY ? p.ldx : p.ldm;
+    const int col_end = min(cols, t.n0 + t.bn), nchunk = t.bn / 16;
+    const int row0 = t.m0 + (int)sm.rank * NS_HALF + quad * 32;
+    const int src = ns_src(it.step), dst = ns_dst(it.step), acc = n & 1;
+    const int64_t mat = (int64_t)it.buf * rows * ld, lane_at = (int64_t)(row0 + lr) * ld + t.n0 + lc;
+    const int rows_left = rows - row0 - lr;          // row 16 i + lr exists when 16 i < rows_left
+    const int64_t in_at = (APPLY && src == 0 ? (int64_t)it.e * rows * ld : mat) + lane_at;
+    const __half* in_h = (APPLY ? p.xh[src] : p.A[0]) + in_at;
+    const __half* in_l = (APPLY ? p.xl[src] : p.A[1]) + in_at;
+    const bool lo_in = APPLY || p.terms == 3;
+    const bool to_b = MODE == NS_M_POLY || p.coef[3 * it.step + 2] == 0.f;
+    __half* out_h = (APPLY ? p.xh[dst] : to_b ? p.B[0] : p.A[0]) + mat;
+    __half* out_l = (APPLY ? p.xl[dst] : to_b ? p.B[1] : p.A[1]) + mat;
+    uint4 nh[2], nl[2];
+    auto fetch = [&](int ch, int i) {
+        nh[i] = nl[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (t.n0 + ch * 16 + lc < col_end && 16 * i < rows_left) {
+            const int64_t at = (int64_t)(16 * i) * ld + ch * 16;
+            nh[i] = __ldcg(reinterpret_cast<const uint4*>(in_h + at));
+            if (lo_in) nl[i] = __ldcg(reinterpret_cast<const uint4*>(in_l + at));
+        }
+    };
+    // What the tile reads was written before its products could start.  Usually that is so already
+    // and the first loads go out before the accumulator is complete; no polling here (sixteen
+    // warps of every CTA on one counter held up its writers: 9 us a tile).
+    auto ready = [&]() {
+        int ok = 0;
+        if (lane == 0) ok = ld_acquire(p.u.prog + it.e) >= p.need[it.stage];
+        return __shfl_sync(0xffffffffu, ok, 0) != 0;
+    };
+    const bool early = MODE != NS_M_GRAM && first < nchunk && ready();
+    if (early) {
+        fetch(first, 0);
+        fetch(first, 1);
+    }
+    if (!mbar_wait(sm.tfull + 8 * acc, (uint32_t)(n >> 1) & 1u, p.limit_ns, abort_flag)) {
+        ns_abort(abort_flag, p.status, SITE_NS_WAIT_TFULL, it.e);
+        return false;
+    }
+    tc_fence_after();
+    if (MODE != NS_M_GRAM && first < nchunk && !early) {
+        ready();   // (it is: orders the reads)
+        fetch(first, 0);
+        fetch(first, 1);
+    }
+    const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * NS_MAXBN;
+    const uint32_t tempty = peer_addr(sm.tempty, 0) + 8 * acc;
+    if (first >= nchunk) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive_remote(tempty);
+    }
+    // mirror images (symmetric outputs): needed where a column lies past the row's tile column
+    const bool mirror = !APPLY && (row0 / p.bn_s + 1) * p.bn_s <= (col_end - 1) / NS_BM * NS_BM;
+#pragma unroll 1
+    for (int ch = first; ch < nchunk; ch += NS_CH) {
+        uint32_t v[16];
+        tmem_ld_32x32b_x16(tbase + ch * 16, v);
+        tmem_wait_ld();
+        if (ch + NS_CH >= nchunk) {   // this warp's last read of the accumulator
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(tempty);
+        }
+        float4* o = reinterpret_cast<float4*>(stg + lane * NS_STG_LD);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = row0 + 8 * i + lr, off = ch * 32 + lc, col = t.n0 + off;
-                    nh[i] = nl[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (ph && row < rows && off < t.bn && col < cols) {
-                        const int64_t at = base + (int64_t)row * ld + col;
-                        nh[i] = __ldcg(reinterpret_cast<const uint4*>(ph + at));
-                        if (pl) nl[i] = __ldcg(reinterpret_cast<const uint4*>(pl + at));
-                    }
+        for (int i = 0; i < 4; ++i)
+            o[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
+                               __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+        __syncwarp();
+        const int col = t.n0 + ch * 16 + lc;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float4* cell = reinterpret_cast<float4*>(stg + (16 * i + lr) * NS_STG_LD + lc);
+            const float4 d0 = cell[0], d1 = cell[1];
+            float x[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
+            if (MODE == NS_M_GRAM) {
+                const float sc = to_b ? p.coef[3 * it.step + 1] * NS_INV_S : NS_INV_S;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] *= sc;
+            } else {
+                float h[8];
+                unpack_half8(nh[i], h);
+                const float fd = APPLY ? NS_INV_S : p.coef[3 * it.step + 2] * NS_INV_S;
+                const float fh = p.coef[3 * it.step + (APPLY ? 0 : 1)];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = fmaf(fd, x[j], fh * h[j]);
+                if (lo_in) {
+                    const float fl = APPLY ? p.lo_coef[it.step] : fh;
+                    unpack_half8(nl[i], h);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = fmaf(fl, h[j], x[j]);
                 }
-            };
-            if (ph) {
-                int ok = 1;
-                if (lane == 0) ok = ns_wait(p, it.e, p.need[it.stage], abort_flag, SITE_NS_WAIT_INPUT);
-                if (!__shfl_sync(0xffffffffu, ok, 0)) return;
+                if (ch + NS_CH < nchunk) fetch(ch + 4, i);
             }
-            if (half < nchunk) fetch(half);
-            const int acc = n & 1;
-            if (!mbar_wait(sm.tfull + 8 * acc, (uint32_t)(n >> 1) & 1u, p.limit_ns, abort_flag)) {
-                ns_abort(abort_flag, p.status, SITE_NS_WAIT_TFULL, id);
-                return;
-            }
-            ++n;
-            tc_fence_after();
-            const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * NS_MAXBN;
-            if (half >= nchunk) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_remote(tempty_leader + 8 * acc);
-            }
-            for (int ch = half; ch < nchunk; ch += 2) {
-                uint32_t v[32];
-                tmem_ld_32x32b_x32(tbase + ch * 32, v);
-                tmem_wait_ld();
-                if (ch + 2 >= nchunk) {   // this warp's last read of the accumulator
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_remote(tempty_leader + 8 * acc);
+            const bool in = col < col_end && 16 * i < rows_left;
+            if (MODE == NS_M_GRAM || MODE == NS_M_POLY || MODE == NS_M_X) {
+                uint4 hi, lo;
+                split8(x, hi, lo);
+                if (in) {
+                    const int64_t at = lane_at + (int64_t)(16 * i) * ld + ch * 16;
+                    *reinterpret_cast<uint4*>(out_h + at) = hi;
+                    if (lo_in) *reinterpret_cast<uint4*>(out_l + at) = lo;
                 }
-                uint4 xh[4], xl[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    xh[i] = nh[i];
-                    xl[i] = nl[i];
+                if (mirror) {
+                    cell[0] = make_float4(x[0], x[1], x[2], x[3]);
+                    cell[1] = make_float4(x[4], x[5], x[6], x[7]);
                 }
-                if (ch + 2 < nchunk) fetch(ch + 2);
+            } else if (in) {
+                const int nc = p.c - col, row = row0 + 16 * i + lr;   // nc: columns of this group that exist
+                if (MODE == NS_M_O) {
+                    __nv_bfloat16* out = p.O + it.e * p.st_o + row * p.ld_o + col;
+                    if (p.vec_o && nc >= 8) {
+                        *reinterpret_cast<uint4*>(out) = pack_bf16x8(x, NS_INV_S);
+                    } else {
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    if ((lane >> 4) == hh) {
-                        float4* o = reinterpret_cast<float4*>(stg + (lane & 15) * NS_STG_LD);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            o[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
-                                               __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+                        for (int j = 0; j < 8; ++j)
+                            if (j < nc) out[j] = __float2bfloat16_rn(x[j] * NS_INV_S);
                     }
-                    __syncwarp();
+                } else {
+                    const int64_t wat = it.e * p.st_w + row * p.ld_w + col;
+                    const float rate = p.rate * NS_INV_S;
+                    float wv[8];
+                    load8<float, true>(p.W + wat, nc, wv);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int row = row0 + hh * 16 + 8 * i + lr, off = ch * 32 + lc, col = t.n0 + off;
-                        float4* cell = reinterpret_cast<float4*>(stg + (8 * i + lr) * NS_STG_LD + lc);
-                        const float4 d0 = cell[0], d1 = cell[1];
-                        float d[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w}, x[8], y[8];
-                        unpack_half8(xh[2 * hh + i], x);
-                        unpack_half8(xl[2 * hh + i], y);
-                        const bool in = row < rows && off < t.bn && col < cols;
-                        const int64_t at = base + (int64_t)row * ld + col;
-                        if (apply) {
+                    for (int j = 0; j < 8; ++j) wv[j] = fmaf(-rate, x[j], p.decay * wv[j]);
+                    store8<true>(p.W + wat, nc, wv);
+                    if (p.Wb && nc >= 8) *reinterpret_cast<uint4*>(p.Wb + wat) = pack_bf16x8(wv, 1.0f);
+                    else if (p.Wb) {
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                x[j] = fmaf(NS_INV_S, d[j], fmaf(ca, x[j], p.lo_coef[it.step] * y[j]));
-                            if (!last) {
-                                uint4 hi, lo;
-                                split8(x, hi, lo);
-                                if (in) {
-                                    *reinterpret_cast<uint4*>(p.xh[src ^ 1] + at) = hi;
-                                    *reinterpret_cast<uint4*>(p.xl[src ^ 1] + at) = lo;
-                                }
-                            } else if (in) {
-                                const int nc = p.c - col;   // columns of this group that exist
-                                if (p.O) {
-                                    __nv_bfloat16* o = p.O + it.e * p.st_o + row * p.ld_o + col;
-                                    if (p.vec_o && nc >= 8) {
-                                        *reinterpret_cast<uint4*>(o) = pack_bf16x8(x, NS_INV_S);
-                                    } else {
-#pragma unroll
-                                        for (int j = 0; j < 8; ++j)
-                                            if (j < nc) o[j] = __float2bfloat16_rn(x[j] * NS_INV_S);
-                                    }
-                                } else {
-                                    const int64_t wat = it.e * p.st_w + row * p.ld_w + col;
-                                    const float rate = p.rate * NS_INV_S;
-                                    load8<float, true>(p.W + wat, nc, y);
-#pragma unroll
-                                    for (int j = 0; j < 8; ++j) y[j] = fmaf(-rate, x[j], p.decay * y[j]);
-                                    store8<true>(p.W + wat, nc, y);
-                                    if (p.Wb) {
-                                        if (nc >= 8) {
-                                            *reinterpret_cast<uint4*>(p.Wb + wat) = pack_bf16x8(y, 1.0f);
-                                        } else {
-#pragma unroll
-                                            for (int j = 0; j < 8; ++j)
-                                                if (j < nc) p.Wb[wat + j] = __float2bfloat16_rn(y[j]);
-                                        }
-                                    }
-                                }
-                            }
-                        } else {
-                            // Gram: A = D.  Polynomial: B = b A + c D.  A step with c = 0 has no
-                            // polynomial stage: its Gram writes B = b D.
-                            if (gram) {
-                                const float sc = cc == 0.f ? cb * NS_INV_S : NS_INV_S;
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) x[j] = d[j] * sc;
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) x[j] = fmaf(cc * NS_INV_S, d[j], cb * (x[j] + y[j]));
-                            }
-                            uint4 hi, lo;
-                            split8(x, hi, lo);
-                            __half* const* out = gram && cc != 0.f ? p.A : p.B;
-                            if (in) {
-                                *reinterpret_cast<uint4*>(out[0] + at) = hi;
-                                if (p.terms == 3) *reinterpret_cast<uint4*>(out[1] + at) = lo;
-                            }
-                            cell[0] = make_float4(x[0], x[1], x[2], x[3]);
-                            cell[1] = make_float4(x[4], x[5], x[6], x[7]);
-                        }
-                    }
-                    __syncwarp();
-                    if (!apply) {
-                        // mirror images of the 16 x 32 values, where their own tiles are not
-                        // computed: a lane takes 8 rows of a column
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int j = ch * 32 + 16 * i + (lane >> 1), col = t.n0 + j, r8 = (lane & 1) * 8;
-                            const int row = row0 + hh * 16 + r8;
-                            const int col_end = (row / p.bn_s + 1) * p.bn_s;   // end of the tile column holding `row`
-                            if (j < t.bn && col < p.m && row < p.m && col_end <= col / NS_BM * NS_BM) {
-                                float x[8];
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) x[q] = stg[(r8 + q) * NS_STG_LD + 16 * i + (lane >> 1)];
-                                uint4 hi, lo;
-                                split8(x, hi, lo);
-                                __half* const* out = gram && cc != 0.f ? p.A : p.B;
-                                const int64_t at = base + (int64_t)col * ld + row;
-                                *reinterpret_cast<uint4*>(out[0] + at) = hi;
-                                if (p.terms == 3) *reinterpret_cast<uint4*>(out[1] + at) = lo;
-                            }
-                        }
-                        __syncwarp();
+                        for (int j = 0; j < 8; ++j)
+                            if (j < nc) p.Wb[wat + j] = __float2bfloat16_rn(wv[j]);
                     }
                 }
             }
         }
+        __syncwarp();
+        if (mirror) {   // a lane takes 8 rows of a column, twice
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int j = lane >> 1, cj = t.n0 + ch * 16 + j, r8 = 16 * i + (lane & 1) * 8, row = row0 + r8;
+                const int past = (row / p.bn_s + 1) * p.bn_s;   // end of the tile column that holds `row`
+                if (cj < col_end && row < p.m && past <= cj / NS_BM * NS_BM) {
+                    float x[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) x[q] = stg[(r8 + q) * NS_STG_LD + j];
+                    uint4 hi, lo;
+                    split8(x, hi, lo);
+                    const int64_t at = (int64_t)cj * ld + row;
+                    *reinterpret_cast<uint4*>(out_h + at) = hi;
+                    if (lo_in) *reinterpret_cast<uint4*>(out_l + at) = lo;
+                }
+            }
+            __syncwarp();
+        }
+    }
+    return true;
+}
+
+__device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, volatile int* abort_flag) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float* stg = sm.stg + warp * NS_STG_ROWS * NS_STG_LD;
+    int n = 0;
+    NsWalk w = ns_walk_start(p);
+    for (int id = sm.pair; id < p.total; id += sm.npairs, ++n) {
+        const NsItem it = ns_item(p, w, id);
+        const NsTile t = ns_tile(p, it);
+        bool ok;
+        if (it.kind == NS_GRAM) ok = ns_epi_tile<NS_M_GRAM>(p, sm, it, t, stg, tmem, n, abort_flag);
+        else if (it.kind == NS_POLY) ok = ns_epi_tile<NS_M_POLY>(p, sm, it, t, stg, tmem, n, abort_flag);
+        else if (it.step < p.steps - 1) ok = ns_epi_tile<NS_M_X>(p, sm, it, t, stg, tmem, n, abort_flag);
+        else if (p.O) ok = ns_epi_tile<NS_M_O>(p, sm, it, t, stg, tmem, n, abort_flag);
+        else ok = ns_epi_tile<NS_M_W>(p, sm, it, t, stg, tmem, n, abort_flag);
+        if (!ok) return;
         fence_proxy_async_all();   // what was written will be read by TMA
         __syncwarp();
         if (lane == 0) add_release(p.u.prog + it.e, 1);
@@ -953,7 +968,7 @@ inline size_t up256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 constexpr int64_t NS_L2_BYTES = 72ll << 20;
 
 struct NsLayout {
-    size_t prog, part, xh0, xh1, xl0, xl1, A, Al, B, Bl, total;
+    size_t prog, part, x0h, x0l, xh0, xh1, xl0, xl1, A, Al, B, Bl, total;
     int chunks, groups, n_groups, group_max, slots, terms;
 };
 NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
@@ -980,6 +995,8 @@ NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     L.part = take((size_t)N * L.chunks * 3 * sizeof(float));
     const size_t x = (size_t)L.slots * r * ldx * 2, a = (size_t)L.slots * m * ldm * 2;
     const bool thin = m <= NS_THIN;
+    L.x0h = take(thin ? 0 : (size_t)N * r * ldx * 2);
+    L.x0l = take(thin ? 0 : (size_t)N * r * ldx * 2);
     L.xh0 = take(thin ? 0 : x);
     L.xh1 = take(thin ? 0 : x);
     L.xl0 = take(thin ? 0 : x);
@@ -1011,8 +1028,8 @@ size_t ns_workspace_bytes(int64_t N, int64_t r, int64_t c) {
     full = full * NS_LANES < N ? full * NS_LANES : N;
     if (full > 0) {
         const NsLayout F = ns_layout(full, r, c);
-        const size_t per = 4 + (size_t)L.chunks * 3 * sizeof(float);
-        const size_t v = F.total + (size_t)(N - full) * per + 512;
+        const size_t per = 4 + (size_t)L.chunks * 3 * sizeof(float) + (m <= NS_THIN ? 0 : 4 * (size_t)r * ldx);
+        const size_t v = F.total + (size_t)(N - full) * per + 1024;
         if (v > most) most = v;
     }
     return most;
@@ -1052,7 +1069,6 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
 
     a.steps = q.steps;
     int stage = 0;
-    a.kind[stage++] = NS_LOAD;
     for (int it = 0; it < q.steps; ++it) {
         for (int j = 0; j < 3; ++j) a.coef[3 * it + j] = q.coef[3 * it + j];
         // lo in the last two steps: see the file comment
@@ -1082,19 +1098,26 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
         count_launches(1);
         return e != cudaSuccess ? e : cudaGetLastError();
     }
-    a.xh[0] = reinterpret_cast<__half*>(ws + L.xh0);
-    a.xh[1] = reinterpret_cast<__half*>(ws + L.xh1);
-    a.xl[0] = reinterpret_cast<__half*>(ws + L.xl0);
-    a.xl[1] = reinterpret_cast<__half*>(ws + L.xl1);
+    a.xh[0] = reinterpret_cast<__half*>(ws + L.x0h);
+    a.xl[0] = reinterpret_cast<__half*>(ws + L.x0l);
+    a.xh[1] = reinterpret_cast<__half*>(ws + L.xh0);
+    a.xh[2] = reinterpret_cast<__half*>(ws + L.xh1);
+    a.xl[1] = reinterpret_cast<__half*>(ws + L.xl0);
+    a.xl[2] = reinterpret_cast<__half*>(ws + L.xl1);
+    e = launch_pdl(muon_scale_kernel, dim3((unsigned)L.chunks, (unsigned)a.N), dim3(NS_PRO_THREADS), 0, s, a.u, a.xh[0],
+                   a.xl[0]);
+    count_launches(1);
+    if (e != cudaSuccess) return e;
     a.A[0] = reinterpret_cast<__half*>(ws + L.A);
     a.A[1] = reinterpret_cast<__half*>(ws + L.Al);
     a.B[0] = reinterpret_cast<__half*>(ws + L.B);
     a.B[1] = reinterpret_cast<__half*>(ws + L.Bl);
     bool ok = true;
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 3; ++i)
         for (int j = 0; j < 2; ++j)
-            ok = ok && make_weight_tmap_strided(&a.tX[i][j], j ? a.xl[i] : a.xh[i], a.c, a.r, L.slots, a.ldx,
+            ok = ok && make_weight_tmap_strided(&a.tX[i][j], j ? a.xl[i] : a.xh[i], a.c, a.r, i ? L.slots : a.N, a.ldx,
                                                 (int64_t)a.r * a.ldx);
+    for (int i = 0; i < 2; ++i) {
         ok = ok && make_weight_tmap_strided(&a.tA[i], a.A[i], a.m, a.m, L.slots, a.ldm, (int64_t)a.m * a.ldm) &&
              make_weight_tmap_strided(&a.tB[i], a.B[i], a.m, a.m, L.slots, a.ldm, (int64_t)a.m * a.ldm);
     }
@@ -1105,7 +1128,6 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.mt_x = (a.r + NS_BM - 1) / NS_BM;
     int sym = 0;
     for (int i = 0; i < a.mt_s; ++i) sym += a.nt_s - i * NS_BM / a.bn_s;
-    a.tiles[NS_LOAD] = (L.groups + NS_LOAD_GROUPS - 1) / NS_LOAD_GROUPS;
     a.tiles[NS_GRAM] = a.tiles[NS_POLY] = sym;
     a.tiles[NS_APPLY] = a.mt_x * a.nt_x;
     int64_t items = 0;
@@ -1119,6 +1141,8 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.total = (int)items;
     a.n_groups = L.n_groups;
     a.group_max = L.group_max;
+    a.base_size = a.N / L.n_groups;
+    a.big_groups = a.N % L.n_groups;
     static bool attr_set[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
