@@ -51,6 +51,7 @@ enum Site : int {
     SITE_NS_DRAIN = 44,
     SITE_NS_WAIT_INPUT = 45,
     SITE_NS_WAIT_BUFFER = 46,
+    SITE_NS_WAIT_SLOT = 47,
     SITE_FEW_WAIT_EMPTY = 50,
     SITE_FEW_WAIT_FULL = 51,
     SITE_FEW_WAIT_TFULL = 52,

@@ -269,34 +269,39 @@ constexpr int NS_BM = 256;            // output rows per tile: a CTA pair, 128 r
 constexpr int NS_HALF = 128;
 constexpr int NS_MAXBN = 256;         // output columns per tile at most (one tcgen05.mma)
 constexpr int NS_BK = 64;             // K per ring stage: one 128-byte swizzle row of fp16
-constexpr int NS_STAGES = 5;
+constexpr int NS_STAGES = 4;
 constexpr int NS_BOX = 64 * NS_BK * 2;                     // bytes of one 64 x 64 TMA box
 constexpr int NS_STAGE_BYTES = (NS_HALF + NS_MAXBN / 2) / 64 * NS_BOX;   // a CTA's A rows and half of B
-constexpr int NS_EPI_WARPS = 8;       // two per TMEM lane quadrant, 16-column chunks in turn
-constexpr int NS_CH = NS_EPI_WARPS / 4;   // a warp takes every NS_CH-th chunk
-constexpr int NS_WARP_LOAD = NS_EPI_WARPS;
+constexpr int NS_EPI_WARPS = 8;       // two per TMEM lane quadrant: 32 of a block's 64 columns each
+constexpr int NS_WARP_LOAD = NS_EPI_WARPS;        // operand loads
 constexpr int NS_WARP_MMA = NS_EPI_WARPS + 1;
-constexpr int NS_THREADS = (NS_EPI_WARPS + 2) * 32;
-constexpr int NS_STG_LD = 20;         // floats per staged row (16 values, padded)
-constexpr int NS_STG_ROWS = 32;       // a warp's rows
-constexpr int NS_STG_BYTES = NS_EPI_WARPS * NS_STG_ROWS * NS_STG_LD * 4;
-constexpr int NS_SMEM = NS_STAGES * NS_STAGE_BYTES + NS_STG_BYTES + 1024 + 256;
-static_assert(NS_SMEM <= 232448, "shared memory of one CTA");
+constexpr int NS_WARP_IN = NS_EPI_WARPS + 2;      // loads of what the epilogue reads
+constexpr int NS_WARP_OUT = NS_EPI_WARPS + 3;     // stores of what it writes
+constexpr int NS_THREADS = (NS_EPI_WARPS + 4) * 32;
+// Epilogue blocks: the CTA's 128 rows x 64 columns, in two regions of two boxes (hi and lo, or a
+// value and its mirror image; together one fp32 block).
+constexpr int NS_REGION = 2 * NS_BOX;
+constexpr int NS_SLOTS = 3;
+constexpr int NS_SLOT_BYTES = 2 * NS_REGION;
+constexpr int NS_BARS = 2 * NS_STAGES + 5 + 3 * NS_SLOTS;
+constexpr int NS_SMEM = NS_STAGES * NS_STAGE_BYTES + NS_SLOTS * NS_SLOT_BYTES + 1024 + 256;
+static_assert(NS_SMEM <= 232448 && NS_BARS * 8 + 8 <= 256, "shared memory of one CTA");
 
 constexpr int NS_LANES = 3;           // groups of matrices under way, a stage apart
 constexpr int NS_MAX_STAGES = 3 * NS_MAX_STEPS;
-constexpr int NS_DONE = 2 * NS_EPI_WARPS;   // a finished item's contribution to its matrix's counter
+constexpr int NS_DONE = 2;            // a finished item's contribution to its matrix's counter (both CTAs)
 
 enum NsKind : int { NS_GRAM = 0, NS_POLY = 1, NS_APPLY = 2 };
 
 struct NsArgs {
     CUtensorMap tX[3][2], tA[2], tB[2];   // [X0, buffer 0, 1][hi, lo]; 3-D maps {inner, rows, matrices
                                           //   (X0) or slots}, boxes 64 x 64
+    CUtensorMap tO;                    // the result, where its rows are 16-byte aligned (vec_o)
     UpdateArgs u;
     __half *xh[3], *xl[3];             // X0 [N][r][ldx]; X, ping-pong [slots][r][ldx] (lo in place with one term)
     __half *A[2], *B[2];               // hi, lo (lo with three terms only) [slots][m][ldm]
     int N, r, c, m, ldx, ldm, tall, terms;
-    int bn_s, nt_s, mt_s, bn_x, nt_x, mt_x;   // tiles of m x m and of r x c outputs
+    int bn, nt_x, mt_x, mt_s, nt_s;    // tile width (64, 128 or 256); tiles of r x c and m x m outputs
     int tiles[3];                      // items of a matrix's stage, by kind
     int n_stages, n_groups, group_max; // stages of a matrix; groups of matrices; their largest size
     int base_size, big_groups;         // the first big_groups of them hold base_size + 1, the others base_size
@@ -392,46 +397,47 @@ __device__ __forceinline__ int ns_dst(int s) { return 1 + (s & 1); }
 
 struct NsTile {
     int m0, n0, bn, num_kb;            // num_kb: K blocks of one term
+    bool mirror;                       // symmetric output: also write its mirror image
     const CUtensorMap *a[2], *b[2];    // operands, hi and lo
     int za, zb;                        // their matrix or slot
     bool a_mn, b_mn;
 };
 
-// First needed tile of row tile i of a symmetric output: tiles left of it lie strictly below
-// the diagonal and are written as mirror images.
-__device__ __forceinline__ int sym_first(const NsArgs& p, int i) { return i * NS_BM / p.bn_s; }
-
 // Operand layouts of a product: an operand whose K runs along the rows of its array is read
 // MN-major, one whose K runs along the columns K-major; no array is ever transposed.
 //   r <= c:  Gram  X X^T both K-major;   apply B X: B K-major, X MN-major
 //   r >  c:  Gram  X^T X both MN-major;  apply X B: both K-major (B is symmetric)
+// Symmetric outputs: row tile i has the column tiles from the diagonal on; those past its own
+// columns are mirrored.
 __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
     NsTile t;
     const int src = ns_src(it.step);
-    int k = p.m;
+    int k = p.m, cols = p.m;
     if (it.kind == NS_APPLY) {
-        t.m0 = it.tile / p.nt_x * NS_BM;
-        t.n0 = it.tile % p.nt_x * p.bn_x;
-        t.bn = p.bn_x;
+        const int i = it.tile / p.nt_x;
+        t.m0 = i * NS_BM;
+        t.n0 = (it.tile - i * p.nt_x) * p.bn;
+        cols = p.c;
+        t.mirror = false;
         t.a_mn = false;
         t.b_mn = !p.tall;
         t.za = p.tall && src == 0 ? it.e : it.buf;
         t.zb = !p.tall && src == 0 ? it.e : it.buf;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            t.a[i] = p.tall ? &p.tX[src][i] : &p.tB[i];
-            t.b[i] = p.tall ? &p.tB[i] : &p.tX[src][i];
+        for (int j = 0; j < 2; ++j) {
+            t.a[j] = p.tall ? &p.tX[src][j] : &p.tB[j];
+            t.b[j] = p.tall ? &p.tB[j] : &p.tX[src][j];
         }
     } else {
+        const int per = NS_BM / p.bn;
         int q = it.tile, i = 0;
-        for (; i < p.mt_s - 1; ++i) {
-            const int n = p.nt_s - sym_first(p, i);
-            if (q < n) break;
-            q -= n;
+        while (i < p.mt_s - 1 && q >= p.nt_s - i * per) {
+            q -= p.nt_s - i * per;
+            ++i;
         }
         t.m0 = i * NS_BM;
-        t.n0 = (sym_first(p, i) + q) * p.bn_s;
-        t.bn = p.bn_s;
+        t.n0 = (i * per + q) * p.bn;
+        t.mirror = t.n0 >= t.m0 + NS_BM;
         const bool gram = it.kind == NS_GRAM;
         if (gram) k = p.tall ? p.r : p.c;
         t.a_mn = t.b_mn = gram && p.tall;
@@ -439,6 +445,7 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) t.a[j] = t.b[j] = gram ? &p.tX[src][j] : &p.tA[j];
     }
+    t.bn = min(p.bn, (cols - t.n0 + 31) & ~31);   // a multiple of 32: each CTA holds half of B
     t.num_kb = (k + NS_BK - 1) / NS_BK;
     return t;
 }
@@ -449,8 +456,10 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn_maj
 }
 
 struct NsSmem {
-    uint32_t ring, full, empty, tfull, tempty, drain;
-    float* stg;
+    uint32_t ring, slots;
+    uint32_t full, empty, tfull, tempty, drain;
+    uint32_t in, done, free_;   // per epilogue slot: inputs landed; results written; stores have read it
+    uint8_t* slot_ptr;
     uint32_t rank;
     int pair, npairs;
 };
@@ -579,202 +588,290 @@ __device__ __forceinline__ void unpack_half8(const uint4& u, float (&v)[8]) {
         v[2 * q + 1] = f.y;
     }
 }
-__device__ __forceinline__ uint4 pack_bf16x8(const float (&v)[8], float sc) {
-    return make_uint4(pack_bf16x2(v[0] * sc, v[1] * sc), pack_bf16x2(v[2] * sc, v[3] * sc),
-                      pack_bf16x2(v[4] * sc, v[5] * sc), pack_bf16x2(v[6] * sc, v[7] * sc));
-}
 
-enum NsMode : int { NS_M_GRAM, NS_M_POLY, NS_M_X, NS_M_O, NS_M_W };
-
-// One tile of one warp: TMEM lanes 32 (w % 4) .. of the CTA's 128 rows, the 16-column chunks
-// w / 4, w / 4 + 2, ...  The accumulator rows pass a per-warp buffer so that two consecutive lanes
-// hold 16 consecutive columns of a row and every global access of a warp covers sixteen whole
-// 32-byte (fp16) sectors; what a chunk reads from L2 is loaded a chunk ahead.  One instance per
-// MODE, so that each loop holds only the code that its tiles run:
+// Which regions of an epilogue block a tile reads and writes.
 //   GRAM: A = D (a step with c = 0 has no polynomial stage: B = b D);  POLY: B = b A + c D;
 //   X: X = a X + D in the working format;  O, W: the same of the last step, to the outputs.
-template <int MODE>
-__device__ __forceinline__ bool ns_epi_tile(const NsArgs& p, const NsSmem& sm, const NsItem& it, const NsTile& t,
-                                            float* stg, uint32_t tmem, int n, volatile int* abort_flag) {
-    constexpr bool APPLY = MODE >= NS_M_X;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = warp & 3, first = warp >> 2;
-    const int lr = lane >> 1, lc = (lane & 1) * 8;   // a lane's row (of 16) and first column after staging
-    const int rows = APPLY ? p.r : p.m, cols = APPLY ? p.c : p.m, ld = APPLY ? p.ldx : p.ldm;
-    const int col_end = min(cols, t.n0 + t.bn), nchunk = t.bn / 16;
-    const int row0 = t.m0 + (int)sm.rank * NS_HALF + quad * 32;
-    const int src = ns_src(it.step), dst = ns_dst(it.step), acc = n & 1;
-    const int64_t mat = (int64_t)it.buf * rows * ld, lane_at = (int64_t)(row0 + lr) * ld + t.n0 + lc;
-    const int rows_left = rows - row0 - lr;          // row 16 i + lr exists when 16 i < rows_left
-    const int64_t in_at = (APPLY && src == 0 ? (int64_t)it.e * rows * ld : mat) + lane_at;
-    const __half* in_h = (APPLY ? p.xh[src] : p.A[0]) + in_at;
-    const __half* in_l = (APPLY ? p.xl[src] : p.A[1]) + in_at;
-    const bool lo_in = APPLY || p.terms == 3;
-    const bool to_b = MODE == NS_M_POLY || p.coef[3 * it.step + 2] == 0.f;
-    __half* out_h = (APPLY ? p.xh[dst] : to_b ? p.B[0] : p.A[0]) + mat;
-    __half* out_l = (APPLY ? p.xl[dst] : to_b ? p.B[1] : p.A[1]) + mat;
-    uint4 nh[2], nl[2];
-    auto fetch = [&](int ch, int i) {
-        nh[i] = nl[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (t.n0 + ch * 16 + lc < col_end && 16 * i < rows_left) {
-            const int64_t at = (int64_t)(16 * i) * ld + ch * 16;
-            nh[i] = __ldcg(reinterpret_cast<const uint4*>(in_h + at));
-            if (lo_in) nl[i] = __ldcg(reinterpret_cast<const uint4*>(in_l + at));
-        }
-    };
-    // What the tile reads was written before its products could start.  Usually that is so already
-    // and the first loads go out before the accumulator is complete; no polling here (sixteen
-    // warps of every CTA on one counter held up its writers: 9 us a tile).
-    auto ready = [&]() {
-        int ok = 0;
-        if (lane == 0) ok = ld_acquire(p.u.prog + it.e) >= p.need[it.stage];
-        return __shfl_sync(0xffffffffu, ok, 0) != 0;
-    };
-    const bool early = MODE != NS_M_GRAM && first < nchunk && ready();
-    if (early) {
-        fetch(first, 0);
-        fetch(first, 1);
-    }
-    if (!mbar_wait(sm.tfull + 8 * acc, (uint32_t)(n >> 1) & 1u, p.limit_ns, abort_flag)) {
-        ns_abort(abort_flag, p.status, SITE_NS_WAIT_TFULL, it.e);
-        return false;
-    }
-    tc_fence_after();
-    if (MODE != NS_M_GRAM && first < nchunk && !early) {
-        ready();   // (it is: orders the reads)
-        fetch(first, 0);
-        fetch(first, 1);
-    }
-    const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * NS_MAXBN;
-    const uint32_t tempty = peer_addr(sm.tempty, 0) + 8 * acc;
-    if (first >= nchunk) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive_remote(tempty);
-    }
-    // mirror images (symmetric outputs): needed where a column lies past the row's tile column
-    const bool mirror = !APPLY && (row0 / p.bn_s + 1) * p.bn_s <= (col_end - 1) / NS_BM * NS_BM;
-#pragma unroll 1
-    for (int ch = first; ch < nchunk; ch += NS_CH) {
-        uint32_t v[16];
-        tmem_ld_32x32b_x16(tbase + ch * 16, v);
-        tmem_wait_ld();
-        if (ch + NS_CH >= nchunk) {   // this warp's last read of the accumulator
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_remote(tempty);
-        }
-        float4* o = reinterpret_cast<float4*>(stg + lane * NS_STG_LD);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            o[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
-                               __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
-        __syncwarp();
-        const int col = t.n0 + ch * 16 + lc;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            float4* cell = reinterpret_cast<float4*>(stg + (16 * i + lr) * NS_STG_LD + lc);
-            const float4 d0 = cell[0], d1 = cell[1];
-            float x[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
-            if (MODE == NS_M_GRAM) {
-                const float sc = to_b ? p.coef[3 * it.step + 1] * NS_INV_S : NS_INV_S;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] *= sc;
-            } else {
-                float h[8];
-                unpack_half8(nh[i], h);
-                const float fd = APPLY ? NS_INV_S : p.coef[3 * it.step + 2] * NS_INV_S;
-                const float fh = p.coef[3 * it.step + (APPLY ? 0 : 1)];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = fmaf(fd, x[j], fh * h[j]);
-                if (lo_in) {
-                    const float fl = APPLY ? p.lo_coef[it.step] : fh;
-                    unpack_half8(nl[i], h);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = fmaf(fl, h[j], x[j]);
-                }
-                if (ch + NS_CH < nchunk) fetch(ch + 4, i);
-            }
-            const bool in = col < col_end && 16 * i < rows_left;
-            if (MODE == NS_M_GRAM || MODE == NS_M_POLY || MODE == NS_M_X) {
-                uint4 hi, lo;
-                split8(x, hi, lo);
-                if (in) {
-                    const int64_t at = lane_at + (int64_t)(16 * i) * ld + ch * 16;
-                    *reinterpret_cast<uint4*>(out_h + at) = hi;
-                    if (lo_in) *reinterpret_cast<uint4*>(out_l + at) = lo;
-                }
-                if (mirror) {
-                    cell[0] = make_float4(x[0], x[1], x[2], x[3]);
-                    cell[1] = make_float4(x[4], x[5], x[6], x[7]);
-                }
-            } else if (in) {
-                const int nc = p.c - col, row = row0 + 16 * i + lr;   // nc: columns of this group that exist
-                if (MODE == NS_M_O) {
-                    __nv_bfloat16* out = p.O + it.e * p.st_o + row * p.ld_o + col;
-                    if (p.vec_o && nc >= 8) {
-                        *reinterpret_cast<uint4*>(out) = pack_bf16x8(x, NS_INV_S);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (j < nc) out[j] = __float2bfloat16_rn(x[j] * NS_INV_S);
-                    }
-                } else {
-                    const int64_t wat = it.e * p.st_w + row * p.ld_w + col;
-                    const float rate = p.rate * NS_INV_S;
-                    float wv[8];
-                    load8<float, true>(p.W + wat, nc, wv);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) wv[j] = fmaf(-rate, x[j], p.decay * wv[j]);
-                    store8<true>(p.W + wat, nc, wv);
-                    if (p.Wb && nc >= 8) *reinterpret_cast<uint4*>(p.Wb + wat) = pack_bf16x8(wv, 1.0f);
-                    else if (p.Wb) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (j < nc) p.Wb[wat + j] = __float2bfloat16_rn(wv[j]);
-                    }
-                }
-            }
-        }
-        __syncwarp();
-        if (mirror) {   // a lane takes 8 rows of a column, twice
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int j = lane >> 1, cj = t.n0 + ch * 16 + j, r8 = 16 * i + (lane & 1) * 8, row = row0 + r8;
-                const int past = (row / p.bn_s + 1) * p.bn_s;   // end of the tile column that holds `row`
-                if (cj < col_end && row < p.m && past <= cj / NS_BM * NS_BM) {
-                    float x[8];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) x[q] = stg[(r8 + q) * NS_STG_LD + j];
-                    uint4 hi, lo;
-                    split8(x, hi, lo);
-                    const int64_t at = (int64_t)cj * ld + row;
-                    *reinterpret_cast<uint4*>(out_h + at) = hi;
-                    if (lo_in) *reinterpret_cast<uint4*>(out_l + at) = lo;
-                }
-            }
-            __syncwarp();
-        }
-    }
-    return true;
+enum NsMode : int { NS_M_GRAM, NS_M_POLY, NS_M_X, NS_M_O, NS_M_W };
+__device__ __forceinline__ int ns_mode(const NsArgs& p, const NsItem& it) {
+    if (it.kind != NS_APPLY) return it.kind == NS_GRAM ? NS_M_GRAM : NS_M_POLY;
+    return it.step < p.steps - 1 ? NS_M_X : p.O ? NS_M_O : NS_M_W;
 }
 
-__device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, volatile int* abort_flag) {
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(tm),
+                 "r"(c0), "r"(c1), "r"(c2), "r"(src)
+                 : "memory");
+}
+
+// What the epilogue reads of A (polynomial) or X (apply), block by block into its slots: one
+// thread.  Gram blocks read nothing; their slots are handed on as they become free.
+__device__ void ns_inputs(const NsArgs& p, const NsSmem& sm, volatile int* abort_flag) {
+    int s = 0;
+    uint32_t ph = 0;
+    NsWalk w = ns_walk_start(p);
+    for (int id = sm.pair; id < p.total; id += sm.npairs) {
+        const NsItem it = ns_item(p, w, id);
+        const NsTile t = ns_tile(p, it);
+        const int mode = ns_mode(p, it), src = ns_src(it.step);
+        const bool lo = mode >= NS_M_X || (mode == NS_M_POLY && p.terms == 3);
+        const int row = t.m0 + (int)sm.rank * NS_HALF, z = mode >= NS_M_X && src == 0 ? it.e : it.buf;
+        const CUtensorMap* mh = mode >= NS_M_X ? &p.tX[src][0] : &p.tA[0];
+        const CUtensorMap* ml = mode >= NS_M_X ? &p.tX[src][1] : &p.tA[1];
+        if (mode != NS_M_GRAM) {
+            if (!ns_wait(p, it.e, p.need[it.stage], abort_flag, SITE_NS_WAIT_INPUT)) return;
+            fence_proxy_async_all();
+        }
+        for (int c0 = 0; c0 < t.bn; c0 += 64) {
+            if (!mbar_wait(sm.free_ + 8 * s, ph ^ 1u, p.limit_ns, abort_flag)) {
+                ns_abort(abort_flag, p.status, SITE_NS_WAIT_SLOT, id);
+                return;
+            }
+            const uint32_t bar = sm.in + 8 * s, at = sm.slots + s * NS_SLOT_BYTES;
+            if (mode == NS_M_GRAM) {
+                mbar_arrive(bar);
+            } else {
+                mbar_arrive_expect_tx(bar, lo ? 2 * NS_REGION : NS_REGION);
+                tma_load_3d(at, mh, bar, t.n0 + c0, row, z);
+                tma_load_3d(at + NS_BOX, mh, bar, t.n0 + c0, row + 64, z);
+                if (lo) {
+                    tma_load_3d(at + NS_REGION, ml, bar, t.n0 + c0, row, z);
+                    tma_load_3d(at + NS_REGION + NS_BOX, ml, bar, t.n0 + c0, row + 64, z);
+                }
+            }
+            if (++s == NS_SLOTS) {
+                s = 0;
+                ph ^= 1u;
+            }
+        }
+    }
+}
+
+// Stores the epilogue's finished blocks, hands their slots back and counts finished tiles: one
+// thread.
+__device__ void ns_outputs(const NsArgs& p, const NsSmem& sm, volatile int* abort_flag) {
+    int s = 0;
+    uint32_t ph = 0;
+    NsWalk w = ns_walk_start(p);
+    for (int id = sm.pair; id < p.total; id += sm.npairs) {
+        const NsItem it = ns_item(p, w, id);
+        const NsTile t = ns_tile(p, it);
+        const int mode = ns_mode(p, it), row = t.m0 + (int)sm.rank * NS_HALF;
+        const int rows = mode >= NS_M_X ? p.r : p.m, cols = mode >= NS_M_X ? p.c : p.m;
+        const bool to_b = mode == NS_M_POLY || (mode == NS_M_GRAM && p.coef[3 * it.step + 2] == 0.f);
+        const bool lo = mode == NS_M_X || (mode < NS_M_X && p.terms == 3);
+        const int dst = ns_dst(it.step), z = mode == NS_M_O ? it.e : it.buf;
+        const CUtensorMap* mh = mode == NS_M_O ? &p.tO : mode == NS_M_X ? &p.tX[dst][0] : to_b ? &p.tB[0] : &p.tA[0];
+        const CUtensorMap* ml = mode == NS_M_X ? &p.tX[dst][1] : to_b ? &p.tB[1] : &p.tA[1];
+        const bool store = mode != NS_M_W && (mode != NS_M_O || p.vec_o);
+        for (int c0 = 0; c0 < t.bn; c0 += 64) {
+            if (!mbar_wait(sm.done + 8 * s, ph, p.limit_ns, abort_flag)) {
+                ns_abort(abort_flag, p.status, SITE_NS_WAIT_SLOT, -id);
+                break;
+            }
+            const uint32_t at = sm.slots + s * NS_SLOT_BYTES;
+            const int col = t.n0 + c0;
+            if (store && col < cols) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {   // boxes that start past the array's end are not stored
+                    if (row + 64 * q >= rows) continue;
+                    tma_store_3d(mh, at + q * NS_BOX, col, row + 64 * q, z);
+                    if (lo) tma_store_3d(ml, at + NS_REGION + q * NS_BOX, col, row + 64 * q, z);
+                    else if (t.mirror) tma_store_3d(mh, at + NS_REGION + q * NS_BOX, row + 64 * q, col, z);
+                }
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            }
+            mbar_arrive(sm.free_ + 8 * s);
+            if (++s == NS_SLOTS) {
+                s = 0;
+                ph ^= 1u;
+            }
+        }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // (bounded by the copies themselves)
+        if (*abort_flag) return;
+        fence_proxy_async_all();
+        add_release(p.u.prog + it.e, 1);
+    }
+}
+
+// 16-byte chunk c (8 fp16) of row r of a region: the TMA boxes' 128-byte swizzle.
+__device__ __forceinline__ uint8_t* ns_cell(uint8_t* region, int r, int c) {
+    return region + r * 128 + ((c ^ (r & 7)) << 4);
+}
+// 16-byte chunk c (4 fp32 of 16) of row r of an fp32 block.
+__device__ __forceinline__ float4* ns_cell32(uint8_t* slot, int r, int c) {
+    return reinterpret_cast<float4*>(slot + r * 256 + ((c ^ (r & 15)) << 4));
+}
+
+// Barrier of the epilogue warps.
+__device__ __forceinline__ void ns_epi_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// A warp's 32 columns (half of the block) of one block: thread = row.  One instance per MODE, so
+// that each holds only the code that its tiles run.
+template <int MODE>
+__device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, const NsTile& t, uint8_t* slot, int row,
+                                         int half, int rank, int c0, const uint32_t (&v)[32]) {
+    constexpr bool APPLY = MODE >= NS_M_X;
+    const float cc = p.coef[3 * it.step + 2], cb = p.coef[3 * it.step + 1];
+    const float fd = MODE == NS_M_GRAM ? (cc == 0.f ? cb * NS_INV_S : NS_INV_S) : MODE == NS_M_POLY ? cc * NS_INV_S : NS_INV_S;
+    const float fh = APPLY ? p.coef[3 * it.step] : cb, fl = APPLY ? p.lo_coef[it.step] : cb;
+    const bool lo_in = APPLY || p.terms == 3;
+    float keep[MODE == NS_M_W ? 32 : 1];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int c = half * 4 + g;
+        uint4* ch = reinterpret_cast<uint4*>(ns_cell(slot, row, c));
+        uint4* cl = reinterpret_cast<uint4*>(ns_cell(slot + NS_REGION, row, c));
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = fd * __uint_as_float(v[8 * g + j]);
+        if (MODE != NS_M_GRAM) {
+            float h[8];
+            unpack_half8(*ch, h);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = fmaf(fh, h[j], x[j]);
+            if (lo_in) {
+                unpack_half8(*cl, h);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = fmaf(fl, h[j], x[j]);
+            }
+        }
+        if (MODE == NS_M_W) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) keep[(8 * g + j) % (MODE == NS_M_W ? 32 : 1)] = x[j];
+        } else if (MODE == NS_M_O) {
+            *ch = make_uint4(pack_bf16x2(x[0] * NS_INV_S, x[1] * NS_INV_S), pack_bf16x2(x[2] * NS_INV_S, x[3] * NS_INV_S),
+                             pack_bf16x2(x[4] * NS_INV_S, x[5] * NS_INV_S), pack_bf16x2(x[6] * NS_INV_S, x[7] * NS_INV_S));
+        } else {
+            uint4 hi, lo;
+            split8(x, hi, lo);
+            *ch = hi;
+            if (lo_in) {
+                *cl = lo;
+            } else if (t.mirror) {   // column j of the block is row j of the mirror boxes
+                const uint32_t hw[4] = {hi.x, hi.y, hi.z, hi.w};
+                uint8_t* box = slot + NS_REGION + (row >> 6) * NS_BOX;
+                const int rr = row & 63;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<uint16_t*>(ns_cell(box, c * 8 + j, rr >> 3) + (rr & 7) * 2) =
+                        (uint16_t)(j & 1 ? hw[j >> 1] >> 16 : hw[j >> 1] & 0xffffu);
+            }
+        }
+    }
+    if (MODE == NS_M_W) {
+        // the block in fp32 where its inputs were, then rows of W in whole 256-byte pieces
+        ns_epi_sync();
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+            *ns_cell32(slot, row, half * 8 + g) =
+                make_float4(keep[(4 * g) % (MODE == NS_M_W ? 32 : 1)], keep[(4 * g + 1) % (MODE == NS_M_W ? 32 : 1)],
+                            keep[(4 * g + 2) % (MODE == NS_M_W ? 32 : 1)], keep[(4 * g + 3) % (MODE == NS_M_W ? 32 : 1)]);
+        ns_epi_sync();
+        const float rate = p.rate * NS_INV_S;
+        const int q = threadIdx.x & 15, col = t.n0 + c0 + 4 * q, nc = p.c - col;
+        const int64_t base = it.e * p.st_w + col;
+        if (4 * q < t.bn - c0 && nc > 0) {
+#pragma unroll 4
+            for (int r = threadIdx.x >> 4; r < NS_HALF; r += 16) {
+                const int gr = t.m0 + rank * NS_HALF + r;
+                if (gr >= p.r) break;
+                const int64_t at = base + gr * p.ld_w;
+                const float4 x = *ns_cell32(slot, r, q);
+                if (nc >= 4) {
+                    float4 o = *reinterpret_cast<const float4*>(p.W + at);
+                    o.x = fmaf(-rate, x.x, p.decay * o.x);
+                    o.y = fmaf(-rate, x.y, p.decay * o.y);
+                    o.z = fmaf(-rate, x.z, p.decay * o.z);
+                    o.w = fmaf(-rate, x.w, p.decay * o.w);
+                    *reinterpret_cast<float4*>(p.W + at) = o;
+                    if (p.Wb)
+                        *reinterpret_cast<uint2*>(p.Wb + at) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
+                } else {
+                    const float xs[3] = {x.x, x.y, x.z};
+#pragma unroll
+                    for (int j = 0; j < 3; ++j)
+                        if (j < nc) {
+                            const float o = fmaf(-rate, xs[j], p.decay * p.W[at + j]);
+                            p.W[at + j] = o;
+                            if (p.Wb) p.Wb[at + j] = __float2bfloat16_rn(o);
+                        }
+                }
+            }
+        }
+    } else if (MODE == NS_M_O) {
+        if (!p.vec_o) {   // rows off 16-byte bounds: no TMA store; columns in turn over the threads
+            ns_epi_sync();
+            const int q = threadIdx.x & 63, col = t.n0 + c0 + q;
+            if (q < t.bn - c0 && col < p.c)
+                for (int r = threadIdx.x >> 6; r < NS_HALF; r += 4) {
+                    const int gr = t.m0 + rank * NS_HALF + r;
+                    if (gr >= p.r) break;
+                    p.O[it.e * p.st_o + gr * p.ld_o + col] =
+                        *reinterpret_cast<const __nv_bfloat16*>(ns_cell(slot, r, q >> 3) + (q & 7) * 2);
+                }
+        }
+    }
+}
+
+// Eight warps: warp w reads TMEM lanes 32 (w % 4) .. and half w / 4 of each 64-column block.  A
+// thread's values are consecutive in its row, as they are in the blocks' swizzled rows, so what
+// the tile reads and writes in fp16 goes through shared memory in place, 16 bytes at a time, and
+// between there and L2 by TMA.  One thread waits for the accumulator and decides for all, as
+// some modes meet at barriers within a block.
+__device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, volatile int* abort_flag,
+                            volatile int* go) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    float* stg = sm.stg + warp * NS_STG_ROWS * NS_STG_LD;
-    int n = 0;
+    const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
+    int n = 0, s = 0;
+    uint32_t ph = 0;
     NsWalk w = ns_walk_start(p);
     for (int id = sm.pair; id < p.total; id += sm.npairs, ++n) {
         const NsItem it = ns_item(p, w, id);
         const NsTile t = ns_tile(p, it);
-        bool ok;
-        if (it.kind == NS_GRAM) ok = ns_epi_tile<NS_M_GRAM>(p, sm, it, t, stg, tmem, n, abort_flag);
-        else if (it.kind == NS_POLY) ok = ns_epi_tile<NS_M_POLY>(p, sm, it, t, stg, tmem, n, abort_flag);
-        else if (it.step < p.steps - 1) ok = ns_epi_tile<NS_M_X>(p, sm, it, t, stg, tmem, n, abort_flag);
-        else if (p.O) ok = ns_epi_tile<NS_M_O>(p, sm, it, t, stg, tmem, n, abort_flag);
-        else ok = ns_epi_tile<NS_M_W>(p, sm, it, t, stg, tmem, n, abort_flag);
-        if (!ok) return;
-        fence_proxy_async_all();   // what was written will be read by TMA
-        __syncwarp();
-        if (lane == 0) add_release(p.u.prog + it.e, 1);
+        const int mode = ns_mode(p, it), acc = n & 1;
+        if (threadIdx.x == 0) {
+            const bool ok = mbar_wait(sm.tfull + 8 * acc, (uint32_t)(n >> 1) & 1u, p.limit_ns, abort_flag);
+            if (!ok) ns_abort(abort_flag, p.status, SITE_NS_WAIT_TFULL, id);
+            go[acc] = ok;
+        }
+        ns_epi_sync();
+        if (!go[acc]) return;
+        tc_fence_after();
+        const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * NS_MAXBN;
+        const uint32_t tempty = peer_addr(sm.tempty, 0) + 8 * acc;
+#pragma unroll 1
+        for (int c0 = 0; c0 < t.bn; c0 += 64) {
+            uint8_t* slot = sm.slot_ptr + s * NS_SLOT_BYTES;
+            uint32_t v[32];
+            tmem_ld_32x32b_x32(tbase + c0 + half * 32, v);   // (past a 32-wide last block: not used)
+            if (threadIdx.x == 0) {
+                const bool ok = mbar_wait(sm.in + 8 * s, ph, p.limit_ns, abort_flag);
+                if (!ok) ns_abort(abort_flag, p.status, SITE_NS_WAIT_SLOT, id);
+                go[2 + s] = ok;
+            }
+            ns_epi_sync();
+            tmem_wait_ld();
+            if (c0 + 64 >= t.bn) {   // this warp's last read of the accumulator
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote(tempty);
+            }
+            if (!go[2 + s]) return;
+            if (mode == NS_M_GRAM) ns_block<NS_M_GRAM>(p, it, t, slot, row, half, (int)sm.rank, c0, v);
+            else if (mode == NS_M_POLY) ns_block<NS_M_POLY>(p, it, t, slot, row, half, (int)sm.rank, c0, v);
+            else if (mode == NS_M_X) ns_block<NS_M_X>(p, it, t, slot, row, half, (int)sm.rank, c0, v);
+            else if (mode == NS_M_O) ns_block<NS_M_O>(p, it, t, slot, row, half, (int)sm.rank, c0, v);
+            else ns_block<NS_M_W>(p, it, t, slot, row, half, (int)sm.rank, c0, v);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sm.done + 8 * s);
+            if (++s == NS_SLOTS) {
+                s = 0;
+                ph ^= 1u;
+            }
+        }
     }
 }
 
@@ -783,17 +880,22 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ns_smem_raw) + 1023) &
                                                ~static_cast<uintptr_t>(1023));
     uint8_t* after = smem + NS_STAGES * NS_STAGE_BYTES;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(after + NS_STG_BYTES);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * NS_STAGES + 5);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(after + NS_SLOTS * NS_SLOT_BYTES);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + NS_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    __shared__ int go[2 + NS_SLOTS];
     NsSmem sm;
     sm.ring = smem_u32(smem);
-    sm.stg = reinterpret_cast<float*>(after);
+    sm.slot_ptr = after;
+    sm.slots = smem_u32(after);
     sm.full = smem_u32(bars);
     sm.empty = sm.full + 8 * NS_STAGES;
     sm.tfull = sm.empty + 8 * NS_STAGES;
     sm.tempty = sm.tfull + 16;
     sm.drain = sm.tempty + 16;
+    sm.in = sm.drain + 8;
+    sm.done = sm.in + 8 * NS_SLOTS;
+    sm.free_ = sm.done + 8 * NS_SLOTS;
     sm.rank = cluster_rank();
     sm.pair = blockIdx.x >> 1;
     sm.npairs = gridDim.x >> 1;
@@ -808,6 +910,11 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
             mbar_init(sm.tempty + 8 * a, 2 * NS_EPI_WARPS);
         }
         mbar_init(sm.drain, 1);
+        for (int s = 0; s < NS_SLOTS; ++s) {
+            mbar_init(sm.in + 8 * s, 1);
+            mbar_init(sm.done + 8 * s, NS_EPI_WARPS);
+            mbar_init(sm.free_ + 8 * s, 1);
+        }
         *abort_flag = 0;
         mbar_fence_init();
     }
@@ -822,11 +929,15 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     pdl_wait();
     const uint32_t tmem = *tmem_slot;
     if (warp < NS_EPI_WARPS) {
-        ns_epilogue(p, sm, tmem, abort_flag);
+        ns_epilogue(p, sm, tmem, abort_flag, go);
     } else if (warp == NS_WARP_LOAD) {
         if (elect_one()) ns_producer(p, sm, abort_flag);
-    } else {
+    } else if (warp == NS_WARP_MMA) {
         if (sm.rank == 0 && elect_one()) ns_mma(p, sm, tmem, abort_flag);
+    } else if (warp == NS_WARP_IN) {
+        if (elect_one()) ns_inputs(p, sm, abort_flag);
+    } else if (warp == NS_WARP_OUT) {
+        if (elect_one()) ns_outputs(p, sm, abort_flag);
     }
     __syncwarp();
     tc_fence_before();
@@ -950,14 +1061,6 @@ __global__ void __launch_bounds__(NS_THIN_THREADS) ns_thin_kernel(const __grid_c
         }
         __syncthreads();
     }
-}
-
-// Width of the n-tiles of an output of n columns: as few tiles as 256-wide MMAs allow, of equal
-// width, a multiple of 32 (each CTA of a pair holds half of the columns).
-void ns_tiles(int n, int* bn, int* nt) {
-    const int t = (n + NS_MAXBN - 1) / NS_MAXBN;
-    *bn = ((n + t - 1) / t + 31) / 32 * 32;
-    *nt = (n + *bn - 1) / *bn;
 }
 
 inline int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
@@ -1121,13 +1224,19 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
         ok = ok && make_weight_tmap_strided(&a.tA[i], a.A[i], a.m, a.m, L.slots, a.ldm, (int64_t)a.m * a.ldm) &&
              make_weight_tmap_strided(&a.tB[i], a.B[i], a.m, a.m, L.slots, a.ldm, (int64_t)a.m * a.ldm);
     }
+    if (a.O && a.vec_o)
+        ok = ok && make_weight_tmap_strided(&a.tO, a.O, a.c, a.r, a.N, a.ld_o, a.N > 1 ? a.st_o : (int64_t)a.r * a.ld_o);
     if (!ok) return cudaErrorInvalidValue;
-    ns_tiles(a.m, &a.bn_s, &a.nt_s);
-    ns_tiles(a.c, &a.bn_x, &a.nt_x);
+    // 256-column tiles, narrower ones where the matrices under way have fewer than there are pairs
     a.mt_s = (a.m + NS_BM - 1) / NS_BM;
     a.mt_x = (a.r + NS_BM - 1) / NS_BM;
+    for (a.bn = NS_MAXBN;; a.bn /= 2) {
+        a.nt_s = (a.m + a.bn - 1) / a.bn;
+        a.nt_x = (a.c + a.bn - 1) / a.bn;
+        if (a.bn == 64 || L.slots * a.mt_x * a.nt_x >= sms / 2) break;
+    }
     int sym = 0;
-    for (int i = 0; i < a.mt_s; ++i) sym += a.nt_s - i * NS_BM / a.bn_s;
+    for (int i = 0; i < a.mt_s; ++i) sym += a.nt_s - i * (NS_BM / a.bn);
     a.tiles[NS_GRAM] = a.tiles[NS_POLY] = sym;
     a.tiles[NS_APPLY] = a.mt_x * a.nt_x;
     int64_t items = 0;
