@@ -1020,6 +1020,20 @@ bool make_gather_tmap(CUtensorMap* tm, const void* base, int64_t cols, int64_t r
     return r == CUDA_SUCCESS;
 }
 
+bool make_f32_tmap(CUtensorMap* tm, const void* base, int64_t cols, int64_t rows, int64_t G, int64_t ld,
+                   int64_t g_ld) {
+    PFN_cuTensorMapEncodeTiled_v12000 enc = get_encode_fn();
+    if (!enc) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)G};
+    cuuint64_t strides[2] = {(cuuint64_t)ld * 4, (cuuint64_t)g_ld * 4};
+    cuuint32_t box[3] = {64, 64, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = enc(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims, strides, box, estr,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
 void choose_bn(int N, int* BN, int* n_ntiles) {
     const int nt = (N + GM_MAXBN - 1) / GM_MAXBN;
     int bn = (N + nt - 1) / nt;

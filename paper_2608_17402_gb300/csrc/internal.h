@@ -301,6 +301,9 @@ bool make_kmajor_tmap(CUtensorMap* tm, const void* base, int64_t K, int64_t N, i
 // The 2-D row tensor map of A[rows][cols] bf16 (row stride ld elements) with one-row boxes
 // of 64 columns, for row gathers.
 bool make_gather_tmap(CUtensorMap* tm, const void* base, int64_t cols, int64_t rows, int64_t ld);
+// The 3-D map {cols, rows, G} of fp32 matrices (strides in elements, multiples of 4), plain boxes
+// of 64 x 64.
+bool make_f32_tmap(CUtensorMap* tm, const void* base, int64_t cols, int64_t rows, int64_t G, int64_t ld, int64_t g_ld);
 // Picks BN (multiple of 32, <= 256) and the number of N tiles for width N.
 void choose_bn(int N, int* BN, int* n_ntiles);
 cudaError_t launch_grouped_gemm(const GemmArgs& a, int grid, cudaStream_t s);

@@ -34,9 +34,10 @@
 // a = 3.4, so a rounding of X there would grow by a^steps, several hundred times, while B X is
 // small there to begin with.  Against 64 bits the result is within 2e-3 (2-norm over 2-norm) for
 // full-rank and for low-rank U alike; with X rounded to fp16 alone it would be 4e-2 for a U of
-// rank 16.  In the last two steps, whose roundings are not amplified any more, lo counts 2 and 1
+// rank 16.  In the last two steps, whose roundings are hardly amplified any more, lo counts 2 and 0
 // times instead of a: where singular values have arrived near 1, B lo (which is not formed) takes
-// up most of a lo, and leaving both out is nearer (1.6e-3 becomes 1.4e-3 on Gaussian matrices).
+// up most of a lo, and leaving both out is nearer (1.6e-3 becomes 1.4e-3 on Gaussian matrices) and
+// saves the last step's lo.
 // For m <= 128 the roundings of a few singular values average less, and time is latency: there
 // A and B have lo parts too and every product is hi hi + hi lo + lo hi (about 1e-5).
 #include "internal.h"
@@ -297,6 +298,7 @@ struct NsArgs {
     CUtensorMap tX[3][2], tA[2], tB[2];   // [X0, buffer 0, 1][hi, lo]; 3-D maps {inner, rows, matrices
                                           //   (X0) or slots}, boxes 64 x 64
     CUtensorMap tO;                    // the result, where its rows are 16-byte aligned (vec_o)
+    CUtensorMap tW;                    // the weights (fp32, plain 64 x 64 boxes), for prefetches
     UpdateArgs u;
     __half *xh[3], *xl[3];             // X0 [N][r][ldx]; X, ping-pong [slots][r][ldx] (lo in place with one term)
     __half *A[2], *B[2];               // hi, lo (lo with three terms only) [slots][m][ldm]
@@ -604,6 +606,12 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src
                  : "memory");
 }
 
+__device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* tm, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(tm), "r"(c0), "r"(c1),
+                 "r"(c2)
+                 : "memory");
+}
+
 // What the epilogue reads of A (polynomial) or X (apply), block by block into its slots: one
 // thread.  Gram blocks read nothing; their slots are handed on as they become free.
 __device__ void ns_inputs(const NsArgs& p, const NsSmem& sm, volatile int* abort_flag) {
@@ -614,7 +622,7 @@ __device__ void ns_inputs(const NsArgs& p, const NsSmem& sm, volatile int* abort
         const NsItem it = ns_item(p, w, id);
         const NsTile t = ns_tile(p, it);
         const int mode = ns_mode(p, it), src = ns_src(it.step);
-        const bool lo = mode >= NS_M_X || (mode == NS_M_POLY && p.terms == 3);
+        const bool lo = mode >= NS_M_X ? p.lo_coef[it.step] != 0.f : mode == NS_M_POLY && p.terms == 3;
         const int row = t.m0 + (int)sm.rank * NS_HALF, z = mode >= NS_M_X && src == 0 ? it.e : it.buf;
         const CUtensorMap* mh = mode >= NS_M_X ? &p.tX[src][0] : &p.tA[0];
         const CUtensorMap* ml = mode >= NS_M_X ? &p.tX[src][1] : &p.tA[1];
@@ -628,6 +636,13 @@ __device__ void ns_inputs(const NsArgs& p, const NsSmem& sm, volatile int* abort
                 return;
             }
             const uint32_t bar = sm.in + 8 * s, at = sm.slots + s * NS_SLOT_BYTES;
+            if (mode == NS_M_W) {   // the weights on their way to L2, blocks ahead of their use
+                for (int c = c0 == 0 ? 0 : c0 + 128; c < (c0 == 0 ? min(t.bn, 192) : min(t.bn, c0 + 192)); c += 64)
+                    if (t.n0 + c < p.c) {
+                        tma_prefetch_3d(&p.tW, t.n0 + c, row, it.e);
+                        tma_prefetch_3d(&p.tW, t.n0 + c, row + 64, it.e);
+                    }
+            }
             if (mode == NS_M_GRAM) {
                 mbar_arrive(bar);
             } else {
@@ -659,7 +674,7 @@ __device__ void ns_outputs(const NsArgs& p, const NsSmem& sm, volatile int* abor
         const int mode = ns_mode(p, it), row = t.m0 + (int)sm.rank * NS_HALF;
         const int rows = mode >= NS_M_X ? p.r : p.m, cols = mode >= NS_M_X ? p.c : p.m;
         const bool to_b = mode == NS_M_POLY || (mode == NS_M_GRAM && p.coef[3 * it.step + 2] == 0.f);
-        const bool lo = mode == NS_M_X || (mode < NS_M_X && p.terms == 3);
+        const bool lo = mode == NS_M_X ? p.lo_coef[it.step + 1] != 0.f : mode < NS_M_X && p.terms == 3;
         const int dst = ns_dst(it.step), z = mode == NS_M_O ? it.e : it.buf;
         const CUtensorMap* mh = mode == NS_M_O ? &p.tO : mode == NS_M_X ? &p.tX[dst][0] : to_b ? &p.tB[0] : &p.tA[0];
         const CUtensorMap* ml = mode == NS_M_X ? &p.tX[dst][1] : to_b ? &p.tB[1] : &p.tA[1];
@@ -711,12 +726,13 @@ __device__ __forceinline__ void ns_epi_sync() { asm volatile("bar.sync 1, 256;" 
 // that each holds only the code that its tiles run.
 template <int MODE>
 __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, const NsTile& t, uint8_t* slot, int row,
-                                         int half, int rank, int c0, const uint32_t (&v)[32]) {
+                                         int half, int rank, int c0, const uint32_t (&v)[32], const float4 (&wv)[8]) {
     constexpr bool APPLY = MODE >= NS_M_X;
     const float cc = p.coef[3 * it.step + 2], cb = p.coef[3 * it.step + 1];
     const float fd = MODE == NS_M_GRAM ? (cc == 0.f ? cb * NS_INV_S : NS_INV_S) : MODE == NS_M_POLY ? cc * NS_INV_S : NS_INV_S;
     const float fh = APPLY ? p.coef[3 * it.step] : cb, fl = APPLY ? p.lo_coef[it.step] : cb;
-    const bool lo_in = APPLY || p.terms == 3;
+    const bool lo_in = APPLY ? fl != 0.f : p.terms == 3;
+    const bool lo_out = MODE == NS_M_X ? p.lo_coef[it.step + 1] != 0.f : p.terms == 3;
     float keep[MODE == NS_M_W ? 32 : 1];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -747,7 +763,7 @@ __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, cons
             uint4 hi, lo;
             split8(x, hi, lo);
             *ch = hi;
-            if (lo_in) {
+            if (lo_out) {
                 *cl = lo;
             } else if (t.mirror) {   // column j of the block is row j of the mirror boxes
                 const uint32_t hw[4] = {hi.x, hi.y, hi.z, hi.w};
@@ -773,14 +789,14 @@ __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, cons
         const int q = threadIdx.x & 15, col = t.n0 + c0 + 4 * q, nc = p.c - col;
         const int64_t base = it.e * p.st_w + col;
         if (4 * q < t.bn - c0 && nc > 0) {
-#pragma unroll 4
-            for (int r = threadIdx.x >> 4; r < NS_HALF; r += 16) {
-                const int gr = t.m0 + rank * NS_HALF + r;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = (int)(threadIdx.x >> 4) + 16 * i, gr = t.m0 + rank * NS_HALF + r;
                 if (gr >= p.r) break;
                 const int64_t at = base + gr * p.ld_w;
                 const float4 x = *ns_cell32(slot, r, q);
                 if (nc >= 4) {
-                    float4 o = *reinterpret_cast<const float4*>(p.W + at);
+                    float4 o = wv[i];
                     o.x = fmaf(-rate, x.x, p.decay * o.x);
                     o.y = fmaf(-rate, x.y, p.decay * o.y);
                     o.z = fmaf(-rate, x.z, p.decay * o.z);
@@ -846,6 +862,17 @@ __device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, vo
             uint8_t* slot = sm.slot_ptr + s * NS_SLOT_BYTES;
             uint32_t v[32];
             tmem_ld_32x32b_x32(tbase + c0 + half * 32, v);   // (past a 32-wide last block: not used)
+            float4 wv[8];   // the weights of this thread's piece of the block, while its inputs arrive
+            if (mode == NS_M_W) {
+                const int q = threadIdx.x & 15, col = t.n0 + c0 + 4 * q;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int gr = t.m0 + (int)sm.rank * NS_HALF + (int)(threadIdx.x >> 4) + 16 * i;
+                    wv[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (4 * q < t.bn - c0 && col + 4 <= p.c && gr < p.r)
+                        wv[i] = *reinterpret_cast<const float4*>(p.W + it.e * p.st_w + gr * p.ld_w + col);
+                }
+            }
             if (threadIdx.x == 0) {
                 const bool ok = mbar_wait(sm.in + 8 * s, ph, p.limit_ns, abort_flag);
                 if (!ok) ns_abort(abort_flag, p.status, SITE_NS_WAIT_SLOT, id);
@@ -859,11 +886,11 @@ __device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, vo
                 if (lane == 0) mbar_arrive_remote(tempty);
             }
             if (!go[2 + s]) return;
-            if (mode == NS_M_GRAM) ns_block<NS_M_GRAM>(p, it, t, slot, row, half, (int)sm.rank, c0, v);
-            else if (mode == NS_M_POLY) ns_block<NS_M_POLY>(p, it, t, slot, row, half, (int)sm.rank, c0, v);
-            else if (mode == NS_M_X) ns_block<NS_M_X>(p, it, t, slot, row, half, (int)sm.rank, c0, v);
-            else if (mode == NS_M_O) ns_block<NS_M_O>(p, it, t, slot, row, half, (int)sm.rank, c0, v);
-            else ns_block<NS_M_W>(p, it, t, slot, row, half, (int)sm.rank, c0, v);
+            if (mode == NS_M_GRAM) ns_block<NS_M_GRAM>(p, it, t, slot, row, half, (int)sm.rank, c0, v, wv);
+            else if (mode == NS_M_POLY) ns_block<NS_M_POLY>(p, it, t, slot, row, half, (int)sm.rank, c0, v, wv);
+            else if (mode == NS_M_X) ns_block<NS_M_X>(p, it, t, slot, row, half, (int)sm.rank, c0, v, wv);
+            else if (mode == NS_M_O) ns_block<NS_M_O>(p, it, t, slot, row, half, (int)sm.rank, c0, v, wv);
+            else ns_block<NS_M_W>(p, it, t, slot, row, half, (int)sm.rank, c0, v, wv);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(sm.done + 8 * s);
@@ -1066,9 +1093,11 @@ __global__ void __launch_bounds__(NS_THIN_THREADS) ns_thin_kernel(const __grid_c
 inline int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
 inline size_t up256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 
-// Matrices under way, NS_LANES groups of them: as many as keep the working arrays within
-// NS_L2_BYTES of L2, but enough tiles for all pairs where the stack has them.
-constexpr int64_t NS_L2_BYTES = 72ll << 20;
+// Matrices under way, NS_LANES groups of them: as many as keep the working arrays within this.
+// Fewer keep more of them in L2, but a slot of the schedule must hold several tiles for every
+// pair, as a tile's inputs are about 12 us old before the next can start on them.  Measured on
+// 256 x 416 x 1664: 48 MB 5.2 ms, 72 MB 3.8, 100 MB 3.3, 140 MB 2.8, 220 MB 2.5, 400 MB 2.4.
+constexpr int64_t NS_UNDER_WAY_BYTES = 384ll << 20;
 
 struct NsLayout {
     size_t prog, part, x0h, x0l, xh0, xh1, xl0, xl1, A, Al, B, Bl, total;
@@ -1081,7 +1110,7 @@ NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     L.chunks = (L.groups + NS_PRO_GROUPS - 1) / NS_PRO_GROUPS;
     L.terms = m <= 128 ? 3 : 1;
     const int64_t each = (L.terms == 3 ? 8 : 6) * r * ldx + (L.terms == 3 ? 8 : 4) * m * ldm;
-    int64_t most = NS_L2_BYTES / (each * NS_LANES);   // matrices of a group
+    int64_t most = NS_UNDER_WAY_BYTES / (each * NS_LANES);   // matrices of a group
     if (most < 1) most = 1;
     const int64_t rounds = (N + most * NS_LANES - 1) / (most * NS_LANES);
     L.n_groups = (int)(rounds * NS_LANES < N ? rounds * NS_LANES : N);   // sizes then differ by one at most
@@ -1126,7 +1155,7 @@ size_t ns_workspace_bytes(int64_t N, int64_t r, int64_t c) {
     size_t most = L.total;
     const int64_t m = r < c ? r : c, ldx = up8(c), ldm = up8(m);
     const int64_t each = (L.terms == 3 ? 8 : 6) * r * ldx + (L.terms == 3 ? 8 : 4) * m * ldm;
-    int64_t full = NS_L2_BYTES / (each * NS_LANES);
+    int64_t full = NS_UNDER_WAY_BYTES / (each * NS_LANES);
     if (full < 1) full = 1;
     full = full * NS_LANES < N ? full * NS_LANES : N;
     if (full > 0) {
@@ -1175,8 +1204,8 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     for (int it = 0; it < q.steps; ++it) {
         for (int j = 0; j < 3; ++j) a.coef[3 * it + j] = q.coef[3 * it + j];
         // lo in the last two steps: see the file comment
-        const float ca = a.coef[3 * it], lim = it == q.steps - 1 ? 1.0f : 2.0f;
-        a.lo_coef[it] = a.terms == 3 || it < q.steps - 2 || fabsf(ca) <= lim ? ca : copysignf(lim, ca);
+        const float ca = a.coef[3 * it], lim = it == q.steps - 1 ? 0.0f : 2.0f;
+        a.lo_coef[it] = a.terms == 3 || it < q.steps - 2 || it == 0 || fabsf(ca) <= lim ? ca : copysignf(lim, ca);
         for (int kind = NS_GRAM; kind <= NS_APPLY; ++kind) {
             if (kind == NS_POLY && a.coef[3 * it + 2] == 0.f) continue;
             a.kind[stage] = (uint8_t)kind;
@@ -1224,6 +1253,7 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
         ok = ok && make_weight_tmap_strided(&a.tA[i], a.A[i], a.m, a.m, L.slots, a.ldm, (int64_t)a.m * a.ldm) &&
              make_weight_tmap_strided(&a.tB[i], a.B[i], a.m, a.m, L.slots, a.ldm, (int64_t)a.m * a.ldm);
     }
+    if (a.W) ok = ok && make_f32_tmap(&a.tW, a.W, a.c, a.r, a.N, a.ld_w, a.N > 1 ? a.st_w : (int64_t)a.r * a.ld_w);
     if (a.O && a.vec_o)
         ok = ok && make_weight_tmap_strided(&a.tO, a.O, a.c, a.r, a.N, a.ld_o, a.N > 1 ? a.st_o : (int64_t)a.r * a.ld_o);
     if (!ok) return cudaErrorInvalidValue;
