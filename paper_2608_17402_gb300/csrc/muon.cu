@@ -8,9 +8,9 @@
 // U from the momentum on the way in and applies the result to the weights on the way out.
 //
 // Kernels
-//   muon_moment_kernel  one pass over the gradient: momentum update (M <- mu M + G) and, per
-//                       chunk, partial sums of squares of U.  Bound by memory.
-//   muon_scale_kernel   X0 in the working format from U and its norm.  Bound by memory.
+//   muon_update_kernel  momentum update (M <- mu M + G), |U|, and X0 in the working format, a
+//                       cluster of CTAs per matrix.  Bound by memory.  For few matrices,
+//   muon_moment_kernel  and muon_scale_kernel do the same in two passes of all SMs.
 //   ns_kernel           the three products of every step on tcgen05 CTA pairs in one persistent
 //                       launch, with the output or the weight update in the last one's epilogue.
 //   ns_thin_kernel      all of that for matrices whose smaller side is at most 32, in fp32.
@@ -133,17 +133,15 @@ struct UpdateArgs {
     int32_t* prog;        // progress counters of the matrices, cleared here
 };
 
+// Sums of squares of the update over groups [g0, g1) of matrix e, by the whole CTA (threads 0..2
+// get them); with a momentum, M is brought up to date on the way.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(NS_PRO_THREADS) muon_moment_kernel(const __grid_constant__ UpdateArgs p) {
-    pdl_wait();
-    const int e = blockIdx.y;
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.prog[e] = 0;
-    const int g0 = blockIdx.x * NS_PRO_GROUPS, g1 = min(g0 + NS_PRO_GROUPS, p.groups);
+__device__ __forceinline__ float update_squares(const UpdateArgs& p, int e, int g0, int g1) {
     const T* U = static_cast<const T*>(p.U) + e * p.st_u;
     float* M = p.M ? p.M + e * p.st_u : nullptr;
     float s0 = 0.f, s1 = 0.f, s2 = 0.f;
 #pragma unroll 2
-    for (int g = g0 + (int)threadIdx.x; g < g1; g += NS_PRO_THREADS) {
+    for (int g = g0 + (int)threadIdx.x; g < g1; g += (int)blockDim.x) {
         const int row = g / p.gpr, col = (g - row * p.gpr) * 8, n = p.c - col;
         const int64_t at = row * p.ld_u + col;
         float v[8];
@@ -165,7 +163,7 @@ __global__ void __launch_bounds__(NS_PRO_THREADS) muon_moment_kernel(const __gri
             s2 = fmaf(u, u, s2);
         }
     }
-    __shared__ float red[3][NS_PRO_THREADS / 32];
+    __shared__ float red[3][32];
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         s0 += __shfl_xor_sync(0xffffffffu, s0, o);
@@ -179,11 +177,34 @@ __global__ void __launch_bounds__(NS_PRO_THREADS) muon_moment_kernel(const __gri
         red[2][warp] = s2;
     }
     __syncthreads();
-    if (threadIdx.x < 3) {
-        float s = 0.f;
-        for (int w = 0; w < NS_PRO_THREADS / 32; ++w) s += red[threadIdx.x][w];
-        p.part[((int64_t)e * p.chunks + blockIdx.x) * 3 + threadIdx.x] = s;
+    float s = 0.f;
+    if (threadIdx.x < 3)
+        for (int w = 0; w < (int)blockDim.x / 32; ++w) s += red[threadIdx.x][w];
+    return s;
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(NS_PRO_THREADS) muon_moment_kernel(const __grid_constant__ UpdateArgs p) {
+    pdl_wait();
+    const int e = blockIdx.y;
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.prog[e] = 0;
+    const int g0 = blockIdx.x * NS_PRO_GROUPS;
+    const float s = update_squares<T, VEC>(p, e, g0, min(g0 + NS_PRO_GROUPS, p.groups));
+    if (threadIdx.x < 3) p.part[((int64_t)e * p.chunks + blockIdx.x) * 3 + threadIdx.x] = s;
+}
+
+// The factors of X0 = (v * pre) * post from the three sums of squares of a matrix.
+__device__ __forceinline__ void scales_of(float s0, float s1, float s2, float& pre, float& post) {
+    float s = s0;
+    pre = 1.f;
+    if (isinf(s0)) {
+        s = s1;
+        pre = NS_DOWN;
+    } else if (s0 < NS_TINY) {
+        s = s2;
+        pre = NS_UP;
     }
+    post = s == 0.f ? 0.f : 1.0f / sqrtf(s);   // a zero matrix stays zero; NaN stays NaN
 }
 
 // X0 = (v * pre) * post from the matrix's partial sums, by one warp (every lane gets the result;
@@ -202,16 +223,7 @@ __device__ __forceinline__ void norm_scales(const UpdateArgs& u, int e, float& p
         s1 += __shfl_xor_sync(0xffffffffu, s1, o);
         s2 += __shfl_xor_sync(0xffffffffu, s2, o);
     }
-    float s = s0;
-    pre = 1.f;
-    if (isinf(s0)) {
-        s = s1;
-        pre = NS_DOWN;
-    } else if (s0 < NS_TINY) {
-        s = s2;
-        pre = NS_UP;
-    }
-    post = s == 0.f ? 0.f : 1.0f / sqrtf(s);   // a zero matrix stays zero; NaN stays NaN
+    scales_of(s0, s1, s2, pre, post);
 }
 
 // Eight values of the update U of matrix e (n of them exist).
@@ -240,18 +252,12 @@ __device__ __forceinline__ void update8(const UpdateArgs& u, int e, int row, int
     }
 }
 
-// X0 = U / |U| in the working format.
-__global__ void __launch_bounds__(NS_PRO_THREADS) muon_scale_kernel(const __grid_constant__ UpdateArgs u, __half* xh,
-                                                                    __half* xl) {
-    pdl_wait();
-    const int e = blockIdx.y;
-    float pre, post;
-    norm_scales(u, e, pre, post);
-    post *= NS_S;
-    const int g0 = blockIdx.x * NS_PRO_GROUPS, g1 = min(g0 + NS_PRO_GROUPS, u.groups);
+// Groups [g0, g1) of X0 = U / |U| in the working format.
+__device__ __forceinline__ void scale_groups(const UpdateArgs& u, int e, int g0, int g1, float pre, float post,
+                                             __half* xh, __half* xl) {
     const int64_t base = (int64_t)e * u.groups * 8;
 #pragma unroll 2
-    for (int g = g0 + (int)threadIdx.x; g < g1; g += NS_PRO_THREADS) {
+    for (int g = g0 + (int)threadIdx.x; g < g1; g += (int)blockDim.x) {
         const int row = g / u.gpr, col = (g - row * u.gpr) * 8;
         float v[8];
         update8(u, e, row, col, u.c - col, v);
@@ -262,6 +268,48 @@ __global__ void __launch_bounds__(NS_PRO_THREADS) muon_scale_kernel(const __grid
         *reinterpret_cast<uint4*>(xh + base + (int64_t)g * 8) = hi;
         *reinterpret_cast<uint4*>(xl + base + (int64_t)g * 8) = lo;
     }
+}
+
+__global__ void __launch_bounds__(NS_PRO_THREADS) muon_scale_kernel(const __grid_constant__ UpdateArgs u, __half* xh,
+                                                                    __half* xl) {
+    pdl_wait();
+    const int e = blockIdx.y;
+    float pre, post;
+    norm_scales(u, e, pre, post);
+    const int g0 = blockIdx.x * NS_PRO_GROUPS;
+    scale_groups(u, e, g0, min(g0 + NS_PRO_GROUPS, u.groups), pre, post * NS_S, xh, xl);
+}
+
+// Both passes in one launch, a cluster of 8 CTAs per matrix: the sums are exchanged through
+// distributed shared memory (added in CTA order), and the second read of a CTA's eighth of the
+// matrix comes from L2, where the first has just brought it: one CTA of 1024 threads per SM, so
+// that what all of them are at (256 x 416 x 1664: 53 MB) stays there.
+constexpr int NS_PRO_CLUSTER = 8, NS_PRO_CTHREADS = 1024;
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(NS_PRO_CTHREADS, 1) muon_update_kernel(const __grid_constant__ UpdateArgs p, __half* xh,
+                                                                     __half* xl) {
+    pdl_wait();
+    __shared__ float mine[3], scale[2];
+    const int e = blockIdx.x / NS_PRO_CLUSTER, rank = blockIdx.x % NS_PRO_CLUSTER;
+    if (rank == 0 && threadIdx.x == 0) p.prog[e] = 0;
+    const int each = (p.groups + NS_PRO_CLUSTER - 1) / NS_PRO_CLUSTER;
+    const int g0 = min(rank * each, p.groups), g1 = min(g0 + each, p.groups);
+    const float s = update_squares<T, VEC>(p, e, g0, g1);
+    if (threadIdx.x < 3) mine[threadIdx.x] = s;
+    cluster_sync();
+    if (threadIdx.x == 0) {
+        float t[3] = {};
+        for (int r = 0; r < NS_PRO_CLUSTER; ++r)
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                float v;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer_addr(smem_u32(mine + i), r)));
+                t[i] += v;
+            }
+        scales_of(t[0], t[1], t[2], scale[0], scale[1]);
+    }
+    cluster_sync();   // (also: nobody leaves while its sums are being read)
+    scale_groups(p, e, g0, g1, scale[0], scale[1] * NS_S, xh, xl);
 }
 
 // ------------------------------------------------------------------ products
@@ -400,6 +448,7 @@ __device__ __forceinline__ int ns_dst(int s) { return 1 + (s & 1); }
 struct NsTile {
     int m0, n0, bn, num_kb;            // num_kb: K blocks of one term
     bool mirror;                       // symmetric output: also write its mirror image
+    bool same;                         // A's and B's shares of each CTA are the same box: loaded once
     const CUtensorMap *a[2], *b[2];    // operands, hi and lo
     int za, zb;                        // their matrix or slot
     bool a_mn, b_mn;
@@ -420,7 +469,7 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
         t.m0 = i * NS_BM;
         t.n0 = (it.tile - i * p.nt_x) * p.bn;
         cols = p.c;
-        t.mirror = false;
+        t.mirror = t.same = false;
         t.a_mn = false;
         t.b_mn = !p.tall;
         t.za = p.tall && src == 0 ? it.e : it.buf;
@@ -448,6 +497,8 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
         for (int j = 0; j < 2; ++j) t.a[j] = t.b[j] = gram ? &p.tX[src][j] : &p.tA[j];
     }
     t.bn = min(p.bn, (cols - t.n0 + 31) & ~31);   // a multiple of 32: each CTA holds half of B
+    // a 256-wide tile on the diagonal: rows and columns of a CTA coincide
+    if (it.kind != NS_APPLY) t.same = t.n0 == t.m0 && t.bn == NS_BM && p.terms == 1;
     t.num_kb = (k + NS_BK - 1) / NS_BK;
     return t;
 }
@@ -501,7 +552,7 @@ __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abo
                          : it.prev >= 0 && !ns_wait(p, it.prev, p.need[p.n_stages], abort_flag, SITE_NS_WAIT_BUFFER))
             return;
         fence_proxy_async_all();   // the inputs were written by ordinary stores
-        const int nbox = (t.bn / 2 + 63) / 64;
+        const int nbox = t.same ? 0 : (t.bn / 2 + 63) / 64;
         const uint32_t bytes = 2u * (uint32_t)(2 + nbox) * NS_BOX;
         const int mm = t.m0 + (int)sm.rank * NS_HALF, nn = t.n0 + (int)sm.rank * (t.bn / 2);
         for (int term = 0; term < p.terms; ++term) {
@@ -541,7 +592,7 @@ __device__ __forceinline__ void ns_mma(const NsArgs& p, const NsSmem& sm, uint32
         const NsTile t = ns_tile(p, it);
         const uint32_t idesc = idesc_f16_f32(NS_BM, t.bn, t.a_mn, t.b_mn);
         const uint64_t ad0 = smem_desc_sw128(sm.ring, t.a_mn ? NS_BOX : 16, 1024);
-        const uint64_t bd0 = smem_desc_sw128(sm.ring + 2 * NS_BOX, t.b_mn ? NS_BOX : 16, 1024);
+        const uint64_t bd0 = smem_desc_sw128(sm.ring + (t.same ? 0 : 2 * NS_BOX), t.b_mn ? NS_BOX : 16, 1024);
         const uint32_t as = (t.a_mn ? 2048 : 32) >> 4, bs = (t.b_mn ? 2048 : 32) >> 4;
         const int acc = n & 1;
         if (!mbar_wait(sm.tempty + 8 * acc, ((uint32_t)(n >> 1) & 1u) ^ 1u, p.limit_ns, abort_flag)) {
@@ -1141,9 +1192,37 @@ NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     return L;
 }
 
+// The update's norms (and momentum), and X0 unless the matrices are thin.  One launch with a
+// cluster per matrix where there are matrices enough for all SMs and what the SMs are at stays in
+// L2, else two launches over all of them (steps on 64 x 1024 x 512: 562 us against 587; on
+// 256 x 1664 x 416, 105 MB at a time: 2.93 ms against 2.91).
+constexpr int64_t NS_PRO_L2_BYTES = 88ll << 20;
 template <typename T, bool VEC>
-cudaError_t launch_moment(const UpdateArgs& p, int N, cudaStream_t s) {
-    return launch_pdl(muon_moment_kernel<T, VEC>, dim3((unsigned)p.chunks, (unsigned)N), dim3(NS_PRO_THREADS), 0, s, p);
+cudaError_t launch_prologue(const UpdateArgs& p, int N, bool thin, __half* xh, __half* xl, int sms, cudaStream_t s) {
+    const int64_t each = (int64_t)p.groups * 8 / NS_PRO_CLUSTER * ((int)sizeof(T) + (p.M ? 4 : 0));   // bytes of a CTA
+    if (!thin && N * NS_PRO_CLUSTER >= sms && each * sms <= NS_PRO_L2_BYTES) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(N * NS_PRO_CLUSTER));
+        cfg.blockDim = dim3(NS_PRO_CTHREADS);
+        cfg.stream = s;
+        cudaLaunchAttribute at[2];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = NS_PRO_CLUSTER;
+        at[0].val.clusterDim.y = 1;
+        at[0].val.clusterDim.z = 1;
+        at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see launch_pdl
+        at[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 2;
+        count_launches(1);
+        return cudaLaunchKernelEx(&cfg, muon_update_kernel<T, VEC>, p, xh, xl);
+    }
+    const dim3 grid((unsigned)p.chunks, (unsigned)N);
+    cudaError_t e = launch_pdl(muon_moment_kernel<T, VEC>, grid, dim3(NS_PRO_THREADS), 0, s, p);
+    count_launches(1);
+    if (e != cudaSuccess || thin) return e;
+    count_launches(1);
+    return launch_pdl(muon_scale_kernel, grid, dim3(NS_PRO_THREADS), 0, s, p, xh, xl);
 }
 
 }  // namespace
@@ -1193,10 +1272,16 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.u.chunks = L.chunks;
     a.u.part = reinterpret_cast<float*>(ws + L.part);
     a.u.prog = reinterpret_cast<int32_t*>(ws + L.prog);
+    a.xh[0] = reinterpret_cast<__half*>(ws + L.x0h);
+    a.xl[0] = reinterpret_cast<__half*>(ws + L.x0l);
+    const bool thin = a.m <= NS_THIN;
     cudaError_t e;
-    if (q.u_bf16) e = a.u.vec ? launch_moment<__nv_bfloat16, true>(a.u, q.N, s) : launch_moment<__nv_bfloat16, false>(a.u, q.N, s);
-    else e = a.u.vec ? launch_moment<float, true>(a.u, q.N, s) : launch_moment<float, false>(a.u, q.N, s);
-    count_launches(1);
+    if (q.u_bf16)
+        e = a.u.vec ? launch_prologue<__nv_bfloat16, true>(a.u, q.N, thin, a.xh[0], a.xl[0], sms, s)
+                    : launch_prologue<__nv_bfloat16, false>(a.u, q.N, thin, a.xh[0], a.xl[0], sms, s);
+    else
+        e = a.u.vec ? launch_prologue<float, true>(a.u, q.N, thin, a.xh[0], a.xl[0], sms, s)
+                    : launch_prologue<float, false>(a.u, q.N, thin, a.xh[0], a.xl[0], sms, s);
     if (e != cudaSuccess) return e;
 
     a.steps = q.steps;
@@ -1225,21 +1310,15 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.rate = q.rate;
     a.status = reinterpret_cast<DevStatus*>(ws);
     a.limit_ns = limit_ns;
-    if (a.m <= NS_THIN) {
+    if (thin) {
         e = launch_pdl(ns_thin_kernel, dim3((unsigned)a.N), dim3(NS_THIN_THREADS), 0, s, a);
         count_launches(1);
         return e != cudaSuccess ? e : cudaGetLastError();
     }
-    a.xh[0] = reinterpret_cast<__half*>(ws + L.x0h);
-    a.xl[0] = reinterpret_cast<__half*>(ws + L.x0l);
     a.xh[1] = reinterpret_cast<__half*>(ws + L.xh0);
     a.xh[2] = reinterpret_cast<__half*>(ws + L.xh1);
     a.xl[1] = reinterpret_cast<__half*>(ws + L.xl0);
     a.xl[2] = reinterpret_cast<__half*>(ws + L.xl1);
-    e = launch_pdl(muon_scale_kernel, dim3((unsigned)L.chunks, (unsigned)a.N), dim3(NS_PRO_THREADS), 0, s, a.u, a.xh[0],
-                   a.xl[0]);
-    count_launches(1);
-    if (e != cudaSuccess) return e;
     a.A[0] = reinterpret_cast<__half*>(ws + L.A);
     a.A[1] = reinterpret_cast<__half*>(ws + L.Al);
     a.B[0] = reinterpret_cast<__half*>(ws + L.B);
