@@ -964,6 +964,15 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
             if (p.W3) tma_prefetch_desc(&p.tS3);
         }
     }
+    __syncwarp();
+    if (warp == FEW_WARP_MMA) {
+        tmem_alloc(smem_u32(tmem_slot), p.tmem_cols);
+        tmem_relinquish();
+    }
+    auto give_up = [&]() {   // a grid barrier timed out (all threads): nothing but TMEM is held
+        __syncthreads();
+        if (warp == FEW_WARP_MMA) tmem_dealloc(*tmem_slot, p.tmem_cols);
+    };
     pdl_wait();
     // counters of this call, used only after the grid barrier
     for (int i = blockIdx.x * FEW_THREADS + threadIdx.x; i < p.n_counters; i += gridDim.x * FEW_THREADS)
@@ -978,7 +987,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
         const float v = few_norm(p, t0 + warp * step);
         if ((threadIdx.x & 31) == 0) xn[warp] = v;
     }
-    if (!few_barrier(p.status, p.limit_ns)) return;
+    if (!few_barrier(p.status, p.limit_ns)) return give_up();
     if (everywhere) {
         int32_t* s_idx = reinterpret_cast<int32_t*>(smem + p.T * sel_bytes);
         float* s_gate = reinterpret_cast<float*>(s_idx + n);
@@ -1000,13 +1009,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
             few_select(p, t0 + i * step, step, min(most, mine - i), xn, smem, p.idx, p.gate);
             __syncthreads();
         }
-        if (!few_barrier(p.status, p.limit_ns)) return;
+        if (!few_barrier(p.status, p.limit_ns)) return give_up();
         few_plan<false>(p, L, p.idx, p.gate, smem);
-    }
-    __syncwarp();
-    if (warp == FEW_WARP_MMA) {
-        tmem_alloc(smem_u32(tmem_slot), p.tmem_cols);
-        tmem_relinquish();
     }
     fence_proxy_async_smem();   // the router's use of the ring, before TMA writes to it
     tc_fence_before();

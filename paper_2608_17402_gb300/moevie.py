@@ -110,8 +110,9 @@ def _p(t):
 
 
 def _stream(stream=None):
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is None:   # the current stream's handle, without building a Stream object (3 us)
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return ctypes.c_void_p(stream.cuda_stream)
 
 
 def _call(name, *args):
@@ -135,6 +136,8 @@ def row_ld(h: int) -> int:
 
 def _rows_ok(t) -> bool:
     """t [..., h] has row stride row_ld(h) and is otherwise packed."""
+    if t.shape[-1] % 8 == 0:   # no pad
+        return t.is_contiguous()
     want = 1
     for i in range(t.dim() - 1, -1, -1):
         if t.shape[i] != 1 and t.stride(i) != want:
@@ -306,14 +309,14 @@ class LayerWeights:
 
     def c_struct(self) -> _Layer:
         d, E, k, h, hs = self.dims
-        for name in ("W1", "W3", "Ws1", "Ws3"):
-            if getattr(self, name) is not None:
-                _want_rows(getattr(self, name), torch.bfloat16, name)
-        return _Layer(d, E, k, h, hs, self.W_r.data_ptr(), self.b.data_ptr(), self.W1.data_ptr(),
-                      self.W2.data_ptr(), 0 if self.Ws1 is None else self.Ws1.data_ptr(),
-                      0 if self.Ws2 is None else self.Ws2.data_ptr(), float(self.lam),
-                      0 if self.W3 is None else self.W3.data_ptr(),
-                      0 if self.Ws3 is None else self.Ws3.data_ptr())
+        W1, W3, Ws1, Ws2, Ws3 = self.W1, self.W3, self.Ws1, self.Ws2, self.Ws3
+        for name, t in (("W1", W1), ("W3", W3), ("Ws1", Ws1), ("Ws3", Ws3)):
+            if t is not None:
+                _want_rows(t, torch.bfloat16, name)
+        return _Layer(d, E, k, h, hs, self.W_r.data_ptr(), self.b.data_ptr(), W1.data_ptr(),
+                      self.W2.data_ptr(), 0 if Ws1 is None else Ws1.data_ptr(),
+                      0 if Ws2 is None else Ws2.data_ptr(), float(self.lam),
+                      0 if W3 is None else W3.data_ptr(), 0 if Ws3 is None else Ws3.data_ptr())
 
 
 def moevie_moe_forward(layer: LayerWeights, x, ws: Workspace, y=None, routing=False, stream=None):
@@ -451,17 +454,20 @@ def moevie_moe_few(layer: LayerWeights, x, ws: FewWorkspace, y=None, routing=Fal
     """The layer forward for up to 64 tokens x bf16 [T, d]; returns y bf16 [T, d], with
     ``routing=True`` (y, idx int32 [T, k], gate fp32 [T, k])."""
     _want(x, torch.bfloat16, "x")
-    T, d = x.shape
-    k = layer.k
-    if d != layer.W_r.shape[0]:
-        raise ValueError(f"x: expected [T, {layer.W_r.shape[0]}], got {tuple(x.shape)}")
-    dev = x.device
-    y = _want(y, torch.bfloat16, "y") if y is not None else torch.empty((T, d), dtype=torch.bfloat16, device=dev)
-    if y.shape != x.shape:
-        raise ValueError(f"y: expected {tuple(x.shape)}, got {tuple(y.shape)}")
-    idx = torch.empty((T, k), dtype=torch.int32, device=dev) if routing else None
-    gate = torch.empty((T, k), dtype=torch.float32, device=dev) if routing else None
     L = layer.c_struct()
+    shape = x.shape
+    if len(shape) != 2 or shape[1] != L.d:
+        raise ValueError(f"x: expected [T, {L.d}], got {tuple(shape)}")
+    T, k = shape[0], L.k
+    if y is None:
+        y = torch.empty_like(x)
+    elif _want(y, torch.bfloat16, "y").shape != shape:
+        raise ValueError(f"y: expected {tuple(shape)}, got {tuple(y.shape)}")
+    idx = gate = None
+    if routing:
+        dev = x.device
+        idx = torch.empty((T, k), dtype=torch.int32, device=dev)
+        gate = torch.empty((T, k), dtype=torch.float32, device=dev)
     _call("moevie_moe_few", ctypes.byref(L), _p(x), T, _p(y), _p(idx), _p(gate), ws.ptr, ws.nbytes,
           _stream(stream))
     return (y, idx, gate) if routing else y
