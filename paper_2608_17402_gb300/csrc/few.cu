@@ -49,7 +49,7 @@ constexpr int FEW_RT_K = 512;         // rows of W_r staged at a time
 constexpr int FEW_RT_XLD = FEW_RT_K + 16;      // row strides of the staged x (bf16; rows 16-byte
 constexpr int FEW_RT_WLD = FEW_RT_K + 4;       //   aligned) and W_r^T (fp32)
 constexpr int FEW_SMEM_MAX = 232448 - 3072;   // 227 KB less the kernel's static variables
-constexpr int FEW_BAR_BYTES = 512, FEW_FLAG_BYTES = 576;
+constexpr int FEW_BAR_BYTES = 512, FEW_FLAG_BYTES = 576;   // (multiples of 64)
 // Parts of K at most: of a routed and of a shared down item.
 constexpr int FEW_MAX_P2 = 4, FEW_MAX_P2S = 8;
 
@@ -239,11 +239,58 @@ __device__ __forceinline__ float key_value(uint32_t u) {
     return __uint_as_float((u & 0x80000000u) ? u ^ 0x80000000u : ~u);
 }
 
+// k rounds of arg-max over a token's keys, by one warp: lane l holds experts l, l + 32, ... in
+// registers (NQMAX >= NQ of them).  sel: the selected, a bit per expert; lo, hi: order of the lowest
+// lower bound of a selected key and of the highest upper bound of an unselected one (a NaN
+// lower bound counts as lowest, a NaN upper bound as highest).  (Counting the experts ahead of
+// each expert, with all threads, took 3.2 us for 256 experts; this 1 us.)
+template <int NQMAX>
+__device__ __forceinline__ void few_rounds(int k, int NQ, const uint32_t* ok, const float* er, uint32_t* sel,
+                                           uint32_t& lo, uint32_t& hi) {
+    const int lane = threadIdx.x & 31;
+    uint32_t key[NQMAX], mine = 0u;
+#pragma unroll
+    for (int q = 0; q < NQMAX; ++q) key[q] = q < NQ ? ok[q * 32 + lane] : 0u;
+    for (int j = 0; j < k; ++j) {
+        uint32_t top = 0u;
+#pragma unroll
+        for (int q = 0; q < NQMAX; ++q) top = max(top, key[q]);
+        top = __reduce_max_sync(0xffffffffu, top);
+        int first = NQMAX;   // lowest of this lane's experts with that key
+#pragma unroll
+        for (int q = NQMAX - 1; q >= 0; --q)
+            if (key[q] == top) first = q;
+        const int e = __reduce_min_sync(0xffffffffu, first * 32 + lane);
+        if (first * 32 + lane == e) {
+            mine |= 1u << first;
+#pragma unroll
+            for (int q = 0; q < NQMAX; ++q)
+                if (q == first) key[q] = 0u;
+        }
+    }
+    uint32_t l = 0xffffffffu, h = 0u;
+#pragma unroll
+    for (int q = 0; q < NQMAX; ++q) {
+        if (q >= NQ) break;
+        const uint32_t o = ok[q * 32 + lane];
+        if (o != 0u) {
+            const float v = key_value(o), r = er[q * 32 + lane], a = v - r, b = v + r;
+            if (mine >> q & 1u) l = min(l, a == a ? key_order(a) : 0u);
+            else h = max(h, b == b ? key_order(b) : 0xffffffffu);
+        }
+        const uint32_t m = __ballot_sync(0xffffffffu, mine >> q & 1u);
+        if (lane == 0) sel[q] = m;
+    }
+    l = __reduce_min_sync(0xffffffffu, l);
+    h = __reduce_max_sync(0xffffffffu, h);
+    if (lane == 0) {
+        lo = l;
+        hi = h;
+    }
+}
+
 // Selection and gates of the CTA's tokens t0, t0 + step, ... (n <= FEW_SEL_WARPS of them), by all
-// threads.  xn: |x_t| of each.  buf: FEW_SEL_BYTES per expert and token.  A thread takes
-// (token, expert) pairs, a warp 32 consecutive experts of one token; the selected are those
-// with fewer than k experts ahead of them (larger key, or the same and a lower id), counted
-// directly: no round waits for another.
+// threads.  xn: |x_t| of each.  buf: FEW_SEL_BYTES per expert and token.
 __device__ void few_select(const FewArgs& p, int t0, int step, int n, const float* xn, uint8_t* buf,
                            int32_t* out_idx, float* out_gate) {
     __shared__ uint32_t s_lo[FEW_SEL_WARPS], s_hi[FEW_SEL_WARPS], s_sel[FEW_SEL_WARPS][32];
@@ -257,11 +304,7 @@ __device__ void few_select(const FewArgs& p, int t0, int step, int n, const floa
     auto lg_of = [&](int w) { return reinterpret_cast<float*>(base(w) + Ep * 12); };
     auto er_of = [&](int w) { return reinterpret_cast<float*>(base(w) + Ep * 16); };
     auto cand_of = [&](int w) { return reinterpret_cast<uint16_t*>(base(w) + Ep * 20); };
-    if (threadIdx.x < FEW_SEL_WARPS) {
-        s_lo[threadIdx.x] = 0xffffffffu;   // lowest lower bound of a selected key
-        s_hi[threadIdx.x] = 0u;            // highest upper bound of an unselected one
-        n_cand[threadIdx.x] = 0;
-    }
+    if (threadIdx.x < FEW_SEL_WARPS) n_cand[threadIdx.x] = 0;
     for (int q = warp; q < n * NQ; q += FEW_WARPS) {
         const int w = q / NQ, e = (q - w * NQ) * 32 + lane;
         uint32_t o = 0u;
@@ -278,44 +321,12 @@ __device__ void few_select(const FewArgs& p, int t0, int step, int n, const floa
         ok_of(w)[e] = o;
     }
     __syncthreads();
-    for (int q = warp; q < n * NQ; q += FEW_WARPS) {
-        const int w = q / NQ, e0 = (q - w * NQ) * 32, e = e0 + lane;
-        const uint4* all = reinterpret_cast<const uint4*>(ok_of(w));
-        const uint32_t o = ok_of(w)[e];
-        int ahead = 0;
-#pragma unroll 8
-        for (int j = 0; j < e0 / 4; ++j) {
-            const uint4 u = all[j];
-            ahead += (u.x >= o) + (u.y >= o) + (u.z >= o) + (u.w >= o);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int j = e0 / 4 + i;
-            const uint4 u = all[j];
-            ahead += (u.x > o || (u.x == o && 4 * j < e)) + (u.y > o || (u.y == o && 4 * j + 1 < e)) +
-                     (u.z > o || (u.z == o && 4 * j + 2 < e)) + (u.w > o || (u.w == o && 4 * j + 3 < e));
-        }
-#pragma unroll 8
-        for (int j = e0 / 4 + 8; j < Ep / 4; ++j) {
-            const uint4 u = all[j];
-            ahead += (u.x > o) + (u.y > o) + (u.z > o) + (u.w > o);
-        }
-        const bool sel = e < p.E && ahead < p.k;
-        const uint32_t m = __ballot_sync(0xffffffffu, sel);
-        // bounds (a NaN lower bound counts as lowest, a NaN upper bound as highest)
-        uint32_t lo = 0xffffffffu, hi = 0u;
-        if (e < p.E) {
-            const float v = key_value(o), r = er_of(w)[e];
-            if (sel) lo = (v - r == v - r) ? key_order(v - r) : 0u;
-            else hi = (v + r == v + r) ? key_order(v + r) : 0xffffffffu;
-        }
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        if (lane == 0) {
-            s_sel[w][e0 / 32] = m;
-            atomicMin(&s_lo[w], lo);
-            atomicMax(&s_hi[w], hi);
-        }
+    if (warp < n) {
+        const uint32_t* ok = ok_of(warp);
+        const float* er = er_of(warp);
+        if (NQ <= 2) few_rounds<2>(p.k, NQ, ok, er, s_sel[warp], s_lo[warp], s_hi[warp]);
+        else if (NQ <= 8) few_rounds<8>(p.k, NQ, ok, er, s_sel[warp], s_lo[warp], s_hi[warp]);
+        else few_rounds<32>(p.k, NQ, ok, er, s_sel[warp], s_lo[warp], s_hi[warp]);
     }
     __syncthreads();
     // Where the lowest selected key may not be above the highest unselected one: an expert whose
@@ -407,13 +418,23 @@ __device__ void few_select(const FewArgs& p, int t0, int step, int n, const floa
 // another entry, whose weights then come from L2: with larger N operands the ring would hold fewer
 // weights in flight for every expert.
 //
-// Built by every CTA from the selection; kept in shared memory.
+// Built by every CTA from the selection; kept in shared memory (128 bytes at most).
 struct FewPlan {
     int n_act;              // entries
     int tw, nt, nt_s;       // up items: columns (64 or 128), tiles of h and of h_s
     int tw2, ntd, P2, P2s;  // down items: columns, tiles of d, parts of K (routed, shared)
     int n_up_shared, n_up, n_down_shared, n_items;   // items: up, then down (shared first in each)
+    float inv_sh, inv_nt, inv_ntd, inv_P2, inv_P2s;  // reciprocals of the divisors below
 };
+
+// q / d for 0 <= q < 2^24, from an approximate reciprocal (integer division takes some 100 cycles,
+// and four roles of every CTA decode every item).
+__device__ __forceinline__ int few_div(int q, int d, float inv) {
+    int r = (int)((float)q * inv);
+    r += (r + 1) * d <= q ? 1 : 0;
+    r -= r * d > q ? 1 : 0;
+    return r;
+}
 
 struct FewItem {
     int up, shared, i;      // i: entry (routed), block of nb tokens (shared)
@@ -445,19 +466,22 @@ __device__ __forceinline__ FewItem few_item(const FewArgs& p, const FewLists& L,
         it.kb0 = 0;
         it.kb1 = p.nkb_d * (p.W3 ? 2 : 1);
         if (!it.shared) q -= pl.n_up_shared;
-        const int per = it.shared ? p.n_sh : pl.nt, r = q / per;   // shared: the blocks of a tile side by side
+        const int per = it.shared ? p.n_sh : pl.nt;   // shared: the blocks of a tile side by side
+        const int r = few_div(q, per, it.shared ? pl.inv_sh : pl.inv_nt);
         it.i = it.shared ? q - r * per : r;
         it.n0 = (it.shared ? r : q - r * per) * pl.tw;
     } else {
         if (!it.shared) q -= pl.n_down_shared;
-        const int P = it.shared ? pl.P2s : pl.P2, nkb = it.shared ? p.nkb_hs : p.nkb_h, r = q / P;
-        const int per = it.shared ? p.n_sh : pl.ntd, v = r / per;
+        const int P = it.shared ? pl.P2s : pl.P2, nkb = it.shared ? p.nkb_hs : p.nkb_h;
+        const int r = few_div(q, P, it.shared ? pl.inv_P2s : pl.inv_P2);
+        const int per = it.shared ? p.n_sh : pl.ntd, v = few_div(r, per, it.shared ? pl.inv_sh : pl.inv_ntd);
         it.part = q - r * P;
         it.i = it.shared ? r - v * per : v;
         it.tw = pl.tw2;
         it.n0 = (it.shared ? v : r - v * per) * pl.tw2;
-        it.kb0 = it.part * nkb / P;
-        it.kb1 = (it.part + 1) * nkb / P;
+        const float inv = it.shared ? pl.inv_P2s : pl.inv_P2;
+        it.kb0 = few_div(it.part * nkb, P, inv);
+        it.kb1 = few_div((it.part + 1) * nkb, P, inv);
     }
     it.e = it.shared ? 0 : L.act[it.i];
     it.row0 = it.shared ? it.i * p.nb : L.off[it.i];
@@ -578,6 +602,11 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
             pl.n_up = n_act * pl.nt + pl.n_up_shared;
             pl.n_down_shared = p.n_sh * pl.ntd * pl.P2s;
             pl.n_items = pl.n_up + pl.n_down_shared + n_act * pl.ntd * pl.P2;
+            pl.inv_sh = 1.0f / (float)max(p.n_sh, 1);
+            pl.inv_nt = 1.0f / (float)pl.nt;
+            pl.inv_ntd = 1.0f / (float)pl.ntd;
+            pl.inv_P2 = 1.0f / (float)pl.P2;
+            pl.inv_P2s = 1.0f / (float)pl.P2s;
         }
     }
     __syncthreads();
@@ -901,7 +930,7 @@ __host__ __device__ inline FewSizes few_sizes(int T, int k, int E) {
     const int n = T * k, na = few_entries(T, k, E);
     z.stage_bytes = FEW_TILE_BYTES + 2 * few_nb(T) * 128;
     // plan, gate, row_of, act, off, cnt, row_tok
-    z.lists = 64 + ((4 * n + 2 * n + 4 * na + na + n + 15) & ~15);
+    z.lists = 128 + ((4 * n + 2 * n + 4 * na + na + n + 15) & ~15);
     const int left = FEW_SMEM_MAX - 1024 - FEW_BAR_BYTES - FEW_FLAG_BYTES - z.lists;
     z.stages = left / z.stage_bytes;
     if (z.stages > 12) z.stages = 12;
@@ -924,7 +953,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     const int n = p.T * p.k, na = p.na_max;
     FewLists L;
     L.plan = reinterpret_cast<FewPlan*>(at);
-    L.gate = reinterpret_cast<float*>(at + 64);
+    L.gate = reinterpret_cast<float*>(at + 128);
     L.row_of = reinterpret_cast<uint16_t*>(L.gate + n);
     L.act = L.row_of + n;
     L.off = L.act + na;
