@@ -54,6 +54,15 @@ constexpr int FEW_BAR_BYTES = 512, FEW_FLAG_BYTES = 576;   // (multiples of 64)
 constexpr int FEW_MAX_P2 = 4, FEW_MAX_P2S = 8;
 
 __device__ __forceinline__ int up16(int v) { return (v + 15) & ~15; }
+// q / d for 0 <= q < 2^24, from an approximate reciprocal: integer division takes some hundred
+// cycles, and the way from the router to the first weights is a chain of such small steps.
+__device__ __forceinline__ int few_div(int q, int d, float inv) {
+    int r = (int)((float)q * inv);
+    r += (r + 1) * d <= q ? 1 : 0;
+    r -= r * d > q ? 1 : 0;
+    return r;
+}
+
 // Barrier of one epilogue group's 128 threads.
 __device__ __forceinline__ void epi_sync(int group) { asm volatile("bar.sync %0, 128;" ::"r"(group + 1) : "memory"); }
 // 32 lanes x 8 consecutive 32-bit columns (thread i: lane base + i).
@@ -100,14 +109,14 @@ __device__ bool few_barrier(DevStatus* st, uint64_t limit_ns) {
 // share kp of K; lane (ep, ks): experts ep and ep + 4, four K of every 32.
 __device__ void few_logits(const FewArgs& p, uint8_t* smem) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int TG = (p.T + 7) / 8, KP = FEW_WARPS / TG;
+    const int TG = (p.T + 7) / 8, KP = p.rt_kp;   // KP = FEW_WARPS / TG
     float* ws = reinterpret_cast<float*>(smem);
     float* red = ws + 8 * FEW_RT_WLD;      // [KP][8 TG][8]
     float* redq = red + FEW_WARPS * 64;    // [KP][8]
     __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(redq + FEW_WARPS * 8);
-    const int g = warp % TG, kp = warp / TG, ep = lane >> 3, ks = lane & 7;
+    const int kp = few_div(warp, TG, __fdividef(1.0f, (float)TG)), g = warp - kp * TG, ep = lane >> 3, ks = lane & 7;
     for (int item = blockIdx.x; item < p.rt_eb * p.rt_parts; item += gridDim.x) {
-        const int e0 = item % p.rt_eb * 8, ds = item / p.rt_eb;
+        const int ds = few_div(item, p.rt_eb, __fdividef(1.0f, (float)p.rt_eb)), e0 = (item - ds * p.rt_eb) * 8;
         const int d0 = ds * p.rt_dch, d1 = min(p.d, d0 + p.rt_dch);
         float tot[2][8] = {}, sq[2] = {};
         for (int k0 = d0; k0 < d1; k0 += FEW_RT_K) {
@@ -231,117 +240,137 @@ __device__ __forceinline__ float few_norm(const FewArgs& p, int t) {
 }
 
 // Bytes of shared memory per expert (E rounded up to 32) that one token's selection takes:
-// 64-bit key, order of the fp32 key, logit, key half-width, list of experts to decide exactly.
-constexpr int FEW_SEL_BYTES = 24;
+// bounds of the key (later the 64-bit key), the fp32 key, all as their order; logit; list of experts
+// to decide exactly.
+constexpr int FEW_SEL_BYTES = 18;
 
-// The float that key_order maps to u (NaN for 1).
-__device__ __forceinline__ float key_value(uint32_t u) {
-    return __uint_as_float((u & 0x80000000u) ? u ^ 0x80000000u : ~u);
-}
-
-// k rounds of arg-max over a token's keys, by one warp: lane l holds experts l, l + 32, ... in
-// registers (NQMAX >= NQ of them).  sel: the selected, a bit per expert; lo, hi: order of the lowest
-// lower bound of a selected key and of the highest upper bound of an unselected one (a NaN
-// lower bound counts as lowest, a NaN upper bound as highest).  (Counting the experts ahead of
-// each expert, with all threads, took 3.2 us for 256 experts; this 1 us.)
+// k rounds of arg-max over a token's keys, by one warp: lane l holds the order of experts l,
+// l + 32, ... in registers (NQMAX >= NQ of them).  Lane j < k returns the j-th selected expert.
+// lo, hi: the lowest lower bound of a selected key and the highest upper bound of another one.
 template <int NQMAX>
-__device__ __forceinline__ void few_rounds(int k, int NQ, const uint32_t* ok, const float* er, uint32_t* sel,
-                                           uint32_t& lo, uint32_t& hi) {
+__device__ __forceinline__ int few_rounds(int k, int NQ, const uint32_t* ok, const uint32_t* lob, const uint32_t* hib,
+                                          uint32_t& lo, uint32_t& hi) {
     const int lane = threadIdx.x & 31;
-    uint32_t key[NQMAX], mine = 0u;
+    uint32_t key[NQMAX];
+    int mine = 0;
 #pragma unroll
     for (int q = 0; q < NQMAX; ++q) key[q] = q < NQ ? ok[q * 32 + lane] : 0u;
+#pragma unroll 1
     for (int j = 0; j < k; ++j) {
         uint32_t top = 0u;
 #pragma unroll
         for (int q = 0; q < NQMAX; ++q) top = max(top, key[q]);
         top = __reduce_max_sync(0xffffffffu, top);
-        int first = NQMAX;   // lowest of this lane's experts with that key
+        int e = NQMAX * 32;   // the lowest id with that key
 #pragma unroll
         for (int q = NQMAX - 1; q >= 0; --q)
-            if (key[q] == top) first = q;
-        const int e = __reduce_min_sync(0xffffffffu, first * 32 + lane);
-        if (first * 32 + lane == e) {
-            mine |= 1u << first;
+            if (key[q] == top) e = q * 32 + lane;
+        e = __reduce_min_sync(0xffffffffu, e);
 #pragma unroll
-            for (int q = 0; q < NQMAX; ++q)
-                if (q == first) key[q] = 0u;
-        }
+        for (int q = 0; q < NQMAX; ++q)
+            if (e == q * 32 + lane) key[q] = 0u;
+        if (lane == j) mine = e;
     }
-    uint32_t l = 0xffffffffu, h = 0u;
+    hi = 0u;
 #pragma unroll
-    for (int q = 0; q < NQMAX; ++q) {
-        if (q >= NQ) break;
-        const uint32_t o = ok[q * 32 + lane];
-        if (o != 0u) {
-            const float v = key_value(o), r = er[q * 32 + lane], a = v - r, b = v + r;
-            if (mine >> q & 1u) l = min(l, a == a ? key_order(a) : 0u);
-            else h = max(h, b == b ? key_order(b) : 0xffffffffu);
-        }
-        const uint32_t m = __ballot_sync(0xffffffffu, mine >> q & 1u);
-        if (lane == 0) sel[q] = m;
-    }
-    l = __reduce_min_sync(0xffffffffu, l);
-    h = __reduce_max_sync(0xffffffffu, h);
-    if (lane == 0) {
-        lo = l;
-        hi = h;
+    for (int q = 0; q < NQMAX; ++q)
+        if (key[q] != 0u) hi = max(hi, hib[q * 32 + lane]);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    lo = __reduce_min_sync(0xffffffffu, lane < k ? lob[mine] : 0xffffffffu);
+    return mine;
+}
+
+// Places of a token's selected experts (lane j < k holds the j-th; ascending ids) and their gates,
+// by one warp; with `mask` also the token's bit in each of those experts' token masks.
+__device__ __forceinline__ void few_place(const FewArgs& p, int t, int mine, const float* lg, int32_t* out_idx,
+                                          float* out_gate, unsigned long long* mask) {
+    const int lane = threadIdx.x & 31;
+    const float s = lane < p.k ? __fdividef(1.0f, 1.0f + expf(-lg[mine])) : 0.f;
+    const float sum = warp_sum(s);
+    int at = t * p.k;
+#pragma unroll 1
+    for (int j = 0; j < p.k; ++j) at += __shfl_sync(0xffffffffu, mine, j) < mine;
+    if (lane < p.k) {
+        out_idx[at] = mine;
+        out_gate[at] = __fdividef(s, sum);
+        if (mask) atomicOr(&mask[mine], 1ull << t);
     }
 }
 
 // Selection and gates of the CTA's tokens t0, t0 + step, ... (n <= FEW_SEL_WARPS of them), by all
 // threads.  xn: |x_t| of each.  buf: FEW_SEL_BYTES per expert and token.
 __device__ void few_select(const FewArgs& p, int t0, int step, int n, const float* xn, uint8_t* buf,
-                           int32_t* out_idx, float* out_gate) {
-    __shared__ uint32_t s_lo[FEW_SEL_WARPS], s_hi[FEW_SEL_WARPS], s_sel[FEW_SEL_WARPS][32];
+                           int32_t* out_idx, float* out_gate, unsigned long long* mask) {
+    __shared__ uint32_t s_sel[FEW_SEL_WARPS][32];
     __shared__ int n_cand[FEW_SEL_WARPS];
-    __shared__ float s_sig[FEW_SEL_WARPS][32];
     __shared__ double part64[FEW_WARPS][4];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, NQ = (p.E + 31) / 32, Ep = NQ * 32;
     auto base = [&](int w) { return buf + (size_t)w * Ep * FEW_SEL_BYTES; };
-    auto kd_of = [&](int w) { return reinterpret_cast<double*>(base(w)); };
+    auto lob_of = [&](int w) { return reinterpret_cast<uint32_t*>(base(w)); };
+    auto hib_of = [&](int w) { return reinterpret_cast<uint32_t*>(base(w) + Ep * 4); };
+    auto kd_of = [&](int w) { return reinterpret_cast<double*>(base(w)); };   // in the bounds' place
     auto ok_of = [&](int w) { return reinterpret_cast<uint32_t*>(base(w) + Ep * 8); };
     auto lg_of = [&](int w) { return reinterpret_cast<float*>(base(w) + Ep * 12); };
-    auto er_of = [&](int w) { return reinterpret_cast<float*>(base(w) + Ep * 16); };
-    auto cand_of = [&](int w) { return reinterpret_cast<uint16_t*>(base(w) + Ep * 20); };
-    if (threadIdx.x < FEW_SEL_WARPS) n_cand[threadIdx.x] = 0;
+    auto cand_of = [&](int w) { return reinterpret_cast<uint16_t*>(base(w) + Ep * 16); };
+    const float inv_NQ = __fdividef(1.0f, (float)NQ);
     for (int q = warp; q < n * NQ; q += FEW_WARPS) {
-        const int w = q / NQ, e = (q - w * NQ) * 32 + lane;
-        uint32_t o = 0u;
+        const int w = few_div(q, NQ, inv_NQ), e = (q - w * NQ) * 32 + lane;
+        uint32_t o = 0u, ob = 0u, oa = 0u;
         if (e < p.E) {
             const float s = sum_parts(p.part + (int64_t)(t0 + w * step) * p.E + e, (int64_t)p.T * p.E, p.rt_parts);
             const float w2 = sum_parts(p.wsq + e, p.E, p.rt_parts);
             const float v = __fdividef(1.0f, 1.0f + __expf(-s)) + __ldg(p.b + e);
+            // Half-width of the key: a quarter (the sigmoid's largest slope; and some, for the
+            // square root) of the logit's error bound, and the fp32 evaluation (fast sigmoid:
+            // under 1e-6; the sum's rounding).  A NaN bound bounds nothing.
+            float wn;
+            asm("sqrt.approx.f32 %0, %1;" : "=f"(wn) : "f"(w2));
+            const float r = 0.2501f * p.rt_err * xn[w] * wn + 2e-6f + 2.4e-7f * fabsf(v), a = v - r, b = v + r;
             o = key_order(v);
+            oa = a == a ? key_order(a) : 0u;
+            ob = b == b ? key_order(b) : 0xffffffffu;
             lg_of(w)[e] = s;
-            // Half-width of the key: a quarter (the sigmoid's largest slope) of the logit's error
-            // bound, and the fp32 evaluation (fast sigmoid: under 1e-6; the sum's rounding).
-            er_of(w)[e] = 0.25f * p.rt_err * xn[w] * sqrtf(w2) + 2e-6f + 2.4e-7f * fabsf(v);
         }
         ok_of(w)[e] = o;
+        lob_of(w)[e] = oa;
+        hib_of(w)[e] = ob;
     }
     __syncthreads();
+    int unsure = 0;
     if (warp < n) {
-        const uint32_t* ok = ok_of(warp);
-        const float* er = er_of(warp);
-        if (NQ <= 2) few_rounds<2>(p.k, NQ, ok, er, s_sel[warp], s_lo[warp], s_hi[warp]);
-        else if (NQ <= 8) few_rounds<8>(p.k, NQ, ok, er, s_sel[warp], s_lo[warp], s_hi[warp]);
-        else few_rounds<32>(p.k, NQ, ok, er, s_sel[warp], s_lo[warp], s_hi[warp]);
+        const uint32_t *ok = ok_of(warp), *lob = lob_of(warp), *hib = hib_of(warp);
+        uint32_t lo, hi;
+        int mine;
+        if (NQ <= 2) mine = few_rounds<2>(p.k, NQ, ok, lob, hib, lo, hi);
+        else if (NQ <= 8) mine = few_rounds<8>(p.k, NQ, ok, lob, hib, lo, hi);
+        else mine = few_rounds<32>(p.k, NQ, ok, lob, hib, lo, hi);
+        if (lane == 0) n_cand[warp] = 0;
+        if (p.k == p.E || lo > hi) {
+            few_place(p, t0 + warp * step, mine, lg_of(warp), out_idx, out_gate, mask);
+        } else {
+            // The lowest selected key may not be above the highest other one.  An expert whose
+            // lower bound is above every other upper bound is in, one whose upper bound is below
+            // every selected lower bound is out; the rest get exact keys.
+            unsure = 1;
+            s_sel[warp][lane] = 0u;
+            __syncwarp();
+            if (lane < p.k) atomicOr(&s_sel[warp][mine >> 5], 1u << (mine & 31));
+            __syncwarp();
+            int nc = 0;
+            for (int q = 0; q < NQ; ++q) {
+                const int e = q * 32 + lane;
+                const bool sel = s_sel[warp][q] >> lane & 1u;
+                const bool c = e < p.E && (sel ? lob[e] <= hi : hib[e] >= lo);
+                const uint32_t m = __ballot_sync(0xffffffffu, c), ms = __ballot_sync(0xffffffffu, sel && !c);
+                if (c) cand_of(warp)[nc + __popc(m & ((1u << lane) - 1u))] = (uint16_t)e;
+                __syncwarp();
+                if (lane == 0) s_sel[warp][q] = ms;
+                nc += __popc(m);
+            }
+            if (lane == 0) n_cand[warp] = nc;
+        }
     }
-    __syncthreads();
-    // Where the lowest selected key may not be above the highest unselected one: an expert whose
-    // lower bound is above every unselected upper bound is in, one whose upper bound is below
-    // every selected lower bound is out, the rest get exact keys.
-    for (int q = warp; q < n * NQ; q += FEW_WARPS) {
-        const int w = q / NQ, e0 = (q - w * NQ) * 32, e = e0 + lane;
-        if (s_lo[w] > s_hi[w] || e >= p.E) continue;
-        const float v = key_value(ok_of(w)[e]), r = er_of(w)[e];
-        const bool sel = s_sel[w][e0 / 32] >> lane & 1u;
-        const uint32_t lo = (v - r == v - r) ? key_order(v - r) : 0u;
-        const uint32_t hi = (v + r == v + r) ? key_order(v + r) : 0xffffffffu;
-        if (sel ? lo <= s_hi[w] : hi >= s_lo[w]) cand_of(w)[atomicAdd(&n_cand[w], 1)] = (uint16_t)e;
-    }
-    __syncthreads();
+    if (!__syncthreads_or(unsure)) return;
     for (int w = 0; w < n; ++w) {
         const int nc = n_cand[w];
         if (nc == 0) continue;
@@ -369,7 +398,6 @@ __device__ void few_select(const FewArgs& p, int t0, int step, int n, const floa
                 double t = 0.0;
                 for (int j = 0; j < FEW_WARPS; ++j) t += part64[j][threadIdx.x];
                 kd_of(w)[e] = 1.0 / (1.0 + exp(-t)) + (double)__ldg(p.b + e);
-                atomicAnd(&s_sel[w][e / 32], ~(1u << (e & 31)));
             }
             __syncthreads();
         }
@@ -391,25 +419,16 @@ __device__ void few_select(const FewArgs& p, int t0, int step, int n, const floa
         }
         __syncthreads();
     }
-    // Places in ascending order of ids; the gates' sum in that order.
-    for (int q = warp; q < n * NQ; q += FEW_WARPS) {
-        const int w = q / NQ, qe = q - w * NQ;
-        const uint32_t m = s_sel[w][qe];
-        if (m == 0u) continue;
-        int j = __popc(m & ((1u << lane) - 1u));
-        for (int i = 0; i < qe; ++i) j += __popc(s_sel[w][i]);
-        if (m >> lane & 1u) {
-            out_idx[(t0 + w * step) * p.k + j] = qe * 32 + lane;
-            s_sig[w][j] = 1.0f / (1.0f + expf(-lg_of(w)[qe * 32 + lane]));
+    if (warp < n && n_cand[warp] > 0) {
+        int mine = 0, at = 0;
+        for (int q = 0; q < NQ; ++q) {
+            const uint32_t m = s_sel[warp][q];
+            if (lane >= at && lane < at + __popc(m)) mine = q * 32 + (int)__fns(m, 0, lane - at + 1);
+            at += __popc(m);
         }
+        few_place(p, t0 + warp * step, mine, lg_of(warp), out_idx, out_gate, mask);
     }
     __syncthreads();
-    for (int q = threadIdx.x; q < n * p.k; q += FEW_THREADS) {
-        const int w = q / p.k, j = q - w * p.k;
-        float sum = 0.f;
-        for (int i = 0; i < p.k; ++i) sum += s_sig[w][i];
-        out_gate[(t0 + w * step) * p.k + j] = s_sig[w][j] / sum;
-    }
 }
 
 // ----------------------------------------------------- 3. work of a call
@@ -426,15 +445,6 @@ struct FewPlan {
     int n_up_shared, n_up, n_down_shared, n_items;   // items: up, then down (shared first in each)
     float inv_sh, inv_nt, inv_ntd, inv_P2, inv_P2s;  // reciprocals of the divisors below
 };
-
-// q / d for 0 <= q < 2^24, from an approximate reciprocal (integer division takes some 100 cycles,
-// and four roles of every CTA decode every item).
-__device__ __forceinline__ int few_div(int q, int d, float inv) {
-    int r = (int)((float)q * inv);
-    r += (r + 1) * d <= q ? 1 : 0;
-    r -= r * d > q ? 1 : 0;
-    return r;
-}
 
 struct FewItem {
     int up, shared, i;      // i: entry (routed), block of nb tokens (shared)
@@ -494,7 +504,7 @@ __device__ __forceinline__ FewItem few_item(const FewArgs& p, const FewLists& L,
 // 6600 GB/s (measured with tiles streamed by 8 to 152 SMs); the last, partial round of items runs
 // at its own c; 400 ns an item besides.
 __device__ __forceinline__ float few_time(int items, int blocks, int kb, int ctas) {
-    const int rounds = items / ctas, rest = items - rounds * ctas;
+    const int rounds = few_div(items, ctas, __fdividef(1.0f, (float)ctas)), rest = items - rounds * ctas;
     const float one = fmaxf((float)kb / 70.0f, 200.0f), all = (float)kb / 6600.0f;
     return rounds * (blocks * fmaxf(one, all * ctas) + 400.0f) +
            (rest > 0 ? blocks * fmaxf(one, all * rest) + 400.0f : 0.0f);
@@ -505,20 +515,18 @@ __device__ __forceinline__ int few_fastest(float t) {
     return (int)(__reduce_min_sync(0xffffffffu, c) & 31u);
 }
 
-// Expert lists and the plan from the selection (idx, gate of all slots).  tmp: 10 bytes per
-// expert of scratch.  The selection lies in shared memory, or in global memory where other CTAs
-// wrote it.
+// Expert lists and the plan from the selection (idx, gate of all slots).  mask: the experts'
+// token masks; off: 2 bytes per expert of scratch.  The selection and its masks lie in shared memory
+// (SHARED_SEL), or other CTAs wrote the selection to global memory and the masks are built here.
 template <bool SHARED_SEL>
 __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx, const float* gate,
-                         uint8_t* tmp) {
-    __shared__ int n_in[32], rows_in[32];   // of each 32 experts: how many have tokens, their rows
-    unsigned long long* mask = reinterpret_cast<unsigned long long*>(tmp);   // tokens of each expert
-    uint16_t* off = reinterpret_cast<uint16_t*>(mask + p.E);                 // first row of each expert
+                         unsigned long long* mask, uint16_t* off) {
+    __shared__ int n_in[32], rows_in[32];   // of each 32 experts: entries, rows
     auto load = [](const auto* q) { return SHARED_SEL ? *q : __ldcg(q); };
     const int n = p.T * p.k, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int e = threadIdx.x; e < p.E; e += FEW_THREADS) mask[e] = 0ull;
     if (threadIdx.x < 32) n_in[threadIdx.x] = rows_in[threadIdx.x] = 0;
-    __syncthreads();
+    if (!SHARED_SEL)
+        for (int e = threadIdx.x; e < p.E; e += FEW_THREADS) mask[e] = 0ull;
     constexpr int PER = (MOEVIE_FEW_MAX_TOKENS * 32 + FEW_THREADS - 1) / FEW_THREADS;   // slots of a thread
     int my_e[PER];
     float my_g[PER];
@@ -529,13 +537,16 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
         my_e[i] = load(idx + s);
         my_g[i] = load(gate + s);
     }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int s = threadIdx.x + i * FEW_THREADS;
-        if (s >= n) break;
-        atomicOr(&mask[my_e[i]], 1ull << (s / p.k));
-    }
     __syncthreads();
+    if (!SHARED_SEL) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int s = threadIdx.x + i * FEW_THREADS;
+            if (s >= n) break;
+            atomicOr(&mask[my_e[i]], 1ull << few_div(s, p.k, p.inv_k));
+        }
+        __syncthreads();
+    }
     const int sh = p.nb == 16 ? 4 : 5;
     for (int q = warp; q * 32 < p.E; q += FEW_WARPS) {
         const int e = q * 32 + lane, c = e < p.E ? __popcll(mask[e]) : 0;
@@ -578,35 +589,41 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
     if (warp == FEW_WARPS - 1) {
         // 64-column items where 128-column ones are too few to keep all SMs streaming; down items
         // may also split K (their partial rows are joined anyway).
-        const int ctas = (int)gridDim.x, bn = up16(min((n + n_act - 1) / n_act, p.nb)) * 128, mats = p.W3 ? 2 : 1;
-        const int tw_l = 128 >> (lane & 1);
-        const int tiles_l = n_act * ((p.h + tw_l - 1) / tw_l) + p.n_sh * ((p.hs + tw_l - 1) / tw_l);
+        // (shifts and reciprocals: this is on the way of every CTA's first load)
+        const int ctas = (int)gridDim.x, mats = p.W3 ? 2 : 1;
+        const int bn = up16(min((int)__fdividef((float)(n + n_act - 1), (float)n_act), p.nb)) * 128;
+        const int s_l = 7 - (lane & 1), tw_l = 1 << s_l;
+        const int tiles_l = n_act * ((p.h + tw_l - 1) >> s_l) + p.n_sh * ((p.hs + tw_l - 1) >> s_l);
         const int up = few_fastest(lane < 2 ? few_time(tiles_l, mats * p.nkb_d, tw_l * 128 + bn, ctas) : 3.0e38f);
-        const int P_l = (lane >> 1) + 1, ntd_l = (p.d + tw_l - 1) / tw_l;
-        const int items_l = ntd_l * P_l * (n_act + p.n_sh * ((p.nkb_hs + p.nkb_h - 1) / p.nkb_h));
+        const int P_l = (lane >> 1) + 1, ntd_l = (p.d + tw_l - 1) >> s_l;
+        const int items_l = ntd_l * P_l * (n_act + p.n_sh * p.sh_ratio);
+        const int blocks_l = (int)__fdividef((float)(p.nkb_h + P_l - 1) + 0.5f, (float)P_l);
         const int dn = few_fastest(P_l <= FEW_MAX_P2 && P_l <= p.nkb_h
-                                       ? few_time(items_l, (p.nkb_h + P_l - 1) / P_l, tw_l * 128 + 2 * bn, ctas)
+                                       ? few_time(items_l, blocks_l, tw_l * 128 + 2 * bn, ctas)
                                        : 3.0e38f);
         if (lane == 0) {
             FewPlan& pl = *L.plan;
+            const int s1 = 7 - up, s2 = 7 - (dn & 1), P2 = (dn >> 1) + 1;
             pl.n_act = n_act;
-            pl.tw = 128 >> up;
-            pl.nt = (p.h + pl.tw - 1) / pl.tw;
-            pl.nt_s = (p.hs + pl.tw - 1) / pl.tw;
-            pl.tw2 = 128 >> (dn & 1);
-            pl.P2 = (dn >> 1) + 1;
-            pl.ntd = (p.d + pl.tw2 - 1) / pl.tw2;
+            pl.tw = 1 << s1;
+            pl.nt = (p.h + pl.tw - 1) >> s1;
+            pl.nt_s = (p.hs + pl.tw - 1) >> s1;
+            pl.tw2 = 1 << s2;
+            pl.P2 = P2;
+            pl.ntd = (p.d + pl.tw2 - 1) >> s2;
             // shared down items about as long as the routed ones
-            pl.P2s = p.hs > 0 ? min(min(FEW_MAX_P2S, p.nkb_hs), max(1, (p.nkb_hs * pl.P2 + p.nkb_h / 2) / p.nkb_h)) : 1;
+            pl.P2s = p.hs > 0 ? min(min(FEW_MAX_P2S, p.nkb_hs),
+                                    max(1, (int)__fdividef((float)(p.nkb_hs * P2) + 0.5f * p.nkb_h, (float)p.nkb_h)))
+                              : 1;
             pl.n_up_shared = p.n_sh * pl.nt_s;
             pl.n_up = n_act * pl.nt + pl.n_up_shared;
             pl.n_down_shared = p.n_sh * pl.ntd * pl.P2s;
-            pl.n_items = pl.n_up + pl.n_down_shared + n_act * pl.ntd * pl.P2;
-            pl.inv_sh = 1.0f / (float)max(p.n_sh, 1);
-            pl.inv_nt = 1.0f / (float)pl.nt;
-            pl.inv_ntd = 1.0f / (float)pl.ntd;
-            pl.inv_P2 = 1.0f / (float)pl.P2;
-            pl.inv_P2s = 1.0f / (float)pl.P2s;
+            pl.n_items = pl.n_up + pl.n_down_shared + n_act * pl.ntd * P2;
+            pl.inv_sh = __fdividef(1.0f, (float)max(p.n_sh, 1));
+            pl.inv_nt = __fdividef(1.0f, (float)pl.nt);
+            pl.inv_ntd = __fdividef(1.0f, (float)pl.ntd);
+            pl.inv_P2 = __fdividef(1.0f, (float)P2);
+            pl.inv_P2s = __fdividef(1.0f, (float)pl.P2s);
         }
     }
     __syncthreads();
@@ -614,7 +631,7 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
     for (int i = 0; i < PER; ++i) {
         const int s = threadIdx.x + i * FEW_THREADS;
         if (s >= n) break;
-        const int t = s / p.k, e = my_e[i];
+        const int t = few_div(s, p.k, p.inv_k), e = my_e[i];
         const int row = off[e] + __popcll(mask[e] & ((1ull << t) - 1ull));
         L.row_tok[row] = (uint8_t)t;
         L.row_of[s] = (uint16_t)row;
@@ -637,6 +654,7 @@ __device__ __forceinline__ void few_abort(volatile int* flag, DevStatus* st, int
 // Weight tiles of every item; never waits for anything but a free stage.
 __device__ void few_load_w(const FewArgs& p, const FewSmem& sm, const FewLists& L, volatile int* abort_flag) {
     const int n_items = L.plan->n_items;
+    const uint64_t pol = l2_policy_evict_first();
     int s = 0;
     uint32_t ph = 0;
     for (int id = blockIdx.x; id < n_items; id += gridDim.x) {
@@ -653,8 +671,8 @@ __device__ void few_load_w(const FewArgs& p, const FewSmem& sm, const FewLists& 
             mbar_arrive_expect_tx(bar, it.tw * 128);
             const CUtensorMap* m = (two & kb) ? a3 : a;
             const int k0 = (kb >> two) * 64;
-            tma_load_3d(dst, m, bar, it.n0, k0, it.e);
-            if (it.tw == 128) tma_load_3d(dst + FEW_TILE_BYTES / 2, m, bar, it.n0 + 64, k0, it.e);
+            tma_load_3d_hint(dst, m, bar, it.n0, k0, it.e, pol);
+            if (it.tw == 128) tma_load_3d_hint(dst + FEW_TILE_BYTES / 2, m, bar, it.n0 + 64, k0, it.e, pol);
             if (++s == sm.stages) {
                 s = 0;
                 ph ^= 1u;
@@ -1008,7 +1026,12 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
         p.done_up[i] = 0;
     few_logits(p, smem);
     const int sel_bytes = (p.E + 31) / 32 * 32 * FEW_SEL_BYTES, ring_bytes = z.stages * z.stage_bytes;
-    const bool everywhere = p.T <= FEW_SEL_WARPS && p.T * sel_bytes + 8 * n <= ring_bytes;
+    // (then the selection and the masks lie behind the tokens' selection buffers)
+    const bool everywhere = p.T <= FEW_SEL_WARPS && p.T * sel_bytes + 10 * p.E + 8 * n + 16 <= ring_bytes;
+    unsigned long long* mask = reinterpret_cast<unsigned long long*>(smem + (everywhere ? p.T * sel_bytes : 0));
+    uint16_t* off = reinterpret_cast<uint16_t*>(mask + p.E);
+    if (everywhere)
+        for (int e = threadIdx.x; e < p.E; e += FEW_THREADS) mask[e] = 0ull;
     // tokens of this CTA: all, or every gridDim.x-th
     const int t0 = everywhere ? 0 : blockIdx.x, step = everywhere ? 1 : (int)gridDim.x;
     const int mine = everywhere ? p.T : (p.T - t0 + step - 1) / step;
@@ -1018,16 +1041,15 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     }
     if (!few_barrier(p.status, p.limit_ns)) return give_up();
     if (everywhere) {
-        int32_t* s_idx = reinterpret_cast<int32_t*>(smem + p.T * sel_bytes);
+        int32_t* s_idx = reinterpret_cast<int32_t*>(off + ((p.E + 1) & ~1));
         float* s_gate = reinterpret_cast<float*>(s_idx + n);
-        few_select(p, 0, 1, mine, xn, smem, s_idx, s_gate);
-        __syncthreads();
+        few_select(p, 0, 1, mine, xn, smem, s_idx, s_gate, mask);
         if (blockIdx.x == 0)
             for (int i = threadIdx.x; i < n; i += FEW_THREADS) {
                 p.idx[i] = s_idx[i];
                 p.gate[i] = s_gate[i];
             }
-        few_plan<true>(p, L, s_idx, s_gate, smem);
+        few_plan<true>(p, L, s_idx, s_gate, mask, off);
     } else {
         const int most = min(FEW_SEL_WARPS, ring_bytes / sel_bytes);   // (one batch, unless the GPU is tiny)
         for (int i = 0; i < mine; i += most) {
@@ -1035,11 +1057,10 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
                 if (i + warp < mine && warp < most) xn[warp] = few_norm(p, t0 + (i + warp) * step);
                 __syncthreads();
             }
-            few_select(p, t0 + i * step, step, min(most, mine - i), xn, smem, p.idx, p.gate);
-            __syncthreads();
+            few_select(p, t0 + i * step, step, min(most, mine - i), xn, smem, p.idx, p.gate, nullptr);
         }
         if (!few_barrier(p.status, p.limit_ns)) return give_up();
-        few_plan<false>(p, L, p.idx, p.gate, smem);
+        few_plan<false>(p, L, p.idx, p.gate, mask, off);
     }
     fence_proxy_async_smem();   // the router's use of the ring, before TMA writes to it
     tc_fence_before();
@@ -1136,11 +1157,13 @@ cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaS
     a.tmem_cols = 32;
     while (a.tmem_cols < 2 * a.acc_cols) a.tmem_cols *= 2;
     a.rt_eb = (a.E + 7) / 8;
+    a.inv_k = 1.0f / (float)a.k;
+    a.sh_ratio = (a.nkb_hs + a.nkb_h - 1) / a.nkb_h;
     a.rt_parts = few_rt_parts(a.d, a.E, sms);
     a.rt_dch = (int)up8((a.d + a.rt_parts - 1) / a.rt_parts);
     // length of the summation chains of a logit (few_logits): 8 products, their sums (one more per
     // staged block), the lanes, the warps, the parts; times 2^-24, with room for second order
-    const int kp = FEW_WARPS / ((a.T + 7) / 8), blocks = (a.rt_dch + FEW_RT_K - 1) / FEW_RT_K;
+    const int kp = a.rt_kp = FEW_WARPS / ((a.T + 7) / 8), blocks = (a.rt_dch + FEW_RT_K - 1) / FEW_RT_K;
     const int chain = 8 + (a.rt_dch / (64 * kp) + 2 * blocks) + 3 + kp + a.rt_parts;
     a.rt_err = 1.01f * (float)chain * 5.9604645e-8f;
 

@@ -377,6 +377,9 @@ struct FewArgs {
     int nkb_d, nkb_h, nkb_hs; // 64-row blocks of K
     int acc_cols, tmem_cols;
     int rt_eb, rt_parts, rt_dch;   // router: blocks of 8 experts, parts of d and their length
+    int rt_kp;                // warps that share K in a part
+    int sh_ratio;             // K blocks of h_s over those of h, rounded up
+    float inv_k;
     float rt_err;             // logit error bound over |x| |W_r[:, e]|
     DevStatus* status;
     uint64_t limit_ns;
