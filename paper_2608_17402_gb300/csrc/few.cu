@@ -103,7 +103,37 @@ __device__ bool few_barrier(DevStatus* st, uint64_t limit_ns) {
 
 // ------------------------------------------------------------- 1. logits
 
-// part[ds][t][e] and wsq[ds][e] of this CTA's blocks of 8 experts x parts of d.  Up to
+// Two fp32 values in one register pair, and a fused multiply-add or a sum of both in one instruction.
+__device__ __forceinline__ uint64_t f32x2(float a, float b) {
+    return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a);
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float both(uint64_t v) {
+    return __uint_as_float((uint32_t)v) + __uint_as_float((uint32_t)(v >> 32));
+}
+// Sums v[0..7] over the 8 lanes that differ in bits 0 to 2: lane l gets that of v[l & 7].
+__device__ __forceinline__ float sum8(const float v[8]) {
+    const int lane = threadIdx.x & 31;
+    float a[4], b[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        a[i] = (lane & 4 ? v[i + 4] : v[i]) + __shfl_xor_sync(0xffffffffu, lane & 4 ? v[i] : v[i + 4], 4);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        b[i] = (lane & 2 ? a[i + 2] : a[i]) + __shfl_xor_sync(0xffffffffu, lane & 2 ? a[i] : a[i + 2], 2);
+    return (lane & 1 ? b[1] : b[0]) + __shfl_xor_sync(0xffffffffu, lane & 1 ? b[0] : b[1], 1);
+}
+
+// part[ds][t][e], wsq[ds][e] and xsq[ds][t] of this CTA's blocks of 8 experts x parts of d.  Up to
 // FEW_RT_K rows at a time are staged by cp.async, all copies in flight at once: x as bf16
 // [8 TG][FEW_RT_XLD], W_r^T as fp32 [8][FEW_RT_WLD].  A warp sums 8 tokens (group g) over its
 // share kp of K; lane (ep, ks): experts ep and ep + 4, four K of every 32.
@@ -113,12 +143,14 @@ __device__ void few_logits(const FewArgs& p, uint8_t* smem) {
     float* ws = reinterpret_cast<float*>(smem);
     float* red = ws + 8 * FEW_RT_WLD;      // [KP][8 TG][8]
     float* redq = red + FEW_WARPS * 64;    // [KP][8]
-    __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(redq + FEW_WARPS * 8);
+    float* redx = redq + FEW_WARPS * 8;    // [KP][8 TG]
+    __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(redx + FEW_WARPS * 8);
     const int kp = few_div(warp, TG, __fdividef(1.0f, (float)TG)), g = warp - kp * TG, ep = lane >> 3, ks = lane & 7;
     for (int item = blockIdx.x; item < p.rt_eb * p.rt_parts; item += gridDim.x) {
         const int ds = few_div(item, p.rt_eb, __fdividef(1.0f, (float)p.rt_eb)), e0 = (item - ds * p.rt_eb) * 8;
         const int d0 = ds * p.rt_dch, d1 = min(p.d, d0 + p.rt_dch);
-        float tot[2][8] = {}, sq[2] = {};
+        uint64_t tot[2][8] = {}, sq[2] = {};   // sums of the even and of the odd K
+        float xq = 0.f;                        // lane l: |x|^2 of token 8 g + (l & 7)
         for (int k0 = d0; k0 < d1; k0 += FEW_RT_K) {
             const int kc = min(FEW_RT_K, d1 - k0), kcp = (kc + 31) & ~31;
             for (int q = threadIdx.x; q < kcp * 8; q += FEW_THREADS) {
@@ -136,53 +168,77 @@ __device__ void few_logits(const FewArgs& p, uint8_t* smem) {
             cp_async_wait_all();
             __syncthreads();
             if (kp < KP) {
-                float acc[2][8] = {};
-                int n = 0;
-                for (int it = kp; it < kcp / 32; it += KP) {
+                uint64_t acc[2][8] = {};
+                auto products = [&](int it) {   // 32 rows
                     const int k = it * 32 + ks * 4;
-                    const float4 w0 = *reinterpret_cast<const float4*>(ws + ep * FEW_RT_WLD + k);
-                    const float4 w1 = *reinterpret_cast<const float4*>(ws + (ep + 4) * FEW_RT_WLD + k);
-                    sq[0] = fmaf(w0.x, w0.x, fmaf(w0.y, w0.y, fmaf(w0.z, w0.z, fmaf(w0.w, w0.w, sq[0]))));
-                    sq[1] = fmaf(w1.x, w1.x, fmaf(w1.y, w1.y, fmaf(w1.z, w1.z, fmaf(w1.w, w1.w, sq[1]))));
+                    const ulonglong2 w0 = *reinterpret_cast<const ulonglong2*>(ws + ep * FEW_RT_WLD + k);
+                    const ulonglong2 w1 = *reinterpret_cast<const ulonglong2*>(ws + (ep + 4) * FEW_RT_WLD + k);
+                    sq[0] = fma2(w0.x, w0.x, fma2(w0.y, w0.y, sq[0]));
+                    sq[1] = fma2(w1.x, w1.x, fma2(w1.y, w1.y, sq[1]));
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {   // (rows past T hold no token: their sums are dropped)
                         const uint2 xx = *reinterpret_cast<const uint2*>(xs + (8 * g + i) * FEW_RT_XLD + k);
-                        const float x0 = __uint_as_float(xx.x << 16), x1 = __uint_as_float(xx.x & 0xffff0000u);
-                        const float x2 = __uint_as_float(xx.y << 16), x3 = __uint_as_float(xx.y & 0xffff0000u);
-                        acc[0][i] = fmaf(x3, w0.w, fmaf(x2, w0.z, fmaf(x1, w0.y, fmaf(x0, w0.x, acc[0][i]))));
-                        acc[1][i] = fmaf(x3, w1.w, fmaf(x2, w1.z, fmaf(x1, w1.y, fmaf(x0, w1.x, acc[1][i]))));
+                        const uint64_t x0 = f32x2(__uint_as_float(xx.x << 16), __uint_as_float(xx.x & 0xffff0000u));
+                        const uint64_t x1 = f32x2(__uint_as_float(xx.y << 16), __uint_as_float(xx.y & 0xffff0000u));
+                        acc[0][i] = fma2(x1, w0.y, fma2(x0, w0.x, acc[0][i]));
+                        acc[1][i] = fma2(x1, w1.y, fma2(x0, w1.x, acc[1][i]));
                     }
-                    if (++n & 1) continue;   // short chains: 8 products, then their sums
+                };
+                int it = kp;
+#pragma unroll 1
+                for (; it + KP < kcp / 32; it += 2 * KP) {
+                    products(it);
+                    products(it + KP);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                    for (int i = 0; i < 8; ++i)   // short chains: 4 products, then their sums
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
-                            tot[u][i] += acc[u][i];
-                            acc[u][i] = 0.f;
+                            tot[u][i] = add2(tot[u][i], acc[u][i]);
+                            acc[u][i] = 0ull;
                         }
                 }
+                if (it < kcp / 32) products(it);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    tot[0][i] += acc[0][i];
-                    tot[1][i] += acc[1][i];
+                    tot[0][i] = add2(tot[0][i], acc[0][i]);
+                    tot[1][i] = add2(tot[1][i], acc[1][i]);
+                }
+                if (e0 == 0) {   // squares of x: lanes ep take every fourth of the warp's 32 columns
+                    uint64_t x2[8] = {};
+#pragma unroll 1
+                    for (int xi = kp + KP * ep; xi < kcp / 32; xi += 4 * KP)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const uint2 xx =
+                                *reinterpret_cast<const uint2*>(xs + (8 * g + i) * FEW_RT_XLD + xi * 32 + ks * 4);
+                            const uint64_t x0 = f32x2(__uint_as_float(xx.x << 16), __uint_as_float(xx.x & 0xffff0000u));
+                            const uint64_t x1 = f32x2(__uint_as_float(xx.y << 16), __uint_as_float(xx.y & 0xffff0000u));
+                            x2[i] = fma2(x1, x1, fma2(x0, x0, x2[i]));
+                        }
+                    float v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = both(x2[i]);
+                    float q = sum8(v);
+                    q += __shfl_xor_sync(0xffffffffu, q, 8);
+                    xq += q + __shfl_xor_sync(0xffffffffu, q, 16);
                 }
             }
             __syncthreads();
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+            float v[8], q = both(sq[u]);
 #pragma unroll
-            for (int o = 1; o < 8; o <<= 1) {
+            for (int i = 0; i < 8; ++i) v[i] = both(tot[u][i]);
+            const float sum = sum8(v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) tot[u][i] += __shfl_xor_sync(0xffffffffu, tot[u][i], o);
-                sq[u] += __shfl_xor_sync(0xffffffffu, sq[u], o);
-            }
-            if (kp < KP && ks == 0) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) red[(kp * 8 * TG + 8 * g + i) * 8 + ep + 4 * u] = tot[u][i];
-                if (g == 0) redq[kp * 8 + ep + 4 * u] = sq[u];
+            for (int o = 1; o < 8; o <<= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
+            if (kp < KP) {
+                red[(kp * 8 * TG + 8 * g + ks) * 8 + ep + 4 * u] = sum;
+                if (g == 0 && ks == 0) redq[kp * 8 + ep + 4 * u] = q;
             }
         }
+        if (e0 == 0 && kp < KP && lane < 8) redx[kp * 8 * TG + 8 * g + lane] = xq;
         __syncthreads();
         for (int q = threadIdx.x; q < (p.T + 1) * 8; q += FEW_THREADS) {
             const int t = q >> 3, e = q & 7;
@@ -191,6 +247,11 @@ __device__ void few_logits(const FewArgs& p, uint8_t* smem) {
             if (t < p.T) {
                 for (int j = 0; j < KP; ++j) s += red[(j * 8 * TG + t) * 8 + e];
                 p.part[((int64_t)ds * p.T + t) * p.E + e0 + e] = s;
+                if (q == t * 8 && e0 == 0) {
+                    s = 0.f;
+                    for (int j = 0; j < KP; ++j) s += redx[j * 8 * TG + t];
+                    p.xsq[ds * p.T + t] = s;
+                }
             } else {
                 for (int j = 0; j < KP; ++j) s += redq[j * 8 + e];
                 p.wsq[ds * p.E + e0 + e] = s;
@@ -223,20 +284,6 @@ __device__ __forceinline__ float sum_parts(const float* q, int64_t stride, int n
 #pragma unroll
     for (int j = 1; j < 8; ++j) s += v[j];
     return s;
-}
-
-// |x_t|, by one warp.
-__device__ __forceinline__ float few_norm(const FewArgs& p, int t) {
-    const uint4* x = reinterpret_cast<const uint4*>(p.x + (int64_t)t * p.d);
-    float s = 0.f;
-#pragma unroll 4
-    for (int c = threadIdx.x & 31; c < p.d / 8; c += 32) {
-        float v[8];
-        unpack_bf16x8(__ldg(x + c), v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
-    }
-    return sqrtf(warp_sum(s));
 }
 
 // Bytes of shared memory per expert (E rounded up to 32) that one token's selection takes:
@@ -298,8 +345,8 @@ __device__ __forceinline__ void few_place(const FewArgs& p, int t, int mine, con
 }
 
 // Selection and gates of the CTA's tokens t0, t0 + step, ... (n <= FEW_SEL_WARPS of them), by all
-// threads.  xn: |x_t| of each.  buf: FEW_SEL_BYTES per expert and token.
-__device__ void few_select(const FewArgs& p, int t0, int step, int n, const float* xn, uint8_t* buf,
+// threads.  buf: FEW_SEL_BYTES per expert and token.
+__device__ void few_select(const FewArgs& p, int t0, int step, int n, uint8_t* buf,
                            int32_t* out_idx, float* out_gate, unsigned long long* mask) {
     __shared__ uint32_t s_sel[FEW_SEL_WARPS][32];
     __shared__ int n_cand[FEW_SEL_WARPS];
@@ -319,13 +366,15 @@ __device__ void few_select(const FewArgs& p, int t0, int step, int n, const floa
         if (e < p.E) {
             const float s = sum_parts(p.part + (int64_t)(t0 + w * step) * p.E + e, (int64_t)p.T * p.E, p.rt_parts);
             const float w2 = sum_parts(p.wsq + e, p.E, p.rt_parts);
+            const float x2 = sum_parts(p.xsq + t0 + w * step, p.T, p.rt_parts);
             const float v = __fdividef(1.0f, 1.0f + __expf(-s)) + __ldg(p.b + e);
             // Half-width of the key: a quarter (the sigmoid's largest slope; and some, for the
             // square root) of the logit's error bound, and the fp32 evaluation (fast sigmoid:
             // under 1e-6; the sum's rounding).  A NaN bound bounds nothing.
-            float wn;
+            float wn, xn;
             asm("sqrt.approx.f32 %0, %1;" : "=f"(wn) : "f"(w2));
-            const float r = 0.2501f * p.rt_err * xn[w] * wn + 2e-6f + 2.4e-7f * fabsf(v), a = v - r, b = v + r;
+            asm("sqrt.approx.f32 %0, %1;" : "=f"(xn) : "f"(x2));
+            const float r = 0.2501f * p.rt_err * xn * wn + 2e-6f + 2.4e-7f * fabsf(v), a = v - r, b = v + r;
             o = key_order(v);
             oa = a == a ? key_order(a) : 0u;
             ob = b == b ? key_order(b) : 0xffffffffu;
@@ -966,7 +1015,6 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     volatile int* flags = reinterpret_cast<volatile int*>(after);            // 2 x 65 ints
     volatile int* abort_flag = flags + 130;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(after) + 131;
-    float* xn = reinterpret_cast<float*>(after) + 132;                       // [FEW_SEL_WARPS]
     uint8_t* at = after + FEW_FLAG_BYTES;
     const int n = p.T * p.k, na = p.na_max;
     FewLists L;
@@ -1035,15 +1083,11 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     // tokens of this CTA: all, or every gridDim.x-th
     const int t0 = everywhere ? 0 : blockIdx.x, step = everywhere ? 1 : (int)gridDim.x;
     const int mine = everywhere ? p.T : (p.T - t0 + step - 1) / step;
-    if (warp < min(mine, FEW_SEL_WARPS)) {   // while the other CTAs arrive
-        const float v = few_norm(p, t0 + warp * step);
-        if ((threadIdx.x & 31) == 0) xn[warp] = v;
-    }
     if (!few_barrier(p.status, p.limit_ns)) return give_up();
     if (everywhere) {
         int32_t* s_idx = reinterpret_cast<int32_t*>(off + ((p.E + 1) & ~1));
         float* s_gate = reinterpret_cast<float*>(s_idx + n);
-        few_select(p, 0, 1, mine, xn, smem, s_idx, s_gate, mask);
+        few_select(p, 0, 1, mine, smem, s_idx, s_gate, mask);
         if (blockIdx.x == 0)
             for (int i = threadIdx.x; i < n; i += FEW_THREADS) {
                 p.idx[i] = s_idx[i];
@@ -1053,11 +1097,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     } else {
         const int most = min(FEW_SEL_WARPS, ring_bytes / sel_bytes);   // (one batch, unless the GPU is tiny)
         for (int i = 0; i < mine; i += most) {
-            if (i > 0) {
-                if (i + warp < mine && warp < most) xn[warp] = few_norm(p, t0 + (i + warp) * step);
-                __syncthreads();
-            }
-            few_select(p, t0 + i * step, step, min(most, mine - i), xn, smem, p.idx, p.gate, nullptr);
+            few_select(p, t0 + i * step, step, min(most, mine - i), smem, p.idx, p.gate, nullptr);
         }
         if (!few_barrier(p.status, p.limit_ns)) return give_up();
         few_plan<false>(p, L, p.idx, p.gate, mask, off);
@@ -1098,7 +1138,7 @@ int few_rt_parts(int d, int E, int ctas) {
 }
 
 struct FewLayout {
-    size_t idx, gate, part, wsq, counters, H, Hs, y_part, total;
+    size_t idx, gate, part, wsq, xsq, counters, H, Hs, y_part, total;
     int64_t n_done, n_y_cnt;
 };
 FewLayout few_layout(int64_t T, int64_t d, int64_t E, int64_t k, int64_t h, int64_t hs) {
@@ -1114,6 +1154,7 @@ FewLayout few_layout(int64_t T, int64_t d, int64_t E, int64_t k, int64_t h, int6
     L.gate = take(4 * n);
     L.part = take(4 * 8 * T * E);
     L.wsq = take(4 * 8 * E);
+    L.xsq = take(4 * 8 * T);
     L.n_done = na + (T + few_nb((int)T) - 1) / few_nb((int)T);
     L.n_y_cnt = T * ((d + 63) / 64);   // at most: 64-column items
     L.counters = take(4 * (L.n_done + L.n_y_cnt));
@@ -1137,6 +1178,7 @@ cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaS
     if (!a.gate) a.gate = reinterpret_cast<float*>(ws + L.gate);
     a.part = reinterpret_cast<float*>(ws + L.part);
     a.wsq = reinterpret_cast<float*>(ws + L.wsq);
+    a.xsq = reinterpret_cast<float*>(ws + L.xsq);
     a.done_up = reinterpret_cast<int32_t*>(ws + L.counters);
     a.y_cnt = a.done_up + L.n_done;
     a.n_counters = (int)(L.n_done + L.n_y_cnt);
@@ -1164,7 +1206,7 @@ cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaS
     // length of the summation chains of a logit (few_logits): 8 products, their sums (one more per
     // staged block), the lanes, the warps, the parts; times 2^-24, with room for second order
     const int kp = a.rt_kp = FEW_WARPS / ((a.T + 7) / 8), blocks = (a.rt_dch + FEW_RT_K - 1) / FEW_RT_K;
-    const int chain = 8 + (a.rt_dch / (64 * kp) + 2 * blocks) + 3 + kp + a.rt_parts;
+    const int chain = 5 + (a.rt_dch / (64 * kp) + 2 * blocks) + 3 + kp + a.rt_parts;
     a.rt_err = 1.01f * (float)chain * 5.9604645e-8f;
 
     bool ok = make_weight_tmap_strided(&a.tW1, a.W1, a.h, a.d, a.E, a.hp, (int64_t)a.d * a.hp) &&

@@ -367,7 +367,8 @@ struct FewArgs {
     CUtensorMap tW1, tW3, tW2, tS1, tS3, tS2;   // weights, 3-D {N, K, E}, boxes 64 x 64
     CUtensorMap tX;                             // token rows, one-row boxes (gather)
     CUtensorMap tH, tHs;                        // hidden rows, 3-D {h, rows, 2}, boxes 64 x 16
-    float *part, *wsq;        // router: partial logits [rt_parts][T][E], sums of squares [rt_parts][E]
+    // router: partial logits [rt_parts][T][E], sums of squares [rt_parts][E] (W_r), [rt_parts][T] (x)
+    float *part, *wsq, *xsq;
     int32_t *done_up, *y_cnt; // counters, n_counters in a row from done_up
     int n_counters;
     __nv_bfloat16 *H, *Hs;    // hidden rows, hi then lo: [2][T k][ldh], [2][T][ldhs]
