@@ -49,7 +49,7 @@ constexpr int FEW_RT_K = 512;         // rows of W_r staged at a time
 constexpr int FEW_RT_XLD = FEW_RT_K + 16;      // row strides of the staged x (bf16; rows 16-byte
 constexpr int FEW_RT_WLD = FEW_RT_K + 4;       //   aligned) and W_r^T (fp32)
 constexpr int FEW_SMEM_MAX = 232448 - 3072;   // 227 KB less the kernel's static variables
-constexpr int FEW_BAR_BYTES = 512, FEW_FLAG_BYTES = 576;   // (multiples of 64)
+constexpr int FEW_BAR_BYTES = 512, FEW_FLAG_BYTES = 64;   // (multiples of 64)
 // Parts of K at most: of a routed and of a shared down item.
 constexpr int FEW_MAX_P2 = 4, FEW_MAX_P2S = 8;
 
@@ -841,15 +841,83 @@ __device__ void few_mma(const FewArgs& p, const FewSmem& sm, const FewLists& L, 
     }
 }
 
+// y of the tokens: a warp per token and column tile of the down items (two tokens where tiles have
+// 64 columns), the same share for every warp of the grid, each when its tile's last part has been
+// counted.  Slots in order, a slot's parts in order.  A lane holds the index and the weight of one
+// row; four columns each.  (Summed by whoever came last, a tile of 32 tokens was eight tokens' loads
+// one after the other in one warp, while the rest of the grid had finished: 6 us at the end of 64
+// tokens of 8 slots.)
+__device__ void few_combine(const FewArgs& p, const FewLists& L, const FewPlan& pl, volatile int* abort_flag) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int width = pl.tw2 == 128 ? 32 : 16, sub = lane & (width - 1), half = lane != sub;
+    const int per = 32 / width, nr = p.k * pl.P2, na = nr + (p.hs > 0 ? pl.P2s : 0), slots = p.T * p.k;
+    for (int u = warp * gridDim.x + blockIdx.x; u < (p.T + per - 1) / per * pl.ntd; u += gridDim.x * FEW_EPI_WARPS) {
+        const int tp = few_div(u, pl.ntd, pl.inv_ntd), dt = u - tp * pl.ntd, t = tp * per + half;
+        const int cc = dt * pl.tw2 + sub * 4;   // d is a multiple of 8
+        const bool in = t < p.T && cc < p.d;
+        uint64_t t0 = 0;
+        for (uint32_t i = 1;; ++i) {
+            const bool done = sub != 0 || t >= p.T || ld_acquire(p.y_cnt + t * pl.ntd + dt) >= na;
+            if (__all_sync(0xffffffffu, done)) break;
+            __nanosleep(100);
+            if ((i & 63u) != 0u) continue;
+            const uint64_t now = globaltimer_ns();
+            if (t0 == 0) t0 = now;
+            if (__any_sync(0xffffffffu, now - t0 > p.limit_ns || *abort_flag)) {
+                if (lane == 0) few_abort(abort_flag, p.status, SITE_FEW_WAIT_Y, u);
+                return;
+            }
+        }
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int r0 = 0; r0 < na; r0 += width) {
+            const int r = r0 + sub;
+            int row = 0;
+            float g = 0.f;
+            if (t < p.T && r < nr) {
+                const int j = few_div(r, pl.P2, pl.inv_P2), q = t * p.k + j;
+                row = (r - j * pl.P2) * slots + L.row_of[q];
+                g = L.gate[q];
+            } else if (t < p.T && r < na) {
+                row = pl.P2 * slots + (r - nr) * p.T + t;
+                g = p.lambda;
+            }
+            for (int i0 = 0; i0 < width && r0 + i0 < na; i0 += 8) {
+                float4 a[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {   // eight rows' loads in flight
+                    const int at = __shfl_sync(0xffffffffu, row, i0 + i, width);
+                    a[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (in && r0 + i0 + i < na)
+                        a[i] = __ldcg(reinterpret_cast<const float4*>(p.y_part + (int64_t)at * p.d + cc));
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float gi = __shfl_sync(0xffffffffu, g, i0 + i, width);
+                    if (r0 + i0 + i >= na) break;
+                    y.x = fmaf(gi, a[i].x, y.x);
+                    y.y = fmaf(gi, a[i].y, y.y);
+                    y.z = fmaf(gi, a[i].z, y.z);
+                    y.w = fmaf(gi, a[i].w, y.w);
+                }
+            }
+        }
+        if (in) {
+            uint2 o;
+            o.x = pack_bf16x2(y.x, y.y);
+            o.y = pack_bf16x2(y.z, y.w);
+            *reinterpret_cast<uint2*>(p.y + (int64_t)t * p.d + cc) = o;
+        }
+    }
+}
+
 // Two groups of four warps take the CTA's items in turn (accumulator = group), so that the trips
 // to L2 of one item's bookkeeping overlap the next item's.  Warp w of a group reads TMEM lanes
 // 32 w .. (its columns of W) for all tokens.  One thread waits and decides for its group, so
 // that the warps take the same way through its barriers.
 __device__ void few_epilogue(const FewArgs& p, const FewSmem& sm, const FewLists& L, uint32_t tmem,
-                             volatile int* abort_flag, volatile int* flags_all) {
+                             volatile int* abort_flag, volatile int* flags) {
     const int group = threadIdx.x >> 7, tid = threadIdx.x & 127, warp = tid >> 5, lane = tid & 31;
     const FewPlan pl = *L.plan;
-    volatile int* flags = flags_all + group * 65;
     const bool two = p.W3 != nullptr;
     const int64_t slots = (int64_t)p.T * p.k;
     const uint32_t tb = tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)(group * p.acc_cols);
@@ -859,10 +927,10 @@ __device__ void few_epilogue(const FewArgs& p, const FewSmem& sm, const FewLists
         if (tid == 0) {
             const bool ok = mbar_wait(sm.tfull + 8 * group, (uint32_t)n & 1u, p.limit_ns, abort_flag);
             if (!ok) few_abort(abort_flag, p.status, SITE_FEW_WAIT_TFULL, id);
-            flags[64] = ok;
+            flags[group] = ok;
         }
         epi_sync(group);
-        if (!flags[64]) return;
+        if (!flags[group]) return;
         tc_fence_after();
         const int c = tid, N = up16(it.cnt);
         const bool active = 32 * warp < it.tw;
@@ -921,63 +989,12 @@ __device__ void few_epilogue(const FewArgs& p, const FewSmem& sm, const FewLists
             __syncwarp();
             if (lane == 0) mbar_arrive(sm.tempty + 8 * group);
             epi_sync(group);
-            const int dt = it.n0 / it.tw, want = p.k * pl.P2 + (p.hs > 0 ? pl.P2s : 0);
-            if (tid < it.cnt) {
-                const int t = it.shared ? it.row0 + tid : L.row_tok[it.row0 + tid];
-                flags[tid] = add_acq_rel(p.y_cnt + t * pl.ntd + dt, 1) == want - 1 ? t : -1;
-            }
-            epi_sync(group);
-            // Tokens that are now complete in these columns: slots in order, a slot's parts in
-            // order.  A lane holds the offset and the weight of one row; four columns each.
-            for (int j = warp; j < it.cnt; j += 4) {
-                const int t = flags[j];
-                if (t < 0) continue;
-                const int cc = it.n0 + lane * 4, nr = p.k * pl.P2, na = want;   // d is a multiple of 8
-                const bool in = lane * 4 < it.tw && cc < p.d;
-                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int r0 = 0; r0 < na; r0 += 32) {
-                    const int r = r0 + lane;
-                    int64_t row = 0;
-                    float g = 0.f;
-                    if (r < nr) {
-                        const int q = t * p.k + r / pl.P2;
-                        row = (int64_t)(r % pl.P2) * slots + L.row_of[q];
-                        g = L.gate[q];
-                    } else if (r < na) {
-                        row = (int64_t)pl.P2 * slots + (int64_t)(r - nr) * p.T + t;
-                        g = p.lambda;
-                    }
-                    row = row * p.d + cc - lane * 4;
-                    for (int i0 = 0; i0 < 32 && r0 + i0 < na; i0 += 8) {
-                        float4 a[8];
-                        float gi[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {   // eight rows' loads in flight
-                            const int64_t at = __shfl_sync(0xffffffffu, row, i0 + i);
-                            gi[i] = __shfl_sync(0xffffffffu, g, i0 + i);
-                            a[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                            if (in && r0 + i0 + i < na)
-                                a[i] = __ldcg(reinterpret_cast<const float4*>(p.y_part + at + lane * 4));
-                        }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            if (r0 + i0 + i >= na) break;
-                            y.x = fmaf(gi[i], a[i].x, y.x);
-                            y.y = fmaf(gi[i], a[i].y, y.y);
-                            y.z = fmaf(gi[i], a[i].z, y.z);
-                            y.w = fmaf(gi[i], a[i].w, y.w);
-                        }
-                    }
-                }
-                if (in) {
-                    uint2 u;
-                    u.x = pack_bf16x2(y.x, y.y);
-                    u.y = pack_bf16x2(y.z, y.w);
-                    *reinterpret_cast<uint2*>(p.y + (int64_t)t * p.d + cc) = u;
-                }
-            }
+            const int dt = it.tw == 128 ? it.n0 >> 7 : it.n0 >> 6;
+            if (tid < it.cnt)
+                add_release(p.y_cnt + (it.shared ? it.row0 + tid : L.row_tok[it.row0 + tid]) * pl.ntd + dt, 1);
         }
     }
+    few_combine(p, L, pl, abort_flag);
 }
 
 // ----------------------------------------------------------------- kernel
@@ -1012,9 +1029,9 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     const FewSizes z = few_sizes(p.T, p.k, p.E);
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + z.stages * z.stage_bytes);
     uint8_t* after = reinterpret_cast<uint8_t*>(bars) + FEW_BAR_BYTES;
-    volatile int* flags = reinterpret_cast<volatile int*>(after);            // 2 x 65 ints
-    volatile int* abort_flag = flags + 130;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(after) + 131;
+    volatile int* flags = reinterpret_cast<volatile int*>(after);            // of the epilogue groups
+    volatile int* abort_flag = flags + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(after) + 3;
     uint8_t* at = after + FEW_FLAG_BYTES;
     const int n = p.T * p.k, na = p.na_max;
     FewLists L;
