@@ -60,6 +60,7 @@ enum Site : int {
     SITE_FEW_BARRIER = 55,
     SITE_FEW_DRAIN = 56,
     SITE_FEW_WAIT_Y = 57,
+    SITE_FEW_WAIT_TURN = 58,
 };
 
 __device__ __forceinline__ void report(DevStatus* st, int code, int site, int a, int b) {

@@ -40,11 +40,12 @@ namespace {
 constexpr int FEW_EPI_WARPS = 8;      // two groups of four (one warp per TMEM lane quadrant)
 constexpr int FEW_WARP_W = 8;         // weight loads
 constexpr int FEW_WARP_MMA = 9;
-constexpr int FEW_WARP_B = 10;        // token / hidden loads
+constexpr int FEW_WARP_B = 10;        // token / hidden loads: two warps in turn
 constexpr int FEW_WARPS = 12;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
 constexpr int FEW_SEL_WARPS = 8;      // tokens that every CTA selects for itself
 constexpr int FEW_TILE_BYTES = 128 * 64 * 2;   // 128 columns x 64 K rows of a weight matrix
+constexpr int FEW_TOKEN_BYTES = 2 * 32 * 128;   // token rows of a stage
 constexpr int FEW_RT_K = 512;         // rows of W_r staged at a time
 constexpr int FEW_RT_XLD = FEW_RT_K + 16;      // row strides of the staged x (bf16; rows 16-byte
 constexpr int FEW_RT_WLD = FEW_RT_K + 4;       //   aligned) and W_r^T (fp32)
@@ -498,7 +499,7 @@ struct FewPlan {
 struct FewItem {
     int up, shared, i;      // i: entry (routed), block of nb tokens (shared)
     int e;
-    int n0, tw, kb0, kb1;   // columns; K blocks (up, SwiGLU: gate and up blocks alternate)
+    int n0, tw, kb0, kb1;   // columns; K blocks of 64
     int part;               // down: K part
     int cnt, row0;          // tokens, first row
 };
@@ -523,7 +524,7 @@ __device__ __forceinline__ FewItem few_item(const FewArgs& p, const FewLists& L,
     if (it.up) {
         it.tw = pl.tw;
         it.kb0 = 0;
-        it.kb1 = p.nkb_d * (p.W3 ? 2 : 1);
+        it.kb1 = p.nkb_d;
         if (!it.shared) q -= pl.n_up_shared;
         const int per = it.shared ? p.n_sh : pl.nt;   // shared: the blocks of a tile side by side
         const int r = few_div(q, per, it.shared ? pl.inv_sh : pl.inv_nt);
@@ -546,6 +547,31 @@ __device__ __forceinline__ FewItem few_item(const FewArgs& p, const FewLists& L,
     it.row0 = it.shared ? it.i * p.nb : L.off[it.i];
     it.cnt = it.shared ? min(p.nb, p.T - it.row0) : L.cnt[it.i];
     return it;
+}
+
+// How an item goes through the ring.  A stage holds two halves of 64 columns x 64 K of weights and
+// the token blocks that they meet.  128-column items: a K block's columns (SwiGLU: the gate's and
+// the up projection's in turn); 64-column ones: the gate's and the up projection's columns of a K
+// block (SwiGLU up items), else two K blocks, where both token blocks fit.  (One K block a stage
+// left half the ring empty for 64-column items: one token's up items took 217 ns per 8 KB, with
+// two 145 ns.)
+struct FewSteps {
+    int n;               // stages
+    int wide, two;       // 128 columns; SwiGLU up item
+    int alt, pair;       // wide and two; two K blocks a stage
+    int half2, last2;    // the second half is used, in the last stage
+};
+__device__ __forceinline__ FewSteps few_steps(const FewArgs& p, const FewItem& it) {
+    FewSteps r;
+    const int nk = it.kb1 - it.kb0;
+    r.two = it.up && p.W3;
+    r.wide = it.tw == 128;
+    r.alt = r.wide & r.two;
+    r.pair = !r.wide && !r.two && (it.up ? 2 : 4) * up16(it.cnt) * 128 <= FEW_TOKEN_BYTES;
+    r.n = r.pair ? (nk + 1) >> 1 : nk << r.alt;
+    r.half2 = r.wide | r.two | r.pair;
+    r.last2 = r.pair ? (nk & 1) ^ 1 : r.half2;
+    return r;
 }
 
 // Estimated time (ns) of `items` items of `blocks` K blocks of `kb` bytes: an SM takes a block
@@ -639,16 +665,21 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
         // 64-column items where 128-column ones are too few to keep all SMs streaming; down items
         // may also split K (their partial rows are joined anyway).
         // (shifts and reciprocals: this is on the way of every CTA's first load)
-        const int ctas = (int)gridDim.x, mats = p.W3 ? 2 : 1;
+        const int ctas = (int)gridDim.x;
         const int bn = up16(min((int)__fdividef((float)(n + n_act - 1), (float)n_act), p.nb)) * 128;
         const int s_l = 7 - (lane & 1), tw_l = 1 << s_l;
         const int tiles_l = n_act * ((p.h + tw_l - 1) >> s_l) + p.n_sh * ((p.hs + tw_l - 1) >> s_l);
-        const int up = few_fastest(lane < 2 ? few_time(tiles_l, mats * p.nkb_d, tw_l * 128 + bn, ctas) : 3.0e38f);
+        const bool w128 = s_l == 7;
+        const int up_steps = p.W3 ? (w128 ? 2 : 1) * p.nkb_d : w128 ? p.nkb_d : (p.nkb_d + 1) >> 1;
+        const int up = few_fastest(
+            lane < 2 ? few_time(tiles_l, up_steps, FEW_TILE_BYTES + (w128 || p.W3 ? bn : 2 * bn), ctas) : 3.0e38f);
         const int P_l = (lane >> 1) + 1, ntd_l = (p.d + tw_l - 1) >> s_l;
         const int items_l = ntd_l * P_l * (n_act + p.n_sh * p.sh_ratio);
         const int blocks_l = (int)__fdividef((float)(p.nkb_h + P_l - 1) + 0.5f, (float)P_l);
+        const bool pair_l = !w128 && 4 * bn <= FEW_TOKEN_BYTES;
         const int dn = few_fastest(P_l <= FEW_MAX_P2 && P_l <= p.nkb_h
-                                       ? few_time(items_l, blocks_l, tw_l * 128 + 2 * bn, ctas)
+                                       ? few_time(items_l, pair_l ? (blocks_l + 1) >> 1 : blocks_l,
+                                                  (pair_l ? 2 : 1) * (tw_l * 128 + 2 * bn), ctas)
                                        : 3.0e38f);
         if (lane == 0) {
             FewPlan& pl = *L.plan;
@@ -692,6 +723,8 @@ __device__ void few_plan(const FewArgs& p, const FewLists& L, const int32_t* idx
 
 struct FewSmem {
     uint32_t ring, full, empty, tfull, tempty, drain;
+    uint32_t b_turn;           // barriers of the two warps that load the N operand
+    volatile int* b_next;
     int stages, stage_bytes;   // a stage: weights (FEW_TILE_BYTES), then the N operand
 };
 
@@ -708,20 +741,23 @@ __device__ void few_load_w(const FewArgs& p, const FewSmem& sm, const FewLists& 
     uint32_t ph = 0;
     for (int id = blockIdx.x; id < n_items; id += gridDim.x) {
         const FewItem it = few_item(p, L, id);
+        const FewSteps st = few_steps(p, it);
         const CUtensorMap* a = it.up ? (it.shared ? &p.tS1 : &p.tW1) : (it.shared ? &p.tS2 : &p.tW2);
         const CUtensorMap* a3 = it.shared ? &p.tS3 : &p.tW3;
-        const int two = it.up && p.W3;
-        for (int kb = it.kb0; kb < it.kb1; ++kb) {
+        const int n2 = it.n0 + (st.wide ? 64 : 0), dk2 = st.pair ? 64 : 0;
+        int k = it.kb0 * 64;
+        for (int i = 0; i < st.n; ++i) {
             if (!mbar_wait(sm.empty + 8 * s, ph ^ 1u, p.limit_ns, abort_flag)) {
                 few_abort(abort_flag, p.status, SITE_FEW_WAIT_EMPTY, id);
                 return;
             }
             const uint32_t bar = sm.full + 8 * s, dst = sm.ring + s * sm.stage_bytes;
-            mbar_arrive_expect_tx(bar, it.tw * 128);
-            const CUtensorMap* m = (two & kb) ? a3 : a;
-            const int k0 = (kb >> two) * 64;
-            tma_load_3d_hint(dst, m, bar, it.n0, k0, it.e, pol);
-            if (it.tw == 128) tma_load_3d_hint(dst + FEW_TILE_BYTES / 2, m, bar, it.n0 + 64, k0, it.e, pol);
+            const int second = i + 1 < st.n ? st.half2 : st.last2, odd = st.alt & i;
+            mbar_arrive_expect_tx(bar, (1 + second) * (FEW_TILE_BYTES / 2));
+            tma_load_3d_hint(dst, odd ? a3 : a, bar, it.n0, k, it.e, pol);
+            if (second)
+                tma_load_3d_hint(dst + FEW_TILE_BYTES / 2, st.alt == odd && st.two ? a3 : a, bar, n2, k + dk2, it.e, pol);
+            k += st.pair ? 128 : st.alt == odd ? 64 : 0;
             if (++s == sm.stages) {
                 s = 0;
                 ph ^= 1u;
@@ -731,23 +767,30 @@ __device__ void few_load_w(const FewArgs& p, const FewSmem& sm, const FewLists& 
 }
 
 // The N operand: token rows (up) or the two pieces of the hidden rows (down: hi, then lo N rows
-// further), after the entry's up items are done.  Rows past the entry's last token repeat its
-// first (up) or hold whatever follows (down): their columns of D are not read.
-__device__ void few_load_b(const FewArgs& p, const FewSmem& sm, const FewLists& L, volatile int* abort_flag) {
+// further), after the entry's up items are done.  Up to 16 tokens: all of them, in order, in one
+// copy, whichever the entry has.  More: a gather of the entry's; rows past its last token repeat
+// its first.  Rows past the last one hold whatever follows (down).  Columns of D that are not the
+// entry's are not read.
+//
+// Two warps in turn, an item each: while one loads, the other decodes its item and waits for the
+// hidden rows (a trip to L2, 0.7 us of the 1.5 us that a short item took).
+__device__ void few_load_b(const FewArgs& p, const FewSmem& sm, const FewLists& L, int who, volatile int* abort_flag) {
     const int n_items = L.plan->n_items;
-    int s = 0;
-    uint32_t ph = 0;
-    for (int id = blockIdx.x; id < n_items; id += gridDim.x) {
+    const bool direct = p.T <= 16;
+    volatile int* next = sm.b_next;   // stage and phase where the other warp stopped
+    uint32_t turn = 0;
+    for (int id = blockIdx.x + who * gridDim.x; id < n_items; id += 2 * gridDim.x, turn ^= 1u) {
         const FewItem it = few_item(p, L, id);
-        const int N = up16(it.cnt);
+        const FewSteps st = few_steps(p, it);
+        const int N = up16(it.cnt), bytes = (it.up ? 1 : 2) * N * 128;
         int tok[32];
-        if (it.up) {
+        if (it.up && !direct) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 const int j = i < it.cnt ? i : 0;
                 if (i < N) tok[i] = it.shared ? it.row0 + j : L.row_tok[it.row0 + j];
             }
-        } else {
+        } else if (!it.up) {
             const int32_t* c = p.done_up + (it.shared ? p.na_max + it.i : it.i);
             const int want = it.shared ? L.plan->nt_s : L.plan->nt;
             const uint64_t t0 = globaltimer_ns();
@@ -758,33 +801,49 @@ __device__ void few_load_b(const FewArgs& p, const FewSmem& sm, const FewLists& 
                 }
             fence_proxy_async_all();   // the hidden rows were written by ordinary stores
         }
-        const int two = it.up && p.W3;
         const CUtensorMap* h = it.shared ? &p.tHs : &p.tH;
-        for (int kb = it.kb0; kb < it.kb1; ++kb) {
+        // (who 0's first turn passes: the phase before the first)
+        if (!mbar_wait(sm.b_turn + 8 * who, turn ^ (who == 0 ? 1u : 0u), p.limit_ns, abort_flag)) {
+            few_abort(abort_flag, p.status, SITE_FEW_WAIT_TURN, id);
+            return;
+        }
+        int s = next[0];
+        uint32_t ph = (uint32_t)next[1];
+        int k = it.kb0 * 64;
+        for (int i = 0; i < st.n; ++i) {
             if (!mbar_wait(sm.empty + 8 * s, ph ^ 1u, p.limit_ns, abort_flag)) {
                 few_abort(abort_flag, p.status, SITE_FEW_WAIT_EMPTY, -id);
                 return;
             }
-            const uint32_t bar = sm.full + 8 * s, dst = sm.ring + s * sm.stage_bytes + FEW_TILE_BYTES;
-            mbar_arrive_expect_tx(bar, (it.up ? 1 : 2) * N * 128);
-            const int k0 = (kb >> two) * 64;
-            if (it.up) {
+            const uint32_t bar = sm.full + 8 * s;
+            uint32_t dst = sm.ring + s * sm.stage_bytes + FEW_TILE_BYTES;
+            const int blocks = st.pair && (i + 1 < st.n || st.last2) ? 2 : 1;
+            mbar_arrive_expect_tx(bar, blocks * bytes);
+            for (int k1 = k; k1 < k + 64 * blocks; k1 += 64, dst += bytes) {
+                if (!it.up) {
 #pragma unroll
-                for (int r = 0; r < 32; r += 4)
-                    if (r < N) tma_gather4(dst + r * 128, &p.tX, bar, k0, tok[r], tok[r + 1], tok[r + 2], tok[r + 3]);
-            } else {
+                    for (int r = 0; r < 32; r += 16)
+                        if (r < N) {
+                            tma_load_3d(dst + r * 128, h, bar, k1, it.row0 + r, 0);
+                            tma_load_3d(dst + (N + r) * 128, h, bar, k1, it.row0 + r, 1);
+                        }
+                } else if (direct) {
+                    tma_load_3d(dst, &p.tX, bar, k1, 0, 0);
+                } else {
 #pragma unroll
-                for (int r = 0; r < 32; r += 16)
-                    if (r < N) {
-                        tma_load_3d(dst + r * 128, h, bar, k0, it.row0 + r, 0);
-                        tma_load_3d(dst + (N + r) * 128, h, bar, k0, it.row0 + r, 1);
-                    }
+                    for (int r = 0; r < 32; r += 4)
+                        if (r < N) tma_gather4(dst + r * 128, &p.tX, bar, k1, tok[r], tok[r + 1], tok[r + 2], tok[r + 3]);
+                }
             }
+            k += st.pair ? 128 : st.alt ? (i & 1) * 64 : 64;
             if (++s == sm.stages) {
                 s = 0;
                 ph ^= 1u;
             }
         }
+        next[0] = s;
+        next[1] = (int)ph;
+        mbar_arrive(sm.b_turn + 8 * (who ^ 1));
     }
 }
 
@@ -801,9 +860,10 @@ __device__ void few_mma(const FewArgs& p, const FewSmem& sm, const FewLists& L, 
     for (int id = blockIdx.x; id < n_items; id += gridDim.x, ++n) {
         const FewItem it = few_item(p, L, id);
         // down: hi and lo pieces of the tokens side by side, added by the epilogue
-        const uint32_t idesc = idesc_bf16_f32(128, (it.up ? 1 : 2) * up16(it.cnt), true, false);
-        const int acc = n & 1;
-        const int two = it.up && p.W3;   // gate blocks into columns 0 .., up blocks into nb ..
+        const int N = up16(it.cnt), acc = n & 1;
+        const uint32_t idesc = idesc_bf16_f32(128, (it.up ? 1 : 2) * N, true, false);
+        const FewSteps st = few_steps(p, it);
+        const uint32_t bd2 = st.pair ? ((it.up ? 1 : 2) * N * 128) >> 4 : 0, dd2 = st.two ? p.nb : 0;
         if (!mbar_wait(sm.tempty + 8 * acc, ((uint32_t)(n >> 1) & 1u) ^ 1u, p.limit_ns, abort_flag)) {
             few_abort(abort_flag, p.status, SITE_FEW_WAIT_TEMPTY, id);
             break;
@@ -811,18 +871,25 @@ __device__ void few_mma(const FewArgs& p, const FewSmem& sm, const FewLists& L, 
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)(acc * p.acc_cols);
         bool ok = true;
-        for (int kb = it.kb0; kb < it.kb1; ++kb) {
+        for (int i = 0; i < st.n; ++i) {
             if (!mbar_wait(sm.full + 8 * s, ph, p.limit_ns, abort_flag)) {
                 few_abort(abort_flag, p.status, SITE_FEW_WAIT_FULL, id);
                 ok = false;
                 break;
             }
+            // gate columns into 0 .., up columns into nb ..
             const uint64_t wd = wd0 + (uint64_t)((s * sm.stage_bytes) >> 4);
             const uint64_t bd = bd0 + (uint64_t)((s * sm.stage_bytes) >> 4);
+            const uint32_t d0 = d + (st.alt & i ? p.nb : 0), add = i > st.alt ? 1u : 0u;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                tc_mma_bf16(d + ((two & kb) ? p.nb : 0), wd + q * (2048 >> 4), bd + q * (32 >> 4), idesc,
-                            (kb > it.kb0 + two || q != 0) ? 1u : 0u);
+            for (int q = 0; q < 4; ++q)
+                tc_mma_bf16(d0, wd + q * (2048 >> 4), bd + q * (32 >> 4), idesc, add | (q != 0 ? 1u : 0u));
+            if (!st.wide && (i + 1 < st.n ? st.half2 : st.last2)) {
+                const uint32_t add2 = add | (uint32_t)st.pair;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    tc_mma_bf16(d + dd2, wd + ((8192 + q * 2048) >> 4), bd + bd2 + q * (32 >> 4), idesc,
+                                add2 | (q != 0 ? 1u : 0u));
             }
             issued = true;
             tc_commit(sm.empty + 8 * s);
@@ -939,8 +1006,15 @@ __device__ void few_epilogue(const FewArgs& p, const FewSmem& sm, const FewLists
             const bool ok = c < it.tw && col < h;
             __nv_bfloat16* hi = (it.shared ? p.Hs : p.H) + (int64_t)it.row0 * ld + col;
             __nv_bfloat16* lo = hi + (it.shared ? (int64_t)p.T : slots) * ld;
-            for (int j0 = 0; j0 < it.cnt && active; j0 += 8) {
+            // columns of D that are the entry's tokens, in the order of its rows
+            uint32_t own = 0xffffffffu >> (32 - it.cnt);
+            if (p.T <= 16 && !it.shared) {
+                own = 0u;
+                for (int j = 0; j < it.cnt; ++j) own |= 1u << L.row_tok[it.row0 + j];
+            }
+            for (int j0 = 0; j0 < 32 && (own >> j0) != 0u && active; j0 += 8) {
                 uint32_t u[8], v[8];
+                if ((own >> j0 & 0xffu) == 0u) continue;
                 tmem_ld_32x32b_x8(tb + j0, u);
                 if (two) tmem_ld_32x32b_x8(tb + p.nb + j0, v);
                 tmem_wait_ld();
@@ -957,10 +1031,11 @@ __device__ void few_epilogue(const FewArgs& p, const FewSmem& sm, const FewLists
                 }
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (ok && j0 + i < it.cnt) {   // two bf16 pieces: 16 significant bits
+                    if (ok && (own >> (j0 + i) & 1u)) {   // two bf16 pieces: 16 significant bits
+                        const int64_t r = __popc(own & ((1u << (j0 + i)) - 1u));
                         const __nv_bfloat16 a = __float2bfloat16_rn(f[i]);
-                        hi[(int64_t)(j0 + i) * ld] = a;
-                        lo[(int64_t)(j0 + i) * ld] = __float2bfloat16_rn(f[i] - __bfloat162float(a));
+                        hi[r * ld] = a;
+                        lo[r * ld] = __float2bfloat16_rn(f[i] - __bfloat162float(a));
                     }
             }
             tc_fence_before();
@@ -1012,7 +1087,7 @@ __host__ __device__ inline int few_entries(int T, int k, int E) {   // at most
 __host__ __device__ inline FewSizes few_sizes(int T, int k, int E) {
     FewSizes z;
     const int n = T * k, na = few_entries(T, k, E);
-    z.stage_bytes = FEW_TILE_BYTES + 2 * few_nb(T) * 128;
+    z.stage_bytes = FEW_TILE_BYTES + FEW_TOKEN_BYTES;
     // plan, gate, row_of, act, off, cnt, row_tok
     z.lists = 128 + ((4 * n + 2 * n + 4 * na + na + n + 15) & ~15);
     const int left = FEW_SMEM_MAX - 1024 - FEW_BAR_BYTES - FEW_FLAG_BYTES - z.lists;
@@ -1051,6 +1126,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     sm.tfull = sm.empty + 8 * 12;
     sm.tempty = sm.tfull + 16;
     sm.drain = sm.tempty + 16;
+    sm.b_turn = sm.drain + 8;
+    sm.b_next = flags + 4;
     const int warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         for (int s = 0; s < z.stages; ++s) {
@@ -1062,6 +1139,9 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
             mbar_init(sm.tempty + 8 * a, FEW_EPI_WARPS / 2);
         }
         mbar_init(sm.drain, 1);
+        mbar_init(sm.b_turn, 1);
+        mbar_init(sm.b_turn + 8, 1);
+        sm.b_next[0] = sm.b_next[1] = 0;
         *abort_flag = 0;
         mbar_fence_init();
         tma_prefetch_desc(&p.tW1);
@@ -1130,8 +1210,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
         if (elect_one()) few_load_w(p, sm, L, abort_flag);
     } else if (warp == FEW_WARP_MMA) {
         if (elect_one()) few_mma(p, sm, L, tmem, abort_flag);
-    } else if (warp == FEW_WARP_B) {
-        if (elect_one()) few_load_b(p, sm, L, abort_flag);
+    } else {
+        if (elect_one()) few_load_b(p, sm, L, warp - FEW_WARP_B, abort_flag);
     }
     __syncwarp();
     tc_fence_before();
@@ -1228,7 +1308,8 @@ cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaS
 
     bool ok = make_weight_tmap_strided(&a.tW1, a.W1, a.h, a.d, a.E, a.hp, (int64_t)a.d * a.hp) &&
               make_weight_tmap_strided(&a.tW2, a.W2, a.d, a.h, a.E, a.d, (int64_t)a.h * a.d) &&
-              make_gather_tmap(&a.tX, a.x, a.d, a.T, a.d) &&
+              (a.T <= 16 ? make_kmajor_tmap(&a.tX, a.x, a.d, a.T, 1, a.d, (int64_t)a.T * a.d, 16)
+                         : make_gather_tmap(&a.tX, a.x, a.d, a.T, a.d)) &&
               make_kmajor_tmap(&a.tH, a.H, a.h, n, 2, a.ldh, (int64_t)n * a.ldh, 16);
     if (ok && a.W3) ok = make_weight_tmap_strided(&a.tW3, a.W3, a.h, a.d, a.E, a.hp, (int64_t)a.d * a.hp);
     if (ok && a.hs > 0) {

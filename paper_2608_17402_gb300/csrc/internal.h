@@ -365,7 +365,7 @@ struct FewArgs {
     __nv_bfloat16* y;
 
     CUtensorMap tW1, tW3, tW2, tS1, tS3, tS2;   // weights, 3-D {N, K, E}, boxes 64 x 64
-    CUtensorMap tX;                             // token rows, one-row boxes (gather)
+    CUtensorMap tX;                             // token rows: boxes 64 x 16, or one-row boxes (gather)
     CUtensorMap tH, tHs;                        // hidden rows, 3-D {h, rows, 2}, boxes 64 x 16
     // router: partial logits [rt_parts][T][E], sums of squares [rt_parts][E] (W_r), [rt_parts][T] (x)
     float *part, *wsq, *xsq;
