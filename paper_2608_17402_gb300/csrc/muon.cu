@@ -777,7 +777,8 @@ __device__ __forceinline__ void ns_epi_sync() { asm volatile("bar.sync 1, 256;" 
 // that each holds only the code that its tiles run.
 template <int MODE>
 __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, const NsTile& t, uint8_t* slot, int row,
-                                         int half, int rank, int c0, const uint32_t (&v)[32], const float4 (&wv)[8]) {
+                                         int half, int rank, int c0, bool live, const uint32_t (&v)[32],
+                                         const float4 (&wv)[8]) {
     constexpr bool APPLY = MODE >= NS_M_X;
     const float cc = p.coef[3 * it.step + 2], cb = p.coef[3 * it.step + 1];
     const float fd = MODE == NS_M_GRAM ? (cc == 0.f ? cb * NS_INV_S : NS_INV_S) : MODE == NS_M_POLY ? cc * NS_INV_S : NS_INV_S;
@@ -785,6 +786,15 @@ __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, cons
     const bool lo_in = APPLY ? fl != 0.f : p.terms == 3;
     const bool lo_out = MODE == NS_M_X ? p.lo_coef[it.step + 1] != 0.f : p.terms == 3;
     float keep[MODE == NS_M_W ? 32 : 1];
+    uint4 hin[4], lin[4];   // all inputs before the first output (in place: no load passes a store)
+    if (MODE != NS_M_GRAM) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) hin[g] = *reinterpret_cast<const uint4*>(ns_cell(slot, row, half * 4 + g));
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            lin[g] = lo_in ? *reinterpret_cast<const uint4*>(ns_cell(slot + NS_REGION, row, half * 4 + g))
+                           : make_uint4(0u, 0u, 0u, 0u);
+    }
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         const int c = half * 4 + g;
@@ -795,14 +805,12 @@ __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, cons
         for (int j = 0; j < 8; ++j) x[j] = fd * __uint_as_float(v[8 * g + j]);
         if (MODE != NS_M_GRAM) {
             float h[8];
-            unpack_half8(*ch, h);
+            unpack_half8(hin[g], h);
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = fmaf(fh, h[j], x[j]);
-            if (lo_in) {
-                unpack_half8(*cl, h);
+            unpack_half8(lin[g], h);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = fmaf(fl, h[j], x[j]);
-            }
+            for (int j = 0; j < 8; ++j) x[j] = fmaf(fl, h[j], x[j]);
         }
         if (MODE == NS_M_W) {
 #pragma unroll
@@ -839,7 +847,7 @@ __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, cons
         const float rate = p.rate * NS_INV_S;
         const int q = threadIdx.x & 15, col = t.n0 + c0 + 4 * q, nc = p.c - col;
         const int64_t base = it.e * p.st_w + col;
-        if (4 * q < t.bn - c0 && nc > 0) {
+        if (live && 4 * q < t.bn - c0 && nc > 0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int r = (int)(threadIdx.x >> 4) + 16 * i, gr = t.m0 + rank * NS_HALF + r;
@@ -871,7 +879,7 @@ __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, cons
         if (!p.vec_o) {   // rows off 16-byte bounds: no TMA store; columns in turn over the threads
             ns_epi_sync();
             const int q = threadIdx.x & 63, col = t.n0 + c0 + q;
-            if (q < t.bn - c0 && col < p.c)
+            if (live && q < t.bn - c0 && col < p.c)
                 for (int r = threadIdx.x >> 6; r < NS_HALF; r += 4) {
                     const int gr = t.m0 + rank * NS_HALF + r;
                     if (gr >= p.r) break;
@@ -885,26 +893,25 @@ __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, cons
 // Eight warps: warp w reads TMEM lanes 32 (w % 4) .. and half w / 4 of each 64-column block.  A
 // thread's values are consecutive in its row, as they are in the blocks' swizzled rows, so what
 // the tile reads and writes in fp16 goes through shared memory in place, 16 bytes at a time, and
-// between there and L2 by TMA.  One thread waits for the accumulator and decides for all, as
-// some modes meet at barriers within a block.
-__device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, volatile int* abort_flag,
-                            volatile int* go) {
+// between there and L2 by TMA.  The warps go through the blocks each at its own pace (in step, by a
+// barrier per block, they all waited for each other's latencies).  A wait that gives up is recorded
+// and the warp goes on without writing results: some modes meet at barriers within a block, which
+// every warp must reach.
+__device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, volatile int* abort_flag) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
     int n = 0, s = 0;
     uint32_t ph = 0;
+    bool live = true;
     NsWalk w = ns_walk_start(p);
     for (int id = sm.pair; id < p.total; id += sm.npairs, ++n) {
         const NsItem it = ns_item(p, w, id);
         const NsTile t = ns_tile(p, it);
         const int mode = ns_mode(p, it), acc = n & 1;
-        if (threadIdx.x == 0) {
-            const bool ok = mbar_wait(sm.tfull + 8 * acc, (uint32_t)(n >> 1) & 1u, p.limit_ns, abort_flag);
-            if (!ok) ns_abort(abort_flag, p.status, SITE_NS_WAIT_TFULL, id);
-            go[acc] = ok;
+        if (!mbar_wait(sm.tfull + 8 * acc, (uint32_t)(n >> 1) & 1u, p.limit_ns, abort_flag)) {
+            ns_abort(abort_flag, p.status, SITE_NS_WAIT_TFULL, id);
+            live = false;
         }
-        ns_epi_sync();
-        if (!go[acc]) return;
         tc_fence_after();
         const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * NS_MAXBN;
         const uint32_t tempty = peer_addr(sm.tempty, 0) + 8 * acc;
@@ -924,24 +931,21 @@ __device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, vo
                         wv[i] = *reinterpret_cast<const float4*>(p.W + it.e * p.st_w + gr * p.ld_w + col);
                 }
             }
-            if (threadIdx.x == 0) {
-                const bool ok = mbar_wait(sm.in + 8 * s, ph, p.limit_ns, abort_flag);
-                if (!ok) ns_abort(abort_flag, p.status, SITE_NS_WAIT_SLOT, id);
-                go[2 + s] = ok;
+            if (!mbar_wait(sm.in + 8 * s, ph, p.limit_ns, abort_flag)) {
+                ns_abort(abort_flag, p.status, SITE_NS_WAIT_SLOT, id);
+                live = false;
             }
-            ns_epi_sync();
             tmem_wait_ld();
             if (c0 + 64 >= t.bn) {   // this warp's last read of the accumulator
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_remote(tempty);
             }
-            if (!go[2 + s]) return;
-            if (mode == NS_M_GRAM) ns_block<NS_M_GRAM>(p, it, t, slot, row, half, (int)sm.rank, c0, v, wv);
-            else if (mode == NS_M_POLY) ns_block<NS_M_POLY>(p, it, t, slot, row, half, (int)sm.rank, c0, v, wv);
-            else if (mode == NS_M_X) ns_block<NS_M_X>(p, it, t, slot, row, half, (int)sm.rank, c0, v, wv);
-            else if (mode == NS_M_O) ns_block<NS_M_O>(p, it, t, slot, row, half, (int)sm.rank, c0, v, wv);
-            else ns_block<NS_M_W>(p, it, t, slot, row, half, (int)sm.rank, c0, v, wv);
+            if (mode == NS_M_GRAM) ns_block<NS_M_GRAM>(p, it, t, slot, row, half, (int)sm.rank, c0, live, v, wv);
+            else if (mode == NS_M_POLY) ns_block<NS_M_POLY>(p, it, t, slot, row, half, (int)sm.rank, c0, live, v, wv);
+            else if (mode == NS_M_X) ns_block<NS_M_X>(p, it, t, slot, row, half, (int)sm.rank, c0, live, v, wv);
+            else if (mode == NS_M_O) ns_block<NS_M_O>(p, it, t, slot, row, half, (int)sm.rank, c0, live, v, wv);
+            else ns_block<NS_M_W>(p, it, t, slot, row, half, (int)sm.rank, c0, live, v, wv);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(sm.done + 8 * s);
@@ -961,7 +965,6 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     uint64_t* bars = reinterpret_cast<uint64_t*>(after + NS_SLOTS * NS_SLOT_BYTES);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + NS_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    __shared__ int go[2 + NS_SLOTS];
     NsSmem sm;
     sm.ring = smem_u32(smem);
     sm.slot_ptr = after;
@@ -1007,7 +1010,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     pdl_wait();
     const uint32_t tmem = *tmem_slot;
     if (warp < NS_EPI_WARPS) {
-        ns_epilogue(p, sm, tmem, abort_flag, go);
+        ns_epilogue(p, sm, tmem, abort_flag);
     } else if (warp == NS_WARP_LOAD) {
         if (elect_one()) ns_producer(p, sm, abort_flag);
     } else if (warp == NS_WARP_MMA) {
