@@ -447,6 +447,7 @@ __device__ __forceinline__ int ns_dst(int s) { return 1 + (s & 1); }
 
 struct NsTile {
     int m0, n0, bn, num_kb;            // num_kb: K blocks of one term
+    int mma_n;                         // columns that are computed
     bool mirror;                       // symmetric output: also write its mirror image
     bool same;                         // A's and B's shares of each CTA are the same box: loaded once
     const CUtensorMap *a[2], *b[2];    // operands, hi and lo
@@ -497,8 +498,10 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
         for (int j = 0; j < 2; ++j) t.a[j] = t.b[j] = gram ? &p.tX[src][j] : &p.tA[j];
     }
     t.bn = min(p.bn, (cols - t.n0 + 31) & ~31);   // a multiple of 32: each CTA holds half of B
-    // a 256-wide tile on the diagonal: rows and columns of a CTA coincide
-    if (it.kind != NS_APPLY) t.same = t.n0 == t.m0 && t.bn == NS_BM && p.terms == 1;
+    // A tile on the diagonal: rows and columns of a CTA coincide.  One that the matrix's end trims is
+    // computed 256 wide all the same (the products are bound by L2, not by the tensor cores).
+    if (it.kind != NS_APPLY) t.same = t.n0 == t.m0 && p.bn == NS_BM && p.terms == 1;
+    t.mma_n = t.same ? NS_BM : t.bn;
     t.num_kb = (k + NS_BK - 1) / NS_BK;
     return t;
 }
@@ -590,7 +593,7 @@ __device__ __forceinline__ void ns_mma(const NsArgs& p, const NsSmem& sm, uint32
     for (int id = sm.pair; id < p.total; id += sm.npairs) {
         const NsItem it = ns_item(p, w, id);
         const NsTile t = ns_tile(p, it);
-        const uint32_t idesc = idesc_f16_f32(NS_BM, t.bn, t.a_mn, t.b_mn);
+        const uint32_t idesc = idesc_f16_f32(NS_BM, t.mma_n, t.a_mn, t.b_mn);
         const uint64_t ad0 = smem_desc_sw128(sm.ring, t.a_mn ? NS_BOX : 16, 1024);
         const uint64_t bd0 = smem_desc_sw128(sm.ring + (t.same ? 0 : 2 * NS_BOX), t.b_mn ? NS_BOX : 16, 1024);
         const uint32_t as = (t.a_mn ? 2048 : 32) >> 4, bs = (t.b_mn ? 2048 : 32) >> 4;
