@@ -318,9 +318,11 @@ constexpr int NS_BM = 256;            // output rows per tile: a CTA pair, 128 r
 constexpr int NS_HALF = 128;
 constexpr int NS_MAXBN = 256;         // output columns per tile at most (one tcgen05.mma)
 constexpr int NS_BK = 64;             // K per ring stage: one 128-byte swizzle row of fp16
-constexpr int NS_STAGES = 4;
 constexpr int NS_BOX = 64 * NS_BK * 2;                     // bytes of one 64 x 64 TMA box
-constexpr int NS_STAGE_BYTES = (NS_HALF + NS_MAXBN / 2) / 64 * NS_BOX;   // a CTA's A rows and half of B
+// The ring: a stage holds a CTA's A rows and its half of B, three boxes or (256-wide tiles) four; five
+// or four stages (five instead of four for the narrow tiles of few matrices: 1024 x 1024 135 -> 134 us).
+constexpr int NS_RING_BYTES = 16 * NS_BOX;
+constexpr int NS_RING_MAX = 5;        // stages at most
 constexpr int NS_EPI_WARPS = 8;       // two per TMEM lane quadrant: 32 of a block's 64 columns each
 constexpr int NS_WARP_LOAD = NS_EPI_WARPS;        // operand loads
 constexpr int NS_WARP_MMA = NS_EPI_WARPS + 1;
@@ -332,8 +334,8 @@ constexpr int NS_THREADS = (NS_EPI_WARPS + 4) * 32;
 constexpr int NS_REGION = 2 * NS_BOX;
 constexpr int NS_SLOTS = 3;
 constexpr int NS_SLOT_BYTES = 2 * NS_REGION;
-constexpr int NS_BARS = 2 * NS_STAGES + 5 + 3 * NS_SLOTS;
-constexpr int NS_SMEM = NS_STAGES * NS_STAGE_BYTES + NS_SLOTS * NS_SLOT_BYTES + 1024 + 256;
+constexpr int NS_BARS = 2 * NS_RING_MAX + 5 + 3 * NS_SLOTS;
+constexpr int NS_SMEM = NS_RING_BYTES + NS_SLOTS * NS_SLOT_BYTES + 1024 + 256;
 static_assert(NS_SMEM <= 232448 && NS_BARS * 8 + 8 <= 256, "shared memory of one CTA");
 
 constexpr int NS_LANES = 3;           // groups of matrices under way, a stage apart
@@ -514,6 +516,7 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn_maj
 struct NsSmem {
     uint32_t ring, slots;
     uint32_t full, empty, tfull, tempty, drain;
+    int stages, stage_bytes;    // of the ring
     uint32_t in, done, free_;   // per epilogue slot: inputs landed; results written; stores have read it
     uint8_t* slot_ptr;
     uint32_t rank;
@@ -565,7 +568,7 @@ __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abo
                     ns_abort(abort_flag, p.status, SITE_NS_WAIT_EMPTY, id);
                     return;
                 }
-                const uint32_t bar = full_leader + 8 * s, dst = sm.ring + s * NS_STAGE_BYTES;
+                const uint32_t bar = full_leader + 8 * s, dst = sm.ring + s * sm.stage_bytes;
                 if (sm.rank == 0) mbar_arrive_expect_tx(sm.full + 8 * s, bytes);
                 const int kk = kb * NS_BK;
 #pragma unroll
@@ -575,7 +578,7 @@ __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abo
                 for (int j = 0; j < nbox; ++j)
                     tma_load_3d_pair(dst + (2 + j) * NS_BOX, mb, bar, t.b_mn ? nn + 64 * j : kk,
                                      t.b_mn ? kk : nn + 64 * j, t.zb);
-                if (++s == NS_STAGES) {
+                if (++s == sm.stages) {
                     s = 0;
                     ph ^= 1u;
                 }
@@ -613,14 +616,14 @@ __device__ __forceinline__ void ns_mma(const NsArgs& p, const NsSmem& sm, uint32
                 ok = false;
                 break;
             }
-            const uint64_t ad = ad0 + (uint64_t)((s * NS_STAGE_BYTES) >> 4);
-            const uint64_t bd = bd0 + (uint64_t)((s * NS_STAGE_BYTES) >> 4);
+            const uint64_t ad = ad0 + (uint64_t)((s * sm.stage_bytes) >> 4);
+            const uint64_t bd = bd0 + (uint64_t)((s * sm.stage_bytes) >> 4);
 #pragma unroll
             for (int q = 0; q < NS_BK / 16; ++q)
                 tc_mma_bf16_pair(d, ad + q * as, bd + q * bs, idesc, (kb | q) != 0 ? 1u : 0u);
             issued = true;
             tc_commit_pair(sm.empty + 8 * s);
-            if (++s == NS_STAGES) {
+            if (++s == sm.stages) {
                 s = 0;
                 ph ^= 1u;
             }
@@ -964,7 +967,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     extern __shared__ uint8_t ns_smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ns_smem_raw) + 1023) &
                                                ~static_cast<uintptr_t>(1023));
-    uint8_t* after = smem + NS_STAGES * NS_STAGE_BYTES;
+    uint8_t* after = smem + NS_RING_BYTES;
     uint64_t* bars = reinterpret_cast<uint64_t*>(after + NS_SLOTS * NS_SLOT_BYTES);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + NS_BARS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -973,19 +976,21 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     sm.slot_ptr = after;
     sm.slots = smem_u32(after);
     sm.full = smem_u32(bars);
-    sm.empty = sm.full + 8 * NS_STAGES;
-    sm.tfull = sm.empty + 8 * NS_STAGES;
+    sm.empty = sm.full + 8 * NS_RING_MAX;
+    sm.tfull = sm.empty + 8 * NS_RING_MAX;
     sm.tempty = sm.tfull + 16;
     sm.drain = sm.tempty + 16;
     sm.in = sm.drain + 8;
     sm.done = sm.in + 8 * NS_SLOTS;
     sm.free_ = sm.done + 8 * NS_SLOTS;
+    sm.stage_bytes = (p.bn == NS_MAXBN ? 4 : 3) * NS_BOX;
+    sm.stages = p.bn == NS_MAXBN ? 4 : NS_RING_MAX;
     sm.rank = cluster_rank();
     sm.pair = blockIdx.x >> 1;
     sm.npairs = gridDim.x >> 1;
     const int warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < NS_STAGES; ++s) {
+        for (int s = 0; s < sm.stages; ++s) {
             mbar_init(sm.full + 8 * s, 1);
             mbar_init(sm.empty + 8 * s, 1);
         }
