@@ -202,3 +202,14 @@ def test_few_refusals():
     n0 = moevie.moevie_launch_count()
     assert moevie.moevie_moe_few(W, x[:0], ws).shape == (0, 64)
     assert moevie.moevie_launch_count() == n0
+
+
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("T,d,E,k,h,hs", [
+    (16, 200, 6, 3, 72, 40), (17, 200, 6, 3, 72, 40), (1, 328, 9, 9, 328, 328), (64, 1000, 90, 6, 520, 264),
+    (60, 72, 33, 32, 130, 0), (31, 1032, 5, 2, 65, 129), (2, 2048, 300, 1, 8, 8)])
+def test_few_odd_blocks(T, d, E, k, h, hs, act):
+    """Odd numbers of K blocks, token counts around the one-copy bound of 16, wide and narrow
+    tiles of both activations, entries of more than 32 tokens."""
+    cfg = workloads.small_config(T=T, d=d, E=E, k=k, h=h, h_s=hs, lam=1.5, seed=T * 17 + d, act=act)
+    _check(workloads.make_layer(cfg))
