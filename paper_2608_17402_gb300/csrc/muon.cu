@@ -16,15 +16,15 @@
 //   ns_thin_kernel      all of that for matrices whose smaller side is at most 32, in fp32.
 //
 // ns_kernel.  Work items are (matrix, stage, tile): a Gram, a polynomial and an apply stage for
-// each step.  Only a few matrices are under way at a time, in buffers that are
-// used again for the next ones, so that everything between X0 and the result stays in L2 (with all matrices under way at once the apply stage alone
-// moved 1.4 GB a step and took 755 us of a 1000 us step on 256 x 416 x 1664).  The matrices under
-// way form NS_LANES groups that are one stage apart; in each slot of the schedule every group
-// advances by a stage, so that a tile's inputs were finished about a slot of other tiles earlier
-// and its pair rarely waits.  A counter per matrix holds the finished tiles of its stages, which
-// follow one another; an item waits for the count of all earlier stages.  Items are dealt to the
-// pairs round-robin in schedule order and depend on earlier slots only; all pairs are co-resident
-// (cooperative launch).
+// each step.  Only some of the matrices are under way at a time, in buffers that are used again
+// for the next ones, so that most of what lies between X0 and the result is still in L2 when it is
+// read (all matrices under way at once: the apply stage alone moved 1.4 GB a step, 755 us of a
+// 1000 us step on 256 x 416 x 1664).  The matrices under way form NS_LANES groups that are one stage
+// apart; in each slot of the schedule every group advances by a stage, so that a tile's inputs were
+// finished about a slot of other tiles earlier and its pair rarely waits.  A counter per matrix
+// holds the finished tiles of its stages, which follow one another; an item waits for the count of
+// all earlier stages.  Items are dealt to the pairs round-robin in schedule order and depend on
+// earlier slots only; all pairs are co-resident (cooperative launch).
 //
 // Working format.  X is held as hi + lo, two fp16 values (22 significant bits), times 2^10; A and B
 // as fp16 times 2^10.  The tensor cores multiply the hi parts (fp16 has three bits more than bf16
@@ -40,6 +40,15 @@
 // saves the last step's lo.
 // For m <= 128 the roundings of a few singular values average less, and time is latency: there
 // A and B have lo parts too and every product is hi hi + hi lo + lo hi (about 1e-5).
+//
+// What bounds it, measured on one GB300 (five steps; floors are the products of one term, symmetric
+// ones counted half, at the measured 1894 TFLOP/s): 256 x 416 x 1664 2.39 ms (floor 0.63), 16 x 768 x 768
+// 0.24 ms (0.077), a step on 64 x 1024 x 512 0.56 ms (0.16).  Traffic between L2 and the SMs comes
+// first (16 MB per matrix and step of 416 x 1664, 8.6 TB/s in all), not the tensor cores (26 to 32%) or
+// HBM: in a copy without the epilogue's arithmetic the first case took 2.30 ms, without its loads
+// 2.20, without the stores 2.01, without all three 1.79; prefetches into L2 ahead of the loads cost 3 to
+// 20%.  One 1024 x 1024 matrix (134 us) is a chain of 15 dependent stages of 9 us: hand-over between
+// CTAs 3 us, 16 K blocks 5 us.
 #include "internal.h"
 
 #include <cuda_fp16.h>
@@ -284,6 +293,8 @@ __global__ void __launch_bounds__(NS_PRO_THREADS) muon_scale_kernel(const __grid
 // distributed shared memory (added in CTA order), and the second read of a CTA's eighth of the
 // matrix comes from L2, where the first has just brought it: one CTA of 1024 threads per SM, so
 // that what all of them are at (256 x 416 x 1664: 53 MB) stays there.
+// Memory bound: 256 x 416 x 1664 with momentum 610 us, 4.65 TB/s (two launches over all SMs take the
+// same there, but 587 us instead of 562 for a whole step on 64 x 1024 x 512).
 constexpr int NS_PRO_CLUSTER = 8, NS_PRO_CTHREADS = 1024;
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(NS_PRO_CTHREADS, 1) muon_update_kernel(const __grid_constant__ UpdateArgs p, __half* xh,
@@ -358,6 +369,7 @@ struct NsArgs {
     int n_stages, n_groups, group_max; // stages of a matrix; groups of matrices; their largest size
     int base_size, big_groups;         // the first big_groups of them hold base_size + 1, the others base_size
     int total;                         // items
+    int thin_cluster;                  // CTAs per thin matrix
     uint8_t kind[NS_MAX_STAGES], step[NS_MAX_STAGES];
     int need[NS_MAX_STAGES + 1];       // counter value at which a stage's inputs are complete
     float coef[3 * NS_MAX_STEPS], lo_coef[NS_MAX_STEPS];   // lo_coef: multiplier of lo in a X
@@ -1040,113 +1052,186 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
 
 // ------------------------------------------------------------- thin matrices
 
-// m <= NS_THIN: one CTA per matrix, fp32 throughout.  All factors of the step polynomials are
-// polynomials of A = X0 X0^T and commute, so the iteration runs on m x m matrices in shared
-// memory (P = a I + b A + c A^2, Q <- P Q, A <- P A P) and X is read twice: for A and for
+// m <= NS_THIN: fp32 throughout.  All factors of the step polynomials are polynomials of
+// A = X0 X0^T and commute, so the iteration runs on symmetric 32 x 32 matrices in shared memory
+// (P = a I + b A + c A^2, Q <- P Q, A <- P A P; zeros past m) and X is read twice: for A and for
 // Q X0.  Thin matrices are kept off the tensor cores for accuracy as much as for time: with few
 // singular values the fp16 roundings do not average out over the entries (a 1 x n matrix is one
 // number per step, and its result was 5e-3 off), and their tiles would be mostly empty.
+//
+// A cluster of up to 8 CTAs per matrix, each with every so many 128 columns of the long side; the
+// parts of A are added in CTA order over distributed shared memory, and every CTA iterates for
+// itself.  Bound by latency (loads of a chunk 3 us, the iteration 8 us): 32 x 2048 27 us, a stack of 256
+// of them 155 us (with one CTA a matrix and scalar products 335 and 504).
 constexpr int NS_THIN = 32;
 constexpr int NS_THIN_THREADS = 256;
-constexpr int NS_THIN_K = 64;
+constexpr int NS_THIN_K = 128;
+constexpr int NS_THIN_LD = NS_THIN + 4;
+constexpr int NS_THIN_CLUSTER = 8;
 
-__device__ __forceinline__ void ns_out1(const NsArgs& p, int e, int row, int col, float v) {
-    if (p.O) {
-        p.O[e * p.st_o + row * p.ld_o + col] = __float2bfloat16_rn(v);
-    } else {
-        const int64_t at = e * p.st_w + row * p.ld_w + col;
-        const float w = fmaf(-p.rate, v, p.decay * p.W[at]);
-        p.W[at] = w;
-        if (p.Wb) p.Wb[at] = __float2bfloat16_rn(w);
-    }
-}
-
-__global__ void __launch_bounds__(NS_THIN_THREADS) ns_thin_kernel(const __grid_constant__ NsArgs p) {
+__global__ void __launch_bounds__(NS_THIN_THREADS, 3) ns_thin_kernel(const __grid_constant__ NsArgs p) {
     pdl_wait();
-    __shared__ float A[NS_THIN][NS_THIN + 1], P[NS_THIN][NS_THIN + 1], Q[NS_THIN][NS_THIN + 1],
-        T[NS_THIN][NS_THIN + 1], xs[NS_THIN][NS_THIN_K + 1];
-    const int e = blockIdx.x, m = p.m, n = p.tall ? p.r : p.c, tid = threadIdx.x;
-    constexpr int PER = NS_THIN * NS_THIN / NS_THIN_THREADS;
+    typedef float Square[NS_THIN][NS_THIN_LD];
+    __shared__ __align__(16) Square sq[4];
+    __shared__ __align__(16) float xs[NS_THIN][NS_THIN_K + 4];
+    const int tid = threadIdx.x, m = p.m, n = p.tall ? p.r : p.c;
+    const int C = p.thin_cluster, e = blockIdx.x / C, rank = blockIdx.x % C;
+    const int chunks = (n + NS_THIN_K - 1) / NS_THIN_K;
     float pre, post;
     norm_scales(p.u, e, pre, post);
-    auto stage = [&](int k0) {   // xs[i][kk] = X0 (i, k0 + kk) of the m x n orientation
-        for (int q = tid; q < m * NS_THIN_K; q += NS_THIN_THREADS) {
-            const int i = p.tall ? q % m : q / NS_THIN_K, kk = p.tall ? q / m : q % NS_THIN_K;
-            float v = 0.f;
-            if (k0 + kk < n) {
-                const int64_t at = e * p.u.st_u + (p.tall ? (int64_t)(k0 + kk) * p.u.ld_u + i : i * p.u.ld_u + k0 + kk);
-                if (p.u.M && !p.u.nesterov) {
-                    v = p.u.M[at];
-                } else {
-                    v = p.u.u_bf16 ? as_f32(static_cast<const __nv_bfloat16*>(p.u.U)[at])
-                                   : static_cast<const float*>(p.u.U)[at];
-                    if (p.u.M) v = fmaf(p.u.mu, p.u.M[at], v);
-                }
-                v = (v * pre) * post;
-            }
-            xs[i][kk] = v;
-        }
-    };
-    // out = L R, every operand m x m in shared memory, `out` none of them
-    auto product = [&](float (*out)[NS_THIN + 1], const float (*L)[NS_THIN + 1], const float (*R)[NS_THIN + 1]) {
-        for (int q = tid; q < m * m; q += NS_THIN_THREADS) {
-            const int i = q / m, j = q - i * m;
-            float s = 0.f;
-            for (int k = 0; k < m; ++k) s = fmaf(L[i][k], R[k][j], s);
-            out[i][j] = s;
-        }
-        __syncthreads();
-    };
-    float acc[PER] = {};
-    for (int k0 = 0; k0 < n; k0 += NS_THIN_K) {
-        stage(k0);
-        __syncthreads();
+    // A thread's 16 elements of a chunk, in memory order over the threads: (i0 + di u, k0 + kk0 + dk u)
+    constexpr int PER = NS_THIN * NS_THIN_K / NS_THIN_THREADS;
+    const int i0 = p.tall ? tid & 31 : tid / NS_THIN_K, di = p.tall ? 0 : NS_THIN_THREADS / NS_THIN_K;
+    const int kk0 = p.tall ? tid >> 5 : tid & (NS_THIN_K - 1), dk = p.tall ? NS_THIN_THREADS / 32 : 0;
+    auto inside = [&](int k0, int u) { return i0 + di * u < m && k0 + kk0 + dk * u < n; };
+    auto load = [&](int k0, auto get) {
+        const int64_t at = e * p.u.st_u + (p.tall ? (k0 + kk0) * p.u.ld_u + i0 : i0 * p.u.ld_u + k0 + kk0);
+        const int64_t d = (p.tall ? dk : di) * p.u.ld_u;
+        float v[PER];
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int q = tid + u * NS_THIN_THREADS, i = q / m, j = q - i * m;
-            if (q < m * m) {
-                float s = acc[u];
-                for (int kk = 0; kk < NS_THIN_K; ++kk) s = fmaf(xs[i][kk], xs[j][kk], s);
-                acc[u] = s;
+        for (int u = 0; u < PER; ++u) v[u] = inside(k0, u) ? get(at + u * d) : 0.f;
+#pragma unroll
+        for (int u = 0; u < PER; ++u) xs[i0 + di * u][kk0 + dk * u] = (v[u] * pre) * post;
+    };
+    auto stage = [&](int k0) {   // xs[i][kk] = X0 (i, k0 + kk) of the m x n orientation
+        const float* M = p.u.M;
+        const float* U = static_cast<const float*>(p.u.U);
+        const __nv_bfloat16* B = static_cast<const __nv_bfloat16*>(p.u.U);
+        const float mu = p.u.mu;
+        if (M && !p.u.nesterov) load(k0, [=](int64_t a) { return M[a]; });
+        else if (M) load(k0, [=](int64_t a) { return fmaf(mu, M[a], U[a]); });   // (with a momentum, U is fp32)
+        else if (p.u.u_bf16) load(k0, [=](int64_t a) { return as_f32(B[a]); });
+        else load(k0, [=](int64_t a) { return U[a]; });
+        __syncthreads();
+    };
+    // A: four groups of 64 threads share a chunk's columns, a thread has rows ti + 8 u, columns tj + 8 v
+    {
+        const int g = tid >> 6, ti = tid >> 3 & 7, tj = tid & 7;
+        float acc[4][4] = {};
+        for (int ch = rank; ch < chunks; ch += C) {
+            stage(ch * NS_THIN_K);
+#pragma unroll 2
+            for (int q = 0; q < NS_THIN_K / 16; ++q) {
+                const int kk = (g * (NS_THIN_K / 16) + q) * 4;
+                float4 a[4], b[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    a[u] = *reinterpret_cast<const float4*>(&xs[ti + 8 * u][kk]);
+                    b[u] = *reinterpret_cast<const float4*>(&xs[tj + 8 * u][kk]);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        acc[u][v] = fmaf(a[u].w, b[v].w, fmaf(a[u].z, b[v].z, fmaf(a[u].y, b[v].y, fmaf(a[u].x, b[v].x, acc[u][v]))));
             }
+            if (chunks > C) __syncthreads();   // (one chunk a CTA: it stays for the end)
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sq[g][ti + 8 * u][tj + 8 * v] = acc[u][v];
         __syncthreads();
     }
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-        const int q = tid + u * NS_THIN_THREADS;
-        if (q < m * m) A[q / m][q % m] = acc[u];
+    // a thread's four elements of a square: row tid / 8, columns 4 (tid % 8) ..
+    const int er = tid >> 3, ec = (tid & 7) * 4;
+    auto at4 = [&](Square& S) { return reinterpret_cast<float4*>(&S[er][ec]); };
+    float4 sum = *at4(sq[0]);
+    for (int g = 1; g < 4; ++g) {
+        const float4 v = *at4(sq[g]);
+        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+    }
+    *at4(sq[0]) = sum;   // (read by this thread alone so far)
+    if (C > 1) {
+        const uint32_t mine = smem_u32(at4(sq[0]));
+        cluster_sync();
+        sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int r = 0; r < C; ++r) {
+            float4 v;
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                         : "r"(peer_addr(mine, r)));
+            sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+        }
+        cluster_sync();   // every CTA has read the parts
+        *at4(sq[0]) = sum;
     }
     __syncthreads();
+    // out = L R for symmetric operands, `out` none of them; 2 x 2 elements a thread
+    auto product = [&](Square& out, const Square& L, const Square& R) {
+        const int i = (tid >> 4) * 2, j = (tid & 15) * 2;
+        float2 r0 = make_float2(0.f, 0.f), r1 = r0;
+#pragma unroll 8
+        for (int k = 0; k < NS_THIN; ++k) {
+            const float2 l = *reinterpret_cast<const float2*>(&L[k][i]), r = *reinterpret_cast<const float2*>(&R[k][j]);
+            r0 = make_float2(fmaf(l.x, r.x, r0.x), fmaf(l.x, r.y, r0.y));
+            r1 = make_float2(fmaf(l.y, r.x, r1.x), fmaf(l.y, r.y, r1.y));
+        }
+        *reinterpret_cast<float2*>(&out[i][j]) = r0;
+        *reinterpret_cast<float2*>(&out[i + 1][j]) = r1;
+        __syncthreads();
+    };
+    Square& A = sq[0];
+    Square& P = sq[1];
+    int iq = 2, it2 = 3;   // where Q and the scratch matrix are
     for (int it = 0; it < p.steps; ++it) {
         const float ca = p.coef[3 * it], cb = p.coef[3 * it + 1], cc = p.coef[3 * it + 2];
-        product(T, A, A);
-        for (int q = tid; q < m * m; q += NS_THIN_THREADS) {
-            const int i = q / m, j = q - i * m;
-            P[i][j] = fmaf(cc, T[i][j], cb * A[i][j]) + (i == j ? ca : 0.f);
-            if (it == 0) Q[i][j] = P[i][j];
-        }
+        product(sq[it2], A, A);
+        const float4 a = *at4(A), t = *at4(sq[it2]);
+        float4 v = make_float4(fmaf(cc, t.x, cb * a.x), fmaf(cc, t.y, cb * a.y), fmaf(cc, t.z, cb * a.z), fmaf(cc, t.w, cb * a.w));
+        v.x += er == ec ? ca : 0.f;
+        v.y += er == ec + 1 ? ca : 0.f;
+        v.z += er == ec + 2 ? ca : 0.f;
+        v.w += er == ec + 3 ? ca : 0.f;
+        *at4(P) = v;
+        if (it == 0) *at4(sq[iq]) = v;
         __syncthreads();
         if (it > 0) {
-            product(T, P, Q);
-            for (int q = tid; q < m * m; q += NS_THIN_THREADS) Q[q / m][q % m] = T[q / m][q % m];
-            __syncthreads();
+            product(sq[it2], P, sq[iq]);
+            iq ^= 1;   // 2 and 3 change places
+            it2 ^= 1;
         }
         if (it + 1 < p.steps) {
-            product(T, P, A);
-            product(A, T, P);
+            product(sq[it2], P, A);
+            product(A, sq[it2], P);
         }
     }
-    for (int k0 = 0; k0 < n; k0 += NS_THIN_K) {
-        stage(k0);
+    // Q X0: 4 rows x 4 columns a thread, through xs to memory order
+    const Square& Q = sq[iq];
+    for (int ch = rank; ch < chunks; ch += C) {
+        const int k0 = ch * NS_THIN_K, c4 = (tid & 31) * 4, r4 = (tid >> 5) * 4;
+        if (chunks > C) stage(k0);
+        float4 o[4] = {};
+#pragma unroll 4
+        for (int j = 0; j < m; ++j) {
+            const float4 x = *reinterpret_cast<const float4*>(&xs[j][c4]), q = *reinterpret_cast<const float4*>(&Q[j][r4]);
+            const float qs[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                o[u] = make_float4(fmaf(qs[u], x.x, o[u].x), fmaf(qs[u], x.y, o[u].y), fmaf(qs[u], x.z, o[u].z),
+                                   fmaf(qs[u], x.w, o[u].w));
+        }
         __syncthreads();
-        for (int q = tid; q < m * NS_THIN_K; q += NS_THIN_THREADS) {
-            const int i = p.tall ? q % m : q / NS_THIN_K, kk = p.tall ? q / m : q % NS_THIN_K;
-            if (k0 + kk < n) {
-                float s = 0.f;
-                for (int j = 0; j < m; ++j) s = fmaf(Q[i][j], xs[j][kk], s);
-                ns_out1(p, e, p.tall ? k0 + kk : i, p.tall ? i : k0 + kk, s);
-            }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) *reinterpret_cast<float4*>(&xs[r4 + u][c4]) = o[u];
+        __syncthreads();
+        const int64_t base = (p.O ? e * p.st_o : e * p.st_w), ld = p.O ? p.ld_o : p.ld_w;
+        const int64_t at = base + (p.tall ? (k0 + kk0) * ld + i0 : i0 * ld + k0 + kk0), d = (p.tall ? dk : di) * ld;
+        if (p.O) {
+#pragma unroll
+            for (int u = 0; u < PER; ++u)
+                if (inside(k0, u)) p.O[at + u * d] = __float2bfloat16_rn(xs[i0 + di * u][kk0 + dk * u]);
+        } else {
+            float w[PER];
+#pragma unroll
+            for (int u = 0; u < PER; ++u) w[u] = inside(k0, u) ? p.W[at + u * d] : 0.f;
+#pragma unroll
+            for (int u = 0; u < PER; ++u)
+                if (inside(k0, u)) {
+                    w[u] = fmaf(-p.rate, xs[i0 + di * u][kk0 + dk * u], p.decay * w[u]);
+                    p.W[at + u * d] = w[u];
+                    if (p.Wb) p.Wb[at + u * d] = __float2bfloat16_rn(w[u]);
+                }
         }
         __syncthreads();
     }
@@ -1322,7 +1407,24 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.status = reinterpret_cast<DevStatus*>(ws);
     a.limit_ns = limit_ns;
     if (thin) {
-        e = launch_pdl(ns_thin_kernel, dim3((unsigned)a.N), dim3(NS_THIN_THREADS), 0, s, a);
+        // CTAs of a matrix: one per 128 columns, up to about eight CTAs per SM in all
+        const int n = a.tall ? a.r : a.c, room = 8 * sms / a.N;
+        a.thin_cluster = (n + NS_THIN_K - 1) / NS_THIN_K;
+        if (a.thin_cluster > NS_THIN_CLUSTER) a.thin_cluster = NS_THIN_CLUSTER;
+        if (a.thin_cluster > room) a.thin_cluster = room > 1 ? room : 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(a.N * a.thin_cluster));
+        cfg.blockDim = dim3(NS_THIN_THREADS);
+        cfg.stream = s;
+        cudaLaunchAttribute at[2];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = (unsigned)a.thin_cluster;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see launch_pdl
+        at[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 2;
+        e = cudaLaunchKernelEx(&cfg, ns_thin_kernel, a);
         count_launches(1);
         return e != cudaSuccess ? e : cudaGetLastError();
     }

@@ -218,3 +218,54 @@ def test_empty_stack_is_a_no_op():
     n0 = moevie.moevie_launch_count()
     assert moevie.moevie_orthogonalize(U, ws).shape == (0, 16, 16)
     assert moevie.moevie_launch_count() == n0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,r,c", [(1, 32, 2048), (3, 20, 1500), (2, 2048, 32), (300, 16, 300), (1, 1500, 5),
+                                   (2, 31, 129), (1, 7, 4000), (700, 9, 140), (2, 1, 1030)])
+def test_orthogonalize_thin(N, r, c, dtype):
+    """At most 32 rows or columns against a long side: one CTA, or several that share it."""
+    g = torch.Generator(device="cuda").manual_seed(N + r * 3 + c)
+    U = torch.randn(N, r, c, generator=g, device="cuda").to(dtype)
+    _check(_run(U), U, [COEF] * 5)
+    _check(_run(U, steps=1), U, [COEF])
+
+
+def test_orthogonalize_thin_nonfinite_zero_and_strides():
+    g = torch.Generator(device="cuda").manual_seed(11)
+    U = torch.randn(5, 24, 700, generator=g, device="cuda")
+    U[1, 2, 3] = float("nan")
+    U[2] = 0.0
+    U[3, 23, 699] = float("inf")
+    O = _run(U)
+    _check(O[[0, 4]], U[[0, 4]], [COEF] * 5)
+    assert torch.isnan(O[1]).all() and torch.isnan(O[3]).all() and torch.count_nonzero(O[2]) == 0
+    wide = torch.randn(5, 26, 713, generator=g, device="cuda")
+    out = torch.full((5, 26, 713), 7.0, dtype=torch.bfloat16, device="cuda")
+    O = _run(wide[:, 1:25, 5:705], out=out[:, 1:25, 5:705])
+    _check(O, wide[:, 1:25, 5:705], [COEF] * 5)
+    out[:, 1:25, 5:705] = 7.0
+    assert torch.all(out == 7.0)
+
+
+@pytest.mark.parametrize("N,r,c", [(2, 16, 1200), (3, 700, 30), (400, 8, 72)])
+def test_muon_update_thin(N, r, c):
+    g = torch.Generator(device="cuda").manual_seed(N + r + c)
+
+    def rows(std, dtype=torch.float32):
+        return moevie.moevie_pad_rows((torch.randn(N, r, c, generator=g, device="cuda") * std).to(dtype))
+    W, M, G = rows(r ** -0.5), rows(1e-3), rows(1e-3)
+    Wb = moevie.moevie_pad_rows(W.to(torch.bfloat16))
+    lr, mu, scale = 0.01, 0.9, 0.2 * max(r, c) ** 0.5
+    w, m, gr = _f64(W), _f64(M), _f64(G)
+    ws = moevie.OrthoWorkspace(N, r, c)
+    for nesterov in (True, False):
+        moevie.moevie_muon_update(W, M, G, ws, lr=lr, momentum=mu, nesterov=nesterov, W_bf16=Wb)
+        m = mu * m + gr
+        O = _stack64(gr + mu * m if nesterov else m, [COEF] * 5)
+        w = w - lr * scale * O
+    check_status(ws)
+    assert _rel(_f64(M), m) <= 4 * 2.0 ** -24
+    err = np.linalg.norm(_f64(W) - w)
+    assert err <= 2 * lr * scale * REL * np.linalg.norm(O) + 8 * 2.0 ** -24 * np.linalg.norm(w), err
+    assert torch.equal(Wb, W.to(torch.bfloat16))
