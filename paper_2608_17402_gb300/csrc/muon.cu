@@ -8,9 +8,11 @@
 // U from the momentum on the way in and applies the result to the weights on the way out.
 //
 // Kernels
-//   muon_update_kernel  momentum update (M <- mu M + G), |U|, and X0 in the working format, a
-//                       cluster of CTAs per matrix.  Bound by memory.  For few matrices,
-//   muon_moment_kernel  and muon_scale_kernel do the same in two passes of all SMs.
+//   muon_moment_kernel  momentum update (M <- mu M + G) and |U|.
+//   muon_scale_kernel   X0 in the working format.  Both are bound by memory (with momentum 16 bytes
+//                       an element: 256 x 416 x 1664 in 610 us, 4.65 TB/s); a cluster per matrix that
+//                       did both in one launch, its second read from L2, took the same or longer
+//                       (256 x 416 x 1664 without momentum, all steps: 2.39 ms against 2.35).
 //   ns_kernel           the three products of every step on tcgen05 CTA pairs in one persistent
 //                       launch, with the output or the weight update in the last one's epilogue.
 //   ns_thin_kernel      all of that for matrices whose smaller side is at most 32, in fp32.
@@ -126,7 +128,10 @@ constexpr float NS_UP = 1.2379400392853803e+27f;    // 2^90
 constexpr float NS_TINY = 8.271806125530277e-25f;   // 2^-80
 
 constexpr int NS_PRO_THREADS = 256;
-constexpr int NS_PRO_GROUPS = 4096;   // groups of 8 values per CTA
+// Groups of 8 values per CTA: four a thread (with 16 a thread one 1024 x 1024 matrix took 134 us
+// instead of 125, 64 x 1024 x 512 574 instead of 557), and more where a matrix would have more than 128
+// CTAs, as each reads all their sums.
+constexpr int NS_PRO_GROUPS = 1024, NS_PRO_CHUNKS = 128;
 
 // Where the update U comes from.
 struct UpdateArgs {
@@ -137,7 +142,7 @@ struct UpdateArgs {
     float mu;
     int nesterov;
     int r, c, gpr;        // gpr: groups of 8 per row
-    int groups, chunks;   // groups of 8 per matrix, chunks of NS_PRO_GROUPS of them
+    int groups, chunk, chunks;   // groups of 8 per matrix, per chunk; chunks
     float* part;          // sums of squares [N][chunks][3]
     int32_t* prog;        // progress counters of the matrices, cleared here
 };
@@ -197,8 +202,8 @@ __global__ void __launch_bounds__(NS_PRO_THREADS) muon_moment_kernel(const __gri
     pdl_wait();
     const int e = blockIdx.y;
     if (blockIdx.x == 0 && threadIdx.x == 0) p.prog[e] = 0;
-    const int g0 = blockIdx.x * NS_PRO_GROUPS;
-    const float s = update_squares<T, VEC>(p, e, g0, min(g0 + NS_PRO_GROUPS, p.groups));
+    const int g0 = blockIdx.x * p.chunk;
+    const float s = update_squares<T, VEC>(p, e, g0, min(g0 + p.chunk, p.groups));
     if (threadIdx.x < 3) p.part[((int64_t)e * p.chunks + blockIdx.x) * 3 + threadIdx.x] = s;
 }
 
@@ -285,42 +290,8 @@ __global__ void __launch_bounds__(NS_PRO_THREADS) muon_scale_kernel(const __grid
     const int e = blockIdx.y;
     float pre, post;
     norm_scales(u, e, pre, post);
-    const int g0 = blockIdx.x * NS_PRO_GROUPS;
-    scale_groups(u, e, g0, min(g0 + NS_PRO_GROUPS, u.groups), pre, post * NS_S, xh, xl);
-}
-
-// Both passes in one launch, a cluster of 8 CTAs per matrix: the sums are exchanged through
-// distributed shared memory (added in CTA order), and the second read of a CTA's eighth of the
-// matrix comes from L2, where the first has just brought it: one CTA of 1024 threads per SM, so
-// that what all of them are at (256 x 416 x 1664: 53 MB) stays there.
-// Memory bound: 256 x 416 x 1664 with momentum 610 us, 4.65 TB/s (two launches over all SMs take the
-// same there, but 587 us instead of 562 for a whole step on 64 x 1024 x 512).
-constexpr int NS_PRO_CLUSTER = 8, NS_PRO_CTHREADS = 1024;
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(NS_PRO_CTHREADS, 1) muon_update_kernel(const __grid_constant__ UpdateArgs p, __half* xh,
-                                                                     __half* xl) {
-    pdl_wait();
-    __shared__ float mine[3], scale[2];
-    const int e = blockIdx.x / NS_PRO_CLUSTER, rank = blockIdx.x % NS_PRO_CLUSTER;
-    if (rank == 0 && threadIdx.x == 0) p.prog[e] = 0;
-    const int each = (p.groups + NS_PRO_CLUSTER - 1) / NS_PRO_CLUSTER;
-    const int g0 = min(rank * each, p.groups), g1 = min(g0 + each, p.groups);
-    const float s = update_squares<T, VEC>(p, e, g0, g1);
-    if (threadIdx.x < 3) mine[threadIdx.x] = s;
-    cluster_sync();
-    if (threadIdx.x == 0) {
-        float t[3] = {};
-        for (int r = 0; r < NS_PRO_CLUSTER; ++r)
-#pragma unroll
-            for (int i = 0; i < 3; ++i) {
-                float v;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer_addr(smem_u32(mine + i), r)));
-                t[i] += v;
-            }
-        scales_of(t[0], t[1], t[2], scale[0], scale[1]);
-    }
-    cluster_sync();   // (also: nobody leaves while its sums are being read)
-    scale_groups(p, e, g0, g1, scale[0], scale[1] * NS_S, xh, xl);
+    const int g0 = blockIdx.x * u.chunk;
+    scale_groups(u, e, g0, min(g0 + u.chunk, u.groups), pre, post * NS_S, xh, xl);
 }
 
 // ------------------------------------------------------------------ products
@@ -1248,13 +1219,15 @@ constexpr int64_t NS_UNDER_WAY_BYTES = 384ll << 20;
 
 struct NsLayout {
     size_t prog, part, x0h, x0l, xh0, xh1, xl0, xl1, A, Al, B, Bl, total;
-    int chunks, groups, n_groups, group_max, slots, terms;
+    int chunk, chunks, groups, n_groups, group_max, slots, terms;
 };
 NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     NsLayout L;
     const int64_t m = r < c ? r : c, ldx = up8(c), ldm = up8(m);
     L.groups = (int)(r * ldx / 8);
-    L.chunks = (L.groups + NS_PRO_GROUPS - 1) / NS_PRO_GROUPS;
+    L.chunk = (L.groups + NS_PRO_CHUNKS - 1) / NS_PRO_CHUNKS;
+    if (L.chunk < NS_PRO_GROUPS) L.chunk = NS_PRO_GROUPS;
+    L.chunks = (L.groups + L.chunk - 1) / L.chunk;
     L.terms = m <= 128 ? 3 : 1;
     const int64_t each = (L.terms == 3 ? 8 : 6) * r * ldx + (L.terms == 3 ? 8 : 4) * m * ldm;
     int64_t most = NS_UNDER_WAY_BYTES / (each * NS_LANES);   // matrices of a group
@@ -1288,31 +1261,9 @@ NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     return L;
 }
 
-// The update's norms (and momentum), and X0 unless the matrices are thin.  One launch with a
-// cluster per matrix where there are matrices enough for all SMs and what the SMs are at stays in
-// L2, else two launches over all of them (steps on 64 x 1024 x 512: 562 us against 587; on
-// 256 x 1664 x 416, 105 MB at a time: 2.93 ms against 2.91).
-constexpr int64_t NS_PRO_L2_BYTES = 88ll << 20;
+// The update's norms (and momentum), and X0 unless the matrices are thin.
 template <typename T, bool VEC>
-cudaError_t launch_prologue(const UpdateArgs& p, int N, bool thin, __half* xh, __half* xl, int sms, cudaStream_t s) {
-    const int64_t each = (int64_t)p.groups * 8 / NS_PRO_CLUSTER * ((int)sizeof(T) + (p.M ? 4 : 0));   // bytes of a CTA
-    if (!thin && N * NS_PRO_CLUSTER >= sms && each * sms <= NS_PRO_L2_BYTES) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(N * NS_PRO_CLUSTER));
-        cfg.blockDim = dim3(NS_PRO_CTHREADS);
-        cfg.stream = s;
-        cudaLaunchAttribute at[2];
-        at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = NS_PRO_CLUSTER;
-        at[0].val.clusterDim.y = 1;
-        at[0].val.clusterDim.z = 1;
-        at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see launch_pdl
-        at[1].val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = at;
-        cfg.numAttrs = 2;
-        count_launches(1);
-        return cudaLaunchKernelEx(&cfg, muon_update_kernel<T, VEC>, p, xh, xl);
-    }
+cudaError_t launch_prologue(const UpdateArgs& p, int N, bool thin, __half* xh, __half* xl, cudaStream_t s) {
     const dim3 grid((unsigned)p.chunks, (unsigned)N);
     cudaError_t e = launch_pdl(muon_moment_kernel<T, VEC>, grid, dim3(NS_PRO_THREADS), 0, s, p);
     count_launches(1);
@@ -1365,6 +1316,7 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.u.c = q.c;
     a.u.gpr = a.ldx / 8;
     a.u.groups = L.groups;
+    a.u.chunk = L.chunk;
     a.u.chunks = L.chunks;
     a.u.part = reinterpret_cast<float*>(ws + L.part);
     a.u.prog = reinterpret_cast<int32_t*>(ws + L.prog);
@@ -1373,11 +1325,11 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     const bool thin = a.m <= NS_THIN;
     cudaError_t e;
     if (q.u_bf16)
-        e = a.u.vec ? launch_prologue<__nv_bfloat16, true>(a.u, q.N, thin, a.xh[0], a.xl[0], sms, s)
-                    : launch_prologue<__nv_bfloat16, false>(a.u, q.N, thin, a.xh[0], a.xl[0], sms, s);
+        e = a.u.vec ? launch_prologue<__nv_bfloat16, true>(a.u, q.N, thin, a.xh[0], a.xl[0], s)
+                    : launch_prologue<__nv_bfloat16, false>(a.u, q.N, thin, a.xh[0], a.xl[0], s);
     else
-        e = a.u.vec ? launch_prologue<float, true>(a.u, q.N, thin, a.xh[0], a.xl[0], sms, s)
-                    : launch_prologue<float, false>(a.u, q.N, thin, a.xh[0], a.xl[0], sms, s);
+        e = a.u.vec ? launch_prologue<float, true>(a.u, q.N, thin, a.xh[0], a.xl[0], s)
+                    : launch_prologue<float, false>(a.u, q.N, thin, a.xh[0], a.xl[0], s);
     if (e != cudaSuccess) return e;
 
     a.steps = q.steps;
