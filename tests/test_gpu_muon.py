@@ -269,3 +269,20 @@ def test_muon_update_thin(N, r, c):
     err = np.linalg.norm(_f64(W) - w)
     assert err <= 2 * lr * scale * REL * np.linalg.norm(O) + 8 * 2.0 ** -24 * np.linalg.norm(w), err
     assert torch.equal(Wb, W.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("N,r,c,rank", [(2, 100, 512, 7), (1, 2048, 128, 128), (3, 64, 700, 1), (150, 64, 64, 64),
+                                        (40, 33, 65, 33), (130, 120, 70, 9), (17, 128, 130, 128)])
+def test_orthogonalize_narrow(N, r, c, rank):
+    """33 to 128 rows or columns, few matrices and many (a cluster for each, or the tensor
+    cores), full rank and low rank; a repeated call gives the same bits."""
+    g = torch.Generator(device="cuda").manual_seed(N + r + c + rank)
+    if rank < min(r, c):
+        U = torch.randn(N, r, rank, generator=g, device="cuda") @ torch.randn(N, rank, c, generator=g, device="cuda")
+    else:
+        U = torch.randn(N, r, c, generator=g, device="cuda")
+    O = _run(U)
+    _check(O, U, [COEF] * 5)
+    assert torch.equal(_run(U), O)
+    cubic = (1.5, -0.5, 0.0)
+    _check(_run(U, steps=2, coef=cubic), U, [cubic] * 2)
