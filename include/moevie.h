@@ -322,6 +322,8 @@ moevie_status moevie_moe_few(const moevie_layer* layer, const void* x, int64_t T
  *   O: bf16, row stride ld_o >= cols, matrix stride stride_o.  O does not overlap U.
  * Arithmetic: fp16 tensor-core operands (scaled), fp32 accumulation, X carried in 22 bits:
  * the result is within 2e-3 (2-norm) of the formula's, before its rounding to bf16.
+ * (Matrices of which one side is at most 32, and few matrices of which one is at most 128:
+ * fp32 throughout.)
  * coef: HOST memory, steps x 3 floats, finite; 1 <= steps <= 32.  Sizes: rows and cols in
  * [1, 8192], 0 <= N <= 65535, else MOEVIE_ERR_UNSUPPORTED; N == 0 launches nothing.  ws:
  * moevie_orthogonalize_workspace_size bytes, set up with moevie_workspace_init. */

@@ -16,6 +16,7 @@
 //   ns_kernel           the three products of every step on tcgen05 CTA pairs in one persistent
 //                       launch, with the output or the weight update in the last one's epilogue.
 //   ns_thin_kernel      all of that for matrices whose smaller side is at most 32, in fp32.
+//   ns_small_kernel     the same for few matrices whose smaller side is 33 to 128.
 //
 // ns_kernel.  Work items are (matrix, stage, tile): a Gram, a polynomial and an apply stage for
 // each step.  Only some of the matrices are under way at a time, in buffers that are used again
@@ -40,8 +41,8 @@
 // times instead of a: where singular values have arrived near 1, B lo (which is not formed) takes
 // up most of a lo, and leaving both out is nearer (1.6e-3 becomes 1.4e-3 on Gaussian matrices) and
 // saves the last step's lo.
-// For m <= 128 the roundings of a few singular values average less, and time is latency: there
-// A and B have lo parts too and every product is hi hi + hi lo + lo hi (about 1e-5).
+// For m <= 128 the roundings of a few singular values average less, and time is latency: there (in
+// stacks that are not left to ns_small_kernel) A and B have lo parts too and every product is hi hi + hi lo + lo hi (about 1e-5).
 //
 // What bounds it, measured on one GB300 (five steps; floors are the products of one term, symmetric
 // ones counted half, at the measured 1894 TFLOP/s): 256 x 416 x 1664 2.39 ms (floor 0.63), 16 x 768 x 768
@@ -52,6 +53,8 @@
 // 20%.  One 1024 x 1024 matrix (134 us) is a chain of 15 dependent stages of 9 us: hand-over between
 // CTAs 3 us, 16 K blocks 5 us.
 #include "internal.h"
+
+#include <atomic>
 
 #include <cuda_fp16.h>
 
@@ -1040,6 +1043,71 @@ constexpr int NS_THIN_K = 128;
 constexpr int NS_THIN_LD = NS_THIN + 4;
 constexpr int NS_THIN_CLUSTER = 8;
 
+// A thread's elements of a chunk of S x K of the m x n orientation, in memory order over the
+// threads: (i0 + di u, kk0 + dk u).
+template <int S, int K>
+struct NsPlace {
+    int i0, di, kk0, dk;
+    static constexpr int PER = S * K / NS_THIN_THREADS;
+    __device__ __forceinline__ explicit NsPlace(bool tall) {
+        const int t = threadIdx.x;
+        i0 = tall ? t % S : t / K;
+        kk0 = tall ? t / S : t % K;
+        di = tall ? 0 : NS_THIN_THREADS / K;
+        dk = tall ? NS_THIN_THREADS / S : 0;
+    }
+};
+// xs[i][kk] = X0 (i, k0 + kk), zeros outside, by the whole CTA.
+template <int S, int K>
+__device__ __forceinline__ void ns_stage(const NsArgs& p, int e, int k0, float pre, float post, float (*xs)[K + 4]) {
+    const NsPlace<S, K> w(p.tall);
+    const int m = p.m, n = p.tall ? p.r : p.c;
+    const int64_t at = e * p.u.st_u + (p.tall ? (k0 + w.kk0) * p.u.ld_u + w.i0 : w.i0 * p.u.ld_u + k0 + w.kk0);
+    const int64_t d = (p.tall ? w.dk : w.di) * p.u.ld_u;
+    auto load = [&](auto get) {
+        float v[w.PER];
+#pragma unroll
+        for (int u = 0; u < w.PER; ++u)
+            v[u] = w.i0 + w.di * u < m && k0 + w.kk0 + w.dk * u < n ? get(at + u * d) : 0.f;
+#pragma unroll
+        for (int u = 0; u < w.PER; ++u) xs[w.i0 + w.di * u][w.kk0 + w.dk * u] = (v[u] * pre) * post;
+    };
+    const float* M = p.u.M;
+    const float* U = static_cast<const float*>(p.u.U);
+    const __nv_bfloat16* B = static_cast<const __nv_bfloat16*>(p.u.U);
+    const float mu = p.u.mu;
+    if (M && !p.u.nesterov) load([=](int64_t a) { return M[a]; });
+    else if (M) load([=](int64_t a) { return fmaf(mu, M[a], U[a]); });   // (with a momentum, U is fp32)
+    else if (p.u.u_bf16) load([=](int64_t a) { return as_f32(B[a]); });
+    else load([=](int64_t a) { return U[a]; });
+    __syncthreads();
+}
+// The chunk's results from xs to O, or into the weights.
+template <int S, int K>
+__device__ __forceinline__ void ns_store(const NsArgs& p, int e, int k0, const float (*xs)[K + 4]) {
+    const NsPlace<S, K> w(p.tall);
+    const int m = p.m, n = p.tall ? p.r : p.c;
+    const int64_t ld = p.O ? p.ld_o : p.ld_w, d = (p.tall ? w.dk : w.di) * ld;
+    const int64_t at = e * (p.O ? p.st_o : p.st_w) + (p.tall ? (k0 + w.kk0) * ld + w.i0 : w.i0 * ld + k0 + w.kk0);
+    auto inside = [&](int u) { return w.i0 + w.di * u < m && k0 + w.kk0 + w.dk * u < n; };
+    if (p.O) {
+#pragma unroll
+        for (int u = 0; u < w.PER; ++u)
+            if (inside(u)) p.O[at + u * d] = __float2bfloat16_rn(xs[w.i0 + w.di * u][w.kk0 + w.dk * u]);
+        return;
+    }
+    float v[w.PER];
+#pragma unroll
+    for (int u = 0; u < w.PER; ++u) v[u] = inside(u) ? p.W[at + u * d] : 0.f;
+#pragma unroll
+    for (int u = 0; u < w.PER; ++u)
+        if (inside(u)) {
+            const float o = fmaf(-p.rate, xs[w.i0 + w.di * u][w.kk0 + w.dk * u], p.decay * v[u]);
+            p.W[at + u * d] = o;
+            if (p.Wb) p.Wb[at + u * d] = __float2bfloat16_rn(o);
+        }
+}
+
 __global__ void __launch_bounds__(NS_THIN_THREADS, 3) ns_thin_kernel(const __grid_constant__ NsArgs p) {
     pdl_wait();
     typedef float Square[NS_THIN][NS_THIN_LD];
@@ -1050,31 +1118,7 @@ __global__ void __launch_bounds__(NS_THIN_THREADS, 3) ns_thin_kernel(const __gri
     const int chunks = (n + NS_THIN_K - 1) / NS_THIN_K;
     float pre, post;
     norm_scales(p.u, e, pre, post);
-    // A thread's 16 elements of a chunk, in memory order over the threads: (i0 + di u, k0 + kk0 + dk u)
-    constexpr int PER = NS_THIN * NS_THIN_K / NS_THIN_THREADS;
-    const int i0 = p.tall ? tid & 31 : tid / NS_THIN_K, di = p.tall ? 0 : NS_THIN_THREADS / NS_THIN_K;
-    const int kk0 = p.tall ? tid >> 5 : tid & (NS_THIN_K - 1), dk = p.tall ? NS_THIN_THREADS / 32 : 0;
-    auto inside = [&](int k0, int u) { return i0 + di * u < m && k0 + kk0 + dk * u < n; };
-    auto load = [&](int k0, auto get) {
-        const int64_t at = e * p.u.st_u + (p.tall ? (k0 + kk0) * p.u.ld_u + i0 : i0 * p.u.ld_u + k0 + kk0);
-        const int64_t d = (p.tall ? dk : di) * p.u.ld_u;
-        float v[PER];
-#pragma unroll
-        for (int u = 0; u < PER; ++u) v[u] = inside(k0, u) ? get(at + u * d) : 0.f;
-#pragma unroll
-        for (int u = 0; u < PER; ++u) xs[i0 + di * u][kk0 + dk * u] = (v[u] * pre) * post;
-    };
-    auto stage = [&](int k0) {   // xs[i][kk] = X0 (i, k0 + kk) of the m x n orientation
-        const float* M = p.u.M;
-        const float* U = static_cast<const float*>(p.u.U);
-        const __nv_bfloat16* B = static_cast<const __nv_bfloat16*>(p.u.U);
-        const float mu = p.u.mu;
-        if (M && !p.u.nesterov) load(k0, [=](int64_t a) { return M[a]; });
-        else if (M) load(k0, [=](int64_t a) { return fmaf(mu, M[a], U[a]); });   // (with a momentum, U is fp32)
-        else if (p.u.u_bf16) load(k0, [=](int64_t a) { return as_f32(B[a]); });
-        else load(k0, [=](int64_t a) { return U[a]; });
-        __syncthreads();
-    };
+    auto stage = [&](int k0) { ns_stage<NS_THIN, NS_THIN_K>(p, e, k0, pre, post, xs); };
     // A: four groups of 64 threads share a chunk's columns, a thread has rows ti + 8 u, columns tj + 8 v
     {
         const int g = tid >> 6, ti = tid >> 3 & 7, tj = tid & 7;
@@ -1186,24 +1230,208 @@ __global__ void __launch_bounds__(NS_THIN_THREADS, 3) ns_thin_kernel(const __gri
 #pragma unroll
         for (int u = 0; u < 4; ++u) *reinterpret_cast<float4*>(&xs[r4 + u][c4]) = o[u];
         __syncthreads();
-        const int64_t base = (p.O ? e * p.st_o : e * p.st_w), ld = p.O ? p.ld_o : p.ld_w;
-        const int64_t at = base + (p.tall ? (k0 + kk0) * ld + i0 : i0 * ld + k0 + kk0), d = (p.tall ? dk : di) * ld;
-        if (p.O) {
+        ns_store<NS_THIN, NS_THIN_K>(p, e, k0, xs);
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------- few narrow matrices
+
+// NS_THIN < m <= S (64 or 128), the same iteration in fp32 by a cluster of 8 CTAs per matrix: each
+// forms the part of A from its columns of X and then has S / 8 rows of every product.  All factors
+// being symmetric and commuting, rows of Q P, A P and (A P) P need only the CTA's own rows of the
+// left factor, so P and A alone are shared, in every CTA's memory.  For few matrices: on the tensor
+// cores the Gram product of one such matrix is a single tile, n / 64 K blocks of three terms one
+// after the other, five times.
+// Bound by shared memory and the fp32 units of its 8 SMs: 128 x 2048 in 136 us, of which the 19 products
+// of 128 x 128 are about 80.
+constexpr int NS_SMALL_K = 64;
+template <int S>
+constexpr int ns_small_smem() {
+    return 4 * ((2 * S + 2 * (S / 8)) * (S + 4) + S * (NS_SMALL_K + 4));
+}
+
+// Writes N (2 or 4) consecutive floats at the same place of every CTA of the cluster.
+template <int N>
+__device__ __forceinline__ void ns_share(const float* at, const float (&v)[N]) {
+    const uint32_t mine = smem_u32(at);
 #pragma unroll
-            for (int u = 0; u < PER; ++u)
-                if (inside(k0, u)) p.O[at + u * d] = __float2bfloat16_rn(xs[i0 + di * u][kk0 + dk * u]);
-        } else {
-            float w[PER];
+    for (int r = 0; r < 8; ++r) {
+        const uint32_t a = peer_addr(mine, r);
+        if (N == 4)
+            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v[0]), "f"(v[1]),
+                         "f"(v[N - 2]), "f"(v[N - 1])
+                         : "memory");
+        else
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(v[0]), "f"(v[1]) : "memory");
+    }
+}
+
+// out[i] = rows[i] . R for a warp's rows; a lane has CT consecutive columns.
+template <int S, int NR>
+__device__ __forceinline__ void ns_rows(float (&out)[NR][S / 32], const float* const (&rows)[NR], const float (*Rm)[S + 4]) {
+    constexpr int CT = S / 32;
+    const int c = (threadIdx.x & 31) * CT;
 #pragma unroll
-            for (int u = 0; u < PER; ++u) w[u] = inside(k0, u) ? p.W[at + u * d] : 0.f;
+    for (int i = 0; i < NR; ++i)
 #pragma unroll
-            for (int u = 0; u < PER; ++u)
-                if (inside(k0, u)) {
-                    w[u] = fmaf(-p.rate, xs[i0 + di * u][kk0 + dk * u], p.decay * w[u]);
-                    p.W[at + u * d] = w[u];
-                    if (p.Wb) p.Wb[at + u * d] = __float2bfloat16_rn(w[u]);
-                }
+        for (int j = 0; j < CT; ++j) out[i][j] = 0.f;
+#pragma unroll 2
+    for (int k = 0; k < S; k += 4) {
+        float l[NR][4];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) *reinterpret_cast<float4*>(l[i]) = *reinterpret_cast<const float4*>(rows[i] + k);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float r[CT];
+            if (CT == 4) *reinterpret_cast<float4*>(r) = *reinterpret_cast<const float4*>(&Rm[k + q][c]);
+            else *reinterpret_cast<float2*>(r) = *reinterpret_cast<const float2*>(&Rm[k + q][c]);
+#pragma unroll
+            for (int i = 0; i < NR; ++i)
+#pragma unroll
+                for (int j = 0; j < CT; ++j) out[i][j] = fmaf(l[i][q], r[j], out[i][j]);
         }
+    }
+}
+
+template <int S>
+__global__ void __launch_bounds__(NS_THIN_THREADS, S == 64 ? 2 : 1) ns_small_kernel(const __grid_constant__ NsArgs p) {
+    constexpr int R = S / 8, LD = S + 4, K = NS_SMALL_K, TI = S / 16, CT = S / 32, RW = R / 8;
+    extern __shared__ __align__(16) float ns_small_mem[];
+    typedef float Row[LD];
+    Row* A = reinterpret_cast<Row*>(ns_small_mem);
+    Row* P = A + S;
+    Row* Qs = P + S;   // this CTA's rows of Q and of A P
+    Row* Ts = Qs + R;
+    typedef float XRow[K + 4];
+    XRow* xs = reinterpret_cast<XRow*>(Ts + R);
+    pdl_wait();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, m = p.m, n = p.tall ? p.r : p.c;
+    const int e = blockIdx.x / 8, rank = (int)cluster_rank(), chunks = (n + K - 1) / K;
+    float pre, post;
+    norm_scales(p.u, e, pre, post);
+    {   // this CTA's part of A: rows ti + 16 u, columns tj + 16 v
+        const int ti = tid >> 4, tj = tid & 15;
+        float acc[TI][TI] = {};
+        for (int ch = rank; ch < chunks; ch += 8) {
+            ns_stage<S, K>(p, e, ch * K, pre, post, xs);
+#pragma unroll 1
+            for (int kk = 0; kk < K; kk += 4) {
+                float4 b[TI];
+#pragma unroll
+                for (int v = 0; v < TI; ++v) b[v] = *reinterpret_cast<const float4*>(&xs[tj + 16 * v][kk]);
+#pragma unroll
+                for (int u = 0; u < TI; ++u) {
+                    const float4 a = *reinterpret_cast<const float4*>(&xs[ti + 16 * u][kk]);
+#pragma unroll
+                    for (int v = 0; v < TI; ++v)
+                        acc[u][v] = fmaf(a.w, b[v].w, fmaf(a.z, b[v].z, fmaf(a.y, b[v].y, fmaf(a.x, b[v].x, acc[u][v]))));
+                }
+            }
+            if (chunks > 8) __syncthreads();   // (one chunk a CTA: it stays for the end)
+        }
+#pragma unroll
+        for (int u = 0; u < TI; ++u)
+#pragma unroll
+            for (int v = 0; v < TI; ++v) A[ti + 16 * u][tj + 16 * v] = acc[u][v];
+    }
+    // the sum of the parts, this CTA's rows first, then everyone's
+    const int row0 = rank * R + warp * RW, col = lane * CT;   // a warp's rows, a lane's columns
+    float sum[RW][CT] = {};
+    cluster_sync();
+#pragma unroll
+    for (int i = 0; i < RW; ++i)
+#pragma unroll
+        for (int j = 0; j < CT; j += 2) {
+            const uint32_t mine = smem_u32(&A[row0 + i][col + j]);
+            for (int r = 0; r < 8; ++r) {
+                float x, y;
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(peer_addr(mine, r)));
+                sum[i][j] += x;
+                sum[i][j + 1] += y;
+            }
+        }
+    cluster_sync();
+#pragma unroll
+    for (int i = 0; i < RW; ++i) ns_share<CT>(&A[row0 + i][col], sum[i]);
+    cluster_sync();
+    const float* ra[RW];
+#pragma unroll
+    for (int i = 0; i < RW; ++i) ra[i] = A[row0 + i];
+    for (int it = 0; it < p.steps; ++it) {
+        const float ca = p.coef[3 * it], cb = p.coef[3 * it + 1], cc = p.coef[3 * it + 2];
+        const bool last = it + 1 == p.steps;
+        float t[RW][CT];
+        ns_rows<S, RW>(t, ra, A);
+#pragma unroll
+        for (int i = 0; i < RW; ++i) {
+#pragma unroll
+            for (int j = 0; j < CT; ++j) {
+                t[i][j] = fmaf(cc, t[i][j], cb * A[row0 + i][col + j]) + (row0 + i == col + j ? ca : 0.f);
+                if (it == 0) Qs[warp * RW + i][col + j] = t[i][j];
+            }
+            ns_share<CT>(&P[row0 + i][col], t[i]);
+        }
+        cluster_sync();   // P is complete
+        // rows of Q P and of A P, then of (A P) P; a warp's rows of Q and A P are its own
+        float o[2 * RW][CT];
+        const float* rows[2 * RW];
+#pragma unroll
+        for (int i = 0; i < RW; ++i) {
+            rows[i] = Qs[warp * RW + i];
+            rows[RW + i] = ra[i];
+        }
+        ns_rows<S, 2 * RW>(o, rows, P);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < RW; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) {
+                if (it > 0) Qs[warp * RW + i][col + j] = o[i][j];
+                Ts[warp * RW + i][col + j] = o[RW + i][j];
+            }
+        __syncwarp();
+        if (last) break;
+#pragma unroll
+        for (int i = 0; i < RW; ++i) ra[i] = Ts[warp * RW + i];
+        ns_rows<S, RW>(t, ra, P);
+#pragma unroll
+        for (int i = 0; i < RW; ++i) {
+            ns_share<CT>(&A[row0 + i][col], t[i]);
+            ra[i] = A[row0 + i];
+        }
+        cluster_sync();   // A is complete, and P free
+    }
+    cluster_sync();   // P free
+#pragma unroll
+    for (int i = 0; i < RW; ++i) {
+        float q[CT];
+#pragma unroll
+        for (int j = 0; j < CT; ++j) q[j] = Qs[warp * RW + i][col + j];
+        ns_share<CT>(&P[row0 + i][col], q);
+    }
+    cluster_sync();
+    // Q X0: S / 16 rows x 4 columns a thread, through xs to memory order
+    for (int ch = rank; ch < chunks; ch += 8) {
+        const int c4 = (tid & 15) * 4, r0 = (tid >> 4) * TI;
+        if (chunks > 8) ns_stage<S, K>(p, e, ch * K, pre, post, xs);
+        float4 o[TI] = {};
+#pragma unroll 2
+        for (int j = 0; j < m; ++j) {
+            const float4 x = *reinterpret_cast<const float4*>(&xs[j][c4]);
+            float q[TI];
+#pragma unroll
+            for (int u = 0; u < TI; u += 4) *reinterpret_cast<float4*>(q + u) = *reinterpret_cast<const float4*>(&P[j][r0 + u]);
+#pragma unroll
+            for (int u = 0; u < TI; ++u)
+                o[u] = make_float4(fmaf(q[u], x.x, o[u].x), fmaf(q[u], x.y, o[u].y), fmaf(q[u], x.z, o[u].z),
+                                   fmaf(q[u], x.w, o[u].w));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < TI; ++u) *reinterpret_cast<float4*>(&xs[r0 + u][c4]) = o[u];
+        __syncthreads();
+        ns_store<S, K>(p, e, ch * K, xs);
         __syncthreads();
     }
 }
@@ -1293,6 +1521,66 @@ size_t ns_workspace_bytes(int64_t N, int64_t r, int64_t c) {
     return most;
 }
 
+namespace {
+// Launch attributes of a kernel with a cluster per matrix.
+struct NsClusterLaunch {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[2];
+    NsClusterLaunch(int N, int ctas, int smem, cudaStream_t s) {
+        cfg.gridDim = dim3((unsigned)(N * ctas));
+        cfg.blockDim = dim3(NS_THIN_THREADS);
+        cfg.dynamicSmemBytes = (size_t)smem;
+        cfg.stream = s;
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = (unsigned)ctas;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see launch_pdl
+        at[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 2;
+    }
+};
+// Clusters of ns_small_kernel<S> that run at a time on the current device (0: none).
+template <int S>
+int ns_small_clusters() {
+    static std::atomic<int> cache[64];   // count + 1
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    int n = cache[dev].load(std::memory_order_relaxed) - 1;
+    if (n >= 0) return n;
+    n = 0;
+    NsClusterLaunch l(1, 8, ns_small_smem<S>(), nullptr);
+    l.cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(ns_small_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, ns_small_smem<S>()) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, ns_small_kernel<S>, &l.cfg) != cudaSuccess || n < 0) {
+        cudaGetLastError();
+        n = 0;
+    }
+    cache[dev].store(n + 1, std::memory_order_relaxed);
+    return n;
+}
+// Whether the cluster kernel is the faster one for N matrices m x n: times (us, five steps) of both,
+// fitted to measurements at m of 64, 100 and 128, n of 64 to 2048, N of 1 to 128.  One 64 x 2048: 51
+// against 165 on the tensor cores, 32 of them 80 and 327, 128 of 64 x 64 149 and 101; one 128 x 2048 136
+// and 174, 2048 x 100 134 and 284, 32 of 128 x 512 256 and 139.
+bool ns_small_pays(int N, int m, int n, bool tall) {
+    if (m <= NS_THIN || m > 128) return false;
+    const int at_once = m <= 64 ? ns_small_clusters<64>() : ns_small_clusters<128>();
+    if (at_once <= 0) return false;
+    const int full = N / at_once, rest = N - full * at_once;
+    float here = 5.0f, tensor;
+    if (m <= 64) {   // two CTAs per SM; half as many clusters have an SM per CTA
+        here += full * (36.0f + 0.0177f * n);
+        if (rest > 0) here += 2 * rest <= at_once ? 26.0f + 0.0105f * n : 36.0f + 0.0177f * n;
+        tensor = 70.0f + 0.046f * n + N * (0.1f + 0.0017f * n);
+    } else {
+        here += (full + (rest > 0 ? 1 : 0)) * (80.0f + 0.025f * n);
+        tensor = 80.0f + (tall ? 0.1f : 0.046f) * n + N * (0.05f + 0.0023f * n);
+    }
+    return here < tensor;
+}
+}  // namespace
+
 cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t limit_ns, cudaStream_t s) {
     const NsLayout L = ns_layout(q.N, q.r, q.c);
     NsArgs a = {};
@@ -1322,14 +1610,14 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.u.prog = reinterpret_cast<int32_t*>(ws + L.prog);
     a.xh[0] = reinterpret_cast<__half*>(ws + L.x0h);
     a.xl[0] = reinterpret_cast<__half*>(ws + L.x0l);
-    const bool thin = a.m <= NS_THIN;
+    const bool thin = a.m <= NS_THIN, small = !thin && a.m <= 128 && ns_small_pays(a.N, a.m, a.tall ? a.r : a.c, a.tall);
     cudaError_t e;
     if (q.u_bf16)
-        e = a.u.vec ? launch_prologue<__nv_bfloat16, true>(a.u, q.N, thin, a.xh[0], a.xl[0], s)
-                    : launch_prologue<__nv_bfloat16, false>(a.u, q.N, thin, a.xh[0], a.xl[0], s);
+        e = a.u.vec ? launch_prologue<__nv_bfloat16, true>(a.u, q.N, thin || small, a.xh[0], a.xl[0], s)
+                    : launch_prologue<__nv_bfloat16, false>(a.u, q.N, thin || small, a.xh[0], a.xl[0], s);
     else
-        e = a.u.vec ? launch_prologue<float, true>(a.u, q.N, thin, a.xh[0], a.xl[0], s)
-                    : launch_prologue<float, false>(a.u, q.N, thin, a.xh[0], a.xl[0], s);
+        e = a.u.vec ? launch_prologue<float, true>(a.u, q.N, thin || small, a.xh[0], a.xl[0], s)
+                    : launch_prologue<float, false>(a.u, q.N, thin || small, a.xh[0], a.xl[0], s);
     if (e != cudaSuccess) return e;
 
     a.steps = q.steps;
@@ -1358,25 +1646,22 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.rate = q.rate;
     a.status = reinterpret_cast<DevStatus*>(ws);
     a.limit_ns = limit_ns;
-    if (thin) {
-        // CTAs of a matrix: one per 128 columns, up to about eight CTAs per SM in all
-        const int n = a.tall ? a.r : a.c, room = 8 * sms / a.N;
-        a.thin_cluster = (n + NS_THIN_K - 1) / NS_THIN_K;
-        if (a.thin_cluster > NS_THIN_CLUSTER) a.thin_cluster = NS_THIN_CLUSTER;
-        if (a.thin_cluster > room) a.thin_cluster = room > 1 ? room : 1;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(a.N * a.thin_cluster));
-        cfg.blockDim = dim3(NS_THIN_THREADS);
-        cfg.stream = s;
-        cudaLaunchAttribute at[2];
-        at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = (unsigned)a.thin_cluster;
-        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-        at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see launch_pdl
-        at[1].val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = at;
-        cfg.numAttrs = 2;
-        e = cudaLaunchKernelEx(&cfg, ns_thin_kernel, a);
+    if (thin || small) {
+        if (small && a.m <= 64) {
+            NsClusterLaunch l(a.N, 8, ns_small_smem<64>(), s);
+            e = cudaLaunchKernelEx(&l.cfg, ns_small_kernel<64>, a);
+        } else if (small) {
+            NsClusterLaunch l(a.N, 8, ns_small_smem<128>(), s);
+            e = cudaLaunchKernelEx(&l.cfg, ns_small_kernel<128>, a);
+        } else {
+            // CTAs of a matrix: one per 128 columns, up to about eight CTAs per SM in all
+            const int n = a.tall ? a.r : a.c, room = 8 * sms / a.N;
+            a.thin_cluster = (n + NS_THIN_K - 1) / NS_THIN_K;
+            if (a.thin_cluster > NS_THIN_CLUSTER) a.thin_cluster = NS_THIN_CLUSTER;
+            if (a.thin_cluster > room) a.thin_cluster = room > 1 ? room : 1;
+            NsClusterLaunch l(a.N, a.thin_cluster, 0, s);
+            e = cudaLaunchKernelEx(&l.cfg, ns_thin_kernel, a);
+        }
         count_launches(1);
         return e != cudaSuccess ? e : cudaGetLastError();
     }
