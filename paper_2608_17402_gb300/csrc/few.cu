@@ -32,9 +32,8 @@
 // for nothing.  All waits have time limits.
 //
 // What bounds it, measured on one GB300 (against the time of the weights' bytes at the measured
-// copy bandwidth of 6.77 TB/s).  Many tokens: the weights' bytes; 64 tokens, d 1664, 256 experts of
-// h 416, 8 slots: 93 us, bytes 91 (part of them still in L2 from the call before).  16 tokens, 128
-// experts: 33 us (29).  One token: a chain of dependent steps, each a trip to L2 or HBM (0.7 to
+// copy bandwidth of 6.77 TB/s).  Many tokens: the weights' bytes behind a front of 11 to 15 us; 64
+// tokens, d 1664, 8 slots, 171 of 256 experts of h 416 touched: 91 us, bytes 72.  One token: a chain of dependent steps, each a trip to L2 or HBM (0.7 to
 // 1.5 us): 23 us at d 1536, 8 slots, h 768 (bytes 5.6): 2 launch, 4 logits and barrier, 2 selection,
 // 1.2 plan, 5.5 up, 2.4 activation and hand-over, 2.8 down, 3 sum.  The code before the first weight
 // load is kept short rather than unrolled: run once per call, it is paced by instruction fetches
