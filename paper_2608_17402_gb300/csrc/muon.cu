@@ -42,7 +42,10 @@
 // up most of a lo, and leaving both out is nearer (1.6e-3 becomes 1.4e-3 on Gaussian matrices) and
 // saves the last step's lo.
 // For m <= 128 the roundings of a few singular values average less, and time is latency: there (in
-// stacks that are not left to ns_small_kernel) A and B have lo parts too and every product is hi hi + hi lo + lo hi (about 1e-5).
+// stacks that are not left to ns_small_kernel) A and B have lo parts too, and the polynomial and the
+// apply product are hi hi + hi lo + lo hi.  The Gram product, whose K is the long side, stays hi hi:
+// over five steps the result is then within 0.8e-3 before its rounding to bf16 (all three products
+// in one term 2e-3 for 64 singular values, the Gram product in three terms too 1e-5).
 //
 // What bounds it, measured on one GB300 (five steps; floors are the products of one term, symmetric
 // ones counted half, at the measured 1894 TFLOP/s): 256 x 416 x 1664 2.39 ms (floor 0.63), 16 x 768 x 768
@@ -436,6 +439,7 @@ __device__ __forceinline__ int ns_dst(int s) { return 1 + (s & 1); }
 struct NsTile {
     int m0, n0, bn, num_kb;            // num_kb: K blocks of one term
     int mma_n;                         // columns that are computed
+    int terms;                         // products: hi hi (1), and hi lo + lo hi (3)
     bool mirror;                       // symmetric output: also write its mirror image
     bool same;                         // A's and B's shares of each CTA are the same box: loaded once
     const CUtensorMap *a[2], *b[2];    // operands, hi and lo
@@ -488,7 +492,8 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
     t.bn = min(p.bn, (cols - t.n0 + 31) & ~31);   // a multiple of 32: each CTA holds half of B
     // A tile on the diagonal: rows and columns of a CTA coincide.  One that the matrix's end trims is
     // computed 256 wide all the same (the products are bound by L2, not by the tensor cores).
-    if (it.kind != NS_APPLY) t.same = t.n0 == t.m0 && p.bn == NS_BM && p.terms == 1;
+    t.terms = it.kind == NS_GRAM ? 1 : p.terms;
+    if (it.kind != NS_APPLY) t.same = t.n0 == t.m0 && p.bn == NS_BM && t.terms == 1;
     t.mma_n = t.same ? NS_BM : t.bn;
     t.num_kb = (k + NS_BK - 1) / NS_BK;
     return t;
@@ -547,7 +552,7 @@ __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abo
         const int nbox = t.same ? 0 : (t.bn / 2 + 63) / 64;
         const uint32_t bytes = 2u * (uint32_t)(2 + nbox) * NS_BOX;
         const int mm = t.m0 + (int)sm.rank * NS_HALF, nn = t.n0 + (int)sm.rank * (t.bn / 2);
-        for (int term = 0; term < p.terms; ++term) {
+        for (int term = 0; term < t.terms; ++term) {
             const CUtensorMap *ma = t.a[term == 2], *mb = t.b[term == 1];   // hi hi, hi lo, lo hi
             for (int kb = 0; kb < t.num_kb; ++kb) {
                 if (!mbar_wait(sm.empty + 8 * s, ph ^ 1u, p.limit_ns, abort_flag)) {
@@ -594,7 +599,7 @@ __device__ __forceinline__ void ns_mma(const NsArgs& p, const NsSmem& sm, uint32
         ++n;
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)acc * NS_MAXBN;
-        const int kbs = t.num_kb * p.terms;
+        const int kbs = t.num_kb * t.terms;
         bool ok = true;
         for (int kb = 0; kb < kbs; ++kb) {
             if (!mbar_wait(sm.full + 8 * s, ph, p.limit_ns, abort_flag)) {
@@ -1241,8 +1246,8 @@ __global__ void __launch_bounds__(NS_THIN_THREADS, 3) ns_thin_kernel(const __gri
 // forms the part of A from its columns of X and then has S / 8 rows of every product.  All factors
 // being symmetric and commuting, rows of Q P, A P and (A P) P need only the CTA's own rows of the
 // left factor, so P and A alone are shared, in every CTA's memory.  For few matrices: on the tensor
-// cores the Gram product of one such matrix is a single tile, n / 64 K blocks of three terms one
-// after the other, five times.
+// cores the Gram product of one such matrix is a single tile, n / 64 K blocks one after the other,
+// and every step three dependent launches' worth of hand-over.
 // Bound by shared memory and the fp32 units of its 8 SMs: 128 x 2048 in 136 us, of which the 19 products
 // of 128 x 128 are about 80.
 constexpr int NS_SMALL_K = 64;
@@ -1561,8 +1566,8 @@ int ns_small_clusters() {
 }
 // Whether the cluster kernel is the faster one for N matrices m x n: times (us, five steps) of both,
 // fitted to measurements at m of 64, 100 and 128, n of 64 to 2048, N of 1 to 128.  One 64 x 2048: 51
-// against 165 on the tensor cores, 32 of them 80 and 327, 128 of 64 x 64 149 and 101; one 128 x 2048 136
-// and 174, 2048 x 100 134 and 284, 32 of 128 x 512 256 and 139.
+// against 105 on the tensor cores, 32 of them 80 and 228, 128 of 64 x 64 149 and 98; 8 of 2048 x 100 135
+// and 195, of 100 x 512 88 and 107, 32 of 128 x 512 256 and 122.
 bool ns_small_pays(int N, int m, int n, bool tall) {
     if (m <= NS_THIN || m > 128) return false;
     const int at_once = m <= 64 ? ns_small_clusters<64>() : ns_small_clusters<128>();
@@ -1572,10 +1577,10 @@ bool ns_small_pays(int N, int m, int n, bool tall) {
     if (m <= 64) {   // two CTAs per SM; half as many clusters have an SM per CTA
         here += full * (36.0f + 0.0177f * n);
         if (rest > 0) here += 2 * rest <= at_once ? 26.0f + 0.0105f * n : 36.0f + 0.0177f * n;
-        tensor = 70.0f + 0.046f * n + N * (0.1f + 0.0017f * n);
+        tensor = 68.0f + 0.018f * n + N * (0.1f + 0.0014f * n);
     } else {
         here += (full + (rest > 0 ? 1 : 0)) * (80.0f + 0.025f * n);
-        tensor = 80.0f + (tall ? 0.1f : 0.046f) * n + N * (0.05f + 0.0023f * n);
+        tensor = (tall ? 92.0f + 0.032f * n : 80.0f + 0.017f * n) + N * (0.1f + 0.0018f * n);
     }
     return here < tensor;
 }
