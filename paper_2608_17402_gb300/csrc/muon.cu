@@ -23,11 +23,12 @@
 // for the next ones, so that most of what lies between X0 and the result is still in L2 when it is
 // read (all matrices under way at once: the apply stage alone moved 1.4 GB a step, 755 us of a
 // 1000 us step on 256 x 416 x 1664).  The matrices under way form NS_LANES groups that are one stage
-// apart; in each slot of the schedule every group advances by a stage, so that a tile's inputs were
-// finished about a slot of other tiles earlier and its pair rarely waits.  A counter per matrix
-// holds the finished tiles of its stages, which follow one another; an item waits for the count of
-// all earlier stages.  Items are dealt to the pairs round-robin in schedule order and depend on
-// earlier slots only; all pairs are co-resident (cooperative launch).
+// apart (one group, if that is the whole stack); in each slot of the schedule every group advances
+// by a stage, so that a tile's inputs were finished about a slot of other tiles earlier and its pair
+// rarely waits.  A counter per matrix holds the finished tiles of its stages, which follow one
+// another; an item waits for the count of all earlier stages.  Items are dealt to the pairs
+// round-robin in schedule order and depend on earlier items only; all pairs are co-resident
+// (cooperative launch).
 //
 // Working format.  X is held as hi + lo, two fp16 values (22 significant bits), times 2^10; A and B
 // as fp16 times 2^10.  The tensor cores multiply the hi parts (fp16 has three bits more than bf16
@@ -48,13 +49,13 @@
 // in one term 2e-3 for 64 singular values, the Gram product in three terms too 1e-5).
 //
 // What bounds it, measured on one GB300 (five steps; floors are the products of one term, symmetric
-// ones counted half, at the measured 1894 TFLOP/s): 256 x 416 x 1664 2.39 ms (floor 0.63), 16 x 768 x 768
-// 0.24 ms (0.077), a step on 64 x 1024 x 512 0.56 ms (0.16).  Traffic between L2 and the SMs comes
-// first (16 MB per matrix and step of 416 x 1664, 8.6 TB/s in all), not the tensor cores (26 to 32%) or
-// HBM: in a copy without the epilogue's arithmetic the first case took 2.30 ms, without its loads
-// 2.20, without the stores 2.01, without all three 1.79; prefetches into L2 ahead of the loads cost 3 to
-// 20%.  One 1024 x 1024 matrix (134 us) is a chain of 15 dependent stages of 9 us: hand-over between
-// CTAs 3 us, 16 K blocks 5 us.
+// ones counted half, at the measured 1894 TFLOP/s): 256 x 416 x 1664 2.33 ms (floor 0.63), 16 x 768 x 768
+// 0.21 ms (0.077), a step on 64 x 1024 x 512 0.56 ms (0.16).  Traffic between L2 and the SMs comes first
+// (16 MB per matrix and step of 416 x 1664, 8.8 TB/s in all), not the tensor cores (26 to 36%) or HBM: in
+// a copy without the epilogue's arithmetic the first case took 0.97 of the time, without its loads
+// 0.93, without the stores 0.85, without all three 0.75; prefetches into L2 ahead of the loads cost 3
+// to 20%.  One 1024 x 1024 matrix (124 us) is a chain of 15 dependent stages of 8 us: hand-over between
+// CTAs 5 us, 16 K blocks 3 us.  So are stacks of up to about 100 narrow matrices (91 x 505 x 92 152 us).
 #include "internal.h"
 
 #include <atomic>
@@ -326,7 +327,8 @@ constexpr int NS_BARS = 2 * NS_RING_MAX + 5 + 3 * NS_SLOTS;
 constexpr int NS_SMEM = NS_RING_BYTES + NS_SLOTS * NS_SLOT_BYTES + 1024 + 256;
 static_assert(NS_SMEM <= 232448 && NS_BARS * 8 + 8 <= 256, "shared memory of one CTA");
 
-constexpr int NS_LANES = 3;           // groups of matrices under way, a stage apart
+constexpr int NS_LANES = 2;           // groups of matrices under way, a stage apart (three: 256 x 416 x 1664
+                                      // 2.38 ms instead of 2.33)
 constexpr int NS_MAX_STAGES = 3 * NS_MAX_STEPS;
 constexpr int NS_DONE = 2;            // a finished item's contribution to its matrix's counter (both CTAs)
 
@@ -1444,10 +1446,12 @@ __global__ void __launch_bounds__(NS_THIN_THREADS, S == 64 ? 2 : 1) ns_small_ker
 inline int64_t up8(int64_t v) { return (v + 7) / 8 * 8; }
 inline size_t up256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 
-// Matrices under way, NS_LANES groups of them: as many as keep the working arrays within this.
-// Fewer keep more of them in L2, but a slot of the schedule must hold several tiles for every
-// pair, as a tile's inputs are about 12 us old before the next can start on them.  Measured on
-// 256 x 416 x 1664: 48 MB 5.2 ms, 72 MB 3.8, 100 MB 3.3, 140 MB 2.8, 220 MB 2.5, 400 MB 2.4.
+// Matrices under way: as many as keep the working arrays within this, in NS_LANES groups.  Fewer
+// keep more of them in L2, but a slot of the schedule must hold several tiles for every pair, as a
+// tile's inputs are about 12 us old before the next can start on them.  Measured on 256 x 416 x 1664:
+// 48 MB 5.2 ms, 72 MB 3.8, 100 MB 3.3, 140 MB 2.8, 220 MB 2.5, 400 MB 2.4.  A stack that is under way as a
+// whole forms one group: with two, its schedule is one stage longer and its tiles wait as much
+// (16 x 768 x 768 212 us instead of 224, 13 x 1889 x 354 263 instead of 297).
 constexpr int64_t NS_UNDER_WAY_BYTES = 384ll << 20;
 
 struct NsLayout {
@@ -1467,7 +1471,7 @@ NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     if (most < 1) most = 1;
     const int64_t rounds = (N + most * NS_LANES - 1) / (most * NS_LANES);
     L.n_groups = (int)(rounds * NS_LANES < N ? rounds * NS_LANES : N);   // sizes then differ by one at most
-    if (L.n_groups < 1) L.n_groups = 1;
+    if (rounds <= 1) L.n_groups = 1;
     L.group_max = (int)((N + L.n_groups - 1) / L.n_groups);
     L.slots = L.group_max * (L.n_groups < NS_LANES ? L.n_groups : NS_LANES);
     size_t o = up256(sizeof(DevStatus));
@@ -1566,8 +1570,8 @@ int ns_small_clusters() {
 }
 // Whether the cluster kernel is the faster one for N matrices m x n: times (us, five steps) of both,
 // fitted to measurements at m of 64, 100 and 128, n of 64 to 2048, N of 1 to 128.  One 64 x 2048: 51
-// against 105 on the tensor cores, 32 of them 80 and 228, 128 of 64 x 64 149 and 98; 8 of 2048 x 100 135
-// and 195, of 100 x 512 88 and 107, 32 of 128 x 512 256 and 122.
+// against 104 on the tensor cores, 32 of them 80 and 178, 128 of 64 x 64 149 and 86; 8 of 2048 x 100 135
+// and 175, of 100 x 512 88 and 100, 32 of 128 x 512 256 and 116.
 bool ns_small_pays(int N, int m, int n, bool tall) {
     if (m <= NS_THIN || m > 128) return false;
     const int at_once = m <= 64 ? ns_small_clusters<64>() : ns_small_clusters<128>();
@@ -1577,10 +1581,10 @@ bool ns_small_pays(int N, int m, int n, bool tall) {
     if (m <= 64) {   // two CTAs per SM; half as many clusters have an SM per CTA
         here += full * (36.0f + 0.0177f * n);
         if (rest > 0) here += 2 * rest <= at_once ? 26.0f + 0.0105f * n : 36.0f + 0.0177f * n;
-        tensor = 68.0f + 0.018f * n + N * (0.1f + 0.0014f * n);
+        tensor = 68.0f + 0.017f * n + N * (0.06f + 0.0013f * n);
     } else {
         here += (full + (rest > 0 ? 1 : 0)) * (80.0f + 0.025f * n);
-        tensor = (tall ? 92.0f + 0.032f * n : 80.0f + 0.017f * n) + N * (0.1f + 0.0018f * n);
+        tensor = (tall ? 92.0f + 0.032f * n : 80.0f + 0.017f * n) + N * (0.05f + 0.0017f * n);
     }
     return here < tensor;
 }
