@@ -343,6 +343,7 @@ struct NsArgs {
     __half *xh[3], *xl[3];             // X0 [N][r][ldx]; X, ping-pong [slots][r][ldx] (lo in place with one term)
     __half *A[2], *B[2];               // hi, lo (lo with three terms only) [slots][m][ldm]
     int N, r, c, m, ldx, ldm, tall, terms;
+    int twin;                          // items are two matrices side by side (then e, buf count twos)
     int bn, nt_x, mt_x, mt_s, nt_s;    // tile width (64, 128 or 256); tiles of r x c and m x m outputs
     int tiles[3];                      // items of a matrix's stage, by kind
     int n_stages, n_groups, group_max; // stages of a matrix; groups of matrices; their largest size
@@ -461,7 +462,7 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
     int k = p.m, cols = p.m;
     if (it.kind == NS_APPLY) {
         const int i = it.tile / p.nt_x;
-        t.m0 = i * NS_BM;
+        t.m0 = i * (p.twin ? NS_HALF : NS_BM);
         t.n0 = (it.tile - i * p.nt_x) * p.bn;
         cols = p.c;
         t.mirror = t.same = false;
@@ -495,8 +496,8 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
     // A tile on the diagonal: rows and columns of a CTA coincide.  One that the matrix's end trims is
     // computed 256 wide all the same (the products are bound by L2, not by the tensor cores).
     t.terms = it.kind == NS_GRAM ? 1 : p.terms;
-    if (it.kind != NS_APPLY) t.same = t.n0 == t.m0 && p.bn == NS_BM && t.terms == 1;
-    t.mma_n = t.same ? NS_BM : t.bn;
+    if (it.kind != NS_APPLY) t.same = t.n0 == t.m0 && (p.bn == NS_BM || p.twin) && t.terms == 1;
+    t.mma_n = t.same ? NS_BM : p.twin ? 2 * t.bn : t.bn;
     t.num_kb = (k + NS_BK - 1) / NS_BK;
     return t;
 }
@@ -504,6 +505,12 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn_major, bool b_mn_major) {
     return (1u << 4) | (static_cast<uint32_t>(a_mn_major) << 15) | (static_cast<uint32_t>(b_mn_major) << 16) |
            ((static_cast<uint32_t>(N) >> 3) << 17) | ((static_cast<uint32_t>(M) >> 4) << 24);
+}
+
+// A CTA's matrix or slot, given an item's; its first row in a tile.
+__device__ __forceinline__ int ns_own(const NsArgs& p, int z, uint32_t rank) { return p.twin ? 2 * z + (int)rank : z; }
+__device__ __forceinline__ int ns_row(const NsArgs& p, const NsTile& t, uint32_t rank) {
+    return t.m0 + (p.twin ? 0 : (int)rank * NS_HALF);
 }
 
 struct NsSmem {
@@ -551,9 +558,10 @@ __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abo
                          : it.prev >= 0 && !ns_wait(p, it.prev, p.need[p.n_stages], abort_flag, SITE_NS_WAIT_BUFFER))
             return;
         fence_proxy_async_all();   // the inputs were written by ordinary stores
-        const int nbox = t.same ? 0 : (t.bn / 2 + 63) / 64;
+        const int nbox = t.same ? 0 : ((p.twin ? t.bn : t.bn / 2) + 63) / 64;
         const uint32_t bytes = 2u * (uint32_t)(2 + nbox) * NS_BOX;
-        const int mm = t.m0 + (int)sm.rank * NS_HALF, nn = t.n0 + (int)sm.rank * (t.bn / 2);
+        const int mm = ns_row(p, t, sm.rank), nn = t.n0 + (p.twin ? 0 : (int)sm.rank * (t.bn / 2));
+        const int za = ns_own(p, t.za, sm.rank), zb = ns_own(p, t.zb, sm.rank);   // (past the last: zeros)
         for (int term = 0; term < t.terms; ++term) {
             const CUtensorMap *ma = t.a[term == 2], *mb = t.b[term == 1];   // hi hi, hi lo, lo hi
             for (int kb = 0; kb < t.num_kb; ++kb) {
@@ -567,10 +575,10 @@ __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abo
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
                     tma_load_3d_pair(dst + j * NS_BOX, ma, bar, t.a_mn ? mm + 64 * j : kk, t.a_mn ? kk : mm + 64 * j,
-                                     t.za);
+                                     za);
                 for (int j = 0; j < nbox; ++j)
                     tma_load_3d_pair(dst + (2 + j) * NS_BOX, mb, bar, t.b_mn ? nn + 64 * j : kk,
-                                     t.b_mn ? kk : nn + 64 * j, t.zb);
+                                     t.b_mn ? kk : nn + 64 * j, zb);
                 if (++s == sm.stages) {
                     s = 0;
                     ph ^= 1u;
@@ -673,7 +681,8 @@ __device__ void ns_inputs(const NsArgs& p, const NsSmem& sm, volatile int* abort
         const NsTile t = ns_tile(p, it);
         const int mode = ns_mode(p, it), src = ns_src(it.step);
         const bool lo = mode >= NS_M_X ? p.lo_coef[it.step] != 0.f : mode == NS_M_POLY && p.terms == 3;
-        const int row = t.m0 + (int)sm.rank * NS_HALF, z = mode >= NS_M_X && src == 0 ? it.e : it.buf;
+        const int row = ns_row(p, t, sm.rank), e = ns_own(p, it.e, sm.rank);
+        const int z = mode >= NS_M_X && src == 0 ? e : ns_own(p, it.buf, sm.rank);
         const CUtensorMap* mh = mode >= NS_M_X ? &p.tX[src][0] : &p.tA[0];
         const CUtensorMap* ml = mode >= NS_M_X ? &p.tX[src][1] : &p.tA[1];
         if (mode != NS_M_GRAM) {
@@ -688,9 +697,9 @@ __device__ void ns_inputs(const NsArgs& p, const NsSmem& sm, volatile int* abort
             const uint32_t bar = sm.in + 8 * s, at = sm.slots + s * NS_SLOT_BYTES;
             if (mode == NS_M_W) {   // the weights on their way to L2, blocks ahead of their use
                 for (int c = c0 == 0 ? 0 : c0 + 128; c < (c0 == 0 ? min(t.bn, 192) : min(t.bn, c0 + 192)); c += 64)
-                    if (t.n0 + c < p.c) {
-                        tma_prefetch_3d(&p.tW, t.n0 + c, row, it.e);
-                        tma_prefetch_3d(&p.tW, t.n0 + c, row + 64, it.e);
+                    if (t.n0 + c < p.c && e < p.N) {
+                        tma_prefetch_3d(&p.tW, t.n0 + c, row, e);
+                        tma_prefetch_3d(&p.tW, t.n0 + c, row + 64, e);
                     }
             }
             if (mode == NS_M_GRAM) {
@@ -721,14 +730,14 @@ __device__ void ns_outputs(const NsArgs& p, const NsSmem& sm, volatile int* abor
     for (int id = sm.pair; id < p.total; id += sm.npairs) {
         const NsItem it = ns_item(p, w, id);
         const NsTile t = ns_tile(p, it);
-        const int mode = ns_mode(p, it), row = t.m0 + (int)sm.rank * NS_HALF;
+        const int mode = ns_mode(p, it), row = ns_row(p, t, sm.rank), e = ns_own(p, it.e, sm.rank);
         const int rows = mode >= NS_M_X ? p.r : p.m, cols = mode >= NS_M_X ? p.c : p.m;
         const bool to_b = mode == NS_M_POLY || (mode == NS_M_GRAM && p.coef[3 * it.step + 2] == 0.f);
         const bool lo = mode == NS_M_X ? p.lo_coef[it.step + 1] != 0.f : mode < NS_M_X && p.terms == 3;
-        const int dst = ns_dst(it.step), z = mode == NS_M_O ? it.e : it.buf;
+        const int dst = ns_dst(it.step), z = mode == NS_M_O ? e : ns_own(p, it.buf, sm.rank);
         const CUtensorMap* mh = mode == NS_M_O ? &p.tO : mode == NS_M_X ? &p.tX[dst][0] : to_b ? &p.tB[0] : &p.tA[0];
         const CUtensorMap* ml = mode == NS_M_X ? &p.tX[dst][1] : to_b ? &p.tB[1] : &p.tA[1];
-        const bool store = mode != NS_M_W && (mode != NS_M_O || p.vec_o);
+        const bool store = mode != NS_M_W && (mode != NS_M_O || (p.vec_o && e < p.N));
         for (int c0 = 0; c0 < t.bn; c0 += 64) {
             if (!mbar_wait(sm.done + 8 * s, ph, p.limit_ns, abort_flag)) {
                 ns_abort(abort_flag, p.status, SITE_NS_WAIT_SLOT, -id);
@@ -904,15 +913,18 @@ __device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, vo
     bool live = true;
     NsWalk w = ns_walk_start(p);
     for (int id = sm.pair; id < p.total; id += sm.npairs, ++n) {
-        const NsItem it = ns_item(p, w, id);
+        NsItem it = ns_item(p, w, id);
         const NsTile t = ns_tile(p, it);
-        const int mode = ns_mode(p, it), acc = n & 1;
+        const int mode = ns_mode(p, it), acc = n & 1, rank = p.twin ? 0 : (int)sm.rank;
+        it.e = ns_own(p, it.e, sm.rank);
+        const bool real = it.e < p.N;   // (an odd stack's last item has one matrix)
         if (!mbar_wait(sm.tfull + 8 * acc, (uint32_t)(n >> 1) & 1u, p.limit_ns, abort_flag)) {
             ns_abort(abort_flag, p.status, SITE_NS_WAIT_TFULL, id);
             live = false;
         }
         tc_fence_after();
-        const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * NS_MAXBN;
+        const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * NS_MAXBN +
+                               (p.twin ? sm.rank * (uint32_t)(t.mma_n / 2) : 0u);
         const uint32_t tempty = peer_addr(sm.tempty, 0) + 8 * acc;
 #pragma unroll 1
         for (int c0 = 0; c0 < t.bn; c0 += 64) {
@@ -924,9 +936,9 @@ __device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, vo
                 const int q = threadIdx.x & 15, col = t.n0 + c0 + 4 * q;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int gr = t.m0 + (int)sm.rank * NS_HALF + (int)(threadIdx.x >> 4) + 16 * i;
+                    const int gr = t.m0 + rank * NS_HALF + (int)(threadIdx.x >> 4) + 16 * i;
                     wv[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (4 * q < t.bn - c0 && col + 4 <= p.c && gr < p.r)
+                    if (real && 4 * q < t.bn - c0 && col + 4 <= p.c && gr < p.r)
                         wv[i] = *reinterpret_cast<const float4*>(p.W + it.e * p.st_w + gr * p.ld_w + col);
                 }
             }
@@ -940,11 +952,11 @@ __device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, vo
                 __syncwarp();
                 if (lane == 0) mbar_arrive_remote(tempty);
             }
-            if (mode == NS_M_GRAM) ns_block<NS_M_GRAM>(p, it, t, slot, row, half, (int)sm.rank, c0, live, v, wv);
-            else if (mode == NS_M_POLY) ns_block<NS_M_POLY>(p, it, t, slot, row, half, (int)sm.rank, c0, live, v, wv);
-            else if (mode == NS_M_X) ns_block<NS_M_X>(p, it, t, slot, row, half, (int)sm.rank, c0, live, v, wv);
-            else if (mode == NS_M_O) ns_block<NS_M_O>(p, it, t, slot, row, half, (int)sm.rank, c0, live, v, wv);
-            else ns_block<NS_M_W>(p, it, t, slot, row, half, (int)sm.rank, c0, live, v, wv);
+            if (mode == NS_M_GRAM) ns_block<NS_M_GRAM>(p, it, t, slot, row, half, rank, c0, live && real, v, wv);
+            else if (mode == NS_M_POLY) ns_block<NS_M_POLY>(p, it, t, slot, row, half, rank, c0, live && real, v, wv);
+            else if (mode == NS_M_X) ns_block<NS_M_X>(p, it, t, slot, row, half, rank, c0, live && real, v, wv);
+            else if (mode == NS_M_O) ns_block<NS_M_O>(p, it, t, slot, row, half, rank, c0, live && real, v, wv);
+            else ns_block<NS_M_W>(p, it, t, slot, row, half, rank, c0, live && real, v, wv);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(sm.done + 8 * s);
@@ -976,8 +988,9 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     sm.in = sm.drain + 8;
     sm.done = sm.in + 8 * NS_SLOTS;
     sm.free_ = sm.done + 8 * NS_SLOTS;
-    sm.stage_bytes = (p.bn == NS_MAXBN ? 4 : 3) * NS_BOX;
-    sm.stages = p.bn == NS_MAXBN ? 4 : NS_RING_MAX;
+    const bool four = p.bn == NS_MAXBN || p.twin;
+    sm.stage_bytes = (four ? 4 : 3) * NS_BOX;
+    sm.stages = four ? 4 : NS_RING_MAX;
     sm.rank = cluster_rank();
     sm.pair = blockIdx.x >> 1;
     sm.npairs = gridDim.x >> 1;
@@ -1453,10 +1466,17 @@ inline size_t up256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 // whole forms one group: with two, its schedule is one stage longer and its tiles wait as much
 // (16 x 768 x 768 212 us instead of 224, 13 x 1889 x 354 263 instead of 297).
 constexpr int64_t NS_UNDER_WAY_BYTES = 384ll << 20;
+// Stacks of at least so many wide matrices of m <= 128 go through the tiles two by two, a CTA of the
+// pair for each: rows 0 .. 127 of a tile and the first half of its columns belong to the one, the
+// rest to the other (what the MMA forms of one's rows and the other's columns is not read).  One by
+// one, every tile left a CTA without rows: 147 of 90 x 770 390 us instead of 266, 128 of 128 x 2048 574
+// instead of 471.  Tall matrices fill both CTAs in the apply stage and lose (64 of 2048 x 100 345 us
+// instead of 365 two by two), as do squares (64 of 128 x 128 100 and 109).
+constexpr int NS_TWIN_MIN = 64;
 
 struct NsLayout {
     size_t prog, part, x0h, x0l, xh0, xh1, xl0, xl1, A, Al, B, Bl, total;
-    int chunk, chunks, groups, n_groups, group_max, slots, terms;
+    int chunk, chunks, groups, n_groups, group_max, slots, terms, twin, units;
 };
 NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     NsLayout L;
@@ -1467,13 +1487,16 @@ NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     L.chunks = (L.groups + L.chunk - 1) / L.chunk;
     L.terms = m <= 128 ? 3 : 1;
     const int64_t each = (L.terms == 3 ? 8 : 6) * r * ldx + (L.terms == 3 ? 8 : 4) * m * ldm;
-    int64_t most = NS_UNDER_WAY_BYTES / (each * NS_LANES);   // matrices of a group
+    L.twin = m > NS_THIN && m <= NS_HALF && r < c && N >= NS_TWIN_MIN;
+    const int64_t units = L.twin ? (N + 1) / 2 : N;          // what items are made of
+    L.units = (int)units;
+    int64_t most = NS_UNDER_WAY_BYTES / (each * (L.twin ? 2 : 1) * NS_LANES);   // units of a group
     if (most < 1) most = 1;
-    const int64_t rounds = (N + most * NS_LANES - 1) / (most * NS_LANES);
-    L.n_groups = (int)(rounds * NS_LANES < N ? rounds * NS_LANES : N);   // sizes then differ by one at most
+    const int64_t rounds = (units + most * NS_LANES - 1) / (most * NS_LANES);
+    L.n_groups = (int)(rounds * NS_LANES < units ? rounds * NS_LANES : units);   // sizes then differ by one at most
     if (rounds <= 1) L.n_groups = 1;
-    L.group_max = (int)((N + L.n_groups - 1) / L.n_groups);
-    L.slots = L.group_max * (L.n_groups < NS_LANES ? L.n_groups : NS_LANES);
+    L.group_max = (int)((units + L.n_groups - 1) / L.n_groups);
+    L.slots = L.group_max * (L.n_groups < NS_LANES ? L.n_groups : NS_LANES) * (L.twin ? 2 : 1);
     size_t o = up256(sizeof(DevStatus));
     auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -1697,11 +1720,13 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     if (!ok) return cudaErrorInvalidValue;
     // 256-column tiles, narrower ones where the matrices under way have fewer than there are pairs
     a.mt_s = (a.m + NS_BM - 1) / NS_BM;
-    a.mt_x = (a.r + NS_BM - 1) / NS_BM;
-    for (a.bn = NS_MAXBN;; a.bn /= 2) {
+    a.twin = L.twin;
+    const int rows = a.twin ? NS_HALF : NS_BM;
+    a.mt_x = (a.r + rows - 1) / rows;
+    for (a.bn = a.twin ? NS_HALF : NS_MAXBN;; a.bn /= 2) {
         a.nt_s = (a.m + a.bn - 1) / a.bn;
         a.nt_x = (a.c + a.bn - 1) / a.bn;
-        if (a.bn == 64 || L.slots * a.mt_x * a.nt_x >= sms / 2) break;
+        if (a.twin || a.bn == 64 || L.slots * a.mt_x * a.nt_x >= sms / 2) break;
     }
     int sym = 0;
     for (int i = 0; i < a.mt_s; ++i) sym += a.nt_s - i * (NS_BM / a.bn);
@@ -1713,13 +1738,13 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
         items += a.tiles[a.kind[i]];
     }
     a.need[a.n_stages] = (int)items * NS_DONE;
-    items *= a.N;
+    items *= L.units;
     if (items >= (int64_t(1) << 31) - 65536) return cudaErrorInvalidValue;
     a.total = (int)items;
     a.n_groups = L.n_groups;
     a.group_max = L.group_max;
-    a.base_size = a.N / L.n_groups;
-    a.big_groups = a.N % L.n_groups;
+    a.base_size = L.units / L.n_groups;
+    a.big_groups = L.units % L.n_groups;
     static bool attr_set[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);

@@ -286,3 +286,42 @@ def test_orthogonalize_narrow(N, r, c, rank):
     assert torch.equal(_run(U), O)
     cubic = (1.5, -0.5, 0.0)
     _check(_run(U, steps=2, coef=cubic), U, [cubic] * 2)
+
+
+@pytest.mark.parametrize("N,r,c", [(65, 100, 300), (71, 300, 90), (101, 128, 520), (64, 128, 128), (67, 97, 1000),
+                                   (90, 641, 66)])
+def test_orthogonalize_stacks_of_narrow_matrices(N, r, c):
+    """Stacks whose matrices go through the tiles two by two: odd and even ones, wide and tall;
+    rows that are not 16 bytes apart."""
+    g = torch.Generator(device="cuda").manual_seed(N + r + c)
+    U = torch.randn(N, r, c, generator=g, device="cuda")
+    U[3] = 0.0
+    U[N - 1] *= 1e-20
+    O = _run(U)
+    _check(O, U, [COEF] * 5)
+    out = torch.full((N, r + 1, c + 3), 7.0, dtype=torch.bfloat16, device="cuda")
+    assert torch.equal(_run(U, out=out[:, :r, 1:c + 1]), O)
+    out[:, :r, 1:c + 1] = 7.0
+    assert torch.all(out == 7.0)
+
+
+@pytest.mark.parametrize("N,r,c", [(67, 96, 200), (65, 200, 72)])
+def test_muon_update_of_stacks_of_narrow_matrices(N, r, c):
+    g = torch.Generator(device="cuda").manual_seed(N + r + c)
+
+    def rows(std, dtype=torch.float32):
+        return moevie.moevie_pad_rows((torch.randn(N, r, c, generator=g, device="cuda") * std).to(dtype))
+    W, M, G = rows(r ** -0.5), rows(1e-3), rows(1e-3)
+    Wb = moevie.moevie_pad_rows(W.to(torch.bfloat16))
+    lr, mu, scale = 0.01, 0.9, 0.2 * max(r, c) ** 0.5
+    w, m, gr = _f64(W), _f64(M), _f64(G)
+    ws = moevie.OrthoWorkspace(N, r, c)
+    moevie.moevie_muon_update(W, M, G, ws, lr=lr, momentum=mu, W_bf16=Wb)
+    check_status(ws)
+    m = mu * m + gr
+    O = _stack64(gr + mu * m, [COEF] * 5)
+    w = w - lr * scale * O
+    for e in (0, 1, N - 2, N - 1):
+        err = np.linalg.norm(_f64(W)[e] - w[e])
+        assert err <= lr * scale * REL * np.linalg.norm(O[e]) + 8 * 2.0 ** -24 * np.linalg.norm(w[e]), (e, err)
+    assert torch.equal(Wb, W.to(torch.bfloat16))
