@@ -343,7 +343,6 @@ struct NsArgs {
     __half *xh[3], *xl[3];             // X0 [N][r][ldx]; X, ping-pong [slots][r][ldx] (lo in place with one term)
     __half *A[2], *B[2];               // hi, lo (lo with three terms only) [slots][m][ldm]
     int N, r, c, m, ldx, ldm, tall, terms;
-    int twin;                          // items are two matrices side by side (then e, buf count twos)
     int bn, nt_x, mt_x, mt_s, nt_s;    // tile width (64, 128 or 256); tiles of r x c and m x m outputs
     int tiles[3];                      // items of a matrix's stage, by kind
     int n_stages, n_groups, group_max; // stages of a matrix; groups of matrices; their largest size
@@ -439,6 +438,7 @@ __device__ __forceinline__ NsItem ns_item(const NsArgs& p, NsWalk& w, int id) {
 __device__ __forceinline__ int ns_src(int s) { return s == 0 ? 0 : 2 - (s & 1); }
 __device__ __forceinline__ int ns_dst(int s) { return 1 + (s & 1); }
 
+// TWIN below: items are two matrices side by side, a CTA for each; their e and buf then count twos.
 struct NsTile {
     int m0, n0, bn, num_kb;            // num_kb: K blocks of one term
     int mma_n;                         // columns that are computed
@@ -456,13 +456,14 @@ struct NsTile {
 //   r >  c:  Gram  X^T X both MN-major;  apply X B: both K-major (B is symmetric)
 // Symmetric outputs: row tile i has the column tiles from the diagonal on; those past its own
 // columns are mirrored.
+template <bool TWIN>
 __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
     NsTile t;
     const int src = ns_src(it.step);
     int k = p.m, cols = p.m;
     if (it.kind == NS_APPLY) {
         const int i = it.tile / p.nt_x;
-        t.m0 = i * (p.twin ? NS_HALF : NS_BM);
+        t.m0 = i * (TWIN ? NS_HALF : NS_BM);
         t.n0 = (it.tile - i * p.nt_x) * p.bn;
         cols = p.c;
         t.mirror = t.same = false;
@@ -496,8 +497,8 @@ __device__ __forceinline__ NsTile ns_tile(const NsArgs& p, const NsItem& it) {
     // A tile on the diagonal: rows and columns of a CTA coincide.  One that the matrix's end trims is
     // computed 256 wide all the same (the products are bound by L2, not by the tensor cores).
     t.terms = it.kind == NS_GRAM ? 1 : p.terms;
-    if (it.kind != NS_APPLY) t.same = t.n0 == t.m0 && (p.bn == NS_BM || p.twin) && t.terms == 1;
-    t.mma_n = t.same ? NS_BM : p.twin ? 2 * t.bn : t.bn;
+    if (it.kind != NS_APPLY) t.same = t.n0 == t.m0 && (p.bn == NS_BM || TWIN) && t.terms == 1;
+    t.mma_n = t.same ? NS_BM : TWIN ? 2 * t.bn : t.bn;
     t.num_kb = (k + NS_BK - 1) / NS_BK;
     return t;
 }
@@ -508,9 +509,11 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn_maj
 }
 
 // A CTA's matrix or slot, given an item's; its first row in a tile.
-__device__ __forceinline__ int ns_own(const NsArgs& p, int z, uint32_t rank) { return p.twin ? 2 * z + (int)rank : z; }
+template <bool TWIN>
+__device__ __forceinline__ int ns_own(const NsArgs& p, int z, uint32_t rank) { return TWIN ? 2 * z + (int)rank : z; }
+template <bool TWIN>
 __device__ __forceinline__ int ns_row(const NsArgs& p, const NsTile& t, uint32_t rank) {
-    return t.m0 + (p.twin ? 0 : (int)rank * NS_HALF);
+    return t.m0 + (TWIN ? 0 : (int)rank * NS_HALF);
 }
 
 struct NsSmem {
@@ -545,6 +548,7 @@ __device__ __forceinline__ bool ns_wait(const NsArgs& p, int e, int want, volati
 
 // TMA producer (one thread per CTA): the CTA's 128 rows of A and its half of B's columns; the
 // leader posts the byte count of both CTAs on its full barrier.
+template <bool TWIN>
 __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abort_flag) {
     const uint32_t full_leader = peer_addr(sm.full, 0);
     int s = 0;
@@ -552,16 +556,16 @@ __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abo
     NsWalk w = ns_walk_start(p);
     for (int id = sm.pair; id < p.total; id += sm.npairs) {
         const NsItem it = ns_item(p, w, id);
-        const NsTile t = ns_tile(p, it);
+        const NsTile t = ns_tile<TWIN>(p, it);
         // the matrix's earlier stages; before its first, the last user of its buffers
         if (it.stage > 0 ? !ns_wait(p, it.e, p.need[it.stage], abort_flag, SITE_NS_WAIT_INPUT)
                          : it.prev >= 0 && !ns_wait(p, it.prev, p.need[p.n_stages], abort_flag, SITE_NS_WAIT_BUFFER))
             return;
         fence_proxy_async_all();   // the inputs were written by ordinary stores
-        const int nbox = t.same ? 0 : ((p.twin ? t.bn : t.bn / 2) + 63) / 64;
+        const int nbox = t.same ? 0 : ((TWIN ? t.bn : t.bn / 2) + 63) / 64;
         const uint32_t bytes = 2u * (uint32_t)(2 + nbox) * NS_BOX;
-        const int mm = ns_row(p, t, sm.rank), nn = t.n0 + (p.twin ? 0 : (int)sm.rank * (t.bn / 2));
-        const int za = ns_own(p, t.za, sm.rank), zb = ns_own(p, t.zb, sm.rank);   // (past the last: zeros)
+        const int mm = ns_row<TWIN>(p, t, sm.rank), nn = t.n0 + (TWIN ? 0 : (int)sm.rank * (t.bn / 2));
+        const int za = ns_own<TWIN>(p, t.za, sm.rank), zb = ns_own<TWIN>(p, t.zb, sm.rank);   // (past the last: zeros)
         for (int term = 0; term < t.terms; ++term) {
             const CUtensorMap *ma = t.a[term == 2], *mb = t.b[term == 1];   // hi hi, hi lo, lo hi
             for (int kb = 0; kb < t.num_kb; ++kb) {
@@ -589,6 +593,7 @@ __device__ void ns_producer(const NsArgs& p, const NsSmem& sm, volatile int* abo
 }
 
 // MMA issuer: one thread of the leader CTA.
+template <bool TWIN>
 __device__ __forceinline__ void ns_mma(const NsArgs& p, const NsSmem& sm, uint32_t tmem, volatile int* abort_flag) {
     int s = 0, n = 0;
     uint32_t ph = 0;
@@ -596,7 +601,7 @@ __device__ __forceinline__ void ns_mma(const NsArgs& p, const NsSmem& sm, uint32
     NsWalk w = ns_walk_start(p);
     for (int id = sm.pair; id < p.total; id += sm.npairs) {
         const NsItem it = ns_item(p, w, id);
-        const NsTile t = ns_tile(p, it);
+        const NsTile t = ns_tile<TWIN>(p, it);
         const uint32_t idesc = idesc_f16_f32(NS_BM, t.mma_n, t.a_mn, t.b_mn);
         const uint64_t ad0 = smem_desc_sw128(sm.ring, t.a_mn ? NS_BOX : 16, 1024);
         const uint64_t bd0 = smem_desc_sw128(sm.ring + (t.same ? 0 : 2 * NS_BOX), t.b_mn ? NS_BOX : 16, 1024);
@@ -672,17 +677,18 @@ __device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* tm, int c0, i
 
 // What the epilogue reads of A (polynomial) or X (apply), block by block into its slots: one
 // thread.  Gram blocks read nothing; their slots are handed on as they become free.
+template <bool TWIN>
 __device__ void ns_inputs(const NsArgs& p, const NsSmem& sm, volatile int* abort_flag) {
     int s = 0;
     uint32_t ph = 0;
     NsWalk w = ns_walk_start(p);
     for (int id = sm.pair; id < p.total; id += sm.npairs) {
         const NsItem it = ns_item(p, w, id);
-        const NsTile t = ns_tile(p, it);
+        const NsTile t = ns_tile<TWIN>(p, it);
         const int mode = ns_mode(p, it), src = ns_src(it.step);
         const bool lo = mode >= NS_M_X ? p.lo_coef[it.step] != 0.f : mode == NS_M_POLY && p.terms == 3;
-        const int row = ns_row(p, t, sm.rank), e = ns_own(p, it.e, sm.rank);
-        const int z = mode >= NS_M_X && src == 0 ? e : ns_own(p, it.buf, sm.rank);
+        const int row = ns_row<TWIN>(p, t, sm.rank), e = ns_own<TWIN>(p, it.e, sm.rank);
+        const int z = mode >= NS_M_X && src == 0 ? e : ns_own<TWIN>(p, it.buf, sm.rank);
         const CUtensorMap* mh = mode >= NS_M_X ? &p.tX[src][0] : &p.tA[0];
         const CUtensorMap* ml = mode >= NS_M_X ? &p.tX[src][1] : &p.tA[1];
         if (mode != NS_M_GRAM) {
@@ -723,18 +729,19 @@ __device__ void ns_inputs(const NsArgs& p, const NsSmem& sm, volatile int* abort
 
 // Stores the epilogue's finished blocks, hands their slots back and counts finished tiles: one
 // thread.
+template <bool TWIN>
 __device__ void ns_outputs(const NsArgs& p, const NsSmem& sm, volatile int* abort_flag) {
     int s = 0;
     uint32_t ph = 0;
     NsWalk w = ns_walk_start(p);
     for (int id = sm.pair; id < p.total; id += sm.npairs) {
         const NsItem it = ns_item(p, w, id);
-        const NsTile t = ns_tile(p, it);
-        const int mode = ns_mode(p, it), row = ns_row(p, t, sm.rank), e = ns_own(p, it.e, sm.rank);
+        const NsTile t = ns_tile<TWIN>(p, it);
+        const int mode = ns_mode(p, it), row = ns_row<TWIN>(p, t, sm.rank), e = ns_own<TWIN>(p, it.e, sm.rank);
         const int rows = mode >= NS_M_X ? p.r : p.m, cols = mode >= NS_M_X ? p.c : p.m;
         const bool to_b = mode == NS_M_POLY || (mode == NS_M_GRAM && p.coef[3 * it.step + 2] == 0.f);
         const bool lo = mode == NS_M_X ? p.lo_coef[it.step + 1] != 0.f : mode < NS_M_X && p.terms == 3;
-        const int dst = ns_dst(it.step), z = mode == NS_M_O ? e : ns_own(p, it.buf, sm.rank);
+        const int dst = ns_dst(it.step), z = mode == NS_M_O ? e : ns_own<TWIN>(p, it.buf, sm.rank);
         const CUtensorMap* mh = mode == NS_M_O ? &p.tO : mode == NS_M_X ? &p.tX[dst][0] : to_b ? &p.tB[0] : &p.tA[0];
         const CUtensorMap* ml = mode == NS_M_X ? &p.tX[dst][1] : to_b ? &p.tB[1] : &p.tA[1];
         const bool store = mode != NS_M_W && (mode != NS_M_O || (p.vec_o && e < p.N));
@@ -905,6 +912,7 @@ __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, cons
 // barrier per block, they all waited for each other's latencies).  A wait that gives up is recorded
 // and the warp goes on without writing results: some modes meet at barriers within a block, which
 // every warp must reach.
+template <bool TWIN>
 __device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, volatile int* abort_flag) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
@@ -914,9 +922,9 @@ __device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, vo
     NsWalk w = ns_walk_start(p);
     for (int id = sm.pair; id < p.total; id += sm.npairs, ++n) {
         NsItem it = ns_item(p, w, id);
-        const NsTile t = ns_tile(p, it);
-        const int mode = ns_mode(p, it), acc = n & 1, rank = p.twin ? 0 : (int)sm.rank;
-        it.e = ns_own(p, it.e, sm.rank);
+        const NsTile t = ns_tile<TWIN>(p, it);
+        const int mode = ns_mode(p, it), acc = n & 1, rank = TWIN ? 0 : (int)sm.rank;
+        it.e = ns_own<TWIN>(p, it.e, sm.rank);
         const bool real = it.e < p.N;   // (an odd stack's last item has one matrix)
         if (!mbar_wait(sm.tfull + 8 * acc, (uint32_t)(n >> 1) & 1u, p.limit_ns, abort_flag)) {
             ns_abort(abort_flag, p.status, SITE_NS_WAIT_TFULL, id);
@@ -924,7 +932,7 @@ __device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, vo
         }
         tc_fence_after();
         const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * NS_MAXBN +
-                               (p.twin ? sm.rank * (uint32_t)(t.mma_n / 2) : 0u);
+                               (TWIN ? sm.rank * (uint32_t)(t.mma_n / 2) : 0u);
         const uint32_t tempty = peer_addr(sm.tempty, 0) + 8 * acc;
 #pragma unroll 1
         for (int c0 = 0; c0 < t.bn; c0 += 64) {
@@ -968,6 +976,7 @@ __device__ void ns_epilogue(const NsArgs& p, const NsSmem& sm, uint32_t tmem, vo
     }
 }
 
+template <bool TWIN>
 __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant__ NsArgs p) {
     extern __shared__ uint8_t ns_smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ns_smem_raw) + 1023) &
@@ -988,7 +997,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     sm.in = sm.drain + 8;
     sm.done = sm.in + 8 * NS_SLOTS;
     sm.free_ = sm.done + 8 * NS_SLOTS;
-    const bool four = p.bn == NS_MAXBN || p.twin;
+    const bool four = p.bn == NS_MAXBN || TWIN;
     sm.stage_bytes = (four ? 4 : 3) * NS_BOX;
     sm.stages = four ? 4 : NS_RING_MAX;
     sm.rank = cluster_rank();
@@ -1024,15 +1033,15 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     pdl_wait();
     const uint32_t tmem = *tmem_slot;
     if (warp < NS_EPI_WARPS) {
-        ns_epilogue(p, sm, tmem, abort_flag);
+        ns_epilogue<TWIN>(p, sm, tmem, abort_flag);
     } else if (warp == NS_WARP_LOAD) {
-        if (elect_one()) ns_producer(p, sm, abort_flag);
+        if (elect_one()) ns_producer<TWIN>(p, sm, abort_flag);
     } else if (warp == NS_WARP_MMA) {
-        if (sm.rank == 0 && elect_one()) ns_mma(p, sm, tmem, abort_flag);
+        if (sm.rank == 0 && elect_one()) ns_mma<TWIN>(p, sm, tmem, abort_flag);
     } else if (warp == NS_WARP_IN) {
-        if (elect_one()) ns_inputs(p, sm, abort_flag);
+        if (elect_one()) ns_inputs<TWIN>(p, sm, abort_flag);
     } else if (warp == NS_WARP_OUT) {
-        if (elect_one()) ns_outputs(p, sm, abort_flag);
+        if (elect_one()) ns_outputs<TWIN>(p, sm, abort_flag);
     }
     __syncwarp();
     tc_fence_before();
@@ -1720,13 +1729,12 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     if (!ok) return cudaErrorInvalidValue;
     // 256-column tiles, narrower ones where the matrices under way have fewer than there are pairs
     a.mt_s = (a.m + NS_BM - 1) / NS_BM;
-    a.twin = L.twin;
-    const int rows = a.twin ? NS_HALF : NS_BM;
+    const int rows = L.twin ? NS_HALF : NS_BM;
     a.mt_x = (a.r + rows - 1) / rows;
-    for (a.bn = a.twin ? NS_HALF : NS_MAXBN;; a.bn /= 2) {
+    for (a.bn = L.twin ? NS_HALF : NS_MAXBN;; a.bn /= 2) {
         a.nt_s = (a.m + a.bn - 1) / a.bn;
         a.nt_x = (a.c + a.bn - 1) / a.bn;
-        if (a.twin || a.bn == 64 || L.slots * a.mt_x * a.nt_x >= sms / 2) break;
+        if (L.twin || a.bn == 64 || L.slots * a.mt_x * a.nt_x >= sms / 2) break;
     }
     int sym = 0;
     for (int i = 0; i < a.mt_s; ++i) sym += a.nt_s - i * (NS_BM / a.bn);
@@ -1749,7 +1757,8 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev >= 0 && dev < 64 && !attr_set[dev]) {
-        e = cudaFuncSetAttribute(ns_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM);
+        e = cudaFuncSetAttribute(ns_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM);
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
@@ -1770,7 +1779,7 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     at[2].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 3;
-    e = cudaLaunchKernelEx(&cfg, ns_kernel, a);
+    e = cudaLaunchKernelEx(&cfg, L.twin ? ns_kernel<true> : ns_kernel<false>, a);
     count_launches(1);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
