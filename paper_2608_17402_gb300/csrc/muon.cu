@@ -663,6 +663,12 @@ __device__ __forceinline__ int ns_mode(const NsArgs& p, const NsItem& it) {
     return it.step < p.steps - 1 ? NS_M_X : p.O ? NS_M_O : NS_M_W;
 }
 
+// Whether a tile stores lo parts: those of X are read by the next step's a X term (unless it counts
+// them 0 times) and, with three terms, by its products whatever a is.
+__device__ __forceinline__ bool ns_lo_out(const NsArgs& p, int mode, int step) {
+    return mode <= NS_M_X && (p.terms == 3 || (mode == NS_M_X && p.lo_coef[step + 1] != 0.f));
+}
+
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(tm),
                  "r"(c0), "r"(c1), "r"(c2), "r"(src)
@@ -740,7 +746,7 @@ __device__ void ns_outputs(const NsArgs& p, const NsSmem& sm, volatile int* abor
         const int mode = ns_mode(p, it), row = ns_row<TWIN>(p, t, sm.rank), e = ns_own<TWIN>(p, it.e, sm.rank);
         const int rows = mode >= NS_M_X ? p.r : p.m, cols = mode >= NS_M_X ? p.c : p.m;
         const bool to_b = mode == NS_M_POLY || (mode == NS_M_GRAM && p.coef[3 * it.step + 2] == 0.f);
-        const bool lo = mode == NS_M_X ? p.lo_coef[it.step + 1] != 0.f : mode < NS_M_X && p.terms == 3;
+        const bool lo = ns_lo_out(p, mode, it.step);
         const int dst = ns_dst(it.step), z = mode == NS_M_O ? e : ns_own<TWIN>(p, it.buf, sm.rank);
         const CUtensorMap* mh = mode == NS_M_O ? &p.tO : mode == NS_M_X ? &p.tX[dst][0] : to_b ? &p.tB[0] : &p.tA[0];
         const CUtensorMap* ml = mode == NS_M_X ? &p.tX[dst][1] : to_b ? &p.tB[1] : &p.tA[1];
@@ -799,7 +805,7 @@ __device__ __forceinline__ void ns_block(const NsArgs& p, const NsItem& it, cons
     const float fd = MODE == NS_M_GRAM ? (cc == 0.f ? cb * NS_INV_S : NS_INV_S) : MODE == NS_M_POLY ? cc * NS_INV_S : NS_INV_S;
     const float fh = APPLY ? p.coef[3 * it.step] : cb, fl = APPLY ? p.lo_coef[it.step] : cb;
     const bool lo_in = APPLY ? fl != 0.f : p.terms == 3;
-    const bool lo_out = MODE == NS_M_X ? p.lo_coef[it.step + 1] != 0.f : p.terms == 3;
+    const bool lo_out = ns_lo_out(p, MODE, it.step);
     float keep[MODE == NS_M_W ? 32 : 1];
     uint4 hin[4], lin[4];   // all inputs before the first output (in place: no load passes a store)
     if (MODE != NS_M_GRAM) {

@@ -1,0 +1,31 @@
+"""moevie_orthogonalize and moevie_muon_update where their coefficients, sizes or stacks are
+unusual, against the formulas evaluated in 64 bits.  Tolerances are those of
+test_gpu_muon.py unless a test derives its own."""
+import pytest
+import torch
+
+from paper_2608_17402_gb300 import moevie
+from tests._gpu import check_status
+from tests.test_gpu_muon import COEF, _check
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("N,r,c", [(101, 128, 520), (71, 300, 90), (2, 200, 300)])
+def test_steps_without_a_linear_term(N, r, c):
+    """A step with a = 0 takes nothing of X but its products, whose lower parts still count: a
+    middle and a last step of that kind, on a workspace that held NaN before it was set up.
+
+    Tolerance: a cubic step has the relative error of one Gram product (two roundings of X,
+    2 x 2.8e-4) and passes on three times that of its input; the quintic before it has 5.6e-4,
+    the one after it adds as much: 2.8e-3 at the most, 3.3e-3 with the rounding to bf16."""
+    g = torch.Generator(device="cuda").manual_seed(N + r)
+    U = torch.randn(N, r, c, generator=g, device="cuda")
+    cubic = (0.0, 2.5, -1.5)
+    for coefs in ([COEF, cubic, COEF], [COEF, cubic]):
+        ws = moevie.OrthoWorkspace(N, r, c)
+        ws.buf.fill_(255)   # NaN in every floating-point format
+        moevie.moevie_workspace_init(ws)
+        O = moevie.moevie_orthogonalize(U, ws, coef=coefs, steps=len(coefs))
+        check_status(ws)
+        _check(O, U, coefs)
