@@ -324,8 +324,11 @@ moevie_status moevie_moe_few(const moevie_layer* layer, const void* x, int64_t T
  * the result is within 2e-3 (2-norm) of the formula's, before its rounding to bf16.
  * (Matrices of which one side is at most 32, and few matrices of which one is at most 128:
  * fp32 throughout.)
- * coef: HOST memory, steps x 3 floats, finite; 1 <= steps <= 32.  Sizes: rows and cols in
- * [1, 8192], 0 <= N <= 65535, else MOEVIE_ERR_UNSUPPORTED; N == 0 launches nothing.  ws:
+ * coef: HOST memory, steps x 3 floats, finite; 1 <= steps <= 32.  For matrices whose smaller
+ * side is above 32, all steps from singular values in [0, 1] on must keep those of X (but the
+ * last), of A and of b A + c A^2 at 60 or below, as fp16 holds them (the usual quintics stay
+ * below 10), else MOEVIE_ERR_UNSUPPORTED.  Sizes: rows and cols in [1, 8192],
+ * 0 <= N <= 65535, else MOEVIE_ERR_UNSUPPORTED; N == 0 launches nothing.  ws:
  * moevie_orthogonalize_workspace_size bytes, set up with moevie_workspace_init. */
 moevie_status moevie_orthogonalize_workspace_size(int64_t N, int64_t rows, int64_t cols, size_t* bytes);
 moevie_status moevie_orthogonalize(const void* U, int u_bf16, int64_t ld_u, int64_t stride_u, int64_t N,

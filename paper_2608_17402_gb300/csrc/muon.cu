@@ -32,9 +32,10 @@
 //
 // Working format.  X is held as hi + lo, two fp16 values (22 significant bits), times 2^10; A and B
 // as fp16 times 2^10.  The tensor cores multiply the hi parts (fp16 has three bits more than bf16
-// at the same rate, and every entry of X, A and B is bounded by a few units, so its range
-// suffices), accumulate in fp32, and the a X term is added from hi and lo in fp32.  That term is
-// what keeps the directions in which U is (nearly) singular clean: each step multiplies them by
+// at the same rate; its range suffices as no entry exceeds the largest singular value, which the
+// caller's coefficients must keep at 60 or below), accumulate in fp32, and the a X term is added from
+// hi and lo in fp32.  That term is what keeps the directions in which U is (nearly) singular clean:
+// each step multiplies them by
 // a = 3.4, so a rounding of X there would grow by a^steps, several hundred times, while B X is
 // small there to begin with.  Against 64 bits the result is within 2e-3 (2-norm over 2-norm) for
 // full-rank and for low-rank U alike; with X rounded to fp16 alone it would be 4e-2 for a U of
@@ -66,8 +67,7 @@ namespace mv {
 
 namespace {
 
-constexpr float NS_S = 1024.0f;           // scale of X, A, B in the working format
-constexpr float NS_INV_S = 1.0f / 1024.0f;
+constexpr float NS_INV_S = 1.0f / NS_S;
 
 // ----------------------------------------------------- element loads (prologue)
 
@@ -1072,7 +1072,6 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
 // parts of A are added in CTA order over distributed shared memory, and every CTA iterates for
 // itself.  Bound by latency (loads of a chunk 3 us, the iteration 8 us): 32 x 2048 27 us, a stack of 256
 // of them 155 us (with one CTA a matrix and scalar products 335 and 504).
-constexpr int NS_THIN = 32;
 constexpr int NS_THIN_THREADS = 256;
 constexpr int NS_THIN_K = 128;
 constexpr int NS_THIN_LD = NS_THIN + 4;

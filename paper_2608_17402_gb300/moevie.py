@@ -517,7 +517,9 @@ def _stack(t, dtypes, name):
 
 def moevie_orthogonalize(U, ws: OrthoWorkspace, coef=NS_COEF, steps=5, out=None, stream=None):
     """Newton-Schulz orthogonalisation of U [N, rows, cols] (or one matrix [rows, cols]), fp32
-    or bf16, each matrix by itself; returns bf16 of U's shape (``out`` when given)."""
+    or bf16, each matrix by itself; returns bf16 of U's shape (``out`` when given).  ``coef``: one
+    (a, b, c), or one per step; above 32 rows and columns they must keep singular values of
+    [0, 1] within what fp16 holds (moevie.h)."""
     N, r, c, ld, st = _stack(U, (torch.float32, torch.bfloat16), "U")
     O = out if out is not None else torch.empty(U.shape, dtype=torch.bfloat16, device=U.device)
     if O.shape != U.shape:

@@ -6,7 +6,7 @@ import torch
 
 from paper_2608_17402_gb300 import moevie
 from tests._gpu import check_status
-from tests.test_gpu_muon import COEF, _check
+from tests.test_gpu_muon import COEF, _check, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +29,18 @@ def test_steps_without_a_linear_term(N, r, c):
         O = moevie.moevie_orthogonalize(U, ws, coef=coefs, steps=len(coefs))
         check_status(ws)
         _check(O, U, coefs)
+
+
+def test_entries_near_the_end_of_16_bits():
+    """Coefficients under which X reaches 7, A 49 and b A + c A^2 48.5, on matrices whose largest
+    singular value is that of a single entry."""
+    coefs = [(7.0, 0.0, 0.0), (1.0, 0.5, 0.01)]
+    U = torch.zeros(3, 200, 260, device="cuda")
+    U[0, 7, 11] = -3.0
+    U[1, 199, 259] = 1e-3
+    U[2, 0, 0], U[2, 130, 140] = 1.0, 1e-4
+    _check(_run(U, steps=2, coef=coefs), U, coefs)
+    _check(_run(U[:, :, :20], steps=2, coef=(100.0, 0.0, 0.0)), U[:, :, :20], [(100.0, 0.0, 0.0)] * 2)
+    with pytest.raises(moevie.MoevieError) as e:
+        _run(U, steps=2, coef=(100.0, 0.0, 0.0))
+    assert e.value.code == 2
