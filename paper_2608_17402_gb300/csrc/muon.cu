@@ -39,10 +39,11 @@
 // a = 3.4, so a rounding of X there would grow by a^steps, several hundred times, while B X is
 // small there to begin with.  Against 64 bits the result is within 2e-3 (2-norm over 2-norm) for
 // full-rank and for low-rank U alike; with X rounded to fp16 alone it would be 4e-2 for a U of
-// rank 16.  In the last two steps, whose roundings are hardly amplified any more, lo counts 2 and 0
-// times instead of a: where singular values have arrived near 1, B lo (which is not formed) takes
-// up most of a lo, and leaving both out is nearer (1.6e-3 becomes 1.4e-3 on Gaussian matrices) and
-// saves the last step's lo.
+// rank 16.  In the last two steps lo counts 2 and 0 times instead of a, where neither step's a exceeds
+// NS_LO_MAX: where singular values have arrived near 1, B lo (which is not formed) takes up most of
+// a lo, and leaving both out is nearer (1.6e-3 becomes 1.4e-3 on Gaussian matrices) and saves the
+// last step's lo.  The price is a 2e-4 of |X| in the null directions of U: 1.5e-3 instead of 3e-4 for
+// rank 1 with a = 3.4, but 8e-3 with a = 20 and a result of half X (1.5e-3 with all of lo).
 // For m <= 128 the roundings of a few singular values average less, and time is latency: there (in
 // stacks that are not left to ns_small_kernel) A and B have lo parts too, and the polynomial and the
 // apply product are hi hi + hi lo + lo hi.  The Gram product, whose K is the long side, stays hi hi:
@@ -327,6 +328,7 @@ constexpr int NS_BARS = 2 * NS_RING_MAX + 5 + 3 * NS_SLOTS;
 constexpr int NS_SMEM = NS_RING_BYTES + NS_SLOTS * NS_SLOT_BYTES + 1024 + 256;
 static_assert(NS_SMEM <= 232448 && NS_BARS * 8 + 8 <= 256, "shared memory of one CTA");
 
+constexpr float NS_LO_MAX = 3.5f;     // largest a of the last two steps at which lo may count less
 constexpr int NS_LANES = 2;           // groups of matrices under way, a stage apart (three: 256 x 416 x 1664
                                       // 2.38 ms instead of 2.33)
 constexpr int NS_MAX_STAGES = 3 * NS_MAX_STEPS;
@@ -1671,8 +1673,9 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     for (int it = 0; it < q.steps; ++it) {
         for (int j = 0; j < 3; ++j) a.coef[3 * it + j] = q.coef[3 * it + j];
         // lo in the last two steps: see the file comment
-        const float ca = a.coef[3 * it], lim = it == q.steps - 1 ? 0.0f : 2.0f;
-        a.lo_coef[it] = a.terms == 3 || it < q.steps - 2 || it == 0 || fabsf(ca) <= lim ? ca : copysignf(lim, ca);
+        const float ca = q.coef[3 * it], last = fabsf(q.coef[3 * (q.steps - 1)]), lim = it == q.steps - 1 ? 0.0f : 2.0f;
+        const bool less = a.terms == 1 && it >= q.steps - 2 && it > 0 && fabsf(ca) <= NS_LO_MAX && last <= NS_LO_MAX;
+        a.lo_coef[it] = less && fabsf(ca) > lim ? copysignf(lim, ca) : ca;
         for (int kind = NS_GRAM; kind <= NS_APPLY; ++kind) {
             if (kind == NS_POLY && a.coef[3 * it + 2] == 0.f) continue;
             a.kind[stage] = (uint8_t)kind;

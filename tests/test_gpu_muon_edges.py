@@ -44,3 +44,21 @@ def test_entries_near_the_end_of_16_bits():
     with pytest.raises(moevie.MoevieError) as e:
         _run(U, steps=2, coef=(100.0, 0.0, 0.0))
     assert e.value.code == 2
+
+
+@pytest.mark.parametrize("N,r,c", [(2, 300, 520), (1, 520, 300)])
+def test_last_steps_with_a_large_linear_term(N, r, c):
+    """What a step makes of X's lower part in the null directions of U is a times as large as
+    it was: with a = 20 and a result of half X, 8e-3 of the result if it is left out.
+
+    Tolerance: X of rank 1 has entries u_i v_j.  Rounding A's, B's and X's by relative 2.8e-4
+    (rms) turns the product of B = -19.5 u u^T and X by 2.8e-4 x 19.5 sqrt(3 / m) each, as the
+    errors average over m entries: 5.5e-4 for m = 300, 9.5e-4 in quadrature, 1.9e-3 of the
+    result.  With the rounding to bf16, 1.7e-3, in quadrature: 2.6e-3."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    U = torch.randn(N, r, 1, generator=g, device="cuda") @ torch.randn(N, 1, c, generator=g, device="cuda")
+    for coefs in ([(1.5, -0.5, 0.0), (20.0, -38.75, 19.25)],):
+        _check(_run(U, steps=2, coef=coefs), U, coefs)
+    # one step before the last: its null directions reach the end through a quintic step
+    coefs = [(1.5, -0.5, 0.0), (20.0, -38.5, 19.5), (1.5, -0.5, 0.0)]
+    _check(_run(U, steps=3, coef=coefs), U, coefs)
