@@ -37,8 +37,10 @@
 // hi and lo in fp32.  That term is what keeps the directions in which U is (nearly) singular clean:
 // each step multiplies them by
 // a = 3.4, so a rounding of X there would grow by a^steps, several hundred times, while B X is
-// small there to begin with.  Against 64 bits the result is within 2e-3 (2-norm over 2-norm) for
-// full-rank and for low-rank U alike; with X rounded to fp16 alone it would be 4e-2 for a U of
+// small there to begin with.  Against 64 bits the result (default quintic, five steps) is within 2e-3
+// (2-norm over 2-norm) for full-rank and for low-rank U alike, as roundings average over the entries;
+// where a few entries hold all of U they do not, and a singular value may be off by 2e-2 (the header
+// says what to expect of other coefficients).  With X rounded to fp16 alone it would be 4e-2 for a U of
 // rank 16.  In the last two steps lo counts 2 and 0 times instead of a, where neither step's a exceeds
 // NS_LO_MAX: where singular values have arrived near 1, B lo (which is not formed) takes up most of
 // a lo, and leaving both out is nearer (1.6e-3 becomes 1.4e-3 on Gaussian matrices) and saves the

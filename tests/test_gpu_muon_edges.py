@@ -1,12 +1,13 @@
 """moevie_orthogonalize and moevie_muon_update where their coefficients, sizes or stacks are
 unusual, against the formulas evaluated in 64 bits.  Tolerances are those of
 test_gpu_muon.py unless a test derives its own."""
+import numpy as np
 import pytest
 import torch
 
 from paper_2608_17402_gb300 import moevie
 from tests._gpu import check_status
-from tests.test_gpu_muon import COEF, _check, _run
+from tests.test_gpu_muon import COEF, _check, _f64, _ns64, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +63,37 @@ def test_last_steps_with_a_large_linear_term(N, r, c):
     # one step before the last: its null directions reach the end through a quintic step
     coefs = [(1.5, -0.5, 0.0), (20.0, -38.5, 19.5), (1.5, -0.5, 0.0)]
     _check(_run(U, steps=3, coef=coefs), U, coefs)
+
+
+def test_matrices_of_a_few_entries():
+    """Matrices with at most one entry in a row and a column: every entry is a singular value by
+    itself, and no rounding averages.
+
+    Tolerance, entry by entry, with u = 2^-11 the largest relative rounding of an fp16 operand:
+    A = x^2 is off by 3u (X twice, its own rounding) and A^2 by 6u, B = b A + c A^2 is rounded
+    again and meets a rounded X; in the last two steps up to |a| - 2 and |a| of X's lower part
+    are left out; and each step passes on |p'(x)| times the error of its input.  Second-order
+    terms: a fifth more per step.  At the end half an ulp of bf16, 2^-9."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    N, r, c = 60, 150, 260
+    U = torch.zeros(N, r, c, device="cuda")
+    for e in range(N):
+        k = 1 + e % 6
+        i = torch.randperm(r, generator=g, device="cuda")[:k]
+        j = torch.randperm(c, generator=g, device="cuda")[:k]
+        U[e, i, j] = torch.randn(k, generator=g, device="cuda")
+    O = _f64(_run(U))
+    u = 2.0 ** -11
+    for got, mat in zip(O, _f64(U)):
+        want = _ns64(mat, [COEF] * 5)
+        assert np.all(got[mat == 0] == 0)
+        for q in zip(*np.nonzero(mat)):
+            x, err = abs(mat[q]) / np.linalg.norm(mat), 2.0 ** -22
+            for it in range(5):
+                a, b, cc = COEF
+                t = x * x
+                B, p, slope = b * t + cc * t * t, abs(x * (a + b * t + cc * t * t)), abs(a + 3 * b * t + 5 * cc * t * t)
+                drop = a if it == 4 else a - 2 if it == 3 else 0.0
+                err = 1.2 * x * (slope * err + u * (3 * abs(b) * t + 6 * cc * t * t + 2 * abs(B) + drop)) / p
+                x = p
+            assert abs(got[q] - want[q]) <= (err + 2.0 ** -9) * abs(want[q]), (got[q], want[q], err)
