@@ -1496,6 +1496,26 @@ struct NsLayout {
     size_t prog, part, x0h, x0l, xh0, xh1, xl0, xl1, A, Al, B, Bl, total;
     int chunk, chunks, groups, n_groups, group_max, slots, terms, twin, units;
 };
+int ns_terms(int64_t m) { return m <= 128 ? 3 : 1; }
+// Whether stacks of N matrices go through the tiles two by two.
+bool ns_twin(int64_t N, int64_t r, int64_t c) { return r > NS_THIN && r <= NS_HALF && r < c && N >= NS_TWIN_MIN; }
+// Units (matrices, or twos) of a group at most.
+int64_t ns_group_most(int64_t r, int64_t c, bool twin) {
+    const int64_t m = r < c ? r : c, x = r * up8(c), a = m * up8(m);
+    const int64_t each = ns_terms(m) == 3 ? 8 * x + 8 * a : 6 * x + 4 * a, most = NS_UNDER_WAY_BYTES / (each * (twin ? 2 : 1) * NS_LANES);
+    return most > 1 ? most : 1;
+}
+// Matrices under way at most in any stack of up to N: all of a stack that fits in one round, which
+// more matrices, as they take more rounds of even size, fall short of.
+int64_t ns_most_slots(int64_t N, int64_t r, int64_t c) {
+    auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
+    if (!ns_twin(N, r, c)) return least(N, ns_group_most(r, c, false) * NS_LANES);
+    const int64_t single = least(NS_TWIN_MIN - 1, ns_group_most(r, c, false) * NS_LANES);
+    const int64_t twos = 2 * least((N + 1) / 2, ns_group_most(r, c, true) * NS_LANES);
+    return single > twos ? single : twos;
+}
+
+// The schedule's groups and the places of the buffers in the workspace; total: for any stack of up to N.
 NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     NsLayout L;
     const int64_t m = r < c ? r : c, ldx = up8(c), ldm = up8(m);
@@ -1503,18 +1523,17 @@ NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     L.chunk = (L.groups + NS_PRO_CHUNKS - 1) / NS_PRO_CHUNKS;
     if (L.chunk < NS_PRO_GROUPS) L.chunk = NS_PRO_GROUPS;
     L.chunks = (L.groups + L.chunk - 1) / L.chunk;
-    L.terms = m <= 128 ? 3 : 1;
-    const int64_t each = (L.terms == 3 ? 8 : 6) * r * ldx + (L.terms == 3 ? 8 : 4) * m * ldm;
-    L.twin = m > NS_THIN && m <= NS_HALF && r < c && N >= NS_TWIN_MIN;
+    L.terms = ns_terms(m);
+    L.twin = ns_twin(N, r, c);
     const int64_t units = L.twin ? (N + 1) / 2 : N;          // what items are made of
     L.units = (int)units;
-    int64_t most = NS_UNDER_WAY_BYTES / (each * (L.twin ? 2 : 1) * NS_LANES);   // units of a group
-    if (most < 1) most = 1;
+    const int64_t most = ns_group_most(r, c, L.twin);
     const int64_t rounds = (units + most * NS_LANES - 1) / (most * NS_LANES);
     L.n_groups = (int)(rounds * NS_LANES < units ? rounds * NS_LANES : units);   // sizes then differ by one at most
     if (rounds <= 1) L.n_groups = 1;
     L.group_max = (int)((units + L.n_groups - 1) / L.n_groups);
     L.slots = L.group_max * (L.n_groups < NS_LANES ? L.n_groups : NS_LANES) * (L.twin ? 2 : 1);
+    const size_t room = (size_t)ns_most_slots(N, r, c);      // at least `slots`
     size_t o = up256(sizeof(DevStatus));
     auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -1523,7 +1542,7 @@ NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     };
     L.prog = take((size_t)N * 4);
     L.part = take((size_t)N * L.chunks * 3 * sizeof(float));
-    const size_t x = (size_t)L.slots * r * ldx * 2, a = (size_t)L.slots * m * ldm * 2;
+    const size_t x = room * r * ldx * 2, a = room * m * ldm * 2;
     const bool thin = m <= NS_THIN;
     L.x0h = take(thin ? 0 : (size_t)N * r * ldx * 2);
     L.x0l = take(thin ? 0 : (size_t)N * r * ldx * 2);
@@ -1552,24 +1571,8 @@ cudaError_t launch_prologue(const UpdateArgs& p, int N, bool thin, __half* xh, _
 
 }  // namespace
 
-// Monotone in N: a larger stack may have smaller groups under way, so the sizes of all smaller
-// stacks' buffers are bounded by those of one full set of groups.
-size_t ns_workspace_bytes(int64_t N, int64_t r, int64_t c) {
-    const NsLayout L = ns_layout(N, r, c);
-    size_t most = L.total;
-    const int64_t m = r < c ? r : c, ldx = up8(c), ldm = up8(m);
-    const int64_t each = (L.terms == 3 ? 8 : 6) * r * ldx + (L.terms == 3 ? 8 : 4) * m * ldm;
-    int64_t full = NS_UNDER_WAY_BYTES / (each * NS_LANES);
-    if (full < 1) full = 1;
-    full = full * NS_LANES < N ? full * NS_LANES : N;
-    if (full > 0) {
-        const NsLayout F = ns_layout(full, r, c);
-        const size_t per = 4 + (size_t)L.chunks * 3 * sizeof(float) + (m <= NS_THIN ? 0 : 4 * (size_t)r * ldx);
-        const size_t v = F.total + (size_t)(N - full) * per + 1024;
-        if (v > most) most = v;
-    }
-    return most;
-}
+// Monotone in N, as each buffer's size is.
+size_t ns_workspace_bytes(int64_t N, int64_t r, int64_t c) { return ns_layout(N, r, c).total; }
 
 namespace {
 // Launch attributes of a kernel with a cluster per matrix.

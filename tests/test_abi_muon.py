@@ -61,3 +61,18 @@ def test_coefficients_have_to_fit_16_bits(lib, coefs):
         want = 3 if fits else 2
         assert _codes(lib, coefs, rows, cols, N) == (want, want), (rows, cols)
     assert _codes(lib, coefs, 32, 4000) == _codes(lib, coefs, 4000, 7) == (3, 3)
+
+
+@pytest.mark.parametrize("r,c,Ns", [
+    (128, 2560, range(1, 400)), (128, 5760, range(1, 200)), (100, 1000, range(1, 1000)), (126, 1316, range(230, 560)),
+    (100, 1024, range(400, 480)), (33, 40, range(1, 300)), (416, 1664, range(1, 300)), (1664, 416, range(1, 300)),
+    (2560, 128, range(1, 400)), (16, 2048, range(1, 300)), (8192, 8192, range(0, 40)), (129, 300, range(1, 700)),
+    (64, 64, range(1, 2000)), (128, 8192, range(50, 200)), (100, 520, list(range(62, 68)) + [65534, 65535])])
+def test_workspace_of_a_larger_stack_serves_smaller_ones(lib, r, c, Ns):
+    """Stacks of up to N matrices fit a workspace for N."""
+    out = ctypes.c_size_t(0)
+    prev = 0
+    for N in Ns:
+        assert lib.moevie_orthogonalize_workspace_size(N, r, c, ctypes.byref(out)) == 0
+        assert out.value >= prev, N
+        prev = out.value

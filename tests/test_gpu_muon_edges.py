@@ -97,3 +97,15 @@ def test_matrices_of_a_few_entries():
                 err = 1.2 * x * (slope * err + u * (3 * abs(b) * t + 6 * cc * t * t + 2 * abs(B) + drop)) / p
                 x = p
             assert abs(got[q] - want[q]) <= (err + 2.0 ** -9) * abs(want[q]), (got[q], want[q], err)
+
+
+def test_workspace_of_a_larger_stack():
+    """A stack that is under way as a whole, in the workspace of one that goes in rounds."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    U = torch.randn(144, 128, 2560, generator=g, device="cuda")
+    ws = moevie.OrthoWorkspace(145, 128, 2560)
+    O = moevie.moevie_orthogonalize(U, ws)
+    check_status(ws)
+    assert torch.equal(O, _run(U))
+    for e in (0, 1, 142, 143):
+        _check(O[e:e + 1], U[e:e + 1], [COEF] * 5)
