@@ -341,7 +341,8 @@ moevie_status moevie_moe_few(const moevie_layer* layer, const void* x, int64_t T
  * side is above 32, all steps from singular values in [0, 1] on must keep those of X (but the
  * last), of A and of b A + c A^2 at 60 or below, as fp16 holds them (the usual quintics stay
  * below 10), else MOEVIE_ERR_UNSUPPORTED.  Sizes: rows and cols in [1, 8192],
- * 0 <= N <= 65535, else MOEVIE_ERR_UNSUPPORTED; N == 0 launches nothing.  ws:
+ * 0 <= N <= 65535, matrix strides below 2^38, else MOEVIE_ERR_UNSUPPORTED; N == 0 launches
+ * nothing.  ws:
  * moevie_orthogonalize_workspace_size bytes, set up with moevie_workspace_init. */
 moevie_status moevie_orthogonalize_workspace_size(int64_t N, int64_t rows, int64_t cols, size_t* bytes);
 moevie_status moevie_orthogonalize(const void* U, int u_bf16, int64_t ld_u, int64_t stride_u, int64_t N,
@@ -357,7 +358,9 @@ moevie_status moevie_orthogonalize(const void* U, int u_bf16, int64_t ld_u, int6
  * >= cols) and matrix stride `stride` (a multiple of 8, >= rows ld), 16-byte aligned: the
  * layout of W1 and of dW1.  Pad columns are neither read nor written.  A zero U (an expert
  * that got no token, without momentum) only decays its weights.  Workspace, coef, steps and
- * sizes as for moevie_orthogonalize. */
+ * sizes as for moevie_orthogonalize.  Where a status other than MOEVIE_OK is returned for these
+ * reasons, M and W are as they were; after a timeout on the device (moevie_get_device_status)
+ * they are undefined. */
 moevie_status moevie_muon_update(float* W, void* W_bf16, float* M, const float* G, int64_t N, int64_t rows,
                                  int64_t cols, int64_t ld, int64_t stride, float lr, float momentum,
                                  int nesterov, float weight_decay, float scale, const float* coef, int steps,

@@ -1085,6 +1085,7 @@ moevie_status moevie_orthogonalize(const void* U, int u_bf16, int64_t ld_u, int6
     if (ld_u < cols || ld_o < cols || ld_u >= (int64_t(1) << 31) || ld_o >= (int64_t(1) << 31))
         return MOEVIE_ERR_INVALID_ARG;
     if (N > 1 && (stride_u < 0 || stride_o < (rows - 1) * ld_o + cols)) return MOEVIE_ERR_INVALID_ARG;
+    if (N > 1 && (stride_u >= NS_MAX_STRIDE || stride_o >= NS_MAX_STRIDE)) return MOEVIE_ERR_UNSUPPORTED;
     if (ws_bytes < ns_workspace_bytes(N, rows, cols)) return MOEVIE_ERR_WORKSPACE;
     NsCall q = {};
     q.N = (int)N;
@@ -1117,7 +1118,7 @@ moevie_status moevie_muon_update(float* W, void* W_bf16, float* M, const float* 
     if (!W || !M || !G || !ws) return MOEVIE_ERR_INVALID_ARG;
     if (!a16(W) || !a16(W_bf16) || !a16(M) || !a16(G) || !a16(ws)) return MOEVIE_ERR_INVALID_ARG;
     if (ld < cols || ld >= (int64_t(1) << 31) || (N > 1 && stride < rows * ld)) return MOEVIE_ERR_INVALID_ARG;
-    if (ld % 8 != 0 || (N > 1 && stride % 8 != 0)) return MOEVIE_ERR_UNSUPPORTED;
+    if (ld % 8 != 0 || (N > 1 && (stride % 8 != 0 || stride >= NS_MAX_STRIDE))) return MOEVIE_ERR_UNSUPPORTED;
     if (ws_bytes < ns_workspace_bytes(N, rows, cols)) return MOEVIE_ERR_WORKSPACE;
     NsCall q = {};
     q.N = (int)N;

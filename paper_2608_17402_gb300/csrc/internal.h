@@ -392,6 +392,7 @@ cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaS
 
 constexpr int64_t NS_MAX_DIM = 8192;    // rows and columns of a matrix
 constexpr int64_t NS_MAX_COUNT = 65535; // matrices of a stack
+constexpr int64_t NS_MAX_STRIDE = int64_t(1) << 38;   // elements; a tensor map's strides end at 2^40 bytes
 constexpr int NS_MAX_STEPS = 32;
 constexpr int NS_THIN = 32;             // matrices of up to so many rows or columns: fp32 throughout
 constexpr float NS_S = 1024.0f;         // scale of X, A and b A + c A^2 in fp16

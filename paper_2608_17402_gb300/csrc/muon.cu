@@ -1593,24 +1593,34 @@ struct NsClusterLaunch {
         cfg.numAttrs = 2;
     }
 };
-// Clusters of ns_small_kernel<S> that run at a time on the current device (0: none).
-template <int S>
-int ns_small_clusters() {
-    static std::atomic<int> cache[64];   // count + 1
+// Clusters of `ctas` CTAs of a kernel that run at a time on the current device (0: none), its shared
+// memory attribute set on the way; `cache`: per device, count + 1.
+int clusters_at_once(std::atomic<int> (&cache)[64], void (*kern)(NsArgs), int ctas, int threads, int smem) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-    int n = cache[dev].load(std::memory_order_relaxed) - 1;
+    int n = cache[dev].load(std::memory_order_acquire) - 1;
     if (n >= 0) return n;
     n = 0;
-    NsClusterLaunch l(1, 8, ns_small_smem<S>(), nullptr);
+    NsClusterLaunch l(1, ctas, smem, nullptr);
+    l.cfg.blockDim = dim3((unsigned)threads);
     l.cfg.numAttrs = 1;
-    if (cudaFuncSetAttribute(ns_small_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, ns_small_smem<S>()) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, ns_small_kernel<S>, &l.cfg) != cudaSuccess || n < 0) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kern, &l.cfg) != cudaSuccess || n < 0) {
         cudaGetLastError();
         n = 0;
     }
-    cache[dev].store(n + 1, std::memory_order_relaxed);
+    cache[dev].store(n + 1, std::memory_order_release);
     return n;
+}
+template <int S>
+int ns_small_clusters() {
+    static std::atomic<int> cache[64];
+    return clusters_at_once(cache, ns_small_kernel<S>, 8, NS_THIN_THREADS, ns_small_smem<S>());
+}
+template <bool TWIN>
+int ns_pairs() {
+    static std::atomic<int> cache[64];
+    return clusters_at_once(cache, ns_kernel<TWIN>, 2, NS_THREADS, NS_SMEM);
 }
 // Whether the cluster kernel is the faster one for N matrices m x n: times (us, five steps) of both,
 // fitted to measurements at m of 64, 100 and 128, n of 64 to 2048, N of 1 to 128.  One 64 x 2048: 51
@@ -1664,14 +1674,6 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.xh[0] = reinterpret_cast<__half*>(ws + L.x0h);
     a.xl[0] = reinterpret_cast<__half*>(ws + L.x0l);
     const bool thin = a.m <= NS_THIN, small = !thin && a.m <= 128 && ns_small_pays(a.N, a.m, a.tall ? a.r : a.c, a.tall);
-    cudaError_t e;
-    if (q.u_bf16)
-        e = a.u.vec ? launch_prologue<__nv_bfloat16, true>(a.u, q.N, thin || small, a.xh[0], a.xl[0], s)
-                    : launch_prologue<__nv_bfloat16, false>(a.u, q.N, thin || small, a.xh[0], a.xl[0], s);
-    else
-        e = a.u.vec ? launch_prologue<float, true>(a.u, q.N, thin || small, a.xh[0], a.xl[0], s)
-                    : launch_prologue<float, false>(a.u, q.N, thin || small, a.xh[0], a.xl[0], s);
-    if (e != cudaSuccess) return e;
 
     a.steps = q.steps;
     int stage = 0;
@@ -1700,7 +1702,18 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.rate = q.rate;
     a.status = reinterpret_cast<DevStatus*>(ws);
     a.limit_ns = limit_ns;
+    // The prologue brings M up to date in place, so it is enqueued after all that can fail on the host.
+    auto prologue = [&]() {
+        const bool alone = thin || small;
+        if (q.u_bf16)
+            return a.u.vec ? launch_prologue<__nv_bfloat16, true>(a.u, q.N, alone, a.xh[0], a.xl[0], s)
+                           : launch_prologue<__nv_bfloat16, false>(a.u, q.N, alone, a.xh[0], a.xl[0], s);
+        return a.u.vec ? launch_prologue<float, true>(a.u, q.N, alone, a.xh[0], a.xl[0], s)
+                       : launch_prologue<float, false>(a.u, q.N, alone, a.xh[0], a.xl[0], s);
+    };
+    cudaError_t e;
     if (thin || small) {
+        if ((e = prologue()) != cudaSuccess) return e;
         if (small && a.m <= 64) {
             NsClusterLaunch l(a.N, 8, ns_small_smem<64>(), s);
             e = cudaLaunchKernelEx(&l.cfg, ns_small_kernel<64>, a);
@@ -1766,18 +1779,11 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.group_max = L.group_max;
     a.base_size = L.units / L.n_groups;
     a.big_groups = L.units % L.n_groups;
-    static bool attr_set[64] = {};
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (dev >= 0 && dev < 64 && !attr_set[dev]) {
-        e = cudaFuncSetAttribute(ns_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(ns_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM);
-        if (e != cudaSuccess) return e;
-        attr_set[dev] = true;
-    }
-    const int64_t pairs = items < sms / 2 ? items : sms / 2;
+    const int most = L.twin ? ns_pairs<true>() : ns_pairs<false>();   // co-resident, as they wait on one another
+    if (most <= 0) return cudaErrorCooperativeLaunchTooLarge;
+    const int64_t pairs = items < most ? items : most;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * (pairs < 1 ? 1 : pairs)));
+    cfg.gridDim = dim3((unsigned)(2 * pairs));
     cfg.blockDim = dim3(NS_THREADS);
     cfg.dynamicSmemBytes = NS_SMEM;
     cfg.stream = s;
@@ -1792,6 +1798,7 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     at[2].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 3;
+    if ((e = prologue()) != cudaSuccess) return e;
     e = cudaLaunchKernelEx(&cfg, L.twin ? ns_kernel<true> : ns_kernel<false>, a);
     count_launches(1);
     return e != cudaSuccess ? e : cudaGetLastError();

@@ -76,3 +76,24 @@ def test_workspace_of_a_larger_stack_serves_smaller_ones(lib, r, c, Ns):
         assert lib.moevie_orthogonalize_workspace_size(N, r, c, ctypes.byref(out)) == 0
         assert out.value >= prev, N
         prev = out.value
+
+
+def test_strides_that_no_tensor_map_holds_are_refused_before_the_momentum_moves(lib):
+    """A call that the host refuses has launched nothing, M's update included."""
+    P = ctypes.c_void_p
+    fake, far = P(0x1000), 1 << 38
+    co = (ctypes.c_float * 3)(*QUINTIC)
+    n0 = moevie.moevie_launch_count()
+    for rows, cols in ((64, 96), (200, 304), (8, 8)):
+        def muon(stride, N=2):
+            return lib.moevie_muon_update(fake, fake, fake, fake, N, rows, cols, cols, stride, 0.1, 0.9, 1, 0.0, 1.0, co,
+                                          1, fake, 1 << 40 if stride >= far else 0, None)
+
+        def ortho(su, so):
+            return lib.moevie_orthogonalize(fake, 0, cols, su, 2, rows, cols, co, 1, fake, cols, so, fake,
+                                            1 << 40 if max(su, so) >= far else 0, None)
+        assert muon(far) == muon(1 << 45) == muon(1 << 60) == 2
+        assert ortho(far, rows * cols) == ortho(rows * cols, far) == 2
+        assert muon(far - 8) == ortho(far - 8, far - 8) == 3   # (a workspace of no size)
+        assert muon(1 << 60, N=0) == 0
+    assert moevie.moevie_launch_count() == n0
