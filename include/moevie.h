@@ -302,7 +302,9 @@ moevie_status moevie_moe_backward(const moevie_layer* layer, const void* x, cons
  * y is as precise as 32-bit arithmetic rounded once to bf16.  Each token's y depends on that
  * token alone, and results do not depend on timing.
  * Sizes: those of moevie_moe_forward, k <= 32 and d, h, h_s <= 65535; T == 0 launches nothing.
- * ws: moevie_few_workspace_size(T_max, ...) bytes, set up with moevie_workspace_init. */
+ * ws: moevie_few_workspace_size(T_max, ...) bytes, set up with moevie_workspace_init.  After
+ * MOEVIE_ERR_TIMEOUT in its status set it up again: calls may leave their outputs as they were
+ * until then. */
 #define MOEVIE_FEW_MAX_TOKENS 64
 moevie_status moevie_few_workspace_size(int64_t T_max, int64_t d, int64_t E, int64_t k, int64_t h,
                                         int64_t h_s, size_t* bytes);

@@ -84,28 +84,31 @@ __device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[
         : "memory");
 }
 
+constexpr unsigned long long FEW_BROKEN = 1ull << 63;   // mark of a count
 // Grid barrier on a counter that only grows (64 bits; every launch adds the same multiple of the
 // grid's size): one atomic per CTA and no reset, so its cost is two trips to L2.  Gives up
-// after the time limit (false, recorded).
+// after the time limit (false, recorded).  The count then need not be a multiple of the grid any
+// more, and a later barrier could pass early, so it is marked, and no barrier passes on a marked count:
+// neither in this launch nor in a later one, until the workspace is set up again.
 __device__ bool few_barrier(DevStatus* st, uint64_t limit_ns) {
     __shared__ int s_ok;
     __syncthreads();
     if (threadIdx.x == 0) {
         unsigned long long ticket, now;
         asm volatile("atom.add.acq_rel.gpu.global.u64 %0, [%1], 1;" : "=l"(ticket) : "l"(&st->few_arrivals) : "memory");
-        const unsigned long long want = (ticket / gridDim.x + 1) * gridDim.x;
+        // (a marked ticket waits for nothing)
+        const unsigned long long want = ticket < FEW_BROKEN ? (ticket / gridDim.x + 1) * gridDim.x : 0ull;
         const uint64_t t0 = globaltimer_ns();
-        int ok = 1;
-        for (uint32_t i = 1;; ++i) {
+        now = ticket;
+        for (uint32_t i = 1; now < want; ++i) {
             asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(now) : "l"(&st->few_arrivals) : "memory");
-            if (now >= want) break;
-            if ((i & 63u) == 0u && globaltimer_ns() - t0 > limit_ns) {
-                ok = 0;
+            if ((i & 63u) == 0u && now < want && globaltimer_ns() - t0 > limit_ns) {
+                atomicOr(&st->few_arrivals, FEW_BROKEN);
                 report(st, MOEVIE_ERR_TIMEOUT, SITE_FEW_BARRIER, (int)blockIdx.x, (int)(want - now));
-                break;
+                now = FEW_BROKEN;
             }
         }
-        s_ok = ok;
+        s_ok = now < FEW_BROKEN;
     }
     __syncthreads();
     return s_ok != 0;
