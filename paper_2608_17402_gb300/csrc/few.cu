@@ -947,6 +947,7 @@ __device__ void few_combine(const FewArgs& p, const FewLists& L, const FewPlan& 
                 return;
             }
         }
+        __syncwarp();   // what one lane has acquired, all lanes may read (a vote does not order memory)
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int r0 = 0; r0 < na; r0 += width) {
             const int r = r0 + sub;

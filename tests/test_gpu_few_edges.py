@@ -1,5 +1,6 @@
-"""moevie_moe_few on a workspace whose grid barrier has timed out.  Nothing here faults, traps or
-hangs the GPU: the test sets the mark that a timed-out barrier leaves."""
+"""moevie_moe_few where its CTAs wait on one another: a grid barrier that has timed out, parts that
+are summed as they arrive.  Nothing here faults, traps or
+hangs the GPU: the first test sets the mark that a timed-out barrier leaves."""
 import pytest
 import torch
 
@@ -36,4 +37,21 @@ def test_few_does_not_run_after_a_barrier_timed_out(T):
     moevie.moevie_workspace_init(ws)
     for _ in range(2):
         assert torch.equal(moevie.moevie_moe_few(W, x, ws, y=y), want)
+    check_status(ws)
+
+
+@pytest.mark.parametrize("T", [2, 16, 64])
+def test_few_gives_the_same_bits_every_time(T):
+    """The sum over a token's parts starts as soon as the last of them is counted: a part read too
+    early would be that of the call before, which here ran on other tokens."""
+    lay = workloads.make_layer(workloads.small_config(T=T, d=520, E=24, k=6, h=200, h_s=136, seed=T + 1))
+    x, W = layer_to_device(lay)
+    c = lay.cfg
+    ws = moevie.FewWorkspace(c.T, c.d, c.E, c.k, c.h, c.h_s)
+    other = x.flip(0).neg().contiguous()
+    want, want_other = moevie.moevie_moe_few(W, x, ws), moevie.moevie_moe_few(W, other, ws)
+    got = []
+    for _ in range(40):
+        got.append((moevie.moevie_moe_few(W, x, ws), moevie.moevie_moe_few(W, other, ws)))
+    assert all(torch.equal(a, want) and torch.equal(b, want_other) for a, b in got)
     check_status(ws)
