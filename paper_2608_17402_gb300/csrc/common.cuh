@@ -181,6 +181,19 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint64_
     }
 }
 
+// A CTA whose pipeline gave up may still have copies under way into its shared memory, on barriers
+// whose other arrivals never come, so no barrier says when they have landed.  They take
+// microseconds: before such a CTA (or its pair) ends, a millisecond passes.  Called by one whole
+// warp, after a barrier behind the last copy and before what it ends the CTA (or the pair) with.
+static __device__ __noinline__ void wait_for_copies() {
+    const uint64_t t0 = globaltimer_ns();
+    for (int i = 0; i < 100000 && globaltimer_ns() - t0 < 1000000ull; ++i) __nanosleep(1000);
+    __syncwarp();
+}
+__device__ __forceinline__ void settle_copies(const volatile int* abort_flag) {
+    if (*abort_flag) wait_for_copies();
+}
+
 // ------------------------------------------- publishing data between CTAs
 
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }

@@ -1230,6 +1230,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) few_kernel(const __grid_consta
     tc_fence_before();
     __syncthreads();
     if (warp == FEW_WARP_MMA) {
+        settle_copies(abort_flag);
         tc_fence_after();
         tmem_dealloc(tmem, p.tmem_cols);
     }

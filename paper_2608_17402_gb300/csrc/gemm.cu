@@ -940,6 +940,7 @@ __global__ void __launch_bounds__(GM_THREADS, 1) grouped_gemm_kernel(const __gri
 
     tc_fence_before();
     __syncthreads();
+    if (warp == GM_WARP_MMA) settle_copies(abort_flag);
     cluster_sync();   // the leader's MMAs have drained; both CTAs are done with TMEM
     if (warp == GM_WARP_MMA) {
         tc_fence_after();

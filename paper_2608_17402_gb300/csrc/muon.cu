@@ -1056,6 +1056,7 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (warp == NS_WARP_MMA) settle_copies(abort_flag);
     cluster_sync();   // the leader's MMAs have drained; both CTAs are done with TMEM
     if (warp == NS_WARP_MMA) {
         tc_fence_after();
