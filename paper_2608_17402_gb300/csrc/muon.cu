@@ -356,6 +356,7 @@ struct NsArgs {
     uint8_t kind[NS_MAX_STAGES], step[NS_MAX_STAGES];
     int need[NS_MAX_STAGES + 1];       // counter value at which a stage's inputs are complete
     float coef[3 * NS_MAX_STEPS], lo_coef[NS_MAX_STEPS];   // lo_coef: multiplier of lo in a X
+    float lo_keep[NS_MAX_STEPS];       // nonzero: the step's X is stored with its lo part
     int steps;
     __nv_bfloat16* O;                  // orthogonalised matrices (or NULL)
     int64_t ld_o, st_o;
@@ -667,10 +668,9 @@ __device__ __forceinline__ int ns_mode(const NsArgs& p, const NsItem& it) {
     return it.step < p.steps - 1 ? NS_M_X : p.O ? NS_M_O : NS_M_W;
 }
 
-// Whether a tile stores lo parts: those of X are read by the next step's a X term (unless it counts
-// them 0 times) and, with three terms, by its products whatever a is.
+// Whether a tile stores lo parts.
 __device__ __forceinline__ bool ns_lo_out(const NsArgs& p, int mode, int step) {
-    return mode <= NS_M_X && (p.terms == 3 || (mode == NS_M_X && p.lo_coef[step + 1] != 0.f));
+    return mode == NS_M_X ? p.lo_keep[step] != 0.f : mode < NS_M_X && p.terms == 3;
 }
 
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src, int c0, int c1, int c2) {
@@ -1691,6 +1691,9 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
         }
     }
     a.n_stages = stage;
+    // X's lo part is read by the next step's a X term, unless it counts 0 times there, and, with three
+    // terms, by its products whatever a is.
+    for (int it = 0; it + 1 < q.steps; ++it) a.lo_keep[it] = a.terms == 3 ? 1.0f : a.lo_coef[it + 1];
     a.O = q.O;
     a.ld_o = q.ld_o;
     a.st_o = q.st_o;
