@@ -40,6 +40,8 @@
 // (a selection by unrolled counting took 6 us where this one takes 2).
 #include <math.h>
 
+#include <atomic>
+
 #include "internal.h"
 
 namespace mv {
@@ -1333,13 +1335,13 @@ cudaError_t launch_few(FewArgs a, uint8_t* ws, int sms, uint64_t limit_ns, cudaS
         if (ok && a.W3) ok = make_weight_tmap_strided(&a.tS3, a.Ws3, a.hs, a.d, 1, a.hsp, (int64_t)a.d * a.hsp);
     }
     if (!ok) return cudaErrorInvalidValue;
-    static bool attr_set[64] = {};
+    static std::atomic<bool> attr_set[64];
     int dev = 0;
     cudaGetDevice(&dev);
-    if (dev >= 0 && dev < 64 && !attr_set[dev]) {
+    if (dev >= 0 && dev < 64 && !attr_set[dev].load(std::memory_order_acquire)) {   // idempotent: no lock needed
         const cudaError_t e = cudaFuncSetAttribute(few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM_MAX);
         if (e != cudaSuccess) return e;
-        attr_set[dev] = true;
+        attr_set[dev].store(true, std::memory_order_release);
     }
     const FewSizes z = few_sizes(a.T, a.k, a.E);
     const cudaError_t e = launch_pdl_coop(few_kernel, dim3((unsigned)sms), dim3(FEW_THREADS), z.total, s, a);

@@ -51,6 +51,8 @@
 #include <cudaTypedefs.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "internal.h"
 
 namespace mv {
@@ -949,7 +951,8 @@ __global__ void __launch_bounds__(GM_THREADS, 1) grouped_gemm_kernel(const __gri
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 get_encode_fn() {
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+    static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> found{nullptr};
+    PFN_cuTensorMapEncodeTiled_v12000 fn = found.load(std::memory_order_acquire);
     if (!fn) {
         void* ptr = nullptr;
         cudaDriverEntryPointQueryResult q;
@@ -957,6 +960,7 @@ PFN_cuTensorMapEncodeTiled_v12000 get_encode_fn() {
                                              cudaEnableDefault, &q) == cudaSuccess &&
             q == cudaDriverEntryPointSuccess)
             fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
+        found.store(fn, std::memory_order_release);
     }
     return fn;
 }
@@ -1071,16 +1075,16 @@ cudaError_t launch_grouped_gemm(const GemmArgs& a, int grid, cudaStream_t s) {
     else if (a.epi == EPI_ADD_F32) kern = a.stg_rows == 32 ? kerns[0] : kerns[1];
     else if (a.epi == EPI_STORE_F32 || a.epi == EPI_SUM2_F32) kern = kerns[2];
     else kern = kerns[3];
-    static bool attr_set[64] = {};
+    static std::atomic<bool> attr_set[64];
     int dev = 0;
     cudaGetDevice(&dev);
-    if (dev >= 0 && dev < 64 && !attr_set[dev]) {
+    if (dev >= 0 && dev < 64 && !attr_set[dev].load(std::memory_order_acquire)) {   // idempotent: no lock needed
         for (Kern k : kerns) {
             cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                  GM_SMEM_BYTES_MAX);
             if (e != cudaSuccess) return e;
         }
-        attr_set[dev] = true;
+        attr_set[dev].store(true, std::memory_order_release);
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((grid + 1) & ~1));   // whole pairs
