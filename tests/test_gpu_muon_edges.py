@@ -7,7 +7,7 @@ import torch
 
 from paper_2608_17402_gb300 import moevie
 from tests._gpu import check_status
-from tests.test_gpu_muon import COEF, _check, _f64, _ns64, _run
+from tests.test_gpu_muon import COEF, REL, _check, _f64, _ns64, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -109,3 +109,80 @@ def test_workspace_of_a_larger_stack():
     assert torch.equal(O, _run(U))
     for e in (0, 1, 142, 143):
         _check(O[e:e + 1], U[e:e + 1], [COEF] * 5)
+
+
+# Stacks that go through the schedule in several groups, a stage apart, whose buffers serve one
+# matrix after the other; 256-wide tiles of matrices above 128 rows and columns.  With them, per
+# matrix, whether: groups are of unequal size; a mirrored tile, a tile on the diagonal, one that the
+# matrix's end trims is 256 wide; the last item of a stack that goes two by two has one matrix.
+
+
+def _close_on_gpu(O, U, coefs=(COEF,) * 5):
+    """The check of every matrix, in 64 bits on the GPU."""
+    X = U.double()
+    X = X / torch.linalg.vector_norm(X, dim=(1, 2), keepdim=True)
+    flip = X.shape[1] > X.shape[2]
+    X = X.mT if flip else X
+    for a, b, c in coefs:
+        A = X @ X.mT
+        X = a * X + (b * A + c * (A @ A)) @ X
+    X = X.mT if flip else X
+    assert torch.isfinite(O).all()
+    rel = torch.linalg.vector_norm(O.double() - X, dim=(1, 2)) / torch.linalg.vector_norm(X, dim=(1, 2))
+    assert rel.max().item() <= REL, (int(rel.argmax()), rel.max().item())
+    return X
+
+
+@pytest.mark.parametrize("N,r,c,dtype", [
+    (256, 416, 1664, torch.float32), (251, 416, 1664, torch.bfloat16), (97, 1664, 416, torch.float32),
+    (301, 128, 2048, torch.float32), (90, 700, 850, torch.float32), (3, 2900, 5000, torch.bfloat16)])
+def test_stacks_in_several_groups(N, r, c, dtype):
+    g = torch.Generator(device="cuda").manual_seed(N)
+    U = torch.randn(N, r, c, generator=g, device="cuda").to(dtype)
+    O = _run(U)
+    _close_on_gpu(O, U)
+    assert torch.equal(_run(U), O)
+
+
+@pytest.mark.parametrize("N,r,c", [(40, 300, 520), (20, 768, 768), (31, 1280, 854), (40, 290, 1000), (13, 513, 1100),
+                                   (80, 257, 256), (100, 180, 250)])
+def test_wide_tiles(N, r, c):
+    g = torch.Generator(device="cuda").manual_seed(N)
+    U = torch.randn(N, r, c, generator=g, device="cuda")
+    U[1] = torch.randn(r, 9, generator=g, device="cuda") @ torch.randn(9, c, generator=g, device="cuda")
+    U[2] = 0.0
+    O = _run(U)
+    keep = torch.arange(N, device="cuda") != 2
+    _close_on_gpu(O[keep], U[keep])
+    assert torch.count_nonzero(O[2]) == 0
+
+
+@pytest.mark.parametrize("N,r,c,nesterov", [(131, 416, 1664, True), (130, 1664, 416, False), (301, 128, 2048, True),
+                                            (31, 1280, 854, True)])
+def test_muon_update_of_large_stacks(N, r, c, nesterov):
+    g = torch.Generator(device="cuda").manual_seed(N)
+
+    def rows(std):
+        return moevie.moevie_pad_rows(torch.randn(N, r, c, generator=g, device="cuda") * std)
+    W, M, G = rows(r ** -0.5), rows(1e-3), rows(1e-3)
+    Wb = moevie.moevie_pad_rows(W.to(torch.bfloat16))
+    lr, mu, wd, scale = 0.02, 0.95, 0.1, 0.2 * max(r, c) ** 0.5
+    m = mu * M.double() + G.double()
+    u = G.double() + mu * m if nesterov else m
+    w = (1 - lr * wd) * W.double()
+    ws = moevie.OrthoWorkspace(N, r, c)
+    moevie.moevie_muon_update(W, M, G, ws, lr=lr, momentum=mu, weight_decay=wd, nesterov=nesterov, W_bf16=Wb)
+    check_status(ws)
+    assert (torch.linalg.vector_norm(M.double() - m) <= 4 * 2.0 ** -24 * torch.linalg.vector_norm(m)).item()
+    X = u / torch.linalg.vector_norm(u, dim=(1, 2), keepdim=True)
+    X = X.mT if r > c else X
+    for _ in range(5):
+        A = X @ X.mT
+        X = COEF[0] * X + (COEF[1] * A + COEF[2] * (A @ A)) @ X
+    X = X.mT if r > c else X
+    w = w - lr * scale * X
+    norm = torch.linalg.vector_norm
+    err = norm(W.double() - w, dim=(1, 2))
+    most = lr * scale * REL * norm(X, dim=(1, 2)) + 8 * 2.0 ** -24 * norm(w, dim=(1, 2))
+    assert (err <= most).all(), (err / most).max().item()
+    assert torch.equal(Wb, W.to(torch.bfloat16))
