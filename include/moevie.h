@@ -299,8 +299,9 @@ moevie_status moevie_moe_backward(const moevie_layer* layer, const void* x, cons
  * returned).  The selection is that of exact arithmetic up to the rounding of a 64-bit sum
  * (products of bf16 and fp32 are exact in 64 bits; keys in 64 bits; ties to the lowest id; a
  * key that is NaN comes after every number).  Hidden activations keep more than bf16's bits, so
- * y is as precise as 32-bit arithmetic rounded once to bf16.  Each token's y depends on that
- * token alone, and results do not depend on timing.
+ * y is as precise as 32-bit arithmetic rounded once to bf16.  A token's ids and y do not depend
+ * on the others' values but for the order of sums: how those are split goes by the number of
+ * tokens and by what they select.  The same call gives the same bits.
  * Sizes: those of moevie_moe_forward, k <= 32 and d, h, h_s <= 65535; T == 0 launches nothing.
  * ws: moevie_few_workspace_size(T_max, ...) bytes, set up with moevie_workspace_init.  After
  * MOEVIE_ERR_TIMEOUT in its status set it up again: calls may leave their outputs as they were

@@ -33,9 +33,11 @@
 //
 // What bounds it, measured on one GB300 (against the time of the weights' bytes at the measured
 // copy bandwidth of 6.77 TB/s).  Many tokens: the weights' bytes behind a front of 11 to 15 us; 64
-// tokens, d 1664, 8 slots, 171 of 256 experts of h 416 touched: 91 us, bytes 72.  One token: a chain of dependent steps, each a trip to L2 or HBM (0.7 to
-// 1.5 us): 23 us at d 1536, 8 slots, h 768 (bytes 5.6): 2 launch, 4 logits and barrier, 2 selection,
-// 1.2 plan, 5.5 up, 2.4 activation and hand-over, 2.8 down, 3 sum.  The code before the first weight
+// tokens, d 1664, 8 slots, 171 of 256 experts of h 416 touched: 94 us, bytes 72.  One token: a chain of
+// dependent steps, each a trip to L2 or HBM (0.7 to 1.5 us): 25 us at d 1536, 8 slots, h 768 (bytes
+// 5.6) with the weights in L2 from the call before, 33 with cold ones; of the former about 2 launch, 4
+// logits and barrier, 2 selection, 1.2 plan, 5.5 up, 2.4 activation and hand-over, 2.8 down, 3 sum.
+// The same layer by the batch path takes 54 to 58 and 65 us.  The code before the first weight
 // load is kept short rather than unrolled: run once per call, it is paced by instruction fetches
 // (a selection by unrolled counting took 6 us where this one takes 2).
 #include <math.h>

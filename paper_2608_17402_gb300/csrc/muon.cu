@@ -9,8 +9,9 @@
 //
 // Kernels
 //   muon_moment_kernel  momentum update (M <- mu M + G) and |U|.
-//   muon_scale_kernel   X0 in the working format.  Both are bound by memory (with momentum 16 bytes
-//                       an element: 256 x 416 x 1664 in 610 us, 4.65 TB/s); a cluster per matrix that
+//   muon_scale_kernel   X0 in the working format.  Both are bound by memory: with momentum 20 bytes an
+//                       element (G, M, M back; M again, X0's two parts; with Nesterov G again, 24):
+//                       256 x 1664 x 416 in 610 us, 5.8 TB/s.  A cluster per matrix that
 //                       did both in one launch, its second read from L2, took the same or longer
 //                       (256 x 416 x 1664 without momentum, all steps: 2.39 ms against 2.35).
 //   ns_kernel           the three products of every step on tcgen05 CTA pairs in one persistent
@@ -1282,7 +1283,7 @@ __global__ void __launch_bounds__(NS_THIN_THREADS, 3) ns_thin_kernel(const __gri
 // left factor, so P and A alone are shared, in every CTA's memory.  For few matrices: on the tensor
 // cores the Gram product of one such matrix is a single tile, n / 64 K blocks one after the other,
 // and every step three dependent launches' worth of hand-over.
-// Bound by shared memory and the fp32 units of its 8 SMs: 128 x 2048 in 136 us, of which the 19 products
+// Bound by shared memory and the fp32 units of its 8 SMs: 128 x 2048 in 113 us, of which the 19 products
 // of 128 x 128 are about 80.
 constexpr int NS_SMALL_K = 64;
 template <int S>
