@@ -1251,15 +1251,27 @@ __global__ void __launch_bounds__(NS_THIN_THREADS, 3) ns_thin_kernel(const __gri
             product(A, sq[it2], P);
         }
     }
+    // Q is the product of the steps' P, the last one leftmost: in that order a rounding in one of them is
+    // multiplied by those after it, as in the iteration on X itself.  (In the other order, that of the
+    // transpose, the last P's roundings go through all earlier ones: on X0 of rank 1 the result was off
+    // by 0.8.)  Transposed, so that a row's factors lie side by side.
+    {
+        const float4 v = *at4(sq[iq]);
+        sq[it2][ec][er] = v.x;
+        sq[it2][ec + 1][er] = v.y;
+        sq[it2][ec + 2][er] = v.z;
+        sq[it2][ec + 3][er] = v.w;
+        __syncthreads();
+    }
     // Q X0: 4 rows x 4 columns a thread, through xs to memory order
-    const Square& Q = sq[iq];
+    const Square& QT = sq[it2];
     for (int ch = rank; ch < chunks; ch += C) {
         const int k0 = ch * NS_THIN_K, c4 = (tid & 31) * 4, r4 = (tid >> 5) * 4;
         if (chunks > C) stage(k0);
         float4 o[4] = {};
 #pragma unroll 4
         for (int j = 0; j < m; ++j) {
-            const float4 x = *reinterpret_cast<const float4*>(&xs[j][c4]), q = *reinterpret_cast<const float4*>(&Q[j][r4]);
+            const float4 x = *reinterpret_cast<const float4*>(&xs[j][c4]), q = *reinterpret_cast<const float4*>(&QT[j][r4]);
             const float qs[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int u = 0; u < 4; ++u)

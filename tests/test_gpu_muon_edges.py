@@ -186,3 +186,33 @@ def test_muon_update_of_large_stacks(N, r, c, nesterov):
     most = lr * scale * REL * norm(X, dim=(1, 2)) + 8 * 2.0 ** -24 * norm(w, dim=(1, 2))
     assert (err <= most).all(), (err / most).max().item()
     assert torch.equal(Wb, W.to(torch.bfloat16))
+
+
+# Tolerance of thin matrices of low or nearly low rank: fp32 throughout, so that null directions hold
+# 2^-24 of X, multiplied by a = 3.4445 in every step (3e-5 after five), and within the m x m iteration
+# by a^2; a hundred such roundings are 3e-3, with the rounding to bf16, 1.7e-3, 3.5e-3: REL.
+
+
+@pytest.mark.parametrize("N,r,c,rank", [(16, 25, 95, 1), (5, 8, 53, 1), (3, 114, 16, 1), (1, 30, 35, 3), (36, 312, 4, 1),
+                                        (3, 2, 25, 1), (93, 10, 3, 1), (2, 32, 2048, 4), (19, 7, 239, 1),
+                                        (13, 314, 26, 3), (2, 2048, 32, 1), (300, 24, 30, 2)])
+def test_thin_matrices_of_low_rank(N, r, c, rank):
+    g = torch.Generator(device="cuda").manual_seed(N * r + c)
+    U = torch.randn(N, r, rank, generator=g, device="cuda") @ torch.randn(N, rank, c, generator=g, device="cuda")
+    _check(_run(U), U, [COEF] * 5)
+    b = U.to(torch.bfloat16)   # of full rank again, with singular values at its roundings
+    _check(_run(b), b, [COEF] * 5)
+
+
+@pytest.mark.parametrize("N,r,c", [(292, 3, 3), (83, 2, 3), (97, 14, 15), (111, 4, 2), (400, 1, 2)])
+def test_small_square_matrices(N, r, c):
+    """Many of them, so that some are nearly singular; the update of one step too."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    U = torch.randn(N, r, c, generator=g, device="cuda")
+    _check(_run(U), U, [COEF] * 5)
+    G = moevie.moevie_pad_rows(U)
+    W, M = (moevie.moevie_pad_rows(torch.zeros_like(U)) for _ in range(2))
+    ws = moevie.OrthoWorkspace(N, r, c)
+    moevie.moevie_muon_update(W, M, G, ws, lr=1.0, momentum=0.0, scale=-1.0)
+    check_status(ws)
+    _check(W, U, [COEF] * 5)
