@@ -325,18 +325,18 @@ moevie_status moevie_moe_few(const moevie_layer* layer, const void* x, int64_t T
  *   O: bf16, row stride ld_o >= cols, matrix stride stride_o.  O does not overlap U.
  * Arithmetic: fp16 tensor-core operands (11 bits), fp32 accumulation, X carried from step to
  * step in 22 bits (where |a| <= 3.5 in the last two steps, the last one takes 11).  Matrices of
- * which one side is at most 32, and few matrices of which one is at most 128: fp32 throughout;
- * stacks of the latter: 22-bit operands but for X X^T.  Each step rounds anew and multiplies what
- * was there by the slope of its polynomial, so the error depends on coefficients and matrix.  In
- * 2-norm, before the rounding to bf16, against the formula's result:
+ * which one side is at most 128: 22-bit operands but for X X^T.  Of which one side is at most 32,
+ * and few matrices (some tens) of which one is at most 64: fp32 throughout.  Each step rounds anew
+ * and multiplies what was there by the slope of its polynomial, so the error depends on
+ * coefficients and matrix.  In 2-norm, before the rounding to bf16, against the formula's result:
  *   - coefficients (3.4445, -4.7750, 2.0315), five steps, matrices whose singular vectors are
  *     spread over their entries (as gradients' are), of full or low rank: 1e-3 to 2e-3, and
  *     below 1e-3 where one side is at most 128;
  *   - the same, but matrices of a few large entries, whose roundings do not average: up to
  *     2e-2 for a singular value that the steps' slopes (up to 4) magnify;
- *   - directions that are null in U hold X's rounding (2^-22), which every step multiplies by
- *     a: matrices of low rank take about eight such steps, and after twelve what was rounding
- *     counts as much as what was U (in 32 bits after fourteen);
+ *   - directions that are null in U hold X's rounding (2^-22; 2^-24 in fp32), which every step
+ *     multiplies by a: matrices of low rank take about eight such steps, and after twelve
+ *     (fourteen) what was rounding counts as much as what was U;
  *   - coefficients whose polynomials are steep where singular values arrive lose as much as
  *     their slopes say: first steps such as (8.29, -23.6, 17.3), slope 24 at 1, leave several
  *     percent on matrices of rank 1.

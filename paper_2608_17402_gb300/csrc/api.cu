@@ -1033,9 +1033,8 @@ static moevie_status check_ns(int64_t N, int64_t rows, int64_t cols) {
 
 // Coefficients of matrices whose smaller side is m.  Above NS_THIN, X, A and b A + c A^2 are held in
 // fp16 at NS_S, which ends at 64: singular values from 0 to 1, as X0 has, must keep all three under
-// NS_MAX_ENTRY (no entry exceeds the largest singular value; the rest is for roundings).  The
-// largest value of a step's polynomial lies at the end of the interval or where its derivative is
-// zero.  Asked of every m > NS_THIN alike, so that a stack's size does not decide.
+// NS_MAX_ENTRY (no entry exceeds the largest singular value; the rest is for roundings).  Asked of
+// every m > NS_THIN alike, so that a stack's size does not decide.
 static moevie_status check_coef(const float* coef, int steps, int64_t m) {
     if (!coef || steps < 1) return MOEVIE_ERR_INVALID_ARG;
     if (steps > NS_MAX_STEPS) return MOEVIE_ERR_UNSUPPORTED;
@@ -1044,22 +1043,10 @@ static moevie_status check_coef(const float* coef, int steps, int64_t m) {
     if (m <= NS_THIN) return MOEVIE_OK;
     double s = 1.0;   // largest singular value of X
     for (int it = 0; it < steps; ++it) {
-        const double a = coef[3 * it], b = coef[3 * it + 1], c = coef[3 * it + 2], t = s * s;
-        auto poly = [&](double u) { return fabs(b * u + c * u * u); };
-        double most = c != 0.0 ? fmax(t, poly(t)) : poly(t);
-        if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < t) most = fmax(most, poly(-b / (2.0 * c)));
-        if (!(most <= NS_MAX_ENTRY)) return MOEVIE_ERR_UNSUPPORTED;
-        if (it + 1 == steps) break;   // the result itself is not held in fp16
-        auto next = [&](double u) { return fabs(sqrt(u) * (a + b * u + c * u * u)); };
-        s = next(t);
-        // (a + 3 b u + 5 c u^2 = 0; its roots as 2 q / .., which c = 0 leaves finite)
-        const double disc = 9.0 * b * b - 20.0 * a * c;
-        if (disc >= 0.0) {
-            const double q = -0.5 * (3.0 * b + copysign(sqrt(disc), b));
-            for (const double u : {q != 0.0 ? a / q : -1.0, c != 0.0 ? q / (5.0 * c) : -1.0})
-                if (u > 0.0 && u < t) s = fmax(s, next(u));
-        }
-        if (!(s <= NS_MAX_ENTRY)) return MOEVIE_ERR_UNSUPPORTED;
+        const NsBounds b = ns_bounds(coef + 3 * it, s);
+        if (!(b.b <= NS_MAX_ENTRY) || (coef[3 * it + 2] != 0.f && !(s * s <= NS_MAX_ENTRY))) return MOEVIE_ERR_UNSUPPORTED;
+        s = b.largest;
+        if (it + 1 < steps && !(s <= NS_MAX_ENTRY)) return MOEVIE_ERR_UNSUPPORTED;   // (the result is not held in fp16)
     }
     return MOEVIE_OK;
 }

@@ -417,6 +417,12 @@ struct NsCall {
     int steps;
 };
 size_t ns_workspace_bytes(int64_t N, int64_t r, int64_t c);
+// Of a step (a, b, c) over singular values s' in [0, s]: the largest result, gain |p(s')| / s' and
+// eigenvalue of b A + c A^2.
+struct NsBounds {
+    double largest, gain, b;
+};
+NsBounds ns_bounds(const float* coef, double s);
 cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t limit_ns, cudaStream_t s);
 
 // ---------------------------------------- permute without a caller workspace

@@ -17,7 +17,7 @@
 //   ns_kernel           the three products of every step on tcgen05 CTA pairs in one persistent
 //                       launch, with the output or the weight update in the last one's epilogue.
 //   ns_thin_kernel      all of that for matrices whose smaller side is at most 32, in fp32.
-//   ns_small_kernel     the same for few matrices whose smaller side is 33 to 128.
+//   ns_small_kernel     the same for few matrices whose smaller side is 33 to 64.
 //
 // ns_kernel.  Work items are (matrix, stage, tile): a Gram, a polynomial and an apply stage for
 // each step.  Only some of the matrices are under way at a time, in buffers that are used again
@@ -47,9 +47,9 @@
 // a lo, and leaving both out is nearer (1.6e-3 becomes 1.4e-3 on Gaussian matrices) and saves the
 // last step's lo.  The price is a 2e-4 of |X| in the null directions of U: 1.5e-3 instead of 3e-4 for
 // rank 1 with a = 3.4, but 8e-3 with a = 20 and a result of half X (1.5e-3 with all of lo).
-// For m <= 128 the roundings of a few singular values average less, and time is latency: there (in
-// stacks that are not left to ns_small_kernel) A and B have lo parts too, and the polynomial and the
-// apply product are hi hi + hi lo + lo hi.  The Gram product, whose K is the long side, stays hi hi:
+// For m <= 128 the roundings of a few singular values average less, and time is latency: there (where
+// ns_small_kernel does not take them) A and B have lo parts too, and the polynomial and the apply
+// product are hi hi + hi lo + lo hi.  The Gram product, whose K is the long side, stays hi hi:
 // over five steps the result is then within 0.8e-3 before its rounding to bf16 (all three products
 // in one term 2e-3 for 64 singular values, the Gram product in three terms too 1e-5).
 //
@@ -62,6 +62,8 @@
 // to 20%.  One 1024 x 1024 matrix (124 us) is a chain of 15 dependent stages of 8 us: hand-over between
 // CTAs 5 us, 16 K blocks 3 us.  So are stacks of up to about 100 narrow matrices (91 x 505 x 92 152 us).
 #include "internal.h"
+
+#include <math.h>
 
 #include <atomic>
 
@@ -354,6 +356,8 @@ struct NsArgs {
     int base_size, big_groups;         // the first big_groups of them hold base_size + 1, the others base_size
     int total;                         // items
     int thin_cluster;                  // CTAs per thin matrix
+    float* X1;                         // X between segments [N][r][ldx] (thin and few narrow matrices)
+    uint8_t restart[NS_MAX_STEPS];     // the step starts a segment (the same)
     uint8_t kind[NS_MAX_STAGES], step[NS_MAX_STAGES];
     int need[NS_MAX_STAGES + 1];       // counter value at which a stage's inputs are complete
     float coef[3 * NS_MAX_STEPS], lo_coef[NS_MAX_STEPS];   // lo_coef: multiplier of lo in a X
@@ -1070,15 +1074,22 @@ __global__ void __launch_bounds__(NS_THREADS, 1) ns_kernel(const __grid_constant
 // m <= NS_THIN: fp32 throughout.  All factors of the step polynomials are polynomials of
 // A = X0 X0^T and commute, so the iteration runs on symmetric 32 x 32 matrices in shared memory
 // (P = a I + b A + c A^2, Q <- P Q, A <- P A P; zeros past m) and X is read twice: for A and for
+// Q X0.  But each A <- P A P multiplies the roundings of A between its null directions by up to
+// the square of the polynomial's largest gain (a^2 = 12 for the default quintic), where the iteration
+// on X multiplies X's by the gain.  So the steps are cut into segments: a new one, which forms A from X
+// again, begins before a step for which that growth would pass NS_GROWTH (the default quintic: after
+// three steps).  Errors on X0 of rank 1: five steps 4e-5 (in one segment 2e-3), seven 5e-4 (0.25), ten
+// 1e-2 (NaN), as the iteration on X in fp32 has them; cut after two steps they are the same.
 // Q X0.  Thin matrices are kept off the tensor cores for accuracy as much as for time: with few
 // singular values the fp16 roundings do not average out over the entries (a 1 x n matrix is one
 // number per step, and its result was 5e-3 off), and their tiles would be mostly empty.
 //
 // A cluster of up to 8 CTAs per matrix, each with every so many 128 columns of the long side; the
 // parts of A are added in CTA order over distributed shared memory, and every CTA iterates for
-// itself.  Bound by latency (loads of a chunk 3 us, the iteration 8 us): 32 x 2048 27 us, a stack of 256
-// of them 155 us (with one CTA a matrix and scalar products 335 and 504).
+// itself.  Bound by latency (loads of a chunk 3 us, the iteration 8 us): 32 x 2048 34 us, a stack of 256
+// of them 255 us, of which the second segment's passes over X are 10 and 97.
 constexpr int NS_THIN_THREADS = 256;
+constexpr double NS_GROWTH = 150.0;   // of roundings in A within a segment
 constexpr int NS_THIN_K = 128;
 constexpr int NS_THIN_LD = NS_THIN + 4;
 constexpr int NS_THIN_CLUSTER = 8;
@@ -1097,14 +1108,17 @@ struct NsPlace {
         dk = tall ? NS_THIN_THREADS / S : 0;
     }
 };
-// xs[i][kk] = X0 (i, k0 + kk), zeros outside, by the whole CTA.
+// xs[i][kk] = X (i, k0 + kk), zeros outside, by the whole CTA: X0 from the update (`first`), or X as the
+// segment before left it.
 template <int S, int K>
-__device__ __forceinline__ void ns_stage(const NsArgs& p, int e, int k0, float pre, float post, float (*xs)[K + 4]) {
+__device__ __forceinline__ void ns_stage(const NsArgs& p, int e, int k0, bool first, float pre, float post,
+                                         float (*xs)[K + 4]) {
     const NsPlace<S, K> w(p.tall);
     const int m = p.m, n = p.tall ? p.r : p.c;
-    const int64_t at = e * p.u.st_u + (p.tall ? (k0 + w.kk0) * p.u.ld_u + w.i0 : w.i0 * p.u.ld_u + k0 + w.kk0);
-    const int64_t d = (p.tall ? w.dk : w.di) * p.u.ld_u;
-    auto load = [&](auto get) {
+    const int64_t ld = first ? p.u.ld_u : p.ldx, d = (p.tall ? w.dk : w.di) * ld;
+    const int64_t at = e * (first ? p.u.st_u : (int64_t)p.r * p.ldx) +
+                       (p.tall ? (k0 + w.kk0) * ld + w.i0 : w.i0 * ld + k0 + w.kk0);
+    auto load = [&](auto get, float pre, float post) {
         float v[w.PER];
 #pragma unroll
         for (int u = 0; u < w.PER; ++u)
@@ -1115,21 +1129,31 @@ __device__ __forceinline__ void ns_stage(const NsArgs& p, int e, int k0, float p
     const float* M = p.u.M;
     const float* U = static_cast<const float*>(p.u.U);
     const __nv_bfloat16* B = static_cast<const __nv_bfloat16*>(p.u.U);
+    const float* X = p.X1;
     const float mu = p.u.mu;
-    if (M && !p.u.nesterov) load([=](int64_t a) { return M[a]; });
-    else if (M) load([=](int64_t a) { return fmaf(mu, M[a], U[a]); });   // (with a momentum, U is fp32)
-    else if (p.u.u_bf16) load([=](int64_t a) { return as_f32(B[a]); });
-    else load([=](int64_t a) { return U[a]; });
+    if (!first) load([=](int64_t a) { return X[a]; }, 1.f, 1.f);
+    else if (M && !p.u.nesterov) load([=](int64_t a) { return M[a]; }, pre, post);
+    else if (M) load([=](int64_t a) { return fmaf(mu, M[a], U[a]); }, pre, post);   // (with a momentum, U is fp32)
+    else if (p.u.u_bf16) load([=](int64_t a) { return as_f32(B[a]); }, pre, post);
+    else load([=](int64_t a) { return U[a]; }, pre, post);
     __syncthreads();
 }
-// The chunk's results from xs to O, or into the weights.
+// The chunk's results from xs to O or into the weights (`last`), or for the next segment, in which the
+// same thread reads each element again.
 template <int S, int K>
-__device__ __forceinline__ void ns_store(const NsArgs& p, int e, int k0, const float (*xs)[K + 4]) {
+__device__ __forceinline__ void ns_store(const NsArgs& p, int e, int k0, bool last, const float (*xs)[K + 4]) {
     const NsPlace<S, K> w(p.tall);
     const int m = p.m, n = p.tall ? p.r : p.c;
-    const int64_t ld = p.O ? p.ld_o : p.ld_w, d = (p.tall ? w.dk : w.di) * ld;
-    const int64_t at = e * (p.O ? p.st_o : p.st_w) + (p.tall ? (k0 + w.kk0) * ld + w.i0 : w.i0 * ld + k0 + w.kk0);
+    const int64_t ld = !last ? p.ldx : p.O ? p.ld_o : p.ld_w, d = (p.tall ? w.dk : w.di) * ld;
+    const int64_t at = e * (!last ? (int64_t)p.r * p.ldx : p.O ? p.st_o : p.st_w) +
+                       (p.tall ? (k0 + w.kk0) * ld + w.i0 : w.i0 * ld + k0 + w.kk0);
     auto inside = [&](int u) { return w.i0 + w.di * u < m && k0 + w.kk0 + w.dk * u < n; };
+    if (!last) {
+#pragma unroll
+        for (int u = 0; u < w.PER; ++u)
+            if (inside(u)) p.X1[at + u * d] = xs[w.i0 + w.di * u][w.kk0 + w.dk * u];
+        return;
+    }
     if (p.O) {
 #pragma unroll
         for (int u = 0; u < w.PER; ++u)
@@ -1158,333 +1182,311 @@ __global__ void __launch_bounds__(NS_THIN_THREADS, 3) ns_thin_kernel(const __gri
     const int chunks = (n + NS_THIN_K - 1) / NS_THIN_K;
     float pre, post;
     norm_scales(p.u, e, pre, post);
-    auto stage = [&](int k0) { ns_stage<NS_THIN, NS_THIN_K>(p, e, k0, pre, post, xs); };
     // A: four groups of 64 threads share a chunk's columns, a thread has rows ti + 8 u, columns tj + 8 v
-    {
-        const int g = tid >> 6, ti = tid >> 3 & 7, tj = tid & 7;
-        float acc[4][4] = {};
-        for (int ch = rank; ch < chunks; ch += C) {
-            stage(ch * NS_THIN_K);
+    const int g = tid >> 6, ti = tid >> 3 & 7, tj = tid & 7;
+    float acc[4][4] = {};
+    auto gram = [&]() {   // of the chunk in xs
 #pragma unroll 2
-            for (int q = 0; q < NS_THIN_K / 16; ++q) {
-                const int kk = (g * (NS_THIN_K / 16) + q) * 4;
-                float4 a[4], b[4];
+        for (int q = 0; q < NS_THIN_K / 16; ++q) {
+            const int kk = (g * (NS_THIN_K / 16) + q) * 4;
+            float4 a[4], b[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    a[u] = *reinterpret_cast<const float4*>(&xs[ti + 8 * u][kk]);
-                    b[u] = *reinterpret_cast<const float4*>(&xs[tj + 8 * u][kk]);
-                }
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        acc[u][v] = fmaf(a[u].w, b[v].w, fmaf(a[u].z, b[v].z, fmaf(a[u].y, b[v].y, fmaf(a[u].x, b[v].x, acc[u][v]))));
+            for (int u = 0; u < 4; ++u) {
+                a[u] = *reinterpret_cast<const float4*>(&xs[ti + 8 * u][kk]);
+                b[u] = *reinterpret_cast<const float4*>(&xs[tj + 8 * u][kk]);
             }
-            if (chunks > C) __syncthreads();   // (one chunk a CTA: it stays for the end)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const float lo = fmaf(a[u].y, b[v].y, fmaf(a[u].x, b[v].x, acc[u][v]));
+                    acc[u][v] = fmaf(a[u].w, b[v].w, fmaf(a[u].z, b[v].z, lo));
+                }
         }
+        if (chunks > C) __syncthreads();   // (one chunk a CTA: it stays in xs)
+    };
+    for (int ch = rank; ch < chunks; ch += C) {
+        ns_stage<NS_THIN, NS_THIN_K>(p, e, ch * NS_THIN_K, true, pre, post, xs);
+        gram();
+    }
+    for (int s0 = 0, s1; s0 < p.steps; s0 = s1) {   // segments [s0, s1)
+        for (s1 = s0 + 1; s1 < p.steps && !p.restart[s1]; ++s1) {}
+        const bool last = s1 == p.steps;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) sq[g][ti + 8 * u][tj + 8 * v] = acc[u][v];
+            for (int v = 0; v < 4; ++v) {
+                sq[g][ti + 8 * u][tj + 8 * v] = acc[u][v];
+                acc[u][v] = 0.f;
+            }
         __syncthreads();
-    }
-    // a thread's four elements of a square: row tid / 8, columns 4 (tid % 8) ..
-    const int er = tid >> 3, ec = (tid & 7) * 4;
-    auto at4 = [&](Square& S) { return reinterpret_cast<float4*>(&S[er][ec]); };
-    float4 sum = *at4(sq[0]);
-    for (int g = 1; g < 4; ++g) {
-        const float4 v = *at4(sq[g]);
-        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
-    }
-    *at4(sq[0]) = sum;   // (read by this thread alone so far)
-    if (C > 1) {
-        const uint32_t mine = smem_u32(at4(sq[0]));
-        cluster_sync();
-        sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int r = 0; r < C; ++r) {
-            float4 v;
-            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                         : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                         : "r"(peer_addr(mine, r)));
+        // a thread's four elements of a square: row tid / 8, columns 4 (tid % 8) ..
+        const int er = tid >> 3, ec = (tid & 7) * 4;
+        auto at4 = [&](Square& S) { return reinterpret_cast<float4*>(&S[er][ec]); };
+        float4 sum = *at4(sq[0]);
+        for (int g = 1; g < 4; ++g) {
+            const float4 v = *at4(sq[g]);
             sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
         }
-        cluster_sync();   // every CTA has read the parts
-        *at4(sq[0]) = sum;
-    }
-    __syncthreads();
-    // out = L R for symmetric operands, `out` none of them; 2 x 2 elements a thread
-    auto product = [&](Square& out, const Square& L, const Square& R) {
-        const int i = (tid >> 4) * 2, j = (tid & 15) * 2;
-        float2 r0 = make_float2(0.f, 0.f), r1 = r0;
+        *at4(sq[0]) = sum;   // (read by this thread alone so far)
+        if (C > 1) {
+            const uint32_t mine = smem_u32(at4(sq[0]));
+            cluster_sync();
+            sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int r = 0; r < C; ++r) {
+                float4 v;
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                             : "r"(peer_addr(mine, r)));
+                sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+            }
+            cluster_sync();   // every CTA has read the parts
+            *at4(sq[0]) = sum;
+        }
+        __syncthreads();
+        // out = L R for symmetric operands, `out` none of them; 2 x 2 elements a thread
+        auto product = [&](Square& out, const Square& L, const Square& R) {
+            const int i = (tid >> 4) * 2, j = (tid & 15) * 2;
+            float2 r0 = make_float2(0.f, 0.f), r1 = r0;
 #pragma unroll 8
-        for (int k = 0; k < NS_THIN; ++k) {
-            const float2 l = *reinterpret_cast<const float2*>(&L[k][i]), r = *reinterpret_cast<const float2*>(&R[k][j]);
-            r0 = make_float2(fmaf(l.x, r.x, r0.x), fmaf(l.x, r.y, r0.y));
-            r1 = make_float2(fmaf(l.y, r.x, r1.x), fmaf(l.y, r.y, r1.y));
+            for (int k = 0; k < NS_THIN; ++k) {
+                const float2 l = *reinterpret_cast<const float2*>(&L[k][i]), r = *reinterpret_cast<const float2*>(&R[k][j]);
+                r0 = make_float2(fmaf(l.x, r.x, r0.x), fmaf(l.x, r.y, r0.y));
+                r1 = make_float2(fmaf(l.y, r.x, r1.x), fmaf(l.y, r.y, r1.y));
+            }
+            *reinterpret_cast<float2*>(&out[i][j]) = r0;
+            *reinterpret_cast<float2*>(&out[i + 1][j]) = r1;
+            __syncthreads();
+        };
+        Square& A = sq[0];
+        Square& P = sq[1];
+        int iq = 2, it2 = 3;   // where Q and the scratch matrix are
+        for (int it = s0; it < s1; ++it) {
+            const float ca = p.coef[3 * it], cb = p.coef[3 * it + 1], cc = p.coef[3 * it + 2];
+            product(sq[it2], A, A);
+            const float4 a = *at4(A), t = *at4(sq[it2]);
+            float4 v = make_float4(fmaf(cc, t.x, cb * a.x), fmaf(cc, t.y, cb * a.y), fmaf(cc, t.z, cb * a.z), fmaf(cc, t.w, cb * a.w));
+            v.x += er == ec ? ca : 0.f;
+            v.y += er == ec + 1 ? ca : 0.f;
+            v.z += er == ec + 2 ? ca : 0.f;
+            v.w += er == ec + 3 ? ca : 0.f;
+            *at4(P) = v;
+            if (it == s0) *at4(sq[iq]) = v;
+            __syncthreads();
+            if (it > s0) {
+                product(sq[it2], P, sq[iq]);
+                iq ^= 1;   // 2 and 3 change places
+                it2 ^= 1;
+            }
+            if (it + 1 < s1) {
+                product(sq[it2], P, A);
+                product(A, sq[it2], P);
+            }
         }
-        *reinterpret_cast<float2*>(&out[i][j]) = r0;
-        *reinterpret_cast<float2*>(&out[i + 1][j]) = r1;
-        __syncthreads();
-    };
-    Square& A = sq[0];
-    Square& P = sq[1];
-    int iq = 2, it2 = 3;   // where Q and the scratch matrix are
-    for (int it = 0; it < p.steps; ++it) {
-        const float ca = p.coef[3 * it], cb = p.coef[3 * it + 1], cc = p.coef[3 * it + 2];
-        product(sq[it2], A, A);
-        const float4 a = *at4(A), t = *at4(sq[it2]);
-        float4 v = make_float4(fmaf(cc, t.x, cb * a.x), fmaf(cc, t.y, cb * a.y), fmaf(cc, t.z, cb * a.z), fmaf(cc, t.w, cb * a.w));
-        v.x += er == ec ? ca : 0.f;
-        v.y += er == ec + 1 ? ca : 0.f;
-        v.z += er == ec + 2 ? ca : 0.f;
-        v.w += er == ec + 3 ? ca : 0.f;
-        *at4(P) = v;
-        if (it == 0) *at4(sq[iq]) = v;
-        __syncthreads();
-        if (it > 0) {
-            product(sq[it2], P, sq[iq]);
-            iq ^= 1;   // 2 and 3 change places
-            it2 ^= 1;
+        // Q is the product of the steps' P, the last one leftmost: in that order a rounding in one of them is
+        // multiplied by those after it, as in the iteration on X itself.  (In the other order, that of the
+        // transpose, the last P's roundings go through all earlier ones: on X0 of rank 1 the result was off
+        // by 0.8.)  Transposed, so that a row's factors lie side by side.
+        {
+            const float4 v = *at4(sq[iq]);
+            sq[it2][ec][er] = v.x;
+            sq[it2][ec + 1][er] = v.y;
+            sq[it2][ec + 2][er] = v.z;
+            sq[it2][ec + 3][er] = v.w;
+            __syncthreads();
         }
-        if (it + 1 < p.steps) {
-            product(sq[it2], P, A);
-            product(A, sq[it2], P);
-        }
-    }
-    // Q is the product of the steps' P, the last one leftmost: in that order a rounding in one of them is
-    // multiplied by those after it, as in the iteration on X itself.  (In the other order, that of the
-    // transpose, the last P's roundings go through all earlier ones: on X0 of rank 1 the result was off
-    // by 0.8.)  Transposed, so that a row's factors lie side by side.
-    {
-        const float4 v = *at4(sq[iq]);
-        sq[it2][ec][er] = v.x;
-        sq[it2][ec + 1][er] = v.y;
-        sq[it2][ec + 2][er] = v.z;
-        sq[it2][ec + 3][er] = v.w;
-        __syncthreads();
-    }
-    // Q X0: 4 rows x 4 columns a thread, through xs to memory order
-    const Square& QT = sq[it2];
-    for (int ch = rank; ch < chunks; ch += C) {
-        const int k0 = ch * NS_THIN_K, c4 = (tid & 31) * 4, r4 = (tid >> 5) * 4;
-        if (chunks > C) stage(k0);
-        float4 o[4] = {};
+        // Q X: 4 rows x 4 columns a thread, through xs to memory order; the next segment's A on the way
+        const Square& QT = sq[it2];
+        for (int ch = rank; ch < chunks; ch += C) {
+            const int k0 = ch * NS_THIN_K, c4 = (tid & 31) * 4, r4 = (tid >> 5) * 4;
+            if (chunks > C) ns_stage<NS_THIN, NS_THIN_K>(p, e, k0, s0 == 0, pre, post, xs);
+            float4 o[4] = {};
 #pragma unroll 4
-        for (int j = 0; j < m; ++j) {
-            const float4 x = *reinterpret_cast<const float4*>(&xs[j][c4]), q = *reinterpret_cast<const float4*>(&QT[j][r4]);
-            const float qs[4] = {q.x, q.y, q.z, q.w};
+            for (int j = 0; j < m; ++j) {
+                const float4 x = *reinterpret_cast<const float4*>(&xs[j][c4]), q = *reinterpret_cast<const float4*>(&QT[j][r4]);
+                const float qs[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                o[u] = make_float4(fmaf(qs[u], x.x, o[u].x), fmaf(qs[u], x.y, o[u].y), fmaf(qs[u], x.z, o[u].z),
-                                   fmaf(qs[u], x.w, o[u].w));
+                for (int u = 0; u < 4; ++u)
+                    o[u] = make_float4(fmaf(qs[u], x.x, o[u].x), fmaf(qs[u], x.y, o[u].y), fmaf(qs[u], x.z, o[u].z),
+                                       fmaf(qs[u], x.w, o[u].w));
+            }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < 4; ++u) *reinterpret_cast<float4*>(&xs[r4 + u][c4]) = o[u];
+            __syncthreads();
+            if (last || chunks > C) ns_store<NS_THIN, NS_THIN_K>(p, e, k0, last, xs);
+            if (last) __syncthreads();
+            else gram();
         }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < 4; ++u) *reinterpret_cast<float4*>(&xs[r4 + u][c4]) = o[u];
-        __syncthreads();
-        ns_store<NS_THIN, NS_THIN_K>(p, e, k0, xs);
-        __syncthreads();
     }
 }
 
 // ---------------------------------------------------- few narrow matrices
 
-// NS_THIN < m <= S (64 or 128), the same iteration in fp32 by a cluster of 8 CTAs per matrix: each
-// forms the part of A from its columns of X and then has S / 8 rows of every product.  All factors
+// NS_THIN < m <= NS_SMALL, the same iteration in fp32 by a cluster of 8 CTAs per matrix: each forms
+// the part of A from its columns of X and then has 8 rows of every product, one a warp.  All factors
 // being symmetric and commuting, rows of Q P, A P and (A P) P need only the CTA's own rows of the
 // left factor, so P and A alone are shared, in every CTA's memory.  For few matrices: on the tensor
 // cores the Gram product of one such matrix is a single tile, n / 64 K blocks one after the other,
 // and every step three dependent launches' worth of hand-over.
-// Bound by shared memory and the fp32 units of its 8 SMs: 128 x 2048 in 113 us, of which the 19 products
-// of 128 x 128 are about 80.
+// Bound by shared memory and the fp32 units of its 8 SMs: 64 x 512 in 37 us, 64 x 2048 in 73, 12 for each
+// pass over X.  (128 x 2048 in the same way took 200 us, 115 on the tensor cores; 256 x 100, the best
+// of those above 64, 104 and 100.)
+constexpr int NS_SMALL = 64;
 constexpr int NS_SMALL_K = 64;
-template <int S>
-constexpr int ns_small_smem() {
-    return 4 * ((2 * S + 2 * (S / 8)) * (S + 4) + S * (NS_SMALL_K + 4));
-}
+constexpr int NS_SMALL_ROWS = NS_SMALL / 8;   // of a CTA
+constexpr int NS_SMALL_LD = NS_SMALL + 4;
+constexpr int NS_SMALL_SMEM = 4 * ((2 * NS_SMALL + 2 * NS_SMALL_ROWS) * NS_SMALL_LD + NS_SMALL * (NS_SMALL_K + 4));
 
-// Writes N (2 or 4) consecutive floats at the same place of every CTA of the cluster.
-template <int N>
-__device__ __forceinline__ void ns_share(const float* at, const float (&v)[N]) {
+// Writes two consecutive floats at the same place of every CTA of the cluster.
+__device__ __forceinline__ void ns_share(const float* at, const float (&v)[2]) {
     const uint32_t mine = smem_u32(at);
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        const uint32_t a = peer_addr(mine, r);
-        if (N == 4)
-            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v[0]), "f"(v[1]),
-                         "f"(v[N - 2]), "f"(v[N - 1])
-                         : "memory");
-        else
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(v[0]), "f"(v[1]) : "memory");
-    }
+    for (int r = 0; r < 8; ++r)
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(peer_addr(mine, r)), "f"(v[0]), "f"(v[1]) : "memory");
 }
 
-// out[i] = rows[i] . R for a warp's rows; a lane has CT consecutive columns.
-template <int S, int NR>
-__device__ __forceinline__ void ns_rows(float (&out)[NR][S / 32], const float* const (&rows)[NR], const float (*Rm)[S + 4]) {
-    constexpr int CT = S / 32;
-    const int c = (threadIdx.x & 31) * CT;
+// out[i] = rows[i] . R; a lane has two consecutive columns.
+template <int NR>
+__device__ __forceinline__ void ns_rows(float (&out)[NR][2], const float* const (&rows)[NR], const float (*Rm)[NS_SMALL_LD]) {
+    const int c = (threadIdx.x & 31) * 2;
 #pragma unroll
-    for (int i = 0; i < NR; ++i)
-#pragma unroll
-        for (int j = 0; j < CT; ++j) out[i][j] = 0.f;
+    for (int i = 0; i < NR; ++i) out[i][0] = out[i][1] = 0.f;
 #pragma unroll 2
-    for (int k = 0; k < S; k += 4) {
+    for (int k = 0; k < NS_SMALL; k += 4) {
         float l[NR][4];
 #pragma unroll
         for (int i = 0; i < NR; ++i) *reinterpret_cast<float4*>(l[i]) = *reinterpret_cast<const float4*>(rows[i] + k);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            float r[CT];
-            if (CT == 4) *reinterpret_cast<float4*>(r) = *reinterpret_cast<const float4*>(&Rm[k + q][c]);
-            else *reinterpret_cast<float2*>(r) = *reinterpret_cast<const float2*>(&Rm[k + q][c]);
+            const float2 r = *reinterpret_cast<const float2*>(&Rm[k + q][c]);
 #pragma unroll
-            for (int i = 0; i < NR; ++i)
-#pragma unroll
-                for (int j = 0; j < CT; ++j) out[i][j] = fmaf(l[i][q], r[j], out[i][j]);
+            for (int i = 0; i < NR; ++i) {
+                out[i][0] = fmaf(l[i][q], r.x, out[i][0]);
+                out[i][1] = fmaf(l[i][q], r.y, out[i][1]);
+            }
         }
     }
 }
 
-template <int S>
-__global__ void __launch_bounds__(NS_THIN_THREADS, S == 64 ? 2 : 1) ns_small_kernel(const __grid_constant__ NsArgs p) {
-    constexpr int R = S / 8, LD = S + 4, K = NS_SMALL_K, TI = S / 16, CT = S / 32, RW = R / 8;
+__global__ void __launch_bounds__(NS_THIN_THREADS, 2) ns_small_kernel(const __grid_constant__ NsArgs p) {
+    constexpr int S = NS_SMALL, K = NS_SMALL_K, TI = S / 16;
     extern __shared__ __align__(16) float ns_small_mem[];
-    typedef float Row[LD];
+    typedef float Row[NS_SMALL_LD];
     Row* A = reinterpret_cast<Row*>(ns_small_mem);
     Row* P = A + S;
     Row* Qs = P + S;   // this CTA's rows of Q and of A P
-    Row* Ts = Qs + R;
+    Row* Ts = Qs + NS_SMALL_ROWS;
     typedef float XRow[K + 4];
-    XRow* xs = reinterpret_cast<XRow*>(Ts + R);
+    XRow* xs = reinterpret_cast<XRow*>(Ts + NS_SMALL_ROWS);
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, m = p.m, n = p.tall ? p.r : p.c;
     const int e = blockIdx.x / 8, rank = (int)cluster_rank(), chunks = (n + K - 1) / K;
     float pre, post;
     norm_scales(p.u, e, pre, post);
-    {   // this CTA's part of A: rows ti + 16 u, columns tj + 16 v
-        const int ti = tid >> 4, tj = tid & 15;
-        float acc[TI][TI] = {};
-        for (int ch = rank; ch < chunks; ch += 8) {
-            ns_stage<S, K>(p, e, ch * K, pre, post, xs);
+    // this CTA's part of A: rows ti + 16 u, columns tj + 16 v
+    const int ti = tid >> 4, tj = tid & 15;
+    float acc[TI][TI] = {};
+    auto gram = [&]() {   // of the chunk in xs
 #pragma unroll 1
-            for (int kk = 0; kk < K; kk += 4) {
-                float4 b[TI];
+        for (int kk = 0; kk < K; kk += 4) {
+            float4 b[TI];
 #pragma unroll
-                for (int v = 0; v < TI; ++v) b[v] = *reinterpret_cast<const float4*>(&xs[tj + 16 * v][kk]);
+            for (int v = 0; v < TI; ++v) b[v] = *reinterpret_cast<const float4*>(&xs[tj + 16 * v][kk]);
 #pragma unroll
-                for (int u = 0; u < TI; ++u) {
-                    const float4 a = *reinterpret_cast<const float4*>(&xs[ti + 16 * u][kk]);
+            for (int u = 0; u < TI; ++u) {
+                const float4 a = *reinterpret_cast<const float4*>(&xs[ti + 16 * u][kk]);
 #pragma unroll
-                    for (int v = 0; v < TI; ++v)
-                        acc[u][v] = fmaf(a.w, b[v].w, fmaf(a.z, b[v].z, fmaf(a.y, b[v].y, fmaf(a.x, b[v].x, acc[u][v]))));
-                }
+                for (int v = 0; v < TI; ++v)
+                    acc[u][v] = fmaf(a.w, b[v].w, fmaf(a.z, b[v].z, fmaf(a.y, b[v].y, fmaf(a.x, b[v].x, acc[u][v]))));
             }
-            if (chunks > 8) __syncthreads();   // (one chunk a CTA: it stays for the end)
         }
+        if (chunks > 8) __syncthreads();   // (one chunk a CTA: it stays in xs)
+    };
+    for (int ch = rank; ch < chunks; ch += 8) {
+        ns_stage<S, K>(p, e, ch * K, true, pre, post, xs);
+        gram();
+    }
+    for (int s0 = 0, s1; s0 < p.steps; s0 = s1) {   // segments [s0, s1)
+        for (s1 = s0 + 1; s1 < p.steps && !p.restart[s1]; ++s1) {}
+        const bool final = s1 == p.steps;
 #pragma unroll
         for (int u = 0; u < TI; ++u)
 #pragma unroll
-            for (int v = 0; v < TI; ++v) A[ti + 16 * u][tj + 16 * v] = acc[u][v];
-    }
-    // the sum of the parts, this CTA's rows first, then everyone's
-    const int row0 = rank * R + warp * RW, col = lane * CT;   // a warp's rows, a lane's columns
-    float sum[RW][CT] = {};
-    cluster_sync();
-#pragma unroll
-    for (int i = 0; i < RW; ++i)
-#pragma unroll
-        for (int j = 0; j < CT; j += 2) {
-            const uint32_t mine = smem_u32(&A[row0 + i][col + j]);
-            for (int r = 0; r < 8; ++r) {
-                float x, y;
-                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(peer_addr(mine, r)));
-                sum[i][j] += x;
-                sum[i][j + 1] += y;
+            for (int v = 0; v < TI; ++v) {
+                A[ti + 16 * u][tj + 16 * v] = acc[u][v];
+                acc[u][v] = 0.f;
             }
+        // the sum of the parts, this CTA's rows first, then everyone's
+        const int row = rank * NS_SMALL_ROWS + warp, col = lane * 2;   // a warp's row, a lane's columns
+        float t[1][2] = {};
+        cluster_sync();
+        const uint32_t mine = smem_u32(&A[row][col]);
+        for (int r = 0; r < 8; ++r) {
+            float x, y;
+            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(peer_addr(mine, r)));
+            t[0][0] += x;
+            t[0][1] += y;
         }
-    cluster_sync();
+        cluster_sync();
+        ns_share(&A[row][col], t[0]);
+        cluster_sync();
+        for (int it = s0; it < s1; ++it) {
+            const float ca = p.coef[3 * it], cb = p.coef[3 * it + 1], cc = p.coef[3 * it + 2];
+            const float* const a_row[1] = {A[row]};
+            ns_rows<1>(t, a_row, A);
 #pragma unroll
-    for (int i = 0; i < RW; ++i) ns_share<CT>(&A[row0 + i][col], sum[i]);
-    cluster_sync();
-    const float* ra[RW];
-#pragma unroll
-    for (int i = 0; i < RW; ++i) ra[i] = A[row0 + i];
-    for (int it = 0; it < p.steps; ++it) {
-        const float ca = p.coef[3 * it], cb = p.coef[3 * it + 1], cc = p.coef[3 * it + 2];
-        const bool last = it + 1 == p.steps;
-        float t[RW][CT];
-        ns_rows<S, RW>(t, ra, A);
-#pragma unroll
-        for (int i = 0; i < RW; ++i) {
-#pragma unroll
-            for (int j = 0; j < CT; ++j) {
-                t[i][j] = fmaf(cc, t[i][j], cb * A[row0 + i][col + j]) + (row0 + i == col + j ? ca : 0.f);
-                if (it == 0) Qs[warp * RW + i][col + j] = t[i][j];
+            for (int j = 0; j < 2; ++j) {
+                t[0][j] = fmaf(cc, t[0][j], cb * A[row][col + j]) + (row == col + j ? ca : 0.f);
+                if (it == s0) Qs[warp][col + j] = t[0][j];
             }
-            ns_share<CT>(&P[row0 + i][col], t[i]);
-        }
-        cluster_sync();   // P is complete
-        // rows of Q P and of A P, then of (A P) P; a warp's rows of Q and A P are its own
-        float o[2 * RW][CT];
-        const float* rows[2 * RW];
+            ns_share(&P[row][col], t[0]);
+            cluster_sync();   // P is complete
+            // rows of Q P and of A P, then of (A P) P; a warp's rows of Q and A P are its own
+            float o[2][2];
+            const float* const rows[2] = {Qs[warp], A[row]};
+            ns_rows<2>(o, rows, P);
+            __syncwarp();
 #pragma unroll
-        for (int i = 0; i < RW; ++i) {
-            rows[i] = Qs[warp * RW + i];
-            rows[RW + i] = ra[i];
-        }
-        ns_rows<S, 2 * RW>(o, rows, P);
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < RW; ++i)
-#pragma unroll
-            for (int j = 0; j < CT; ++j) {
-                if (it > 0) Qs[warp * RW + i][col + j] = o[i][j];
-                Ts[warp * RW + i][col + j] = o[RW + i][j];
+            for (int j = 0; j < 2; ++j) {
+                if (it > s0) Qs[warp][col + j] = o[0][j];
+                Ts[warp][col + j] = o[1][j];
             }
-        __syncwarp();
-        if (last) break;
-#pragma unroll
-        for (int i = 0; i < RW; ++i) ra[i] = Ts[warp * RW + i];
-        ns_rows<S, RW>(t, ra, P);
-#pragma unroll
-        for (int i = 0; i < RW; ++i) {
-            ns_share<CT>(&A[row0 + i][col], t[i]);
-            ra[i] = A[row0 + i];
+            __syncwarp();
+            if (it + 1 == s1) break;
+            const float* const t_row[1] = {Ts[warp]};
+            ns_rows<1>(t, t_row, P);
+            ns_share(&A[row][col], t[0]);
+            cluster_sync();   // A is complete, and P free
         }
-        cluster_sync();   // A is complete, and P free
-    }
-    cluster_sync();   // P free
-#pragma unroll
-    for (int i = 0; i < RW; ++i) {
-        float q[CT];
-#pragma unroll
-        for (int j = 0; j < CT; ++j) q[j] = Qs[warp * RW + i][col + j];
-        ns_share<CT>(&P[row0 + i][col], q);
-    }
-    cluster_sync();
-    // Q X0: S / 16 rows x 4 columns a thread, through xs to memory order
-    for (int ch = rank; ch < chunks; ch += 8) {
-        const int c4 = (tid & 15) * 4, r0 = (tid >> 4) * TI;
-        if (chunks > 8) ns_stage<S, K>(p, e, ch * K, pre, post, xs);
-        float4 o[TI] = {};
+        cluster_sync();   // P free
+        const float q2[2] = {Qs[warp][col], Qs[warp][col + 1]};
+        ns_share(&P[row][col], q2);
+        cluster_sync();
+        // Q X: 4 rows x 4 columns a thread, through xs to memory order; the next segment's A on the way
+        for (int ch = rank; ch < chunks; ch += 8) {
+            const int c4 = (tid & 15) * 4, r0 = (tid >> 4) * TI;
+            if (chunks > 8) ns_stage<S, K>(p, e, ch * K, s0 == 0, pre, post, xs);
+            float4 o[TI] = {};
 #pragma unroll 2
-        for (int j = 0; j < m; ++j) {
-            const float4 x = *reinterpret_cast<const float4*>(&xs[j][c4]);
-            float q[TI];
+            for (int j = 0; j < m; ++j) {
+                const float4 x = *reinterpret_cast<const float4*>(&xs[j][c4]);
+                float q[TI];
 #pragma unroll
-            for (int u = 0; u < TI; u += 4) *reinterpret_cast<float4*>(q + u) = *reinterpret_cast<const float4*>(&P[j][r0 + u]);
+                for (int u = 0; u < TI; u += 4) *reinterpret_cast<float4*>(q + u) = *reinterpret_cast<const float4*>(&P[j][r0 + u]);
 #pragma unroll
-            for (int u = 0; u < TI; ++u)
-                o[u] = make_float4(fmaf(q[u], x.x, o[u].x), fmaf(q[u], x.y, o[u].y), fmaf(q[u], x.z, o[u].z),
-                                   fmaf(q[u], x.w, o[u].w));
+                for (int u = 0; u < TI; ++u)
+                    o[u] = make_float4(fmaf(q[u], x.x, o[u].x), fmaf(q[u], x.y, o[u].y), fmaf(q[u], x.z, o[u].z),
+                                       fmaf(q[u], x.w, o[u].w));
+            }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < TI; ++u) *reinterpret_cast<float4*>(&xs[r0 + u][c4]) = o[u];
+            __syncthreads();
+            if (final || chunks > 8) ns_store<S, K>(p, e, ch * K, final, xs);
+            if (final) __syncthreads();
+            else gram();
         }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < TI; ++u) *reinterpret_cast<float4*>(&xs[r0 + u][c4]) = o[u];
-        __syncthreads();
-        ns_store<S, K>(p, e, ch * K, xs);
-        __syncthreads();
     }
 }
 
@@ -1558,7 +1560,7 @@ NsLayout ns_layout(int64_t N, int64_t r, int64_t c) {
     L.part = take((size_t)N * L.chunks * 3 * sizeof(float));
     const size_t x = room * r * ldx * 2, a = room * m * ldm * 2;
     const bool thin = m <= NS_THIN;
-    L.x0h = take(thin ? 0 : (size_t)N * r * ldx * 2);
+    L.x0h = take((size_t)N * r * ldx * (thin ? 4 : 2));   // (thin, and few narrow matrices from here on: X in fp32)
     L.x0l = take(thin ? 0 : (size_t)N * r * ldx * 2);
     L.xh0 = take(thin ? 0 : x);
     L.xh1 = take(thin ? 0 : x);
@@ -1626,37 +1628,58 @@ int clusters_at_once(std::atomic<int> (&cache)[64], void (*kern)(NsArgs), int ct
     cache[dev].store(n + 1, std::memory_order_release);
     return n;
 }
-template <int S>
 int ns_small_clusters() {
     static std::atomic<int> cache[64];
-    return clusters_at_once(cache, ns_small_kernel<S>, 8, NS_THIN_THREADS, ns_small_smem<S>());
+    return clusters_at_once(cache, ns_small_kernel, 8, NS_THIN_THREADS, NS_SMALL_SMEM);
 }
 template <bool TWIN>
 int ns_pairs() {
     static std::atomic<int> cache[64];
     return clusters_at_once(cache, ns_kernel<TWIN>, 2, NS_THREADS, NS_SMEM);
 }
-// Whether the cluster kernel is the faster one for N matrices m x n: times (us, five steps) of both,
-// fitted to measurements at m of 64, 100 and 128, n of 64 to 2048, N of 1 to 128.  One 64 x 2048: 51
-// against 104 on the tensor cores, 32 of them 80 and 178, 128 of 64 x 64 149 and 86; 8 of 2048 x 100 135
-// and 175, of 100 x 512 88 and 100, 32 of 128 x 512 256 and 116.
+// Whether the cluster kernel is the faster one for N matrices m x n: times (us, five steps of the default
+// quintic) of both, fitted to measurements at m of 40 and 64, n of 64 to 4096, N of 1 to 100.  Cluster
+// kernel and tensor cores: one 64 x 64 37 and 69, one 64 x 2048 73 and 104, 32 of them 120 and 180, 64
+// 232 and 213; 64 of 64 x 64 96 and 77; 18 of 4096 x 64 201 and 191.
 bool ns_small_pays(int N, int m, int n, bool tall) {
-    if (m <= NS_THIN || m > 128) return false;
-    const int at_once = m <= 64 ? ns_small_clusters<64>() : ns_small_clusters<128>();
+    if (m <= NS_THIN || m > NS_SMALL) return false;
+    const int at_once = ns_small_clusters();
     if (at_once <= 0) return false;
+    // two CTAs per SM; up to a quarter as many clusters have an SM per CTA; up to 512 columns stay on chip
     const int full = N / at_once, rest = N - full * at_once;
-    float here = 5.0f, tensor;
-    if (m <= 64) {   // two CTAs per SM; half as many clusters have an SM per CTA
-        here += full * (36.0f + 0.0177f * n);
-        if (rest > 0) here += 2 * rest <= at_once ? 26.0f + 0.0105f * n : 36.0f + 0.0177f * n;
-        tensor = 68.0f + 0.017f * n + N * (0.06f + 0.0013f * n);
-    } else {
-        here += (full + (rest > 0 ? 1 : 0)) * (80.0f + 0.025f * n);
-        tensor = (tall ? 92.0f + 0.032f * n : 80.0f + 0.017f * n) + N * (0.05f + 0.0017f * n);
-    }
+    const float here = 5.0f + full * (48.0f + 0.041f * fmaxf(0.f, n - 450.0f)) +
+                       (rest == 0 ? 0.f : 4 * rest <= at_once ? 32.0f + 0.0227f * fmaxf(0.f, n - 430.0f)
+                                                               : 48.0f + 0.041f * fmaxf(0.f, n - 450.0f));
+    const float tensor = tall ? 68.0f + 0.016f * n + N * (0.08f + 0.00072f * n)
+                              : 68.0f + 0.017f * n + (N >= NS_TWIN_MIN ? 0.7f : 1.0f) * N * (0.12f + 0.00115f * n);
     return here < tensor;
 }
 }  // namespace
+
+// Largest values over a step's singular values in [0, s]: each lies at the end of the interval or where
+// the derivative is zero.
+NsBounds ns_bounds(const float* coef, double s) {
+    const double a = coef[0], b = coef[1], c = coef[2], t = s * s;
+    NsBounds r;
+    auto b_of = [&](double u) { return fabs(b * u + c * u * u); };
+    auto gain_of = [&](double u) { return fabs(a + b * u + c * u * u); };
+    const double v = c != 0.0 ? -b / (2.0 * c) : -1.0;
+    r.b = b_of(t);
+    r.gain = fmax(gain_of(0.0), gain_of(t));
+    if (v > 0.0 && v < t) {
+        r.b = fmax(r.b, b_of(v));
+        r.gain = fmax(r.gain, gain_of(v));
+    }
+    r.largest = s * gain_of(t);
+    // (a + 3 b u + 5 c u^2 = 0; one root by a quotient that c = 0 leaves finite)
+    const double disc = 9.0 * b * b - 20.0 * a * c;
+    if (disc >= 0.0) {
+        const double q = -0.5 * (3.0 * b + copysign(sqrt(disc), b));
+        for (const double u : {q != 0.0 ? a / q : -1.0, c != 0.0 ? q / (5.0 * c) : -1.0})
+            if (u > 0.0 && u < t) r.largest = fmax(r.largest, sqrt(u) * gain_of(u));
+    }
+    return r;
+}
 
 cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t limit_ns, cudaStream_t s) {
     const NsLayout L = ns_layout(q.N, q.r, q.c);
@@ -1687,7 +1710,8 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     a.u.prog = reinterpret_cast<int32_t*>(ws + L.prog);
     a.xh[0] = reinterpret_cast<__half*>(ws + L.x0h);
     a.xl[0] = reinterpret_cast<__half*>(ws + L.x0l);
-    const bool thin = a.m <= NS_THIN, small = !thin && a.m <= 128 && ns_small_pays(a.N, a.m, a.tall ? a.r : a.c, a.tall);
+    a.X1 = reinterpret_cast<float*>(ws + L.x0h);
+    const bool thin = a.m <= NS_THIN, small = ns_small_pays(a.N, a.m, a.tall ? a.r : a.c, a.tall);
 
     a.steps = q.steps;
     int stage = 0;
@@ -1704,6 +1728,14 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
         }
     }
     a.n_stages = stage;
+    double largest = 1.0, growth = 1.0;   // singular value of X; of roundings in A since the segment began
+    for (int it = 0; it < q.steps; ++it) {
+        const NsBounds b = ns_bounds(q.coef + 3 * it, largest);
+        a.restart[it] = it > 0 && !(growth <= NS_GROWTH);
+        if (a.restart[it]) growth = 1.0;
+        growth *= b.gain > 1.0 ? b.gain * b.gain : 1.0;
+        largest = b.largest;
+    }
     // X's lo part is read by the next step's a X term, unless it counts 0 times there, and, with three
     // terms, by its products whatever a is.
     for (int it = 0; it + 1 < q.steps; ++it) a.lo_keep[it] = a.terms == 3 ? 1.0f : a.lo_coef[it + 1];
@@ -1731,12 +1763,9 @@ cudaError_t launch_newton_schulz(const NsCall& q, uint8_t* ws, int sms, uint64_t
     cudaError_t e;
     if (thin || small) {
         if ((e = prologue()) != cudaSuccess) return e;
-        if (small && a.m <= 64) {
-            NsClusterLaunch l(a.N, 8, ns_small_smem<64>(), s);
-            e = cudaLaunchKernelEx(&l.cfg, ns_small_kernel<64>, a);
-        } else if (small) {
-            NsClusterLaunch l(a.N, 8, ns_small_smem<128>(), s);
-            e = cudaLaunchKernelEx(&l.cfg, ns_small_kernel<128>, a);
+        if (small) {
+            NsClusterLaunch l(a.N, 8, NS_SMALL_SMEM, s);
+            e = cudaLaunchKernelEx(&l.cfg, ns_small_kernel, a);
         } else {
             // CTAs of a matrix: one per 128 columns, up to about eight CTAs per SM in all
             const int n = a.tall ? a.r : a.c, room = 8 * sms / a.N;

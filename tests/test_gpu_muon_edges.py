@@ -7,7 +7,7 @@ import torch
 
 from paper_2608_17402_gb300 import moevie
 from tests._gpu import check_status
-from tests.test_gpu_muon import COEF, REL, _check, _f64, _ns64, _run
+from tests.test_gpu_muon import COEF, REL, _check, _f64, _ns64, _rel, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -216,3 +216,42 @@ def test_small_square_matrices(N, r, c):
     moevie.moevie_muon_update(W, M, G, ws, lr=1.0, momentum=0.0, scale=-1.0)
     check_status(ws)
     _check(W, U, [COEF] * 5)
+
+
+@pytest.mark.parametrize("steps", [6, 7, 10])
+@pytest.mark.parametrize("N,r,c,rank", [(16, 25, 95, 1), (2, 32, 2048, 4), (3, 114, 16, 1), (1, 32, 8192, 2), (300, 24, 1500, 3),
+                                        (2, 50, 520, 1), (1, 64, 300, 8), (1, 64, 2048, 3), (1, 2048, 60, 5),
+                                        (3, 33, 40, 1)])
+def test_many_steps_of_low_rank_in_32_bits(N, r, c, rank, steps):
+    """Thin and few narrow matrices, in fp32.  X's null directions hold roundings of 2^-24 from every
+    step, which the steps after it multiply by a: a^steps 2^-24 sqrt(3) from the first one, 1.4 times
+    that from all, several operations a step; 2^-21 a^steps of a result of 0.7 to 1.2 allows for six."""
+    g = torch.Generator(device="cuda").manual_seed(N * r + c + steps)
+    U = torch.randn(N, r, rank, generator=g, device="cuda") @ torch.randn(N, rank, c, generator=g, device="cuda")
+    got, want = _f64(_run(U, steps=steps)), _f64(U)
+    for e in range(N):
+        w = _ns64(want[e], [COEF] * steps)
+        assert _rel(got[e], w) <= REL + 2.0 ** -21 * COEF[0] ** steps, (e, _rel(got[e], w))
+
+
+@pytest.mark.parametrize("steps", [6, 7])
+@pytest.mark.parametrize("N,r,c,rank", [(2, 100, 520, 1), (1, 128, 2048, 3), (1, 2048, 100, 5), (70, 120, 300, 2)])
+def test_many_steps_of_low_rank_in_22_bits(N, r, c, rank, steps):
+    """The same where X is carried in 22 bits: four times the rounding and half as many operations."""
+    g = torch.Generator(device="cuda").manual_seed(N * r + c + steps)
+    U = torch.randn(N, r, rank, generator=g, device="cuda") @ torch.randn(N, rank, c, generator=g, device="cuda")
+    got, want = _f64(_run(U, steps=steps)), _f64(U)
+    for e in range(N):
+        w = _ns64(want[e], [COEF] * steps)
+        assert _rel(got[e], w) <= REL + 2.0 ** -20 * COEF[0] ** steps, (e, _rel(got[e], w))
+
+
+@pytest.mark.parametrize("N,r,c", [(16, 25, 95), (2, 32, 2048), (50, 3, 3), (1, 32, 8192), (2, 50, 520), (1, 64, 2048),
+                                   (1, 2048, 60), (3, 64, 64)])
+def test_many_steps_in_32_bits(N, r, c):
+    """Full rank and up to 32 steps: nothing is null, so REL, which has room for the roundings of a
+    step (1e-6) times the slopes of those after it."""
+    g = torch.Generator(device="cuda").manual_seed(N * r + c)
+    U = torch.randn(N, r, c, generator=g, device="cuda")
+    for coefs in ([COEF] * 12, [(1.5, -0.5, 0.0)] * 32):
+        _check(_run(U, steps=len(coefs), coef=coefs), U, coefs)
