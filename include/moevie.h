@@ -369,6 +369,119 @@ moevie_status moevie_muon_update(float* W, void* W_bf16, float* M, const float* 
                                  int nesterov, float weight_decay, float scale, const float* coef, int steps,
                                  void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------ a residual block's steps around the layer
+ *
+ * Between the layer f = y(u) and the next one a block norms, gates and adds (Sec. 2.1: the layer
+ * takes the place of the MLP in a pre-norm block):
+ *     r1 = residual_scale r + gate * N_post(f),      u = N_pre(r1).
+ * N is an RMS norm, N(x) = x / sqrt(mean(x^2) + eps) w + b, or a layer norm, which first subtracts
+ * the row's mean.  The gate has d values for every run of tokens: one run (LayerScale), or one for
+ * each image or clip (a gate that a condition modulates). */
+#define MOEVIE_NORM_NONE 0
+#define MOEVIE_NORM_RMS 1
+#define MOEVIE_NORM_LAYER 2
+
+typedef struct moevie_norms {
+    int64_t d;              /* d % 8 == 0, d <= 8192 */
+    int32_t pre, post;      /* MOEVIE_NORM_*: N_pre, N_post */
+    const float* w_pre;     /* fp32 [d] each; NULL: 1 for w, 0 for b */
+    const float* b_pre;
+    const float* w_post;
+    const float* b_post;
+    const float* gate;      /* fp32 [G, d] or NULL: 1 */
+    const int32_t* seg;     /* int32 [G + 1], device: run g is rows [seg[g], seg[g + 1]); NULL: one run
+                             * of all rows (G = 1).  Ascending within [0, T] (else MOEVIE_ERR_DEVICE in the
+                             * status); runs may be empty.  Rows in front of seg[0] and from seg[G] on are
+                             * padding: never read, and left as they were in every output. */
+    int64_t G;
+    float residual_scale;   /* finite */
+    float eps;              /* > 0, finite */
+} moevie_norms;
+
+/* Rows [T, d] of one of three types; an MOEVIE_Q8 is an 8-bit checkpoint (moevie_checkpoint_store). */
+#define MOEVIE_BF16 0
+#define MOEVIE_F32 1
+#define MOEVIE_Q8 2
+typedef struct moevie_rows {
+    const void* data;       /* bf16, fp32, or int8 codes */
+    const float* scale;     /* MOEVIE_Q8: fp32 [T, ceil(d / 128)]; ignored otherwise */
+    int32_t type;
+} moevie_rows;
+
+/* 8-bit checkpoint of activations x [T, d] (bf16, or fp32 where x_f32): of each row every block of 128
+ * columns (the last one what is left) keeps amax = max |x| as scale = amax / 127 in fp32 and its values as
+ * int8 codes, the whole number nearest to 127 x / amax (an even one between two, decided exactly).  A
+ * value is code * scale, off by at most amax / 254 and a rounding.  A block whose values all lie below
+ * 2^-110 is kept as zeros; one that holds an infinity or a NaN comes back as NaN.  d % 8 == 0;
+ * codes: int8 [T, d], 16-byte aligned; scale: fp32 [T, ceil(d / 128)].  moevie_checkpoint_load writes the
+ * values as bf16 or fp32.  T == 0 launches nothing. */
+moevie_status moevie_checkpoint_store(const void* x, int x_f32, int64_t T, int64_t d, int8_t* codes, float* scale,
+                                      void* stream);
+moevie_status moevie_checkpoint_load(const int8_t* codes, const float* scale, int64_t T, int64_t d, void* x,
+                                     int x_f32, void* stream);
+
+/* The step forward.  r: the residual stream (bf16 or fp32); f: the layer's output, bf16.  Outputs: r_out,
+ * of r's type (may be r itself), u bf16 [T, d], and where not NULL the statistics that the backward
+ * takes, stats_pre and stats_post fp32 [T, 2]: mean (0 for an RMS norm) and 1 / sqrt(... + eps) of each
+ * row.  All arithmetic is fp32, u is normed from r1 before its rounding to bf16, and each output is
+ * rounded once.
+ *   f == NULL: the stream's first norm, u = N_pre(r); r may then be an MOEVIE_Q8 (the layer's input formed
+ *   again for its backward); r_out is not written.
+ *   pre == MOEVIE_NORM_NONE: no u (NULL): the stream's last step.  post == MOEVIE_NORM_NONE: N_post(f) = f.
+ *   save_r, save_f (with their scales; NULL: not wanted): 8-bit checkpoints of r and f, what
+ *   moevie_checkpoint_store gives for them, written while they are read for the last time.
+ * ws: moevie_residual_norm_workspace_size(T_max, d, G) bytes, set up with moevie_workspace_init.
+ * T < 2^31, G < 2^31; T == 0 launches nothing. */
+moevie_status moevie_residual_norm_workspace_size(int64_t T_max, int64_t d, int64_t G, size_t* bytes);
+moevie_status moevie_residual_norm(const moevie_norms* n, const moevie_rows* r, const void* f, int64_t T, void* r_out,
+                                   void* u, float* stats_pre, float* stats_post, int8_t* save_r, float* save_r_scale,
+                                   int8_t* save_f, float* save_f_scale, void* ws, size_t ws_bytes, void* stream);
+
+/* Its backward: from dr1 (the gradient of r1 but for what comes through u; of the residual stream's type,
+ * fp32 where res_f32, else bf16; NULL: zero) and du (the gradient of u, fp32 where du_f32, e.g. dx of
+ * moevie_moe_backward, else bf16; NULL with pre == MOEVIE_NORM_NONE):
+ *     dR = dr1 + the gradient that N_pre passes on,   dr = residual_scale dR,
+ *     df = the gradient that N_post passes on from gate * dR,
+ * and the gradients of w_pre, b_pre, w_post, b_post [d] and gate [G, d], fp32 (each NULL: not wanted).
+ * r1 and f are the forward's rows, or their checkpoints (MOEVIE_Q8); r1 whole is of the residual stream's
+ * type, f whole is bf16.  stats_pre, stats_post: as the forward wrote them.  dr is of dr1's type and may be
+ * dr1 itself; df is bf16, dy of moevie_moe_backward.
+ *   df == NULL: the forward ran without f; f, stats_post and the gradients of w_post, b_post and gate
+ *   are then NULL, and dr = dR.  f may be NULL where post == MOEVIE_NORM_NONE and dgate is not wanted.
+ * Sums over rows are fp32, in an order that goes by T, d and the runs alone: the same call gives
+ * the same bits.  Rows outside every run do not enter them; a run without rows gets a zero dgate.
+ * T == 0 launches nothing.  ws as for moevie_residual_norm. */
+moevie_status moevie_residual_norm_backward(const moevie_norms* n, const void* dr1, int res_f32, const void* du,
+                                            int du_f32, const moevie_rows* r1, const moevie_rows* f,
+                                            const float* stats_pre, const float* stats_post, int64_t T, void* dr,
+                                            void* df, float* dw_pre, float* db_pre, float* dw_post, float* db_post,
+                                            float* dgate, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------ balance loss
+ *
+ * The auxiliary loss that the loss-free bias (moevie_update_bias) stands in for, for training with
+ * both or with it alone.  s fp32 [T, E] (rows ld_s apart): the router's logits; idx int32 [T, k]: the
+ * selection (e.g. moevie_routing.idx).  Over every run b of T_b tokens (seg, G as in moevie_norms; NULL: one
+ * run of all tokens; one run for each sequence balances each by itself), with n_be the ids of its tokens
+ * that are e and p_te = softmax(s_t)_e (MOEVIE_SCORE_SOFTMAX) or sigmoid(s_te) / sum_j sigmoid(s_tj)
+ * (MOEVIE_SCORE_SIGMOID, the scores behind Eqs. 4-5):
+ *     loss = coef sum_b (T_b / T) sum_e (E n_be / (k T_b)) (mean over the run of p_te),
+ * T the tokens of all runs: coef for loads that are even.  The counts carry no gradient.  Outputs: loss fp32
+ * [1], counts int32 [G, E], and ds fp32 [T, E] (rows ld_ds apart; NULL: not wanted; may be s itself with
+ * ld_ds = ld_s), the gradient of loss, which moevie_moe_backward_balanced takes.  Rows outside every run are
+ * neither read nor written.  A logit of minus infinity has no probability; a row of nothing else adds
+ * nothing, its ds is zero; a NaN, or plus infinity under a softmax, gives NaN in its row and in loss.  An id
+ * outside [0, E) is not counted, and is MOEVIE_ERR_DEVICE in the status, as are runs that do not ascend
+ * within [0, T].  fp32 arithmetic; the same call gives the same bits.  1 <= k <= E <= 1024, T k < 2^31, else
+ * MOEVIE_ERR_UNSUPPORTED.  T == 0: loss and counts are zeros.  ws: moevie_balance_workspace_size(T_max, E, k,
+ * G_max) bytes, set up with moevie_workspace_init. */
+#define MOEVIE_SCORE_SOFTMAX 0
+#define MOEVIE_SCORE_SIGMOID 1
+moevie_status moevie_balance_workspace_size(int64_t T_max, int64_t E, int64_t k, int64_t G, size_t* bytes);
+moevie_status moevie_balance_loss(const float* s, int64_t ld_s, const int32_t* idx, int64_t T, int64_t E, int64_t k,
+                                  const int32_t* seg, int64_t G, int score, float coef, float* loss, int32_t* counts,
+                                  float* ds, int64_t ld_ds, void* ws, size_t ws_bytes, void* stream);
+
 /* Synchronise `stream`, then read the workspace's device status into *out
  * (MOEVIE_OK when no device-side error was recorded).  `detail` (host, may be
  * NULL) receives 4 ints: code, site, and two values describing the failure. */

@@ -1127,6 +1127,290 @@ moevie_status moevie_muon_update(float* W, void* W_bf16, float* M, const float* 
                                             static_cast<cudaStream_t>(stream)));
 }
 
+// ------------------------------------------- a residual block's steps around the layer
+
+namespace {
+
+constexpr int64_t NORM_MAX_D = 8192;   // one CTA of 1024 threads holds a row
+
+inline bool is_finite(float v) { return fabsf(v) <= 3.402823466e38f; }
+inline bool a4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+inline bool a8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+
+moevie_status check_rows_sizes(int64_t T, int64_t d) {
+    if (T < 0 || d <= 0) return MOEVIE_ERR_INVALID_ARG;
+    if (d % 8 != 0 || T >= (int64_t(1) << 31) || d >= (int64_t(1) << 24)) return MOEVIE_ERR_UNSUPPORTED;
+    return MOEVIE_OK;
+}
+
+moevie_status check_norm_sizes(int64_t T, int64_t d, int64_t G) {
+    const moevie_status c = check_rows_sizes(T, d);
+    if (c != MOEVIE_OK) return c;
+    if (G < 1) return MOEVIE_ERR_INVALID_ARG;
+    return d > NORM_MAX_D || G >= (int64_t(1) << 31) ? MOEVIE_ERR_UNSUPPORTED : MOEVIE_OK;
+}
+
+moevie_status check_norms(const moevie_norms* n, int64_t T) {
+    if (!n) return MOEVIE_ERR_INVALID_ARG;
+    const moevie_status c = check_norm_sizes(T, n->d, n->G);
+    if (c != MOEVIE_OK) return c;
+    for (const int32_t kind : {n->pre, n->post})
+        if (kind < MOEVIE_NORM_NONE || kind > MOEVIE_NORM_LAYER) return MOEVIE_ERR_INVALID_ARG;
+    if (!is_finite(n->residual_scale) || !is_finite(n->eps) || !(n->eps > 0.f)) return MOEVIE_ERR_INVALID_ARG;
+    if (!n->seg && n->G != 1) return MOEVIE_ERR_INVALID_ARG;
+    if (!a4(n->seg)) return MOEVIE_ERR_INVALID_ARG;
+    for (const float* p : {n->w_pre, n->b_pre, n->w_post, n->b_post, n->gate})
+        if (!a16(p)) return MOEVIE_ERR_INVALID_ARG;
+    return MOEVIE_OK;
+}
+
+// Rows that a call reads: present, of a type it takes, aligned.
+bool rows_ok(const moevie_rows* r, bool f32_ok, bool bf16_ok, bool q8_ok) {
+    if (!r || !r->data || !a16(r->data)) return false;
+    if (r->type == MOEVIE_F32) return f32_ok;
+    if (r->type == MOEVIE_BF16) return bf16_ok;
+    return r->type == MOEVIE_Q8 && q8_ok && r->scale && a4(r->scale);
+}
+
+struct NormLayout {
+    size_t rec_pre, rec_post, group_runs, total;
+};
+NormLayout norm_layout(int64_t T, int64_t d, int64_t G) {
+    NormLayout L;
+    const size_t n = (size_t)norm_groups(T, (int)d);
+    size_t o = sizeof(DevStatus);
+    L.rec_pre = o;
+    o += up256(n * 2 * d * 4);
+    L.rec_post = o;
+    o += up256((n + (size_t)G - 1) * 2 * d * 4);
+    L.group_runs = o;
+    o += up256(n * sizeof(int2));
+    L.total = o;
+    return L;
+}
+
+moevie_status check_balance(int64_t T, int64_t E, int64_t k, int64_t G) {
+    const moevie_status c = check_sizes(T, 8, E, k, 0, 0);
+    if (c != MOEVIE_OK) return c;
+    if (G < 1) return MOEVIE_ERR_INVALID_ARG;
+    return G >= (int64_t(1) << 31) ? MOEVIE_ERR_UNSUPPORTED : MOEVIE_OK;
+}
+
+struct BalanceLayout {
+    size_t part, cta_sum, total;
+};
+BalanceLayout balance_layout(int64_t T, int64_t E, int64_t k, int64_t G) {
+    BalanceLayout L;
+    size_t o = sizeof(DevStatus);
+    L.cta_sum = o;
+    o += up256(BAL_MAX_GRID * sizeof(double2));
+    L.part = o;
+    o += up256((size_t)bal_max_parts(T, k, G) * E * 4);
+    L.total = o;
+    return L;
+}
+
+}  // namespace
+
+moevie_status moevie_checkpoint_store(const void* x, int x_f32, int64_t T, int64_t d, int8_t* codes, float* scale,
+                                      void* stream) {
+    const moevie_status c = check_rows_sizes(T, d);
+    if (c != MOEVIE_OK) return c;
+    if (x_f32 != 0 && x_f32 != 1) return MOEVIE_ERR_INVALID_ARG;
+    if (T == 0) return MOEVIE_OK;
+    if (!x || !codes || !scale || !a16(x) || !a16(codes) || !a4(scale)) return MOEVIE_ERR_INVALID_ARG;
+    return cuda_status(launch_q8_store(x, x_f32, T, (int)d, codes, scale, static_cast<cudaStream_t>(stream)));
+}
+
+moevie_status moevie_checkpoint_load(const int8_t* codes, const float* scale, int64_t T, int64_t d, void* x,
+                                     int x_f32, void* stream) {
+    const moevie_status c = check_rows_sizes(T, d);
+    if (c != MOEVIE_OK) return c;
+    if (x_f32 != 0 && x_f32 != 1) return MOEVIE_ERR_INVALID_ARG;
+    if (T == 0) return MOEVIE_OK;
+    if (!x || !codes || !scale || !a16(x) || !a16(codes) || !a4(scale)) return MOEVIE_ERR_INVALID_ARG;
+    return cuda_status(launch_q8_load(codes, scale, T, (int)d, x, x_f32, static_cast<cudaStream_t>(stream)));
+}
+
+moevie_status moevie_residual_norm_workspace_size(int64_t T_max, int64_t d, int64_t G, size_t* bytes) {
+    if (!bytes) return MOEVIE_ERR_INVALID_ARG;
+    const moevie_status c = check_norm_sizes(T_max, d, G);
+    if (c != MOEVIE_OK) return c;
+    *bytes = norm_layout(T_max, d, G).total;
+    return MOEVIE_OK;
+}
+
+moevie_status moevie_residual_norm(const moevie_norms* n, const moevie_rows* r, const void* f, int64_t T, void* r_out,
+                                   void* u, float* stats_pre, float* stats_post, int8_t* save_r, float* save_r_scale,
+                                   int8_t* save_f, float* save_f_scale, void* ws, size_t ws_bytes, void* stream) {
+    moevie_status c = check_norms(n, T);
+    if (c != MOEVIE_OK) return c;
+    const bool join = f != nullptr, norm = n->pre != MOEVIE_NORM_NONE;
+    if (!join && !norm) return MOEVIE_ERR_INVALID_ARG;   // nothing to do
+    if (T == 0) return MOEVIE_OK;
+    if (!rows_ok(r, true, true, !join && !save_r) || !ws || !a16(ws)) return MOEVIE_ERR_INVALID_ARG;
+    if (join && (!a16(f) || !r_out || !a16(r_out))) return MOEVIE_ERR_INVALID_ARG;
+    if (norm != (u != nullptr) || !a16(u)) return MOEVIE_ERR_INVALID_ARG;
+    if (!a8(stats_pre) || !a8(stats_post)) return MOEVIE_ERR_INVALID_ARG;
+    if (save_r && (!a16(save_r) || !save_r_scale || !a4(save_r_scale))) return MOEVIE_ERR_INVALID_ARG;
+    if (save_f && (!join || !a16(save_f) || !save_f_scale || !a4(save_f_scale))) return MOEVIE_ERR_INVALID_ARG;
+    if (ws_bytes < norm_layout(T, n->d, n->G).total) return MOEVIE_ERR_WORKSPACE;
+    NormArgs a = {};
+    a.r = r->data;
+    a.r_scale = r->scale;
+    a.r_q8 = r->type == MOEVIE_Q8;
+    a.f = static_cast<const __nv_bfloat16*>(f);
+    a.r_out = r_out;
+    a.u = static_cast<__nv_bfloat16*>(u);
+    a.w_pre = n->w_pre;
+    a.b_pre = n->b_pre;
+    a.w_post = n->post == MOEVIE_NORM_NONE ? nullptr : n->w_post;
+    a.b_post = n->post == MOEVIE_NORM_NONE ? nullptr : n->b_post;
+    a.gate = n->gate;
+    a.seg = n->seg;
+    a.stats_pre = reinterpret_cast<float2*>(stats_pre);
+    a.stats_post = reinterpret_cast<float2*>(stats_post);
+    a.qr = save_r;
+    a.qr_scale = save_r_scale;
+    a.qf = save_f;
+    a.qf_scale = save_f_scale;
+    a.st = static_cast<DevStatus*>(ws);
+    a.T = T;
+    a.G = n->G;
+    a.d = (int)n->d;
+    a.pre = n->pre;
+    a.post = n->post;
+    a.alpha = n->residual_scale;
+    a.eps = n->eps;
+    return cuda_status(launch_norm_forward(a, r->type == MOEVIE_F32, static_cast<cudaStream_t>(stream)));
+}
+
+moevie_status moevie_residual_norm_backward(const moevie_norms* n, const void* dr1, int res_f32, const void* du,
+                                            int du_f32, const moevie_rows* r1, const moevie_rows* f,
+                                            const float* stats_pre, const float* stats_post, int64_t T, void* dr,
+                                            void* df, float* dw_pre, float* db_pre, float* dw_post, float* db_post,
+                                            float* dgate, void* ws, size_t ws_bytes, void* stream) {
+    moevie_status c = check_norms(n, T);
+    if (c != MOEVIE_OK) return c;
+    if ((res_f32 != 0 && res_f32 != 1) || (du_f32 != 0 && du_f32 != 1)) return MOEVIE_ERR_INVALID_ARG;
+    const bool join = df != nullptr, norm = n->pre != MOEVIE_NORM_NONE, post = join && n->post != MOEVIE_NORM_NONE;
+    if (T == 0) return MOEVIE_OK;
+    if (!dr || !a16(dr) || !a16(dr1) || !a16(df) || !ws || !a16(ws)) return MOEVIE_ERR_INVALID_ARG;
+    if (!join && !norm) return MOEVIE_ERR_INVALID_ARG;
+    if (norm ? !du || !a16(du) || !stats_pre || !a8(stats_pre) || !rows_ok(r1, res_f32 != 0, res_f32 == 0, true)
+             : du || dw_pre || db_pre || !dr1)
+        return MOEVIE_ERR_INVALID_ARG;
+    if (!post && (dw_post || db_post)) return MOEVIE_ERR_INVALID_ARG;
+    if (dgate && (!join || !n->gate)) return MOEVIE_ERR_INVALID_ARG;
+    if (post && (!stats_post || !a8(stats_post))) return MOEVIE_ERR_INVALID_ARG;
+    const bool read_f = post || dgate;
+    if (read_f && !rows_ok(f, false, true, true)) return MOEVIE_ERR_INVALID_ARG;
+    for (const float* p : {dw_pre, db_pre, dw_post, db_post, dgate})
+        if (!a4(p)) return MOEVIE_ERR_INVALID_ARG;
+    const NormLayout L = norm_layout(T, n->d, n->G);
+    if (ws_bytes < L.total) return MOEVIE_ERR_WORKSPACE;
+    NormBwdArgs a = {};
+    a.dr1 = dr1;
+    a.du = du;
+    if (norm) {
+        a.r1 = r1->data;
+        a.r1_scale = r1->scale;
+        a.r_q8 = r1->type == MOEVIE_Q8;
+        a.w_pre = n->w_pre;
+        a.stats_pre = reinterpret_cast<const float2*>(stats_pre);
+    }
+    if (read_f) {
+        a.f = f->data;
+        a.f_scale = f->scale;
+        a.f_q8 = f->type == MOEVIE_Q8;
+    }
+    if (post) {
+        a.w_post = n->w_post;
+        a.stats_post = reinterpret_cast<const float2*>(stats_post);
+    }
+    a.gate = n->gate;
+    a.seg = n->seg;
+    a.dr = dr;
+    a.df = static_cast<__nv_bfloat16*>(df);
+    a.rec_pre = dw_pre || db_pre ? at<float>(ws, L.rec_pre) : nullptr;
+    a.rec_post = dw_post || db_post || dgate ? at<float>(ws, L.rec_post) : nullptr;
+    a.group_runs = at<int2>(ws, L.group_runs);
+    a.st = static_cast<DevStatus*>(ws);
+    a.T = T;
+    a.G = n->G;
+    a.d = (int)n->d;
+    a.pre = n->pre;
+    a.post = post ? n->post : MOEVIE_NORM_NONE;
+    a.alpha = join ? n->residual_scale : 1.0f;
+    NormSumArgs q = {};
+    q.rec_pre = a.rec_pre;
+    q.rec_post = a.rec_post;
+    q.gate = n->gate;
+    q.w_post = post ? n->w_post : nullptr;
+    q.b_post = post ? n->b_post : nullptr;
+    q.group_runs = a.group_runs;
+    q.seg = n->seg;
+    q.dw_pre = dw_pre;
+    q.db_pre = db_pre;
+    q.dw_post = dw_post;
+    q.db_post = db_post;
+    q.dgate = dgate;
+    q.T = T;
+    q.G = n->G;
+    q.d = (int)n->d;
+    return cuda_status(launch_norm_backward(a, res_f32, du_f32, q, static_cast<cudaStream_t>(stream)));
+}
+
+moevie_status moevie_balance_workspace_size(int64_t T_max, int64_t E, int64_t k, int64_t G, size_t* bytes) {
+    if (!bytes) return MOEVIE_ERR_INVALID_ARG;
+    const moevie_status c = check_balance(T_max, E, k, G);
+    if (c != MOEVIE_OK) return c;
+    *bytes = balance_layout(T_max, E, k, G).total;
+    return MOEVIE_OK;
+}
+
+moevie_status moevie_balance_loss(const float* s, int64_t ld_s, const int32_t* idx, int64_t T, int64_t E, int64_t k,
+                                  const int32_t* seg, int64_t G, int score, float coef, float* loss, int32_t* counts,
+                                  float* ds, int64_t ld_ds, void* ws, size_t ws_bytes, void* stream) {
+    const moevie_status c = check_balance(T, E, k, G);
+    if (c != MOEVIE_OK) return c;
+    if ((score != MOEVIE_SCORE_SOFTMAX && score != MOEVIE_SCORE_SIGMOID) || !is_finite(coef)) return MOEVIE_ERR_INVALID_ARG;
+    if (!seg && G != 1) return MOEVIE_ERR_INVALID_ARG;
+    if (!loss || !counts || !a4(loss) || !a4(counts) || !a4(seg)) return MOEVIE_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        MV_TRY(cudaMemsetAsync(loss, 0, 4, st));
+        MV_TRY(cudaMemsetAsync(counts, 0, 4 * (size_t)G * E, st));
+        return MOEVIE_OK;
+    }
+    if (!s || !idx || !ws || !a4(s) || !a4(idx) || !a4(ds) || !a16(ws)) return MOEVIE_ERR_INVALID_ARG;
+    if (ld_s < E || ld_s >= (int64_t(1) << 31) || (ds && (ld_ds < E || ld_ds >= (int64_t(1) << 31))))
+        return MOEVIE_ERR_INVALID_ARG;
+    if (ds == s && ld_ds != ld_s) return MOEVIE_ERR_INVALID_ARG;
+    const BalanceLayout L = balance_layout(T, E, k, G);
+    if (ws_bytes < L.total) return MOEVIE_ERR_WORKSPACE;
+    BalanceArgs a = {};
+    a.s = s;
+    a.idx = idx;
+    a.seg = seg;
+    a.loss = loss;
+    a.counts = counts;
+    a.ds = ds;
+    a.part = at<int32_t>(ws, L.part);
+    a.cta_sum = at<double2>(ws, L.cta_sum);
+    a.st = static_cast<DevStatus*>(ws);
+    a.T = T;
+    a.G = G;
+    a.ld_s = ld_s;
+    a.ld_ds = ld_ds;
+    a.E = (int)E;
+    a.k = (int)k;
+    a.parts = bal_parts(T, k, G);
+    a.score = score;
+    a.coef = coef;
+    return cuda_status(launch_balance(a, st));
+}
+
 moevie_status moevie_get_device_status(const void* ws, void* stream, moevie_status* out,
                                        int32_t* detail) {
     if (!ws || !out) return MOEVIE_ERR_INVALID_ARG;

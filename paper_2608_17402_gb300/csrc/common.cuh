@@ -26,7 +26,8 @@ struct DevStatus {
     int bar_gen;     //   and the barrier's generation (bumped by the last arrival)
     int pad0;
     unsigned long long few_arrivals;   // grid barriers of the few-token kernel: CTAs arrived so far
-    int pad[54];
+    unsigned bal_ticket;   // CTAs of the balance loss that are done (0 between calls)
+    int pad[53];
 };
 static_assert(sizeof(DevStatus) == 256, "status block is 256 bytes");
 
@@ -61,6 +62,8 @@ enum Site : int {
     SITE_FEW_DRAIN = 56,
     SITE_FEW_WAIT_Y = 57,
     SITE_FEW_WAIT_TURN = 58,
+    SITE_RUNS = 60,
+    SITE_BALANCE_ID = 61,
 };
 
 __device__ __forceinline__ void report(DevStatus* st, int code, int site, int a, int b) {

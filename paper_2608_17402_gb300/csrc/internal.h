@@ -472,4 +472,80 @@ cudaError_t launch_combine(const __nv_bfloat16* rows, const int32_t* inv, const 
                            __nv_bfloat16* y, cudaStream_t s);
 cudaError_t launch_wait_probe(DevStatus* st, uint64_t limit_ns, cudaStream_t s);
 
+
+// ----------------------------------------- residual norms and 8-bit checkpoints (norm.cu)
+
+constexpr int GB300_SMS = 152;   // grids and workspaces are sized for this many, whatever the device
+
+// r1 = alpha r + gate * N_post(f) (f == nullptr: r1 = r, not written), u = N_pre(r1) (u == nullptr: not wanted)
+struct NormArgs {
+    const void* r;
+    const float* r_scale;       // r_q8: r holds int8 codes, their scales [T][nb]
+    const __nv_bfloat16* f;
+    void* r_out;
+    __nv_bfloat16* u;
+    const float *w_pre, *b_pre, *w_post, *b_post;
+    const float* gate;          // [G][d] or nullptr
+    const int32_t* seg;         // [G + 1] or nullptr: one run of all T rows
+    float2 *stats_pre, *stats_post;
+    int8_t *qr, *qf;            // checkpoints of r and f, or nullptr
+    float *qr_scale, *qf_scale;
+    DevStatus* st;
+    int64_t T, G, n_groups;
+    int d, nb, gw, groups, pre, post, r_q8;
+    float alpha, eps;
+};
+struct NormBwdArgs {
+    const void *dr1, *du, *r1, *f;
+    const float *r1_scale, *f_scale;   // r_q8, f_q8: their rows are int8 codes
+    const float2 *stats_pre, *stats_post;
+    const float *w_pre, *w_post, *gate;
+    const int32_t* seg;
+    void* dr;
+    __nv_bfloat16* df;
+    float* rec_pre;             // [n_groups][2][d]: dw_pre, db_pre of every group; nullptr: not wanted
+    float* rec_post;            // [n_groups + G - 1][2][d]: A, B of group gid in run g at g + gid; nullptr: not wanted
+    int2* group_runs;           // [n_groups]: first and last run of every group (G > 1)
+    DevStatus* st;
+    int64_t T, G, n_groups;
+    int d, nb, gw, groups, pre, post, r_q8, f_q8;
+    float alpha;
+};
+struct NormSumArgs {
+    const float *rec_pre, *rec_post, *gate, *w_post, *b_post;
+    const int2* group_runs;
+    const int32_t* seg;
+    float *dw_pre, *db_pre, *dw_post, *db_post, *dgate;
+    int64_t T, G, n_groups;
+    int d;
+};
+int64_t norm_groups(int64_t T, int d);   // row groups of norm_backward_kernel: its records
+cudaError_t launch_norm_forward(NormArgs a, int r_f32, cudaStream_t s);
+cudaError_t launch_norm_backward(NormBwdArgs a, int r_f32, int du_f32, NormSumArgs sums, cudaStream_t s);
+cudaError_t launch_q8_store(const void* x, int x_f32, int64_t T, int d, int8_t* codes, float* scales, cudaStream_t s);
+cudaError_t launch_q8_load(const int8_t* codes, const float* scales, int64_t T, int d, void* x, int x_f32,
+                           cudaStream_t s);
+
+// ----------------------------------------- balance loss (balance.cu)
+
+constexpr int BAL_MAX_PARTS = 32;   // CTAs that count one run's ids
+struct BalanceArgs {
+    const float* s;
+    const int32_t* idx;
+    const int32_t* seg;     // [G + 1] or nullptr
+    float* loss;
+    int32_t* counts;        // [G][E]
+    float* ds;              // or nullptr
+    int32_t* part;          // [G][parts][E] counts of parts of a run
+    double2* cta_sum;       // [grid]: sum of p . c and number of rows with a probability
+    DevStatus* st;
+    int64_t T, G, ld_s, ld_ds;
+    int E, k, parts, score;
+    float coef;
+};
+int bal_parts(int64_t T, int64_t k, int64_t G);
+int64_t bal_max_parts(int64_t T, int64_t k, int64_t G);   // of all runs, for up to T tokens and G runs
+constexpr int BAL_MAX_GRID = GB300_SMS * 2;
+cudaError_t launch_balance(const BalanceArgs& a, cudaStream_t s);
+
 }  // namespace mv

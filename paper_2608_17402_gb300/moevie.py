@@ -30,6 +30,9 @@ C_ENTRY_POINTS = ("moevie_status_string", "moevie_version", "moevie_workspace_si
                   "moevie_update_bias", "moevie_backward_workspace_size", "moevie_moe_backward",
                   "moevie_few_workspace_size", "moevie_moe_few",
                   "moevie_orthogonalize_workspace_size", "moevie_orthogonalize", "moevie_muon_update",
+                  "moevie_checkpoint_store", "moevie_checkpoint_load", "moevie_residual_norm_workspace_size",
+                  "moevie_residual_norm", "moevie_residual_norm_backward", "moevie_balance_workspace_size",
+                  "moevie_balance_loss",
                   "moevie_test_route_logits",
                   "moevie_test_fallback_count", "moevie_test_expert_hidden",
                   "moevie_test_moe_forward_events", "moevie_test_wait_timeout")
@@ -52,6 +55,17 @@ class _Layer(ctypes.Structure):
 class _Routing(ctypes.Structure):
     _fields_ = [("idx", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("counts", ctypes.c_void_p),
                 ("offsets", ctypes.c_void_p), ("perm", ctypes.c_void_p), ("inv", ctypes.c_void_p)]
+
+
+class _Norms(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int64), ("pre", ctypes.c_int32), ("post", ctypes.c_int32),
+                ("w_pre", ctypes.c_void_p), ("b_pre", ctypes.c_void_p), ("w_post", ctypes.c_void_p),
+                ("b_post", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("seg", ctypes.c_void_p),
+                ("G", ctypes.c_int64), ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("type", ctypes.c_int32)]
 
 
 def load():
@@ -90,6 +104,15 @@ def load():
                                  ctypes.c_int),
         "moevie_muon_update": ([P] * 4 + [I64] * 5 + [F, F, ctypes.c_int, F, F, P, ctypes.c_int, P, SZ, P],
                                ctypes.c_int),
+        "moevie_checkpoint_store": ([P, ctypes.c_int, I64, I64, P, P, P], ctypes.c_int),
+        "moevie_checkpoint_load": ([P, P, I64, I64, P, ctypes.c_int, P], ctypes.c_int),
+        "moevie_residual_norm_workspace_size": ([I64] * 3 + [P], ctypes.c_int),
+        "moevie_residual_norm": ([P, P, P, I64] + [P] * 9 + [SZ, P], ctypes.c_int),
+        "moevie_residual_norm_backward": ([P, P, ctypes.c_int, P, ctypes.c_int, P, P, P, P, I64] + [P] * 8 + [SZ, P],
+                                          ctypes.c_int),
+        "moevie_balance_workspace_size": ([I64] * 4 + [P], ctypes.c_int),
+        "moevie_balance_loss": ([P, I64, P, I64, I64, I64, P, I64, ctypes.c_int, F, P, P, P, I64, P, SZ, P],
+                                ctypes.c_int),
         "moevie_test_route_logits": ([P, P, I64, I64, I64, P, P, SZ, P], ctypes.c_int),
         "moevie_test_fallback_count": ([P, P, P], ctypes.c_int),
         "moevie_test_expert_hidden": ([P, P, P, P, I64, I64, I64, I64, I64, P, P, SZ, P],
@@ -550,6 +573,324 @@ def moevie_muon_update(W, M, G, ws: OrthoWorkspace, lr, momentum=0.95, weight_de
           float(momentum), int(bool(nesterov)), float(weight_decay), float(s), _coef(coef, steps), steps, ws.ptr,
           ws.nbytes, _stream(stream))
     return W
+
+
+# ------------------------------- a residual block's steps around the layer
+
+_KINDS = {None: 0, "rms": 1, "layer": 2}
+_SCORES = {"softmax": 0, "sigmoid": 1}
+_ROW_TYPES = {torch.bfloat16: 0, torch.float32: 1}
+Q8_BLOCK = 128   # columns that share a scale
+
+
+def _rows(t, shape, dtypes, name):
+    """``t`` as a contiguous CUDA tensor of ``shape`` on the current device."""
+    if not (t.is_cuda and t.dtype in dtypes and t.is_contiguous() and t.shape == shape):
+        raise ValueError(f"{name}: expected a contiguous CUDA tensor {tuple(shape)} of {dtypes}, got {t.dtype} on "
+                         f"{t.device} with shape {tuple(t.shape)} and strides {t.stride()}")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+    return t
+
+
+_BF16, _F32, _I32, _I8 = (torch.bfloat16,), (torch.float32,), (torch.int32,), (torch.int8,)
+_RES = (torch.bfloat16, torch.float32)
+
+
+@dataclass
+class Checkpoint:
+    """Activations [T, d] in 8 bits (moevie_checkpoint_store): int8 codes, and for every row and 128
+    columns an fp32 scale."""
+    codes: torch.Tensor   # int8 [T, d]
+    scale: torch.Tensor   # fp32 [T, ceil(d / 128)]
+
+    @classmethod
+    def empty(cls, T, d, device="cuda"):
+        return cls(torch.empty((T, d), dtype=torch.int8, device=device),
+                   torch.empty((T, -(-d // Q8_BLOCK)), dtype=torch.float32, device=device))
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    def check(self, shape, name):
+        _rows(self.codes, shape, _I8, name + ".codes")
+        _rows(self.scale, (shape[0], -(-shape[1] // Q8_BLOCK)), _F32, name + ".scale")
+        return self
+
+
+def moevie_checkpoint_store(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
+    """The 8-bit checkpoint of x [T, d] (bf16 or fp32), in ``out`` where given."""
+    if x.dim() != 2:
+        raise ValueError(f"x: expected [T, d], got {tuple(x.shape)}")
+    _rows(x, x.shape, _RES, "x")
+    T, d = x.shape
+    out = Checkpoint.empty(T, d, x.device) if out is None else out.check(x.shape, "out")
+    _call("moevie_checkpoint_store", _p(x), int(x.dtype == torch.float32), T, d, _p(out.codes), _p(out.scale),
+          _stream(stream))
+    return out
+
+
+def moevie_checkpoint_load(ck: Checkpoint, dtype=torch.bfloat16, out=None, stream=None):
+    """The values of a checkpoint as bf16 or fp32 [T, d] (``out``'s type where it is given)."""
+    shape = ck.codes.shape
+    ck.check(shape, "ck")
+    out = torch.empty(shape, dtype=dtype, device=ck.codes.device) if out is None else out
+    _rows(out, shape, _RES, "out")
+    _call("moevie_checkpoint_load", _p(ck.codes), _p(ck.scale), shape[0], shape[1], _p(out),
+          int(out.dtype == torch.float32), _stream(stream))
+    return out
+
+
+@dataclass
+class ResidualNorm:
+    """A block's norms, gate and residual scale (moevie_norms): r1 = residual_scale r + gate * N_post(f),
+    u = N_pre(r1).  ``pre`` and ``post``: "rms", "layer" or None.  Weights and biases fp32 [d] (None: 1 and 0);
+    gate fp32 [G, d] (None: 1) for the G runs of rows seg[g] to seg[g + 1] (int32 [G + 1]; None: one run of all)."""
+    d: int
+    pre: str | None = "layer"
+    post: str | None = None
+    w_pre: torch.Tensor | None = None
+    b_pre: torch.Tensor | None = None
+    w_post: torch.Tensor | None = None
+    b_post: torch.Tensor | None = None
+    gate: torch.Tensor | None = None
+    seg: torch.Tensor | None = None
+    residual_scale: float = 1.0
+    eps: float = 1e-6
+
+    @property
+    def G(self):
+        return 1 if self.seg is None else self.seg.numel() - 1
+
+    def c_struct(self) -> _Norms:
+        d, G = self.d, self.G
+        for name in ("w_pre", "b_pre", "w_post", "b_post"):
+            t = getattr(self, name)
+            if t is not None:
+                _rows(t, (d,), _F32, name)
+        if self.seg is not None:
+            _rows(self.seg, (G + 1,), _I32, "seg")
+        if self.gate is not None:
+            _rows(self.gate, (G, d), _F32, "gate")
+        return _Norms(d, _KINDS[self.pre], _KINDS[self.post], *(None if t is None else t.data_ptr() for t in (
+            self.w_pre, self.b_pre, self.w_post, self.b_post, self.gate, self.seg)), G, self.residual_scale, self.eps)
+
+
+def moevie_residual_norm_workspace_size(T_max, d, G=1) -> int:
+    out = ctypes.c_size_t(0)
+    _call("moevie_residual_norm_workspace_size", T_max, d, G, ctypes.byref(out))
+    return out.value
+
+
+class ResidualNormWorkspace(Workspace):
+    """Caller-owned device scratch of moevie_residual_norm and its backward (up to ``T_max`` rows, ``G`` runs)."""
+
+    def __init__(self, T_max, d, G=1, device="cuda", stream=None):
+        self.dims = (T_max, d, G)
+        self.nbytes = moevie_residual_norm_workspace_size(T_max, d, G)
+        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        moevie_workspace_init(self, stream)
+
+
+@dataclass
+class ResidualNormOut:
+    """What moevie_residual_norm gives; a member that the call has no use for is None."""
+    r: torch.Tensor | None            # r1 [T, d], of the residual stream's type
+    u: torch.Tensor | None            # bf16 [T, d]
+    stats_pre: torch.Tensor | None    # fp32 [T, 2]: mean and 1 / deviation of every row
+    stats_post: torch.Tensor | None
+    save_r: Checkpoint | None = None
+    save_f: Checkpoint | None = None
+
+    @classmethod
+    def empty(cls, norms: ResidualNorm, T, dtype=torch.bfloat16, save=False, join=True, device="cuda"):
+        d = norms.d
+
+        def stats(kind):
+            return torch.empty((T, 2), dtype=torch.float32, device=device) if kind else None
+
+        return cls(torch.empty((T, d), dtype=dtype, device=device) if join else None,
+                   torch.empty((T, d), dtype=torch.bfloat16, device=device) if norms.pre else None,
+                   stats(norms.pre), stats(norms.post if join else None),
+                   Checkpoint.empty(T, d, device) if save else None, Checkpoint.empty(T, d, device) if save and join else None)
+
+
+def _rows_struct(t, shape, dtypes, name):
+    if isinstance(t, Checkpoint):
+        t.check(shape, name)
+        return _Rows(t.codes.data_ptr(), t.scale.data_ptr(), 2)
+    _rows(t, shape, dtypes, name)
+    return _Rows(t.data_ptr(), None, _ROW_TYPES[t.dtype])
+
+
+def _matrix(t, d, name):
+    if len(t.shape) != 2 or t.shape[1] != d:
+        raise ValueError(f"{name}: expected [T, {d}], got {tuple(t.shape)}")
+    return t.shape
+
+
+def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, out: ResidualNormOut | None = None,
+                         save=False, stream=None) -> ResidualNormOut:
+    """r1 = residual_scale r + gate * N_post(f), u = N_pre(r1); r bf16 or fp32 [T, d], f bf16 [T, d] or None
+    (then u = N_pre(r), and r may be a Checkpoint).  ``save``: also the 8-bit checkpoints of r and f.
+    ``out``: a ResidualNormOut whose buffers are written (its members say what is wanted; out.r may be r)."""
+    N = norms.c_struct()
+    shape = _matrix(r, norms.d, "r")
+    T = shape[0]
+    R = _rows_struct(r, shape, _RES, "r")
+    if f is not None:
+        _rows(f, shape, _BF16, "f")
+    if out is None:
+        out = ResidualNormOut.empty(norms, T, r.dtype if R.type != 2 else torch.bfloat16, save, f is not None,
+                                    ws.buf.device)
+    o = out
+    if f is not None:
+        _rows(o.r, shape, (r.dtype,) if R.type != 2 else _RES, "out.r")
+    if o.u is not None:
+        _rows(o.u, shape, _BF16, "out.u")
+    for name, t in (("out.stats_pre", o.stats_pre), ("out.stats_post", o.stats_post)):
+        if t is not None:
+            _rows(t, (T, 2), _F32, name)
+    for name, t in (("out.save_r", o.save_r), ("out.save_f", o.save_f)):
+        if t is not None:
+            t.check(shape, name)
+    qr, qf = o.save_r, o.save_f
+    _call("moevie_residual_norm", ctypes.byref(N), ctypes.byref(R), _p(f), T, _p(o.r if f is not None else None),
+          _p(o.u), _p(o.stats_pre), _p(o.stats_post), _p(qr and qr.codes), _p(qr and qr.scale), _p(qf and qf.codes),
+          _p(qf and qf.scale), ws.ptr, ws.nbytes, _stream(stream))
+    return out
+
+
+@dataclass
+class ResidualNormGrads:
+    """What moevie_residual_norm_backward gives (None: not wanted)."""
+    dr: torch.Tensor
+    df: torch.Tensor | None
+    dw_pre: torch.Tensor | None = None
+    db_pre: torch.Tensor | None = None
+    dw_post: torch.Tensor | None = None
+    db_post: torch.Tensor | None = None
+    dgate: torch.Tensor | None = None
+
+    @classmethod
+    def empty(cls, norms: ResidualNorm, T, dtype=torch.bfloat16, join=True, device="cuda"):
+        def like(t):
+            return None if t is None else torch.empty_like(t)
+
+        post = join and norms.post
+        return cls(torch.empty((T, norms.d), dtype=dtype, device=device),
+                   torch.empty((T, norms.d), dtype=torch.bfloat16, device=device) if join else None,
+                   *(like(t) for t in ((norms.w_pre, norms.b_pre) if norms.pre else (None, None))),
+                   *(like(t) for t in ((norms.w_post, norms.b_post) if post else (None, None))),
+                   like(norms.gate if join else None))
+
+
+def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, stats_post,
+                                  ws: ResidualNormWorkspace, out: ResidualNormGrads | None = None,
+                                  stream=None) -> ResidualNormGrads:
+    """Gradients of moevie_residual_norm.  dr [T, d]: the gradient of r1 but for what comes through u, of the
+    residual stream's type (None: zero); du: the gradient of u, fp32 (dx of moevie_moe_backward) or bf16 (None
+    where norms.pre is None); r (r1) and f: the forward's rows or their Checkpoints; stats as the forward gave
+    them.  A None for f where norms has a post norm or a gate means that the forward ran without f.  Returns
+    dr (may be the given one, as out.dr), df bf16 and the gradients of norms' weights, fp32."""
+    N = norms.c_struct()
+    d = norms.d
+    shape = _matrix(dr if dr is not None else du, d, "dr" if dr is not None else "du")
+    T = shape[0]
+    join = f is not None if out is None else out.df is not None
+    if out is None:
+        dtype = dr.dtype if dr is not None else r.dtype if isinstance(r, torch.Tensor) else torch.bfloat16
+        out = ResidualNormGrads.empty(norms, T, dtype, join, ws.buf.device)
+    o = out
+    _rows(o.dr, shape, _RES, "out.dr")
+    if dr is not None:
+        _rows(dr, shape, (o.dr.dtype,), "dr")
+    if du is not None:
+        _rows(du, shape, _RES, "du")
+    R = _rows_struct(r, shape, (o.dr.dtype,), "r") if r is not None else None
+    Fr = _rows_struct(f, shape, _BF16, "f") if f is not None else None
+    for name, t in (("stats_pre", stats_pre), ("stats_post", stats_post)):
+        if t is not None:
+            _rows(t, (T, 2), _F32, name)
+    if o.df is not None:
+        _rows(o.df, shape, _BF16, "out.df")
+    for name, t in (("dw_pre", o.dw_pre), ("db_pre", o.db_pre), ("dw_post", o.dw_post), ("db_post", o.db_post)):
+        if t is not None:
+            _rows(t, (d,), _F32, "out." + name)
+    if o.dgate is not None:
+        _rows(o.dgate, (norms.G, d), _F32, "out.dgate")
+    _call("moevie_residual_norm_backward", ctypes.byref(N), _p(dr), int(o.dr.dtype == torch.float32), _p(du),
+          int(du is not None and du.dtype == torch.float32), ctypes.byref(R) if R is not None else None,
+          ctypes.byref(Fr) if Fr is not None else None, _p(stats_pre), _p(stats_post), T, _p(o.dr), _p(o.df),
+          _p(o.dw_pre), _p(o.db_pre), _p(o.dw_post), _p(o.db_post), _p(o.dgate), ws.ptr, ws.nbytes, _stream(stream))
+    return out
+
+
+# ------------------------------------------------------------- balance loss
+
+def moevie_balance_workspace_size(T_max, E, k, G=1) -> int:
+    out = ctypes.c_size_t(0)
+    _call("moevie_balance_workspace_size", T_max, E, k, G, ctypes.byref(out))
+    return out.value
+
+
+class BalanceWorkspace(Workspace):
+    """Caller-owned device scratch of moevie_balance_loss (up to ``T_max`` tokens and ``G`` runs)."""
+
+    def __init__(self, T_max, E, k, G=1, device="cuda", stream=None):
+        self.dims = (T_max, E, k, G)
+        self.nbytes = moevie_balance_workspace_size(T_max, E, k, G)
+        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        moevie_workspace_init(self, stream)
+
+
+@dataclass
+class BalanceOut:
+    """What moevie_balance_loss gives."""
+    loss: torch.Tensor            # fp32 [1]
+    counts: torch.Tensor          # int32 [G, E]
+    ds: torch.Tensor | None       # fp32 [T, E], the gradient of the logits (None: not wanted)
+
+    @classmethod
+    def empty(cls, T, E, G=1, grad=True, device="cuda"):
+        return cls(torch.empty(1, dtype=torch.float32, device=device),
+                   torch.empty((G, E), dtype=torch.int32, device=device),
+                   torch.empty((T, E), dtype=torch.float32, device=device) if grad else None)
+
+
+def _logits(t, shape, name):
+    """An fp32 CUDA tensor [T, E] with consecutive columns -> its row stride."""
+    if not (t.is_cuda and t.dtype == torch.float32 and t.shape == shape and (shape[1] <= 1 or t.stride(1) == 1)):
+        raise ValueError(f"{name}: expected an fp32 CUDA tensor {tuple(shape)} with consecutive columns, got {t.dtype} "
+                         f"on {t.device} with shape {tuple(t.shape)} and strides {t.stride()}")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+    return max(shape[1], t.stride(0)) if shape[0] > 1 else shape[1]
+
+
+def moevie_balance_loss(s, idx, ws: BalanceWorkspace, coef=0.01, score="sigmoid", seg=None,
+                        out: BalanceOut | None = None, grad=True, stream=None) -> BalanceOut:
+    """The auxiliary loss of expert loads over every run of tokens (seg int32 [G + 1]; None: one run), from the
+    router's logits s fp32 [T, E] and the selection idx int32 [T, k], with the loads (counts) and ds, the gradient
+    of s.  ``score``: "sigmoid" (the layer's, divided by their sum) or "softmax"."""
+    if s.dim() != 2 or idx.dim() != 2:
+        raise ValueError(f"expected s [T, E] and idx [T, k], got {tuple(s.shape)} and {tuple(idx.shape)}")
+    T, E = s.shape
+    k = idx.shape[1]
+    ld = _logits(s, s.shape, "s")
+    _rows(idx, (T, k), _I32, "idx")
+    G = 1 if seg is None else seg.numel() - 1
+    if seg is not None:
+        _rows(seg, (G + 1,), _I32, "seg")
+    if out is None:
+        out = BalanceOut.empty(T, E, G, grad, s.device)
+    _rows(out.loss, (1,), _F32, "out.loss")
+    _rows(out.counts, (G, E), _I32, "out.counts")
+    ldd = _logits(out.ds, s.shape, "out.ds") if out.ds is not None else 0
+    _call("moevie_balance_loss", _p(s), ld, _p(idx), T, E, k, _p(seg), G, _SCORES[score], float(coef), _p(out.loss),
+          _p(out.counts), _p(out.ds), ldd, ws.ptr, ws.nbytes, _stream(stream))
+    return out
 
 
 def moevie_launch_count() -> int:
