@@ -22,7 +22,42 @@ namespace {
 constexpr int MAX_GROUPS = 8;      // row groups of a CTA
 constexpr float Q8_LEAST = 7.70371978e-34f;   // 2^-110: blocks of smaller values are kept as zeros
 
-// ------------------------------------------------------------ rows of 8 columns
+// ------------------------------------------------------------ 8 columns of a row
+
+// 8 fp32 values as four register pairs, for the two-wide fp32 instructions.
+struct P8 {
+    uint64_t p[4];
+};
+
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t f2_of(float v) { return f2_pack(v, v); }
+__device__ __forceinline__ uint64_t f2_bits(uint32_t lo, uint32_t hi) {
+    return f2_pack(__uint_as_float(lo), __uint_as_float(hi));
+}
+__device__ __forceinline__ P8 p8_of(float v) {
+    P8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.p[i] = f2_of(v);
+    return r;
+}
+// the sum of all eight, and of the products of two eights
+__device__ __forceinline__ float p8_sum(const P8& a) {
+    float x, y;
+    f2_unpack(f2_add(f2_add(a.p[0], a.p[1]), f2_add(a.p[2], a.p[3])), x, y);
+    return x + y;
+}
+__device__ __forceinline__ float p8_dot(const P8& a, const P8& b) {
+    uint64_t s = f2_mul(a.p[0], b.p[0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) s = f2_fma(a.p[i], b.p[i], s);
+    float x, y;
+    f2_unpack(s, x, y);
+    return x + y;
+}
 
 __device__ __forceinline__ uint4 ld16(const void* p) {
     uint4 r;
@@ -36,131 +71,117 @@ __device__ __forceinline__ uint2 ld8(const void* p) {
     asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
     return r;
 }
-// 8 fp32 values; rows start 16 bytes apart
-__device__ __forceinline__ void ld_f8(const float* p, float (&v)[8]) {
-    const uint4 a = ld16(p), b = ld16(p + 4);
-    v[0] = __uint_as_float(a.x), v[1] = __uint_as_float(a.y), v[2] = __uint_as_float(a.z), v[3] = __uint_as_float(a.w);
-    v[4] = __uint_as_float(b.x), v[5] = __uint_as_float(b.y), v[6] = __uint_as_float(b.z), v[7] = __uint_as_float(b.w);
-}
-__device__ __forceinline__ void st_f8(float* p, const float (&v)[8]) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void st_b8(__nv_bfloat16* p, const float (&v)[8]) {
-    uint4 u;
-    u.x = pack_bf16x2(v[0], v[1]);
-    u.y = pack_bf16x2(v[2], v[3]);
-    u.z = pack_bf16x2(v[4], v[5]);
-    u.w = pack_bf16x2(v[6], v[7]);
-    *reinterpret_cast<uint4*>(p) = u;
-}
-// n values of an optional vector (NULL: `other` everywhere)
-__device__ __forceinline__ void ld_param(const float* p, int col, bool act, float other, float (&v)[8]) {
-    if (p && act) {
-        ld_f8(p + col, v);
-    } else {
+__device__ __forceinline__ P8 p8_bf16(const uint4& u) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    P8 r;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = other;
-    }
+    for (int i = 0; i < 4; ++i) r.p[i] = f2_bits(w[i] << 16, w[i] & 0xffff0000u);
+    return r;
 }
-
-// 8 columns as they lie in memory: bf16 (raw.x .. w), fp32 (all of it) or codes (raw.x, raw.y) with
-// their block's scale.
-template <bool F32>
-struct Raw;
-template <>
-struct Raw<false> {
-    uint4 a;
-    float scale;
-};
-template <>
-struct Raw<true> {
-    uint4 a, b;
-    float scale;
-};
-
-template <bool F32>
-__device__ __forceinline__ void ld_whole(const void* base, int64_t at, Raw<F32>& raw) {
-    if constexpr (F32) {
-        const float* p = static_cast<const float*>(base) + at;
-        raw.a = ld16(p);
-        raw.b = ld16(p + 4);
-    } else {
-        raw.a = ld16(static_cast<const __nv_bfloat16*>(base) + at);
-    }
+__device__ __forceinline__ P8 p8_f32(const uint4& a, const uint4& b) {
+    P8 r;
+    r.p[0] = f2_bits(a.x, a.y), r.p[1] = f2_bits(a.z, a.w);
+    r.p[2] = f2_bits(b.x, b.y), r.p[3] = f2_bits(b.z, b.w);
+    return r;
 }
-template <bool F32>
-__device__ __forceinline__ void ld_codes(const void* base, int64_t at, const float* scale, int64_t sat, Raw<F32>& raw) {
-    const uint2 c = ld8(static_cast<const int8_t*>(base) + at);
-    raw.a.x = c.x;
-    raw.a.y = c.y;
-    asm volatile("ld.global.f32 %0, [%1];" : "=f"(raw.scale) : "l"(scale + sat));
-}
-template <bool F32>
-__device__ __forceinline__ void whole_values(const Raw<F32>& raw, float (&v)[8]) {
-    if constexpr (F32) {
-        v[0] = __uint_as_float(raw.a.x), v[1] = __uint_as_float(raw.a.y);
-        v[2] = __uint_as_float(raw.a.z), v[3] = __uint_as_float(raw.a.w);
-        v[4] = __uint_as_float(raw.b.x), v[5] = __uint_as_float(raw.b.y);
-        v[6] = __uint_as_float(raw.b.z), v[7] = __uint_as_float(raw.b.w);
-    } else {
-        unpack_bf16x8(raw.a, v);
-    }
-}
-__device__ __forceinline__ void code_values(uint32_t lo, uint32_t hi, float scale, float (&v)[8]) {
+// int8 codes times their scale: a code + 128 as the low byte of 2^23 is a float that is off by 2^23 + 128
+__device__ __forceinline__ P8 p8_codes(uint32_t lo, uint32_t hi, float scale) {
+    const uint32_t w[2] = {lo ^ 0x80808080u, hi ^ 0x80808080u};
+    const uint64_t off = f2_of(-8388736.0f), s = f2_of(scale);
+    P8 r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        v[i] = (float)(int8_t)(lo >> (8 * i)) * scale;
-        v[4 + i] = (float)(int8_t)(hi >> (8 * i)) * scale;
+        const uint32_t x = w[i / 2];
+        const uint64_t v = f2_bits(__byte_perm(x, 0x4b000000u, 0x7540 + 2 * (i & 1)),
+                                   __byte_perm(x, 0x4b000000u, 0x7541 + 2 * (i & 1)));
+        r.p[i] = f2_mul(f2_add(v, off), s);
     }
+    return r;
+}
+__device__ __forceinline__ void st_f32(float* p, const P8& v) {
+    reinterpret_cast<ulonglong2*>(p)[0] = make_ulonglong2(v.p[0], v.p[1]);
+    reinterpret_cast<ulonglong2*>(p)[1] = make_ulonglong2(v.p[2], v.p[3]);
+}
+__device__ __forceinline__ void st_bf16(__nv_bfloat16* p, const P8& v) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x, y;
+        f2_unpack(v.p[i], x, y);
+        w[i] = pack_bf16x2(x, y);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <bool F32>
+__device__ __forceinline__ void st_rows(void* base, int64_t at, const P8& v) {
+    if constexpr (F32) st_f32(static_cast<float*>(base) + at, v);
+    else st_bf16(static_cast<__nv_bfloat16*>(base) + at, v);
+}
+// 8 of an optional vector (NULL: `other` everywhere), zeros behind a row's end
+__device__ __forceinline__ P8 ld_param(const float* p, int col, bool act, float other) {
+    if (!p || !act) return p8_of(act ? other : 0.f);
+    return p8_f32(ld16(p + col), ld16(p + col + 4));
 }
 
 // ------------------------------------------------------------ 8-bit checkpoints
 
-// The whole number nearest to 127 x / amax, an even one between two.  y is that value in fp32, off
-// by less than 2^-15: where it is that near to a border, 254 x and (2 n + 1) amax, both exact in
+// The whole number nearest to 127 x / amax, an even one between two, where y, that value in fp32
+// (off by less than 2^-15), is too near to a border to tell: 254 x and (2 n + 1) amax, both exact in
 // fp64, decide.
-__device__ __forceinline__ float q8_code(float x, float y, float amax) {
-    float q = rintf(y);
-    if (fabsf(y - q) > 0.4999f) {
-        const float n = floorf(y);
-        const double t = 254.0 * (double)x - (2.0 * (double)n + 1.0) * (double)amax;
-        const bool even = ((int)n & 1) == 0;
-        q = (t > 0.0 || (t == 0.0 && !even)) ? n + 1.0f : n;
-    }
-    return q;
+__device__ __noinline__ float q8_border(float x, float y, float amax) {
+    const float n = floorf(y);
+    const double t = 254.0 * (double)x - (2.0 * (double)n + 1.0) * (double)amax;
+    const bool even = ((int)n & 1) == 0;
+    return (t > 0.0 || (t == 0.0 && !even)) ? n + 1.0f : n;
 }
 
 // Codes of this thread's 8 columns and the scale of the block of 128 that 16 threads share (all of
 // them here).  A block that holds an infinity or a NaN gets scale NaN; one whose values all lie
 // below 2^-110 is kept as zeros.
-__device__ __forceinline__ uint2 q8_block(const float (&x)[8], bool act, float& scale) {
+__device__ __forceinline__ uint2 q8_block(const P8& v, bool act, float& scale) {
+    constexpr float R127 = 1.0f / 127.0f;
+    constexpr float ROUND = 12582912.0f;   // 1.5 * 2^23: adding it rounds to a whole number, whose low byte it shows
+    float x[8];
     uint32_t m = 0;   // the bits of |x| order as the values do, infinities and NaN above them
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f2_unpack(v.p[i], x[2 * i], x[2 * i + 1]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
     if (!act) m = 0;
 #pragma unroll
     for (int o = 8; o; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    uint2 c = make_uint2(0u, 0u);
-    if (m >= 0x7f800000u) {
-        scale = __uint_as_float(0x7fffffffu);
-        return c;
-    }
     const float amax = __uint_as_float(m);
-    if (amax < Q8_LEAST) {
-        scale = 0.f;
-        return c;
+    if (m >= 0x7f800000u || amax < Q8_LEAST) {
+        scale = m >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : 0.f;
+        return make_uint2(0u, 0u);
     }
-    const float inv = 127.0f / amax;
-    scale = amax / 127.0f;
+    float inv;   // good to 2^-22, which q8_border's test allows for
+    asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(amax));
+    inv *= 127.0f;
+    // amax / 127, correctly rounded (Markstein: the remainder of a quotient within one unit corrects it)
+    const float guess = amax * R127;
+    scale = fmaf(fmaf(-127.0f, guess, amax), R127, guess);
+    uint32_t q[8];
+    bool border = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        c.x |= ((uint32_t)(int)q8_code(x[i], x[i] * inv, amax) & 0xffu) << (8 * i);
-        c.y |= ((uint32_t)(int)q8_code(x[4 + i], x[4 + i] * inv, amax) & 0xffu) << (8 * i);
+    for (int i = 0; i < 8; ++i) {
+        const float y = x[i] * inv, r = y + ROUND;
+        q[i] = __float_as_uint(r);
+        border |= fabsf(y - (r - ROUND)) > 0.4999f;
     }
+    if (border) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y = x[i] * inv;
+            if (fabsf(y - (__uint_as_float(q[i]) - ROUND)) > 0.4999f)
+                q[i] = __float_as_uint(q8_border(x[i], y, amax) + ROUND);
+        }
+    }
+    uint2 c;
+    c.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+    c.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
     return c;
 }
-
 
 // Blocks of 128 columns (the last one of a row may be shorter), 16 threads each; a thread takes
 // UNITS blocks at a time, their loads under way together.  Blocks are counted row by row; the ones
@@ -189,7 +210,7 @@ __global__ void __launch_bounds__(256) q8_store_kernel(const void* x, int64_t T,
     BlockWalk w((int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), nb);
     // a warp's two blocks leave the loop together: its shuffles need both
     while (__any_sync(0xffffffffu, w.row < T)) {
-        Raw<F32> raw[Q8_UNITS];
+        uint4 lo[Q8_UNITS], hi[Q8_UNITS];
         int64_t at[Q8_UNITS], sat[Q8_UNITS];
         bool act[Q8_UNITS];
 #pragma unroll
@@ -198,18 +219,21 @@ __global__ void __launch_bounds__(256) q8_store_kernel(const void* x, int64_t T,
             act[n] = w.row < T && col < d;
             at[n] = w.row * d + col;
             sat[n] = w.row < T ? w.row * nb + w.block : -1;
-            if (act[n]) ld_whole<F32>(x, at[n], raw[n]);
+            if (act[n]) {
+                if constexpr (F32) {
+                    lo[n] = ld16(static_cast<const float*>(x) + at[n]);
+                    hi[n] = ld16(static_cast<const float*>(x) + at[n] + 4);
+                } else {
+                    lo[n] = ld16(static_cast<const __nv_bfloat16*>(x) + at[n]);
+                }
+            }
             w.advance(step_rows, step_blocks, nb);
         }
 #pragma unroll
         for (int n = 0; n < Q8_UNITS; ++n) {
-            float v[8], scale;
-            if (act[n]) {
-                whole_values<F32>(raw[n], v);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = 0.f;
-            }
+            float scale;
+            P8 v = p8_of(0.f);
+            if (act[n]) v = F32 ? p8_f32(lo[n], hi[n]) : p8_bf16(lo[n]);
             const uint2 c = q8_block(v, act[n], scale);
             if (act[n]) *reinterpret_cast<uint2*>(codes + at[n]) = c;
             if (lane16 == 0 && sat[n] >= 0) scales[sat[n]] = scale;
@@ -240,71 +264,112 @@ __global__ void __launch_bounds__(256) q8_load_kernel(const int8_t* codes, const
 #pragma unroll
         for (int n = 0; n < Q8_UNITS; ++n) {
             if (at[n] < 0) continue;
-            float v[8];
-            code_values(c[n].x, c[n].y, scale[n], v);
-            if constexpr (F32)
-                st_f8(static_cast<float*>(x) + at[n], v);
-            else
-                st_b8(static_cast<__nv_bfloat16*>(x) + at[n], v);
+            st_rows<F32>(x, at[n], p8_codes(c[n].x, c[n].y, scale[n]));
         }
     }
 }
 
 // ------------------------------------------------------------ sums over a row
 
-// One row's warps: wi of gw, of group `group` of the CTA (named barrier group + 1).
+// A row's warps: wi of gw, of group `group` of the CTA (named barrier group + 1).
 struct RowGroup {
     int gw, wi, lane, group;
     int buf;        // which half of the group's shared memory the next sum takes
-    float* part;    // [2][2][32]
+    float* part;    // [2][32 warps][4], zeros behind the gw-th warp
 };
+constexpr int PART_HALF = 128, GROUP_PART = 2 * PART_HALF;
 
-__device__ __forceinline__ float warp_sum_f(float v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+__device__ __forceinline__ RowGroup row_group(int gw, float* s_part) {
+    RowGroup g;
+    g.lane = threadIdx.x & 31;
+    g.gw = gw;
+    g.group = (threadIdx.x >> 5) / gw;
+    g.wi = (threadIdx.x >> 5) - g.group * gw;
+    g.buf = 0;
+    g.part = s_part + g.group * GROUP_PART;
+    for (int i = g.wi * 32 + g.lane; i < GROUP_PART; i += gw * 32) g.part[i] = 0.f;
+    return g;
+}
+__device__ __forceinline__ void group_barrier(const RowGroup& g) {
+    asm volatile("bar.sync %0, %1;" ::"r"(g.group + 1), "r"(g.gw * 32) : "memory");
 }
 
-// v[n] <- the sum of v[n] over the row's threads, the same bits in all of them.  One barrier: a
-// warp that passes the next one's has read this one's half.
+// v[n] <- the sum of v[n] over the row's threads, the same bits in all of them; N = 1, 2 or 4.  The
+// sums share one set of shuffles: after the first steps each lane carries one of them, the n-th
+// lanes 32 n / N on.  One barrier: a warp that passes the next one's has read this one's half.
 template <int N>
 __device__ __forceinline__ void row_sum(RowGroup& g, float (&v)[N]) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = warp_sum_f(v[n]);
-    if (g.gw == 1) return;
-    float* p = g.part + g.buf * 64;
-    if (g.lane == 0) {
-#pragma unroll
-        for (int n = 0; n < N; ++n) p[n * 32 + g.wi] = v[n];
+    static_assert(N == 1 || N == 2 || N == 4, "");
+    constexpr int SPAN = 32 / N;   // lanes of one sum
+    float x;
+    if constexpr (N == 4) {
+        const bool up = g.lane & 16, up8 = g.lane & 8;
+        const float a = (up ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[2], 16);
+        const float b = (up ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, up ? v[1] : v[3], 16);
+        x = (up8 ? b : a) + __shfl_xor_sync(0xffffffffu, up8 ? a : b, 8);
+    } else if constexpr (N == 2) {
+        const bool up = g.lane & 16;
+        x = (up ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[1], 16);
+    } else {
+        x = v[0];
     }
-    asm volatile("bar.sync %0, %1;" ::"r"(g.group + 1), "r"(g.gw * 32) : "memory");
 #pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = warp_sum_f(g.lane < g.gw ? p[n * 32 + g.lane] : 0.f);
+    for (int o = SPAN / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (g.gw == 1) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = N == 1 ? x : __shfl_sync(0xffffffffu, x, SPAN * n);
+        return;
+    }
+    float* p = g.part + g.buf * PART_HALF;
+    if (g.lane % SPAN == 0) p[g.wi * N + g.lane / SPAN] = x;
+    group_barrier(g);
+    uint64_t s[2] = {0, 0};   // N = 1: sums of every other one; 2: the two; 4: the first and the second two
+#pragma unroll 1
+    for (int w = 0; w < g.gw; w += 4) {   // 4 warps
+        ulonglong2 q[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) q[i] = *reinterpret_cast<const ulonglong2*>(p + w * N + 4 * i);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s[0] = f2_add(s[0], q[i].x);
+            s[N == 4] = f2_add(s[N == 4], q[i].y);
+        }
+    }
+    f2_unpack(s[0], v[0], v[N > 1]);
+    if constexpr (N == 1) {
+        float x0, x1;
+        f2_unpack(s[0], x0, x1);
+        v[0] = x0 + x1;
+    }
+    if constexpr (N == 4) f2_unpack(s[1], v[2], v[3]);
     g.buf ^= 1;
 }
 
-// Mean (0 for an RMS norm) and 1 / sqrt(mean square about it + eps) of a row's values.
-__device__ __forceinline__ float2 row_stats(RowGroup& g, const float (&x)[8], bool act, int kind, float inv_d, float eps) {
-    float mean = 0.f;
+// Of each of the rows x: mean (0 for an RMS norm) and 1 / sqrt(mean square about it + eps); the rows
+// are left less their mean (columns behind a row's end, which are zeros here: anything).
+template <int ROWS>
+__device__ __forceinline__ void row_stats(RowGroup& g, P8 (&x)[ROWS], bool act, int kind, float inv_d, float eps,
+                                          float2 (&st)[ROWS]) {
+    float s[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) st[k].x = 0.f;
     if (kind == MOEVIE_NORM_LAYER) {
-        float s[1] = {0.f};
-        if (act) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[0] += x[i];
-        }
+        for (int k = 0; k < ROWS; ++k) s[k] = p8_sum(x[k]);
         row_sum(g, s);
-        mean = s[0] * inv_d;
-    }
-    float q[1] = {0.f};
-    if (act) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float z = x[i] - mean;
-            q[0] = fmaf(z, z, q[0]);
+        for (int k = 0; k < ROWS; ++k) {
+            st[k].x = s[k] * inv_d;
+            const uint64_t m = f2_of(-st[k].x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[k].p[i] = f2_add(x[k].p[i], m);
         }
     }
-    row_sum(g, q);
-    return make_float2(mean, rsqrtf(fmaf(q[0], inv_d, eps)));
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) s[k] = act ? p8_dot(x[k], x[k]) : 0.f;
+    row_sum(g, s);
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) st[k].y = rsqrtf(fmaf(s[k], inv_d, eps));
 }
 
 // ------------------------------------------------------------ runs of rows
@@ -341,19 +406,128 @@ __device__ __forceinline__ void clip_rows(const Args& a, int64_t& t0, int64_t& t
     t1 = min(t1, (int64_t)a.seg[a.G]);
 }
 
+// ------------------------------------------------------------ rows under way
+
+// A thread's share of the rows that are read: its own 8 columns of each operand, in pieces of 16
+// bytes that it copies into words of shared memory which no other thread touches.  So no barrier
+// stands between a copy and its use.  A row's slot is filled anew as soon as its values are in
+// registers: SLOTS rows are under way while one or two are worked on.
+template <int SLOTS, int PIECES>
+struct RowRing {
+    uint32_t base;   // shared address of this thread's first piece
+    uint32_t step;   // bytes between pieces
+    __device__ __forceinline__ RowRing(void* smem)
+        : base(smem_u32(smem) + threadIdx.x * 16u), step(blockDim.x * 16u) {}
+    __device__ __forceinline__ uint32_t at(int slot, int piece) const {
+        return base + (uint32_t)(slot * PIECES + piece) * step;
+    }
+    static __device__ __forceinline__ int next(int slot) { return slot + 1 == SLOTS ? 0 : slot + 1; }
+};
+__device__ __forceinline__ ulonglong2 ld_shared(uint32_t at) {
+    ulonglong2 r;
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(r.x), "=l"(r.y) : "r"(at) : "memory");
+    return r;
+}
+
+// 8 columns of weights that a thread keeps in words of shared memory of its own rather than in
+// registers, where the row in hand needs them.
+struct Kept {
+    uint32_t at, step;
+    __device__ __forceinline__ Kept(void* smem, int which)
+        : at(smem_u32(smem) + (which * 2 * blockDim.x + threadIdx.x) * 16u), step(blockDim.x * 16u) {}
+    __device__ __forceinline__ void set(const P8& v) const {
+        asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(at), "l"(v.p[0]), "l"(v.p[1]) : "memory");
+        asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(at + step), "l"(v.p[2]), "l"(v.p[3]) : "memory");
+    }
+    __device__ __forceinline__ P8 get() const {
+        P8 v;
+        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v.p[0]), "=l"(v.p[1]) : "r"(at) : "memory");
+        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v.p[2]), "=l"(v.p[3]) : "r"(at + step) : "memory");
+        return v;
+    }
+};
+constexpr int KEPT_BYTES = 64;   // two of them, for each thread
+
+// copies of 16, 8 and 4 bytes, of which `bytes` are read and the rest are zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src, int bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, int bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ P8 p8_bf16(const ulonglong2& u) {
+    return p8_bf16(make_uint4((uint32_t)u.x, (uint32_t)(u.x >> 32), (uint32_t)u.y, (uint32_t)(u.y >> 32)));
+}
+
+// One operand of a row: whole (F32 or bf16), or 8-bit codes with their scale behind them.
+template <bool F32>
+struct Operand {
+    const void* data;
+    const float* scale;
+    bool q8;
+    // 8 columns from element `at` on (their scale: element sat), zeros where not ok
+    template <typename Ring>
+    __device__ __forceinline__ void copy(const Ring& ring, int slot, int piece, int64_t at, int64_t sat, bool ok) const {
+        const uint32_t dst = ring.at(slot, piece);
+        if (q8) {
+            copy8(dst, static_cast<const int8_t*>(data) + (ok ? at : 0), ok ? 8 : 0);
+            copy4(dst + 8, scale + (ok ? sat : 0), ok ? 4 : 0);
+            return;
+        }
+        const char* p = static_cast<const char*>(data) + (ok ? at * (F32 ? 4 : 2) : 0);
+        copy16(dst, p, ok ? 16 : 0);
+        if constexpr (F32) copy16(ring.at(slot, piece + 1), p + (ok ? 16 : 0), ok ? 16 : 0);
+    }
+    template <typename Ring>
+    __device__ __forceinline__ P8 get(const Ring& ring, int slot, int piece) const {
+        const ulonglong2 a = ld_shared(ring.at(slot, piece));
+        if (q8) return p8_codes((uint32_t)a.x, (uint32_t)(a.x >> 32), __uint_as_float((uint32_t)a.y));
+        if constexpr (F32) {
+            const ulonglong2 b = ld_shared(ring.at(slot, piece + 1));
+            P8 r;
+            r.p[0] = a.x, r.p[1] = a.y, r.p[2] = b.x, r.p[3] = b.y;
+            return r;
+        } else {
+            return p8_bf16(a);
+        }
+    }
+    __device__ __forceinline__ P8 read(int64_t at, int64_t sat) const {   // without a ring
+        if (q8) {
+            const uint2 c = ld8(static_cast<const int8_t*>(data) + at);
+            float s;
+            asm volatile("ld.global.f32 %0, [%1];" : "=f"(s) : "l"(scale + sat));
+            return p8_codes(c.x, c.y, s);
+        }
+        if constexpr (F32) {
+            const float* p = static_cast<const float*>(data) + at;
+            return p8_f32(ld16(p), ld16(p + 4));
+        } else {
+            return p8_bf16(ld16(static_cast<const __nv_bfloat16*>(data) + at));
+        }
+    }
+};
+
 // ------------------------------------------------------------ forward
 
-template <bool F32, bool BIG>
-__global__ void __launch_bounds__(BIG ? 1024 : 512, BIG ? 1 : 2) norm_forward_kernel(const NormArgs a) {
-    __shared__ float s_part[MAX_GROUPS * 128];
+// Rows a CTA's threads work on at a time: two, whose sums share shuffles and barriers (one row at a
+// time took 400 us for 65536 x 1664 in fp32, bound by issued instructions), or one in the largest
+// CTAs, whose threads have 64 registers.
+constexpr int rows_at_once(int threads) { return threads == 1024 ? 1 : 2; }
+constexpr int fwd_slots(int threads) { return threads == 1024 ? 3 : 4; }
+constexpr int BWD_SLOTS = 2;
+
+// JOIN: r1 = alpha r + gate * N_post(f) and its norm; otherwise the norm of r alone.  SAVE: 8-bit
+// checkpoints of what is read.  THREADS: a CTA's at most.
+template <bool F32, bool JOIN, bool SAVE, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_kernel(const NormArgs a) {
+    constexpr int ROWS = rows_at_once(THREADS), SLOTS = fwd_slots(THREADS), PR = F32 ? 2 : 1, PIECES = PR + (JOIN ? 1 : 0);
+    extern __shared__ __align__(16) uint8_t s_dyn[];
+    __shared__ __align__(16) float s_part[MAX_GROUPS * GROUP_PART];
     pdl_wait();
-    RowGroup g;
-    g.lane = threadIdx.x & 31;
-    g.gw = a.gw;
-    g.group = (threadIdx.x >> 5) / a.gw;
-    g.wi = (threadIdx.x >> 5) - g.group * a.gw;
-    g.buf = 0;
-    g.part = s_part + g.group * 128;
+    RowGroup g = row_group(a.gw, s_part);
     if (a.seg) check_runs(a.seg, a.G, a.T, a.st);
     const int col = (g.wi * 32 + g.lane) * 8;
     const bool act = col < a.d;
@@ -363,81 +537,123 @@ __global__ void __launch_bounds__(BIG ? 1024 : 512, BIG ? 1 : 2) norm_forward_ke
     clip_rows(a, t0, t1);
     if (t0 >= t1) return;
 
-    const bool join = a.f != nullptr;
-    const float inv_d = 1.0f / (float)a.d;
-    float w1[8], b1[8];
-    ld_param(a.w_pre, col, act, 1.f, w1);
-    ld_param(a.b_pre, col, act, 0.f, b1);
-    float w2[8], b2[8];   // gate * weight, gate * bias
-    int64_t run = 0, run_end = t1;
-    bool fresh = true;
-
-    Raw<F32> rr;
-    uint4 rf = make_uint4(0u, 0u, 0u, 0u);
-    auto fetch = [&](int64_t t) {
-        if (!act) return;
-        const int64_t at = t * a.d + col;
-        if (a.r_q8) ld_codes<F32>(a.r, at, a.r_scale, t * a.nb + (col >> 7), rr);
-        else ld_whole<F32>(a.r, at, rr);
-        if (join) rf = ld16(a.f + at);
+    const RowRing<SLOTS, PIECES> ring(s_dyn + KEPT_BYTES * blockDim.x);
+    const Operand<F32> R{a.r, a.r_scale, !JOIN && a.r_q8};
+    const Operand<false> Fo{a.f, nullptr, false};
+    int slot = 0, fill = 0;
+    int64_t ahead = t0;
+    auto copy_row = [&]() {   // of row `ahead`
+        const bool ok = ahead < t1 && act;
+        const int64_t at = ahead * a.d + col;
+        R.copy(ring, fill, 0, at, ahead * a.nb + (col >> 7), ok);
+        if constexpr (JOIN) Fo.copy(ring, fill, PR, at, 0, ok);
+        cp_async_commit();
+        fill = ring.next(fill);
+        ++ahead;
     };
-    fetch(t0);
-    for (int64_t t = t0; t < t1; ++t) {
-        float r[8], x[8];
+#pragma unroll 1
+    for (int i = 0; i < SLOTS; ++i) copy_row();
+
+    const float inv_d = 1.0f / (float)a.d;
+    const Kept w1(s_dyn, 0), b1(s_dyn, 1);
+    w1.set(ld_param(a.w_pre, col, act, 1.f));
+    b1.set(ld_param(a.b_pre, col, act, 0.f));
+    P8 w2 = p8_of(0.f), b2 = p8_of(0.f);   // gate * weight, gate * bias
+    int64_t run = -1, run_end = t0;
+    if (g.gw > 1) group_barrier(g);   // the zeros of row_group
+
+#pragma unroll 1
+    for (int64_t t = t0; t < t1;) {
+        if (JOIN && t >= run_end) {   // the next run's gate, times the norm's weight and bias
+            run_end = t1;
+            if (a.seg) {
+                run = run < 0 ? run_of(a.seg, a.G, t) : run + 1;
+                while (run + 1 < a.G && a.seg[run + 1] <= t) ++run;
+                run_end = min((int64_t)a.seg[run + 1], t1);
+            } else {
+                run = 0;
+            }
+            const P8 gt = ld_param(a.gate ? a.gate + run * a.d : nullptr, col, act, 1.f);
+            w2 = ld_param(a.w_post, col, act, 1.f);
+            b2 = ld_param(a.b_post, col, act, 0.f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] = x[i] = 0.f;
-        if (act) {
-            if (a.r_q8) code_values(rr.a.x, rr.a.y, rr.scale, r);
-            else whole_values<F32>(rr, r);
-            if (join) unpack_bf16x8(rf, x);
+            for (int i = 0; i < 4; ++i) w2.p[i] = f2_mul(w2.p[i], gt.p[i]), b2.p[i] = f2_mul(b2.p[i], gt.p[i]);
         }
-        if (t + 1 < t1) fetch(t + 1);
-        if (a.qr) {
-            float scale;
-            const uint2 c = q8_block(r, act, scale);
-            if (act) *reinterpret_cast<uint2*>(a.qr + t * a.d + col) = c;
-            if (act && (g.lane & 15) == 0) a.qr_scale[t * a.nb + (col >> 7)] = scale;
+        // rows t and, of the same run, t + 1
+        const bool two = ROWS == 2 && t + 1 < (JOIN ? run_end : t1);
+        cp_async_wait<SLOTS - ROWS>();
+        P8 r[ROWS], x[ROWS];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int at = k ? ring.next(slot) : slot;
+            r[k] = R.get(ring, at, 0);
+            if constexpr (JOIN) x[k] = Fo.get(ring, at, PR);
         }
-        if (a.qf) {
-            float scale;
-            const uint2 c = q8_block(x, act, scale);
-            if (act) *reinterpret_cast<uint2*>(a.qf + t * a.d + col) = c;
-            if (act && (g.lane & 15) == 0) a.qf_scale[t * a.nb + (col >> 7)] = scale;
+        slot = ring.next(slot);
+        copy_row();
+        if (two) {
+            slot = ring.next(slot);
+            copy_row();
         }
-        if (join) {
-            if (fresh || t >= run_end) {   // the run's gate, times the norm's weight and bias
-                if (a.seg) {
-                    run = fresh ? run_of(a.seg, a.G, t) : run + 1;
-                    while (run + 1 < a.G && a.seg[run + 1] <= t) ++run;
-                    run_end = a.seg[run + 1];
+        const int64_t at = t * a.d + col;
+        if constexpr (SAVE) {
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                const bool live = act && (k == 0 || two);
+                const int64_t sat = (t + k) * a.nb + (col >> 7);
+                if (a.qr) {
+                    float scale;
+                    const uint2 c = q8_block(r[k], act, scale);
+                    if (live) *reinterpret_cast<uint2*>(a.qr + at + k * a.d) = c;
+                    if (live && (g.lane & 15) == 0) a.qr_scale[sat] = scale;
                 }
-                fresh = false;
-                float gt[8];
-                ld_param(a.gate ? a.gate + run * a.d : nullptr, col, act, 1.f, gt);
-                ld_param(a.w_post, col, act, 1.f, w2);
-                ld_param(a.b_post, col, act, 0.f, b2);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w2[i] *= gt[i], b2[i] *= gt[i];
+                if (JOIN && a.qf) {
+                    float scale;
+                    const uint2 c = q8_block(x[k], act, scale);
+                    if (live) *reinterpret_cast<uint2*>(a.qf + at + k * a.d) = c;
+                    if (live && (g.lane & 15) == 0) a.qf_scale[sat] = scale;
+                }
             }
-            float2 s = make_float2(0.f, 1.f);
+        }
+        float2 st[ROWS];
+        if constexpr (JOIN) {
             if (a.post != MOEVIE_NORM_NONE) {
-                s = row_stats(g, x, act, a.post, inv_d, a.eps);
-                if (a.stats_post && g.wi == 0 && g.lane == 0) a.stats_post[t] = s;
-            }
+                row_stats(g, x, act, a.post, inv_d, a.eps, st);
+                if (a.stats_post && g.wi == 0 && g.lane == 0) {
+                    a.stats_post[t] = st[0];
+                    if (two) a.stats_post[t + 1] = st[ROWS - 1];
+                }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] = fmaf(a.alpha, r[i], fmaf((x[i] - s.x) * s.y, w2[i], b2[i]));
-            if (act) {
-                if constexpr (F32) st_f8(static_cast<float*>(a.r_out) + t * a.d + col, r);
-                else st_b8(static_cast<__nv_bfloat16*>(a.r_out) + t * a.d + col, r);
+                for (int k = 0; k < ROWS; ++k) {
+                    const uint64_t q = f2_of(st[k].y);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[k].p[i] = f2_mul(x[k].p[i], q);
+                }
+            }
+            const uint64_t al = f2_of(a.alpha);
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r[k].p[i] = f2_fma(al, r[k].p[i], f2_fma(x[k].p[i], w2.p[i], b2.p[i]));
+                if (act && (k == 0 || two)) st_rows<F32>(a.r_out, at + k * a.d, r[k]);
             }
         }
         if (a.u) {
-            const float2 s = row_stats(g, r, act, a.pre, inv_d, a.eps);
-            if (a.stats_pre && g.wi == 0 && g.lane == 0) a.stats_pre[t] = s;
+            row_stats(g, r, act, a.pre, inv_d, a.eps, st);
+            if (a.stats_pre && g.wi == 0 && g.lane == 0) {
+                a.stats_pre[t] = st[0];
+                if (two) a.stats_pre[t + 1] = st[ROWS - 1];
+            }
+            const P8 w = w1.get(), b = b1.get();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] = fmaf((r[i] - s.x) * s.y, w1[i], b1[i]);
-            if (act) st_b8(a.u + t * a.d + col, r);
+            for (int k = 0; k < ROWS; ++k) {
+                const uint64_t q = f2_of(st[k].y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r[k].p[i] = f2_fma(f2_mul(r[k].p[i], q), w.p[i], b.p[i]);
+                if (act && (k == 0 || two)) st_bf16(a.u + at + k * a.d, r[k]);
+            }
         }
+        t += two ? 2 : 1;
     }
 }
 
@@ -447,30 +663,44 @@ __global__ void __launch_bounds__(BIG ? 1024 : 512, BIG ? 1 : 2) norm_forward_ke
 // threads have 64 registers, in shared memory (each thread its own words, no bank shared).
 template <bool SHARED>
 struct Sums {
-    float v[8];
-    __device__ __forceinline__ Sums(float*, int) { clear(); }
-    __device__ __forceinline__ void clear() {
+    P8 v;
+    __device__ __forceinline__ Sums(void*, int) { clear(); }
+    __device__ __forceinline__ void clear() { v = p8_of(0.f); }
+    __device__ __forceinline__ void add(const P8& x) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        for (int i = 0; i < 4; ++i) v.p[i] = f2_add(x.p[i], v.p[i]);
     }
-    __device__ __forceinline__ void add(int i, float x, float y) { v[i] = fmaf(x, y, v[i]); }
-    __device__ __forceinline__ void store(float* p) const { st_f8(p, v); }
+    __device__ __forceinline__ void add(const P8& x, const P8& y) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.p[i] = f2_fma(x.p[i], y.p[i], v.p[i]);
+    }
+    __device__ __forceinline__ void store(float* p) const { st_f32(p, v); }
 };
 template <>
 struct Sums<true> {
-    float* p;
-    __device__ __forceinline__ Sums(float* base, int which) : p(base + which * 8 * blockDim.x + threadIdx.x) { clear(); }
-    __device__ __forceinline__ float& at(int i) const { return p[i * blockDim.x]; }
+    uint64_t* p;
+    __device__ __forceinline__ Sums(void* base, int which)
+        : p(static_cast<uint64_t*>(base) + which * 4 * blockDim.x + threadIdx.x) {
+        clear();
+    }
+    __device__ __forceinline__ uint64_t& at(int i) const { return p[i * blockDim.x]; }
     __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) at(i) = 0.f;
+        for (int i = 0; i < 4; ++i) at(i) = 0;
     }
-    __device__ __forceinline__ void add(int i, float x, float y) { at(i) = fmaf(x, y, at(i)); }
-    __device__ __forceinline__ void store(float* out) const {
-        float v[8];
+    __device__ __forceinline__ void add(const P8& x) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = at(i);
-        st_f8(out, v);
+        for (int i = 0; i < 4; ++i) at(i) = f2_add(x.p[i], at(i));
+    }
+    __device__ __forceinline__ void add(const P8& x, const P8& y) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at(i) = f2_fma(x.p[i], y.p[i], at(i));
+    }
+    __device__ __forceinline__ void store(float* out) const {
+        P8 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.p[i] = at(i);
+        st_f32(out, v);
     }
 };
 
@@ -482,18 +712,15 @@ struct Sums<true> {
 //   dgate = w_post A + b_post B,   dw_post = sum_runs gate A,   db_post = sum_runs gate B.
 // Each group of warps leaves its sums in the workspace: dw_pre and db_pre at record gid, A and B
 // of run g at record g + gid (along the rows g and gid never fall, so that no two share one).
-template <bool F32, bool DUF32, bool BIG>
-__global__ void __launch_bounds__(BIG ? 1024 : 512, 1) norm_backward_kernel(const NormBwdArgs a) {
-    extern __shared__ float s_acc[];   // BIG: 4 sums of 8 columns for each thread
-    __shared__ float s_part[MAX_GROUPS * 128];
+template <bool F32, bool DUF32, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward_kernel(const NormBwdArgs a) {
+    constexpr bool BIG = THREADS == 1024;   // no ring: its memory holds the sums
+    constexpr int ROWS = rows_at_once(THREADS), SLOTS = BWD_SLOTS;
+    constexpr int PR = F32 ? 2 : 1, PU = DUF32 ? 2 : 1, PIECES = 2 * PR + PU + 2;   // the last: the row's statistics
+    extern __shared__ __align__(16) uint8_t s_dyn[];   // Kept; the ring, or (BIG) 4 sums of 8 columns for each thread
+    __shared__ __align__(16) float s_part[MAX_GROUPS * GROUP_PART];
     pdl_wait();
-    RowGroup g;
-    g.lane = threadIdx.x & 31;
-    g.gw = a.gw;
-    g.group = (threadIdx.x >> 5) / a.gw;
-    g.wi = (threadIdx.x >> 5) - g.group * a.gw;
-    g.buf = 0;
-    g.part = s_part + g.group * 128;
+    RowGroup g = row_group(a.gw, s_part);
     if (a.seg) check_runs(a.seg, a.G, a.T, a.st);
     const int col = (g.wi * 32 + g.lane) * 8;
     const bool act = col < a.d;
@@ -502,14 +729,44 @@ __global__ void __launch_bounds__(BIG ? 1024 : 512, 1) norm_backward_kernel(cons
     int64_t t0 = first_row(a.T, gid, a.n_groups), t1 = first_row(a.T, gid + 1, a.n_groups);
     clip_rows(a, t0, t1);
 
+    const bool norm = a.du != nullptr, has_f = a.f != nullptr, join = a.df != nullptr;
+    const bool post = a.post != MOEVIE_NORM_NONE;
+    uint8_t* const s_rows = s_dyn + KEPT_BYTES * blockDim.x;
+    const RowRing<SLOTS, PIECES> ring(s_rows);
+    const Operand<F32> Dr{a.dr1, nullptr, false}, R1{a.r1, a.r1_scale, a.r_q8 != 0};
+    const Operand<DUF32> Du{a.du, nullptr, false};
+    const Operand<false> Fo{a.f, a.f_scale, a.f_q8 != 0};
+    // Two sets of copies: dr1, du and r1, whose slots are free as soon as a row is begun, and f, which
+    // is read half-way.  Both sets of a row are under way while the two rows before it are worked on.
+    int slot = 0;
+    auto copy_first = [&](int to, int64_t t) {
+        if (BIG) return;
+        const bool live = t < t1, ok = live && act;
+        const int64_t at = t * a.d + col;
+        if (a.dr1) Dr.copy(ring, to, 0, at, 0, ok);
+        if (norm) {
+            Du.copy(ring, to, PR, at, 0, ok);
+            R1.copy(ring, to, PR + PU, at, t * a.nb + (col >> 7), ok);
+            copy8(ring.at(to, PIECES - 1), a.stats_pre + (live ? t : 0), live ? 8 : 0);
+        }
+    };
+    auto copy_second = [&](int to, int64_t t) {
+        if (BIG) return;
+        const bool live = t < t1, ok = live && act;
+        if (has_f) Fo.copy(ring, to, 2 * PR + PU, t * a.d + col, t * a.nb + (col >> 7), ok);
+        if (post) copy8(ring.at(to, PIECES - 1) + 8, a.stats_post + (live ? t : 0), live ? 8 : 0);
+    };
+    copy_first(0, t0);
+    copy_first(1, t0 + 1);
+    cp_async_commit();
+    copy_second(0, t0);
+    copy_second(1, t0 + 1);
+    cp_async_commit();
+
     const float inv_d = 1.0f / (float)a.d;
-    const bool has_f = a.f != nullptr;
-    const bool join = a.df != nullptr;
-    float w1[8], cw[8];
-    ld_param(a.w_pre, col, act, 1.f, w1);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) cw[i] = 1.f;
-    Sums<BIG> sw(s_acc, 0), sb(s_acc, 1), sA(s_acc, 2), sB(s_acc, 3);   // dw_pre, db_pre, A, B
+    const Kept w1(s_dyn, 0), cw(s_dyn, 1);   // cw: gate * weight
+    w1.set(ld_param(a.w_pre, col, act, 1.f));
+    Sums<BIG> sw(s_rows, 0), sb(s_rows, 1), sA(s_rows, 2), sB(s_rows, 3);   // dw_pre, db_pre, A, B
     int64_t run = 0, run_end = t1;
 
     auto flush_run = [&]() {
@@ -522,11 +779,11 @@ __global__ void __launch_bounds__(BIG ? 1024 : 512, 1) norm_backward_kernel(cons
     };
     auto load_run = [&]() {
         if (!join) return;
-        float gt[8];
-        ld_param(a.gate ? a.gate + run * a.d : nullptr, col, act, 1.f, gt);
-        ld_param(a.w_post, col, act, 1.f, cw);
+        const P8 gt = ld_param(a.gate ? a.gate + run * a.d : nullptr, col, act, 1.f);
+        P8 w = ld_param(a.w_post, col, act, 1.f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) cw[i] *= gt[i];
+        for (int i = 0; i < 4; ++i) w.p[i] = f2_mul(w.p[i], gt.p[i]);
+        cw.set(w);
     };
     if (t0 < t1) {
         if (a.seg) {
@@ -536,30 +793,10 @@ __global__ void __launch_bounds__(BIG ? 1024 : 512, 1) norm_backward_kernel(cons
         load_run();
     }
     const int64_t first_run = run;
+    if (g.gw > 1) group_barrier(g);   // the zeros of row_group
 
-    Raw<F32> rdr, rr1;
-    Raw<DUF32> rdu;
-    Raw<false> rf;
-    float2 s1 = make_float2(0.f, 0.f), s2 = make_float2(0.f, 1.f);
-    auto fetch = [&](int64_t t) {
-        if (a.du) s1 = a.stats_pre[t];
-        if (a.post != MOEVIE_NORM_NONE) s2 = a.stats_post[t];
-        if (!act) return;
-        const int64_t at = t * a.d + col, sat = t * a.nb + (col >> 7);
-        if (a.dr1) ld_whole<F32>(a.dr1, at, rdr);
-        if (a.du) {
-            ld_whole<DUF32>(a.du, at, rdu);
-            if (a.r_q8) ld_codes<F32>(a.r1, at, a.r1_scale, sat, rr1);
-            else ld_whole<F32>(a.r1, at, rr1);
-        }
-        if (has_f) {
-            if (a.f_q8) ld_codes<false>(a.f, at, a.f_scale, sat, rf);
-            else ld_whole<false>(a.f, at, rf);
-        }
-    };
-    if (!BIG && t0 < t1) fetch(t0);
-    for (int64_t t = t0; t < t1; ++t) {
-        if (BIG) fetch(t);
+#pragma unroll 1
+    for (int64_t t = t0; t < t1;) {
         if (t >= run_end && run + 1 < a.G) {
             do {   // runs without rows get zeros
                 flush_run();
@@ -568,79 +805,129 @@ __global__ void __launch_bounds__(BIG ? 1024 : 512, 1) norm_backward_kernel(cons
             run_end = a.seg[run + 1];
             load_run();
         }
-        float dR[8], x2[8];
+        // rows t and, of the same run, t + 1
+        const bool two = ROWS == 2 && t + 1 < t1 && (t + 1 < run_end || run + 1 >= a.G);
+        const int64_t at = t * a.d + col;
+        const int64_t sat = t * a.nb + (col >> 7);
+        P8 dR[ROWS], x1[ROWS], du[ROWS], x2[ROWS];
+        float2 st1[ROWS], st2[ROWS];
+        if constexpr (BIG) {
+            dR[0] = x1[0] = du[0] = p8_of(0.f);
+            if (act && a.dr1) dR[0] = Dr.read(at, sat);
+            if (act && norm) x1[0] = R1.read(at, sat), du[0] = Du.read(at, sat);
+            if (norm) st1[0] = a.stats_pre[t];
+        } else {
+            cp_async_wait<1>();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dR[i] = x2[i] = 0.f;
-        if (act && a.dr1) whole_values<F32>(rdr, dR);
-        const float2 st2 = s2;
-        if (act && has_f) {
-            if (a.f_q8) code_values(rf.a.x, rf.a.y, rf.scale, x2);
-            else unpack_bf16x8(rf.a, x2);
-        }
-        if (a.du) {
-            float x1[8], du[8];
-            const float2 st1 = s1;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x1[i] = du[i] = 0.f;
-            if (act) {
-                if (a.r_q8) code_values(rr1.a.x, rr1.a.y, rr1.scale, x1);
-                else whole_values<F32>(rr1, x1);
-                whole_values<DUF32>(rdu, du);
-            }
-            if (!BIG && t + 1 < t1) fetch(t + 1);
-            float s[2] = {0.f, 0.f};
-            if (act) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x1[i] = (x1[i] - st1.x) * st1.y;
-                    sw.add(i, du[i], x1[i]);
-                    sb.add(i, du[i], 1.f);
-                    du[i] *= w1[i];
-                    s[0] += du[i];
-                    s[1] = fmaf(du[i], x1[i], s[1]);
+            for (int k = 0; k < ROWS; ++k) {
+                dR[k] = a.dr1 ? Dr.get(ring, slot ^ k, 0) : p8_of(0.f);
+                if (norm) {
+                    x1[k] = R1.get(ring, slot ^ k, PR + PU);
+                    du[k] = Du.get(ring, slot ^ k, PR);
+                    const ulonglong2 q = ld_shared(ring.at(slot ^ k, PIECES - 1));
+                    f2_unpack(q.x, st1[k].x, st1[k].y);
                 }
             }
+            copy_first(slot, t + 2);
+            if (two) copy_first(slot ^ 1, t + 3);
+            cp_async_commit();
+            if (ROWS == 2 && !two) {   // t + 1 is not of this run: nothing of it counts here
+                dR[ROWS - 1] = x1[ROWS - 1] = du[ROWS - 1] = p8_of(0.f);
+                st1[ROWS - 1] = make_float2(0.f, 0.f);
+            }
+        }
+        if (norm) {
+            float s[2 * ROWS];
+            const P8 w = w1.get();
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {   // behind the row's end du and dR are zeros
+                const uint64_t m = f2_of(-st1[k].x), q = f2_of(st1[k].y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x1[k].p[i] = f2_mul(f2_add(x1[k].p[i], m), q);
+                sw.add(du[k], x1[k]);
+                sb.add(du[k]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) du[k].p[i] = f2_mul(du[k].p[i], w.p[i]);
+                s[2 * k] = p8_sum(du[k]);
+                s[2 * k + 1] = p8_dot(du[k], x1[k]);
+            }
             row_sum(g, s);
-            const float m0 = a.pre == MOEVIE_NORM_LAYER ? s[0] * inv_d : 0.f, m1 = s[1] * inv_d;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dR[i] = fmaf(st1.y, fmaf(-x1[i], m1, du[i] - m0), dR[i]);
-        } else if (!BIG && t + 1 < t1) {
-            fetch(t + 1);
-        }
-        if (act && a.dr) {
-            float o[8];
+            for (int k = 0; k < ROWS; ++k) {
+                const uint64_t m0 = f2_of(a.pre == MOEVIE_NORM_LAYER ? -s[2 * k] * inv_d : 0.f);
+                const uint64_t m1 = f2_of(-s[2 * k + 1] * inv_d), q = f2_of(st1[k].y);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = a.alpha * dR[i];
-            if constexpr (F32) st_f8(static_cast<float*>(a.dr) + t * a.d + col, o);
-            else st_b8(static_cast<__nv_bfloat16*>(a.dr) + t * a.d + col, o);
-        }
-        if (!join) continue;
-        if (a.post == MOEVIE_NORM_NONE) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                sA.add(i, dR[i], x2[i]);
-                dR[i] *= cw[i];
-            }
-            if (act) st_b8(a.df + t * a.d + col, dR);
-            continue;
-        }
-        float s[2] = {0.f, 0.f};
-        if (act) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x2[i] = (x2[i] - st2.x) * st2.y;
-                sA.add(i, dR[i], x2[i]);
-                sB.add(i, dR[i], 1.f);
-                dR[i] *= cw[i];
-                s[0] += dR[i];
-                s[1] = fmaf(dR[i], x2[i], s[1]);
+                for (int i = 0; i < 4; ++i)
+                    dR[k].p[i] = f2_fma(q, f2_fma(x1[k].p[i], m1, f2_add(du[k].p[i], m0)), dR[k].p[i]);
             }
         }
-        row_sum(g, s);
-        const float m0 = a.post == MOEVIE_NORM_LAYER ? s[0] * inv_d : 0.f, m1 = s[1] * inv_d;
+        const uint64_t al = f2_of(a.alpha);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dR[i] = st2.y * fmaf(-x2[i], m1, dR[i] - m0);
-        if (act) st_b8(a.df + t * a.d + col, dR);
+        for (int k = 0; k < ROWS; ++k) {
+            P8 o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o.p[i] = f2_mul(al, dR[k].p[i]);
+            if (act && (k == 0 || two)) st_rows<F32>(a.dr, at + k * a.d, o);
+        }
+        if constexpr (BIG) {
+            x2[0] = p8_of(0.f);
+            if (act && has_f) x2[0] = Fo.read(at, sat);
+            if (post) st2[0] = a.stats_post[t];
+        } else {
+            cp_async_wait<1>();
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                x2[k] = has_f ? Fo.get(ring, slot ^ k, 2 * PR + PU) : p8_of(0.f);
+                const ulonglong2 q = ld_shared(ring.at(slot ^ k, PIECES - 1));
+                f2_unpack(q.y, st2[k].x, st2[k].y);
+            }
+            copy_second(slot, t + 2);
+            if (two) copy_second(slot ^ 1, t + 3);
+            cp_async_commit();
+            if (ROWS == 2 && !two) {
+                x2[ROWS - 1] = p8_of(0.f);
+                st2[ROWS - 1] = make_float2(0.f, 0.f);
+                slot ^= 1;
+            }
+        }
+        if (join) {
+            const P8 w = cw.get();
+            if (post) {
+                float s[2 * ROWS];
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    const uint64_t m = f2_of(-st2[k].x), q = f2_of(st2[k].y);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x2[k].p[i] = f2_mul(f2_add(x2[k].p[i], m), q);
+                    sA.add(dR[k], x2[k]);
+                    sB.add(dR[k]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dR[k].p[i] = f2_mul(dR[k].p[i], w.p[i]);
+                    s[2 * k] = act ? p8_sum(dR[k]) : 0.f;
+                    s[2 * k + 1] = act ? p8_dot(dR[k], x2[k]) : 0.f;
+                }
+                row_sum(g, s);
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    const uint64_t m0 = f2_of(a.post == MOEVIE_NORM_LAYER ? -s[2 * k] * inv_d : 0.f);
+                    const uint64_t m1 = f2_of(-s[2 * k + 1] * inv_d), q = f2_of(st2[k].y);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        dR[k].p[i] = f2_mul(q, f2_fma(x2[k].p[i], m1, f2_add(dR[k].p[i], m0)));
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    sA.add(dR[k], x2[k]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dR[k].p[i] = f2_mul(dR[k].p[i], w.p[i]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k)
+                if (act && (k == 0 || two)) st_bf16(a.df + at + k * a.d, dR[k]);
+        }
+        t += two ? 2 : 1;
     }
     const bool any = t0 < t1;
     if (any || a.G == 1) flush_run();   // a group without rows leaves zeros where only one run is
@@ -750,8 +1037,8 @@ NormPlan norm_plan(int64_t T, int d, int threads_sm) {
     p.n_groups = std::min<int64_t>(T, (int64_t)p.grid * p.groups);
     return p;
 }
-constexpr int NORM_BIG_WARPS = 16;   // rows of more warps: the kernels for d > 4096
-constexpr int NORM_FWD_THREADS = 1024, NORM_BWD_THREADS = 512;
+constexpr int NORM_FWD_THREADS = 672, NORM_BWD_THREADS = 512;
+constexpr int NORM_MAX_SMEM = 208 * 1024;   // 1024 threads with three rows of fp32 and bf16 each
 
 template <bool F32>
 cudaError_t q8_store(const void* x, int64_t T, int d, int8_t* codes, float* scales, cudaStream_t s) {
@@ -785,20 +1072,46 @@ cudaError_t launch_q8_load(const int8_t* codes, const float* scales, int64_t T, 
     return e;
 }
 
+// Launches kern with `smem` bytes of dynamic shared memory, which its attribute allows from the first
+// launch on a device on.
+template <typename Args>
+static cudaError_t launch_rows(void (*kern)(Args), std::atomic<bool> (&attr_set)[64], const NormPlan& p, size_t smem,
+                               cudaStream_t s, const Args& a) {
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev >= 0 && dev < 64 && !attr_set[dev].load(std::memory_order_acquire)) {   // idempotent: no lock needed
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_MAX_SMEM);
+        if (e != cudaSuccess) return e;
+        attr_set[dev].store(true, std::memory_order_release);
+    }
+    return launch_pdl(kern, dim3(p.grid), dim3(p.threads), smem, s, a);
+}
+
+template <bool F32, bool JOIN, bool SAVE, int THREADS>
+static cudaError_t norm_forward(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
+    static std::atomic<bool> attr_set[64];
+    const size_t smem = (size_t)(KEPT_BYTES + 16 * fwd_slots(THREADS) * ((F32 ? 2 : 1) + (JOIN ? 1 : 0))) * p.threads;
+    return launch_rows(norm_forward_kernel<F32, JOIN, SAVE, THREADS>, attr_set, p, smem, s, a);
+}
+template <bool F32, bool JOIN, bool SAVE>
+static cudaError_t norm_forward(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
+    if (p.threads <= 256) return norm_forward<F32, JOIN, SAVE, 256>(a, p, s);
+    return p.threads <= 512 ? norm_forward<F32, JOIN, SAVE, 512>(a, p, s) : norm_forward<F32, JOIN, SAVE, 1024>(a, p, s);
+}
+template <bool F32>
+static cudaError_t norm_forward(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
+    const bool save = a.qr || a.qf;
+    if (!a.f) return save ? norm_forward<F32, false, true>(a, p, s) : norm_forward<F32, false, false>(a, p, s);
+    return save ? norm_forward<F32, true, true>(a, p, s) : norm_forward<F32, true, false>(a, p, s);
+}
+
 cudaError_t launch_norm_forward(NormArgs a, int r_f32, cudaStream_t s) {
     const NormPlan p = norm_plan(a.T, a.d, NORM_FWD_THREADS);
     a.gw = p.gw;
     a.groups = p.groups;
     a.n_groups = p.n_groups;
     a.nb = (a.d + 127) / 128;
-    const dim3 grid(p.grid), block(p.threads);
-    cudaError_t e;
-    if (p.gw > NORM_BIG_WARPS)
-        e = r_f32 ? launch_pdl(norm_forward_kernel<true, true>, grid, block, 0, s, a)
-                  : launch_pdl(norm_forward_kernel<false, true>, grid, block, 0, s, a);
-    else
-        e = r_f32 ? launch_pdl(norm_forward_kernel<true, false>, grid, block, 0, s, a)
-                  : launch_pdl(norm_forward_kernel<false, false>, grid, block, 0, s, a);
+    const cudaError_t e = r_f32 ? norm_forward<true>(a, p, s) : norm_forward<false>(a, p, s);
     count_launches(1);
     return e;
 }
@@ -807,21 +1120,16 @@ int64_t norm_groups(int64_t T, int d) {
     return std::max<int64_t>(1, norm_plan(T, d, NORM_BWD_THREADS).n_groups);
 }
 
+template <bool F32, bool DUF32, int THREADS>
+static cudaError_t norm_backward(const NormBwdArgs& a, const NormPlan& p, cudaStream_t s) {
+    static std::atomic<bool> attr_set[64];
+    const int words = THREADS == 1024 ? 8 : BWD_SLOTS * (2 * (F32 ? 2 : 1) + (DUF32 ? 2 : 1) + 2);   // of 16 bytes
+    return launch_rows(norm_backward_kernel<F32, DUF32, THREADS>, attr_set, p, (size_t)(KEPT_BYTES + 16 * words) * p.threads, s, a);
+}
 template <bool F32, bool DUF32>
 static cudaError_t norm_backward(const NormBwdArgs& a, const NormPlan& p, cudaStream_t s) {
-    const dim3 grid(p.grid), block(p.threads);
-    if (p.gw <= NORM_BIG_WARPS) return launch_pdl(norm_backward_kernel<F32, DUF32, false>, grid, block, 0, s, a);
-    const size_t smem = (size_t)32 * 4 * p.threads;
-    static std::atomic<bool> attr_set[64];
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (dev >= 0 && dev < 64 && !attr_set[dev].load(std::memory_order_acquire)) {   // idempotent: no lock needed
-        const cudaError_t e = cudaFuncSetAttribute(norm_backward_kernel<F32, DUF32, true>,
-                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * 4 * 1024);
-        if (e != cudaSuccess) return e;
-        attr_set[dev].store(true, std::memory_order_release);
-    }
-    return launch_pdl(norm_backward_kernel<F32, DUF32, true>, grid, block, smem, s, a);
+    if (p.threads <= 256) return norm_backward<F32, DUF32, 256>(a, p, s);
+    return p.threads <= 512 ? norm_backward<F32, DUF32, 512>(a, p, s) : norm_backward<F32, DUF32, 1024>(a, p, s);
 }
 
 cudaError_t launch_norm_backward(NormBwdArgs a, int r_f32, int du_f32, NormSumArgs sums, cudaStream_t s) {
