@@ -19,7 +19,6 @@ namespace mv {
 
 namespace {
 
-constexpr int MAX_GROUPS = 8;      // row groups of a CTA
 constexpr float Q8_LEAST = 7.70371978e-34f;   // 2^-110: blocks of smaller values are kept as zeros
 
 // ------------------------------------------------------------ 8 columns of a row
@@ -275,9 +274,10 @@ __global__ void __launch_bounds__(256) q8_load_kernel(const int8_t* codes, const
 struct RowGroup {
     int gw, wi, lane, group;
     int buf;        // which half of the group's shared memory the next sum takes
-    float* part;    // [2][32 warps][4], zeros behind the gw-th warp
+    int half;       // floats of one: 4 for each warp
+    float* part;    // zeros behind the gw-th warp
 };
-constexpr int PART_HALF = 128, GROUP_PART = 2 * PART_HALF;
+constexpr int PART_FLOATS = 2 * 4 * 32;   // of a CTA of 32 warps, or of groups of up to 8 in 8
 
 __device__ __forceinline__ RowGroup row_group(int gw, float* s_part) {
     RowGroup g;
@@ -286,8 +286,9 @@ __device__ __forceinline__ RowGroup row_group(int gw, float* s_part) {
     g.group = (threadIdx.x >> 5) / gw;
     g.wi = (threadIdx.x >> 5) - g.group * gw;
     g.buf = 0;
-    g.part = s_part + g.group * GROUP_PART;
-    for (int i = g.wi * 32 + g.lane; i < GROUP_PART; i += gw * 32) g.part[i] = 0.f;
+    g.half = (gw + 3) / 4 * 16;
+    g.part = s_part + g.group * 2 * g.half;
+    for (int i = g.wi * 32 + g.lane; i < 2 * g.half; i += gw * 32) g.part[i] = 0.f;
     return g;
 }
 __device__ __forceinline__ void group_barrier(const RowGroup& g) {
@@ -320,7 +321,7 @@ __device__ __forceinline__ void row_sum(RowGroup& g, float (&v)[N]) {
         for (int n = 0; n < N; ++n) v[n] = N == 1 ? x : __shfl_sync(0xffffffffu, x, SPAN * n);
         return;
     }
-    float* p = g.part + g.buf * PART_HALF;
+    float* p = g.part + g.buf * g.half;
     if (g.lane % SPAN == 0) p[g.wi * N + g.lane / SPAN] = x;
     group_barrier(g);
     uint64_t s[2] = {0, 0};   // N = 1: sums of every other one; 2: the two; 4: the first and the second two
@@ -462,29 +463,30 @@ __device__ __forceinline__ P8 p8_bf16(const ulonglong2& u) {
     return p8_bf16(make_uint4((uint32_t)u.x, (uint32_t)(u.x >> 32), (uint32_t)u.y, (uint32_t)(u.y >> 32)));
 }
 
-// One operand of a row: whole (F32 or bf16), or 8-bit codes with their scale behind them.
-template <bool F32>
+// One operand's rows: whole (F32 or bf16), or, where Q8 allows it and q8 says so, 8-bit codes with
+// their scales.
+template <bool F32, bool Q8>
 struct Operand {
     const void* data;
     const float* scale;
-    bool q8;
-    // 8 columns from element `at` on (their scale: element sat), zeros where not ok
+    int q8;
+    // 8 columns from element `at` on (their scale: element sat), `bytes` (16 or 0) of each piece
     template <typename Ring>
-    __device__ __forceinline__ void copy(const Ring& ring, int slot, int piece, int64_t at, int64_t sat, bool ok) const {
+    __device__ __forceinline__ void copy(const Ring& ring, int slot, int piece, int64_t at, int64_t sat, int bytes) const {
         const uint32_t dst = ring.at(slot, piece);
-        if (q8) {
-            copy8(dst, static_cast<const int8_t*>(data) + (ok ? at : 0), ok ? 8 : 0);
-            copy4(dst + 8, scale + (ok ? sat : 0), ok ? 4 : 0);
+        if (Q8 && q8) {
+            copy8(dst, static_cast<const int8_t*>(data) + at, bytes / 2);
+            copy4(dst + 8, scale + sat, bytes / 4);
             return;
         }
-        const char* p = static_cast<const char*>(data) + (ok ? at * (F32 ? 4 : 2) : 0);
-        copy16(dst, p, ok ? 16 : 0);
-        if constexpr (F32) copy16(ring.at(slot, piece + 1), p + (ok ? 16 : 0), ok ? 16 : 0);
+        const char* p = static_cast<const char*>(data) + at * (F32 ? 4 : 2);
+        copy16(dst, p, bytes);
+        if constexpr (F32) copy16(ring.at(slot, piece + 1), p + 16, bytes);
     }
     template <typename Ring>
     __device__ __forceinline__ P8 get(const Ring& ring, int slot, int piece) const {
         const ulonglong2 a = ld_shared(ring.at(slot, piece));
-        if (q8) return p8_codes((uint32_t)a.x, (uint32_t)(a.x >> 32), __uint_as_float((uint32_t)a.y));
+        if (Q8 && q8) return p8_codes((uint32_t)a.x, (uint32_t)(a.x >> 32), __uint_as_float((uint32_t)a.y));
         if constexpr (F32) {
             const ulonglong2 b = ld_shared(ring.at(slot, piece + 1));
             P8 r;
@@ -495,7 +497,7 @@ struct Operand {
         }
     }
     __device__ __forceinline__ P8 read(int64_t at, int64_t sat) const {   // without a ring
-        if (q8) {
+        if (Q8 && q8) {
             const uint2 c = ld8(static_cast<const int8_t*>(data) + at);
             float s;
             asm volatile("ld.global.f32 %0, [%1];" : "=f"(s) : "l"(scale + sat));
@@ -516,16 +518,18 @@ struct Operand {
 // time took 400 us for 65536 x 1664 in fp32, bound by issued instructions), or one in the largest
 // CTAs, whose threads have 64 registers.
 constexpr int rows_at_once(int threads) { return threads == 1024 ? 1 : 2; }
-constexpr int fwd_slots(int threads) { return threads == 1024 ? 3 : 4; }
+constexpr int fwd_slots(bool f32, int threads) { return f32 || threads == 1024 ? 3 : 4; }
 constexpr int BWD_SLOTS = 2;
 
-// JOIN: r1 = alpha r + gate * N_post(f) and its norm; otherwise the norm of r alone.  SAVE: 8-bit
-// checkpoints of what is read.  THREADS: a CTA's at most.
-template <bool F32, bool JOIN, bool SAVE, int THREADS>
+// JOIN: r1 = alpha r + gate * N_post(f), and its norm; otherwise the norm of r alone.  BOTH: a join with
+// both norms and their statistics (the others ask as they go).  SAVE: 8-bit checkpoints of what is read.
+// THREADS: a CTA's at most.
+template <bool F32, bool JOIN, bool BOTH, bool SAVE, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_kernel(const NormArgs a) {
-    constexpr int ROWS = rows_at_once(THREADS), SLOTS = fwd_slots(THREADS), PR = F32 ? 2 : 1, PIECES = PR + (JOIN ? 1 : 0);
+    constexpr bool BIG = THREADS == 1024;
+    constexpr int ROWS = rows_at_once(THREADS), SLOTS = fwd_slots(F32, THREADS), PR = F32 ? 2 : 1, PIECES = PR + (JOIN ? 1 : 0);
     extern __shared__ __align__(16) uint8_t s_dyn[];
-    __shared__ __align__(16) float s_part[MAX_GROUPS * GROUP_PART];
+    __shared__ __align__(16) float s_part[PART_FLOATS];
     pdl_wait();
     RowGroup g = row_group(a.gw, s_part);
     if (a.seg) check_runs(a.seg, a.G, a.T, a.st);
@@ -537,57 +541,67 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_
     clip_rows(a, t0, t1);
     if (t0 >= t1) return;
 
-    const RowRing<SLOTS, PIECES> ring(s_dyn + KEPT_BYTES * blockDim.x);
-    const Operand<F32> R{a.r, a.r_scale, !JOIN && a.r_q8};
-    const Operand<false> Fo{a.f, nullptr, false};
-    int slot = 0, fill = 0;
-    int64_t ahead = t0;
+    const RowRing<SLOTS, PIECES> ring(s_dyn + (BIG ? 1 : 2) * KEPT_BYTES * blockDim.x);
+    const Operand<F32, !JOIN> R{a.r, a.r_scale, a.r_q8};
+    const Operand<false, false> Fo{a.f, nullptr, 0};
+    const int n = (int)(t1 - t0), d = a.d;
+    int slot = 0, fill = 0, ahead = 0;   // rows count from t0
+    int64_t at_ahead = t0 * d + col, sat_ahead = t0 * a.nb + (col >> 7);
     auto copy_row = [&]() {   // of row `ahead`
-        const bool ok = ahead < t1 && act;
-        const int64_t at = ahead * a.d + col;
-        R.copy(ring, fill, 0, at, ahead * a.nb + (col >> 7), ok);
-        if constexpr (JOIN) Fo.copy(ring, fill, PR, at, 0, ok);
+        const int bytes = ahead < n && act ? 16 : 0;
+        R.copy(ring, fill, 0, at_ahead, sat_ahead, bytes);
+        if constexpr (JOIN) Fo.copy(ring, fill, PR, at_ahead, 0, bytes);
         cp_async_commit();
         fill = ring.next(fill);
         ++ahead;
+        at_ahead += d;
+        if (!JOIN) sat_ahead += a.nb;
     };
 #pragma unroll 1
     for (int i = 0; i < SLOTS; ++i) copy_row();
 
-    const float inv_d = 1.0f / (float)a.d;
+    const float inv_d = 1.0f / (float)d;
     const Kept w1(s_dyn, 0), b1(s_dyn, 1);
     w1.set(ld_param(a.w_pre, col, act, 1.f));
     b1.set(ld_param(a.b_pre, col, act, 0.f));
-    P8 w2 = p8_of(0.f), b2 = p8_of(0.f);   // gate * weight, gate * bias
-    int64_t run = -1, run_end = t0;
+    const Kept w2(s_dyn, BIG ? 0 : 2), b2(s_dyn, BIG ? 1 : 3);   // gate * weight, gate * bias
+    P8 w2_reg = p8_of(0.f), b2_reg = p8_of(0.f);                   // BIG: in registers, shared memory is full
+    int64_t run = -1;
+    int run_end = 0;
+    const bool first = g.wi == 0 && g.lane == 0;
+    float2 *const stats_pre = a.stats_pre + t0, *const stats_post = a.stats_post + t0;
+    int64_t at = t0 * d + col;
     if (g.gw > 1) group_barrier(g);   // the zeros of row_group
 
 #pragma unroll 1
-    for (int64_t t = t0; t < t1;) {
-        if (JOIN && t >= run_end) {   // the next run's gate, times the norm's weight and bias
-            run_end = t1;
+    for (int i = 0; i < n;) {
+        if (JOIN && i >= run_end) {   // the next run's gate, times the norm's weight and bias
+            run_end = n;
             if (a.seg) {
+                const int64_t t = t0 + i;
                 run = run < 0 ? run_of(a.seg, a.G, t) : run + 1;
                 while (run + 1 < a.G && a.seg[run + 1] <= t) ++run;
-                run_end = min((int64_t)a.seg[run + 1], t1);
+                run_end = (int)(min((int64_t)a.seg[run + 1], t1) - t0);
             } else {
                 run = 0;
             }
-            const P8 gt = ld_param(a.gate ? a.gate + run * a.d : nullptr, col, act, 1.f);
-            w2 = ld_param(a.w_post, col, act, 1.f);
-            b2 = ld_param(a.b_post, col, act, 0.f);
+            const P8 gt = ld_param(a.gate ? a.gate + run * d : nullptr, col, act, 1.f);
+            w2_reg = ld_param(a.w_post, col, act, 1.f);
+            b2_reg = ld_param(a.b_post, col, act, 0.f);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w2.p[i] = f2_mul(w2.p[i], gt.p[i]), b2.p[i] = f2_mul(b2.p[i], gt.p[i]);
+            for (int j = 0; j < 4; ++j)
+                w2_reg.p[j] = f2_mul(w2_reg.p[j], gt.p[j]), b2_reg.p[j] = f2_mul(b2_reg.p[j], gt.p[j]);
+            if (!BIG) w2.set(w2_reg), b2.set(b2_reg);
         }
-        // rows t and, of the same run, t + 1
-        const bool two = ROWS == 2 && t + 1 < (JOIN ? run_end : t1);
+        // rows i and, of the same run, i + 1
+        const bool two = ROWS == 2 && i + 1 < (JOIN ? run_end : n);
         cp_async_wait<SLOTS - ROWS>();
         P8 r[ROWS], x[ROWS];
 #pragma unroll
         for (int k = 0; k < ROWS; ++k) {
-            const int at = k ? ring.next(slot) : slot;
-            r[k] = R.get(ring, at, 0);
-            if constexpr (JOIN) x[k] = Fo.get(ring, at, PR);
+            const int from = k ? ring.next(slot) : slot;
+            r[k] = R.get(ring, from, 0);
+            if constexpr (JOIN) x[k] = Fo.get(ring, from, PR);
         }
         slot = ring.next(slot);
         copy_row();
@@ -595,65 +609,67 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_
             slot = ring.next(slot);
             copy_row();
         }
-        const int64_t at = t * a.d + col;
         if constexpr (SAVE) {
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
                 const bool live = act && (k == 0 || two);
-                const int64_t sat = (t + k) * a.nb + (col >> 7);
+                const int64_t sat = (t0 + i + k) * a.nb + (col >> 7);
                 if (a.qr) {
                     float scale;
                     const uint2 c = q8_block(r[k], act, scale);
-                    if (live) *reinterpret_cast<uint2*>(a.qr + at + k * a.d) = c;
+                    if (live) *reinterpret_cast<uint2*>(a.qr + at + k * d) = c;
                     if (live && (g.lane & 15) == 0) a.qr_scale[sat] = scale;
                 }
                 if (JOIN && a.qf) {
                     float scale;
                     const uint2 c = q8_block(x[k], act, scale);
-                    if (live) *reinterpret_cast<uint2*>(a.qf + at + k * a.d) = c;
+                    if (live) *reinterpret_cast<uint2*>(a.qf + at + k * d) = c;
                     if (live && (g.lane & 15) == 0) a.qf_scale[sat] = scale;
                 }
             }
         }
         float2 st[ROWS];
         if constexpr (JOIN) {
-            if (a.post != MOEVIE_NORM_NONE) {
+            if (BOTH || a.post != MOEVIE_NORM_NONE) {
                 row_stats(g, x, act, a.post, inv_d, a.eps, st);
-                if (a.stats_post && g.wi == 0 && g.lane == 0) {
-                    a.stats_post[t] = st[0];
-                    if (two) a.stats_post[t + 1] = st[ROWS - 1];
+                if ((BOTH || a.stats_post) && first) {
+                    stats_post[i] = st[0];
+                    if (two) stats_post[i + 1] = st[ROWS - 1];
                 }
 #pragma unroll
                 for (int k = 0; k < ROWS; ++k) {
                     const uint64_t q = f2_of(st[k].y);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[k].p[i] = f2_mul(x[k].p[i], q);
+                    for (int j = 0; j < 4; ++j) x[k].p[j] = f2_mul(x[k].p[j], q);
                 }
             }
             const uint64_t al = f2_of(a.alpha);
+            if (!BIG) w2_reg = w2.get(), b2_reg = b2.get();
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) r[k].p[i] = f2_fma(al, r[k].p[i], f2_fma(x[k].p[i], w2.p[i], b2.p[i]));
-                if (act && (k == 0 || two)) st_rows<F32>(a.r_out, at + k * a.d, r[k]);
+                for (int j = 0; j < 4; ++j)
+                    r[k].p[j] = f2_fma(al, r[k].p[j], f2_fma(x[k].p[j], w2_reg.p[j], b2_reg.p[j]));
+                if (act && (k == 0 || two)) st_rows<F32>(a.r_out, at + k * d, r[k]);
             }
         }
-        if (a.u) {
+        if (BOTH || a.u) {
             row_stats(g, r, act, a.pre, inv_d, a.eps, st);
-            if (a.stats_pre && g.wi == 0 && g.lane == 0) {
-                a.stats_pre[t] = st[0];
-                if (two) a.stats_pre[t + 1] = st[ROWS - 1];
+            if ((BOTH || a.stats_pre) && first) {
+                stats_pre[i] = st[0];
+                if (two) stats_pre[i + 1] = st[ROWS - 1];
             }
             const P8 w = w1.get(), b = b1.get();
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
                 const uint64_t q = f2_of(st[k].y);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) r[k].p[i] = f2_fma(f2_mul(r[k].p[i], q), w.p[i], b.p[i]);
-                if (act && (k == 0 || two)) st_bf16(a.u + at + k * a.d, r[k]);
+                for (int j = 0; j < 4; ++j) r[k].p[j] = f2_fma(f2_mul(r[k].p[j], q), w.p[j], b.p[j]);
+                if (act && (k == 0 || two)) st_bf16(a.u + at + k * d, r[k]);
             }
         }
-        t += two ? 2 : 1;
+        i += two ? 2 : 1;
+        at += two ? 2 * d : d;
     }
 }
 
@@ -712,13 +728,14 @@ struct Sums<true> {
 //   dgate = w_post A + b_post B,   dw_post = sum_runs gate A,   db_post = sum_runs gate B.
 // Each group of warps leaves its sums in the workspace: dw_pre and db_pre at record gid, A and B
 // of run g at record g + gid (along the rows g and gid never fall, so that no two share one).
-template <bool F32, bool DUF32, int THREADS>
+// ALL: both norms, dr1 and every sum; the others ask as they go.  Q8: r1 and f may be checkpoints.
+template <bool F32, bool DUF32, bool ALL, bool Q8, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward_kernel(const NormBwdArgs a) {
     constexpr bool BIG = THREADS == 1024;   // no ring: its memory holds the sums
-    constexpr int ROWS = rows_at_once(THREADS), SLOTS = BWD_SLOTS;
+    constexpr int ROWS = rows_at_once(THREADS);
     constexpr int PR = F32 ? 2 : 1, PU = DUF32 ? 2 : 1, PIECES = 2 * PR + PU + 2;   // the last: the row's statistics
     extern __shared__ __align__(16) uint8_t s_dyn[];   // Kept; the ring, or (BIG) 4 sums of 8 columns for each thread
-    __shared__ __align__(16) float s_part[MAX_GROUPS * GROUP_PART];
+    __shared__ __align__(16) float s_part[PART_FLOATS];
     pdl_wait();
     RowGroup g = row_group(a.gw, s_part);
     if (a.seg) check_runs(a.seg, a.G, a.T, a.st);
@@ -729,66 +746,72 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     int64_t t0 = first_row(a.T, gid, a.n_groups), t1 = first_row(a.T, gid + 1, a.n_groups);
     clip_rows(a, t0, t1);
 
-    const bool norm = a.du != nullptr, has_f = a.f != nullptr, join = a.df != nullptr;
-    const bool post = a.post != MOEVIE_NORM_NONE;
+    const bool norm = ALL || a.du != nullptr, has_f = ALL || a.f != nullptr, join = ALL || a.df != nullptr;
+    const bool post = ALL || a.post != MOEVIE_NORM_NONE, has_dr = ALL || a.dr1 != nullptr;
     uint8_t* const s_rows = s_dyn + KEPT_BYTES * blockDim.x;
-    const RowRing<SLOTS, PIECES> ring(s_rows);
-    const Operand<F32> Dr{a.dr1, nullptr, false}, R1{a.r1, a.r1_scale, a.r_q8 != 0};
-    const Operand<DUF32> Du{a.du, nullptr, false};
-    const Operand<false> Fo{a.f, a.f_scale, a.f_q8 != 0};
+    const RowRing<BWD_SLOTS, PIECES> ring(s_rows);
+    const Operand<F32, false> Dr{a.dr1, nullptr, 0};
+    const Operand<F32, Q8> R1{a.r1, a.r1_scale, a.r_q8};
+    const Operand<DUF32, false> Du{a.du, nullptr, 0};
+    const Operand<false, Q8> Fo{a.f, a.f_scale, a.f_q8};
+    const int n = t0 < t1 ? (int)(t1 - t0) : 0, d = a.d;   // rows count from t0
+    int64_t at = t0 * d + col, sat = t0 * a.nb + (col >> 7);   // of the row in hand
     // Two sets of copies: dr1, du and r1, whose slots are free as soon as a row is begun, and f, which
     // is read half-way.  Both sets of a row are under way while the two rows before it are worked on.
+    // `on`: rows from the one in hand
     int slot = 0;
-    auto copy_first = [&](int to, int64_t t) {
-        if (BIG) return;
-        const bool live = t < t1, ok = live && act;
-        const int64_t at = t * a.d + col;
-        if (a.dr1) Dr.copy(ring, to, 0, at, 0, ok);
+    auto copy_first = [&](int to, int i, int on) {
+        const int bytes = i + on < n && act ? 16 : 0;
+        if (has_dr) Dr.copy(ring, to, 0, at + on * d, 0, bytes);
         if (norm) {
-            Du.copy(ring, to, PR, at, 0, ok);
-            R1.copy(ring, to, PR + PU, at, t * a.nb + (col >> 7), ok);
-            copy8(ring.at(to, PIECES - 1), a.stats_pre + (live ? t : 0), live ? 8 : 0);
+            Du.copy(ring, to, PR, at + on * d, 0, bytes);
+            R1.copy(ring, to, PR + PU, at + on * d, Q8 ? sat + on * a.nb : 0, bytes);
+            copy8(ring.at(to, PIECES - 1), a.stats_pre + t0 + (i + on), i + on < n ? 8 : 0);
         }
     };
-    auto copy_second = [&](int to, int64_t t) {
-        if (BIG) return;
-        const bool live = t < t1, ok = live && act;
-        if (has_f) Fo.copy(ring, to, 2 * PR + PU, t * a.d + col, t * a.nb + (col >> 7), ok);
-        if (post) copy8(ring.at(to, PIECES - 1) + 8, a.stats_post + (live ? t : 0), live ? 8 : 0);
+    auto copy_second = [&](int to, int i, int on) {
+        const int bytes = i + on < n && act ? 16 : 0;
+        if (has_f) Fo.copy(ring, to, 2 * PR + PU, at + on * d, Q8 ? sat + on * a.nb : 0, bytes);
+        if (post) copy8(ring.at(to, PIECES - 1) + 8, a.stats_post + t0 + (i + on), i + on < n ? 8 : 0);
     };
-    copy_first(0, t0);
-    copy_first(1, t0 + 1);
-    cp_async_commit();
-    copy_second(0, t0);
-    copy_second(1, t0 + 1);
-    cp_async_commit();
+    if constexpr (!BIG) {
+        copy_first(0, 0, 0);
+        copy_first(1, 0, 1);
+        cp_async_commit();
+        copy_second(0, 0, 0);
+        copy_second(1, 0, 1);
+        cp_async_commit();
+    }
 
-    const float inv_d = 1.0f / (float)a.d;
+    const float inv_d = 1.0f / (float)d;
     const Kept w1(s_dyn, 0), cw(s_dyn, 1);   // cw: gate * weight
     w1.set(ld_param(a.w_pre, col, act, 1.f));
     Sums<BIG> sw(s_rows, 0), sb(s_rows, 1), sA(s_rows, 2), sB(s_rows, 3);   // dw_pre, db_pre, A, B
-    int64_t run = 0, run_end = t1;
+    int64_t run = 0;
+    int run_end = n;
 
     auto flush_run = [&]() {
         if (!a.rec_post || !act) return;
-        float* p = a.rec_post + (run + gid) * 2 * a.d + col;
+        float* p = a.rec_post + (run + gid) * 2 * d + col;
         sA.store(p);
-        sB.store(p + a.d);
+        sB.store(p + d);
         sA.clear();
         sB.clear();
     };
     auto load_run = [&]() {
         if (!join) return;
-        const P8 gt = ld_param(a.gate ? a.gate + run * a.d : nullptr, col, act, 1.f);
+        const P8 gt = ld_param(a.gate ? a.gate + run * d : nullptr, col, act, 1.f);
         P8 w = ld_param(a.w_post, col, act, 1.f);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w.p[i] = f2_mul(w.p[i], gt.p[i]);
+        for (int j = 0; j < 4; ++j) w.p[j] = f2_mul(w.p[j], gt.p[j]);
         cw.set(w);
     };
-    if (t0 < t1) {
+    // the end of a run, counted from t0: the last one's rows go to the group's end
+    auto end_of_run = [&]() { return run + 1 < a.G ? (int)(min((int64_t)a.seg[run + 1], t1) - t0) : n; };
+    if (n > 0) {
         if (a.seg) {
             run = run_of(a.seg, a.G, t0);
-            run_end = a.seg[run + 1];
+            run_end = end_of_run();
         }
         load_run();
     }
@@ -796,31 +819,30 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     if (g.gw > 1) group_barrier(g);   // the zeros of row_group
 
 #pragma unroll 1
-    for (int64_t t = t0; t < t1;) {
-        if (t >= run_end && run + 1 < a.G) {
+    for (int i = 0; i < n;) {
+        if (i >= run_end) {
             do {   // runs without rows get zeros
                 flush_run();
                 ++run;
-            } while (run + 1 < a.G && a.seg[run + 1] <= t);
-            run_end = a.seg[run + 1];
+            } while (run + 1 < a.G && a.seg[run + 1] <= t0 + i);
+            run_end = end_of_run();
             load_run();
         }
-        // rows t and, of the same run, t + 1
-        const bool two = ROWS == 2 && t + 1 < t1 && (t + 1 < run_end || run + 1 >= a.G);
-        const int64_t at = t * a.d + col;
-        const int64_t sat = t * a.nb + (col >> 7);
+        // rows i and, of the same run, i + 1
+        const bool two = ROWS == 2 && i + 1 < run_end;
         P8 dR[ROWS], x1[ROWS], du[ROWS], x2[ROWS];
         float2 st1[ROWS], st2[ROWS];
         if constexpr (BIG) {
             dR[0] = x1[0] = du[0] = p8_of(0.f);
-            if (act && a.dr1) dR[0] = Dr.read(at, sat);
+            if (act && has_dr) dR[0] = Dr.read(at, sat);
             if (act && norm) x1[0] = R1.read(at, sat), du[0] = Du.read(at, sat);
-            if (norm) st1[0] = a.stats_pre[t];
+            if (norm) st1[0] = a.stats_pre[t0 + i];
         } else {
             cp_async_wait<1>();
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
-                dR[k] = a.dr1 ? Dr.get(ring, slot ^ k, 0) : p8_of(0.f);
+                if (has_dr) dR[k] = Dr.get(ring, slot ^ k, 0);
+                else dR[k] = p8_of(0.f);
                 if (norm) {
                     x1[k] = R1.get(ring, slot ^ k, PR + PU);
                     du[k] = Du.get(ring, slot ^ k, PR);
@@ -828,10 +850,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
                     f2_unpack(q.x, st1[k].x, st1[k].y);
                 }
             }
-            copy_first(slot, t + 2);
-            if (two) copy_first(slot ^ 1, t + 3);
+            copy_first(slot, i, 2);
+            if (two) copy_first(slot ^ 1, i, 3);
             cp_async_commit();
-            if (ROWS == 2 && !two) {   // t + 1 is not of this run: nothing of it counts here
+            if (ROWS == 2 && !two) {   // i + 1 is not of this run: nothing of it counts here
                 dR[ROWS - 1] = x1[ROWS - 1] = du[ROWS - 1] = p8_of(0.f);
                 st1[ROWS - 1] = make_float2(0.f, 0.f);
             }
@@ -843,11 +865,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
             for (int k = 0; k < ROWS; ++k) {   // behind the row's end du and dR are zeros
                 const uint64_t m = f2_of(-st1[k].x), q = f2_of(st1[k].y);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x1[k].p[i] = f2_mul(f2_add(x1[k].p[i], m), q);
+                for (int j = 0; j < 4; ++j) x1[k].p[j] = f2_mul(f2_add(x1[k].p[j], m), q);
                 sw.add(du[k], x1[k]);
                 sb.add(du[k]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) du[k].p[i] = f2_mul(du[k].p[i], w.p[i]);
+                for (int j = 0; j < 4; ++j) du[k].p[j] = f2_mul(du[k].p[j], w.p[j]);
                 s[2 * k] = p8_sum(du[k]);
                 s[2 * k + 1] = p8_dot(du[k], x1[k]);
             }
@@ -857,8 +879,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
                 const uint64_t m0 = f2_of(a.pre == MOEVIE_NORM_LAYER ? -s[2 * k] * inv_d : 0.f);
                 const uint64_t m1 = f2_of(-s[2 * k + 1] * inv_d), q = f2_of(st1[k].y);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    dR[k].p[i] = f2_fma(q, f2_fma(x1[k].p[i], m1, f2_add(du[k].p[i], m0)), dR[k].p[i]);
+                for (int j = 0; j < 4; ++j)
+                    dR[k].p[j] = f2_fma(q, f2_fma(x1[k].p[j], m1, f2_add(du[k].p[j], m0)), dR[k].p[j]);
             }
         }
         const uint64_t al = f2_of(a.alpha);
@@ -866,23 +888,24 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
         for (int k = 0; k < ROWS; ++k) {
             P8 o;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o.p[i] = f2_mul(al, dR[k].p[i]);
-            if (act && (k == 0 || two)) st_rows<F32>(a.dr, at + k * a.d, o);
+            for (int j = 0; j < 4; ++j) o.p[j] = f2_mul(al, dR[k].p[j]);
+            if (act && (k == 0 || two)) st_rows<F32>(a.dr, at + k * d, o);
         }
         if constexpr (BIG) {
             x2[0] = p8_of(0.f);
             if (act && has_f) x2[0] = Fo.read(at, sat);
-            if (post) st2[0] = a.stats_post[t];
+            if (post) st2[0] = a.stats_post[t0 + i];
         } else {
             cp_async_wait<1>();
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
-                x2[k] = has_f ? Fo.get(ring, slot ^ k, 2 * PR + PU) : p8_of(0.f);
+                if (has_f) x2[k] = Fo.get(ring, slot ^ k, 2 * PR + PU);
+                else x2[k] = p8_of(0.f);
                 const ulonglong2 q = ld_shared(ring.at(slot ^ k, PIECES - 1));
                 f2_unpack(q.y, st2[k].x, st2[k].y);
             }
-            copy_second(slot, t + 2);
-            if (two) copy_second(slot ^ 1, t + 3);
+            copy_second(slot, i, 2);
+            if (two) copy_second(slot ^ 1, i, 3);
             cp_async_commit();
             if (ROWS == 2 && !two) {
                 x2[ROWS - 1] = p8_of(0.f);
@@ -898,13 +921,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
                 for (int k = 0; k < ROWS; ++k) {
                     const uint64_t m = f2_of(-st2[k].x), q = f2_of(st2[k].y);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x2[k].p[i] = f2_mul(f2_add(x2[k].p[i], m), q);
+                    for (int j = 0; j < 4; ++j) x2[k].p[j] = f2_mul(f2_add(x2[k].p[j], m), q);
                     sA.add(dR[k], x2[k]);
                     sB.add(dR[k]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) dR[k].p[i] = f2_mul(dR[k].p[i], w.p[i]);
-                    s[2 * k] = act ? p8_sum(dR[k]) : 0.f;
-                    s[2 * k + 1] = act ? p8_dot(dR[k], x2[k]) : 0.f;
+                    for (int j = 0; j < 4; ++j) dR[k].p[j] = f2_mul(dR[k].p[j], w.p[j]);   // (zeros behind the row's end)
+                    s[2 * k] = p8_sum(dR[k]);
+                    s[2 * k + 1] = p8_dot(dR[k], x2[k]);
                 }
                 row_sum(g, s);
 #pragma unroll
@@ -912,27 +935,28 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
                     const uint64_t m0 = f2_of(a.post == MOEVIE_NORM_LAYER ? -s[2 * k] * inv_d : 0.f);
                     const uint64_t m1 = f2_of(-s[2 * k + 1] * inv_d), q = f2_of(st2[k].y);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        dR[k].p[i] = f2_mul(q, f2_fma(x2[k].p[i], m1, f2_add(dR[k].p[i], m0)));
+                    for (int j = 0; j < 4; ++j)
+                        dR[k].p[j] = f2_mul(q, f2_fma(x2[k].p[j], m1, f2_add(dR[k].p[j], m0)));
                 }
             } else {
 #pragma unroll
                 for (int k = 0; k < ROWS; ++k) {
                     sA.add(dR[k], x2[k]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) dR[k].p[i] = f2_mul(dR[k].p[i], w.p[i]);
+                    for (int j = 0; j < 4; ++j) dR[k].p[j] = f2_mul(dR[k].p[j], w.p[j]);
                 }
             }
 #pragma unroll
             for (int k = 0; k < ROWS; ++k)
-                if (act && (k == 0 || two)) st_bf16(a.df + at + k * a.d, dR[k]);
+                if (act && (k == 0 || two)) st_bf16(a.df + at + k * d, dR[k]);
         }
-        t += two ? 2 : 1;
+        i += two ? 2 : 1;
+        at += two ? 2 * d : d;
+        if (Q8 || BIG) sat += two ? 2 * a.nb : a.nb;
     }
-    const bool any = t0 < t1;
-    if (any || a.G == 1) flush_run();   // a group without rows leaves zeros where only one run is
+    if (n > 0 || a.G == 1) flush_run();   // a group without rows leaves zeros where only one run is
     if (a.group_runs && g.wi == 0 && g.lane == 0)
-        a.group_runs[gid] = any ? make_int2((int)first_run, (int)run) : make_int2(0, -1);
+        a.group_runs[gid] = n > 0 ? make_int2((int)first_run, (int)run) : make_int2(0, -1);
     if (a.rec_pre && act) {
         float* p = a.rec_pre + gid * 2 * a.d + col;
         sw.store(p);
@@ -1087,16 +1111,18 @@ static cudaError_t launch_rows(void (*kern)(Args), std::atomic<bool> (&attr_set)
     return launch_pdl(kern, dim3(p.grid), dim3(p.threads), smem, s, a);
 }
 
-template <bool F32, bool JOIN, bool SAVE, int THREADS>
+template <bool F32, bool JOIN, bool BOTH, bool SAVE, int THREADS>
 static cudaError_t norm_forward(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
     static std::atomic<bool> attr_set[64];
-    const size_t smem = (size_t)(KEPT_BYTES + 16 * fwd_slots(THREADS) * ((F32 ? 2 : 1) + (JOIN ? 1 : 0))) * p.threads;
-    return launch_rows(norm_forward_kernel<F32, JOIN, SAVE, THREADS>, attr_set, p, smem, s, a);
+    const size_t smem = (size_t)((THREADS == 1024 ? 1 : 2) * KEPT_BYTES + 16 * fwd_slots(F32, THREADS) * ((F32 ? 2 : 1) + (JOIN ? 1 : 0))) * p.threads;
+    return launch_rows(norm_forward_kernel<F32, JOIN, BOTH, SAVE, THREADS>, attr_set, p, smem, s, a);
 }
 template <bool F32, bool JOIN, bool SAVE>
 static cudaError_t norm_forward(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
-    if (p.threads <= 256) return norm_forward<F32, JOIN, SAVE, 256>(a, p, s);
-    return p.threads <= 512 ? norm_forward<F32, JOIN, SAVE, 512>(a, p, s) : norm_forward<F32, JOIN, SAVE, 1024>(a, p, s);
+    if (p.threads > 256) return norm_forward<F32, JOIN, false, SAVE, 1024>(a, p, s);
+    if (JOIN && a.post != MOEVIE_NORM_NONE && a.u && a.stats_pre && a.stats_post)
+        return norm_forward<F32, JOIN, JOIN, SAVE, 256>(a, p, s);
+    return norm_forward<F32, JOIN, false, SAVE, 256>(a, p, s);
 }
 template <bool F32>
 static cudaError_t norm_forward(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
@@ -1120,16 +1146,19 @@ int64_t norm_groups(int64_t T, int d) {
     return std::max<int64_t>(1, norm_plan(T, d, NORM_BWD_THREADS).n_groups);
 }
 
-template <bool F32, bool DUF32, int THREADS>
+template <bool F32, bool DUF32, bool ALL, bool Q8, int THREADS>
 static cudaError_t norm_backward(const NormBwdArgs& a, const NormPlan& p, cudaStream_t s) {
     static std::atomic<bool> attr_set[64];
     const int words = THREADS == 1024 ? 8 : BWD_SLOTS * (2 * (F32 ? 2 : 1) + (DUF32 ? 2 : 1) + 2);   // of 16 bytes
-    return launch_rows(norm_backward_kernel<F32, DUF32, THREADS>, attr_set, p, (size_t)(KEPT_BYTES + 16 * words) * p.threads, s, a);
+    return launch_rows(norm_backward_kernel<F32, DUF32, ALL, Q8, THREADS>, attr_set, p,
+                       (size_t)(KEPT_BYTES + 16 * words) * p.threads, s, a);
 }
 template <bool F32, bool DUF32>
 static cudaError_t norm_backward(const NormBwdArgs& a, const NormPlan& p, cudaStream_t s) {
-    if (p.threads <= 256) return norm_backward<F32, DUF32, 256>(a, p, s);
-    return p.threads <= 512 ? norm_backward<F32, DUF32, 512>(a, p, s) : norm_backward<F32, DUF32, 1024>(a, p, s);
+    if (p.threads > 256) return norm_backward<F32, DUF32, false, true, 1024>(a, p, s);
+    if (!a.du || !a.dr1 || !a.df || !a.f || a.post == MOEVIE_NORM_NONE) return norm_backward<F32, DUF32, false, true, 256>(a, p, s);
+    return a.r_q8 || a.f_q8 ? norm_backward<F32, DUF32, true, true, 256>(a, p, s)
+                            : norm_backward<F32, DUF32, true, false, 256>(a, p, s);
 }
 
 cudaError_t launch_norm_backward(NormBwdArgs a, int r_f32, int du_f32, NormSumArgs sums, cudaStream_t s) {
