@@ -97,7 +97,16 @@ __device__ __forceinline__ P8 p8_codes(uint32_t lo, uint32_t hi, float scale) {
     }
     return r;
 }
+// 8 fp32 values in one access, where rows start 32 bytes apart from a multiple of 32
+__device__ __forceinline__ void st_f32_32(float* p, const P8& v) {
+    asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(p), "l"(v.p[0]), "l"(v.p[1]), "l"(v.p[2]), "l"(v.p[3])
+                 : "memory");
+}
 __device__ __forceinline__ void st_f32(float* p, const P8& v) {
+    if ((reinterpret_cast<uintptr_t>(p) & 31) == 0) {
+        st_f32_32(p, v);
+        return;
+    }
     reinterpret_cast<ulonglong2*>(p)[0] = make_ulonglong2(v.p[0], v.p[1]);
     reinterpret_cast<ulonglong2*>(p)[1] = make_ulonglong2(v.p[2], v.p[3]);
 }
@@ -409,18 +418,35 @@ __device__ __forceinline__ void clip_rows(const Args& a, int64_t& t0, int64_t& t
 
 // ------------------------------------------------------------ rows under way
 
-// A thread's share of the rows that are read: its own 8 columns of each operand, in pieces of 16
-// bytes that it copies into words of shared memory which no other thread touches.  So no barrier
-// stands between a copy and its use.  A row's slot is filled anew as soon as its values are in
+// A warp's share of the rows that are read: its 256 columns of each operand, copied ahead into
+// shared memory that no other warp touches, so that no barrier of a row's warps stands between a copy
+// and its use.  An operand of 2 bytes is one piece of 16 bytes to a lane, its own 8 columns; one of
+// fp32 is two pieces, which the lanes copy in the order of memory (every 32-byte sector is asked for
+// once; asked for twice, by the lane that uses each half, the forward of 65536 x 1664 took 267 us
+// instead of 229 and the backward 534 instead of 369) and read back as their own.  A row's slot is filled anew as soon as its values are in
 // registers: SLOTS rows are under way while one or two are worked on.
 template <int SLOTS, int PIECES>
 struct RowRing {
-    uint32_t base;   // shared address of this thread's first piece
-    uint32_t step;   // bytes between pieces
-    __device__ __forceinline__ RowRing(void* smem)
-        : base(smem_u32(smem) + threadIdx.x * 16u), step(blockDim.x * 16u) {}
+    uint32_t base;       // shared address of the warp's first piece
+    uint32_t own;        // this lane's 16 bytes of a piece
+    uint32_t in, lo, hi; // fp32: where the lane copies to in each of the two pieces, and its own columns
+    bool ok, ok_a, ok_b; // whether its own columns, and what it copies of the two pieces, lie in the row
+    // left: columns of the row from the warp's first on
+    __device__ __forceinline__ RowRing(void* smem, int left) {
+        const int lane = threadIdx.x & 31;
+        base = smem_u32(smem) + (threadIdx.x >> 5) * (512u * SLOTS * PIECES);
+        own = lane * 16u;
+        // The 64 times 16 bytes of a warp's 256 columns: neighbours are swapped in every second eight,
+        // so that eight lanes which read every second one meet eight different banks.
+        in = (lane ^ ((lane >> 3) & 1)) * 16u;
+        lo = (2 * lane + ((lane >> 2) & 1)) * 16u;
+        hi = lo ^ 16u;
+        ok = lane * 8 < left;
+        ok_a = lane * 4 < left;
+        ok_b = lane * 4 + 128 < left;
+    }
     __device__ __forceinline__ uint32_t at(int slot, int piece) const {
-        return base + (uint32_t)(slot * PIECES + piece) * step;
+        return base + (uint32_t)(slot * PIECES + piece) * 512u;
     }
     static __device__ __forceinline__ int next(int slot) { return slot + 1 == SLOTS ? 0 : slot + 1; }
 };
@@ -470,31 +496,37 @@ struct Operand {
     const void* data;
     const float* scale;
     int q8;
-    // 8 columns from element `at` on (their scale: element sat), `bytes` (16 or 0) of each piece
+    // the lane's share of a row: its 8 columns begin at element `at`, their scale is element sat;
+    // zeros in place of a row that is not live and of columns behind a row's end
     template <typename Ring>
-    __device__ __forceinline__ void copy(const Ring& ring, int slot, int piece, int64_t at, int64_t sat, int bytes) const {
+    __device__ __forceinline__ void copy(const Ring& ring, int slot, int piece, int64_t at, int64_t sat, bool live) const {
         const uint32_t dst = ring.at(slot, piece);
         if (Q8 && q8) {
-            copy8(dst, static_cast<const int8_t*>(data) + at, bytes / 2);
-            copy4(dst + 8, scale + sat, bytes / 4);
+            const bool ok = live && ring.ok;
+            copy8(dst + ring.own, static_cast<const int8_t*>(data) + at, ok ? 8 : 0);
+            copy4(dst + ring.own + 8, scale + sat, ok ? 4 : 0);
             return;
         }
-        const char* p = static_cast<const char*>(data) + at * (F32 ? 4 : 2);
-        copy16(dst, p, bytes);
-        if constexpr (F32) copy16(ring.at(slot, piece + 1), p + 16, bytes);
+        if constexpr (F32) {
+            const float* p = static_cast<const float*>(data) + at - 4 * (threadIdx.x & 31);
+            copy16(dst + ring.in, p, live && ring.ok_a ? 16 : 0);
+            copy16(dst + ring.in + 512, p + 128, live && ring.ok_b ? 16 : 0);
+        } else {
+            copy16(dst + ring.own, static_cast<const __nv_bfloat16*>(data) + at, live && ring.ok ? 16 : 0);
+        }
     }
     template <typename Ring>
     __device__ __forceinline__ P8 get(const Ring& ring, int slot, int piece) const {
-        const ulonglong2 a = ld_shared(ring.at(slot, piece));
-        if (Q8 && q8) return p8_codes((uint32_t)a.x, (uint32_t)(a.x >> 32), __uint_as_float((uint32_t)a.y));
-        if constexpr (F32) {
-            const ulonglong2 b = ld_shared(ring.at(slot, piece + 1));
+        const uint32_t src = ring.at(slot, piece);
+        if (F32 && !(Q8 && q8)) {
+            const ulonglong2 a = ld_shared(src + ring.lo), b = ld_shared(src + ring.hi);
             P8 r;
             r.p[0] = a.x, r.p[1] = a.y, r.p[2] = b.x, r.p[3] = b.y;
             return r;
-        } else {
-            return p8_bf16(a);
         }
+        const ulonglong2 a = ld_shared(src + ring.own);
+        if (Q8 && q8) return p8_codes((uint32_t)a.x, (uint32_t)(a.x >> 32), __uint_as_float((uint32_t)a.y));
+        return p8_bf16(a);
     }
     __device__ __forceinline__ P8 read(int64_t at, int64_t sat) const {   // without a ring
         if (Q8 && q8) {
@@ -541,16 +573,16 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_
     clip_rows(a, t0, t1);
     if (t0 >= t1) return;
 
-    const RowRing<SLOTS, PIECES> ring(s_dyn + (BIG ? 1 : 2) * KEPT_BYTES * blockDim.x);
+    const RowRing<SLOTS, PIECES> ring(s_dyn + (BIG ? 1 : 2) * KEPT_BYTES * blockDim.x, a.d - g.wi * 256);
     const Operand<F32, !JOIN> R{a.r, a.r_scale, a.r_q8};
     const Operand<false, false> Fo{a.f, nullptr, 0};
     const int n = (int)(t1 - t0), d = a.d;
     int slot = 0, fill = 0, ahead = 0;   // rows count from t0
     int64_t at_ahead = t0 * d + col, sat_ahead = t0 * a.nb + (col >> 7);
     auto copy_row = [&]() {   // of row `ahead`
-        const int bytes = ahead < n && act ? 16 : 0;
-        R.copy(ring, fill, 0, at_ahead, sat_ahead, bytes);
-        if constexpr (JOIN) Fo.copy(ring, fill, PR, at_ahead, 0, bytes);
+        const bool live = ahead < n;
+        R.copy(ring, fill, 0, at_ahead, sat_ahead, live);
+        if constexpr (JOIN) Fo.copy(ring, fill, PR, at_ahead, 0, live);
         cp_async_commit();
         fill = ring.next(fill);
         ++ahead;
@@ -596,6 +628,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_
         // rows i and, of the same run, i + 1
         const bool two = ROWS == 2 && i + 1 < (JOIN ? run_end : n);
         cp_async_wait<SLOTS - ROWS>();
+        __syncwarp();   // the other lanes' copies
         P8 r[ROWS], x[ROWS];
 #pragma unroll
         for (int k = 0; k < ROWS; ++k) {
@@ -604,6 +637,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_
             if constexpr (JOIN) x[k] = Fo.get(ring, from, PR);
         }
         slot = ring.next(slot);
+        __syncwarp();   // read by all lanes
         copy_row();
         if (two) {
             slot = ring.next(slot);
@@ -749,7 +783,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     const bool norm = ALL || a.du != nullptr, has_f = ALL || a.f != nullptr, join = ALL || a.df != nullptr;
     const bool post = ALL || a.post != MOEVIE_NORM_NONE, has_dr = ALL || a.dr1 != nullptr;
     uint8_t* const s_rows = s_dyn + KEPT_BYTES * blockDim.x;
-    const RowRing<BWD_SLOTS, PIECES> ring(s_rows);
+    const RowRing<BWD_SLOTS, PIECES> ring(s_rows, a.d - g.wi * 256);
     const Operand<F32, false> Dr{a.dr1, nullptr, 0};
     const Operand<F32, Q8> R1{a.r1, a.r1_scale, a.r_q8};
     const Operand<DUF32, false> Du{a.du, nullptr, 0};
@@ -761,18 +795,18 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     // `on`: rows from the one in hand
     int slot = 0;
     auto copy_first = [&](int to, int i, int on) {
-        const int bytes = i + on < n && act ? 16 : 0;
-        if (has_dr) Dr.copy(ring, to, 0, at + on * d, 0, bytes);
+        const bool live = i + on < n;
+        if (has_dr) Dr.copy(ring, to, 0, at + on * d, 0, live);
         if (norm) {
-            Du.copy(ring, to, PR, at + on * d, 0, bytes);
-            R1.copy(ring, to, PR + PU, at + on * d, Q8 ? sat + on * a.nb : 0, bytes);
-            copy8(ring.at(to, PIECES - 1), a.stats_pre + t0 + (i + on), i + on < n ? 8 : 0);
+            Du.copy(ring, to, PR, at + on * d, 0, live);
+            R1.copy(ring, to, PR + PU, at + on * d, Q8 ? sat + on * a.nb : 0, live);
+            copy8(ring.at(to, PIECES - 1) + ring.own, a.stats_pre + t0 + (i + on), live ? 8 : 0);
         }
     };
     auto copy_second = [&](int to, int i, int on) {
-        const int bytes = i + on < n && act ? 16 : 0;
-        if (has_f) Fo.copy(ring, to, 2 * PR + PU, at + on * d, Q8 ? sat + on * a.nb : 0, bytes);
-        if (post) copy8(ring.at(to, PIECES - 1) + 8, a.stats_post + t0 + (i + on), i + on < n ? 8 : 0);
+        const bool live = i + on < n;
+        if (has_f) Fo.copy(ring, to, 2 * PR + PU, at + on * d, Q8 ? sat + on * a.nb : 0, live);
+        if (post) copy8(ring.at(to, PIECES - 1) + ring.own + 8, a.stats_post + t0 + (i + on), live ? 8 : 0);
     };
     if constexpr (!BIG) {
         copy_first(0, 0, 0);
@@ -839,6 +873,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
             if (norm) st1[0] = a.stats_pre[t0 + i];
         } else {
             cp_async_wait<1>();
+            __syncwarp();   // the other lanes' copies
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
                 if (has_dr) dR[k] = Dr.get(ring, slot ^ k, 0);
@@ -846,10 +881,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
                 if (norm) {
                     x1[k] = R1.get(ring, slot ^ k, PR + PU);
                     du[k] = Du.get(ring, slot ^ k, PR);
-                    const ulonglong2 q = ld_shared(ring.at(slot ^ k, PIECES - 1));
+                    const ulonglong2 q = ld_shared(ring.at(slot ^ k, PIECES - 1) + ring.own);
                     f2_unpack(q.x, st1[k].x, st1[k].y);
                 }
             }
+            __syncwarp();   // read by all lanes
             copy_first(slot, i, 2);
             if (two) copy_first(slot ^ 1, i, 3);
             cp_async_commit();
@@ -901,7 +937,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
             for (int k = 0; k < ROWS; ++k) {
                 if (has_f) x2[k] = Fo.get(ring, slot ^ k, 2 * PR + PU);
                 else x2[k] = p8_of(0.f);
-                const ulonglong2 q = ld_shared(ring.at(slot ^ k, PIECES - 1));
+                const ulonglong2 q = ld_shared(ring.at(slot ^ k, PIECES - 1) + ring.own);
                 f2_unpack(q.y, st2[k].x, st2[k].y);
             }
             copy_second(slot, i, 2);
