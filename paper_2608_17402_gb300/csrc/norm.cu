@@ -134,55 +134,68 @@ __device__ __forceinline__ P8 ld_param(const float* p, int col, bool act, float 
 // ------------------------------------------------------------ 8-bit checkpoints
 
 // The whole number nearest to 127 x / amax, an even one between two, where y, that value in fp32
-// (off by less than 2^-15), is too near to a border to tell: 254 x and (2 n + 1) amax, both exact in
-// fp64, decide.
+// (off by at most 127 * 2^-21), is too near to a border to tell: 254 x and (2 n + 1) amax, both exact
+// in fp64, decide.
 __device__ __noinline__ float q8_border(float x, float y, float amax) {
     const float n = floorf(y);
     const double t = 254.0 * (double)x - (2.0 * (double)n + 1.0) * (double)amax;
     const bool even = ((int)n & 1) == 0;
     return (t > 0.0 || (t == 0.0 && !even)) ? n + 1.0f : n;
 }
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN where one of them is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 
-// Codes of this thread's 8 columns and the scale of the block of 128 that 16 threads share (all of
-// them here).  A block that holds an infinity or a NaN gets scale NaN; one whose values all lie
-// below 2^-110 is kept as zeros.
-__device__ __forceinline__ uint2 q8_block(const P8& v, bool act, float& scale) {
-    constexpr float R127 = 1.0f / 127.0f;
+// Codes of this thread's 8 columns (zeros behind a row's end) and the scale of the block of 128 that
+// 16 threads share, all of them here.  A block that holds an infinity or a NaN gets scale NaN; one
+// whose values all lie below 2^-110 is kept as zeros.
+__device__ __forceinline__ uint2 q8_block(const P8& v, float& scale) {
     constexpr float ROUND = 12582912.0f;   // 1.5 * 2^23: adding it rounds to a whole number, whose low byte it shows
+    constexpr float NEAR = 0.4999f;        // 0.5 less more than y can be off
+    constexpr float R127 = 1.0f / 127.0f;
     float x[8];
-    uint32_t m = 0;   // the bits of |x| order as the values do, infinities and NaN above them
 #pragma unroll
     for (int i = 0; i < 4; ++i) f2_unpack(v.p[i], x[2 * i], x[2 * i + 1]);
+    float amax = fabsf(x[0]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
-    if (!act) m = 0;
+    for (int i = 1; i < 8; ++i) amax = max_nan(amax, fabsf(x[i]));
 #pragma unroll
-    for (int o = 8; o; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float amax = __uint_as_float(m);
-    if (m >= 0x7f800000u || amax < Q8_LEAST) {
-        scale = m >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : 0.f;
+    for (int o = 8; o; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if (!(amax >= Q8_LEAST && amax <= 3.402823466e38f)) {
+        scale = amax < Q8_LEAST ? 0.f : __uint_as_float(0x7fffffffu);
         return make_uint2(0u, 0u);
     }
-    float inv;   // good to 2^-22, which q8_border's test allows for
+    // 127 / amax, a little more than that (by 2^-22): the one border that whole blocks meet often,
+    // 63.5 at x = amax / 2, is then rounded to 64, as it has to be
+    float inv;
     asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(amax));
-    inv *= 127.0f;
+    inv *= 127.0f * (1.0f + 0x1p-22f);
     // amax / 127, correctly rounded (Markstein: the remainder of a quotient within one unit corrects it)
     const float guess = amax * R127;
     scale = fmaf(fmaf(-127.0f, guess, amax), R127, guess);
     uint32_t q[8];
-    bool border = false;
+    float e[8], worst = 0.f;
+    const uint64_t in2 = f2_of(inv), up = f2_of(ROUND), down = f2_of(-ROUND), minus = f2_of(-1.0f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float y = x[i] * inv, r = y + ROUND;
-        q[i] = __float_as_uint(r);
-        border |= fabsf(y - (r - ROUND)) > 0.4999f;
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t y = f2_mul(v.p[i], in2), r = f2_add(y, up);
+        float r0, r1;
+        f2_unpack(r, r0, r1);
+        q[2 * i] = __float_as_uint(r0);
+        q[2 * i + 1] = __float_as_uint(r1);
+        f2_unpack(f2_fma(f2_add(r, down), minus, y), e[2 * i], e[2 * i + 1]);
+        worst = fmaxf(worst, fmaxf(fabsf(e[2 * i]), fabsf(e[2 * i + 1])));
     }
-    if (border) {
+    if (worst > NEAR) {
+        bool border = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float y = x[i] * inv;
-            if (fabsf(y - (__uint_as_float(q[i]) - ROUND)) > 0.4999f)
-                q[i] = __float_as_uint(q8_border(x[i], y, amax) + ROUND);
+        for (int i = 0; i < 8; ++i) border |= fabsf(e[i]) > NEAR && fabsf(x[i]) != 0.5f * amax;
+        if (border) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (fabsf(e[i]) > NEAR) q[i] = __float_as_uint(q8_border(x[i], x[i] * inv, amax) + ROUND);
         }
     }
     uint2 c;
@@ -242,7 +255,7 @@ __global__ void __launch_bounds__(256) q8_store_kernel(const void* x, int64_t T,
             float scale;
             P8 v = p8_of(0.f);
             if (act[n]) v = F32 ? p8_f32(lo[n], hi[n]) : p8_bf16(lo[n]);
-            const uint2 c = q8_block(v, act[n], scale);
+            const uint2 c = q8_block(v, scale);
             if (act[n]) *reinterpret_cast<uint2*>(codes + at[n]) = c;
             if (lane16 == 0 && sat[n] >= 0) scales[sat[n]] = scale;
         }
@@ -650,13 +663,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_
                 const int64_t sat = (t0 + i + k) * a.nb + (col >> 7);
                 if (a.qr) {
                     float scale;
-                    const uint2 c = q8_block(r[k], act, scale);
+                    const uint2 c = q8_block(r[k], scale);
                     if (live) *reinterpret_cast<uint2*>(a.qr + at + k * d) = c;
                     if (live && (g.lane & 15) == 0) a.qr_scale[sat] = scale;
                 }
                 if (JOIN && a.qf) {
                     float scale;
-                    const uint2 c = q8_block(x[k], act, scale);
+                    const uint2 c = q8_block(x[k], scale);
                     if (live) *reinterpret_cast<uint2*>(a.qf + at + k * d) = c;
                     if (live && (g.lane & 15) == 0) a.qf_scale[sat] = scale;
                 }
@@ -1002,83 +1015,106 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
 
 // The records of norm_backward_kernel added up, in a fixed order.  A CTA of 32 x 32 threads takes
 // 32 columns; its rows of threads share the records out.  blockIdx.y: 0 dw_pre and db_pre; 1 dw_post
-// and db_post (and dgate, where there is one run); 2 and on the gradients of the runs' gates.
+// and db_post (and dgate, where there is one run).
 __global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSumArgs a) {
     __shared__ float s_a[32][33], s_b[32][33];
     pdl_wait();
     const int x = threadIdx.x, y = threadIdx.y;
     const int col = blockIdx.x * 32 + x;
-    const bool act = col < a.d;
+    const bool act = col < a.d, pre = blockIdx.y == 0;
     const int64_t row = 2 * (int64_t)a.d;   // floats of a record
-
-    auto total = [&](float& va, float& vb) {   // over the 32 rows of threads, in row 0
-        s_a[y][x] = va;
-        s_b[y][x] = vb;
-        __syncthreads();
-        va = vb = 0.f;
-        if (y == 0) {
+    const float* rec = pre ? a.rec_pre : a.rec_post;
+    if (!rec) return;
+    rec += col;
+    float va = 0.f, vb = 0.f;
+    if (act) {
+        if (pre || a.G == 1) {
+#pragma unroll 8
+            for (int64_t i = y; i < a.n_groups; i += 32) {
+                va += rec[i * row];
+                vb += rec[i * row + a.d];
+            }
+        } else {   // each record by the gate of its run
+            const float* gate = a.gate ? a.gate + col : nullptr;
+            for (int64_t i = y; i < a.n_groups; i += 4 * 32) {
+                int2 runs[4];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) va += s_a[i][x], vb += s_b[i][x];
-        }
-        __syncthreads();
-    };
-    auto add_records = [&](const float* rec, int64_t lo, int64_t hi, float& va, float& vb) {
-        if (!act) return;
-#pragma unroll 4
-        for (int64_t i = lo + y; i < hi; i += 32) {
-            const float* p = rec + i * row + col;
-            va += p[0];
-            vb += p[a.d];
-        }
-    };
-    const float w2 = act && a.w_post ? a.w_post[col] : 1.f;
-    const float b2 = act && a.b_post ? a.b_post[col] : 0.f;
-
-    if (blockIdx.y == 0) {
-        if (!a.rec_pre) return;
-        float va = 0.f, vb = 0.f;
-        add_records(a.rec_pre, 0, a.n_groups, va, vb);
-        total(va, vb);
-        if (y == 0 && act) {
-            if (a.dw_pre) a.dw_pre[col] = va;
-            if (a.db_pre) a.db_pre[col] = vb;
-        }
-        return;
-    }
-    if (!a.rec_post) return;
-    if (blockIdx.y == 1) {
-        float va = 0.f, vb = 0.f;
-        if (a.G == 1) {
-            add_records(a.rec_post, 0, a.n_groups, va, vb);
-        } else if (act) {
-            for (int64_t gid = y; gid < a.n_groups; gid += 32) {
-                const int2 runs = a.group_runs[gid];
-                for (int64_t g = runs.x; g <= runs.y; ++g) {
-                    const float* p = a.rec_post + (g + gid) * row + col;
-                    const float gt = a.gate ? a.gate[g * a.d + col] : 1.f;
+                for (int u = 0; u < 4; ++u)
+                    runs[u] = i + 32 * u < a.n_groups ? a.group_runs[i + 32 * u] : make_int2(0, -1);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (runs[u].x > runs[u].y) continue;
+                    const int64_t g = runs[u].x;
+                    const float* p = rec + (g + i + 32 * u) * row;
+                    const float gt = gate ? gate[g * a.d] : 1.f;
                     va = fmaf(gt, p[0], va);
                     vb = fmaf(gt, p[a.d], vb);
                 }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    for (int64_t g = (int64_t)runs[u].x + 1; g <= runs[u].y; ++g) {
+                        const float* p = rec + (g + i + 32 * u) * row;
+                        const float gt = gate ? gate[g * a.d] : 1.f;
+                        va = fmaf(gt, p[0], va);
+                        vb = fmaf(gt, p[a.d], vb);
+                    }
             }
         }
-        total(va, vb);
-        if (y == 0 && act) {
-            const float gt = a.G == 1 && a.gate ? a.gate[col] : 1.f;
-            if (a.dw_post) a.dw_post[col] = gt * va;
-            if (a.db_post) a.db_post[col] = gt * vb;
-            if (a.G == 1 && a.dgate) a.dgate[col] = fmaf(w2, va, b2 * vb);
-        }
+    }
+    s_a[y][x] = va;
+    s_b[y][x] = vb;
+    __syncthreads();
+    if (y != 0 || !act) return;
+    va = vb = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) va += s_a[i][x], vb += s_b[i][x];
+    if (pre) {
+        if (a.dw_pre) a.dw_pre[col] = va;
+        if (a.db_pre) a.db_pre[col] = vb;
         return;
     }
-    for (int64_t g = blockIdx.y - 2; g < a.G; g += gridDim.y - 2) {
+    const float gt = a.G == 1 && a.gate ? a.gate[col] : 1.f;
+    if (a.dw_post) a.dw_post[col] = gt * va;
+    if (a.db_post) a.db_post[col] = gt * vb;
+    if (a.G == 1 && a.dgate)
+        a.dgate[col] = fmaf(a.w_post ? a.w_post[col] : 1.f, va, (a.b_post ? a.b_post[col] : 0.f) * vb);
+}
+
+// dgate of several runs: a CTA of 32 x 8 threads takes 32 columns of 8 / lanes runs, `lanes` rows of
+// threads to the records of each (one where a run has few).
+__global__ void __launch_bounds__(256) norm_gates_kernel(const NormSumArgs a, int lanes) {
+    __shared__ float s_a[8][33], s_b[8][33];
+    pdl_wait();
+    const int x = threadIdx.x, y = threadIdx.y, l = y % lanes;
+    const int col = blockIdx.x * 32 + x;
+    const int64_t row = 2 * (int64_t)a.d;
+    const int each = 8 / lanes;
+    const float w2 = a.w_post && col < a.d ? a.w_post[col] : 1.f;
+    const float b2 = a.b_post && col < a.d ? a.b_post[col] : 0.f;
+    for (int64_t g0 = (int64_t)blockIdx.y * each; g0 < a.G; g0 += (int64_t)gridDim.y * each) {
+        const int64_t g = g0 + y / lanes;
         float va = 0.f, vb = 0.f;
-        const int64_t r0 = max((int64_t)a.seg[g], (int64_t)0), r1 = min((int64_t)a.seg[g + 1], a.T);
-        if (r0 < r1) {
-            const int64_t lo = group_of(a.T, r0, a.n_groups), hi = group_of(a.T, r1 - 1, a.n_groups);
-            add_records(a.rec_post + g * row, lo, hi + 1, va, vb);
+        if (g < a.G && col < a.d) {
+            const int64_t r0 = max((int64_t)a.seg[g], (int64_t)0), r1 = min((int64_t)a.seg[g + 1], a.T);
+            if (r0 < r1) {
+                const int64_t hi = group_of(a.T, r1 - 1, a.n_groups);
+                const float* rec = a.rec_post + g * row + col;
+#pragma unroll 4
+                for (int64_t i = group_of(a.T, r0, a.n_groups) + l; i <= hi; i += lanes) {
+                    va += rec[i * row];
+                    vb += rec[i * row + a.d];
+                }
+            }
         }
-        total(va, vb);
-        if (y == 0 && act) a.dgate[g * a.d + col] = fmaf(w2, va, b2 * vb);
+        if (lanes > 1) {
+            s_a[y][x] = va;
+            s_b[y][x] = vb;
+            __syncthreads();
+            va = vb = 0.f;
+            for (int i = 0; i < lanes; ++i) va += s_a[y - l + i][x], vb += s_b[y - l + i][x];
+            __syncthreads();
+        }
+        if (l == 0 && g < a.G && col < a.d) a.dgate[g * a.d + col] = fmaf(w2, va, b2 * vb);
     }
 }
 
@@ -1097,7 +1133,7 @@ NormPlan norm_plan(int64_t T, int d, int threads_sm) {
     p.n_groups = std::min<int64_t>(T, (int64_t)p.grid * p.groups);
     return p;
 }
-constexpr int NORM_FWD_THREADS = 672, NORM_BWD_THREADS = 512;
+constexpr int NORM_FWD_THREADS = 768, NORM_BWD_THREADS = 512;
 constexpr int NORM_MAX_SMEM = 208 * 1024;   // 1024 threads with three rows of fp32 and bf16 each
 
 template <bool F32>
@@ -1209,9 +1245,18 @@ cudaError_t launch_norm_backward(NormBwdArgs a, int r_f32, int du_f32, NormSumAr
     count_launches(1);
     if (e != cudaSuccess || (!a.rec_pre && !a.rec_post)) return e;
     sums.n_groups = a.n_groups;
-    const int64_t gates = sums.G > 1 && sums.dgate ? std::min<int64_t>(sums.G, 4096) : 0;
-    e = launch_pdl(norm_sums_kernel, dim3((unsigned)((a.d + 31) / 32), (unsigned)(2 + gates)), dim3(32, 32), 0, s, sums);
-    count_launches(1);
+    const unsigned cols = (unsigned)((a.d + 31) / 32);
+    if (sums.rec_pre || sums.dw_post || sums.db_post || sums.G == 1) {
+        e = launch_pdl(norm_sums_kernel, dim3(cols, 2), dim3(32, 32), 0, s, sums);
+        count_launches(1);
+        if (e != cudaSuccess) return e;
+    }
+    if (sums.G > 1 && sums.dgate) {
+        const int lanes = a.n_groups / sums.G >= 16 ? 8 : 1;
+        const int64_t each = 8 / lanes, rows = std::min<int64_t>((sums.G + each - 1) / each, 4096);
+        e = launch_pdl(norm_gates_kernel, dim3(cols, (unsigned)rows), dim3(32, 8), 0, s, sums, lanes);
+        count_launches(1);
+    }
     return e;
 }
 
