@@ -113,6 +113,20 @@ __device__ __forceinline__ bool grid_barrier(DevStatus* st, unsigned nblocks, ui
     return s_ok != 0;
 }
 
+// The run that row t lies in, of runs [seg[g], seg[g + 1]): the last g < G with seg[g] <= t, 0 where
+// there is none.  By a whole warp, which looks at 32 of them at a time.
+__device__ __forceinline__ int64_t warp_run_of(const int32_t* seg, int64_t G, int64_t t) {
+    int64_t lo = 0, n = G;   // it is one of the n from lo on
+    while (n > 1) {
+        const int64_t step = (n + 31) / 32, at = lo + (threadIdx.x & 31) * step;
+        const unsigned below = __ballot_sync(0xffffffffu, at < lo + n && seg[at] <= t);
+        const int hit = below ? 31 - __clz(below) : 0;   // (the lanes below it, too, where seg ascends)
+        n = min(step, lo + n - (lo + hit * step));
+        lo += hit * step;
+    }
+    return lo;
+}
+
 // Programmatic dependent launch: a kernel launched with programmatic stream
 // serialization may start while its predecessor finishes; it waits here (at the
 // top, before touching anything the predecessor writes) until that predecessor has

@@ -528,7 +528,7 @@ cudaError_t launch_q8_load(const int8_t* codes, const float* scales, int64_t T, 
 
 // ----------------------------------------- balance loss (balance.cu)
 
-constexpr int BAL_MAX_PARTS = 32;   // CTAs that count one run's ids
+constexpr int BAL_MAX_PARTS = 64;   // CTAs that count one run's ids
 struct BalanceArgs {
     const float* s;
     const int32_t* idx;
@@ -540,7 +540,8 @@ struct BalanceArgs {
     double2* cta_sum;       // [grid]: sum of p . c and number of rows with a probability
     DevStatus* st;
     int64_t T, G, ld_s, ld_ds;
-    int E, k, parts, score;
+    int E, k, score;
+    int parts;              // of a run, counted by bal_count_kernel; 0: counted by bal_main_kernel
     float coef;
 };
 int bal_parts(int64_t T, int64_t k, int64_t G);

@@ -210,82 +210,85 @@ __device__ __forceinline__ uint2 q8_block(const P8& v, float& scale) {
 constexpr int Q8_UNITS = 4;
 
 struct BlockWalk {
-    int64_t row;
-    int block;
-    __device__ __forceinline__ BlockWalk(int64_t u, int nb) : row(u / nb), block((int)(u - row * nb)) {}
-    __device__ __forceinline__ void advance(int64_t step_rows, int step_blocks, int nb) {
-        row += step_rows;
+    int64_t u, at;   // the block's number, and this thread's first element of it
+    int block;       // its place in its row
+    __device__ __forceinline__ BlockWalk(int nb, int d) {
+        u = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+        const int64_t row = u / nb;
+        block = (int)(u - row * nb);
+        at = row * d + block * 128 + (threadIdx.x & 15) * 8;
+    }
+    // step blocks on: step_at elements and step_blocks places, or so much less a row's
+    __device__ __forceinline__ void advance(int64_t step, int64_t step_at, int step_blocks, int nb, int d) {
+        u += step;
+        at += step_at;
         block += step_blocks;
         if (block >= nb) {
             block -= nb;
-            ++row;
+            at += d - nb * 128;
         }
     }
+    __device__ __forceinline__ bool in_row(int d) const { return block * 128 + (int)(threadIdx.x & 15) * 8 < d; }
 };
 
 template <bool F32>
-__global__ void __launch_bounds__(256) q8_store_kernel(const void* x, int64_t T, int d, int nb, int64_t step_rows,
-                                                       int step_blocks, int8_t* codes, float* scales) {
+__global__ void __launch_bounds__(256, F32 ? 3 : 4) q8_store_kernel(const void* x, int64_t blocks, int d, int nb, int64_t step_at,
+                                                          int step_blocks, int8_t* codes, float* scales) {
     pdl_wait();
-    const int lane16 = threadIdx.x & 15;
-    BlockWalk w((int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), nb);
+    const int64_t step = (int64_t)gridDim.x * 16;
+    BlockWalk w(nb, d);
     // a warp's two blocks leave the loop together: its shuffles need both
-    while (__any_sync(0xffffffffu, w.row < T)) {
+    while (__any_sync(0xffffffffu, w.u < blocks)) {
         uint4 lo[Q8_UNITS], hi[Q8_UNITS];
-        int64_t at[Q8_UNITS], sat[Q8_UNITS];
-        bool act[Q8_UNITS];
+        BlockWalk r = w;
 #pragma unroll
         for (int n = 0; n < Q8_UNITS; ++n) {
-            const int col = w.block * 128 + lane16 * 8;
-            act[n] = w.row < T && col < d;
-            at[n] = w.row * d + col;
-            sat[n] = w.row < T ? w.row * nb + w.block : -1;
-            if (act[n]) {
+            lo[n] = hi[n] = make_uint4(0u, 0u, 0u, 0u);
+            if (r.u < blocks && r.in_row(d)) {
                 if constexpr (F32) {
-                    lo[n] = ld16(static_cast<const float*>(x) + at[n]);
-                    hi[n] = ld16(static_cast<const float*>(x) + at[n] + 4);
+                    lo[n] = ld16(static_cast<const float*>(x) + r.at);
+                    hi[n] = ld16(static_cast<const float*>(x) + r.at + 4);
                 } else {
-                    lo[n] = ld16(static_cast<const __nv_bfloat16*>(x) + at[n]);
+                    lo[n] = ld16(static_cast<const __nv_bfloat16*>(x) + r.at);
                 }
             }
-            w.advance(step_rows, step_blocks, nb);
+            r.advance(step, step_at, step_blocks, nb, d);
         }
 #pragma unroll
         for (int n = 0; n < Q8_UNITS; ++n) {
             float scale;
-            P8 v = p8_of(0.f);
-            if (act[n]) v = F32 ? p8_f32(lo[n], hi[n]) : p8_bf16(lo[n]);
-            const uint2 c = q8_block(v, scale);
-            if (act[n]) *reinterpret_cast<uint2*>(codes + at[n]) = c;
-            if (lane16 == 0 && sat[n] >= 0) scales[sat[n]] = scale;
+            const uint2 c = q8_block(F32 ? p8_f32(lo[n], hi[n]) : p8_bf16(lo[n]), scale);
+            if (w.u < blocks) {
+                if (w.in_row(d)) *reinterpret_cast<uint2*>(codes + w.at) = c;
+                if ((threadIdx.x & 15) == 0) scales[w.u] = scale;
+            }
+            w.advance(step, step_at, step_blocks, nb, d);
         }
     }
 }
 
 template <bool F32>
-__global__ void __launch_bounds__(256) q8_load_kernel(const int8_t* codes, const float* scales, int64_t T, int d, int nb,
-                                                      int64_t step_rows, int step_blocks, void* x) {
+__global__ void __launch_bounds__(256) q8_load_kernel(const int8_t* codes, const float* scales, int64_t blocks, int d,
+                                                      int nb, int64_t step_at, int step_blocks, void* x) {
     pdl_wait();
-    const int lane16 = threadIdx.x & 15;
-    BlockWalk w((int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), nb);
-    while (w.row < T) {
+    const int64_t step = (int64_t)gridDim.x * 16;
+    BlockWalk w(nb, d);
+    while (w.u < blocks) {
         uint2 c[Q8_UNITS];
         float scale[Q8_UNITS];
-        int64_t at[Q8_UNITS];
+        BlockWalk r = w;
 #pragma unroll
         for (int n = 0; n < Q8_UNITS; ++n) {
-            const int col = w.block * 128 + lane16 * 8;
-            at[n] = w.row < T && col < d ? w.row * d + col : -1;
-            if (at[n] >= 0) {
-                c[n] = ld8(codes + at[n]);
-                scale[n] = scales[w.row * nb + w.block];
+            if (r.u < blocks && r.in_row(d)) {
+                c[n] = ld8(codes + r.at);
+                scale[n] = scales[r.u];
             }
-            w.advance(step_rows, step_blocks, nb);
+            r.advance(step, step_at, step_blocks, nb, d);
         }
 #pragma unroll
         for (int n = 0; n < Q8_UNITS; ++n) {
-            if (at[n] < 0) continue;
-            st_rows<F32>(x, at[n], p8_codes(c[n].x, c[n].y, scale[n]));
+            if (w.u < blocks && w.in_row(d)) st_rows<F32>(x, w.at, p8_codes(c[n].x, c[n].y, scale[n]));
+            w.advance(step, step_at, step_blocks, nb, d);
         }
     }
 }
@@ -396,17 +399,6 @@ __device__ __forceinline__ void row_stats(RowGroup& g, P8 (&x)[ROWS], bool act, 
 }
 
 // ------------------------------------------------------------ runs of rows
-
-// The run (segment) that row t lies in: the last g with seg[g] <= t, 0 where there is none.
-__device__ __forceinline__ int64_t run_of(const int32_t* seg, int64_t G, int64_t t) {
-    int64_t lo = 0, hi = G;   // seg[lo] <= t < seg[hi], as far as seg says
-    while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (seg[mid] <= t) lo = mid;
-        else hi = mid;
-    }
-    return lo;
-}
 
 // Rows [t0, t1) of group gid of n_groups <= T (each has some); group_of is its inverse.
 __device__ __forceinline__ int64_t first_row(int64_t T, int64_t gid, int64_t n_groups) { return T * gid / n_groups; }
@@ -624,7 +616,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_
             run_end = n;
             if (a.seg) {
                 const int64_t t = t0 + i;
-                run = run < 0 ? run_of(a.seg, a.G, t) : run + 1;
+                run = run < 0 ? warp_run_of(a.seg, a.G, t) : run + 1;
                 while (run + 1 < a.G && a.seg[run + 1] <= t) ++run;
                 run_end = (int)(min((int64_t)a.seg[run + 1], t1) - t0);
             } else {
@@ -857,7 +849,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     auto end_of_run = [&]() { return run + 1 < a.G ? (int)(min((int64_t)a.seg[run + 1], t1) - t0) : n; };
     if (n > 0) {
         if (a.seg) {
-            run = run_of(a.seg, a.G, t0);
+            run = warp_run_of(a.seg, a.G, t0);
             run_end = end_of_run();
         }
         load_run();
@@ -1136,21 +1128,28 @@ NormPlan norm_plan(int64_t T, int d, int threads_sm) {
 constexpr int NORM_FWD_THREADS = 768, NORM_BWD_THREADS = 512;
 constexpr int NORM_MAX_SMEM = 208 * 1024;   // 1024 threads with three rows of fp32 and bf16 each
 
+// Grid of the checkpoint kernels and the step of their walk over the blocks, CTAs_SM to an SM at most.
+struct BlockPlan {
+    int nb, grid, step_blocks;
+    int64_t blocks, step_at;
+    BlockPlan(int64_t T, int d, int ctas_sm) : nb((d + 127) / 128), blocks(T * nb) {
+        grid = (int)std::min<int64_t>((blocks + 16 * Q8_UNITS - 1) / (16 * Q8_UNITS), (int64_t)GB300_SMS * ctas_sm);
+        const int64_t step = (int64_t)grid * 16;
+        step_blocks = (int)(step % nb);
+        step_at = step / nb * d + step_blocks * 128;
+    }
+};
 template <bool F32>
 cudaError_t q8_store(const void* x, int64_t T, int d, int8_t* codes, float* scales, cudaStream_t s) {
-    const int nb = (d + 127) / 128;
-    const int64_t grid = std::min<int64_t>((T * nb + 16 * Q8_UNITS - 1) / (16 * Q8_UNITS), (int64_t)GB300_SMS * 8);
-    const int64_t step = grid * 16;
-    return launch_pdl(q8_store_kernel<F32>, dim3((unsigned)grid), dim3(256), 0, s, x, T, d, nb, step / nb, (int)(step % nb),
-                      codes, scales);
+    const BlockPlan p(T, d, F32 ? 3 : 4);
+    return launch_pdl(q8_store_kernel<F32>, dim3(p.grid), dim3(256), 0, s, x, p.blocks, d, p.nb, p.step_at,
+                      p.step_blocks, codes, scales);
 }
 template <bool F32>
 cudaError_t q8_load(const int8_t* codes, const float* scales, int64_t T, int d, void* x, cudaStream_t s) {
-    const int nb = (d + 127) / 128;
-    const int64_t grid = std::min<int64_t>((T * nb + 16 * Q8_UNITS - 1) / (16 * Q8_UNITS), (int64_t)GB300_SMS * 8);
-    const int64_t step = grid * 16;
-    return launch_pdl(q8_load_kernel<F32>, dim3((unsigned)grid), dim3(256), 0, s, codes, scales, T, d, nb, step / nb,
-                      (int)(step % nb), x);
+    const BlockPlan p(T, d, 6);
+    return launch_pdl(q8_load_kernel<F32>, dim3(p.grid), dim3(256), 0, s, codes, scales, p.blocks, d, p.nb, p.step_at,
+                      p.step_blocks, x);
 }
 
 }  // namespace
