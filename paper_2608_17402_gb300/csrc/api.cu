@@ -1203,7 +1203,7 @@ BalanceLayout balance_layout(int64_t T, int64_t E, int64_t k, int64_t G) {
     BalanceLayout L;
     size_t o = sizeof(DevStatus);
     L.cta_sum = o;
-    o += up256(BAL_MAX_GRID * sizeof(double2));
+    o += up256(BAL_MAX_GRID * sizeof(float2));
     L.part = o;
     o += up256((size_t)bal_max_parts(T, k, G) * E * 4);
     L.total = o;
@@ -1397,7 +1397,7 @@ moevie_status moevie_balance_loss(const float* s, int64_t ld_s, const int32_t* i
     a.counts = counts;
     a.ds = ds;
     a.part = at<int32_t>(ws, L.part);
-    a.cta_sum = at<double2>(ws, L.cta_sum);
+    a.cta_sum = at<float2>(ws, L.cta_sum);
     a.st = static_cast<DevStatus*>(ws);
     a.T = T;
     a.G = G;

@@ -78,49 +78,94 @@ __global__ void __launch_bounds__(BAL_COUNT_THREADS) bal_count_kernel(const Bala
     }
 }
 
-// e^x for x <= 0 to a few units in the last place: 2^t with t = x / ln 2 in two pieces, the lower one
-// by its first-order term (x below -126 ln 2: 0).
+// e^x for x <= 0: 2^(x / ln 2), whose exponent's rounding makes it off by up to |x| 2^-24 of itself
+// and a few units; 0 at minus infinity.
 __device__ __forceinline__ float exp_neg(float x) {
-    constexpr float L2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
-    const float t = x * L2E;
-    const float low = fmaf(x, L2E, -t);   // exact; the rounding of L2E itself is below 2^-26 of t
     float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
-    return t < -126.f ? 0.f : fmaf(r, low * LN2, r);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.44269504088896341f));
+    return r;
+}
+__device__ __forceinline__ uint64_t f2_of(float v) { return f2_pack(v, v); }
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// v[n] <- its sum over the LP lanes of a token, in all of them.  Four sums share the shuffles: after
+// the first two steps each lane carries one of them, the n-th lanes n LP / 4 on.
+template <int LP, int N>
+__device__ __forceinline__ void lane_sums(float (&v)[N]) {
+    if constexpr (N == 4 && LP >= 8) {
+        const int lane = threadIdx.x & 31;
+        const bool up = lane & (LP / 2), up2 = lane & (LP / 4);
+        const float a = (up ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[2], LP / 2);
+        const float b = (up ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, up ? v[1] : v[3], LP / 2);
+        float x = (up2 ? b : a) + __shfl_xor_sync(0xffffffffu, up2 ? a : b, LP / 4);
+#pragma unroll
+        for (int o = LP / 8; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) v[n] = __shfl_sync(0xffffffffu, x, (lane & ~(LP - 1)) + n * (LP / 4));
+    } else {
+#pragma unroll
+        for (int o = LP / 2; o; o >>= 1)
+#pragma unroll
+            for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
+    }
+}
+
+// The even load less than the run's: c of every expert, in s_c[0, n) (0 behind the last).  s_hist: scratch.
+__device__ __forceinline__ void run_loads(const BalanceArgs& a, int64_t b, int64_t r0, int64_t r1, float per_row,
+                                          bool mine, int n, int* s_hist, float* s_c) {
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.E; e += BAL_THREADS) s_hist[e] = 0;
+    __syncthreads();
+    if (a.parts == 0) {
+        count_ids(a, r0 * a.k, r1 * a.k, s_hist);
+    } else {   // threads share the parts of an expert
+        const int lanes = max(1, BAL_THREADS / a.E);
+        for (int i = threadIdx.x; i < a.E * lanes; i += BAL_THREADS) {
+            const int e = i % a.E;
+            int sum = 0;
+#pragma unroll 16
+            for (int p = i / a.E; p < a.parts; p += lanes) sum += a.part[(b * a.parts + p) * a.E + e];
+            atomicAdd(&s_hist[e], sum);
+        }
+    }
+    __syncthreads();
+    const float scale = per_row / ((float)a.k * (float)(r1 - r0));   // coef / (T k T_b)
+    for (int e = threadIdx.x; e < n; e += BAL_THREADS) {
+        const int count = e < a.E ? s_hist[e] : 0;
+        if (mine && e < a.E) a.counts[b * a.E + e] = count;
+        s_c[e] = e < a.E ? scale * (float)((int64_t)a.E * count - (int64_t)a.k * (r1 - r0)) : 0.f;
+    }
+    __syncthreads();
 }
 
 // LP lanes hold a token's logits, VPL groups of VEC columns each; a warp takes 32 / LP tokens at a
 // time, TU times over (the loads of all of them under way together, their sums in one set of
 // shuffles).  8 columns a lane wherever there are as many: fewer leave more of the time to the shuffles.
+// No fp64 on the way: the card's rate for it is 1 / 64 of that for fp32.
 template <int VEC, int LP, int VPL, int TU>
 __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_kernel(const BalanceArgs a) {
-    constexpr int NV = VEC * VPL, TPW = 32 / LP, WARPS = BAL_THREADS / 32;
+    constexpr int NV = VEC * VPL, NP = NV / 2, TPW = 32 / LP, WARPS = BAL_THREADS / 32;
+    static_assert(NV % 2 == 0, "pairs of columns");
     __shared__ __align__(16) float s_c[1024];
     __shared__ int s_hist[1024];
-    __shared__ double s_sum[WARPS];
+    __shared__ float s_sum[WARPS];
     __shared__ int s_rows[WARPS];
     __shared__ unsigned s_last;
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int sub = lane / LP, l = lane % LP;
-    auto column = [&](int v, int j) { return (v * LP + l) * VEC + j; };
+    auto column = [&](int i) { return (i / VEC * LP + l) * VEC + i % VEC; };
 
-    // runs that do not ascend within [0, T]; the loads of runs without a token, and, where they are
-    // counted in parts, of this CTA's share of all runs
+    // runs that do not ascend within [0, T], and the loads of runs without a token
     for (int64_t b = (int64_t)blockIdx.x * BAL_THREADS + threadIdx.x; a.seg && b < a.G; b += (int64_t)gridDim.x * BAL_THREADS) {
         const int x = a.seg[b], y = a.seg[b + 1];
         if (x < 0 || y < x || y > a.T) report(a.st, MOEVIE_ERR_DEVICE, SITE_RUNS, (int)b, y);
-    }
-    for (int64_t b = blockIdx.x; b < a.G; b += gridDim.x) {
-        int64_t r0, r1;
-        run_rows(a, b, r0, r1);
-        if (a.parts == 0 && r1 > r0) continue;
-        for (int e = threadIdx.x; e < a.E; e += BAL_THREADS) {
-            int n = 0;
-#pragma unroll 16
-            for (int p = 0; p < a.parts; ++p) n += a.part[(b * a.parts + p) * a.E + e];
-            a.counts[b * a.E + e] = n;
-        }
+        if (min((int64_t)y, a.T) <= max(x, 0))
+            for (int e = 0; e < a.E; ++e) a.counts[b * a.E + e] = 0;
     }
 
     int64_t lo = 0, hi = a.T;   // rows that lie in some run
@@ -128,8 +173,8 @@ __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_k
         lo = max((int64_t)a.seg[0], (int64_t)0);
         hi = max(lo, min((int64_t)a.seg[a.G], a.T));
     }
-    const double per_row = hi > lo ? (double)a.coef / (double)(hi - lo) : 0.0;
     const int64_t n_rows = hi - lo;
+    const float per_row = n_rows > 0 ? a.coef / (float)n_rows : 0.f;
     const int64_t t0 = lo + n_rows * blockIdx.x / gridDim.x, t1 = lo + n_rows * (blockIdx.x + 1) / gridDim.x;
     float dots = 0.f;   // of the tokens of this lane's group
     int rows = 0;
@@ -139,136 +184,134 @@ __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_k
         run_rows(a, b, r0, r1);
         const int64_t end = min(r1, t1);
         if (end <= t) continue;
-        __syncthreads();
-        if (a.parts == 0) {
-            for (int e = threadIdx.x; e < a.E; e += BAL_THREADS) s_hist[e] = 0;
-            __syncthreads();
-            count_ids(a, r0 * a.k, r1 * a.k, s_hist);
-            __syncthreads();
-        }
-        {   // c of the run: coef / (T k T_b) (E n - k T_b)
-            const double scale = per_row / ((double)a.k * (double)(r1 - r0));
-            const bool mine = a.parts == 0 && r0 >= t0 && r0 < t1;   // its loads are this CTA's to write
-            for (int e = threadIdx.x; e < LP * NV; e += BAL_THREADS) {
-                int n = 0;
-                if (e < a.E) {
-                    if (a.parts == 0) n = s_hist[e];
-#pragma unroll 16
-                    for (int p = 0; p < a.parts; ++p) n += a.part[(b * a.parts + p) * a.E + e];
-                    if (mine) a.counts[b * a.E + e] = n;
-                }
-                s_c[e] = (float)(scale * (double)((int64_t)a.E * n - (int64_t)a.k * (r1 - r0)));
-            }
-        }
-        __syncthreads();
-        float c_reg[NV];   // lanes of more than 8 columns read them from shared memory each time
-        if constexpr (NV <= 8) {
+        run_loads(a, b, r0, r1, per_row, r0 >= t0 && r0 < t1, LP * NV, s_hist, s_c);
+        uint64_t c_reg[NP];   // lanes of more than 8 columns read them from shared memory each time
+        auto c_mem = [&](int i) { return *reinterpret_cast<const uint64_t*>(s_c + column(2 * i)); };
+        if constexpr (VEC == 1) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) c_reg[i] = s_c[column(i / VEC, i % VEC)];
+            for (int i = 0; i < NP; ++i) c_reg[i] = f2_pack(s_c[column(2 * i)], s_c[column(2 * i + 1)]);
+        } else if constexpr (NV <= 8) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) c_reg[i] = c_mem(i);
         }
         auto c = [&](int i) {
-            if constexpr (NV <= 8) return c_reg[i];
-            else return s_c[column(i / VEC, i % VEC)];
+            if constexpr (VEC == 1 || NV <= 8) return c_reg[i];
+            else return c_mem(i);
         };
-        for (int64_t tb = t + (int64_t)warp * TPW * TU; tb < end; tb += (int64_t)WARPS * TPW * TU) {
-            float x[TU][NV], q[TU][NV];   // logits, then scores; and the scores' slopes over themselves
-#pragma unroll
-            for (int u = 0; u < TU; ++u) {
-                const int64_t tt = tb + u * TPW + sub;
+        auto load_row = [&](int64_t tt, uint64_t (&x)[NP]) {
+            const float* src = a.s + tt * a.ld_s;
+            if constexpr (VEC == 4) {
 #pragma unroll
                 for (int v = 0; v < VPL; ++v) {
-                    const bool ok = tt < end && column(v, 0) < a.E;
-                    if constexpr (VEC == 4) {
-                        float4 f = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-                        if (ok) f = *reinterpret_cast<const float4*>(a.s + tt * a.ld_s + column(v, 0));
-                        x[u][v * 4] = f.x, x[u][v * 4 + 1] = f.y, x[u][v * 4 + 2] = f.z, x[u][v * 4 + 3] = f.w;
-                    } else {
-                        x[u][v] = ok ? a.s[tt * a.ld_s + column(v, 0)] : -INFINITY;
-                    }
+                    float4 f = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                    if (tt < end && column(4 * v) < a.E) f = *reinterpret_cast<const float4*>(src + column(4 * v));
+                    x[2 * v] = f2_pack(f.x, f.y);
+                    x[2 * v + 1] = f2_pack(f.z, f.w);
                 }
-            }
-            // e^(x - the row's largest logit), for a softmax; a row without a logit has no probability
-            auto soft = [&](int u) {
-                float m = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) m = fmaxf(m, x[u][i]);
-#pragma unroll
-                for (int o = LP / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                if (m == -INFINITY) m = 0.f;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const float d = x[u][i] - m;
-                    x[u][i] = d != d ? d : exp_neg(d);   // (infinity - infinity)
-                    q[u][i] = 1.f;
-                }
-            };
-            float sums[2 * TU];
-            auto add_up = [&]() {
-#pragma unroll
-                for (int u = 0; u < TU; ++u) {
-                    sums[2 * u] = sums[2 * u + 1] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        sums[2 * u] += x[u][i];
-                        sums[2 * u + 1] = fmaf(x[u][i], c(i), sums[2 * u + 1]);
-                    }
-                }
-#pragma unroll
-                for (int o = LP / 2; o; o >>= 1)
-#pragma unroll
-                    for (int n = 0; n < 2 * TU; ++n) sums[n] += __shfl_xor_sync(0xffffffffu, sums[n], o);
-            };
-            if (a.score == MOEVIE_SCORE_SOFTMAX) {
-#pragma unroll
-                for (int u = 0; u < TU; ++u) soft(u);
-                add_up();
             } else {
-                float keep[TU][NV];
+                float f[NV];
+#pragma unroll
+                for (int i = 0; i < NV; ++i) f[i] = tt < end && column(i) < a.E ? src[column(i)] : -INFINITY;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) x[i] = f2_pack(f[2 * i], f[2 * i + 1]);
+            }
+        };
+        auto add_up = [&](const uint64_t& p, int i, uint64_t (&s)[2]) {
+            s[0] = i ? f2_add(s[0], p) : p;
+            s[1] = i ? f2_fma(p, c(i), s[1]) : f2_mul(p, c(i));
+        };
+        auto total = [&](const uint64_t (&s)[2], float* out) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                float y, z;
+                f2_unpack(s[n], y, z);
+                out[n] = y + z;
+            }
+        };
+        // x <- e^(x - the row's largest logit) = p of a softmax but for its sum, and s its sums, in the
+        // lane; a row without a logit has no probability
+        auto soft = [&](uint64_t (&x)[NP], uint64_t (&s)[2]) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                float y, z;
+                f2_unpack(x[i], y, z);
+                m = fmaxf(m, fmaxf(y, z));
+            }
+#pragma unroll
+            for (int o = LP / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            const uint64_t shift = f2_of(m == -INFINITY ? 0.f : -m);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                float y, z;
+                f2_unpack(f2_add(x[i], shift), y, z);
+                x[i] = f2_pack(exp_neg(y), exp_neg(z));
+                add_up(x[i], i, s);
+            }
+            return m;
+        };
+        for (int64_t tb = t + (int64_t)warp * TPW * TU + sub; tb - sub < end; tb += (int64_t)WARPS * TPW * TU) {
+            uint64_t x[TU][NP];   // logits, then p times its slope by the logit but for sums
+            float sums[2 * TU];   // of p, and of p c
+#pragma unroll
+            for (int u = 0; u < TU; ++u) load_row(tb + u * TPW, x[u]);
+#pragma unroll
+            for (int u = 0; u < TU; ++u) {
+                uint64_t s[2] = {0, 0};
+                if (a.score == MOEVIE_SCORE_SOFTMAX) {
+                    soft(x[u], s);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) {   // sigmoid(v) = r or z r with z = e^-|v|, r = 1 / (1 + z)
+                        float v[2], z[2], r[2];
+                        f2_unpack(x[u][i], v[0], v[1]);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) z[j] = exp_neg(-fabsf(v[j]));
+                        const uint64_t zz = f2_pack(z[0], z[1]);
+                        float d[2];
+                        f2_unpack(f2_add(zz, f2_of(1.f)), d[0], d[1]);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) r[j] = rcp_approx(d[j]);
+                        const uint64_t rr = f2_pack(r[0], r[1]), zr = f2_mul(zz, rr);
+                        float y[2];
+                        f2_unpack(zr, y[0], y[1]);
+                        add_up(f2_pack(v[0] >= 0.f ? r[0] : y[0], v[1] >= 0.f ? r[1] : y[1]), i, s);
+                        x[u][i] = f2_mul(rr, zr);   // sigmoid (1 - sigmoid)
+                    }
+                }
+                total(s, sums + 2 * u);
+            }
+            lane_sums<LP>(sums);
+            if (a.score == MOEVIE_SCORE_SIGMOID) {
+                // Of a row whose logits all lie below -17, sigmoid(s) is e^s to e^-17 of itself, and vanishes
+                // in the end: its probabilities are a softmax.  Its scores add up to less than 1024 e^-17.
                 bool low = false;
 #pragma unroll
-                for (int u = 0; u < TU; ++u) {
-                    float most = 0.f;
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        const float v = x[u][i];
-                        const float z = exp_neg(-fabsf(v));
-                        float r;
-                        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + z));
-                        keep[u][i] = v;
-                        x[u][i] = v >= 0.f ? r : z * r;
-                        q[u][i] = v >= 0.f ? z * r : r;
-                        most = fmaxf(most, x[u][i]);
-                    }
-                    low |= !(most > 1e-18f);
-                }
-                // Sigmoids of a row whose logits all lie below -41 would lose bits, and vanish: there
-                // sigmoid(s) is e^s to e^-41 of itself, and the row's probabilities are a softmax.  (The
-                // rows of a warp go together; whether it is so for a row goes by its largest logit alone.)
+                for (int u = 0; u < TU; ++u) low |= sums[2 * u] < 4.3e-5f;
                 if (__any_sync(0xffffffffu, low)) {
-#pragma unroll
+#pragma unroll 1
                     for (int u = 0; u < TU; ++u) {
-                        float m = -INFINITY;
+                        uint64_t y[NP], s[2] = {0, 0};
+                        load_row(tb + u * TPW, y);
+                        const bool done = soft(y, s) < -17.f;
+                        float w[2];
+                        total(s, w);
+                        lane_sums<LP>(w);
 #pragma unroll
-                        for (int i = 0; i < NV; ++i) m = fmaxf(m, keep[u][i]);
+                        for (int k = 0; k < TU; ++k) {
+                            if (k != u || !done) continue;
+                            sums[2 * k] = w[0];
+                            sums[2 * k + 1] = w[1];
 #pragma unroll
-                        for (int o = LP / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                        if (!(m < -41.f)) continue;
-                        const float shift = m == -INFINITY ? 0.f : m;
-#pragma unroll
-                        for (int i = 0; i < NV; ++i) {
-                            const float d = keep[u][i] - shift;
-                            x[u][i] = d != d ? d : exp_neg(d);
-                            q[u][i] = 1.f;
+                            for (int i = 0; i < NP; ++i) x[k][i] = y[i];
                         }
                     }
                 }
-                add_up();
             }
 #pragma unroll
             for (int u = 0; u < TU; ++u) {
-                const int64_t tt = tb + u * TPW + sub;
+                const int64_t tt = tb + u * TPW;
                 if (tt >= end) continue;
-                float(&p)[NV] = x[u];
                 const float inv = sums[2 * u] == 0.f ? 0.f : 1.f / sums[2 * u];
                 const float dot = sums[2 * u + 1] * inv;
                 if (l == 0) {
@@ -276,17 +319,23 @@ __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_k
                     rows += sums[2 * u] == 0.f ? 0 : 1;
                 }
                 if (!a.ds) continue;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) p[i] *= inv * q[u][i] * (c(i) - dot);
                 float* out = a.ds + tt * a.ld_ds;
+                uint64_t g[NP];
 #pragma unroll
-                for (int v = 0; v < VPL; ++v) {
-                    if (column(v, 0) >= a.E) continue;
-                    if constexpr (VEC == 4)
-                        *reinterpret_cast<float4*>(out + column(v, 0)) =
-                            make_float4(p[v * 4], p[v * 4 + 1], p[v * 4 + 2], p[v * 4 + 3]);
-                    else
-                        out[column(v, 0)] = p[v];
+                for (int i = 0; i < NP; ++i) g[i] = f2_mul(f2_mul(x[u][i], f2_of(inv)), f2_add(c(i), f2_of(-dot)));
+                if constexpr (VEC == 4) {
+#pragma unroll
+                    for (int v = 0; v < VPL; ++v)
+                        if (column(4 * v) < a.E)
+                            *reinterpret_cast<ulonglong2*>(out + column(4 * v)) = make_ulonglong2(g[2 * v], g[2 * v + 1]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) {
+                        float y, z;
+                        f2_unpack(g[i], y, z);
+                        if (column(2 * i) < a.E) out[column(2 * i)] = y;
+                        if (column(2 * i + 1) < a.E) out[column(2 * i + 1)] = z;
+                    }
                 }
             }
         }
@@ -294,39 +343,45 @@ __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_k
     }
 
     // the loss: every CTA's sums, added up in order by the CTA that is done last
-    double sum = dots;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
-        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        dots += __shfl_xor_sync(0xffffffffu, dots, o);
         rows += __shfl_xor_sync(0xffffffffu, rows, o);
     }
     if (lane == 0) {
-        s_sum[warp] = sum;
+        s_sum[warp] = dots;
         s_rows[warp] = rows;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = 0.0;
-        rows = 0;
-        for (int w = 0; w < WARPS; ++w) sum += s_sum[w], rows += s_rows[w];
-        a.cta_sum[blockIdx.x] = make_double2(sum, (double)rows);
+    if (warp != 0) return;
+    dots = lane < WARPS ? s_sum[lane] : 0.f;
+    rows = lane < WARPS ? s_rows[lane] : 0;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        dots += __shfl_xor_sync(0xffffffffu, dots, o);
+        rows += __shfl_xor_sync(0xffffffffu, rows, o);
+    }
+    if (lane == 0) {
+        __stcg(&a.cta_sum[blockIdx.x], make_float2(dots, __int_as_float(rows)));
         __threadfence();
         s_last = atomicInc(&a.st->bal_ticket, gridDim.x - 1) == gridDim.x - 1;   // back to 0 for the next call
+        __threadfence();
     }
-    __syncthreads();
-    if (!s_last || warp != 0) return;
-    __threadfence();
-    double total = 0.0, all = 0.0;
+    __syncwarp();
+    if (!s_last) return;
+    dots = 0.f;
+    int64_t all = 0;
     for (unsigned i = lane; i < gridDim.x; i += 32) {
-        total += __ldcg(&a.cta_sum[i].x);
-        all += __ldcg(&a.cta_sum[i].y);
+        const float2 v = __ldcg(&a.cta_sum[i]);
+        dots += v.x;
+        all += __float_as_int(v.y);
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
-        total += __shfl_xor_sync(0xffffffffu, total, o);
+        dots += __shfl_xor_sync(0xffffffffu, dots, o);
         all += __shfl_xor_sync(0xffffffffu, all, o);
     }
-    if (lane == 0) *a.loss = (float)(total + per_row * all);
+    if (lane == 0) *a.loss = all == n_rows && all > 0 ? a.coef + dots : fmaf(per_row, (float)all, dots);
 }
 
 template <int VEC, int LP, int VPL, int TU>
@@ -369,8 +424,7 @@ cudaError_t launch_balance(const BalanceArgs& a, cudaStream_t s) {
         else if (E <= 512) e = run_main<4, 32, 4, 1>(a, s);
         else e = run_main<4, 32, 8, 1>(a, s);
     } else {   // rows at any alignment
-        if (E <= 8) e = run_main<1, 8, 1, 2>(a, s);
-        else if (E <= 16) e = run_main<1, 8, 2, 2>(a, s);
+        if (E <= 16) e = run_main<1, 8, 2, 2>(a, s);
         else if (E <= 32) e = run_main<1, 8, 4, 2>(a, s);
         else if (E <= 64) e = run_main<1, 8, 8, 2>(a, s);
         else if (E <= 128) e = run_main<1, 16, 8, 2>(a, s);

@@ -537,7 +537,7 @@ struct BalanceArgs {
     int32_t* counts;        // [G][E]
     float* ds;              // or nullptr
     int32_t* part;          // [G][parts][E] counts of parts of a run
-    double2* cta_sum;       // [grid]: sum of p . c and number of rows with a probability
+    float2* cta_sum;        // [grid]: sum of p . c, and the bits of the number of rows with a probability
     DevStatus* st;
     int64_t T, G, ld_s, ld_ds;
     int E, k, score;

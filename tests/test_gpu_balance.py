@@ -149,6 +149,30 @@ def test_nan_stays_in_its_row_and_shows_in_the_loss(score):
     assert torch.equal(got.ds[keep], want.ds[keep]) and torch.equal(got.counts, want.counts)
 
 
+def test_plus_infinity():
+    """A softmax has no value there; sigmoids are 1."""
+    s, idx = make(40, 16, 2)
+    s[3, 5] = float("inf")
+    got = moevie.moevie_balance_loss(s, idx, moevie.BalanceWorkspace(40, 16, 2), 0.03, "softmax")
+    assert bool(torch.isnan(got.loss).all()) and bool(torch.isnan(got.ds[3]).all())
+    assert bool(torch.isfinite(got.ds[[t for t in range(40) if t != 3]]).all())
+    got = moevie.moevie_balance_loss(s, idx, moevie.BalanceWorkspace(40, 16, 2), 0.03, "sigmoid")
+    s[3, 5] = 80.0   # a sigmoid of 1 in fp32, and its slope below every normal number
+    want = moevie.moevie_balance_loss(s, idx, moevie.BalanceWorkspace(40, 16, 2), 0.03, "sigmoid")
+    assert torch.equal(got.loss, want.loss) and float(got.ds[3, 5]) == 0
+    assert bool(((got.ds - want.ds).abs() <= 1e-30).all())
+
+
+@pytest.mark.parametrize("E", [8, 16, 31, 64, 256, 300, 1024])
+def test_low_rows_among_others(E):
+    """Rows of logits far below zero, whose sigmoids have to be taken another way, between ordinary ones: each row's
+    gradient is what it is without the others."""
+    s, idx = make(97, E, 2)
+    shift = torch.tensor([0.0, -12.0, -16.0, -18.0, -30.0, -50.0, -90.0, -1000.0], device="cuda")
+    s += shift[torch.arange(97, device="cuda") % 8][:, None]
+    check(s, idx)
+
+
 def test_even_loads_have_no_gradient_and_the_loss_coef():
     s, _ = make(64, 16, 2)
     idx = torch.stack([torch.arange(64) % 8, 8 + torch.arange(64) % 8], 1).to(torch.int32).cuda()
