@@ -580,25 +580,50 @@ def moevie_muon_update(W, M, G, ws: OrthoWorkspace, lr, momentum=0.95, weight_de
 _KINDS = {None: 0, "rms": 1, "layer": 2}
 _SCORES = {"softmax": 0, "sigmoid": 1}
 _ROW_TYPES = {torch.bfloat16: 0, torch.float32: 1}
+_BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
 Q8_BLOCK = 128   # columns that share a scale
 
 
-def _rows(t, shape, dtypes, name):
-    """``t`` as a contiguous CUDA tensor of ``shape`` on the current device."""
-    if not (t.is_cuda and t.dtype in dtypes and t.is_contiguous() and t.shape == shape):
-        raise ValueError(f"{name}: expected a contiguous CUDA tensor {tuple(shape)} of {dtypes}, got {t.dtype} on "
-                         f"{t.device} with shape {tuple(t.shape)} and strides {t.stride()}")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
-    return t
+def _rows(t, rows, n, dtype, dev, name):
+    """The address of ``t``, a contiguous tensor of n values of ``dtype`` (one, or a tuple) in ``rows`` rows on the
+    current device ``dev``."""
+    dt = t.dtype
+    if not ((dt is dtype or (type(dtype) is tuple and dt in dtype)) and t.get_device() == dev and t.numel() == n and
+            t.is_contiguous() and t.dim() > 0 and t.size(0) == rows):
+        raise ValueError(f"{name}: expected a contiguous tensor of {dtype}, {n} values in {rows} rows on the current device "
+                         f"cuda:{dev}, got {dt} on {t.device} with shape {tuple(t.shape)} and strides {t.stride()}")
+    return t.data_ptr()
 
 
-_BF16, _F32, _I32, _I8 = (torch.bfloat16,), (torch.float32,), (torch.int32,), (torch.int8,)
-_RES = (torch.bfloat16, torch.float32)
+def _device():
+    """The current device.  (Not torch.cuda.current_device(), which first looks whether CUDA is set up.)"""
+    return torch._C._cuda_getDevice()
+
+
+def _on(stream, dev):
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+class _Held:
+    """What a program keeps from call to call: its tensors are checked when they are first used and after every
+    assignment to one of its fields (not when a tensor is changed in place by resize_ or set_)."""
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_checked", None)
+
+    def check(self, *sizes):
+        if self._checked != sizes:
+            self._check(*sizes)
+            object.__setattr__(self, "_checked", sizes)
 
 
 @dataclass
-class Checkpoint:
+class Checkpoint(_Held):
     """Activations [T, d] in 8 bits (moevie_checkpoint_store): int8 codes, and for every row and 128
     columns an fp32 scale."""
     codes: torch.Tensor   # int8 [T, d]
@@ -613,37 +638,41 @@ class Checkpoint:
     def shape(self):
         return self.codes.shape
 
-    def check(self, shape, name):
-        _rows(self.codes, shape, _I8, name + ".codes")
-        _rows(self.scale, (shape[0], -(-shape[1] // Q8_BLOCK)), _F32, name + ".scale")
-        return self
+    def _check(self, T, d, dev):
+        _rows(self.codes, T, T * d, _I8, dev, "checkpoint codes")
+        _rows(self.scale, T, T * -(-d // Q8_BLOCK), _F32, dev, "checkpoint scale")
 
 
 def moevie_checkpoint_store(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
     """The 8-bit checkpoint of x [T, d] (bf16 or fp32), in ``out`` where given."""
     if x.dim() != 2:
         raise ValueError(f"x: expected [T, d], got {tuple(x.shape)}")
-    _rows(x, x.shape, _RES, "x")
     T, d = x.shape
-    out = Checkpoint.empty(T, d, x.device) if out is None else out.check(x.shape, "out")
-    _call("moevie_checkpoint_store", _p(x), int(x.dtype == torch.float32), T, d, _p(out.codes), _p(out.scale),
-          _stream(stream))
+    dev = _device()
+    at = _rows(x, T, T * d, (_BF16, _F32), dev, "x")
+    if out is None:
+        out = Checkpoint.empty(T, d, x.device)
+    out.check(T, d, dev)
+    _call("moevie_checkpoint_store", at, int(x.dtype is _F32), T, d, out.codes.data_ptr(), out.scale.data_ptr(),
+          _on(stream, dev))
     return out
 
 
 def moevie_checkpoint_load(ck: Checkpoint, dtype=torch.bfloat16, out=None, stream=None):
     """The values of a checkpoint as bf16 or fp32 [T, d] (``out``'s type where it is given)."""
-    shape = ck.codes.shape
-    ck.check(shape, "ck")
-    out = torch.empty(shape, dtype=dtype, device=ck.codes.device) if out is None else out
-    _rows(out, shape, _RES, "out")
-    _call("moevie_checkpoint_load", _p(ck.codes), _p(ck.scale), shape[0], shape[1], _p(out),
-          int(out.dtype == torch.float32), _stream(stream))
+    T, d = ck.codes.shape
+    dev = _device()
+    ck.check(T, d, dev)
+    if out is None:
+        out = torch.empty((T, d), dtype=dtype, device=ck.codes.device)
+    at = _rows(out, T, T * d, (_BF16, _F32), dev, "out")
+    _call("moevie_checkpoint_load", ck.codes.data_ptr(), ck.scale.data_ptr(), T, d, at, int(out.dtype is _F32),
+          _on(stream, dev))
     return out
 
 
 @dataclass
-class ResidualNorm:
+class ResidualNorm(_Held):
     """A block's norms, gate and residual scale (moevie_norms): r1 = residual_scale r + gate * N_post(f),
     u = N_pre(r1).  ``pre`` and ``post``: "rms", "layer" or None.  Weights and biases fp32 [d] (None: 1 and 0);
     gate fp32 [G, d] (None: 1) for the G runs of rows seg[g] to seg[g + 1] (int32 [G + 1]; None: one run of all)."""
@@ -663,18 +692,23 @@ class ResidualNorm:
     def G(self):
         return 1 if self.seg is None else self.seg.numel() - 1
 
-    def c_struct(self) -> _Norms:
+    def _check(self, dev):
         d, G = self.d, self.G
         for name in ("w_pre", "b_pre", "w_post", "b_post"):
             t = getattr(self, name)
             if t is not None:
-                _rows(t, (d,), _F32, name)
+                _rows(t, d, d, _F32, dev, name)
         if self.seg is not None:
-            _rows(self.seg, (G + 1,), _I32, "seg")
+            _rows(self.seg, G + 1, G + 1, _I32, dev, "seg")
         if self.gate is not None:
-            _rows(self.gate, (G, d), _F32, "gate")
-        return _Norms(d, _KINDS[self.pre], _KINDS[self.post], *(None if t is None else t.data_ptr() for t in (
-            self.w_pre, self.b_pre, self.w_post, self.b_post, self.gate, self.seg)), G, self.residual_scale, self.eps)
+            _rows(self.gate, G, G * d, _F32, dev, "gate")
+
+    def c_struct(self, dev) -> _Norms:
+        self.check(dev)
+        seg = self.seg
+        return _Norms(self.d, _KINDS[self.pre], _KINDS[self.post], _address(self.w_pre), _address(self.b_pre),
+                      _address(self.w_post), _address(self.b_post), _address(self.gate), _address(seg),
+                      1 if seg is None else seg.numel() - 1, self.residual_scale, self.eps)
 
 
 def moevie_residual_norm_workspace_size(T_max, d, G=1) -> int:
@@ -694,7 +728,7 @@ class ResidualNormWorkspace(Workspace):
 
 
 @dataclass
-class ResidualNormOut:
+class ResidualNormOut(_Held):
     """What moevie_residual_norm gives; a member that the call has no use for is None."""
     r: torch.Tensor | None            # r1 [T, d], of the residual stream's type
     u: torch.Tensor | None            # bf16 [T, d]
@@ -715,19 +749,31 @@ class ResidualNormOut:
                    stats(norms.pre), stats(norms.post if join else None),
                    Checkpoint.empty(T, d, device) if save else None, Checkpoint.empty(T, d, device) if save and join else None)
 
+    def _check(self, T, d, dtype, join, dev):
+        if join:
+            if self.r is None:
+                raise ValueError("out.r: missing")
+            _rows(self.r, T, T * d, dtype, dev, "out.r")
+        if self.u is not None:
+            _rows(self.u, T, T * d, _BF16, dev, "out.u")
+        for name in ("stats_pre", "stats_post"):
+            t = getattr(self, name)
+            if t is not None:
+                _rows(t, T, 2 * T, _F32, dev, "out." + name)
 
-def _rows_struct(t, shape, dtypes, name):
+
+def _rows_struct(t, T, d, dtype, dev, name):
     if isinstance(t, Checkpoint):
-        t.check(shape, name)
+        t.check(T, d, dev)
         return _Rows(t.codes.data_ptr(), t.scale.data_ptr(), 2)
-    _rows(t, shape, dtypes, name)
-    return _Rows(t.data_ptr(), None, _ROW_TYPES[t.dtype])
+    return _Rows(_rows(t, T, T * d, dtype, dev, name), None, _ROW_TYPES[t.dtype])
 
 
 def _matrix(t, d, name):
-    if len(t.shape) != 2 or t.shape[1] != d:
-        raise ValueError(f"{name}: expected [T, {d}], got {tuple(t.shape)}")
-    return t.shape
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != d:
+        raise ValueError(f"{name}: expected [T, {d}], got {tuple(shape)}")
+    return shape[0]
 
 
 def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, out: ResidualNormOut | None = None,
@@ -735,35 +781,28 @@ def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, o
     """r1 = residual_scale r + gate * N_post(f), u = N_pre(r1); r bf16 or fp32 [T, d], f bf16 [T, d] or None
     (then u = N_pre(r), and r may be a Checkpoint).  ``save``: also the 8-bit checkpoints of r and f.
     ``out``: a ResidualNormOut whose buffers are written (its members say what is wanted; out.r may be r)."""
-    N = norms.c_struct()
-    shape = _matrix(r, norms.d, "r")
-    T = shape[0]
-    R = _rows_struct(r, shape, _RES, "r")
-    if f is not None:
-        _rows(f, shape, _BF16, "f")
+    dev, d = _device(), norms.d
+    N = norms.c_struct(dev)
+    T = _matrix(r, d, "r")
+    R = _rows_struct(r, T, d, (_BF16, _F32), dev, "r")
+    join = f is not None
+    F = _rows(f, T, T * d, _BF16, dev, "f") if join else None
+    dtype = _BF16 if R.type == 2 else r.dtype
     if out is None:
-        out = ResidualNormOut.empty(norms, T, r.dtype if R.type != 2 else torch.bfloat16, save, f is not None,
-                                    ws.buf.device)
-    o = out
-    if f is not None:
-        _rows(o.r, shape, (r.dtype,) if R.type != 2 else _RES, "out.r")
-    if o.u is not None:
-        _rows(o.u, shape, _BF16, "out.u")
-    for name, t in (("out.stats_pre", o.stats_pre), ("out.stats_post", o.stats_post)):
-        if t is not None:
-            _rows(t, (T, 2), _F32, name)
-    for name, t in (("out.save_r", o.save_r), ("out.save_f", o.save_f)):
-        if t is not None:
-            t.check(shape, name)
-    qr, qf = o.save_r, o.save_f
-    _call("moevie_residual_norm", ctypes.byref(N), ctypes.byref(R), _p(f), T, _p(o.r if f is not None else None),
-          _p(o.u), _p(o.stats_pre), _p(o.stats_post), _p(qr and qr.codes), _p(qr and qr.scale), _p(qf and qf.codes),
-          _p(qf and qf.scale), ws.ptr, ws.nbytes, _stream(stream))
+        out = ResidualNormOut.empty(norms, T, dtype, save, join, ws.buf.device)
+    out.check(T, d, dtype, join, dev)
+    codes = [None] * 4
+    for i, ck in ((0, out.save_r), (2, out.save_f)):
+        if ck is not None:
+            ck.check(T, d, dev)
+            codes[i], codes[i + 1] = ck.codes.data_ptr(), ck.scale.data_ptr()
+    _call("moevie_residual_norm", ctypes.byref(N), ctypes.byref(R), F, T, out.r.data_ptr() if join else None,
+          _address(out.u), _address(out.stats_pre), _address(out.stats_post), *codes, ws.buf.data_ptr(), ws.nbytes, _on(stream, dev))
     return out
 
 
 @dataclass
-class ResidualNormGrads:
+class ResidualNormGrads(_Held):
     """What moevie_residual_norm_backward gives (None: not wanted)."""
     dr: torch.Tensor
     df: torch.Tensor | None
@@ -785,6 +824,17 @@ class ResidualNormGrads:
                    *(like(t) for t in ((norms.w_post, norms.b_post) if post else (None, None))),
                    like(norms.gate if join else None))
 
+    def _check(self, T, d, G, dev):
+        _rows(self.dr, T, T * d, (_BF16, _F32), dev, "out.dr")
+        if self.df is not None:
+            _rows(self.df, T, T * d, _BF16, dev, "out.df")
+        for name in ("dw_pre", "db_pre", "dw_post", "db_post"):
+            t = getattr(self, name)
+            if t is not None:
+                _rows(t, d, d, _F32, dev, "out." + name)
+        if self.dgate is not None:
+            _rows(self.dgate, G, G * d, _F32, dev, "out.dgate")
+
 
 def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, stats_post,
                                   ws: ResidualNormWorkspace, out: ResidualNormGrads | None = None,
@@ -792,38 +842,25 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
     """Gradients of moevie_residual_norm.  dr [T, d]: the gradient of r1 but for what comes through u, of the
     residual stream's type (None: zero); du: the gradient of u, fp32 (dx of moevie_moe_backward) or bf16 (None
     where norms.pre is None); r (r1) and f: the forward's rows or their Checkpoints; stats as the forward gave
-    them.  A None for f where norms has a post norm or a gate means that the forward ran without f.  Returns
-    dr (may be the given one, as out.dr), df bf16 and the gradients of norms' weights, fp32."""
-    N = norms.c_struct()
-    d = norms.d
-    shape = _matrix(dr if dr is not None else du, d, "dr" if dr is not None else "du")
-    T = shape[0]
-    join = f is not None if out is None else out.df is not None
+    them.  f = None without ``out``: the forward ran without f (with it, out.df says so).  Returns dr (may be the
+    given one, as out.dr), df bf16 and the gradients of norms' weights, fp32."""
+    dev, d = _device(), norms.d
+    N = norms.c_struct(dev)
+    T = _matrix(dr if dr is not None else du, d, "dr" if dr is not None else "du")
     if out is None:
-        dtype = dr.dtype if dr is not None else r.dtype if isinstance(r, torch.Tensor) else torch.bfloat16
-        out = ResidualNormGrads.empty(norms, T, dtype, join, ws.buf.device)
-    o = out
-    _rows(o.dr, shape, _RES, "out.dr")
-    if dr is not None:
-        _rows(dr, shape, (o.dr.dtype,), "dr")
-    if du is not None:
-        _rows(du, shape, _RES, "du")
-    R = _rows_struct(r, shape, (o.dr.dtype,), "r") if r is not None else None
-    Fr = _rows_struct(f, shape, _BF16, "f") if f is not None else None
-    for name, t in (("stats_pre", stats_pre), ("stats_post", stats_post)):
-        if t is not None:
-            _rows(t, (T, 2), _F32, name)
-    if o.df is not None:
-        _rows(o.df, shape, _BF16, "out.df")
-    for name, t in (("dw_pre", o.dw_pre), ("db_pre", o.db_pre), ("dw_post", o.dw_post), ("db_post", o.db_post)):
-        if t is not None:
-            _rows(t, (d,), _F32, "out." + name)
-    if o.dgate is not None:
-        _rows(o.dgate, (norms.G, d), _F32, "out.dgate")
-    _call("moevie_residual_norm_backward", ctypes.byref(N), _p(dr), int(o.dr.dtype == torch.float32), _p(du),
-          int(du is not None and du.dtype == torch.float32), ctypes.byref(R) if R is not None else None,
-          ctypes.byref(Fr) if Fr is not None else None, _p(stats_pre), _p(stats_post), T, _p(o.dr), _p(o.df),
-          _p(o.dw_pre), _p(o.db_pre), _p(o.dw_post), _p(o.db_post), _p(o.dgate), ws.ptr, ws.nbytes, _stream(stream))
+        dtype = dr.dtype if dr is not None else r.dtype if isinstance(r, torch.Tensor) else _BF16
+        out = ResidualNormGrads.empty(norms, T, dtype, f is not None, ws.buf.device)
+    out.check(T, d, N.G, dev)
+    res, n = out.dr.dtype, T * d
+    R = ctypes.byref(_rows_struct(r, T, d, res, dev, "r")) if r is not None else None
+    Fr = ctypes.byref(_rows_struct(f, T, d, _BF16, dev, "f")) if f is not None else None
+    _call("moevie_residual_norm_backward", ctypes.byref(N), _rows(dr, T, n, res, dev, "dr") if dr is not None else None,
+          int(res is _F32), _rows(du, T, n, (_BF16, _F32), dev, "du") if du is not None else None,
+          int(du is not None and du.dtype is _F32), R, Fr,
+          _rows(stats_pre, T, 2 * T, _F32, dev, "stats_pre") if stats_pre is not None else None,
+          _rows(stats_post, T, 2 * T, _F32, dev, "stats_post") if stats_post is not None else None, T, out.dr.data_ptr(),
+          _address(out.df), _address(out.dw_pre), _address(out.db_pre), _address(out.dw_post), _address(out.db_post),
+          _address(out.dgate), ws.buf.data_ptr(), ws.nbytes, _on(stream, dev))
     return out
 
 
@@ -846,7 +883,7 @@ class BalanceWorkspace(Workspace):
 
 
 @dataclass
-class BalanceOut:
+class BalanceOut(_Held):
     """What moevie_balance_loss gives."""
     loss: torch.Tensor            # fp32 [1]
     counts: torch.Tensor          # int32 [G, E]
@@ -858,15 +895,20 @@ class BalanceOut:
                    torch.empty((G, E), dtype=torch.int32, device=device),
                    torch.empty((T, E), dtype=torch.float32, device=device) if grad else None)
 
+    def _check(self, T, E, G, dev):
+        _rows(self.loss, 1, 1, _F32, dev, "out.loss")
+        _rows(self.counts, G, G * E, _I32, dev, "out.counts")
+        if self.ds is not None:
+            _logits(self.ds, T, E, dev, "out.ds")
 
-def _logits(t, shape, name):
-    """An fp32 CUDA tensor [T, E] with consecutive columns -> its row stride."""
-    if not (t.is_cuda and t.dtype == torch.float32 and t.shape == shape and (shape[1] <= 1 or t.stride(1) == 1)):
-        raise ValueError(f"{name}: expected an fp32 CUDA tensor {tuple(shape)} with consecutive columns, got {t.dtype} "
-                         f"on {t.device} with shape {tuple(t.shape)} and strides {t.stride()}")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
-    return max(shape[1], t.stride(0)) if shape[0] > 1 else shape[1]
+
+def _logits(t, T, E, dev, name):
+    """The row stride of an fp32 tensor [T, E] with consecutive columns on the current device."""
+    if not (t.dtype is _F32 and t.get_device() == dev and t.dim() == 2 and t.size(0) == T and t.size(1) == E and
+            (E == 1 or t.stride(1) == 1) and (T <= 1 or t.stride(0) >= E)):
+        raise ValueError(f"{name}: expected an fp32 tensor [{T}, {E}] with consecutive columns on the current device "
+                         f"cuda:{dev}, got {t.dtype} on {t.device} with shape {tuple(t.shape)} and strides {t.stride()}")
+    return t.stride(0) if T > 1 else E
 
 
 def moevie_balance_loss(s, idx, ws: BalanceWorkspace, coef=0.01, score="sigmoid", seg=None,
@@ -877,19 +919,19 @@ def moevie_balance_loss(s, idx, ws: BalanceWorkspace, coef=0.01, score="sigmoid"
     if s.dim() != 2 or idx.dim() != 2:
         raise ValueError(f"expected s [T, E] and idx [T, k], got {tuple(s.shape)} and {tuple(idx.shape)}")
     T, E = s.shape
-    k = idx.shape[1]
-    ld = _logits(s, s.shape, "s")
-    _rows(idx, (T, k), _I32, "idx")
+    k = idx.size(1)
+    dev = _device()
+    ld = _logits(s, T, E, dev, "s")
+    ids = _rows(idx, T, T * k, _I32, dev, "idx")
     G = 1 if seg is None else seg.numel() - 1
-    if seg is not None:
-        _rows(seg, (G + 1,), _I32, "seg")
+    runs = None if seg is None else _rows(seg, G + 1, G + 1, _I32, dev, "seg")
     if out is None:
         out = BalanceOut.empty(T, E, G, grad, s.device)
-    _rows(out.loss, (1,), _F32, "out.loss")
-    _rows(out.counts, (G, E), _I32, "out.counts")
-    ldd = _logits(out.ds, s.shape, "out.ds") if out.ds is not None else 0
-    _call("moevie_balance_loss", _p(s), ld, _p(idx), T, E, k, _p(seg), G, _SCORES[score], float(coef), _p(out.loss),
-          _p(out.counts), _p(out.ds), ldd, ws.ptr, ws.nbytes, _stream(stream))
+    out.check(T, E, G, dev)
+    ds = out.ds
+    _call("moevie_balance_loss", s.data_ptr(), ld, ids, T, E, k, runs, G, _SCORES[score], coef, out.loss.data_ptr(),
+          out.counts.data_ptr(), _address(ds), 0 if ds is None else ds.stride(0) if T > 1 else E, ws.ptr, ws.nbytes,
+          _on(stream, dev))
     return out
 
 
