@@ -482,6 +482,24 @@ moevie_status moevie_balance_loss(const float* s, int64_t ld_s, const int32_t* i
                                   const int32_t* seg, int64_t G, int score, float coef, float* loss, int32_t* counts,
                                   float* ds, int64_t ld_ds, void* ws, size_t ws_bytes, void* stream);
 
+/* The router's logits s = x W_r (Eq. 1) for moevie_balance_loss: x bf16 [T, d], W_r fp32 [d, E], s fp32 [T, E]
+ * with rows E rounded up to a multiple of 32 apart (16-byte aligned; the columns between hold zeros).  On the
+ * tensor cores with fp32 accumulation, W_r as the sum of two bf16 pieces (off by at most 2^-16 of it): the
+ * logits that moevie_route starts from.  ws: moevie_workspace_size(T_max, d, E, 1, 0, 0) bytes or those of the
+ * whole layer. */
+moevie_status moevie_router_logits(const void* x, const float* W_r, int64_t T, int64_t d, int64_t E, float* s, void* ws,
+                                   size_t ws_bytes, void* stream);
+
+/* moevie_moe_backward with a gradient of the logits besides the one through the gates: ds fp32 [T, E], rows
+ * ld_ds >= E apart, every row of it read (e.g. that of moevie_balance_loss):
+ *     dx += ds W_r^T,   dW_r += x^T ds,
+ * ds and W_r rounded to bf16 as GEMM operands, fp32 accumulation.  Everything else, the workspace included,
+ * as for moevie_moe_backward. */
+moevie_status moevie_moe_backward_balanced(const moevie_layer* layer, const void* x, const void* dy, int64_t T,
+                                           const int32_t* idx, const float* ds, int64_t ld_ds, float* dx, float* dW_r,
+                                           float* dW1, float* dW2, float* dW3, float* dWs1, float* dWs2, float* dWs3,
+                                           void* ws, size_t ws_bytes, void* stream);
+
 /* Synchronise `stream`, then read the workspace's device status into *out
  * (MOEVIE_OK when no device-side error was recorded).  `detail` (host, may be
  * NULL) receives 4 ints: code, site, and two values describing the failure. */

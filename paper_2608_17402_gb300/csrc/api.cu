@@ -1542,10 +1542,11 @@ moevie_status moevie_backward_workspace_size(int64_t T_max, int64_t d, int64_t E
     return MOEVIE_OK;
 }
 
-moevie_status moevie_moe_backward(const moevie_layer* Lr, const void* x, const void* dy, int64_t T,
-                                  const int32_t* idx, float* dx, float* dW_r, float* dW1, float* dW2,
-                                  float* dW3, float* dWs1, float* dWs2, float* dWs3, void* ws, size_t ws_bytes,
-                                  void* stream) {
+// ds: a gradient of all logits beside the one through the gates (rows ld_ds apart), or nullptr.
+static moevie_status backward_impl(const moevie_layer* Lr, const void* x, const void* dy, int64_t T,
+                                   const int32_t* idx, const float* ds, int64_t ld_ds, float* dx, float* dW_r,
+                                   float* dW1, float* dW2, float* dW3, float* dWs1, float* dWs2, float* dWs3,
+                                   void* ws, size_t ws_bytes, void* stream) {
     if (!Lr) return MOEVIE_ERR_INVALID_ARG;
     const int64_t d = Lr->d, E = Lr->E, k = Lr->k, h = Lr->h, hs = Lr->h_s;
     moevie_status c = check_bwd_sizes(T, d, E, k, h, hs);
@@ -1634,7 +1635,8 @@ moevie_status moevie_moe_backward(const moevie_layer* Lr, const void* x, const v
         if (swiglu) MV_TRY(launch_bwd_zero(at<int32_t>(ws, L.gcs1), 1, (int)d, (int)hs, hsp, dWs3, sms, s));
     }
     MV_TRY(launch_bwd_zero(at<int32_t>(ws, L.gcr), 1, (int)d, (int)Ep, Ep, dwr, sms, s));
-    MV_TRY(launch_zero_f32(reinterpret_cast<float*>(DS), T * Ep / 2, s));
+    if (ds) MV_TRY(launch_bwd_logits(ds, ld_ds, T, (int)E, (int)Ep, DS, s));
+    else MV_TRY(launch_zero_f32(reinterpret_cast<float*>(DS), T * Ep / 2, s));
     MV_TRY(launch_bwd_gather(xb, static_cast<const __nv_bfloat16*>(dy), ptok, pgate, poff, (int)E, (int)d,
                              L.rows_max, static_cast<__nv_bfloat16*>(Xp), static_cast<__nv_bfloat16*>(Gm), s));
     // 4. up-projection again: u = x W1[e] and a = GELU(u), both kept (bf16; SwiGLU: u, v and a)
@@ -1733,9 +1735,32 @@ moevie_status moevie_moe_backward(const moevie_layer* Lr, const void* x, const v
             if ((c = run_gemm(g, st, s)) != MOEVIE_OK) return c;
         }
     }
+    //    and from the given gradient of all logits, dx += ds W_r^T (bf16; W_r's first piece, K-major as it lies)
+    if (ds) {
+        GemmSpec g{};
+        g.A = DS;
+        g.lda = Ep;
+        g.a_cols = E;
+        g.a_nrows = T;
+        g.m_total = T;
+        g.G = 1;
+        g.W = at<__nv_bfloat16>(ws, L.wsplit);
+        g.b_kmajor = 1;
+        g.b_k_ld = route_concat((int)E) ? 2 * Ep : Ep;
+        g.b_g_ld = d * g.b_k_ld;
+        g.K = (int)E;
+        g.N = (int)d;
+        g.epi = EPI_ADD_F32;
+        g.yacc = dx;
+        g.ldy = d;
+        g.o_nrows = T;
+        g.scale = 1.0f;
+        if ((c = run_gemm(g, st, s)) != MOEVIE_OK) return c;
+    }
     // 7. the router (Eqs. 4-5): ds per token, dx += ds W_r^T, ds into [T][E_pad] bf16
     MV_TRY(launch_bwd_router(idx, at<float>(ws, L.sig), at<float>(ws, L.gate), at<int32_t>(ws, L.slot_prow), dgp,
-                             2 * nt_h, L.rows_max, wrt, (int)dp, T, (int)d, (int)E, (int)k, (int)Ep, dx, DS, s));
+                             2 * nt_h, L.rows_max, wrt, (int)dp, T, (int)d, (int)E, (int)k, (int)Ep, ds, ld_ds, dx,
+                             DS, s));
     // 8. weight gradients, per expert over its padded rows: dW2[e] = a^T (g dy),
     //    dW1[e] = x^T du; and dW_r = x^T ds over all tokens
     auto wgrad = [&](const void* A, int64_t a_cols, int64_t a_rows, int64_t lda, const void* B, int64_t N,
@@ -1867,6 +1892,35 @@ moevie_status moevie_moe_backward(const moevie_layer* Lr, const void* x, const v
                              hsp)) != MOEVIE_OK)
         return c;
     return MOEVIE_OK;
+}
+
+moevie_status moevie_moe_backward(const moevie_layer* layer, const void* x, const void* dy, int64_t T,
+                                  const int32_t* idx, float* dx, float* dW_r, float* dW1, float* dW2,
+                                  float* dW3, float* dWs1, float* dWs2, float* dWs3, void* ws, size_t ws_bytes,
+                                  void* stream) {
+    return backward_impl(layer, x, dy, T, idx, nullptr, 0, dx, dW_r, dW1, dW2, dW3, dWs1, dWs2, dWs3, ws, ws_bytes,
+                         stream);
+}
+
+moevie_status moevie_moe_backward_balanced(const moevie_layer* layer, const void* x, const void* dy, int64_t T,
+                                           const int32_t* idx, const float* ds, int64_t ld_ds, float* dx, float* dW_r,
+                                           float* dW1, float* dW2, float* dW3, float* dWs1, float* dWs2, float* dWs3,
+                                           void* ws, size_t ws_bytes, void* stream) {
+    if (!layer || T < 0) return MOEVIE_ERR_INVALID_ARG;
+    if (T > 0 && (!ds || !a4(ds) || ld_ds < layer->E || ld_ds >= (int64_t(1) << 31))) return MOEVIE_ERR_INVALID_ARG;
+    return backward_impl(layer, x, dy, T, idx, ds, ld_ds, dx, dW_r, dW1, dW2, dW3, dWs1, dWs2, dWs3, ws, ws_bytes,
+                         stream);
+}
+
+moevie_status moevie_router_logits(const void* x, const float* W_r, int64_t T, int64_t d, int64_t E, float* s, void* ws,
+                                   size_t ws_bytes, void* stream) {
+    const moevie_status c = check_sizes(T, d, E, 1, 0, 0);
+    if (c != MOEVIE_OK) return c;
+    if (T == 0) return MOEVIE_OK;
+    if (!x || !W_r || !s || !ws || !a16(x) || !a16(s) || !a16(ws)) return MOEVIE_ERR_INVALID_ARG;
+    const Layout L = make_layout(T, d, E, 1, 0, 0);
+    if (ws_bytes < L.total) return MOEVIE_ERR_WORKSPACE;
+    return route_impl(x, W_r, nullptr, T, d, E, 1, nullptr, nullptr, L, ws, static_cast<cudaStream_t>(stream), true, s);
 }
 
 // ------------------------------------------------------------ test hooks

@@ -19,6 +19,7 @@
 //   bwd_router_kernel  per token: dg_j = dy . E_j(x) from the partial row dots, the gate
 //                      derivative ds (Eqs. 4-5), dx += ds W_r^T, and ds into a dense
 //                      [T][E_pad] bf16 matrix for dW_r = x^T ds
+//   bwd_logits_kernel  a given gradient of all logits (the balance loss's) into that matrix
 #include <math.h>
 
 #include <algorithm>
@@ -265,13 +266,15 @@ __global__ void bwd_gather_kernel(const __nv_bfloat16* __restrict__ x, const __n
 // One warp per token (Eqs. 4-5 backward): dg_j = sum of the nparts partial row dots of
 // its padded row, gdg = sum_j g_j dg_j, ds_j = sigma_j (1 - sigma_j) (dg_j - gdg) / S;
 // dx_t += sum_j ds_j W_r[:, e_j] (after the grouped dx GEMM, same stream; the k columns
-// advance together), and ds_j into ds[t][e_j] (bf16, the rest of the row already zero).
+// advance together), and ds_j into ds[t][e_j] (bf16; the rest of the row is already zero, or, with
+// another gradient ds_in of all logits, that one, which ds_j is added to).
 template <int KB>
 __global__ void __launch_bounds__(256) bwd_router_kernel(
     const int32_t* __restrict__ idx, const float* __restrict__ sig, const float* __restrict__ gate,
     const int32_t* __restrict__ slot_prow, const float* __restrict__ dg_part, int nparts,
     int64_t part_stride, const float* __restrict__ wrt, int dp, int64_t T, int d, int E, int k,
-    int Ep, float* __restrict__ dx, __nv_bfloat16* __restrict__ ds_out) {
+    int Ep, const float* __restrict__ ds_in, int64_t ld_ds, float* __restrict__ dx,
+    __nv_bfloat16* __restrict__ ds_out) {
     pdl_wait();
     const int lane = threadIdx.x & 31;
     const int64_t t = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
@@ -290,7 +293,8 @@ __global__ void __launch_bounds__(256) bwd_router_kernel(
     const float S = warp_sum_f(sg);
     const float gdg = warp_sum_f(g * dg);
     const float ds = lane < k ? sg * (1.f - sg) * (dg - gdg) / S : 0.f;
-    if (lane < k && e >= 0 && e < E) ds_out[t * Ep + e] = __float2bfloat16_rn(ds);
+    if (lane < k && e >= 0 && e < E)
+        ds_out[t * Ep + e] = __float2bfloat16_rn(ds_in ? ds + ds_in[t * ld_ds + e] : ds);
     const float* w[KB];
     float dsj[KB];
 #pragma unroll
@@ -306,6 +310,20 @@ __global__ void __launch_bounds__(256) bwd_router_kernel(
         for (int j = 0; j < KB; ++j)
             if (w[j]) a = fmaf(dsj[j], __ldg(w[j] + i), a);
         dxr[i] = a;
+    }
+}
+
+// ds[t][e] = bf16(src[t][e]) for e < E (src rows ld apart), zeros for E <= e < Ep; two columns a thread.
+__global__ void bwd_logits_kernel(const float* __restrict__ src, int64_t ld, int64_t T, int E, int Ep,
+                                  uint32_t* __restrict__ ds) {
+    pdl_wait();
+    const int half = Ep / 2;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < T * half;
+         i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t t = i / half;
+        const int e = (int)(i - t * half) * 2;
+        const float* p = src + t * ld + e;
+        ds[i] = pack_bf16x2(e < E ? p[0] : 0.f, e + 1 < E ? p[1] : 0.f);
     }
 }
 
@@ -392,18 +410,26 @@ cudaError_t launch_bwd_gather(const __nv_bfloat16* x, const __nv_bfloat16* dy, c
 
 cudaError_t launch_bwd_router(const int32_t* idx, const float* sig, const float* gate, const int32_t* slot_prow,
                               const float* dg_part, int nparts, int64_t part_stride, const float* wrt, int dp,
-                              int64_t T, int d, int E, int k, int Ep, float* dx, __nv_bfloat16* ds,
-                              cudaStream_t s) {
+                              int64_t T, int d, int E, int k, int Ep, const float* ds_in, int64_t ld_ds, float* dx,
+                              __nv_bfloat16* ds, cudaStream_t s) {
     const dim3 grid((unsigned)((T * 32 + 255) / 256));
     cudaError_t e;
     if (k <= 8)
         e = launch_pdl(bwd_router_kernel<8>, grid, dim3(256), 0, s, idx, sig, gate, slot_prow, dg_part, nparts,
-                       part_stride, wrt, dp, T, d, E, k, Ep, dx, ds);
+                       part_stride, wrt, dp, T, d, E, k, Ep, ds_in, ld_ds, dx, ds);
     else if (k <= 32)
         e = launch_pdl(bwd_router_kernel<32>, grid, dim3(256), 0, s, idx, sig, gate, slot_prow, dg_part, nparts,
-                       part_stride, wrt, dp, T, d, E, k, Ep, dx, ds);
+                       part_stride, wrt, dp, T, d, E, k, Ep, ds_in, ld_ds, dx, ds);
     else
         return cudaErrorInvalidValue;
+    count_launches(1);
+    return e;
+}
+
+cudaError_t launch_bwd_logits(const float* src, int64_t ld, int64_t T, int E, int Ep, __nv_bfloat16* ds,
+                              cudaStream_t s) {
+    const cudaError_t e = launch_pdl(bwd_logits_kernel, dim3(grid_of(T * (Ep / 2), 256)), dim3(256), 0, s, src, ld, T, E,
+                                     Ep, reinterpret_cast<uint32_t*>(ds));
     count_launches(1);
     return e;
 }

@@ -344,7 +344,10 @@ cudaError_t launch_bwd_gather(const __nv_bfloat16* x, const __nv_bfloat16* dy, c
 // Router backward per token (Eqs. 4-5): ds, dx += ds W_r^T, ds into [T][Ep] bf16.
 cudaError_t launch_bwd_router(const int32_t* idx, const float* sig, const float* gate, const int32_t* slot_prow,
                               const float* dg_part, int nparts, int64_t part_stride, const float* wrt, int dp,
-                              int64_t T, int d, int E, int k, int Ep, float* dx, __nv_bfloat16* ds,
+                              int64_t T, int d, int E, int k, int Ep, const float* ds_in, int64_t ld_ds, float* dx,
+                              __nv_bfloat16* ds,
+                              cudaStream_t s);
+cudaError_t launch_bwd_logits(const float* src, int64_t ld, int64_t T, int E, int Ep, __nv_bfloat16* ds,
                               cudaStream_t s);
 cudaError_t launch_bwd_copy(const float* src, int64_t ld_src, float* dst, int64_t rows, int64_t cols,
                             cudaStream_t s);

@@ -32,7 +32,7 @@ C_ENTRY_POINTS = ("moevie_status_string", "moevie_version", "moevie_workspace_si
                   "moevie_orthogonalize_workspace_size", "moevie_orthogonalize", "moevie_muon_update",
                   "moevie_checkpoint_store", "moevie_checkpoint_load", "moevie_residual_norm_workspace_size",
                   "moevie_residual_norm", "moevie_residual_norm_backward", "moevie_balance_workspace_size",
-                  "moevie_balance_loss",
+                  "moevie_balance_loss", "moevie_router_logits", "moevie_moe_backward_balanced",
                   "moevie_test_route_logits",
                   "moevie_test_fallback_count", "moevie_test_expert_hidden",
                   "moevie_test_moe_forward_events", "moevie_test_wait_timeout")
@@ -97,6 +97,8 @@ def load():
         "moevie_update_bias": ([P, I64, F, ctypes.c_int, P, P, SZ, P], ctypes.c_int),
         "moevie_backward_workspace_size": ([I64] * 6 + [ctypes.c_int, P], ctypes.c_int),
         "moevie_moe_backward": ([P, P, P, I64, P, P, P, P, P, P, P, P, P, P, SZ, P], ctypes.c_int),
+        "moevie_moe_backward_balanced": ([P, P, P, I64, P, P, I64] + [P] * 9 + [SZ, P], ctypes.c_int),
+        "moevie_router_logits": ([P, P, I64, I64, I64, P, P, SZ, P], ctypes.c_int),
         "moevie_few_workspace_size": ([I64] * 6 + [P], ctypes.c_int),
         "moevie_moe_few": ([P, P, I64, P, P, P, P, SZ, P], ctypes.c_int),
         "moevie_orthogonalize_workspace_size": ([I64] * 3 + [P], ctypes.c_int),
@@ -418,12 +420,14 @@ class BackwardWorkspace(Workspace):
         moevie_workspace_init(self, stream)
 
 
-def moevie_moe_backward(layer: LayerWeights, x, dy, idx, ws: "BackwardWorkspace", stream=None):
+def moevie_moe_backward(layer: LayerWeights, x, dy, idx, ws: "BackwardWorkspace", stream=None, ds=None):
     """Gradients of sum(dy * y) with the selection idx held fixed (GELU or SwiGLU
     experts, with or without a shared expert).  Returns a dict of fp32 tensors: dx [T, d],
     dW_r [d, E], dW1 [E, d, h] (a view of rows row_ld(h) apart), dW2 [E, h, d], dW3 (as
     dW1) for SwiGLU experts, and with a shared expert dWs1 [d, h_s] (a view of rows
-    row_ld(h_s) apart), dWs2 [h_s, d] and, for SwiGLU, dWs3 (as dWs1)."""
+    row_ld(h_s) apart), dWs2 [h_s, d] and, for SwiGLU, dWs3 (as dWs1).  ``ds`` fp32 [T, E]: another
+    gradient of the router's logits (moevie_balance_loss), which dx and dW_r then take too
+    (moevie_moe_backward_balanced)."""
     _want(x, torch.bfloat16, "x")
     _want(dy, torch.bfloat16, "dy")
     _want(idx, torch.int32, "idx")
@@ -442,9 +446,12 @@ def moevie_moe_backward(layer: LayerWeights, x, dy, idx, ws: "BackwardWorkspace"
         if layer.W3 is not None:
             out["dWs3"] = torch.empty((d, row_ld(hs)), dtype=torch.float32, device=dev)
     L = layer.c_struct()
-    _call("moevie_moe_backward", ctypes.byref(L), _p(x), _p(dy), T, _p(idx), _p(out["dx"]), _p(out["dW_r"]),
-          _p(out["dW1"]), _p(out["dW2"]), _p(out.get("dW3")), _p(out.get("dWs1")), _p(out.get("dWs2")),
-          _p(out.get("dWs3")), ws.ptr, ws.nbytes, _stream(stream))
+    name, extra = "moevie_moe_backward", ()
+    if ds is not None:
+        name, extra = "moevie_moe_backward_balanced", (_p(ds), _logits(ds, T, E, _device(), "ds"))
+    _call(name, ctypes.byref(L), _p(x), _p(dy), T, _p(idx), *extra, _p(out["dx"]), _p(out["dW_r"]), _p(out["dW1"]),
+          _p(out["dW2"]), _p(out.get("dW3")), _p(out.get("dWs1")), _p(out.get("dWs2")), _p(out.get("dWs3")), ws.ptr,
+          ws.nbytes, _stream(stream))
     out["dW1"] = out["dW1"][..., :h]
     for name, w in (("dW3", h), ("dWs1", hs), ("dWs3", hs)):
         if name in out:
@@ -880,6 +887,24 @@ class BalanceWorkspace(Workspace):
         self.nbytes = moevie_balance_workspace_size(T_max, E, k, G)
         self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
         moevie_workspace_init(self, stream)
+
+
+def moevie_router_logits(x, W_r, ws: Workspace, s=None, stream=None):
+    """The router's logits [T, E] of x bf16 [T, d] (Eq. 1), a view of fp32 rows that lie E rounded up to a multiple of
+    32 apart (``s``: such a buffer [T, that many])."""
+    _want(x, torch.bfloat16, "x")
+    _want(W_r, torch.float32, "W_r")
+    T, d = x.shape
+    E = W_r.shape[1]
+    E32 = (E + 31) // 32 * 32
+    if W_r.shape[0] != d:
+        raise ValueError(f"W_r: expected [{d}, E], got {tuple(W_r.shape)}")
+    if s is None:
+        s = torch.empty((T, E32), dtype=torch.float32, device=x.device)
+    elif _want(s, torch.float32, "s").shape != (T, E32):
+        raise ValueError(f"s: expected {(T, E32)}, got {tuple(s.shape)}")
+    _call("moevie_router_logits", _p(x), _p(W_r), T, d, E, _p(s), ws.ptr, ws.nbytes, _stream(stream))
+    return s[:, :E]
 
 
 @dataclass
