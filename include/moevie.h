@@ -431,7 +431,7 @@ moevie_status moevie_checkpoint_load(const int8_t* codes, const float* scale, in
  *   save_r, save_f (with their scales; NULL: not wanted): 8-bit checkpoints of r and f, what
  *   moevie_checkpoint_store gives for them, written while they are read for the last time.
  * ws: moevie_residual_norm_workspace_size(T_max, d, G) bytes, set up with moevie_workspace_init.
- * T < 2^31, G < 2^31; T == 0 launches nothing. */
+ * T < 2^31, G <= 2^20; T == 0 launches nothing. */
 moevie_status moevie_residual_norm_workspace_size(int64_t T_max, int64_t d, int64_t G, size_t* bytes);
 moevie_status moevie_residual_norm(const moevie_norms* n, const moevie_rows* r, const void* f, int64_t T, void* r_out,
                                    void* u, float* stats_pre, float* stats_post, int8_t* save_r, float* save_r_scale,

@@ -299,10 +299,10 @@ __global__ void __launch_bounds__(256) q8_load_kernel(const int8_t* codes, const
 struct RowGroup {
     int gw, wi, lane, group;
     int buf;        // which half of the group's shared memory the next sum takes
-    int half;       // floats of one: 4 for each warp
+    int half;       // floats of one: 32, or 64 for more than 16 warps
     float* part;    // zeros behind the gw-th warp
 };
-constexpr int PART_FLOATS = 2 * 4 * 32;   // of a CTA of 32 warps, or of groups of up to 8 in 8
+constexpr int PART_FLOATS = 2 * 32 * 4;   // of a CTA of one group of 32 warps, or of up to 4 groups that share rows out
 
 __device__ __forceinline__ RowGroup row_group(int gw, float* s_part) {
     RowGroup g;
@@ -311,9 +311,10 @@ __device__ __forceinline__ RowGroup row_group(int gw, float* s_part) {
     g.group = (threadIdx.x >> 5) / gw;
     g.wi = (threadIdx.x >> 5) - g.group * gw;
     g.buf = 0;
-    g.half = (gw + 3) / 4 * 16;
-    g.part = s_part + g.group * 2 * g.half;
-    for (int i = g.wi * 32 + g.lane; i < 2 * g.half; i += gw * 32) g.part[i] = 0.f;
+    g.half = gw > 16 ? 64 : 32;
+    g.part = s_part + g.group * 2 * g.half;   // (of groups of one warp never touched)
+    if (gw > 1)
+        for (int i = g.wi * 32 + g.lane; i < 2 * g.half; i += gw * 32) g.part[i] = 0.f;
     return g;
 }
 __device__ __forceinline__ void group_barrier(const RowGroup& g) {
@@ -322,7 +323,8 @@ __device__ __forceinline__ void group_barrier(const RowGroup& g) {
 
 // v[n] <- the sum of v[n] over the row's threads, the same bits in all of them; N = 1, 2 or 4.  The
 // sums share one set of shuffles: after the first steps each lane carries one of them, the n-th
-// lanes 32 n / N on.  One barrier: a warp that passes the next one's has read this one's half.
+// lanes 32 n / N on.  Then a word for each warp and sum, read back one to a lane.  One barrier: a warp
+// that passes the next one's has read this one's half.
 template <int N>
 __device__ __forceinline__ void row_sum(RowGroup& g, float (&v)[N]) {
     static_assert(N == 1 || N == 2 || N == 4, "");
@@ -349,25 +351,16 @@ __device__ __forceinline__ void row_sum(RowGroup& g, float (&v)[N]) {
     float* p = g.part + g.buf * g.half;
     if (g.lane % SPAN == 0) p[g.wi * N + g.lane / SPAN] = x;
     group_barrier(g);
-    uint64_t s[2] = {0, 0};   // N = 1: sums of every other one; 2: the two; 4: the first and the second two
-#pragma unroll 1
-    for (int w = 0; w < g.gw; w += 4) {   // 4 warps
-        ulonglong2 q[N];
+    x = p[g.lane];
+    if (N == 2 && g.gw > 16) x += p[g.lane + 32];
+    constexpr int MOST = N == 4 ? 8 : 32 / N;   // warps whose words 32 lanes hold
 #pragma unroll
-        for (int i = 0; i < N; ++i) q[i] = *reinterpret_cast<const ulonglong2*>(p + w * N + 4 * i);
+    for (int w = 1; w < MOST; w *= 2) {
+        if (w >= 8 && g.gw <= w) break;
+        x += __shfl_xor_sync(0xffffffffu, x, w * N);
+    }
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            s[0] = f2_add(s[0], q[i].x);
-            s[N == 4] = f2_add(s[N == 4], q[i].y);
-        }
-    }
-    f2_unpack(s[0], v[0], v[N > 1]);
-    if constexpr (N == 1) {
-        float x0, x1;
-        f2_unpack(s[0], x0, x1);
-        v[0] = x0 + x1;
-    }
-    if constexpr (N == 4) f2_unpack(s[1], v[2], v[3]);
+    for (int n = 0; n < N; ++n) v[n] = __shfl_sync(0xffffffffu, x, n);
     g.buf ^= 1;
 }
 
@@ -495,21 +488,19 @@ __device__ __forceinline__ P8 p8_bf16(const ulonglong2& u) {
 }
 
 // One operand's rows: whole (F32 or bf16), or, where Q8 allows it and q8 says so, 8-bit codes with
-// their scales.
+// their scales (which the callers copy).
 template <bool F32, bool Q8>
 struct Operand {
     const void* data;
     const float* scale;
     int q8;
-    // the lane's share of a row: its 8 columns begin at element `at`, their scale is element sat;
-    // zeros in place of a row that is not live and of columns behind a row's end
+    // the lane's share of a row: its 8 columns begin at element `at`; zeros in place of a row that is
+    // not live and of columns behind a row's end
     template <typename Ring>
-    __device__ __forceinline__ void copy(const Ring& ring, int slot, int piece, int64_t at, int64_t sat, bool live) const {
+    __device__ __forceinline__ void copy(const Ring& ring, int slot, int piece, int64_t at, bool live) const {
         const uint32_t dst = ring.at(slot, piece);
         if (Q8 && q8) {
-            const bool ok = live && ring.ok;
-            copy8(dst + ring.own, static_cast<const int8_t*>(data) + at, ok ? 8 : 0);
-            copy4(dst + ring.own + 8, scale + sat, ok ? 4 : 0);
+            copy8(dst + ring.own / 2, static_cast<const int8_t*>(data) + at, live && ring.ok ? 8 : 0);
             return;
         }
         if constexpr (F32) {
@@ -521,17 +512,23 @@ struct Operand {
         }
     }
     template <typename Ring>
-    __device__ __forceinline__ P8 get(const Ring& ring, int slot, int piece) const {
+    __device__ __forceinline__ P8 get(const Ring& ring, int slot, int piece, uint32_t scale_at) const {
         const uint32_t src = ring.at(slot, piece);
-        if (F32 && !(Q8 && q8)) {
+        if (Q8 && q8) {
+            uint32_t lo, hi;
+            float s;
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(lo), "=r"(hi) : "r"(src + ring.own / 2) : "memory");
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s) : "r"(scale_at) : "memory");
+            return p8_codes(lo, hi, s);
+        }
+        if constexpr (F32) {
             const ulonglong2 a = ld_shared(src + ring.lo), b = ld_shared(src + ring.hi);
             P8 r;
             r.p[0] = a.x, r.p[1] = a.y, r.p[2] = b.x, r.p[3] = b.y;
             return r;
+        } else {
+            return p8_bf16(ld_shared(src + ring.own));
         }
-        const ulonglong2 a = ld_shared(src + ring.own);
-        if (Q8 && q8) return p8_codes((uint32_t)a.x, (uint32_t)(a.x >> 32), __uint_as_float((uint32_t)a.y));
-        return p8_bf16(a);
     }
     __device__ __forceinline__ P8 read(int64_t at, int64_t sat) const {   // without a ring
         if (Q8 && q8) {
@@ -562,7 +559,7 @@ constexpr int BWD_SLOTS = 2;
 // both norms and their statistics (the others ask as they go).  SAVE: 8-bit checkpoints of what is read.
 // THREADS: a CTA's at most.
 template <bool F32, bool JOIN, bool BOTH, bool SAVE, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? (SAVE ? 3 : 2) : 1) norm_forward_kernel(const NormArgs a) {
     constexpr bool BIG = THREADS == 1024;
     constexpr int ROWS = rows_at_once(THREADS), SLOTS = fwd_slots(F32, THREADS), PR = F32 ? 2 : 1, PIECES = PR + (JOIN ? 1 : 0);
     extern __shared__ __align__(16) uint8_t s_dyn[];
@@ -586,8 +583,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_
     int64_t at_ahead = t0 * d + col, sat_ahead = t0 * a.nb + (col >> 7);
     auto copy_row = [&]() {   // of row `ahead`
         const bool live = ahead < n;
-        R.copy(ring, fill, 0, at_ahead, sat_ahead, live);
-        if constexpr (JOIN) Fo.copy(ring, fill, PR, at_ahead, 0, live);
+        R.copy(ring, fill, 0, at_ahead, live);
+        if constexpr (JOIN) Fo.copy(ring, fill, PR, at_ahead, live);
+        if (!JOIN && a.r_q8) copy4(ring.at(fill, 0) + 256 + g.lane * 4, a.r_scale + sat_ahead, live && act ? 4 : 0);
         cp_async_commit();
         fill = ring.next(fill);
         ++ahead;
@@ -638,8 +636,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) norm_forward_
 #pragma unroll
         for (int k = 0; k < ROWS; ++k) {
             const int from = k ? ring.next(slot) : slot;
-            r[k] = R.get(ring, from, 0);
-            if constexpr (JOIN) x[k] = Fo.get(ring, from, PR);
+            r[k] = R.get(ring, from, 0, ring.at(from, 0) + 256 + g.lane * 4);
+            if constexpr (JOIN) x[k] = Fo.get(ring, from, PR, 0);
         }
         slot = ring.next(slot);
         __syncwarp();   // read by all lanes
@@ -795,23 +793,35 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     const Operand<false, Q8> Fo{a.f, a.f_scale, a.f_q8};
     const int n = t0 < t1 ? (int)(t1 - t0) : 0, d = a.d;   // rows count from t0
     int64_t at = t0 * d + col, sat = t0 * a.nb + (col >> 7);   // of the row in hand
-    // Two sets of copies: dr1, du and r1, whose slots are free as soon as a row is begun, and f, which
+    // Two sets of copies: dr1, du, r1 and the single words, whose slots are free as soon as a row is begun, and f, which
     // is read half-way.  Both sets of a row are under way while the two rows before it are worked on.
     // `on`: rows from the one in hand
     int slot = 0;
+    // A row's last piece: the statistics of N_pre (words 0, 1) and, with the second set, of N_post (2, 3), by
+    // lane 0; the scales of the warp's two blocks of r1 (4, 5) and of f (6, 7), by lanes 0 and 1.
+    const float2 *st1_at = a.stats_pre + t0, *st2_at = a.stats_post + t0;   // of the row in hand
+    const bool scaled = Q8 && g.lane < 2 && g.wi * 2 + g.lane < a.nb;
+    const int64_t scale_at = t0 * a.nb + g.wi * 2 + g.lane;
+    const float* s1_at = Q8 && scaled && a.r_q8 ? a.r1_scale + scale_at : nullptr;
+    const float* s2_at = Q8 && scaled && a.f_q8 ? a.f_scale + scale_at : nullptr;
+    const uint32_t scale_word = (4 + (g.lane >> 4)) * 4;   // r1's; f's two words on
     auto copy_first = [&](int to, int i, int on) {
         const bool live = i + on < n;
-        if (has_dr) Dr.copy(ring, to, 0, at + on * d, 0, live);
+        if (has_dr) Dr.copy(ring, to, 0, at + on * d, live);
         if (norm) {
-            Du.copy(ring, to, PR, at + on * d, 0, live);
-            R1.copy(ring, to, PR + PU, at + on * d, Q8 ? sat + on * a.nb : 0, live);
-            copy8(ring.at(to, PIECES - 1) + ring.own, a.stats_pre + t0 + (i + on), live ? 8 : 0);
+            Du.copy(ring, to, PR, at + on * d, live);
+            R1.copy(ring, to, PR + PU, at + on * d, live);
         }
+        const uint32_t words = ring.at(to, PIECES - 1);
+        if (norm && g.lane == 0) copy8(words, st1_at + on, live ? 8 : 0);
+        if (Q8 && s1_at) copy4(words + 16 + g.lane * 4, s1_at + on * a.nb, live ? 4 : 0);
     };
     auto copy_second = [&](int to, int i, int on) {
         const bool live = i + on < n;
-        if (has_f) Fo.copy(ring, to, 2 * PR + PU, at + on * d, Q8 ? sat + on * a.nb : 0, live);
-        if (post) copy8(ring.at(to, PIECES - 1) + ring.own + 8, a.stats_post + t0 + (i + on), live ? 8 : 0);
+        if (has_f) Fo.copy(ring, to, 2 * PR + PU, at + on * d, live);
+        const uint32_t words = ring.at(to, PIECES - 1);
+        if (post && g.lane == 0) copy8(words + 8, st2_at + on, live ? 8 : 0);
+        if (Q8 && s2_at) copy4(words + 24 + g.lane * 4, s2_at + on * a.nb, live ? 4 : 0);
     };
     if constexpr (!BIG) {
         copy_first(0, 0, 0);
@@ -881,14 +891,14 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
             __syncwarp();   // the other lanes' copies
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
-                if (has_dr) dR[k] = Dr.get(ring, slot ^ k, 0);
+                const uint32_t words = ring.at(slot ^ k, PIECES - 1);
+                if (has_dr) dR[k] = Dr.get(ring, slot ^ k, 0, 0);
                 else dR[k] = p8_of(0.f);
                 if (norm) {
-                    x1[k] = R1.get(ring, slot ^ k, PR + PU);
-                    du[k] = Du.get(ring, slot ^ k, PR);
-                    const ulonglong2 q = ld_shared(ring.at(slot ^ k, PIECES - 1) + ring.own);
-                    f2_unpack(q.x, st1[k].x, st1[k].y);
+                    x1[k] = R1.get(ring, slot ^ k, PR + PU, words + scale_word);
+                    du[k] = Du.get(ring, slot ^ k, PR, 0);
                 }
+                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(st1[k].x), "=f"(st1[k].y) : "r"(words) : "memory");
             }
             __syncwarp();   // read by all lanes
             copy_first(slot, i, 2);
@@ -938,13 +948,15 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
             if (post) st2[0] = a.stats_post[t0 + i];
         } else {
             cp_async_wait<1>();
+            __syncwarp();   // the other lanes' words
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
-                if (has_f) x2[k] = Fo.get(ring, slot ^ k, 2 * PR + PU);
+                const uint32_t words = ring.at(slot ^ k, PIECES - 1) + 8;
+                if (has_f) x2[k] = Fo.get(ring, slot ^ k, 2 * PR + PU, words + scale_word);
                 else x2[k] = p8_of(0.f);
-                const ulonglong2 q = ld_shared(ring.at(slot ^ k, PIECES - 1) + ring.own);
-                f2_unpack(q.y, st2[k].x, st2[k].y);
+                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(st2[k].x), "=f"(st2[k].y) : "r"(words) : "memory");
             }
+            __syncwarp();
             copy_second(slot, i, 2);
             if (two) copy_second(slot ^ 1, i, 3);
             cp_async_commit();
@@ -993,7 +1005,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
         }
         i += two ? 2 : 1;
         at += two ? 2 * d : d;
-        if (Q8 || BIG) sat += two ? 2 * a.nb : a.nb;
+        st1_at += two ? 2 : 1;
+        st2_at += two ? 2 : 1;
+        if (BIG) sat += a.nb;
+        if (Q8 && s1_at) s1_at += two ? 2 * a.nb : a.nb;
+        if (Q8 && s2_at) s2_at += two ? 2 * a.nb : a.nb;
     }
     if (n > 0 || a.G == 1) flush_run();   // a group without rows leaves zeros where only one run is
     if (a.group_runs && g.wi == 0 && g.lane == 0)
@@ -1005,10 +1021,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     }
 }
 
-// The records of norm_backward_kernel added up, in a fixed order.  A CTA of 32 x 32 threads takes
-// 32 columns; its rows of threads share the records out.  blockIdx.y: 0 dw_pre and db_pre; 1 dw_post
-// and db_post (and dgate, where there is one run).
-__global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSumArgs a) {
+// The records of norm_backward_kernel added up, in a fixed order, by CTAs of 32 x 32 threads that take
+// 32 columns each.  blockIdx.y: 0 dw_pre and db_pre; 1 dw_post and db_post (and dgate, where there is
+// one run); 2 and on dgate of several runs, 32 / lanes runs to a CTA.  Rows of threads share the
+// records out (of a run: `lanes` rows).
+__global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSumArgs a, int lanes) {
     __shared__ float s_a[32][33], s_b[32][33];
     pdl_wait();
     const int x = threadIdx.x, y = threadIdx.y;
@@ -1019,7 +1036,22 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSumArgs a) {
     if (!rec) return;
     rec += col;
     float va = 0.f, vb = 0.f;
-    if (act) {
+    int64_t run = 0;   // of this thread, for dgate
+    if (blockIdx.y >= 2) {
+        run = (int64_t)(blockIdx.y - 2) * (32 / lanes) + y / lanes;
+        if (act && run < a.G) {
+            const int64_t r0 = max((int64_t)a.seg[run], (int64_t)0), r1 = min((int64_t)a.seg[run + 1], a.T);
+            if (r0 < r1) {
+                const int64_t hi = group_of(a.T, r1 - 1, a.n_groups);
+                const float* p = rec + run * row;
+#pragma unroll 4
+                for (int64_t i = group_of(a.T, r0, a.n_groups) + y % lanes; i <= hi; i += lanes) {
+                    va += p[i * row];
+                    vb += p[i * row + a.d];
+                }
+            }
+        }
+    } else if (act) {
         if (pre || a.G == 1) {
 #pragma unroll 8
             for (int64_t i = y; i < a.n_groups; i += 32) {
@@ -1053,61 +1085,30 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSumArgs a) {
             }
         }
     }
-    s_a[y][x] = va;
-    s_b[y][x] = vb;
-    __syncthreads();
-    if (y != 0 || !act) return;
-    va = vb = 0.f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) va += s_a[i][x], vb += s_b[i][x];
+    const int share = blockIdx.y >= 2 ? lanes : 32;   // rows of threads to one result
+    if (share > 1) {
+        s_a[y][x] = va;
+        s_b[y][x] = vb;
+        __syncthreads();
+        if (y % share != 0) return;
+        va = vb = 0.f;
+#pragma unroll 8
+        for (int i = 0; i < share; ++i) va += s_a[y + i][x], vb += s_b[y + i][x];
+    }
+    if (!act || run >= a.G) return;
     if (pre) {
         if (a.dw_pre) a.dw_pre[col] = va;
         if (a.db_pre) a.db_pre[col] = vb;
         return;
     }
-    const float gt = a.G == 1 && a.gate ? a.gate[col] : 1.f;
-    if (a.dw_post) a.dw_post[col] = gt * va;
-    if (a.db_post) a.db_post[col] = gt * vb;
-    if (a.G == 1 && a.dgate)
-        a.dgate[col] = fmaf(a.w_post ? a.w_post[col] : 1.f, va, (a.b_post ? a.b_post[col] : 0.f) * vb);
-}
-
-// dgate of several runs: a CTA of 32 x 8 threads takes 32 columns of 8 / lanes runs, `lanes` rows of
-// threads to the records of each (one where a run has few).
-__global__ void __launch_bounds__(256) norm_gates_kernel(const NormSumArgs a, int lanes) {
-    __shared__ float s_a[8][33], s_b[8][33];
-    pdl_wait();
-    const int x = threadIdx.x, y = threadIdx.y, l = y % lanes;
-    const int col = blockIdx.x * 32 + x;
-    const int64_t row = 2 * (int64_t)a.d;
-    const int each = 8 / lanes;
-    const float w2 = a.w_post && col < a.d ? a.w_post[col] : 1.f;
-    const float b2 = a.b_post && col < a.d ? a.b_post[col] : 0.f;
-    for (int64_t g0 = (int64_t)blockIdx.y * each; g0 < a.G; g0 += (int64_t)gridDim.y * each) {
-        const int64_t g = g0 + y / lanes;
-        float va = 0.f, vb = 0.f;
-        if (g < a.G && col < a.d) {
-            const int64_t r0 = max((int64_t)a.seg[g], (int64_t)0), r1 = min((int64_t)a.seg[g + 1], a.T);
-            if (r0 < r1) {
-                const int64_t hi = group_of(a.T, r1 - 1, a.n_groups);
-                const float* rec = a.rec_post + g * row + col;
-#pragma unroll 4
-                for (int64_t i = group_of(a.T, r0, a.n_groups) + l; i <= hi; i += lanes) {
-                    va += rec[i * row];
-                    vb += rec[i * row + a.d];
-                }
-            }
-        }
-        if (lanes > 1) {
-            s_a[y][x] = va;
-            s_b[y][x] = vb;
-            __syncthreads();
-            va = vb = 0.f;
-            for (int i = 0; i < lanes; ++i) va += s_a[y - l + i][x], vb += s_b[y - l + i][x];
-            __syncthreads();
-        }
-        if (l == 0 && g < a.G && col < a.d) a.dgate[g * a.d + col] = fmaf(w2, va, b2 * vb);
+    if (blockIdx.y == 1) {
+        const float gt = a.G == 1 && a.gate ? a.gate[col] : 1.f;
+        if (a.dw_post) a.dw_post[col] = gt * va;
+        if (a.db_post) a.db_post[col] = gt * vb;
+        if (a.G > 1) return;
     }
+    if (a.dgate)
+        a.dgate[run * a.d + col] = fmaf(a.w_post ? a.w_post[col] : 1.f, va, (a.b_post ? a.b_post[col] : 0.f) * vb);
 }
 
 // Warps of a row, row groups of a CTA and the grid: about `threads_sm` threads to an SM.
@@ -1125,7 +1126,9 @@ NormPlan norm_plan(int64_t T, int d, int threads_sm) {
     p.n_groups = std::min<int64_t>(T, (int64_t)p.grid * p.groups);
     return p;
 }
-constexpr int NORM_FWD_THREADS = 768, NORM_BWD_THREADS = 512;
+// Threads to an SM.  Forward: 512 with 128 registers each (65536 x 1664 in fp32: 204 us, with 768 of 80 each 228),
+// but 768 where checkpoints are formed as well, which is bound by instructions, not by bytes.
+constexpr int NORM_FWD_THREADS = 512, NORM_SAVE_THREADS = 768, NORM_BWD_THREADS = 512;
 constexpr int NORM_MAX_SMEM = 208 * 1024;   // 1024 threads with three rows of fp32 and bf16 each
 
 // Grid of the checkpoint kernels and the step of their walk over the blocks, CTAs_SM to an SM at most.
@@ -1203,7 +1206,7 @@ static cudaError_t norm_forward(const NormArgs& a, const NormPlan& p, cudaStream
 }
 
 cudaError_t launch_norm_forward(NormArgs a, int r_f32, cudaStream_t s) {
-    const NormPlan p = norm_plan(a.T, a.d, NORM_FWD_THREADS);
+    const NormPlan p = norm_plan(a.T, a.d, a.qr || a.qf ? NORM_SAVE_THREADS : NORM_FWD_THREADS);
     a.gw = p.gw;
     a.groups = p.groups;
     a.n_groups = p.n_groups;
@@ -1244,18 +1247,15 @@ cudaError_t launch_norm_backward(NormBwdArgs a, int r_f32, int du_f32, NormSumAr
     count_launches(1);
     if (e != cudaSuccess || (!a.rec_pre && !a.rec_post)) return e;
     sums.n_groups = a.n_groups;
-    const unsigned cols = (unsigned)((a.d + 31) / 32);
-    if (sums.rec_pre || sums.dw_post || sums.db_post || sums.G == 1) {
-        e = launch_pdl(norm_sums_kernel, dim3(cols, 2), dim3(32, 32), 0, s, sums);
-        count_launches(1);
-        if (e != cudaSuccess) return e;
-    }
+    int64_t gates = 0;   // CTAs of a column block for dgate of several runs
+    int lanes = 1;
     if (sums.G > 1 && sums.dgate) {
-        const int lanes = a.n_groups / sums.G >= 16 ? 8 : 1;
-        const int64_t each = 8 / lanes, rows = std::min<int64_t>((sums.G + each - 1) / each, 4096);
-        e = launch_pdl(norm_gates_kernel, dim3(cols, (unsigned)rows), dim3(32, 8), 0, s, sums, lanes);
-        count_launches(1);
+        while (lanes < 32 && a.n_groups / sums.G >= 4 * lanes) lanes *= 2;   // a few records to a thread
+        gates = (sums.G + 32 / lanes - 1) / (32 / lanes);
+        if (gates > 65533) return cudaErrorInvalidValue;
     }
+    e = launch_pdl(norm_sums_kernel, dim3((unsigned)((a.d + 31) / 32), (unsigned)(2 + gates)), dim3(32, 32), 0, s, sums, lanes);
+    count_launches(1);
     return e;
 }
 

@@ -55,7 +55,7 @@ WORKSPACE, INVALID, UNSUPPORTED = 3, 1, 2
     (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID),
     (dict(residual_scale=float("inf")), INVALID), (dict(residual_scale=float("nan")), INVALID),
     (dict(residual_scale=0.0), WORKSPACE), (dict(G=0), INVALID), (dict(G=2), INVALID), (dict(G=2, seg=FAKE), WORKSPACE),
-    (dict(G=1 << 31, seg=FAKE), UNSUPPORTED), (dict(seg=FAKE + 2), INVALID), (dict(w_pre=FAKE + 8), INVALID),
+    (dict(G=1 + (1 << 20), seg=FAKE), UNSUPPORTED), (dict(G=1 << 20, seg=FAKE), WORKSPACE), (dict(seg=FAKE + 2), INVALID), (dict(w_pre=FAKE + 8), INVALID),
     (dict(gate=FAKE + 4), INVALID), (dict(b_post=FAKE + 8), INVALID), (dict(post=0, w_post=0), None)])
 def test_descriptions(lib, call, change, code):
     n = norms(**change)
