@@ -520,7 +520,7 @@ struct NormSumArgs {
     const int32_t* seg;
     float *dw_pre, *db_pre, *dw_post, *db_post, *dgate;
     int64_t T, G, n_groups;
-    int d;
+    int d, bias;                // bias: the records' second halves are there
 };
 int64_t norm_groups(int64_t T, int d);   // row groups of norm_backward_kernel: its records
 cudaError_t launch_norm_forward(NormArgs a, int r_f32, cudaStream_t s);

@@ -765,8 +765,9 @@ struct Sums<true> {
 //   dgate = w_post A + b_post B,   dw_post = sum_runs gate A,   db_post = sum_runs gate B.
 // Each group of warps leaves its sums in the workspace: dw_pre and db_pre at record gid, A and B
 // of run g at record g + gid (along the rows g and gid never fall, so that no two share one).
-// ALL: both norms, dr1 and every sum; the others ask as they go.  Q8: r1 and f may be checkpoints.
-template <bool F32, bool DUF32, bool ALL, bool Q8, int THREADS>
+// ALL: both norms, dr1 and f; the others ask as they go.  Q8: r1 and f may be checkpoints.  BIAS: db_pre and B
+// as well.
+template <bool F32, bool DUF32, bool ALL, bool Q8, bool BIAS, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward_kernel(const NormBwdArgs a) {
     constexpr bool BIG = THREADS == 1024;   // no ring: its memory holds the sums
     constexpr int ROWS = rows_at_once(THREADS);
@@ -843,7 +844,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
         if (!a.rec_post || !act) return;
         float* p = a.rec_post + (run + gid) * 2 * d + col;
         sA.store(p);
-        sB.store(p + d);
+        if (BIAS) sB.store(p + d);
         sA.clear();
         sB.clear();
     };
@@ -918,7 +919,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x1[k].p[j] = f2_mul(f2_add(x1[k].p[j], m), q);
                 sw.add(du[k], x1[k]);
-                sb.add(du[k]);
+                if (BIAS) sb.add(du[k]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) du[k].p[j] = f2_mul(du[k].p[j], w.p[j]);
                 s[2 * k] = p8_sum(du[k]);
@@ -976,7 +977,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
 #pragma unroll
                     for (int j = 0; j < 4; ++j) x2[k].p[j] = f2_mul(f2_add(x2[k].p[j], m), q);
                     sA.add(dR[k], x2[k]);
-                    sB.add(dR[k]);
+                    if (BIAS) sB.add(dR[k]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) dR[k].p[j] = f2_mul(dR[k].p[j], w.p[j]);   // (zeros behind the row's end)
                     s[2 * k] = p8_sum(dR[k]);
@@ -1017,7 +1018,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     if (a.rec_pre && act) {
         float* p = a.rec_pre + gid * 2 * a.d + col;
         sw.store(p);
-        sb.store(p + a.d);
+        if (BIAS) sb.store(p + a.d);
     }
 }
 
@@ -1047,7 +1048,7 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSumArgs a, in
 #pragma unroll 4
                 for (int64_t i = group_of(a.T, r0, a.n_groups) + y % lanes; i <= hi; i += lanes) {
                     va += p[i * row];
-                    vb += p[i * row + a.d];
+                    if (a.bias) vb += p[i * row + a.d];
                 }
             }
         }
@@ -1056,7 +1057,7 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSumArgs a, in
 #pragma unroll 8
             for (int64_t i = y; i < a.n_groups; i += 32) {
                 va += rec[i * row];
-                vb += rec[i * row + a.d];
+                if (a.bias) vb += rec[i * row + a.d];
             }
         } else {   // each record by the gate of its run
             const float* gate = a.gate ? a.gate + col : nullptr;
@@ -1072,7 +1073,7 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSumArgs a, in
                     const float* p = rec + (g + i + 32 * u) * row;
                     const float gt = gate ? gate[g * a.d] : 1.f;
                     va = fmaf(gt, p[0], va);
-                    vb = fmaf(gt, p[a.d], vb);
+                    if (a.bias) vb = fmaf(gt, p[a.d], vb);
                 }
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
@@ -1080,7 +1081,7 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSumArgs a, in
                         const float* p = rec + (g + i + 32 * u) * row;
                         const float gt = gate ? gate[g * a.d] : 1.f;
                         va = fmaf(gt, p[0], va);
-                        vb = fmaf(gt, p[a.d], vb);
+                        if (a.bias) vb = fmaf(gt, p[a.d], vb);
                     }
             }
         }
@@ -1220,19 +1221,23 @@ int64_t norm_groups(int64_t T, int d) {
     return std::max<int64_t>(1, norm_plan(T, d, NORM_BWD_THREADS).n_groups);
 }
 
-template <bool F32, bool DUF32, bool ALL, bool Q8, int THREADS>
+template <bool F32, bool DUF32, bool ALL, bool Q8, bool BIAS, int THREADS>
 static cudaError_t norm_backward(const NormBwdArgs& a, const NormPlan& p, cudaStream_t s) {
     static std::atomic<bool> attr_set[64];
     const int words = THREADS == 1024 ? 8 : BWD_SLOTS * (2 * (F32 ? 2 : 1) + (DUF32 ? 2 : 1) + 2);   // of 16 bytes
-    return launch_rows(norm_backward_kernel<F32, DUF32, ALL, Q8, THREADS>, attr_set, p,
+    return launch_rows(norm_backward_kernel<F32, DUF32, ALL, Q8, BIAS, THREADS>, attr_set, p,
                        (size_t)(KEPT_BYTES + 16 * words) * p.threads, s, a);
 }
 template <bool F32, bool DUF32>
-static cudaError_t norm_backward(const NormBwdArgs& a, const NormPlan& p, cudaStream_t s) {
-    if (p.threads > 256) return norm_backward<F32, DUF32, false, true, 1024>(a, p, s);
-    if (!a.du || !a.dr1 || !a.df || !a.f || a.post == MOEVIE_NORM_NONE) return norm_backward<F32, DUF32, false, true, 256>(a, p, s);
-    return a.r_q8 || a.f_q8 ? norm_backward<F32, DUF32, true, true, 256>(a, p, s)
-                            : norm_backward<F32, DUF32, true, false, 256>(a, p, s);
+static cudaError_t norm_backward(const NormBwdArgs& a, const NormPlan& p, bool bias, cudaStream_t s) {
+    if (p.threads > 256) return norm_backward<F32, DUF32, false, true, true, 1024>(a, p, s);
+    if (!a.du || !a.dr1 || !a.df || !a.f || a.post == MOEVIE_NORM_NONE)
+        return norm_backward<F32, DUF32, false, true, true, 256>(a, p, s);
+    if (a.r_q8 || a.f_q8)
+        return bias ? norm_backward<F32, DUF32, true, true, true, 256>(a, p, s)
+                    : norm_backward<F32, DUF32, true, true, false, 256>(a, p, s);
+    return bias ? norm_backward<F32, DUF32, true, false, true, 256>(a, p, s)
+                : norm_backward<F32, DUF32, true, false, false, 256>(a, p, s);
 }
 
 cudaError_t launch_norm_backward(NormBwdArgs a, int r_f32, int du_f32, NormSumArgs sums, cudaStream_t s) {
@@ -1242,8 +1247,10 @@ cudaError_t launch_norm_backward(NormBwdArgs a, int r_f32, int du_f32, NormSumAr
     a.n_groups = p.n_groups;
     a.nb = (a.d + 127) / 128;
     cudaError_t e;
-    if (r_f32) e = du_f32 ? norm_backward<true, true>(a, p, s) : norm_backward<true, false>(a, p, s);
-    else e = du_f32 ? norm_backward<false, true>(a, p, s) : norm_backward<false, false>(a, p, s);
+    const bool bias = sums.db_pre || sums.db_post || (sums.dgate && sums.b_post);
+    sums.bias = bias;
+    if (r_f32) e = du_f32 ? norm_backward<true, true>(a, p, bias, s) : norm_backward<true, false>(a, p, bias, s);
+    else e = du_f32 ? norm_backward<false, true>(a, p, bias, s) : norm_backward<false, false>(a, p, bias, s);
     count_launches(1);
     if (e != cudaSuccess || (!a.rec_pre && !a.rec_post)) return e;
     sums.n_groups = a.n_groups;
