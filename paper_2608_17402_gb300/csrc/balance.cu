@@ -63,6 +63,7 @@ __device__ __forceinline__ void count_ids(const BalanceArgs& a, int64_t i0, int6
 __global__ void __launch_bounds__(BAL_COUNT_THREADS) bal_count_kernel(const BalanceArgs a) {
     __shared__ int hist[1024];
     pdl_wait();
+    asm volatile("griddepcontrol.launch_dependents;");   // bal_main_kernel may start, and waits for this one's end
     const int p = blockIdx.x;
     for (int64_t b = blockIdx.y; b < a.G; b += gridDim.y) {
         for (int e = threadIdx.x; e < a.E; e += BAL_COUNT_THREADS) hist[e] = 0;
@@ -176,6 +177,10 @@ __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_k
     const int64_t n_rows = hi - lo;
     const float per_row = n_rows > 0 ? a.coef / (float)n_rows : 0.f;
     const int64_t t0 = lo + n_rows * blockIdx.x / gridDim.x, t1 = lo + n_rows * (blockIdx.x + 1) / gridDim.x;
+    constexpr uint64_t NONE = 0xff800000ff800000ull;   // two logits of minus infinity
+    bool in[VPL];
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) in[v] = column(VEC * v) < a.E;
     float dots = 0.f;   // of the tokens of this lane's group
     int rows = 0;
     int64_t b = a.seg && t0 < t1 ? warp_run_of(a.seg, a.G, t0) : 0;
@@ -198,20 +203,19 @@ __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_k
             if constexpr (VEC == 1 || NV <= 8) return c_reg[i];
             else return c_mem(i);
         };
-        auto load_row = [&](int64_t tt, uint64_t (&x)[NP]) {
-            const float* src = a.s + tt * a.ld_s;
+        auto load_row = [&](const float* src, bool live, uint64_t (&x)[NP]) {
             if constexpr (VEC == 4) {
 #pragma unroll
                 for (int v = 0; v < VPL; ++v) {
-                    float4 f = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-                    if (tt < end && column(4 * v) < a.E) f = *reinterpret_cast<const float4*>(src + column(4 * v));
-                    x[2 * v] = f2_pack(f.x, f.y);
-                    x[2 * v + 1] = f2_pack(f.z, f.w);
+                    ulonglong2 f = make_ulonglong2(NONE, NONE);
+                    if (live && in[v]) f = *reinterpret_cast<const ulonglong2*>(src + 4 * LP * v);
+                    x[2 * v] = f.x;
+                    x[2 * v + 1] = f.y;
                 }
             } else {
                 float f[NV];
 #pragma unroll
-                for (int i = 0; i < NV; ++i) f[i] = tt < end && column(i) < a.E ? src[column(i)] : -INFINITY;
+                for (int i = 0; i < NV; ++i) f[i] = live && column(i) < a.E ? src[LP * i] : -INFINITY;
 #pragma unroll
                 for (int i = 0; i < NP; ++i) x[i] = f2_pack(f[2 * i], f[2 * i + 1]);
             }
@@ -250,11 +254,18 @@ __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_k
             }
             return m;
         };
-        for (int64_t tb = t + (int64_t)warp * TPW * TU + sub; tb - sub < end; tb += (int64_t)WARPS * TPW * TU) {
+        // rows left to this lane's first one of a round; and where its logits and their gradients lie
+        const float* src = a.s + (t + warp * (TPW * TU) + sub) * a.ld_s + l * VEC;
+        float* dst = a.ds + (t + warp * (TPW * TU) + sub) * a.ld_ds + l * VEC;
+        const int64_t src_u = TPW * a.ld_s, dst_u = TPW * a.ld_ds;
+        int left = (int)(end - t) - warp * (TPW * TU) - sub;
+        const int rounds = (int)((end - t + WARPS * TPW * TU - 1) / (WARPS * TPW * TU));   // of all warps alike
+#pragma unroll 1
+        for (int round = 0; round < rounds; ++round) {
             uint64_t x[TU][NP];   // logits, then p times its slope by the logit but for sums
             float sums[2 * TU];   // of p, and of p c
 #pragma unroll
-            for (int u = 0; u < TU; ++u) load_row(tb + u * TPW, x[u]);
+            for (int u = 0; u < TU; ++u) load_row(src + u * src_u, u * TPW < left, x[u]);
 #pragma unroll
             for (int u = 0; u < TU; ++u) {
                 uint64_t s[2] = {0, 0};
@@ -292,7 +303,7 @@ __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_k
 #pragma unroll 1
                     for (int u = 0; u < TU; ++u) {
                         uint64_t y[NP], s[2] = {0, 0};
-                        load_row(tb + u * TPW, y);
+                        load_row(src + u * src_u, u * TPW < left, y);
                         const bool done = soft(y, s) < -17.f;
                         float w[2];
                         total(s, w);
@@ -310,34 +321,37 @@ __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_k
             }
 #pragma unroll
             for (int u = 0; u < TU; ++u) {
-                const int64_t tt = tb + u * TPW;
-                if (tt >= end) continue;
-                const float inv = sums[2 * u] == 0.f ? 0.f : 1.f / sums[2 * u];
+                if (u * TPW >= left) continue;
+                // (sums of 4e-5 and more, or 0: the approximate reciprocal is as good as a division here)
+                const float inv = sums[2 * u] == 0.f ? 0.f : rcp_approx(sums[2 * u]);
                 const float dot = sums[2 * u + 1] * inv;
                 if (l == 0) {
                     dots += dot;
                     rows += sums[2 * u] == 0.f ? 0 : 1;
                 }
                 if (!a.ds) continue;
-                float* out = a.ds + tt * a.ld_ds;
+                float* out = dst + u * dst_u;
+                const uint64_t scale = f2_of(inv), less = f2_of(-dot);
                 uint64_t g[NP];
 #pragma unroll
-                for (int i = 0; i < NP; ++i) g[i] = f2_mul(f2_mul(x[u][i], f2_of(inv)), f2_add(c(i), f2_of(-dot)));
+                for (int i = 0; i < NP; ++i) g[i] = f2_mul(f2_mul(x[u][i], scale), f2_add(c(i), less));
                 if constexpr (VEC == 4) {
 #pragma unroll
                     for (int v = 0; v < VPL; ++v)
-                        if (column(4 * v) < a.E)
-                            *reinterpret_cast<ulonglong2*>(out + column(4 * v)) = make_ulonglong2(g[2 * v], g[2 * v + 1]);
+                        if (in[v]) *reinterpret_cast<ulonglong2*>(out + 4 * LP * v) = make_ulonglong2(g[2 * v], g[2 * v + 1]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < NP; ++i) {
                         float y, z;
                         f2_unpack(g[i], y, z);
-                        if (column(2 * i) < a.E) out[column(2 * i)] = y;
-                        if (column(2 * i + 1) < a.E) out[column(2 * i + 1)] = z;
+                        if (column(2 * i) < a.E) out[LP * 2 * i] = y;
+                        if (column(2 * i + 1) < a.E) out[LP * (2 * i + 1)] = z;
                     }
                 }
             }
+            left -= WARPS * TPW * TU;
+            src += (WARPS * TU) * src_u;
+            dst += (WARPS * TU) * dst_u;
         }
         t = end;
     }

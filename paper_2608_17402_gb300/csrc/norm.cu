@@ -142,7 +142,18 @@ __device__ __noinline__ float q8_border(float x, float y, float amax) {
     const bool even = ((int)n & 1) == 0;
     return (t > 0.0 || (t == 0.0 && !even)) ? n + 1.0f : n;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {   // NaN where one of them is
+// the largest of three sizes, and the same but NaN where one of them is
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+    float r;
+    asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max_abs_nan(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
@@ -158,9 +169,7 @@ __device__ __forceinline__ uint2 q8_block(const P8& v, float& scale) {
     float x[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) f2_unpack(v.p[i], x[2 * i], x[2 * i + 1]);
-    float amax = fabsf(x[0]);
-#pragma unroll
-    for (int i = 1; i < 8; ++i) amax = max_nan(amax, fabsf(x[i]));
+    float amax = max_nan(max_abs_nan(max_abs_nan(x[0], x[1], x[2]), x[3], x[4]), max_abs_nan(x[5], x[6], x[7]));
 #pragma unroll
     for (int o = 8; o; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     if (!(amax >= Q8_LEAST && amax <= 3.402823466e38f)) {
@@ -186,7 +195,7 @@ __device__ __forceinline__ uint2 q8_block(const P8& v, float& scale) {
         q[2 * i] = __float_as_uint(r0);
         q[2 * i + 1] = __float_as_uint(r1);
         f2_unpack(f2_fma(f2_add(r, down), minus, y), e[2 * i], e[2 * i + 1]);
-        worst = fmaxf(worst, fmaxf(fabsf(e[2 * i]), fabsf(e[2 * i + 1])));
+        worst = max_abs(worst, e[2 * i], e[2 * i + 1]);
     }
     if (worst > NEAR) {
         bool border = false;
