@@ -588,17 +588,18 @@ _KINDS = {None: 0, "rms": 1, "layer": 2}
 _SCORES = {"softmax": 0, "sigmoid": 1}
 _ROW_TYPES = {torch.bfloat16: 0, torch.float32: 1}
 _BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
+_RES = (_BF16, _F32)   # types of a residual stream
 Q8_BLOCK = 128   # columns that share a scale
 
 
-def _rows(t, rows, n, dtype, dev, name):
-    """The address of ``t``, a contiguous tensor of n values of ``dtype`` (one, or a tuple) in ``rows`` rows on the
-    current device ``dev``."""
+def _rows(t, shape, dtype, dev, name):
+    """The address of ``t``, a contiguous tensor of this shape and ``dtype`` (one, or a tuple) on the current
+    device ``dev``."""
     dt = t.dtype
-    if not ((dt is dtype or (type(dtype) is tuple and dt in dtype)) and t.get_device() == dev and t.numel() == n and
-            t.is_contiguous() and t.dim() > 0 and t.size(0) == rows):
-        raise ValueError(f"{name}: expected a contiguous tensor of {dtype}, {n} values in {rows} rows on the current device "
-                         f"cuda:{dev}, got {dt} on {t.device} with shape {tuple(t.shape)} and strides {t.stride()}")
+    if not ((dt is dtype or (type(dtype) is tuple and dt in dtype)) and t.get_device() == dev and t.shape == shape and
+            t.is_contiguous()):
+        raise ValueError(f"{name}: expected a contiguous tensor {tuple(shape)} of {dtype} on the current device cuda:{dev}, "
+                         f"got {dt} on {t.device} with shape {tuple(t.shape)} and strides {t.stride()}")
     return t.data_ptr()
 
 
@@ -646,8 +647,8 @@ class Checkpoint(_Held):
         return self.codes.shape
 
     def _check(self, T, d, dev):
-        _rows(self.codes, T, T * d, _I8, dev, "checkpoint codes")
-        _rows(self.scale, T, T * -(-d // Q8_BLOCK), _F32, dev, "checkpoint scale")
+        _rows(self.codes, (T, d), _I8, dev, "checkpoint codes")
+        _rows(self.scale, (T, -(-d // Q8_BLOCK)), _F32, dev, "checkpoint scale")
 
 
 def moevie_checkpoint_store(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
@@ -656,7 +657,7 @@ def moevie_checkpoint_store(x, out: Checkpoint | None = None, stream=None) -> Ch
         raise ValueError(f"x: expected [T, d], got {tuple(x.shape)}")
     T, d = x.shape
     dev = _device()
-    at = _rows(x, T, T * d, (_BF16, _F32), dev, "x")
+    at = _rows(x, (T, d), _RES, dev, "x")
     if out is None:
         out = Checkpoint.empty(T, d, x.device)
     out.check(T, d, dev)
@@ -672,7 +673,7 @@ def moevie_checkpoint_load(ck: Checkpoint, dtype=torch.bfloat16, out=None, strea
     ck.check(T, d, dev)
     if out is None:
         out = torch.empty((T, d), dtype=dtype, device=ck.codes.device)
-    at = _rows(out, T, T * d, (_BF16, _F32), dev, "out")
+    at = _rows(out, (T, d), _RES, dev, "out")
     _call("moevie_checkpoint_load", ck.codes.data_ptr(), ck.scale.data_ptr(), T, d, at, int(out.dtype is _F32),
           _on(stream, dev))
     return out
@@ -704,17 +705,18 @@ class ResidualNorm(_Held):
         for name in ("w_pre", "b_pre", "w_post", "b_post"):
             t = getattr(self, name)
             if t is not None:
-                _rows(t, d, d, _F32, dev, name)
+                _rows(t, (d,), _F32, dev, name)
         if self.seg is not None:
-            _rows(self.seg, G + 1, G + 1, _I32, dev, "seg")
+            _rows(self.seg, (G + 1,), _I32, dev, "seg")
         if self.gate is not None:
-            _rows(self.gate, G, G * d, _F32, dev, "gate")
+            _rows(self.gate, (G, d), _F32, dev, "gate")
 
     def c_struct(self, dev) -> _Norms:
         self.check(dev)
         seg = self.seg
-        return _Norms(self.d, _KINDS[self.pre], _KINDS[self.post], _address(self.w_pre), _address(self.b_pre),
-                      _address(self.w_post), _address(self.b_post), _address(self.gate), _address(seg),
+        return _Norms(self.d, _KINDS[self.pre], _KINDS[self.post],
+                      *[None if v is None else v.data_ptr()
+                        for v in (self.w_pre, self.b_pre, self.w_post, self.b_post, self.gate, seg)],
                       1 if seg is None else seg.numel() - 1, self.residual_scale, self.eps)
 
 
@@ -760,20 +762,20 @@ class ResidualNormOut(_Held):
         if join:
             if self.r is None:
                 raise ValueError("out.r: missing")
-            _rows(self.r, T, T * d, dtype, dev, "out.r")
+            _rows(self.r, (T, d), dtype, dev, "out.r")
         if self.u is not None:
-            _rows(self.u, T, T * d, _BF16, dev, "out.u")
+            _rows(self.u, (T, d), _BF16, dev, "out.u")
         for name in ("stats_pre", "stats_post"):
             t = getattr(self, name)
             if t is not None:
-                _rows(t, T, 2 * T, _F32, dev, "out." + name)
+                _rows(t, (T, 2), _F32, dev, "out." + name)
 
 
 def _rows_struct(t, T, d, dtype, dev, name):
     if isinstance(t, Checkpoint):
         t.check(T, d, dev)
         return _Rows(t.codes.data_ptr(), t.scale.data_ptr(), 2)
-    return _Rows(_rows(t, T, T * d, dtype, dev, name), None, _ROW_TYPES[t.dtype])
+    return _Rows(_rows(t, (T, d), dtype, dev, name), None, _ROW_TYPES[t.dtype])
 
 
 def _matrix(t, d, name):
@@ -791,9 +793,9 @@ def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, o
     dev, d = _device(), norms.d
     N = norms.c_struct(dev)
     T = _matrix(r, d, "r")
-    R = _rows_struct(r, T, d, (_BF16, _F32), dev, "r")
+    R = _rows_struct(r, T, d, _RES, dev, "r")
     join = f is not None
-    F = _rows(f, T, T * d, _BF16, dev, "f") if join else None
+    F = _rows(f, r.shape, _BF16, dev, "f") if join else None
     dtype = _BF16 if R.type == 2 else r.dtype
     if out is None:
         out = ResidualNormOut.empty(norms, T, dtype, save, join, ws.buf.device)
@@ -832,15 +834,15 @@ class ResidualNormGrads(_Held):
                    like(norms.gate if join else None))
 
     def _check(self, T, d, G, dev):
-        _rows(self.dr, T, T * d, (_BF16, _F32), dev, "out.dr")
+        _rows(self.dr, (T, d), _RES, dev, "out.dr")
         if self.df is not None:
-            _rows(self.df, T, T * d, _BF16, dev, "out.df")
+            _rows(self.df, (T, d), _BF16, dev, "out.df")
         for name in ("dw_pre", "db_pre", "dw_post", "db_post"):
             t = getattr(self, name)
             if t is not None:
-                _rows(t, d, d, _F32, dev, "out." + name)
+                _rows(t, (d,), _F32, dev, "out." + name)
         if self.dgate is not None:
-            _rows(self.dgate, G, G * d, _F32, dev, "out.dgate")
+            _rows(self.dgate, (G, d), _F32, dev, "out.dgate")
 
 
 def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, stats_post,
@@ -858,16 +860,19 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
         dtype = dr.dtype if dr is not None else r.dtype if isinstance(r, torch.Tensor) else _BF16
         out = ResidualNormGrads.empty(norms, T, dtype, f is not None, ws.buf.device)
     out.check(T, d, N.G, dev)
-    res, n = out.dr.dtype, T * d
+    res, shape = out.dr.dtype, (T, d)
     R = ctypes.byref(_rows_struct(r, T, d, res, dev, "r")) if r is not None else None
-    Fr = ctypes.byref(_rows_struct(f, T, d, _BF16, dev, "f")) if f is not None else None
-    _call("moevie_residual_norm_backward", ctypes.byref(N), _rows(dr, T, n, res, dev, "dr") if dr is not None else None,
-          int(res is _F32), _rows(du, T, n, (_BF16, _F32), dev, "du") if du is not None else None,
-          int(du is not None and du.dtype is _F32), R, Fr,
-          _rows(stats_pre, T, 2 * T, _F32, dev, "stats_pre") if stats_pre is not None else None,
-          _rows(stats_post, T, 2 * T, _F32, dev, "stats_post") if stats_post is not None else None, T, out.dr.data_ptr(),
-          _address(out.df), _address(out.dw_pre), _address(out.db_pre), _address(out.dw_post), _address(out.db_post),
-          _address(out.dgate), ws.buf.data_ptr(), ws.nbytes, _on(stream, dev))
+    F = ctypes.byref(_rows_struct(f, T, d, _BF16, dev, "f")) if f is not None else None
+    dr1 = _rows(dr, shape, res, dev, "dr") if dr is not None else None
+    du1 = _rows(du, shape, _RES, dev, "du") if du is not None else None
+    shape = (T, 2)
+    s1 = _rows(stats_pre, shape, _F32, dev, "stats_pre") if stats_pre is not None else None
+    s2 = _rows(stats_post, shape, _F32, dev, "stats_post") if stats_post is not None else None
+    _call("moevie_residual_norm_backward", ctypes.byref(N), dr1, int(res is _F32), du1,
+          int(du is not None and du.dtype is _F32), R, F, s1, s2, T, out.dr.data_ptr(),
+          *[None if v is None else v.data_ptr()
+            for v in (out.df, out.dw_pre, out.db_pre, out.dw_post, out.db_post, out.dgate)],
+          ws.buf.data_ptr(), ws.nbytes, _on(stream, dev))
     return out
 
 
@@ -921,8 +926,8 @@ class BalanceOut(_Held):
                    torch.empty((T, E), dtype=torch.float32, device=device) if grad else None)
 
     def _check(self, T, E, G, dev):
-        _rows(self.loss, 1, 1, _F32, dev, "out.loss")
-        _rows(self.counts, G, G * E, _I32, dev, "out.counts")
+        _rows(self.loss, (1,), _F32, dev, "out.loss")
+        _rows(self.counts, (G, E), _I32, dev, "out.counts")
         if self.ds is not None:
             _logits(self.ds, T, E, dev, "out.ds")
 
@@ -947,9 +952,9 @@ def moevie_balance_loss(s, idx, ws: BalanceWorkspace, coef=0.01, score="sigmoid"
     k = idx.size(1)
     dev = _device()
     ld = _logits(s, T, E, dev, "s")
-    ids = _rows(idx, T, T * k, _I32, dev, "idx")
+    ids = _rows(idx, (T, k), _I32, dev, "idx")
     G = 1 if seg is None else seg.numel() - 1
-    runs = None if seg is None else _rows(seg, G + 1, G + 1, _I32, dev, "seg")
+    runs = None if seg is None else _rows(seg, (G + 1,), _I32, dev, "seg")
     if out is None:
         out = BalanceOut.empty(T, E, G, grad, s.device)
     out.check(T, E, G, dev)

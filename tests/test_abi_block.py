@@ -197,6 +197,6 @@ def test_refusals_of_the_binding():
     with pytest.raises(ValueError):
         moevie._matrix(torch.zeros(4, 32), n.d, "r")
     with pytest.raises(ValueError):
-        moevie._rows(torch.zeros(4, 64), 4, 256, torch.float32, 0, "r")   # not on the device
+        moevie._rows(torch.zeros(4, 64), (4, 64), torch.float32, 0, "r")   # not on the device
     with pytest.raises(KeyError):
         moevie._KINDS["batch"]
