@@ -495,7 +495,7 @@ struct NormArgs {
     float *qr_scale, *qf_scale;
     DevStatus* st;
     int64_t T, G, n_groups;
-    int d, nb, gw, groups, pre, post, r_q8;
+    int d, nb, gw, groups, ranks, span, pre, post, r_q8;   // ranks .. span: see NormPlan
     float alpha, eps;
 };
 struct NormBwdArgs {
@@ -511,7 +511,7 @@ struct NormBwdArgs {
     int2* group_runs;           // [n_groups]: first and last run of every group (G > 1)
     DevStatus* st;
     int64_t T, G, n_groups;
-    int d, nb, gw, groups, pre, post, r_q8, f_q8;
+    int d, nb, gw, groups, ranks, span, pre, post, r_q8, f_q8;
     float alpha;
 };
 struct NormSumArgs {

@@ -19,6 +19,12 @@ namespace mv {
 
 namespace {
 
+// Rows that a row's warps work on at a time: their sums share shuffles and barriers (one row at a time took
+// 400 us for 65536 x 1664 in fp32 where two took 299, bound by issued instructions).
+constexpr int ROWS = 2;
+constexpr int NORM_THREADS = 256;   // of a CTA, at most, but for the forward of rows of more than 2048 columns
+constexpr int fwd_slots(bool f32, bool big) { return f32 || big ? 3 : 4; }   // rows under way
+constexpr int BWD_SLOTS = 2;
 constexpr float Q8_LEAST = 7.70371978e-34f;   // 2^-110: blocks of smaller values are kept as zeros
 
 // ------------------------------------------------------------ 8 columns of a row
@@ -304,37 +310,44 @@ __global__ void __launch_bounds__(256) q8_load_kernel(const int8_t* codes, const
 
 // ------------------------------------------------------------ sums over a row
 
-// A row's warps: wi of gw, of group `group` of the CTA (named barrier group + 1).
+// A row's warps in this CTA: wi of gw, of group `group` (named barrier group + 1).  In the backward a row of
+// more than 2048 columns (WIDE) is shared out over the CTAs of a cluster, `ranks` of them, with one
+// group each.
 struct RowGroup {
-    int gw, wi, lane, group;
+    int gw, wi, lane, group, rank, ranks;
     int buf;        // which half of the group's shared memory the next sum takes
-    int half;       // floats of one: 32, or 64 for more than 16 warps
-    float* part;    // zeros behind the gw-th warp
+    float* part;    // two halves: 32 floats (zeros behind the gw-th warp's), WIDE 128
 };
-constexpr int PART_FLOATS = 2 * 32 * 4;   // of a CTA of one group of 32 warps, or of up to 4 groups that share rows out
+constexpr int PART_FLOATS = 256;   // 4 groups of more than one warp, or one of a cluster's 32
 
-__device__ __forceinline__ RowGroup row_group(int gw, float* s_part) {
+template <bool WIDE>
+__device__ __forceinline__ RowGroup row_group(int gw, int ranks, float* s_part) {
     RowGroup g;
     g.lane = threadIdx.x & 31;
     g.gw = gw;
-    g.group = (threadIdx.x >> 5) / gw;
+    g.group = WIDE ? 0 : (threadIdx.x >> 5) / gw;
     g.wi = (threadIdx.x >> 5) - g.group * gw;
+    g.rank = WIDE ? (int)cluster_rank() : 0;
+    g.ranks = WIDE ? ranks : 1;
     g.buf = 0;
-    g.half = gw > 16 ? 64 : 32;
-    g.part = s_part + g.group * 2 * g.half;   // (of groups of one warp never touched)
-    if (gw > 1)
-        for (int i = g.wi * 32 + g.lane; i < 2 * g.half; i += gw * 32) g.part[i] = 0.f;
+    g.part = s_part + g.group * 64;   // (of groups of one warp never touched)
+    if (!WIDE && gw > 1)
+        for (int i = g.wi * 32 + g.lane; i < 64; i += gw * 32) g.part[i] = 0.f;
     return g;
 }
-__device__ __forceinline__ void group_barrier(const RowGroup& g) {
-    asm volatile("bar.sync %0, %1;" ::"r"(g.group + 1), "r"(g.gw * 32) : "memory");
+// All of a row's warps, in all CTAs that share it.
+template <bool WIDE>
+__device__ __forceinline__ void row_barrier(const RowGroup& g) {
+    __syncwarp();
+    if constexpr (WIDE) cluster_sync();
+    else asm volatile("bar.sync %0, %1;" ::"r"(g.group + 1), "r"(g.gw * 32) : "memory");
 }
 
-// v[n] <- the sum of v[n] over the row's threads, the same bits in all of them; N = 1, 2 or 4.  The
-// sums share one set of shuffles: after the first steps each lane carries one of them, the n-th
-// lanes 32 n / N on.  Then a word for each warp and sum, read back one to a lane.  One barrier: a warp
-// that passes the next one's has read this one's half.
-template <int N>
+// v[n] <- the sum of v[n] over the row's threads, the same bits in all of them; N = 1, 2 or 4.  The sums
+// share one set of shuffles: after the first steps each lane carries one of them, the n-th lanes
+// 32 n / N on.  Then a word for each warp and sum (WIDE: in every CTA of the cluster), read back one or a
+// few to a lane.  One barrier: a warp that passes the next one's has read this one's half.
+template <bool WIDE, int N>
 __device__ __forceinline__ void row_sum(RowGroup& g, float (&v)[N]) {
     static_assert(N == 1 || N == 2 || N == 4, "");
     constexpr int SPAN = 32 / N;   // lanes of one sum
@@ -352,21 +365,30 @@ __device__ __forceinline__ void row_sum(RowGroup& g, float (&v)[N]) {
     }
 #pragma unroll
     for (int o = SPAN / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    if (g.gw == 1) {
+    if (!WIDE && g.gw == 1) {
 #pragma unroll
-        for (int n = 0; n < N; ++n) v[n] = N == 1 ? x : __shfl_sync(0xffffffffu, x, SPAN * n);
+        for (int n = 0; n < N; ++n) v[n] = __shfl_sync(0xffffffffu, x, SPAN * n);
         return;
     }
-    float* p = g.part + g.buf * g.half;
-    if (g.lane % SPAN == 0) p[g.wi * N + g.lane / SPAN] = x;
-    group_barrier(g);
-    x = p[g.lane];
-    if (N == 2 && g.gw > 16) x += p[g.lane + 32];
-    constexpr int MOST = N == 4 ? 8 : 32 / N;   // warps whose words 32 lanes hold
+    float* p = g.part + g.buf * (WIDE ? 128 : 32);
+    if constexpr (WIDE) {
+        if (g.lane % SPAN == 0) {
+            const uint32_t mine = smem_u32(p + (g.rank * g.gw + g.wi) * N + g.lane / SPAN);
+            for (int r = 0; r < g.ranks; ++r)
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_addr(mine, r)), "f"(x) : "memory");
+        }
+        row_barrier<true>(g);
+        x = 0.f;
+        for (int i = g.lane; i < g.ranks * g.gw * N; i += 32) x += p[i];
 #pragma unroll
-    for (int w = 1; w < MOST; w *= 2) {
-        if (w >= 8 && g.gw <= w) break;
-        x += __shfl_xor_sync(0xffffffffu, x, w * N);
+        for (int o = N; o < 32; o *= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
+    } else {
+        if (g.lane % SPAN == 0) p[g.wi * N + g.lane / SPAN] = x;
+        row_barrier<false>(g);
+        x = p[g.lane];
+        constexpr int MOST = N == 1 ? 32 : 8 * N;   // (8 warps to a row, but where one sum at a time is formed)
+#pragma unroll
+        for (int o = N; o < MOST; o *= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) v[n] = __shfl_sync(0xffffffffu, x, n);
@@ -384,7 +406,7 @@ __device__ __forceinline__ void row_stats(RowGroup& g, P8 (&x)[ROWS], bool act, 
     if (kind == MOEVIE_NORM_LAYER) {
 #pragma unroll
         for (int k = 0; k < ROWS; ++k) s[k] = p8_sum(x[k]);
-        row_sum(g, s);
+        row_sum<false>(g, s);
 #pragma unroll
         for (int k = 0; k < ROWS; ++k) {
             st[k].x = s[k] * inv_d;
@@ -395,7 +417,7 @@ __device__ __forceinline__ void row_stats(RowGroup& g, P8 (&x)[ROWS], bool act, 
     }
 #pragma unroll
     for (int k = 0; k < ROWS; ++k) s[k] = act ? p8_dot(x[k], x[k]) : 0.f;
-    row_sum(g, s);
+    row_sum<false>(g, s);
 #pragma unroll
     for (int k = 0; k < ROWS; ++k) st[k].y = rsqrtf(fmaf(s[k], inv_d, eps));
 }
@@ -539,42 +561,22 @@ struct Operand {
             return p8_bf16(ld_shared(src + ring.own));
         }
     }
-    __device__ __forceinline__ P8 read(int64_t at, int64_t sat) const {   // without a ring
-        if (Q8 && q8) {
-            const uint2 c = ld8(static_cast<const int8_t*>(data) + at);
-            float s;
-            asm volatile("ld.global.f32 %0, [%1];" : "=f"(s) : "l"(scale + sat));
-            return p8_codes(c.x, c.y, s);
-        }
-        if constexpr (F32) {
-            const float* p = static_cast<const float*>(data) + at;
-            return p8_f32(ld16(p), ld16(p + 4));
-        } else {
-            return p8_bf16(ld16(static_cast<const __nv_bfloat16*>(data) + at));
-        }
-    }
 };
 
 // ------------------------------------------------------------ forward
 
-// Rows a CTA's threads work on at a time: two, whose sums share shuffles and barriers (one row at a
-// time took 400 us for 65536 x 1664 in fp32, bound by issued instructions), or one in the largest
-// CTAs, whose threads have 64 registers.
-constexpr int rows_at_once(int threads) { return threads == 1024 ? 1 : 2; }
-constexpr int fwd_slots(bool f32, int threads) { return f32 || threads == 1024 ? 3 : 4; }
-constexpr int BWD_SLOTS = 2;
-
 // JOIN: r1 = alpha r + gate * N_post(f), and its norm; otherwise the norm of r alone.  BOTH: a join with
 // both norms and their statistics (the others ask as they go).  SAVE: 8-bit checkpoints of what is read.
-// THREADS: a CTA's at most.
-template <bool F32, bool JOIN, bool BOTH, bool SAVE, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? (SAVE ? 3 : 2) : 1) norm_forward_kernel(const NormArgs a) {
-    constexpr bool BIG = THREADS == 1024;
-    constexpr int ROWS = rows_at_once(THREADS), SLOTS = fwd_slots(F32, THREADS), PR = F32 ? 2 : 1, PIECES = PR + (JOIN ? 1 : 0);
+// BIG: rows of more than 2048 columns, by CTAs of up to 1024 threads of 64 registers, a row at a time (over
+// the CTAs of a cluster, as in the backward, its up to four barriers a row cost more: 8192 x 4096 bf16 135 us
+// instead of 70).
+template <bool F32, bool JOIN, bool BOTH, bool SAVE, bool BIG>
+__global__ void __launch_bounds__(BIG ? 1024 : NORM_THREADS, BIG ? 1 : SAVE ? 3 : 2) norm_forward_kernel(const NormArgs a) {
+    constexpr int ROWS = BIG ? 1 : mv::ROWS, SLOTS = fwd_slots(F32, BIG), PR = F32 ? 2 : 1, PIECES = PR + (JOIN ? 1 : 0);
     extern __shared__ __align__(16) uint8_t s_dyn[];
     __shared__ __align__(16) float s_part[PART_FLOATS];
     pdl_wait();
-    RowGroup g = row_group(a.gw, s_part);
+    RowGroup g = row_group<false>(a.gw, 1, s_part);
     if (a.seg) check_runs(a.seg, a.G, a.T, a.st);
     const int col = (g.wi * 32 + g.lane) * 8;
     const bool act = col < a.d;
@@ -615,7 +617,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? (SAVE ? 3 : 2) : 1) 
     const bool first = g.wi == 0 && g.lane == 0;
     float2 *const stats_pre = a.stats_pre + t0, *const stats_post = a.stats_post + t0;
     int64_t at = t0 * d + col;
-    if (g.gw > 1) group_barrier(g);   // the zeros of row_group
+    if (g.gw > 1) row_barrier<false>(g);   // the zeros of row_group
 
 #pragma unroll 1
     for (int i = 0; i < n;) {
@@ -721,12 +723,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? (SAVE ? 3 : 2) : 1) 
 
 // ------------------------------------------------------------ backward
 
-// Sums of this thread's 8 columns: in registers, or, for the rows of more than 16 warps whose
-// threads have 64 registers, in shared memory (each thread its own words, no bank shared).
-template <bool SHARED>
+// Sums of this thread's 8 columns.
 struct Sums {
     P8 v;
-    __device__ __forceinline__ Sums(void*, int) { clear(); }
+    __device__ __forceinline__ Sums() { clear(); }
     __device__ __forceinline__ void clear() { v = p8_of(0.f); }
     __device__ __forceinline__ void add(const P8& x) {
 #pragma unroll
@@ -737,33 +737,6 @@ struct Sums {
         for (int i = 0; i < 4; ++i) v.p[i] = f2_fma(x.p[i], y.p[i], v.p[i]);
     }
     __device__ __forceinline__ void store(float* p) const { st_f32(p, v); }
-};
-template <>
-struct Sums<true> {
-    uint64_t* p;
-    __device__ __forceinline__ Sums(void* base, int which)
-        : p(static_cast<uint64_t*>(base) + which * 4 * blockDim.x + threadIdx.x) {
-        clear();
-    }
-    __device__ __forceinline__ uint64_t& at(int i) const { return p[i * blockDim.x]; }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) at(i) = 0;
-    }
-    __device__ __forceinline__ void add(const P8& x) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) at(i) = f2_add(x.p[i], at(i));
-    }
-    __device__ __forceinline__ void add(const P8& x, const P8& y) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) at(i) = f2_fma(x.p[i], y.p[i], at(i));
-    }
-    __device__ __forceinline__ void store(float* out) const {
-        P8 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v.p[i] = at(i);
-        st_f32(out, v);
-    }
 };
 
 // Of row t, with x1, x2 the normed rows before weight and bias and inv_s their 1 / deviation:
@@ -776,33 +749,32 @@ struct Sums<true> {
 // of run g at record g + gid (along the rows g and gid never fall, so that no two share one).
 // ALL: both norms, dr1 and f; the others ask as they go.  Q8: r1 and f may be checkpoints.  BIAS: db_pre and B
 // as well.
-template <bool F32, bool DUF32, bool ALL, bool Q8, bool BIAS, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward_kernel(const NormBwdArgs a) {
-    constexpr bool BIG = THREADS == 1024;   // no ring: its memory holds the sums
-    constexpr int ROWS = rows_at_once(THREADS);
+template <bool F32, bool DUF32, bool ALL, bool Q8, bool BIAS, bool WIDE>
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_backward_kernel(const NormBwdArgs a) {
     constexpr int PR = F32 ? 2 : 1, PU = DUF32 ? 2 : 1, PIECES = 2 * PR + PU + 2;   // the last: the row's statistics
-    extern __shared__ __align__(16) uint8_t s_dyn[];   // Kept; the ring, or (BIG) 4 sums of 8 columns for each thread
+    extern __shared__ __align__(16) uint8_t s_dyn[];   // Kept, the ring
     __shared__ __align__(16) float s_part[PART_FLOATS];
     pdl_wait();
-    RowGroup g = row_group(a.gw, s_part);
+    RowGroup g = row_group<WIDE>(a.gw, a.ranks, s_part);
     if (a.seg) check_runs(a.seg, a.G, a.T, a.st);
-    const int col = (g.wi * 32 + g.lane) * 8;
-    const bool act = col < a.d;
-    const int64_t gid = (int64_t)blockIdx.x * a.groups + g.group;
-    if (gid >= a.n_groups) return;
+    const int first_col = WIDE ? g.rank * a.span : 0;               // of this CTA's share of a row,
+    const int cols = WIDE ? min(a.span, a.d - first_col) : a.d;     // and its columns
+    const int col = first_col + (g.wi * 32 + g.lane) * 8;
+    const bool act = col - first_col < cols;
+    const int64_t gid = WIDE ? blockIdx.x / a.ranks : (int64_t)blockIdx.x * a.groups + g.group;
+    if (gid >= a.n_groups) return;   // (whole clusters alike)
     int64_t t0 = first_row(a.T, gid, a.n_groups), t1 = first_row(a.T, gid + 1, a.n_groups);
     clip_rows(a, t0, t1);
 
     const bool norm = ALL || a.du != nullptr, has_f = ALL || a.f != nullptr, join = ALL || a.df != nullptr;
     const bool post = ALL || a.post != MOEVIE_NORM_NONE, has_dr = ALL || a.dr1 != nullptr;
-    uint8_t* const s_rows = s_dyn + KEPT_BYTES * blockDim.x;
-    const RowRing<BWD_SLOTS, PIECES> ring(s_rows, a.d - g.wi * 256);
+    const RowRing<BWD_SLOTS, PIECES> ring(s_dyn + KEPT_BYTES * blockDim.x, cols - g.wi * 256);
     const Operand<F32, false> Dr{a.dr1, nullptr, 0};
     const Operand<F32, Q8> R1{a.r1, a.r1_scale, a.r_q8};
     const Operand<DUF32, false> Du{a.du, nullptr, 0};
     const Operand<false, Q8> Fo{a.f, a.f_scale, a.f_q8};
     const int n = t0 < t1 ? (int)(t1 - t0) : 0, d = a.d;   // rows count from t0
-    int64_t at = t0 * d + col, sat = t0 * a.nb + (col >> 7);   // of the row in hand
+    int64_t at = t0 * d + col;   // of the row in hand
     // Two sets of copies: dr1, du, r1 and the single words, whose slots are free as soon as a row is begun, and f, which
     // is read half-way.  Both sets of a row are under way while the two rows before it are worked on.
     // `on`: rows from the one in hand
@@ -810,8 +782,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     // A row's last piece: the statistics of N_pre (words 0, 1) and, with the second set, of N_post (2, 3), by
     // lane 0; the scales of the warp's two blocks of r1 (4, 5) and of f (6, 7), by lanes 0 and 1.
     const float2 *st1_at = a.stats_pre + t0, *st2_at = a.stats_post + t0;   // of the row in hand
-    const bool scaled = Q8 && g.lane < 2 && g.wi * 2 + g.lane < a.nb;
-    const int64_t scale_at = t0 * a.nb + g.wi * 2 + g.lane;
+    const int block = first_col / 128 + g.wi * 2 + g.lane;
+    const bool scaled = Q8 && g.lane < 2 && block < a.nb;
+    const int64_t scale_at = t0 * a.nb + block;
     const float* s1_at = Q8 && scaled && a.r_q8 ? a.r1_scale + scale_at : nullptr;
     const float* s2_at = Q8 && scaled && a.f_q8 ? a.f_scale + scale_at : nullptr;
     const uint32_t scale_word = (4 + (g.lane >> 4)) * 4;   // r1's; f's two words on
@@ -833,19 +806,17 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
         if (post && g.lane == 0) copy8(words + 8, st2_at + on, live ? 8 : 0);
         if (Q8 && s2_at) copy4(words + 24 + g.lane * 4, s2_at + on * a.nb, live ? 4 : 0);
     };
-    if constexpr (!BIG) {
-        copy_first(0, 0, 0);
-        copy_first(1, 0, 1);
-        cp_async_commit();
-        copy_second(0, 0, 0);
-        copy_second(1, 0, 1);
-        cp_async_commit();
-    }
+    copy_first(0, 0, 0);
+    copy_first(1, 0, 1);
+    cp_async_commit();
+    copy_second(0, 0, 0);
+    copy_second(1, 0, 1);
+    cp_async_commit();
 
     const float inv_d = 1.0f / (float)d;
     const Kept w1(s_dyn, 0), cw(s_dyn, 1);   // cw: gate * weight
     w1.set(ld_param(a.w_pre, col, act, 1.f));
-    Sums<BIG> sw(s_rows, 0), sb(s_rows, 1), sA(s_rows, 2), sB(s_rows, 3);   // dw_pre, db_pre, A, B
+    Sums sw, sb, sA, sB;   // dw_pre, db_pre, A, B
     int64_t run = 0;
     int run_end = n;
 
@@ -875,7 +846,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
         load_run();
     }
     const int64_t first_run = run;
-    if (g.gw > 1) group_barrier(g);   // the zeros of row_group
+    if (WIDE || g.gw > 1) row_barrier<WIDE>(g);   // the zeros of row_group; the cluster's CTAs are there
 
 #pragma unroll 1
     for (int i = 0; i < n;) {
@@ -888,15 +859,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
             load_run();
         }
         // rows i and, of the same run, i + 1
-        const bool two = ROWS == 2 && i + 1 < run_end;
+        const bool two = i + 1 < run_end;
         P8 dR[ROWS], x1[ROWS], du[ROWS], x2[ROWS];
         float2 st1[ROWS], st2[ROWS];
-        if constexpr (BIG) {
-            dR[0] = x1[0] = du[0] = p8_of(0.f);
-            if (act && has_dr) dR[0] = Dr.read(at, sat);
-            if (act && norm) x1[0] = R1.read(at, sat), du[0] = Du.read(at, sat);
-            if (norm) st1[0] = a.stats_pre[t0 + i];
-        } else {
             cp_async_wait<1>();
             __syncwarp();   // the other lanes' copies
 #pragma unroll
@@ -914,11 +879,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
             copy_first(slot, i, 2);
             if (two) copy_first(slot ^ 1, i, 3);
             cp_async_commit();
-            if (ROWS == 2 && !two) {   // i + 1 is not of this run: nothing of it counts here
+            if (!two) {   // i + 1 is not of this run: nothing of it counts here
                 dR[ROWS - 1] = x1[ROWS - 1] = du[ROWS - 1] = p8_of(0.f);
                 st1[ROWS - 1] = make_float2(0.f, 0.f);
             }
-        }
         if (norm) {
             float s[2 * ROWS];
             const P8 w = w1.get();
@@ -934,7 +898,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
                 s[2 * k] = p8_sum(du[k]);
                 s[2 * k + 1] = p8_dot(du[k], x1[k]);
             }
-            row_sum(g, s);
+            row_sum<WIDE>(g, s);
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
                 const uint64_t m0 = f2_of(a.pre == MOEVIE_NORM_LAYER ? -s[2 * k] * inv_d : 0.f);
@@ -952,11 +916,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
             for (int j = 0; j < 4; ++j) o.p[j] = f2_mul(al, dR[k].p[j]);
             if (act && (k == 0 || two)) st_rows<F32>(a.dr, at + k * d, o);
         }
-        if constexpr (BIG) {
-            x2[0] = p8_of(0.f);
-            if (act && has_f) x2[0] = Fo.read(at, sat);
-            if (post) st2[0] = a.stats_post[t0 + i];
-        } else {
             cp_async_wait<1>();
             __syncwarp();   // the other lanes' words
 #pragma unroll
@@ -970,12 +929,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
             copy_second(slot, i, 2);
             if (two) copy_second(slot ^ 1, i, 3);
             cp_async_commit();
-            if (ROWS == 2 && !two) {
+            if (!two) {
                 x2[ROWS - 1] = p8_of(0.f);
                 st2[ROWS - 1] = make_float2(0.f, 0.f);
                 slot ^= 1;
             }
-        }
         if (join) {
             const P8 w = cw.get();
             if (post) {
@@ -992,7 +950,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
                     s[2 * k] = p8_sum(dR[k]);
                     s[2 * k + 1] = p8_dot(dR[k], x2[k]);
                 }
-                row_sum(g, s);
+                row_sum<WIDE>(g, s);
 #pragma unroll
                 for (int k = 0; k < ROWS; ++k) {
                     const uint64_t m0 = f2_of(a.post == MOEVIE_NORM_LAYER ? -s[2 * k] * inv_d : 0.f);
@@ -1017,12 +975,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
         at += two ? 2 * d : d;
         st1_at += two ? 2 : 1;
         st2_at += two ? 2 : 1;
-        if (BIG) sat += a.nb;
         if (Q8 && s1_at) s1_at += two ? 2 * a.nb : a.nb;
         if (Q8 && s2_at) s2_at += two ? 2 * a.nb : a.nb;
     }
     if (n > 0 || a.G == 1) flush_run();   // a group without rows leaves zeros where only one run is
-    if (a.group_runs && g.wi == 0 && g.lane == 0)
+    if (a.group_runs && g.rank == 0 && g.wi == 0 && g.lane == 0)
         a.group_runs[gid] = n > 0 ? make_int2((int)first_run, (int)run) : make_int2(0, -1);
     if (a.rec_pre && act) {
         float* p = a.rec_pre + gid * 2 * a.d + col;
@@ -1121,25 +1078,31 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const NormSumArgs a, in
         a.dgate[run * a.d + col] = fmaf(a.w_post ? a.w_post[col] : 1.f, va, (a.b_post ? a.b_post[col] : 0.f) * vb);
 }
 
-// Warps of a row, row groups of a CTA and the grid: about `threads_sm` threads to an SM.
+// CTAs that share a row and columns of each, warps of a row in a CTA, row groups of a CTA and the grid.
 struct NormPlan {
-    int gw, groups, threads, grid;
+    int ranks, span, gw, groups, threads, grid;
     int64_t n_groups;   // at most T; the last CTA's groups beyond them have nothing to do
 };
-NormPlan norm_plan(int64_t T, int d, int threads_sm) {
+// About `threads_sm` threads to an SM.  shared: rows of more than 2048 columns by clusters, of which at most
+// `clusters` (0: as many as there is room for).
+NormPlan norm_plan(int64_t T, int d, int threads_sm, bool shared, int clusters = 0) {
     NormPlan p;
-    p.gw = (d / 8 + 31) / 32;
-    p.groups = p.gw == 1 ? 8 : p.gw == 2 ? 4 : p.gw <= 4 ? 2 : 1;
+    p.ranks = shared ? (d + 2047) / 2048 : 1;
+    p.span = p.ranks == 1 ? d : ((d + 127) / 128 + p.ranks - 1) / p.ranks * 128;   // whole blocks of a checkpoint
+    p.gw = (p.span / 8 + 31) / 32;
+    p.groups = p.ranks > 1 ? 1 : p.gw == 1 ? 8 : p.gw == 2 ? 4 : p.gw <= 4 ? 2 : 1;
     p.threads = p.gw * 32 * p.groups;
-    const int64_t most = (int64_t)GB300_SMS * std::max(1, threads_sm / p.threads);
-    p.grid = (int)std::max<int64_t>(1, std::min<int64_t>(most, (T + p.groups - 1) / p.groups));
-    p.n_groups = std::min<int64_t>(T, (int64_t)p.grid * p.groups);
+    int64_t most = (int64_t)GB300_SMS * std::max(1, threads_sm / p.threads) / p.ranks;
+    if (clusters > 0) most = std::min<int64_t>(most, clusters);
+    const int64_t units = std::max<int64_t>(1, std::min<int64_t>(most, (T + p.groups - 1) / p.groups));
+    p.grid = (int)units * p.ranks;
+    p.n_groups = std::min<int64_t>(T, units * p.groups);
     return p;
 }
 // Threads to an SM.  Forward: 512 with 128 registers each (65536 x 1664 in fp32: 204 us, with 768 of 80 each 228),
 // but 768 where checkpoints are formed as well, which is bound by instructions, not by bytes.
-constexpr int NORM_FWD_THREADS = 512, NORM_SAVE_THREADS = 768, NORM_BWD_THREADS = 512;
-constexpr int NORM_MAX_SMEM = 208 * 1024;   // 1024 threads with three rows of fp32 and bf16 each
+constexpr int NORM_FWD_THREADS = 512, NORM_SAVE_THREADS = 768, NORM_BIG_THREADS = 1024, NORM_BWD_THREADS = 512;
+constexpr int NORM_MAX_SMEM = 112 * 1024, NORM_BIG_SMEM = 208 * 1024;
 
 // Grid of the checkpoint kernels and the step of their walk over the blocks, CTAs_SM to an SM at most.
 struct BlockPlan {
@@ -1180,86 +1143,127 @@ cudaError_t launch_q8_load(const int8_t* codes, const float* scales, int64_t T, 
     return e;
 }
 
-// Launches kern with `smem` bytes of dynamic shared memory, which its attribute allows from the first
-// launch on a device on.
-template <typename Args>
-static cudaError_t launch_rows(void (*kern)(Args), std::atomic<bool> (&attr_set)[64], const NormPlan& p, size_t smem,
-                               cudaStream_t s, const Args& a) {
-    int dev = 0;
+// What the first launch of a kernel on a device sets up: its shared memory's limit, and, for one of
+// clusters, how many of them run at a time.
+struct RowsKernel {
+    std::atomic<int> ready[64][5][33];   // [device][CTAs of a cluster][warps of a CTA]: 0 not yet, else clusters + 1
+};
+
+// Launches kern for the rows of a with smem_thread bytes of dynamic shared memory for each thread, rows of more
+// than 2048 columns shared out over clusters or by one BIG CTA each.
+template <bool BIG, typename Args>
+static cudaError_t launch_rows(void (*kern)(Args), RowsKernel& k, bool shared, int threads_sm, size_t smem_thread,
+                               cudaStream_t s, Args& a) {
+    constexpr int most_smem = BIG ? NORM_BIG_SMEM : NORM_MAX_SMEM;
+    NormPlan p = norm_plan(a.T, a.d, threads_sm, shared);
+    const size_t smem = smem_thread * p.threads;
+    if (smem > most_smem || p.ranks > 4 || p.threads > (BIG ? 1024 : NORM_THREADS)) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[2];
+    cfg.blockDim = dim3(p.threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see launch_pdl
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)p.ranks;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    int dev = 0, clusters = 0;
     cudaGetDevice(&dev);
-    if (dev >= 0 && dev < 64 && !attr_set[dev].load(std::memory_order_acquire)) {   // idempotent: no lock needed
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_MAX_SMEM);
-        if (e != cudaSuccess) return e;
-        attr_set[dev].store(true, std::memory_order_release);
+    if (dev >= 0 && dev < 64) {
+        std::atomic<int>& ready = k.ready[dev][p.ranks][p.threads / 32];
+        int now = ready.load(std::memory_order_acquire);
+        if (now == 0) {   // idempotent: no lock needed
+            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem);
+            if (e != cudaSuccess) return e;
+            now = 1;
+            if (p.ranks > 1) {
+                cudaLaunchConfig_t most = cfg;
+                most.gridDim = dim3(p.ranks);
+                most.attrs = at + 1;
+                most.numAttrs = 1;
+                int n = 0;
+                if (cudaOccupancyMaxActiveClusters(&n, kern, &most) != cudaSuccess || n < 1) {
+                    cudaGetLastError();
+                    n = GB300_SMS / p.ranks;   // (one to so many SMs)
+                }
+                now = n + 1;
+            }
+            ready.store(now, std::memory_order_release);
+        }
+        clusters = now - 1;
     }
-    return launch_pdl(kern, dim3(p.grid), dim3(p.threads), smem, s, a);
+    if (p.ranks > 1) p = norm_plan(a.T, a.d, threads_sm, shared, clusters);
+    cfg.gridDim = dim3(p.grid);
+    cfg.numAttrs = p.ranks > 1 ? 2 : 1;
+    a.gw = p.gw;
+    a.groups = p.groups;
+    a.ranks = p.ranks;
+    a.span = p.span;
+    a.n_groups = p.n_groups;
+    a.nb = (a.d + 127) / 128;
+    return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
-template <bool F32, bool JOIN, bool BOTH, bool SAVE, int THREADS>
-static cudaError_t norm_forward(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
-    static std::atomic<bool> attr_set[64];
-    const size_t smem = (size_t)((THREADS == 1024 ? 1 : 2) * KEPT_BYTES + 16 * fwd_slots(F32, THREADS) * ((F32 ? 2 : 1) + (JOIN ? 1 : 0))) * p.threads;
-    return launch_rows(norm_forward_kernel<F32, JOIN, BOTH, SAVE, THREADS>, attr_set, p, smem, s, a);
+template <bool F32, bool JOIN, bool BOTH, bool SAVE, bool BIG>
+static cudaError_t norm_forward(NormArgs& a, cudaStream_t s) {
+    static RowsKernel k;
+    return launch_rows<BIG>(norm_forward_kernel<F32, JOIN, BOTH, SAVE, BIG>, k, false,
+                            BIG ? NORM_BIG_THREADS : SAVE ? NORM_SAVE_THREADS : NORM_FWD_THREADS,
+                            (BIG ? 1 : 2) * KEPT_BYTES + 16 * fwd_slots(F32, BIG) * ((F32 ? 2 : 1) + (JOIN ? 1 : 0)), s, a);
 }
 template <bool F32, bool JOIN, bool SAVE>
-static cudaError_t norm_forward(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
-    if (p.threads > 256) return norm_forward<F32, JOIN, false, SAVE, 1024>(a, p, s);
+static cudaError_t norm_forward(NormArgs& a, cudaStream_t s) {
+    if (a.d > 2048) return norm_forward<F32, JOIN, false, SAVE, true>(a, s);
     if (JOIN && a.post != MOEVIE_NORM_NONE && a.u && a.stats_pre && a.stats_post)
-        return norm_forward<F32, JOIN, JOIN, SAVE, 256>(a, p, s);
-    return norm_forward<F32, JOIN, false, SAVE, 256>(a, p, s);
+        return norm_forward<F32, JOIN, JOIN, SAVE, false>(a, s);
+    return norm_forward<F32, JOIN, false, SAVE, false>(a, s);
 }
 template <bool F32>
-static cudaError_t norm_forward(const NormArgs& a, const NormPlan& p, cudaStream_t s) {
+static cudaError_t norm_forward(NormArgs& a, cudaStream_t s) {
     const bool save = a.qr || a.qf;
-    if (!a.f) return save ? norm_forward<F32, false, true>(a, p, s) : norm_forward<F32, false, false>(a, p, s);
-    return save ? norm_forward<F32, true, true>(a, p, s) : norm_forward<F32, true, false>(a, p, s);
+    if (!a.f) return save ? norm_forward<F32, false, true>(a, s) : norm_forward<F32, false, false>(a, s);
+    return save ? norm_forward<F32, true, true>(a, s) : norm_forward<F32, true, false>(a, s);
 }
 
 cudaError_t launch_norm_forward(NormArgs a, int r_f32, cudaStream_t s) {
-    const NormPlan p = norm_plan(a.T, a.d, a.qr || a.qf ? NORM_SAVE_THREADS : NORM_FWD_THREADS);
-    a.gw = p.gw;
-    a.groups = p.groups;
-    a.n_groups = p.n_groups;
-    a.nb = (a.d + 127) / 128;
-    const cudaError_t e = r_f32 ? norm_forward<true>(a, p, s) : norm_forward<false>(a, p, s);
+    const cudaError_t e = r_f32 ? norm_forward<true>(a, s) : norm_forward<false>(a, s);
     count_launches(1);
     return e;
 }
 
 int64_t norm_groups(int64_t T, int d) {
-    return std::max<int64_t>(1, norm_plan(T, d, NORM_BWD_THREADS).n_groups);
+    return std::max<int64_t>(1, norm_plan(T, d, NORM_BWD_THREADS, true).n_groups);
 }
 
-template <bool F32, bool DUF32, bool ALL, bool Q8, bool BIAS, int THREADS>
-static cudaError_t norm_backward(const NormBwdArgs& a, const NormPlan& p, cudaStream_t s) {
-    static std::atomic<bool> attr_set[64];
-    const int words = THREADS == 1024 ? 8 : BWD_SLOTS * (2 * (F32 ? 2 : 1) + (DUF32 ? 2 : 1) + 2);   // of 16 bytes
-    return launch_rows(norm_backward_kernel<F32, DUF32, ALL, Q8, BIAS, THREADS>, attr_set, p,
-                       (size_t)(KEPT_BYTES + 16 * words) * p.threads, s, a);
+template <bool F32, bool DUF32, bool ALL, bool Q8, bool BIAS, bool WIDE>
+static cudaError_t norm_backward(NormBwdArgs& a, cudaStream_t s) {
+    static RowsKernel k;
+    return launch_rows<false>(norm_backward_kernel<F32, DUF32, ALL, Q8, BIAS, WIDE>, k, true, NORM_BWD_THREADS,
+                              KEPT_BYTES + 16 * BWD_SLOTS * (2 * (F32 ? 2 : 1) + (DUF32 ? 2 : 1) + 2), s, a);
+}
+template <bool F32, bool DUF32, bool WIDE>
+static cudaError_t norm_backward(NormBwdArgs& a, bool bias, cudaStream_t s) {
+    if (!a.du || !a.dr1 || !a.df || !a.f || a.post == MOEVIE_NORM_NONE)
+        return norm_backward<F32, DUF32, false, true, true, WIDE>(a, s);
+    if (a.r_q8 || a.f_q8)
+        return bias ? norm_backward<F32, DUF32, true, true, true, WIDE>(a, s)
+                    : norm_backward<F32, DUF32, true, true, false, WIDE>(a, s);
+    return bias ? norm_backward<F32, DUF32, true, false, true, WIDE>(a, s)
+                : norm_backward<F32, DUF32, true, false, false, WIDE>(a, s);
 }
 template <bool F32, bool DUF32>
-static cudaError_t norm_backward(const NormBwdArgs& a, const NormPlan& p, bool bias, cudaStream_t s) {
-    if (p.threads > 256) return norm_backward<F32, DUF32, false, true, true, 1024>(a, p, s);
-    if (!a.du || !a.dr1 || !a.df || !a.f || a.post == MOEVIE_NORM_NONE)
-        return norm_backward<F32, DUF32, false, true, true, 256>(a, p, s);
-    if (a.r_q8 || a.f_q8)
-        return bias ? norm_backward<F32, DUF32, true, true, true, 256>(a, p, s)
-                    : norm_backward<F32, DUF32, true, true, false, 256>(a, p, s);
-    return bias ? norm_backward<F32, DUF32, true, false, true, 256>(a, p, s)
-                : norm_backward<F32, DUF32, true, false, false, 256>(a, p, s);
+static cudaError_t norm_backward(NormBwdArgs& a, bool bias, cudaStream_t s) {
+    return a.d > 2048 ? norm_backward<F32, DUF32, true>(a, bias, s) : norm_backward<F32, DUF32, false>(a, bias, s);
 }
 
 cudaError_t launch_norm_backward(NormBwdArgs a, int r_f32, int du_f32, NormSumArgs sums, cudaStream_t s) {
-    const NormPlan p = norm_plan(a.T, a.d, NORM_BWD_THREADS);
-    a.gw = p.gw;
-    a.groups = p.groups;
-    a.n_groups = p.n_groups;
-    a.nb = (a.d + 127) / 128;
     cudaError_t e;
     const bool bias = sums.db_pre || sums.db_post || (sums.dgate && sums.b_post);
     sums.bias = bias;
-    if (r_f32) e = du_f32 ? norm_backward<true, true>(a, p, bias, s) : norm_backward<true, false>(a, p, bias, s);
-    else e = du_f32 ? norm_backward<false, true>(a, p, bias, s) : norm_backward<false, false>(a, p, bias, s);
+    if (r_f32) e = du_f32 ? norm_backward<true, true>(a, bias, s) : norm_backward<true, false>(a, bias, s);
+    else e = du_f32 ? norm_backward<false, true>(a, bias, s) : norm_backward<false, false>(a, bias, s);
     count_launches(1);
     if (e != cudaSuccess || (!a.rec_pre && !a.rec_post)) return e;
     sums.n_groups = a.n_groups;
