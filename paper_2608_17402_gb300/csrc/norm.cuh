@@ -134,13 +134,18 @@ __device__ __forceinline__ P8 ld_param(const float* p, int col, bool act, float 
 // ------------------------------------------------------------ 8-bit checkpoints
 
 // The whole number nearest to 127 x / amax, an even one between two, where y, that value in fp32
-// (off by at most 127 * 2^-21), is too near to a border to tell: 254 x and (2 n + 1) amax, both exact
-// in fp64, decide.
-__device__ __noinline__ float q8_border(float x, float y, float amax) {
-    const float n = floorf(y);
-    const double t = 254.0 * (double)x - (2.0 * (double)n + 1.0) * (double)amax;
-    const bool even = ((int)n & 1) == 0;
-    return (t > 0.0 || (t == 0.0 && !even)) ? n + 1.0f : n;
+// (off by at most 127 * 2^-21), is too near to a border to tell.  254 x and (2 n + 1) amax decide, each as a
+// rounded product and what it left out (their operands 2^-8 times the values: no overflow; amax >= 2^-110 and
+// |x| >= amax / 254 leave every bit in range).  The rounded products differ by 2^-11 of themselves at most,
+// so their difference is exact; what they left out are whole multiples of x's last place below 2^17 of it, so
+// is theirs; and a rounded sum of the two has the sign of the sum.
+__device__ __forceinline__ float q8_border(float x, float y, float amax) {
+    const float n = floorf(y), m = fmaf(2.0f, n, 1.0f);
+    const float xs = x * 0x1p-8f, as = amax * 0x1p-8f;
+    const float q = 254.0f * xs, p = m * as;
+    const float t = (q - p) + (fmaf(254.0f, xs, -q) - fmaf(m, as, -p));
+    const bool odd = (int)n & 1;
+    return (t > 0.0f || (t == 0.0f && odd)) ? n + 1.0f : n;
 }
 // the largest of three sizes, and the same but NaN where one of them is
 __device__ __forceinline__ float max_abs(float a, float b, float c) {
