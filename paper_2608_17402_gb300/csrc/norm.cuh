@@ -163,6 +163,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+__device__ __forceinline__ float warp_max_nan(float a) {
+    float r;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(a));
+    return r;
+}
 
 // Codes of this thread's 8 columns (zeros behind a row's end) and the scale of the block of 128 that
 // 16 threads share, all of them here.  A block that holds an infinity or a NaN gets scale NaN; one
@@ -175,8 +180,10 @@ __device__ __forceinline__ uint2 q8_block(const P8& v, float& scale) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) f2_unpack(v.p[i], x[2 * i], x[2 * i + 1]);
     float amax = max_nan(max_abs_nan(max_abs_nan(x[0], x[1], x[2]), x[3], x[4]), max_abs_nan(x[5], x[6], x[7]));
-#pragma unroll
-    for (int o = 8; o; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    // over each half of the warp, all its lanes in both reductions
+    const bool upper = threadIdx.x & 16;
+    const float lo = warp_max_nan(upper ? 0.f : amax), hi = warp_max_nan(upper ? amax : 0.f);
+    amax = upper ? hi : lo;
     if (!(amax >= Q8_LEAST && amax <= 3.402823466e38f)) {
         scale = amax < Q8_LEAST ? 0.f : __uint_as_float(0x7fffffffu);
         return make_uint2(0u, 0u);
