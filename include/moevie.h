@@ -472,9 +472,9 @@ moevie_status moevie_residual_norm_backward(const moevie_norms* n, const void* d
  * neither read nor written.  A logit of minus infinity has no probability; a row of nothing else adds
  * nothing, its ds is zero; a NaN, or plus infinity under a softmax, gives NaN in its row and in loss.  An id
  * outside [0, E) is not counted, and is MOEVIE_ERR_DEVICE in the status, as are runs that do not ascend
- * within [0, T].  fp32 arithmetic; the same call gives the same bits.  1 <= k <= E <= 1024, T k < 2^31, else
- * MOEVIE_ERR_UNSUPPORTED.  T == 0: loss and counts are zeros.  ws: moevie_balance_workspace_size(T_max, E, k,
- * G_max) bytes, set up with moevie_workspace_init. */
+ * within [0, T].  fp32 arithmetic; the same call gives the same bits.  1 <= k <= E <= 1024, T k < 2^31 and
+ * G <= 2^20, else MOEVIE_ERR_UNSUPPORTED.  T == 0: loss and counts are zeros.  ws:
+ * moevie_balance_workspace_size(T_max, E, k, G_max) bytes, set up with moevie_workspace_init. */
 #define MOEVIE_SCORE_SOFTMAX 0
 #define MOEVIE_SCORE_SIGMOID 1
 moevie_status moevie_balance_workspace_size(int64_t T_max, int64_t E, int64_t k, int64_t G, size_t* bytes);

@@ -1132,7 +1132,7 @@ moevie_status moevie_muon_update(float* W, void* W_bf16, float* M, const float* 
 namespace {
 
 constexpr int64_t NORM_MAX_D = 8192;   // one CTA of 1024 threads holds a row
-constexpr int64_t NORM_MAX_RUNS = 1 << 20;   // the grid that adds up their gates' gradients
+constexpr int64_t MAX_RUNS = 1 << 20;   // the grid that adds up their gates' gradients; walks past empty runs
 
 inline bool is_finite(float v) { return fabsf(v) <= 3.402823466e38f; }
 inline bool a4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -1148,7 +1148,7 @@ moevie_status check_norm_sizes(int64_t T, int64_t d, int64_t G) {
     const moevie_status c = check_rows_sizes(T, d);
     if (c != MOEVIE_OK) return c;
     if (G < 1) return MOEVIE_ERR_INVALID_ARG;
-    return d > NORM_MAX_D || G > NORM_MAX_RUNS ? MOEVIE_ERR_UNSUPPORTED : MOEVIE_OK;
+    return d > NORM_MAX_D || G > MAX_RUNS ? MOEVIE_ERR_UNSUPPORTED : MOEVIE_OK;
 }
 
 moevie_status check_norms(const moevie_norms* n, int64_t T) {
@@ -1194,7 +1194,7 @@ moevie_status check_balance(int64_t T, int64_t E, int64_t k, int64_t G) {
     const moevie_status c = check_sizes(T, 8, E, k, 0, 0);
     if (c != MOEVIE_OK) return c;
     if (G < 1) return MOEVIE_ERR_INVALID_ARG;
-    return G >= (int64_t(1) << 31) ? MOEVIE_ERR_UNSUPPORTED : MOEVIE_OK;
+    return G > MAX_RUNS ? MOEVIE_ERR_UNSUPPORTED : MOEVIE_OK;
 }
 
 struct BalanceLayout {

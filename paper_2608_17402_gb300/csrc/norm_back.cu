@@ -147,27 +147,27 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_backward_kernel(const No
         const bool two = i + 1 < run_end;
         P8 dR[ROWS], x1[ROWS], du[ROWS], x2[ROWS];
         float2 st1[ROWS], st2[ROWS];
-            cp_async_wait<1>();
-            __syncwarp();   // the other lanes' copies
+        cp_async_wait<1>();
+        __syncwarp();   // the other lanes' copies
 #pragma unroll
-            for (int k = 0; k < ROWS; ++k) {
-                const uint32_t words = ring.at(slot ^ k, PIECES - 1);
-                if (has_dr) dR[k] = Dr.get(ring, slot ^ k, 0, 0);
-                else dR[k] = p8_of(0.f);
-                if (norm) {
-                    x1[k] = R1.get(ring, slot ^ k, PR + PU, words + scale_word);
-                    du[k] = Du.get(ring, slot ^ k, PR, 0);
-                }
-                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(st1[k].x), "=f"(st1[k].y) : "r"(words) : "memory");
+        for (int k = 0; k < ROWS; ++k) {
+            const uint32_t words = ring.at(slot ^ k, PIECES - 1);
+            if (has_dr) dR[k] = Dr.get(ring, slot ^ k, 0, 0);
+            else dR[k] = p8_of(0.f);
+            if (norm) {
+                x1[k] = R1.get(ring, slot ^ k, PR + PU, words + scale_word);
+                du[k] = Du.get(ring, slot ^ k, PR, 0);
             }
-            __syncwarp();   // read by all lanes
-            copy_first(slot, i, 2);
-            if (two) copy_first(slot ^ 1, i, 3);
-            cp_async_commit();
-            if (!two) {   // i + 1 is not of this run: nothing of it counts here
-                dR[ROWS - 1] = x1[ROWS - 1] = du[ROWS - 1] = p8_of(0.f);
-                st1[ROWS - 1] = make_float2(0.f, 0.f);
-            }
+            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(st1[k].x), "=f"(st1[k].y) : "r"(words) : "memory");
+        }
+        __syncwarp();   // read by all lanes
+        copy_first(slot, i, 2);
+        if (two) copy_first(slot ^ 1, i, 3);
+        cp_async_commit();
+        if (!two) {   // i + 1 is not of this run: nothing of it counts here
+            dR[ROWS - 1] = x1[ROWS - 1] = du[ROWS - 1] = p8_of(0.f);
+            st1[ROWS - 1] = make_float2(0.f, 0.f);
+        }
         if (norm) {
             float s[2 * ROWS];
             const P8 w = w1.get();
@@ -201,24 +201,24 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_backward_kernel(const No
             for (int j = 0; j < 4; ++j) o.p[j] = f2_mul(al, dR[k].p[j]);
             if (act && (k == 0 || two)) st_rows<F32>(a.dr, at + k * d, o);
         }
-            cp_async_wait<1>();
-            __syncwarp();   // the other lanes' words
+        cp_async_wait<1>();
+        __syncwarp();   // the other lanes' words
 #pragma unroll
-            for (int k = 0; k < ROWS; ++k) {
-                const uint32_t words = ring.at(slot ^ k, PIECES - 1) + 8;
-                if (has_f) x2[k] = Fo.get(ring, slot ^ k, 2 * PR + PU, words + scale_word);
-                else x2[k] = p8_of(0.f);
-                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(st2[k].x), "=f"(st2[k].y) : "r"(words) : "memory");
-            }
-            __syncwarp();
-            copy_second(slot, i, 2);
-            if (two) copy_second(slot ^ 1, i, 3);
-            cp_async_commit();
-            if (!two) {
-                x2[ROWS - 1] = p8_of(0.f);
-                st2[ROWS - 1] = make_float2(0.f, 0.f);
-                slot ^= 1;
-            }
+        for (int k = 0; k < ROWS; ++k) {
+            const uint32_t words = ring.at(slot ^ k, PIECES - 1) + 8;
+            if (has_f) x2[k] = Fo.get(ring, slot ^ k, 2 * PR + PU, words + scale_word);
+            else x2[k] = p8_of(0.f);
+            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(st2[k].x), "=f"(st2[k].y) : "r"(words) : "memory");
+        }
+        __syncwarp();
+        copy_second(slot, i, 2);
+        if (two) copy_second(slot ^ 1, i, 3);
+        cp_async_commit();
+        if (!two) {
+            x2[ROWS - 1] = p8_of(0.f);
+            st2[ROWS - 1] = make_float2(0.f, 0.f);
+            slot ^= 1;
+        }
         if (join) {
             const P8 w = cw.get();
             if (post) {

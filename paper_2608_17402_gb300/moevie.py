@@ -616,6 +616,21 @@ def _address(t):
     return None if t is None else t.data_ptr()
 
 
+def _scratch(ws, dev):
+    """The address of a workspace on the current device ``dev``."""
+    if ws.buf.get_device() != dev:
+        raise ValueError(f"ws: expected a workspace on the current device cuda:{dev}, got one on {ws.buf.device}")
+    return ws.buf.data_ptr()
+
+
+def _made(stream, make, *args):
+    """make(*args): results whose memory belongs to the stream that writes them (None: the current one)."""
+    if stream is None:
+        return make(*args)
+    with torch.cuda.stream(stream):
+        return make(*args)
+
+
 class _Held:
     """What a program keeps from call to call: its tensors are checked when they are first used and after every
     assignment to one of its fields (not when a tensor is changed in place by resize_ or set_)."""
@@ -659,7 +674,7 @@ def moevie_checkpoint_store(x, out: Checkpoint | None = None, stream=None) -> Ch
     dev = _device()
     at = _rows(x, (T, d), _RES, dev, "x")
     if out is None:
-        out = Checkpoint.empty(T, d, x.device)
+        out = _made(stream, Checkpoint.empty, T, d, x.device)
     out.check(T, d, dev)
     _call("moevie_checkpoint_store", at, int(x.dtype is _F32), T, d, out.codes.data_ptr(), out.scale.data_ptr(),
           _on(stream, dev))
@@ -672,7 +687,7 @@ def moevie_checkpoint_load(ck: Checkpoint, dtype=torch.bfloat16, out=None, strea
     dev = _device()
     ck.check(T, d, dev)
     if out is None:
-        out = torch.empty((T, d), dtype=dtype, device=ck.codes.device)
+        out = _made(stream, lambda: torch.empty((T, d), dtype=dtype, device=ck.codes.device))
     at = _rows(out, (T, d), _RES, dev, "out")
     _call("moevie_checkpoint_load", ck.codes.data_ptr(), ck.scale.data_ptr(), T, d, at, int(out.dtype is _F32),
           _on(stream, dev))
@@ -791,14 +806,14 @@ def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, o
     (then u = N_pre(r), and r may be a Checkpoint).  ``save``: also the 8-bit checkpoints of r and f.
     ``out``: a ResidualNormOut whose buffers are written (its members say what is wanted; out.r may be r)."""
     dev, d = _device(), norms.d
-    N = norms.c_struct(dev)
+    N, at = norms.c_struct(dev), _scratch(ws, dev)
     T = _matrix(r, d, "r")
     R = _rows_struct(r, T, d, _RES, dev, "r")
     join = f is not None
     F = _rows(f, r.shape, _BF16, dev, "f") if join else None
     dtype = _BF16 if R.type == 2 else r.dtype
     if out is None:
-        out = ResidualNormOut.empty(norms, T, dtype, save, join, ws.buf.device)
+        out = _made(stream, ResidualNormOut.empty, norms, T, dtype, save, join, ws.buf.device)
     out.check(T, d, dtype, join, dev)
     codes = [None] * 4
     for i, ck in ((0, out.save_r), (2, out.save_f)):
@@ -806,7 +821,7 @@ def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, o
             ck.check(T, d, dev)
             codes[i], codes[i + 1] = ck.codes.data_ptr(), ck.scale.data_ptr()
     _call("moevie_residual_norm", ctypes.byref(N), ctypes.byref(R), F, T, out.r.data_ptr() if join else None,
-          _address(out.u), _address(out.stats_pre), _address(out.stats_post), *codes, ws.buf.data_ptr(), ws.nbytes, _on(stream, dev))
+          _address(out.u), _address(out.stats_pre), _address(out.stats_post), *codes, at, ws.nbytes, _on(stream, dev))
     return out
 
 
@@ -854,11 +869,11 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
     them.  f = None without ``out``: the forward ran without f (with it, out.df says so).  Returns dr (may be the
     given one, as out.dr), df bf16 and the gradients of norms' weights, fp32."""
     dev, d = _device(), norms.d
-    N = norms.c_struct(dev)
+    N, at = norms.c_struct(dev), _scratch(ws, dev)
     T = _matrix(dr if dr is not None else du, d, "dr" if dr is not None else "du")
     if out is None:
         dtype = dr.dtype if dr is not None else r.dtype if isinstance(r, torch.Tensor) else _BF16
-        out = ResidualNormGrads.empty(norms, T, dtype, f is not None, ws.buf.device)
+        out = _made(stream, ResidualNormGrads.empty, norms, T, dtype, f is not None, ws.buf.device)
     out.check(T, d, N.G, dev)
     res, shape = out.dr.dtype, (T, d)
     R = ctypes.byref(_rows_struct(r, T, d, res, dev, "r")) if r is not None else None
@@ -872,7 +887,7 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
           int(du is not None and du.dtype is _F32), R, F, s1, s2, T, out.dr.data_ptr(),
           *[None if v is None else v.data_ptr()
             for v in (out.df, out.dw_pre, out.db_pre, out.dw_post, out.db_post, out.dgate)],
-          ws.buf.data_ptr(), ws.nbytes, _on(stream, dev))
+          at, ws.nbytes, _on(stream, dev))
     return out
 
 
@@ -905,7 +920,7 @@ def moevie_router_logits(x, W_r, ws: Workspace, s=None, stream=None):
     if W_r.shape[0] != d:
         raise ValueError(f"W_r: expected [{d}, E], got {tuple(W_r.shape)}")
     if s is None:
-        s = torch.empty((T, E32), dtype=torch.float32, device=x.device)
+        s = _made(stream, lambda: torch.empty((T, E32), dtype=torch.float32, device=x.device))
     elif _want(s, torch.float32, "s").shape != (T, E32):
         raise ValueError(f"s: expected {(T, E32)}, got {tuple(s.shape)}")
     _call("moevie_router_logits", _p(x), _p(W_r), T, d, E, _p(s), ws.ptr, ws.nbytes, _stream(stream))
@@ -951,16 +966,16 @@ def moevie_balance_loss(s, idx, ws: BalanceWorkspace, coef=0.01, score="sigmoid"
     T, E = s.shape
     k = idx.size(1)
     dev = _device()
-    ld = _logits(s, T, E, dev, "s")
+    at, ld = _scratch(ws, dev), _logits(s, T, E, dev, "s")
     ids = _rows(idx, (T, k), _I32, dev, "idx")
     G = 1 if seg is None else seg.numel() - 1
     runs = None if seg is None else _rows(seg, (G + 1,), _I32, dev, "seg")
     if out is None:
-        out = BalanceOut.empty(T, E, G, grad, s.device)
+        out = _made(stream, BalanceOut.empty, T, E, G, grad, s.device)
     out.check(T, E, G, dev)
     ds = out.ds
     _call("moevie_balance_loss", s.data_ptr(), ld, ids, T, E, k, runs, G, _SCORES[score], coef, out.loss.data_ptr(),
-          out.counts.data_ptr(), _address(ds), 0 if ds is None else ds.stride(0) if T > 1 else E, ws.ptr, ws.nbytes,
+          out.counts.data_ptr(), _address(ds), 0 if ds is None else ds.stride(0) if T > 1 else E, at, ws.nbytes,
           _on(stream, dev))
     return out
 

@@ -1,6 +1,7 @@
 """C ABI of the residual norms, the checkpoints and the balance loss, host side: what is refused, before anything is
 launched, and the workspaces' sizes.  No call here launches anything."""
 import ctypes
+import types
 
 import pytest
 
@@ -150,7 +151,7 @@ def test_balance_workspace_serves_fewer_tokens_and_runs(lib, E, k):
     (dict(), WORKSPACE), (dict(s=None), INVALID), (dict(s=FAKE + 2), INVALID), (dict(ld_s=15), INVALID), (dict(idx=None), INVALID),
     (dict(T=-1), INVALID), (dict(E=2000, ld_s=2000, ld_ds=2000), UNSUPPORTED), (dict(k=17), UNSUPPORTED), (dict(k=0), INVALID),
     (dict(T=1 << 30, k=4), UNSUPPORTED), (dict(G=2), INVALID), (dict(G=2, seg=FAKE), WORKSPACE), (dict(G=0), INVALID),
-    (dict(score=2), INVALID), (dict(coef=float("nan")), INVALID), (dict(loss=None), INVALID), (dict(counts=None), INVALID),
+    (dict(G=1 << 20, seg=FAKE), WORKSPACE), (dict(G=(1 << 20) + 1, seg=FAKE), UNSUPPORTED), (dict(score=2), INVALID), (dict(coef=float("nan")), INVALID), (dict(loss=None), INVALID), (dict(counts=None), INVALID),
     (dict(ds=None), WORKSPACE), (dict(ds=None, ld_ds=0), WORKSPACE), (dict(ld_ds=8), INVALID), (dict(ds=FAKE, s=FAKE, ld_ds=20), INVALID),
     (dict(ws=None), INVALID)])
 def test_balance_arguments(lib, change, code):
@@ -198,5 +199,7 @@ def test_refusals_of_the_binding():
         moevie._matrix(torch.zeros(4, 32), n.d, "r")
     with pytest.raises(ValueError):
         moevie._rows(torch.zeros(4, 64), (4, 64), torch.float32, 0, "r")   # not on the device
+    with pytest.raises(ValueError):
+        moevie._scratch(types.SimpleNamespace(buf=torch.zeros(4)), 0)      # nor its workspace
     with pytest.raises(KeyError):
         moevie._KINDS["batch"]

@@ -1,5 +1,7 @@
 """moevie_balance_loss against its formula in 64 bits; the gradient against automatic differentiation with the
 counts held fixed, and against differences."""
+import threading
+
 import pytest
 import torch
 
@@ -236,6 +238,51 @@ def test_same_bits_again_on_a_stream_and_in_a_graph():
         graph.replay()
     torch.cuda.synchronize()
     assert same()
+
+
+def test_calls_of_two_threads_on_two_streams():
+    data = [make(30000, 64, 8, skew=1.0), make(9000, 31, 4, seed=5)]
+    spaces = [moevie.BalanceWorkspace(s.shape[0], s.shape[1], idx.shape[1]) for s, idx in data]
+
+    def go(i, stream, out):
+        for _ in range(20):
+            out[i] = moevie.moevie_balance_loss(*data[i], spaces[i], stream=stream)
+
+    want, got = [None, None], [None, None]
+    for i in range(2):
+        go(i, None, want)
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=go, args=(i, torch.cuda.Stream(), got)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for o, w in zip(got, want):
+        assert torch.equal(o.loss, w.loss) and torch.equal(o.counts, w.counts) and torch.equal(o.ds, w.ds)
+
+
+@pytest.mark.parametrize("E", [64, 31])
+def test_large_offsets(E):
+    """Rows of logits and gradients that lie further apart than 32 bits can count."""
+    T, ld = 5, (1 << 29) + 4 if E % 4 == 0 else (1 << 29) + 1
+    if torch.cuda.mem_get_info()[0] < 30e9:
+        pytest.skip("needs 30 GB")
+    s, idx = make(T, E, 4)
+    out = moevie.BalanceOut.empty(T, E)
+    out.ds = torch.empty(T * ld, device="cuda").view(T, ld)[:, :E]
+    far = torch.empty(T * ld, device="cuda").view(T, ld)[:, :E]
+    far.copy_(s)
+    check(far, idx, out=out)
+
+
+def test_empty_runs_between_tokens():
+    """Thousands of runs, nearly all without a token."""
+    G, T = 5000, 60
+    ends = torch.zeros(G + 1, dtype=torch.int32)
+    ends[1000:], ends[4000:], ends[-1] = 20, 21, T
+    s, idx = make(T, 16, 2)
+    check(s, idx, seg=ends.cuda())
 
 
 def test_loss_and_loads_alone_and_no_tokens():

@@ -1,5 +1,7 @@
 """moevie_residual_norm and its backward against their formulas in 64 bits (the backward's by automatic
 differentiation of the forward's formula), at the widths, runs and types where they can go wrong."""
+import threading
+
 import pytest
 import torch
 
@@ -273,6 +275,29 @@ def test_backward_from_checkpoints(T, d, du, res):
     check_backward(c, du=c.du.to(du), q8=True)
 
 
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("T,d,G,gate", [(130, 1288, 1, True), (40, 2304, 6, True), (9, 8192, 1, False), (500, 72, 40, True)])
+def test_backward_without_a_norm_behind_the_layer(T, d, G, gate, bias, q8):
+    check_backward(Case(T, d, BF, "layer", None, bias, gate, G), q8=q8)
+
+
+@pytest.mark.parametrize("d", [1032, 2056])
+@pytest.mark.parametrize("post", ["rms", None])
+def test_backward_of_wanted_gradients_alone(post, d):
+    """Each gradient wanted by itself has the bits of all wanted together, but for sums formed beside others."""
+    c = Case(70, d, F32, "layer", post, G=3)
+    want = check_backward(c)
+    st = stats64(c.r.double(), "layer").float(), stats64(c.f.double(), post).float() if post else None
+    for name in ("dw_pre", "db_pre", "dgate", *(("dw_post", "db_post") if post else ())):
+        o = moevie.ResidualNormGrads(torch.empty_like(want.dr), torch.empty_like(want.df))
+        setattr(o, name, torch.full_like(getattr(want, name), SENTINEL))
+        moevie.moevie_residual_norm_backward(c.norms, c.dr, c.du, c.r, c.f, *st, c.ws, out=o)
+        assert torch.equal(o.dr, want.dr) and torch.equal(o.df, want.df)
+        assert torch.equal(getattr(o, name), getattr(want, name)), name
+    check_status(c.ws)
+
+
 def test_backward_of_the_first_norm():
     for q8 in (False, True):
         for dr1 in (False, True):
@@ -374,6 +399,35 @@ def test_same_bits_again_on_a_stream_and_in_a_graph():
     check_status(c.ws)
 
 
+def test_calls_of_two_threads_on_two_streams():
+    """Two programs at once, each with its workspace and stream, whose outputs the calls make."""
+    cases = [Case(3000, 1288, BF, G=5), Case(800, 2304, F32, "rms", "layer", seed=1)]
+    stats = [[stats64(t.double(), c.p[n]).float() for t, n in ((c.r, "pre"), (c.f, "post"))] for c in cases]
+
+    def go(i, stream, out):
+        c = cases[i]
+        for _ in range(20):
+            out[i] = (moevie.moevie_residual_norm(c.norms, c.r, c.f, c.ws, save=True, stream=stream),
+                      moevie.moevie_residual_norm_backward(c.norms, c.dr, c.du, c.r, c.f, *stats[i], c.ws, stream=stream))
+
+    want, got = [None, None], [None, None]
+    for i in range(2):
+        go(i, None, want)
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=go, args=(i, torch.cuda.Stream(), got)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for (o, g), (wo, wg) in zip(got, want):
+        assert torch.equal(o.u, wo.u) and torch.equal(o.r, wo.r) and torch.equal(o.save_f.codes, wo.save_f.codes)
+        for name in ("dr", "df", "dw_pre", "dw_post", "dgate"):
+            assert torch.equal(getattr(g, name), getattr(wg, name)), name
+    for c in cases:
+        check_status(c.ws)
+
+
 def test_runs_that_do_not_ascend_are_a_device_error():
     for bad in ([0, 30, 20, 50], [-3, 10, 20, 50], [0, 10, 20, 51]):
         c = Case(50, 264, F32, G=3)
@@ -392,14 +446,13 @@ def test_large_offsets():
     free = torch.cuda.mem_get_info()[0]
     if free < 40e9:
         pytest.skip("needs 40 GB")
-    c = Case(1, d, BF, "rms", "rms", gate=False)
     r = torch.zeros(T, d, dtype=BF, device="cuda")
     f = torch.zeros(T, d, dtype=BF, device="cuda")
     tail = Case(5, d, BF, "rms", "rms", gate=False, seed=3)
     r[-5:], f[-5:] = tail.r, tail.f
     ws = moevie.ResidualNormWorkspace(T, d)
     o = moevie.moevie_residual_norm(tail.norms, r, f, ws, save=True)
-    want = moevie.moevie_residual_norm(tail.norms, tail.r, tail.f, c.ws if T < 2 else tail.ws, save=True)
+    want = moevie.moevie_residual_norm(tail.norms, tail.r, tail.f, tail.ws, save=True)
     assert torch.equal(o.u[-5:], want.u) and torch.equal(o.r[-5:], want.r)
     assert torch.equal(o.save_r.codes[-5:], want.save_r.codes) and torch.equal(o.save_f.scale[-5:], want.save_f.scale)
     back = moevie.moevie_checkpoint_load(o.save_f)
