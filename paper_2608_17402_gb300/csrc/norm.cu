@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(256) q8_load_kernel(const int8_t* codes, const
 // the CTAs of a cluster, as in the backward, its up to four barriers a row cost more: 8192 x 4096 bf16 135 us
 // instead of 70).
 template <bool F32, bool JOIN, bool BOTH, bool SAVE, bool BIG>
-__global__ void __launch_bounds__(BIG ? 1024 : NORM_THREADS, BIG ? 1 : SAVE ? 3 : 2) norm_forward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(BIG ? 1024 : NORM_THREADS, BIG ? 1 : norm_more(F32, SAVE) ? 3 : 2) norm_forward_kernel(const NormArgs a) {
     constexpr int ROWS = BIG ? 1 : mv::ROWS, SLOTS = fwd_slots(F32, BIG), PR = F32 ? 2 : 1, PIECES = PR + (JOIN ? 1 : 0);
     extern __shared__ __align__(16) uint8_t s_dyn[];
     __shared__ __align__(16) float s_part[PART_FLOATS];
@@ -310,7 +310,7 @@ template <bool F32, bool JOIN, bool BOTH, bool SAVE, bool BIG>
 static cudaError_t norm_forward(NormArgs& a, cudaStream_t s) {
     static RowsKernel k;
     return launch_rows<BIG>(norm_forward_kernel<F32, JOIN, BOTH, SAVE, BIG>, k, false,
-                            BIG ? NORM_BIG_THREADS : SAVE ? NORM_SAVE_THREADS : NORM_FWD_THREADS,
+                            BIG ? NORM_BIG_THREADS : norm_more(F32, SAVE) ? NORM_MORE_THREADS : NORM_FWD_THREADS,
                             (BIG ? 1 : 2) * KEPT_BYTES + 16 * fwd_slots(F32, BIG) * ((F32 ? 2 : 1) + (JOIN ? 1 : 0)), s, a);
 }
 template <bool F32, bool JOIN, bool SAVE>

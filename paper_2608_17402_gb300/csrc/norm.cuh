@@ -252,7 +252,8 @@ __device__ __forceinline__ RowGroup row_group(int gw, int ranks, float* s_part) 
         for (int i = g.wi * 32 + g.lane; i < 64; i += gw * 32) g.part[i] = 0.f;
     return g;
 }
-// All of a row's warps, in all CTAs that share it.
+// All of a row's warps, in all CTAs that share it.  (With the barrier's number written out for each group the
+// backward of 65536 x 1664 takes 354 us instead of 341, the forward of 16384 x 2048 bf16 65 instead of 55.)
 template <bool WIDE>
 __device__ __forceinline__ void row_barrier(const RowGroup& g) {
     __syncwarp();
@@ -485,6 +486,8 @@ struct NormPlan {
     int ranks, span, gw, groups, threads, grid;
     int64_t n_groups;   // at most T; the last CTA's groups beyond them have nothing to do
 };
+// Barriers whose number comes from a register count as all 16 that a CTA may have, and an SM has 64.
+constexpr int NORM_CTAS_SM = 4;
 // About `threads_sm` threads to an SM.  shared: rows of more than 2048 columns by clusters, of which at most
 // `clusters` (0: as many as there is room for).
 NormPlan norm_plan(int64_t T, int d, int threads_sm, bool shared, int clusters = 0) {
@@ -492,7 +495,14 @@ NormPlan norm_plan(int64_t T, int d, int threads_sm, bool shared, int clusters =
     p.ranks = shared ? (d + 2047) / 2048 : 1;
     p.span = p.ranks == 1 ? d : ((d + 127) / 128 + p.ranks - 1) / p.ranks * 128;   // whole blocks of a checkpoint
     p.gw = (p.span / 8 + 31) / 32;
-    p.groups = p.ranks > 1 ? 1 : p.gw == 1 ? 8 : p.gw == 2 ? 4 : p.gw <= 4 ? 2 : 1;
+    p.groups = 1;
+    if (p.ranks == 1) {   // of CTAs of up to 8 warps the ones of which an SM holds the most warps, large ones first
+        int most = 0;
+        for (int n = std::max(1, 8 / p.gw); n; --n) {
+            const int rows = std::min(NORM_CTAS_SM, threads_sm / (p.gw * 32 * n)) * n;
+            if (rows > most) most = rows, p.groups = n;
+        }
+    }
     p.threads = p.gw * 32 * p.groups;
     int64_t most = (int64_t)GB300_SMS * std::max(1, threads_sm / p.threads) / p.ranks;
     if (clusters > 0) most = std::min<int64_t>(most, clusters);
@@ -501,9 +511,11 @@ NormPlan norm_plan(int64_t T, int d, int threads_sm, bool shared, int clusters =
     p.n_groups = std::min<int64_t>(T, units * p.groups);
     return p;
 }
-// Threads to an SM.  Forward: 512 with 128 registers each (65536 x 1664 in fp32: 204 us, with 768 of 80 each 228),
-// but 768 where checkpoints are formed as well, which is bound by instructions, not by bytes.
-constexpr int NORM_FWD_THREADS = 512, NORM_SAVE_THREADS = 768, NORM_BIG_THREADS = 1024, NORM_BWD_THREADS = 512;
+// Threads to an SM.  Forward of fp32 rows: 512 with 128 registers each (65536 x 1664: 204 us, with 768 of 80 each
+// 228, bound by memory); 768 where rows are bf16 or checkpoints are formed as well, bound by instructions and
+// their latency (bf16 16384 x 1536: 40 us, with 640 of 96 each 43, with 512 49).
+constexpr int NORM_FWD_THREADS = 512, NORM_MORE_THREADS = 768, NORM_BIG_THREADS = 1024, NORM_BWD_THREADS = 512;
+constexpr bool norm_more(bool f32, bool save) { return save || !f32; }
 constexpr int NORM_MAX_SMEM = 112 * 1024, NORM_BIG_SMEM = 208 * 1024;
 
 // What the first launch of a kernel on a device sets up: its shared memory's limit, and, for one of
