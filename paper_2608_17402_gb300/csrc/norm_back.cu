@@ -68,13 +68,14 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_backward_kernel(const No
     // `on`: rows from the one in hand
     int slot = 0;
     // A row's last piece: the statistics of N_pre (words 0, 1) and, with the second set, of N_post (2, 3), by
-    // lane 0; the scales of the warp's two blocks of r1 (4, 5) and of f (6, 7), by lanes 0 and 1.
+    // lane 0; the scales of the warp's two blocks of r1 (4, 5) and of f (6, 7), by lanes 0 and 1, zeros for a block
+    // behind the row's end (its codes are zeros, but what lay there before may be a NaN).
     const float2 *st1_at = a.stats_pre + t0, *st2_at = a.stats_post + t0;   // of the row in hand
     const int block = first_col / 128 + g.wi * 2 + g.lane;
-    const bool scaled = Q8 && g.lane < 2 && block < a.nb;
+    const int scale_bytes = block < a.nb ? 4 : 0;
     const int64_t scale_at = t0 * a.nb + block;
-    const float* s1_at = Q8 && scaled && a.r_q8 ? a.r1_scale + scale_at : nullptr;
-    const float* s2_at = Q8 && scaled && a.f_q8 ? a.f_scale + scale_at : nullptr;
+    const float* s1_at = Q8 && g.lane < 2 && a.r_q8 ? a.r1_scale + scale_at : nullptr;
+    const float* s2_at = Q8 && g.lane < 2 && a.f_q8 ? a.f_scale + scale_at : nullptr;
     const uint32_t scale_word = (4 + (g.lane >> 4)) * 4;   // r1's; f's two words on
     auto copy_first = [&](int to, int i, int on) {
         const bool live = i + on < n;
@@ -85,14 +86,14 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_backward_kernel(const No
         }
         const uint32_t words = ring.at(to, PIECES - 1);
         if (norm && g.lane == 0) copy8(words, st1_at + on, live ? 8 : 0);
-        if (Q8 && s1_at) copy4(words + 16 + g.lane * 4, s1_at + on * a.nb, live ? 4 : 0);
+        if (Q8 && s1_at) copy4(words + 16 + g.lane * 4, s1_at + on * a.nb, live ? scale_bytes : 0);
     };
     auto copy_second = [&](int to, int i, int on) {
         const bool live = i + on < n;
         if (has_f) Fo.copy(ring, to, 2 * PR + PU, at + on * d, live);
         const uint32_t words = ring.at(to, PIECES - 1);
         if (post && g.lane == 0) copy8(words + 8, st2_at + on, live ? 8 : 0);
-        if (Q8 && s2_at) copy4(words + 24 + g.lane * 4, s2_at + on * a.nb, live ? 4 : 0);
+        if (Q8 && s2_at) copy4(words + 24 + g.lane * 4, s2_at + on * a.nb, live ? scale_bytes : 0);
     };
     copy_first(0, 0, 0);
     copy_first(1, 0, 1);

@@ -298,6 +298,26 @@ def test_backward_of_wanted_gradients_alone(post, d):
     check_status(c.ws)
 
 
+@pytest.mark.parametrize("T,d", [(130, 1288), (300, 72), (40, 2056), (9, 8072)])
+def test_backward_from_checkpoints_after_rows_of_nan(T, d):
+    """Rows that end within a warp's first block of a checkpoint: what an earlier call left on chip does not enter."""
+    bad = Case(4000, 2048, F32, "rms", "rms")
+    for t in (bad.r, bad.f, bad.dr, bad.du):
+        t.fill_(float("nan"))
+    c = Case(T, d, BF)
+    want = check_backward(c, q8=True)
+    r, f = moevie.moevie_checkpoint_store(c.r), moevie.moevie_checkpoint_store(c.f)
+    good = [stats64(t.double(), "layer").float() for t in (c.r, c.f)]
+    st = torch.full((4000, 2), float("nan"), device="cuda")
+    for call in (lambda: moevie.moevie_residual_norm(bad.norms, bad.r, bad.f, bad.ws),
+                 lambda: moevie.moevie_residual_norm_backward(bad.norms, bad.dr, bad.du, bad.r, bad.f, st, st, bad.ws)):
+        got = moevie.ResidualNormGrads.empty(c.norms, T, BF)
+        call()
+        moevie.moevie_residual_norm_backward(c.norms, c.dr, c.du, r, f, *good, c.ws, out=got)
+        for name in ("dr", "df", "dw_pre", "db_pre", "dw_post", "db_post", "dgate"):
+            assert torch.equal(getattr(got, name), getattr(want, name)), name
+
+
 def test_backward_of_the_first_norm():
     for q8 in (False, True):
         for dr1 in (False, True):
