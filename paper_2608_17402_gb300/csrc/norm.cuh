@@ -83,18 +83,25 @@ __device__ __forceinline__ P8 p8_f32(const uint4& a, const uint4& b) {
     r.p[2] = f2_bits(b.x, b.y), r.p[3] = f2_bits(b.z, b.w);
     return r;
 }
-// int8 codes times their scale: a code + 128 as the low byte of 2^23 is a float that is off by 2^23 + 128
-__device__ __forceinline__ P8 p8_codes(uint32_t lo, uint32_t hi, float scale) {
+// int8 codes as fp32: a code + 128 as the low byte of 2^23 is a float that is off by 2^23 + 128
+__device__ __forceinline__ P8 p8_codes(uint32_t lo, uint32_t hi) {
     const uint32_t w[2] = {lo ^ 0x80808080u, hi ^ 0x80808080u};
-    const uint64_t off = f2_of(-8388736.0f), s = f2_of(scale);
+    const uint64_t off = f2_of(-8388736.0f);
     P8 r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t x = w[i / 2];
         const uint64_t v = f2_bits(__byte_perm(x, 0x4b000000u, 0x7540 + 2 * (i & 1)),
                                    __byte_perm(x, 0x4b000000u, 0x7541 + 2 * (i & 1)));
-        r.p[i] = f2_mul(f2_add(v, off), s);
+        r.p[i] = f2_add(v, off);
     }
+    return r;
+}
+__device__ __forceinline__ P8 p8_codes(uint32_t lo, uint32_t hi, float scale) {
+    P8 r = p8_codes(lo, hi);
+    const uint64_t s = f2_of(scale);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.p[i] = f2_mul(r.p[i], s);
     return r;
 }
 // 8 fp32 values in one access, where rows start 32 bytes apart from a multiple of 32
@@ -436,6 +443,13 @@ __device__ __forceinline__ P8 p8_bf16(const ulonglong2& u) {
     return p8_bf16(make_uint4((uint32_t)u.x, (uint32_t)(u.x >> 32), (uint32_t)u.y, (uint32_t)(u.y >> 32)));
 }
 
+// (x - st.x) st.y
+__device__ __forceinline__ void normed(P8& x, float2 st) {
+    const uint64_t m = f2_of(-st.x), q = f2_of(st.y);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.p[j] = f2_mul(f2_add(x.p[j], m), q);
+}
+
 // One operand's rows: whole (F32 or bf16), or, where Q8 allows it and q8 says so, 8-bit codes with
 // their scales (which the callers copy).
 template <bool F32, bool Q8>
@@ -461,14 +475,37 @@ struct Operand {
         }
     }
     template <typename Ring>
+    static __device__ __forceinline__ uint2 codes(const Ring& ring, uint32_t src, uint32_t scale_at, float& s) {
+        uint2 c;
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c.x), "=r"(c.y) : "r"(src + ring.own / 2) : "memory");
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s) : "r"(scale_at) : "memory");
+        return c;
+    }
+    // the row normed, (x - st.x) st.y; of codes in one step, c (scale st.y) - st.x st.y, whose rounding is as nothing
+    // to theirs
+    template <typename Ring>
+    __device__ __forceinline__ P8 normed(const Ring& ring, int slot, int piece, uint32_t scale_at, float2 st) const {
+        P8 x;
+        if (Q8 && q8) {
+            float s;
+            const uint2 c = codes(ring, ring.at(slot, piece), scale_at, s);
+            x = p8_codes(c.x, c.y);
+            const uint64_t m = f2_of(-st.x * st.y), q = f2_of(s * st.y);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.p[j] = f2_fma(x.p[j], q, m);
+        } else {
+            x = get(ring, slot, piece, scale_at);
+            mv::normed(x, st);
+        }
+        return x;
+    }
+    template <typename Ring>
     __device__ __forceinline__ P8 get(const Ring& ring, int slot, int piece, uint32_t scale_at) const {
         const uint32_t src = ring.at(slot, piece);
         if (Q8 && q8) {
-            uint32_t lo, hi;
             float s;
-            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(lo), "=r"(hi) : "r"(src + ring.own / 2) : "memory");
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s) : "r"(scale_at) : "memory");
-            return p8_codes(lo, hi, s);
+            const uint2 c = codes(ring, src, scale_at, s);
+            return p8_codes(c.x, c.y, s);
         }
         if constexpr (F32) {
             const ulonglong2 a = ld_shared(src + ring.lo), b = ld_shared(src + ring.hi);
