@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(256) q8_load_kernel(const int8_t* codes, const
 // the CTAs of a cluster, as in the backward, its up to four barriers a row cost more: 8192 x 4096 bf16 135 us
 // instead of 70).
 template <bool F32, bool JOIN, bool BOTH, bool SAVE, bool BIG>
-__global__ void __launch_bounds__(BIG ? 1024 : NORM_THREADS, BIG ? 1 : norm_more(F32, SAVE) ? 3 : 2) norm_forward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(BIG ? 1024 : NORM_THREADS, BIG ? 1 : norm_more(F32, SAVE) ? 3 : 2)
+norm_forward_kernel(const NormArgs a) {
     constexpr int ROWS = BIG ? 1 : mv::ROWS, SLOTS = fwd_slots(F32, BIG), PR = F32 ? 2 : 1, PIECES = PR + (JOIN ? 1 : 0);
     extern __shared__ __align__(16) uint8_t s_dyn[];
     __shared__ __align__(16) float s_part[PART_FLOATS];

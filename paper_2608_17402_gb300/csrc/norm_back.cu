@@ -30,7 +30,7 @@ struct Sums {
 // Each group of warps leaves its sums in the workspace: dw_pre and db_pre at record gid, A and B
 // of run g at record g + gid (along the rows g and gid never fall, so that no two share one).
 // Bound by HBM where rows are whole: 65536 x 1664 in fp32 342 us, 6.4 TB/s with one gate.  From checkpoints, whose
-// decoding adds a third to the instructions, 8192 x 1280 32 us, 3.9 TB/s (54% of the issue slots at 16 warps an
+// decoding adds a quarter to the instructions, 8192 x 1280 31 us, 4.1 TB/s (54% of the issue slots at 16 warps an
 // SM, all that 128 registers a thread leave).
 // KIND: what the call has, beside r1, du and dr1: both norms (ALL); f's gate alone, or not even that (PLAIN, the
 // layer's output added as it is); or anything (ANY, asked as it goes).  Q8: r1 and f may be checkpoints.
@@ -160,7 +160,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_backward_kernel(const No
             else dR[k] = p8_of(0.f);
             asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(st1[k].x), "=f"(st1[k].y) : "r"(words) : "memory");
             if (norm) {
-                x1[k] = Q8 ? R1.normed(ring, slot ^ k, PR + PU, words + scale_word, st1[k]) : R1.get(ring, slot ^ k, PR + PU, 0);
+                x1[k] = Q8 ? R1.normed(ring, slot ^ k, PR + PU, words + scale_word, st1[k])
+                           : R1.get(ring, slot ^ k, PR + PU, 0);
                 du[k] = Du.get(ring, slot ^ k, PR, 0);
             }
         }
