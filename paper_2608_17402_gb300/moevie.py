@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -590,17 +591,22 @@ _ROW_TYPES = {torch.bfloat16: 0, torch.float32: 1}
 _BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
 _RES = (_BF16, _F32)   # types of a residual stream
 Q8_BLOCK = 128   # columns that share a scale
+# moevie_norms and moevie_rows, packed in a fifth of the time that ctypes takes to fill its structures
+_NORMS, _ROWS = struct.Struct("@qiiPPPPPPqff"), struct.Struct("@PPi4x")
+_NORMS_PACK, _ROWS_PACK = _NORMS.pack, _ROWS.pack
 
 
 def _rows(t, shape, dtype, dev, name):
     """The address of ``t``, a contiguous tensor of this shape and ``dtype`` (one, or a tuple) on the current
     device ``dev``."""
     dt = t.dtype
-    if not ((dt is dtype or (type(dtype) is tuple and dt in dtype)) and t.get_device() == dev and t.shape == shape and
+    if ((dt is dtype or (type(dtype) is tuple and dt in dtype)) and t.get_device() == dev and t.shape == shape and
             t.is_contiguous()):
-        raise ValueError(f"{name}: expected a contiguous tensor {tuple(shape)} of {dtype} on the current device cuda:{dev}, "
-                         f"got {dt} on {t.device} with shape {tuple(t.shape)} and strides {t.stride()}")
-    return t.data_ptr()
+        at = t.data_ptr()
+        if at or not t.numel():   # (memory that its storage has given up has no address)
+            return at
+    raise ValueError(f"{name}: expected a contiguous tensor {tuple(shape)} of {dtype} on the current device cuda:{dev}, "
+                     f"got {dt} on {t.device} with shape {tuple(t.shape)}, strides {t.stride()} and address {t.data_ptr()}")
 
 
 def _device():
@@ -612,8 +618,9 @@ def _on(stream, dev):
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
-def _address(t):
-    return None if t is None else t.data_ptr()
+def _maybe(t, shape, dtype, dev, name):
+    """_rows of a tensor that may be None."""
+    return None if t is None else _rows(t, shape, dtype, dev, name)
 
 
 def _scratch(ws, dev):
@@ -631,22 +638,8 @@ def _made(stream, make, *args):
         return make(*args)
 
 
-class _Held:
-    """What a program keeps from call to call: its tensors are checked when they are first used and after every
-    assignment to one of its fields (not when a tensor is changed in place by resize_ or set_)."""
-
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        object.__setattr__(self, "_checked", None)
-
-    def check(self, *sizes):
-        if self._checked != sizes:
-            self._check(*sizes)
-            object.__setattr__(self, "_checked", sizes)
-
-
 @dataclass
-class Checkpoint(_Held):
+class Checkpoint:
     """Activations [T, d] in 8 bits (moevie_checkpoint_store): int8 codes, and for every row and 128
     columns an fp32 scale."""
     codes: torch.Tensor   # int8 [T, d]
@@ -661,9 +654,9 @@ class Checkpoint(_Held):
     def shape(self):
         return self.codes.shape
 
-    def _check(self, T, d, dev):
-        _rows(self.codes, (T, d), _I8, dev, "checkpoint codes")
-        _rows(self.scale, (T, -(-d // Q8_BLOCK)), _F32, dev, "checkpoint scale")
+    def addresses(self, T, d, dev):
+        return (_rows(self.codes, (T, d), _I8, dev, "checkpoint codes"),
+                _rows(self.scale, (T, -(-d // Q8_BLOCK)), _F32, dev, "checkpoint scale"))
 
 
 def moevie_checkpoint_store(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
@@ -675,9 +668,7 @@ def moevie_checkpoint_store(x, out: Checkpoint | None = None, stream=None) -> Ch
     at = _rows(x, (T, d), _RES, dev, "x")
     if out is None:
         out = _made(stream, Checkpoint.empty, T, d, x.device)
-    out.check(T, d, dev)
-    _call("moevie_checkpoint_store", at, int(x.dtype is _F32), T, d, out.codes.data_ptr(), out.scale.data_ptr(),
-          _on(stream, dev))
+    _call("moevie_checkpoint_store", at, int(x.dtype is _F32), T, d, *out.addresses(T, d, dev), _on(stream, dev))
     return out
 
 
@@ -685,17 +676,16 @@ def moevie_checkpoint_load(ck: Checkpoint, dtype=torch.bfloat16, out=None, strea
     """The values of a checkpoint as bf16 or fp32 [T, d] (``out``'s type where it is given)."""
     T, d = ck.codes.shape
     dev = _device()
-    ck.check(T, d, dev)
+    kept = ck.addresses(T, d, dev)
     if out is None:
         out = _made(stream, lambda: torch.empty((T, d), dtype=dtype, device=ck.codes.device))
     at = _rows(out, (T, d), _RES, dev, "out")
-    _call("moevie_checkpoint_load", ck.codes.data_ptr(), ck.scale.data_ptr(), T, d, at, int(out.dtype is _F32),
-          _on(stream, dev))
+    _call("moevie_checkpoint_load", *kept, T, d, at, int(out.dtype is _F32), _on(stream, dev))
     return out
 
 
 @dataclass
-class ResidualNorm(_Held):
+class ResidualNorm:
     """A block's norms, gate and residual scale (moevie_norms): r1 = residual_scale r + gate * N_post(f),
     u = N_pre(r1).  ``pre`` and ``post``: "rms", "layer" or None.  Weights and biases fp32 [d] (None: 1 and 0);
     gate fp32 [G, d] (None: 1) for the G runs of rows seg[g] to seg[g + 1] (int32 [G + 1]; None: one run of all)."""
@@ -715,24 +705,23 @@ class ResidualNorm(_Held):
     def G(self):
         return 1 if self.seg is None else self.seg.numel() - 1
 
-    def _check(self, dev):
-        d, G = self.d, self.G
-        for name in ("w_pre", "b_pre", "w_post", "b_post"):
-            t = getattr(self, name)
-            if t is not None:
-                _rows(t, (d,), _F32, dev, name)
-        if self.seg is not None:
-            _rows(self.seg, (G + 1,), _I32, dev, "seg")
-        if self.gate is not None:
-            _rows(self.gate, (G, d), _F32, dev, "gate")
-
-    def c_struct(self, dev) -> _Norms:
-        self.check(dev)
-        seg = self.seg
-        return _Norms(self.d, _KINDS[self.pre], _KINDS[self.post],
-                      *[None if v is None else v.data_ptr()
-                        for v in (self.w_pre, self.b_pre, self.w_post, self.b_post, self.gate, seg)],
-                      1 if seg is None else seg.numel() - 1, self.residual_scale, self.eps)
+    def c_struct(self, dev) -> bytes:
+        """A moevie_norms.  Every tensor is checked in every call: a program may give one other memory at any time
+        (`.data = ...`, a module's .to())."""
+        d, seg, gate = self.d, self.seg, self.gate
+        w1, b1, w2, b2 = self.w_pre, self.b_pre, self.w_post, self.b_post
+        G = 1 if seg is None else seg.numel() - 1
+        row = (d,)
+        fields = (d, _KINDS[self.pre], _KINDS[self.post], 0 if w1 is None else _rows(w1, row, _F32, dev, "w_pre"),
+                  0 if b1 is None else _rows(b1, row, _F32, dev, "b_pre"),
+                  0 if w2 is None else _rows(w2, row, _F32, dev, "w_post"),
+                  0 if b2 is None else _rows(b2, row, _F32, dev, "b_post"),
+                  0 if gate is None else _rows(gate, (G, d), _F32, dev, "gate"),
+                  0 if seg is None else _rows(seg, (G + 1,), _I32, dev, "seg"), G, self.residual_scale, self.eps)
+        try:
+            return _NORMS_PACK(*fields)
+        except (struct.error, OverflowError):   # numbers beyond their fields: as ctypes takes them, for the library to refuse
+            return bytes(_Norms(*fields))
 
 
 def moevie_residual_norm_workspace_size(T_max, d, G=1) -> int:
@@ -751,8 +740,11 @@ class ResidualNormWorkspace(Workspace):
         moevie_workspace_init(self, stream)
 
 
+_NOT_KEPT = (None,) * 4
+
+
 @dataclass
-class ResidualNormOut(_Held):
+class ResidualNormOut:
     """What moevie_residual_norm gives; a member that the call has no use for is None."""
     r: torch.Tensor | None            # r1 [T, d], of the residual stream's type
     u: torch.Tensor | None            # bf16 [T, d]
@@ -773,24 +765,24 @@ class ResidualNormOut(_Held):
                    stats(norms.pre), stats(norms.post if join else None),
                    Checkpoint.empty(T, d, device) if save else None, Checkpoint.empty(T, d, device) if save and join else None)
 
-    def _check(self, T, d, dtype, join, dev):
-        if join:
-            if self.r is None:
-                raise ValueError("out.r: missing")
-            _rows(self.r, (T, d), dtype, dev, "out.r")
-        if self.u is not None:
-            _rows(self.u, (T, d), _BF16, dev, "out.u")
-        for name in ("stats_pre", "stats_post"):
-            t = getattr(self, name)
-            if t is not None:
-                _rows(t, (T, 2), _F32, dev, "out." + name)
+    def addresses(self, T, d, dtype, join, dev):
+        if join and self.r is None:
+            raise ValueError("out.r: missing")
+        rows, stats = (T, d), (T, 2)
+        u, s1, s2, kr, kf = self.u, self.stats_pre, self.stats_post, self.save_r, self.save_f
+        kept = _NOT_KEPT if kr is None and kf is None else (
+            *(_NOT_KEPT[:2] if kr is None else kr.addresses(T, d, dev)),
+            *(_NOT_KEPT[2:] if kf is None else kf.addresses(T, d, dev)))
+        return (_rows(self.r, rows, dtype, dev, "out.r") if join else None,
+                None if u is None else _rows(u, rows, _BF16, dev, "out.u"),
+                None if s1 is None else _rows(s1, stats, _F32, dev, "out.stats_pre"),
+                None if s2 is None else _rows(s2, stats, _F32, dev, "out.stats_post"), *kept)
 
 
 def _rows_struct(t, T, d, dtype, dev, name):
     if isinstance(t, Checkpoint):
-        t.check(T, d, dev)
-        return _Rows(t.codes.data_ptr(), t.scale.data_ptr(), 2)
-    return _Rows(_rows(t, (T, d), dtype, dev, name), None, _ROW_TYPES[t.dtype])
+        return _ROWS_PACK(*t.addresses(T, d, dev), 2)
+    return _ROWS_PACK(_rows(t, (T, d), dtype, dev, name), 0, _ROW_TYPES[t.dtype])
 
 
 def _matrix(t, d, name):
@@ -811,22 +803,16 @@ def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, o
     R = _rows_struct(r, T, d, _RES, dev, "r")
     join = f is not None
     F = _rows(f, r.shape, _BF16, dev, "f") if join else None
-    dtype = _BF16 if R.type == 2 else r.dtype
+    dtype = _BF16 if isinstance(r, Checkpoint) else r.dtype
     if out is None:
         out = _made(stream, ResidualNormOut.empty, norms, T, dtype, save, join, ws.buf.device)
-    out.check(T, d, dtype, join, dev)
-    codes = [None] * 4
-    for i, ck in ((0, out.save_r), (2, out.save_f)):
-        if ck is not None:
-            ck.check(T, d, dev)
-            codes[i], codes[i + 1] = ck.codes.data_ptr(), ck.scale.data_ptr()
-    _call("moevie_residual_norm", ctypes.byref(N), ctypes.byref(R), F, T, out.r.data_ptr() if join else None,
-          _address(out.u), _address(out.stats_pre), _address(out.stats_post), *codes, at, ws.nbytes, _on(stream, dev))
+    _call("moevie_residual_norm", N, R, F, T, *out.addresses(T, d, dtype, join, dev), at,
+          ws.nbytes, _on(stream, dev))
     return out
 
 
 @dataclass
-class ResidualNormGrads(_Held):
+class ResidualNormGrads:
     """What moevie_residual_norm_backward gives (None: not wanted)."""
     dr: torch.Tensor
     df: torch.Tensor | None
@@ -848,16 +834,12 @@ class ResidualNormGrads(_Held):
                    *(like(t) for t in ((norms.w_post, norms.b_post) if post else (None, None))),
                    like(norms.gate if join else None))
 
-    def _check(self, T, d, G, dev):
-        _rows(self.dr, (T, d), _RES, dev, "out.dr")
-        if self.df is not None:
-            _rows(self.df, (T, d), _BF16, dev, "out.df")
-        for name in ("dw_pre", "db_pre", "dw_post", "db_post"):
-            t = getattr(self, name)
-            if t is not None:
-                _rows(t, (d,), _F32, dev, "out." + name)
-        if self.dgate is not None:
-            _rows(self.dgate, (G, d), _F32, dev, "out.dgate")
+    def addresses(self, T, d, G, dev):
+        rows, row = (T, d), (d,)
+        return (_rows(self.dr, rows, _RES, dev, "out.dr"), _maybe(self.df, rows, _BF16, dev, "out.df"),
+                _maybe(self.dw_pre, row, _F32, dev, "out.dw_pre"), _maybe(self.db_pre, row, _F32, dev, "out.db_pre"),
+                _maybe(self.dw_post, row, _F32, dev, "out.dw_post"), _maybe(self.db_post, row, _F32, dev, "out.db_post"),
+                _maybe(self.dgate, (G, d), _F32, dev, "out.dgate"))
 
 
 def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, stats_post,
@@ -874,20 +856,15 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
     if out is None:
         dtype = dr.dtype if dr is not None else r.dtype if isinstance(r, torch.Tensor) else _BF16
         out = _made(stream, ResidualNormGrads.empty, norms, T, dtype, f is not None, ws.buf.device)
-    out.check(T, d, N.G, dev)
+    results = out.addresses(T, d, norms.G, dev)
     res, shape = out.dr.dtype, (T, d)
-    R = ctypes.byref(_rows_struct(r, T, d, res, dev, "r")) if r is not None else None
-    F = ctypes.byref(_rows_struct(f, T, d, _BF16, dev, "f")) if f is not None else None
-    dr1 = _rows(dr, shape, res, dev, "dr") if dr is not None else None
-    du1 = _rows(du, shape, _RES, dev, "du") if du is not None else None
+    R = _rows_struct(r, T, d, res, dev, "r") if r is not None else None
+    F = _rows_struct(f, T, d, _BF16, dev, "f") if f is not None else None
+    dr1, du1 = _maybe(dr, shape, res, dev, "dr"), _maybe(du, shape, _RES, dev, "du")
     shape = (T, 2)
-    s1 = _rows(stats_pre, shape, _F32, dev, "stats_pre") if stats_pre is not None else None
-    s2 = _rows(stats_post, shape, _F32, dev, "stats_post") if stats_post is not None else None
-    _call("moevie_residual_norm_backward", ctypes.byref(N), dr1, int(res is _F32), du1,
-          int(du is not None and du.dtype is _F32), R, F, s1, s2, T, out.dr.data_ptr(),
-          *[None if v is None else v.data_ptr()
-            for v in (out.df, out.dw_pre, out.db_pre, out.dw_post, out.db_post, out.dgate)],
-          at, ws.nbytes, _on(stream, dev))
+    s1, s2 = _maybe(stats_pre, shape, _F32, dev, "stats_pre"), _maybe(stats_post, shape, _F32, dev, "stats_post")
+    _call("moevie_residual_norm_backward", N, dr1, int(res is _F32), du1,
+          int(du is not None and du.dtype is _F32), R, F, s1, s2, T, *results, at, ws.nbytes, _on(stream, dev))
     return out
 
 
@@ -928,7 +905,7 @@ def moevie_router_logits(x, W_r, ws: Workspace, s=None, stream=None):
 
 
 @dataclass
-class BalanceOut(_Held):
+class BalanceOut:
     """What moevie_balance_loss gives."""
     loss: torch.Tensor            # fp32 [1]
     counts: torch.Tensor          # int32 [G, E]
@@ -940,20 +917,22 @@ class BalanceOut(_Held):
                    torch.empty((G, E), dtype=torch.int32, device=device),
                    torch.empty((T, E), dtype=torch.float32, device=device) if grad else None)
 
-    def _check(self, T, E, G, dev):
-        _rows(self.loss, (1,), _F32, dev, "out.loss")
-        _rows(self.counts, (G, E), _I32, dev, "out.counts")
-        if self.ds is not None:
-            _logits(self.ds, T, E, dev, "out.ds")
+    def addresses(self, T, E, G, dev):
+        """Of loss, counts and ds, and the stride of ds."""
+        ds = self.ds
+        ld = 0 if ds is None else _logits(ds, T, E, dev, "out.ds")
+        return (_rows(self.loss, (1,), _F32, dev, "out.loss"), _rows(self.counts, (G, E), _I32, dev, "out.counts"),
+                None if ds is None else ds.data_ptr(), ld)
 
 
 def _logits(t, T, E, dev, name):
     """The row stride of an fp32 tensor [T, E] with consecutive columns on the current device."""
-    if not (t.dtype is _F32 and t.get_device() == dev and t.dim() == 2 and t.size(0) == T and t.size(1) == E and
-            (E == 1 or t.stride(1) == 1) and (T <= 1 or t.stride(0) >= E)):
-        raise ValueError(f"{name}: expected an fp32 tensor [{T}, {E}] with consecutive columns on the current device "
-                         f"cuda:{dev}, got {t.dtype} on {t.device} with shape {tuple(t.shape)} and strides {t.stride()}")
-    return t.stride(0) if T > 1 else E
+    if t.dtype is _F32 and t.get_device() == dev and t.shape == (T, E):
+        ld, step = t.stride()
+        if (E == 1 or step == 1) and (T <= 1 or ld >= E) and (T == 0 or t.data_ptr()):
+            return ld if T > 1 else E
+    raise ValueError(f"{name}: expected an fp32 tensor [{T}, {E}] with consecutive columns on the current device cuda:{dev}, "
+                     f"got {t.dtype} on {t.device} with shape {tuple(t.shape)}, strides {t.stride()} and address {t.data_ptr()}")
 
 
 def moevie_balance_loss(s, idx, ws: BalanceWorkspace, coef=0.01, score="sigmoid", seg=None,
@@ -972,11 +951,8 @@ def moevie_balance_loss(s, idx, ws: BalanceWorkspace, coef=0.01, score="sigmoid"
     runs = None if seg is None else _rows(seg, (G + 1,), _I32, dev, "seg")
     if out is None:
         out = _made(stream, BalanceOut.empty, T, E, G, grad, s.device)
-    out.check(T, E, G, dev)
-    ds = out.ds
-    _call("moevie_balance_loss", s.data_ptr(), ld, ids, T, E, k, runs, G, _SCORES[score], coef, out.loss.data_ptr(),
-          out.counts.data_ptr(), _address(ds), 0 if ds is None else ds.stride(0) if T > 1 else E, at, ws.nbytes,
-          _on(stream, dev))
+    _call("moevie_balance_loss", s.data_ptr(), ld, ids, T, E, k, runs, G, _SCORES[score], coef,
+          *out.addresses(T, E, G, dev), at, ws.nbytes, _on(stream, dev))
     return out
 
 
