@@ -638,6 +638,12 @@ def _made(stream, make, *args):
         return make(*args)
 
 
+def _new(seg):
+    """How a call makes its buffers: the kernels leave rows outside the runs as they are, and what comes next (the
+    layer and its backward) reads every row."""
+    return torch.empty if seg is None else torch.zeros
+
+
 @dataclass
 class Checkpoint:
     """Activations [T, d] in 8 bits (moevie_checkpoint_store): int8 codes, and for every row and 128
@@ -646,9 +652,9 @@ class Checkpoint:
     scale: torch.Tensor   # fp32 [T, ceil(d / 128)]
 
     @classmethod
-    def empty(cls, T, d, device="cuda"):
-        return cls(torch.empty((T, d), dtype=torch.int8, device=device),
-                   torch.empty((T, -(-d // Q8_BLOCK)), dtype=torch.float32, device=device))
+    def empty(cls, T, d, device="cuda", new=torch.empty):
+        return cls(new((T, d), dtype=torch.int8, device=device),
+                   new((T, -(-d // Q8_BLOCK)), dtype=torch.float32, device=device))
 
     @property
     def shape(self):
@@ -754,16 +760,18 @@ class ResidualNormOut:
     save_f: Checkpoint | None = None
 
     @classmethod
-    def empty(cls, norms: ResidualNorm, T, dtype=torch.bfloat16, save=False, join=True, device="cuda"):
+    def empty(cls, norms: ResidualNorm, T, dtype=torch.bfloat16, save=False, join=True, device="cuda", new=torch.empty):
+        """Buffers for T rows; rows outside norms' runs stay as ``new`` (torch.empty or torch.zeros) makes them."""
         d = norms.d
 
         def stats(kind):
-            return torch.empty((T, 2), dtype=torch.float32, device=device) if kind else None
+            return new((T, 2), dtype=torch.float32, device=device) if kind else None
 
-        return cls(torch.empty((T, d), dtype=dtype, device=device) if join else None,
-                   torch.empty((T, d), dtype=torch.bfloat16, device=device) if norms.pre else None,
+        return cls(new((T, d), dtype=dtype, device=device) if join else None,
+                   new((T, d), dtype=torch.bfloat16, device=device) if norms.pre else None,
                    stats(norms.pre), stats(norms.post if join else None),
-                   Checkpoint.empty(T, d, device) if save else None, Checkpoint.empty(T, d, device) if save and join else None)
+                   Checkpoint.empty(T, d, device, new) if save else None,
+                   Checkpoint.empty(T, d, device, new) if save and join else None)
 
     def addresses(self, T, d, dtype, join, dev):
         if join and self.r is None:
@@ -796,7 +804,8 @@ def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, o
                          save=False, stream=None) -> ResidualNormOut:
     """r1 = residual_scale r + gate * N_post(f), u = N_pre(r1); r bf16 or fp32 [T, d], f bf16 [T, d] or None
     (then u = N_pre(r), and r may be a Checkpoint).  ``save``: also the 8-bit checkpoints of r and f.
-    ``out``: a ResidualNormOut whose buffers are written (its members say what is wanted; out.r may be r)."""
+    ``out``: a ResidualNormOut whose buffers are written (its members say what is wanted; out.r may be r), but for
+    rows outside norms' runs, which stay as they are; in buffers that the call makes they are zeros."""
     dev, d = _device(), norms.d
     N, at = norms.c_struct(dev), _scratch(ws, dev)
     T = _matrix(r, d, "r")
@@ -805,7 +814,7 @@ def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, o
     F = _rows(f, r.shape, _BF16, dev, "f") if join else None
     dtype = _BF16 if isinstance(r, Checkpoint) else r.dtype
     if out is None:
-        out = _made(stream, ResidualNormOut.empty, norms, T, dtype, save, join, ws.buf.device)
+        out = _made(stream, ResidualNormOut.empty, norms, T, dtype, save, join, ws.buf.device, _new(norms.seg))
     _call("moevie_residual_norm", N, R, F, T, *out.addresses(T, d, dtype, join, dev), at,
           ws.nbytes, _on(stream, dev))
     return out
@@ -823,13 +832,14 @@ class ResidualNormGrads:
     dgate: torch.Tensor | None = None
 
     @classmethod
-    def empty(cls, norms: ResidualNorm, T, dtype=torch.bfloat16, join=True, device="cuda"):
+    def empty(cls, norms: ResidualNorm, T, dtype=torch.bfloat16, join=True, device="cuda", new=torch.empty):
+        """Buffers for T rows; rows of dr and df outside norms' runs stay as ``new`` makes them."""
         def like(t):
             return None if t is None else torch.empty_like(t)
 
         post = join and norms.post
-        return cls(torch.empty((T, norms.d), dtype=dtype, device=device),
-                   torch.empty((T, norms.d), dtype=torch.bfloat16, device=device) if join else None,
+        return cls(new((T, norms.d), dtype=dtype, device=device),
+                   new((T, norms.d), dtype=torch.bfloat16, device=device) if join else None,
                    *(like(t) for t in ((norms.w_pre, norms.b_pre) if norms.pre else (None, None))),
                    *(like(t) for t in ((norms.w_post, norms.b_post) if post else (None, None))),
                    like(norms.gate if join else None))
@@ -849,13 +859,14 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
     residual stream's type (None: zero); du: the gradient of u, fp32 (dx of moevie_moe_backward) or bf16 (None
     where norms.pre is None); r (r1) and f: the forward's rows or their Checkpoints; stats as the forward gave
     them.  f = None without ``out``: the forward ran without f (with it, out.df says so).  Returns dr (may be the
-    given one, as out.dr), df bf16 and the gradients of norms' weights, fp32."""
+    given one, as out.dr), df bf16 and the gradients of norms' weights, fp32.  Rows of dr and df outside norms' runs
+    stay as they are in ``out``, and are zeros in buffers that the call makes."""
     dev, d = _device(), norms.d
     N, at = norms.c_struct(dev), _scratch(ws, dev)
     T = _matrix(dr if dr is not None else du, d, "dr" if dr is not None else "du")
     if out is None:
         dtype = dr.dtype if dr is not None else r.dtype if isinstance(r, torch.Tensor) else _BF16
-        out = _made(stream, ResidualNormGrads.empty, norms, T, dtype, f is not None, ws.buf.device)
+        out = _made(stream, ResidualNormGrads.empty, norms, T, dtype, f is not None, ws.buf.device, _new(norms.seg))
     results = out.addresses(T, d, norms.G, dev)
     res, shape = out.dr.dtype, (T, d)
     R = _rows_struct(r, T, d, res, dev, "r") if r is not None else None
@@ -912,10 +923,11 @@ class BalanceOut:
     ds: torch.Tensor | None       # fp32 [T, E], the gradient of the logits (None: not wanted)
 
     @classmethod
-    def empty(cls, T, E, G=1, grad=True, device="cuda"):
+    def empty(cls, T, E, G=1, grad=True, device="cuda", new=torch.empty):
+        """Buffers for T tokens; rows of ds outside the runs stay as ``new`` makes them."""
         return cls(torch.empty(1, dtype=torch.float32, device=device),
                    torch.empty((G, E), dtype=torch.int32, device=device),
-                   torch.empty((T, E), dtype=torch.float32, device=device) if grad else None)
+                   new((T, E), dtype=torch.float32, device=device) if grad else None)
 
     def addresses(self, T, E, G, dev):
         """Of loss, counts and ds, and the stride of ds."""
@@ -939,7 +951,8 @@ def moevie_balance_loss(s, idx, ws: BalanceWorkspace, coef=0.01, score="sigmoid"
                         out: BalanceOut | None = None, grad=True, stream=None) -> BalanceOut:
     """The auxiliary loss of expert loads over every run of tokens (seg int32 [G + 1]; None: one run), from the
     router's logits s fp32 [T, E] and the selection idx int32 [T, k], with the loads (counts) and ds, the gradient
-    of s.  ``score``: "sigmoid" (the layer's, divided by their sum) or "softmax"."""
+    of s.  ``score``: "sigmoid" (the layer's, divided by their sum) or "softmax".  Rows of ds outside the runs stay as
+    they are in ``out``, and are zeros in a buffer that the call makes."""
     if s.dim() != 2 or idx.dim() != 2:
         raise ValueError(f"expected s [T, E] and idx [T, k], got {tuple(s.shape)} and {tuple(idx.shape)}")
     T, E = s.shape
@@ -950,7 +963,7 @@ def moevie_balance_loss(s, idx, ws: BalanceWorkspace, coef=0.01, score="sigmoid"
     G = 1 if seg is None else seg.numel() - 1
     runs = None if seg is None else _rows(seg, (G + 1,), _I32, dev, "seg")
     if out is None:
-        out = _made(stream, BalanceOut.empty, T, E, G, grad, s.device)
+        out = _made(stream, BalanceOut.empty, T, E, G, grad, s.device, _new(seg))
     _call("moevie_balance_loss", s.data_ptr(), ld, ids, T, E, k, runs, G, _SCORES[score], coef,
           *out.addresses(T, E, G, dev), at, ws.nbytes, _on(stream, dev))
     return out

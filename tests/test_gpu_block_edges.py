@@ -1,0 +1,99 @@
+"""The block's steps where memory that nothing wrote would show: padding in buffers that the calls make themselves.  Fresh memory is filled with NaN here (with the largest whole number
+for integer types), as torch does on request."""
+import contextlib
+
+import pytest
+import torch
+
+import workloads
+from paper_2608_17402_gb300 import moevie
+from tests._gpu import check_status, layer_to_device
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@contextlib.contextmanager
+def fresh_memory_is_nan():
+    was = torch.are_deterministic_algorithms_enabled()
+    torch.use_deterministic_algorithms(True)
+    try:
+        assert torch.utils.deterministic.fill_uninitialized_memory
+        yield
+    finally:
+        torch.use_deterministic_algorithms(was)
+
+
+def _layer(T, d, E, k, h, **kw):
+    lay = workloads.make_layer(workloads.small_config(T, d, E, k, h, seed=T + d, **kw))
+    return layer_to_device(lay)[1]
+
+
+def _steps(W, seg, r, dr, du, n0, n1, k):
+    """The first norm, the layer, its balance loss, the join behind it, and all of it back, on buffers that the calls
+    make."""
+    T, d = r.shape
+    E, h = W.W_r.shape[1], W.W2.shape[1]
+    G = seg.numel() - 1
+    norms = [moevie.ResidualNorm(d, seg=seg, **p) for p in (n0, n1)]
+    fwd, bwd = moevie.Workspace(T, d, E, k, h), moevie.BackwardWorkspace(T, d, E, k, h)
+    nws, bws = moevie.ResidualNormWorkspace(T, d, G), moevie.BalanceWorkspace(T, E, k, G)
+    with fresh_memory_is_nan():
+        first = moevie.moevie_residual_norm(norms[0], r, None, nws, save=True)
+        f, rt = moevie.moevie_moe_forward(W, first.u, fwd, routing=True)
+        s = moevie.moevie_router_logits(first.u, W.W_r, fwd)
+        bal = moevie.moevie_balance_loss(s, rt["idx"], bws, 5.0, seg=seg)
+        second = moevie.moevie_residual_norm(norms[1], r, f, nws, save=True)
+        g1 = moevie.moevie_residual_norm_backward(norms[1], dr, du, second.r, second.save_f, second.stats_pre,
+                                                  second.stats_post, nws)
+        gl = moevie.moevie_moe_backward(W, first.u, g1.df, rt["idx"], bwd, ds=bal.ds)
+        g0 = moevie.moevie_residual_norm_backward(norms[0], g1.dr, gl["dx"], first.save_r, None, first.stats_pre, None, nws)
+    for ws in (fwd, bwd, nws, bws):
+        check_status(ws)
+    rows = {"u0": first.u, "r1": second.r, "u1": second.u, "dr1": g1.dr, "df": g1.df, "ds": bal.ds, "dr0": g0.dr,
+            "dx": gl["dx"]}
+    for n, ck in (("r0", first.save_r), ("r", second.save_r), ("f", second.save_f)):
+        rows["codes " + n], rows["scale " + n] = ck.codes, ck.scale
+        rows["kept " + n] = moevie.moevie_checkpoint_load(ck, F32)
+    for n, o in (("0", first), ("1", second)):
+        rows |= {m + n: getattr(o, m) for m in ("stats_pre", "stats_post") if getattr(o, m) is not None}
+    sums = {"loss": bal.loss, "counts": bal.counts, **{n: gl[n] for n in gl if n != "dx"},
+            **{n + "0": getattr(g0, n) for n in ("dw_pre", "db_pre")},
+            **{n + "1": getattr(g1, n) for n in ("dw_pre", "dw_post", "db_post", "dgate")}}
+    return rows, sums
+
+
+@pytest.mark.parametrize("res", [BF, F32])
+@pytest.mark.parametrize("front,behind", [(0, 21), (5, 0), (7, 40), (300, 300)])
+def test_padding_through_the_layer_on_the_calls_own_buffers(front, behind, res):
+    """Rows of padding, which hold NaN in every input, do not change what the others give, and are zeros in everything
+    that the calls make: the same steps without the padding give the same, up to the order of fp32 sums over 300 rows
+    (each term's share of 300 * 2^-24 < 2e-5; the sums of their sizes are some 20 times the results in the norm)."""
+    n, d, E, k, h, G = 300, 136, 8, 2, 64, 3
+    T = front + n + behind
+    W = _layer(n, d, E, k, h)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(front + behind)
+
+    def normal(*shape, std=1.0):
+        return torch.randn(*shape, generator=g, device="cuda") * std
+
+    n0 = dict(pre="layer", w_pre=1 + normal(d, std=0.2), b_pre=normal(d, std=0.1))
+    n1 = dict(pre="rms", post="layer", w_pre=1 + normal(d, std=0.2), w_post=1 + normal(d, std=0.2),
+              b_post=normal(d, std=0.1), gate=normal(G, d, std=0.5), residual_scale=0.75)
+    ends = torch.tensor([0, 77, 77, n], dtype=torch.int32, device="cuda")
+    inputs = [normal(n, d).to(res), normal(n, d, std=1e-2).to(res), normal(n, d, std=1e-2)]
+    padded = [torch.full((T, d), float("nan"), dtype=t.dtype, device="cuda") for t in inputs]
+    for t, p in zip(inputs, padded):
+        p[front:front + n] = t
+    want_rows, want = _steps(W, ends, *inputs, n0, n1, k)
+    got_rows, got = _steps(W, ends + front, *padded, n0, n1, k)
+    for name, t in got_rows.items():
+        outside = torch.cat([t[:front], t[front + n:]]).float()
+        assert not bool(outside.any()), f"{name}: padding holds something"
+    for name in ("u0", "r1", "u1", "codes r0", "codes r", "scale r0", "scale r", "stats_pre0"):
+        assert torch.equal(got_rows[name][front:front + n], want_rows[name]), name
+    assert torch.equal(got["counts"], want["counts"])
+    for name, t in want.items():
+        err = float((got[name].double() - t.double()).norm())
+        assert err <= 1e-3 * float(t.double().norm()), (name, err)
