@@ -452,7 +452,8 @@ moevie_status moevie_residual_norm(const moevie_norms* n, const moevie_rows* r, 
  *   are then NULL, and dr = dR.  f may be NULL where post == MOEVIE_NORM_NONE and dgate is not wanted.
  * Sums over rows are fp32, in an order that goes by T, d and the runs alone: the same call gives
  * the same bits.  Rows outside every run do not enter them; a run without rows gets a zero dgate.
- * T == 0 launches nothing.  ws as for moevie_residual_norm. */
+ * T == 0 launches nothing: the gradients, zeros then, are not written (the Python binding clears them).  ws
+ * as for moevie_residual_norm. */
 moevie_status moevie_residual_norm_backward(const moevie_norms* n, const void* dr1, int res_f32, const void* du,
                                             int du_f32, const moevie_rows* r1, const moevie_rows* f,
                                             const float* stats_pre, const float* stats_post, int64_t T, void* dr,

@@ -638,6 +638,13 @@ def _made(stream, make, *args):
         return make(*args)
 
 
+def _clear(stream, *tensors):
+    with torch.cuda.stream(stream):   # (None: the current one)
+        for t in tensors:
+            if t is not None:
+                t.zero_()
+
+
 def _new(seg):
     """How a call makes its buffers: the kernels leave rows outside the runs as they are, and what comes next (the
     layer and its backward) reads every row."""
@@ -860,7 +867,8 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
     where norms.pre is None); r (r1) and f: the forward's rows or their Checkpoints; stats as the forward gave
     them.  f = None without ``out``: the forward ran without f (with it, out.df says so).  Returns dr (may be the
     given one, as out.dr), df bf16 and the gradients of norms' weights, fp32.  Rows of dr and df outside norms' runs
-    stay as they are in ``out``, and are zeros in buffers that the call makes."""
+    stay as they are in ``out``, and are zeros in buffers that the call makes.  Without rows the weights' gradients
+    are zeros."""
     dev, d = _device(), norms.d
     N, at = norms.c_struct(dev), _scratch(ws, dev)
     T = _matrix(dr if dr is not None else du, d, "dr" if dr is not None else "du")
@@ -876,6 +884,8 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
     s1, s2 = _maybe(stats_pre, shape, _F32, dev, "stats_pre"), _maybe(stats_post, shape, _F32, dev, "stats_post")
     _call("moevie_residual_norm_backward", N, dr1, int(res is _F32), du1,
           int(du is not None and du.dtype is _F32), R, F, s1, s2, T, *results, at, ws.nbytes, _on(stream, dev))
+    if T == 0:   # nothing was launched: sums over no rows
+        _clear(stream, out.dw_pre, out.db_pre, out.dw_post, out.db_post, out.dgate)
     return out
 
 

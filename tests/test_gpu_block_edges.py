@@ -1,5 +1,6 @@
-"""The block's steps where memory that nothing wrote would show: padding in buffers that the calls make themselves.  Fresh memory is filled with NaN here (with the largest whole number
-for integer types), as torch does on request."""
+"""The block's steps where memory that nothing wrote would show: padding in buffers that the calls make themselves, and
+calls without rows.  Fresh memory is filled with NaN here (with the largest whole number for integer types), as torch
+does on request."""
 import contextlib
 
 import pytest
@@ -97,3 +98,28 @@ def test_padding_through_the_layer_on_the_calls_own_buffers(front, behind, res):
     for name, t in want.items():
         err = float((got[name].double() - t.double()).norm())
         assert err <= 1e-3 * float(t.double().norm()), (name, err)
+
+
+def test_without_rows_the_weights_gradients_are_zeros():
+    d, G = 264, 3
+    w = {n: torch.ones(d, device="cuda") for n in ("w_pre", "b_pre", "w_post", "b_post")}
+    norms = moevie.ResidualNorm(d, "layer", "rms", gate=torch.ones(G, d, device="cuda"),
+                                seg=torch.zeros(G + 1, dtype=torch.int32, device="cuda"), **w)
+    ws = moevie.ResidualNormWorkspace(0, d, G)
+    rows, stats = torch.empty(0, d, device="cuda"), torch.empty(0, 2, device="cuda")
+    for stream in (None, torch.cuda.Stream()):
+        with fresh_memory_is_nan():
+            g = moevie.moevie_residual_norm_backward(norms, rows, rows, rows, rows.to(BF), stats, stats, ws, stream=stream)
+        torch.cuda.synchronize()
+        assert g.dr.shape == g.df.shape == (0, d)
+        for name in ("dw_pre", "db_pre", "dw_post", "db_post", "dgate"):
+            assert not bool(getattr(g, name).any()), name
+        # and into buffers of the caller's
+        for name in ("dw_pre", "db_pre", "dw_post", "db_post", "dgate"):
+            getattr(g, name).fill_(3.0)
+        torch.cuda.synchronize()
+        moevie.moevie_residual_norm_backward(norms, rows, rows, rows, rows.to(BF), stats, stats, ws, out=g, stream=stream)
+        torch.cuda.synchronize()
+        for name in ("dw_pre", "db_pre", "dw_post", "db_post", "dgate"):
+            assert not bool(getattr(g, name).any()), name
+    check_status(ws)
