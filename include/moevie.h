@@ -283,7 +283,8 @@ int64_t moevie_shared_groups(int64_t T, int64_t d, int64_t E, int64_t k, int64_t
  * 65535 (h_s too), plus the limits of moevie_moe_forward.  `ws`:
  * moevie_backward_workspace_size(T_max, d, E, k, h, h_s, swiglu) bytes (swiglu nonzero for
  * SwiGLU experts), set up with moevie_workspace_init; device errors land in its status
- * block. */
+ * block.  T == 0 launches nothing: the weights' gradients, zeros then, are not written (the Python
+ * binding clears them). */
 moevie_status moevie_backward_workspace_size(int64_t T_max, int64_t d, int64_t E, int64_t k, int64_t h,
                                              int64_t h_s, int swiglu, size_t* bytes);
 moevie_status moevie_moe_backward(const moevie_layer* layer, const void* x, const void* dy, int64_t T,

@@ -428,7 +428,7 @@ def moevie_moe_backward(layer: LayerWeights, x, dy, idx, ws: "BackwardWorkspace"
     dW1) for SwiGLU experts, and with a shared expert dWs1 [d, h_s] (a view of rows
     row_ld(h_s) apart), dWs2 [h_s, d] and, for SwiGLU, dWs3 (as dWs1).  ``ds`` fp32 [T, E]: another
     gradient of the router's logits (moevie_balance_loss), which dx and dW_r then take too
-    (moevie_moe_backward_balanced)."""
+    (moevie_moe_backward_balanced).  Without tokens the weights' gradients are zeros."""
     _want(x, torch.bfloat16, "x")
     _want(dy, torch.bfloat16, "dy")
     _want(idx, torch.int32, "idx")
@@ -453,6 +453,8 @@ def moevie_moe_backward(layer: LayerWeights, x, dy, idx, ws: "BackwardWorkspace"
     _call(name, ctypes.byref(L), _p(x), _p(dy), T, _p(idx), *extra, _p(out["dx"]), _p(out["dW_r"]), _p(out["dW1"]),
           _p(out["dW2"]), _p(out.get("dW3")), _p(out.get("dWs1")), _p(out.get("dWs2")), _p(out.get("dWs3")), ws.ptr,
           ws.nbytes, _stream(stream))
+    if T == 0:   # nothing was launched: sums over no tokens
+        _clear(stream, *out.values())
     out["dW1"] = out["dW1"][..., :h]
     for name, w in (("dW3", h), ("dWs1", hs), ("dWs3", hs)):
         if name in out:

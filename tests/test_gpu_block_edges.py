@@ -123,3 +123,18 @@ def test_without_rows_the_weights_gradients_are_zeros():
         for name in ("dw_pre", "db_pre", "dw_post", "db_post", "dgate"):
             assert not bool(getattr(g, name).any()), name
     check_status(ws)
+
+
+@pytest.mark.parametrize("act,h_s", [("gelu", 0), ("swiglu", 64)])
+def test_without_tokens_the_layers_gradients_are_zeros(act, h_s):
+    d, E, k, h = 64, 8, 2, 40
+    W = _layer(4, d, E, k, h, act=act, h_s=h_s)
+    ws = moevie.BackwardWorkspace(4, d, E, k, h, h_s=h_s, swiglu=act == "swiglu")
+    x = torch.empty(0, d, dtype=BF, device="cuda")
+    idx = torch.empty(0, k, dtype=torch.int32, device="cuda")
+    for ds in (None, torch.empty(0, E, device="cuda")):
+        with fresh_memory_is_nan():
+            g = moevie.moevie_moe_backward(W, x, x, idx, ws, ds=ds)
+        for name, t in g.items():
+            assert not bool(t.any()), name
+    check_status(ws)
