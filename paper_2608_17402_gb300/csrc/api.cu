@@ -418,7 +418,7 @@ moevie_status route_impl(const void* x, const float* W_r, const float* b, int64_
     } else {    // B [2][dp][Ep]: K = 2 dp, x read twice, once per piece
         g.a_kperiod = (int)dp;
         g.K = (int)(2 * dp);
-        g.N = (int)E;
+        g.N = logits_only ? Ep : (int)E;   // handed out with the columns behind E, whose weights are zeros
         g.N_ld = Ep;
         g.epi = EPI_STORE_F32;
     }

@@ -1,6 +1,6 @@
-"""The block's steps where memory that nothing wrote would show: padding in buffers that the calls make themselves, and
-calls without rows.  Fresh memory is filled with NaN here (with the largest whole number for integer types), as torch
-does on request."""
+"""The block's steps where memory that nothing wrote would show: padding in buffers that the calls make themselves, calls
+without rows, the columns between rows of logits.  Fresh memory is filled with NaN here (with the largest whole number
+for integer types), as torch does on request."""
 import contextlib
 
 import pytest
@@ -138,3 +138,24 @@ def test_without_tokens_the_layers_gradients_are_zeros(act, h_s):
         for name, t in g.items():
             assert not bool(t.any()), name
     check_status(ws)
+
+
+@pytest.mark.parametrize("T,d,E", [(1, 8, 1), (70, 64, 33), (300, 512, 100), (70, 64, 129), (300, 512, 129), (1000, 64, 200),
+                                   (1000, 1024, 200), (33, 768, 510), (64, 64, 1000), (500, 1536, 1000), (3, 264, 1021)])
+def test_columns_between_rows_of_logits_are_zeros(T, d, E):
+    """Rows lie E rounded up to a multiple of 32 apart; K of the product is split (many small widths) or not."""
+    W = _layer(T, d, E, 1, 16)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    x = torch.randn(T, d, generator=g, device="cuda").to(BF)
+    E32 = -(-E // 32) * 32
+    with fresh_memory_is_nan():
+        ws = moevie.Workspace(T, d, E, 1, 16)
+        s = moevie.moevie_router_logits(x, W.W_r, ws)
+    check_status(ws)
+    whole = s.as_strided((T, E32), (E32, 1))
+    assert not bool(whole[:, E:].any())
+    assert bool(torch.isfinite(s).all())
+    mine = torch.full((T, E32), float("nan"), device="cuda")
+    moevie.moevie_router_logits(x, W.W_r, ws, s=mine)
+    assert torch.equal(mine, whole)
