@@ -141,7 +141,7 @@ __device__ __forceinline__ P8 ld_param(const float* p, int col, bool act, float 
 // ------------------------------------------------------------ 8-bit checkpoints
 
 // The whole number nearest to 127 x / amax, an even one between two, where y, that value in fp32
-// (off by at most 127 * 2^-21), is too near to a border to tell.  254 x and (2 n + 1) amax decide, each as a
+// (off by less than 1.2e-4), is too near to a border to tell.  254 x and (2 n + 1) amax decide, each as a
 // rounded product and what it left out (their operands 2^-8 times the values: no overflow; amax >= 2^-110 and
 // |x| >= amax / 254 leave every bit in range).  The rounded products differ by 2^-11 of themselves at most,
 // so their difference is exact; what they left out are whole multiples of x's last place below 2^17 of it, so
@@ -181,7 +181,9 @@ __device__ __forceinline__ float warp_max_nan(float a) {
 // whose values all lie below 2^-110 is kept as zeros.
 __device__ __forceinline__ uint2 q8_block(const P8& v, float& scale) {
     constexpr float ROUND = 12582912.0f;   // 1.5 * 2^23: adding it rounds to a whole number, whose low byte it shows
-    constexpr float NEAR = 0.4999f;        // 0.5 less more than y can be off
+    // 0.5 less more than y can be off: 127 times 2^-23 (the reciprocal), 2^-22 (see below) and three roundings, 7e-5;
+    // from amax 2^126 on, where the reciprocal is subnormal, up to 2^-21 in its place, 1.2e-4
+    constexpr float NEAR = 0.49987f;
     constexpr float R127 = 1.0f / 127.0f;
     float x[8];
 #pragma unroll
@@ -196,7 +198,7 @@ __device__ __forceinline__ uint2 q8_block(const P8& v, float& scale) {
         return make_uint2(0u, 0u);
     }
     // 127 / amax, a little more than that (by 2^-22): the one border that whole blocks meet often,
-    // 63.5 at x = amax / 2, is then rounded to 64, as it has to be
+    // 63.5 at x = amax / 2, is then rounded to 64, as it has to be (a subnormal reciprocal may lose as much)
     float inv;
     asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(amax));
     inv *= 127.0f * (1.0f + 0x1p-22f);
@@ -218,8 +220,9 @@ __device__ __forceinline__ uint2 q8_block(const P8& v, float& scale) {
     }
     if (worst > NEAR) {
         bool border = false;
+        const float half = amax < 0x1p126f ? 0.5f * amax : -1.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) border |= fabsf(e[i]) > NEAR && fabsf(x[i]) != 0.5f * amax;
+        for (int i = 0; i < 8; ++i) border |= fabsf(e[i]) > NEAR && fabsf(x[i]) != half;
         if (border) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)

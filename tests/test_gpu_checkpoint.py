@@ -137,3 +137,27 @@ def test_what_is_refused():
         moevie.moevie_checkpoint_load(ck, torch.float16)
     with pytest.raises(ValueError):
         moevie.moevie_checkpoint_load(ck, out=torch.empty(3, 64, device="cuda"))
+
+
+def test_borders_between_codes_of_the_largest_and_smallest_blocks():
+    """As above where 1 / amax is subnormal, and at the smallest amax that is kept; and amax / 2, 63.5 codes, of many
+    blocks, which is 64."""
+    g = torch.Generator()
+    g.manual_seed(0)
+    top = torch.finfo(torch.float32).max
+    some = torch.ldexp(1 + torch.rand(3000, generator=g), torch.tensor(126)) * torch.randint(1, 3, (3000,), generator=g)
+    some = some[some < top]
+    some = torch.cat([some, torch.tensor([3.3524566e38, 3.35e38, 2.0 ** 127, 2.0 ** 126, 3.4e38, 2.0 ** -110, 1e-33])])
+    rows = torch.zeros(len(some), 128)
+    rows[:, 0], rows[:, 5], rows[:, 77] = some, some / 2, -some / 2
+    ck = _check(rows.cuda())
+    assert bool((ck.codes[:, 5] == 64).all()) and bool((ck.codes[:, 77] == -64).all())
+    rows = []
+    for amax in [2.0 ** 126, 2.0 ** 127, 1.9999999 * 2.0 ** 126, 3.35e38, 3.3524566e38, 3.4e38, 2.0 ** -110, 1e-33]:
+        a = torch.tensor(amax, dtype=torch.float32)
+        half = ((torch.arange(-127, 127, dtype=torch.float64) + 0.5) * a.double() / 127).float()
+        for v in (half, *(torch.nextafter(half, torch.tensor(s)) for s in (float("inf"), float("-inf")))):
+            rows += [torch.cat([a.reshape(1), part]) for part in v.split(127)]
+    x = torch.stack(rows).cuda()
+    assert x.shape[1] == 128
+    _check(x)
