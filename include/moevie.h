@@ -414,7 +414,8 @@ typedef struct moevie_rows {
 /* 8-bit checkpoint of activations x [T, d] (bf16, or fp32 where x_f32): of each row every block of 128
  * columns (the last one what is left) keeps amax = max |x| as scale = amax / 127 in fp32 and its values as
  * int8 codes, the whole number nearest to 127 x / amax (an even one between two, decided exactly).  A
- * value is code * scale, off by at most amax / 254 and a rounding.  A block whose values all lie below
+ * value is code * scale, off by at most amax / 254 and a rounding (where amax is the largest finite float, whose
+ * scale times 127 would not be finite, scale is the next float below).  A block whose values all lie below
  * 2^-110 is kept as zeros; one that holds an infinity or a NaN comes back as NaN.  d % 8 == 0;
  * codes: int8 [T, d], 16-byte aligned; scale: fp32 [T, ceil(d / 128)].  moevie_checkpoint_load writes the
  * values as bf16 or fp32.  T == 0 launches nothing. */

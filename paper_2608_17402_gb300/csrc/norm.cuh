@@ -20,6 +20,7 @@ constexpr int NORM_THREADS = 256;   // of a CTA, at most, but for the forward of
 constexpr int fwd_slots(bool f32, bool big) { return f32 || big ? 3 : 4; }   // rows under way
 constexpr int BWD_SLOTS = 2;
 constexpr float Q8_LEAST = 7.70371978e-34f;   // 2^-110: blocks of smaller values are kept as zeros
+constexpr float Q8_MOST = 0x1.020406p+121f;   // the largest scale: 127 times the next float is no finite one
 
 // ------------------------------------------------------------ 8 columns of a row
 
@@ -202,9 +203,10 @@ __device__ __forceinline__ uint2 q8_block(const P8& v, float& scale) {
     float inv;
     asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(amax));
     inv *= 127.0f * (1.0f + 0x1p-22f);
-    // amax / 127, correctly rounded (Markstein: the remainder of a quotient within one unit corrects it)
+    // amax / 127, correctly rounded (Markstein: the remainder of a quotient within one unit corrects it); of the
+    // largest float the next one below, that its values come back finite
     const float guess = amax * R127;
-    scale = fmaf(fmaf(-127.0f, guess, amax), R127, guess);
+    scale = fminf(fmaf(fmaf(-127.0f, guess, amax), R127, guess), Q8_MOST);
     uint32_t q[8];
     float e[8], worst = 0.f;
     const uint64_t in2 = f2_of(inv), up = f2_of(ROUND), down = f2_of(-ROUND), minus = f2_of(-1.0f);

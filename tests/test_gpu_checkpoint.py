@@ -161,3 +161,19 @@ def test_borders_between_codes_of_the_largest_and_smallest_blocks():
     x = torch.stack(rows).cuda()
     assert x.shape[1] == 128
     _check(x)
+
+
+def test_the_largest_finite_value_comes_back_finite():
+    """127 times the nearest float to its 127th part lies beyond it: the scale is the next float below."""
+    top = torch.finfo(torch.float32).max
+    x = torch.zeros(3, 256, device="cuda")
+    x[0, 3], x[1, 200], x[2, 0], x[2, 1], x[2, 2] = top, -top, top, top / 2, -top / 100
+    ck = moevie.moevie_checkpoint_store(x)
+    got = moevie.moevie_checkpoint_load(ck, torch.float32)
+    assert bool(torch.isfinite(got).all())
+    assert ck.codes[0, 3] == 127 and ck.codes[1, 200] == -127 and ck.codes[2, 1] == 64 and ck.codes[2, 2] == -1
+    scale = ck.scale.repeat_interleave(128, 1).double()
+    assert bool(((got.double() - x.double()).abs() <= (0.5 + 127 * 2.0 ** -22) * scale).all())
+    below = torch.nextafter(torch.tensor(top), torch.tensor(0.0)).item()
+    y = torch.full((1, 128), below, device="cuda")
+    _check(y)
