@@ -333,7 +333,8 @@ __global__ void __launch_bounds__(BAL_THREADS, VEC * VPL > 8 ? 1 : 2) bal_main_k
 #pragma unroll
             for (int u = 0; u < TU; ++u) {
                 if (u * TPW >= left) continue;
-                // (sums of 4e-5 and more, or 0: the approximate reciprocal is as good as a division here)
+                // (Sums are 0, or at least 1 of a softmax and e^-17 of sigmoids, whose largest logit lies at -17 or above,
+                // and at most 1024: the approximate reciprocal is as good as a division there.)
                 const float inv = sums[2 * u] == 0.f ? 0.f : rcp_approx(sums[2 * u]);
                 const float dot = sums[2 * u + 1] * inv;
                 if (l == 0) {

@@ -175,6 +175,28 @@ def test_low_rows_among_others(E):
     check(s, idx)
 
 
+@pytest.mark.parametrize("E", [8, 33, 256, 1000])
+def test_one_logit_at_the_border_of_low_rows(E):
+    """Rows of one logit on either side of -17, where the way to take them changes, over others far below it: their
+    scores add up to as little as e^-17.  An exponential of x is off by |x| 2^-24 of itself, of 60 at most here (below
+    -17 the row's largest logit is taken off first): 2^-18, twice for a probability."""
+    s, idx = make(40, E, 2)
+    for t, top in enumerate((-16.0, -16.9, -16.9999, -17.0, -17.0001, -17.1, -30.0, -88.0, -100.0)):
+        s[t] = top - 43.0
+        s[t, (3 * t) % E] = top
+    ws = moevie.BalanceWorkspace(40, E, 2)
+    out = moevie.moevie_balance_loss(s, idx, ws, 0.03, "sigmoid")
+    check_status(ws)
+    z = s.double().requires_grad_()
+    loss, _, c, p = loss64(z, idx.long(), torch.zeros(40, dtype=torch.int64, device="cuda"), 1, E, 0.03, "sigmoid")
+    (want,) = torch.autograd.grad(loss, z)
+    p, dev = p.detach(), (c - 0.03 / 40).abs()
+    size = (p * dev).sum(1, keepdim=True)
+    tol = 2.0 ** -17 * p * (dev + size) + 2.0 ** -48 * p * c.abs().sum(1, keepdim=True) + 1e-37
+    assert bool(((out.ds.double() - want).abs() <= tol).all())
+    assert abs(float(out.loss) - float(loss.detach())) <= 2.0 ** -17 * (float(size.sum()) + float(loss.detach()))
+
+
 def test_even_loads_have_no_gradient_and_the_loss_coef():
     s, _ = make(64, 16, 2)
     idx = torch.stack([torch.arange(64) % 8, 8 + torch.arange(64) % 8], 1).to(torch.int32).cuda()
