@@ -26,7 +26,12 @@ namespace {
 
 constexpr int BAL_COUNT_THREADS = 1024;
 constexpr int BAL_PART_IDS = 8192;    // ids a CTA of bal_count_kernel counts, about
-constexpr int64_t BAL_FEW_IDS = 65536;   // up to here CTAs of bal_main_kernel count for themselves
+// Up to so many ids, and so many a run in the mean, CTAs of bal_main_kernel count for themselves: a launch less, but
+// each counts every run that it has rows of.  64 experts, 8 ids a token, counted so and by bal_count_kernel, us:
+// one run of 4096 ids 6.1 and 8.3, 16384 8.7 and 8.9, 65536 17.3 and 9.0; 32 runs of 65536 ids together 7.2 and 9.3
+// (16 and 256 experts change sides at the same numbers).  Alike runs would gain beyond the first limit (262144 ids
+// in 32 runs: 9.8 and 11.2); it bounds what a single long one among them can cost.
+constexpr int64_t BAL_FEW_IDS = 65536, BAL_FEW_IDS_RUN = 16384;
 constexpr int BAL_THREADS = 512;
 constexpr int BAL_AHEAD = 2;   // rounds
 
@@ -421,7 +426,7 @@ cudaError_t run_main(const BalanceArgs& a, cudaStream_t s) {
 }  // namespace
 
 int bal_parts(int64_t T, int64_t k, int64_t G) {
-    if (T * k <= BAL_FEW_IDS) return 0;
+    if (T * k <= std::min(BAL_FEW_IDS, G * BAL_FEW_IDS_RUN)) return 0;
     const int64_t n = (T * k + G * BAL_PART_IDS - 1) / (G * BAL_PART_IDS);
     return (int)std::max<int64_t>(1, std::min<int64_t>(n, BAL_MAX_PARTS));
 }

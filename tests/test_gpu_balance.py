@@ -197,6 +197,20 @@ def test_one_logit_at_the_border_of_low_rows(E):
     assert abs(float(out.loss) - float(loss.detach())) <= 2.0 ** -17 * (float(size.sum()) + float(loss.detach()))
 
 
+@pytest.mark.parametrize("T,E,k,G", [(2048, 64, 8, 1), (2049, 64, 8, 1), (4096, 31, 8, 2), (4097, 31, 8, 2), (8192, 16, 8, 4),
+                                     (8193, 16, 8, 32)])
+def test_both_ways_of_counting(T, E, k, G):
+    """On either side of the numbers of ids where the way to count them changes, ids at addresses of 16 bytes and not."""
+    s, idx = make(T, E, k, skew=0.5)
+    gen = torch.Generator()
+    gen.manual_seed(T)
+    seg = runs(T, G, gen) if G > 1 else None
+    want = check(s, idx, seg=seg)
+    apart = torch.empty(T * k + 1, dtype=torch.int32, device="cuda")[1:].view(T, k).copy_(idx)
+    got = check(s, apart, seg=seg)
+    assert torch.equal(got.loss, want.loss) and torch.equal(got.counts, want.counts) and torch.equal(got.ds, want.ds)
+
+
 def test_even_loads_have_no_gradient_and_the_loss_coef():
     s, _ = make(64, 16, 2)
     idx = torch.stack([torch.arange(64) % 8, 8 + torch.arange(64) % 8], 1).to(torch.int32).cuda()
