@@ -865,7 +865,8 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
                                   ws: ResidualNormWorkspace, out: ResidualNormGrads | None = None,
                                   stream=None) -> ResidualNormGrads:
     """Gradients of moevie_residual_norm.  dr [T, d]: the gradient of r1 but for what comes through u, of the
-    residual stream's type (None: zero); du: the gradient of u, fp32 (dx of moevie_moe_backward) or bf16 (None
+    residual stream's type (None: zero; ``out`` or r then say that type, and with r a Checkpoint and no ``out`` it is
+    bf16); du: the gradient of u, fp32 (dx of moevie_moe_backward) or bf16 (None
     where norms.pre is None); r (r1) and f: the forward's rows or their Checkpoints; stats as the forward gave
     them.  f = None without ``out``: the forward ran without f (with it, out.df says so).  Returns dr (may be the
     given one, as out.dr), df bf16 and the gradients of norms' weights, fp32.  Rows of dr and df outside norms' runs
@@ -873,6 +874,8 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
     are zeros."""
     dev, d = _device(), norms.d
     N, at = norms.c_struct(dev), _scratch(ws, dev)
+    if dr is None and du is None:
+        raise ValueError("dr and du: one of them has to be given")
     T = _matrix(dr if dr is not None else du, d, "dr" if dr is not None else "du")
     if out is None:
         dtype = dr.dtype if dr is not None else r.dtype if isinstance(r, torch.Tensor) else _BF16

@@ -146,3 +146,16 @@ def test_a_kept_tensor_without_memory_is_refused(make, no_library):
         storage.resize_(size)
         getattr(owner, field).zero_()
         call()
+
+
+def test_the_type_of_a_stream_without_a_gradient(no_library):
+    """dr = None: the stream's type is that of out.dr, else of r, and bf16 where neither says it."""
+    n, s = moevie.ResidualNorm(D, "layer"), torch.zeros(T, 2)
+    du, ck = torch.zeros(T, D), moevie.Checkpoint.empty(T, D, "cpu")
+    out = moevie.ResidualNormGrads.empty(n, T, F32, join=False, device="cpu")
+
+    def back(r, **kw):
+        return moevie.moevie_residual_norm_backward(n, None, du, r, None, s, None, WS, **kw).dr.dtype
+    assert back(ck, out=out) is F32 and back(torch.zeros(T, D)) is F32 and back(ck) is BF
+    with pytest.raises(ValueError):
+        moevie.moevie_residual_norm_backward(n, None, None, ck, None, s, None, WS)
