@@ -142,7 +142,7 @@ def _stream(stream=None):
 
 
 def _call(name, *args):
-    rc = getattr(load(), name)(*args)
+    rc = getattr(_lib or load(), name)(*args)
     if rc != 0:
         raise MoevieError(name, rc)
 
@@ -599,15 +599,16 @@ _NORMS_PACK, _ROWS_PACK = _NORMS.pack, _ROWS.pack
 
 
 def _rows(t, shape, dtype, dev, name):
-    """The address of ``t``, a contiguous tensor of this shape and ``dtype`` (one, or a tuple) on the current
-    device ``dev``."""
+    """The address of ``t``, a contiguous tensor of this shape (None: any) and ``dtype`` (one, or a tuple) on the
+    current device ``dev``."""
     dt = t.dtype
-    if ((dt is dtype or (type(dtype) is tuple and dt in dtype)) and t.get_device() == dev and t.shape == shape and
-            t.is_contiguous()):
+    if ((dt is dtype or (type(dtype) is tuple and dt in dtype)) and (shape is None or t.shape == shape) and
+            t.get_device() == dev and t.is_contiguous()):
         at = t.data_ptr()
         if at or not t.numel():   # (memory that its storage has given up has no address)
             return at
-    raise ValueError(f"{name}: expected a contiguous tensor {tuple(shape)} of {dtype} on the current device cuda:{dev}, "
+    of = "" if shape is None else f" {tuple(shape)}"
+    raise ValueError(f"{name}: expected a contiguous tensor{of} of {dtype} on the current device cuda:{dev}, "
                      f"got {dt} on {t.device} with shape {tuple(t.shape)}, strides {t.stride()} and address {t.data_ptr()}")
 
 
@@ -618,11 +619,6 @@ def _device():
 
 def _on(stream, dev):
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
-
-
-def _maybe(t, shape, dtype, dev, name):
-    """_rows of a tensor that may be None."""
-    return None if t is None else _rows(t, shape, dtype, dev, name)
 
 
 def _scratch(ws, dev):
@@ -670,17 +666,23 @@ class Checkpoint:
         return self.codes.shape
 
     def addresses(self, T, d, dev):
-        return (_rows(self.codes, (T, d), _I8, dev, "checkpoint codes"),
-                _rows(self.scale, (T, -(-d // Q8_BLOCK)), _F32, dev, "checkpoint scale"))
+        c, s, blocks = self.codes, self.scale, (T, (d + Q8_BLOCK - 1) // Q8_BLOCK)
+        if (c.dtype is _I8 and s.dtype is _F32 and c.shape == (T, d) and s.shape == blocks and c.is_contiguous() and
+                s.is_contiguous() and c.get_device() == dev == s.get_device()):
+            at = c.data_ptr(), s.data_ptr()
+            if at[0] and at[1]:
+                return at
+        return _rows(c, (T, d), _I8, dev, "checkpoint codes"), _rows(s, blocks, _F32, dev, "checkpoint scale")
 
 
 def moevie_checkpoint_store(x, out: Checkpoint | None = None, stream=None) -> Checkpoint:
     """The 8-bit checkpoint of x [T, d] (bf16 or fp32), in ``out`` where given."""
-    if x.dim() != 2:
-        raise ValueError(f"x: expected [T, d], got {tuple(x.shape)}")
-    T, d = x.shape
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError(f"x: expected [T, d], got {tuple(shape)}")
+    T, d = shape
     dev = _device()
-    at = _rows(x, (T, d), _RES, dev, "x")
+    at = _rows(x, None, _RES, dev, "x")
     if out is None:
         out = _made(stream, Checkpoint.empty, T, d, x.device)
     _call("moevie_checkpoint_store", at, int(x.dtype is _F32), T, d, *out.addresses(T, d, dev), _on(stream, dev))
@@ -796,10 +798,11 @@ class ResidualNormOut:
                 None if s2 is None else _rows(s2, stats, _F32, dev, "out.stats_post"), *kept)
 
 
-def _rows_struct(t, T, d, dtype, dev, name):
+def _rows_struct(t, T, d, shape, dtype, dev, name):
+    """A moevie_rows of T rows of d values; shape: (T, d), or None where t's has been looked at."""
     if isinstance(t, Checkpoint):
         return _ROWS_PACK(*t.addresses(T, d, dev), 2)
-    return _ROWS_PACK(_rows(t, (T, d), dtype, dev, name), 0, _ROW_TYPES[t.dtype])
+    return _ROWS_PACK(_rows(t, shape, dtype, dev, name), 0, _ROW_TYPES[t.dtype])
 
 
 def _matrix(t, d, name):
@@ -818,7 +821,7 @@ def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, o
     dev, d = _device(), norms.d
     N, at = norms.c_struct(dev), _scratch(ws, dev)
     T = _matrix(r, d, "r")
-    R = _rows_struct(r, T, d, _RES, dev, "r")
+    R = _rows_struct(r, T, d, None, _RES, dev, "r")
     join = f is not None
     F = _rows(f, r.shape, _BF16, dev, "f") if join else None
     dtype = _BF16 if isinstance(r, Checkpoint) else r.dtype
@@ -855,10 +858,13 @@ class ResidualNormGrads:
 
     def addresses(self, T, d, G, dev):
         rows, row = (T, d), (d,)
-        return (_rows(self.dr, rows, _RES, dev, "out.dr"), _maybe(self.df, rows, _BF16, dev, "out.df"),
-                _maybe(self.dw_pre, row, _F32, dev, "out.dw_pre"), _maybe(self.db_pre, row, _F32, dev, "out.db_pre"),
-                _maybe(self.dw_post, row, _F32, dev, "out.dw_post"), _maybe(self.db_post, row, _F32, dev, "out.db_post"),
-                _maybe(self.dgate, (G, d), _F32, dev, "out.dgate"))
+        df, w1, b1, w2, b2, gate = self.df, self.dw_pre, self.db_pre, self.dw_post, self.db_post, self.dgate
+        return (_rows(self.dr, rows, _RES, dev, "out.dr"), None if df is None else _rows(df, rows, _BF16, dev, "out.df"),
+                None if w1 is None else _rows(w1, row, _F32, dev, "out.dw_pre"),
+                None if b1 is None else _rows(b1, row, _F32, dev, "out.db_pre"),
+                None if w2 is None else _rows(w2, row, _F32, dev, "out.dw_post"),
+                None if b2 is None else _rows(b2, row, _F32, dev, "out.db_post"),
+                None if gate is None else _rows(gate, (G, d), _F32, dev, "out.dgate"))
 
 
 def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, stats_post,
@@ -882,11 +888,13 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
         out = _made(stream, ResidualNormGrads.empty, norms, T, dtype, f is not None, ws.buf.device, _new(norms.seg))
     results = out.addresses(T, d, norms.G, dev)
     res, shape = out.dr.dtype, (T, d)
-    R = _rows_struct(r, T, d, res, dev, "r") if r is not None else None
-    F = _rows_struct(f, T, d, _BF16, dev, "f") if f is not None else None
-    dr1, du1 = _maybe(dr, shape, res, dev, "dr"), _maybe(du, shape, _RES, dev, "du")
+    R = _rows_struct(r, T, d, shape, res, dev, "r") if r is not None else None
+    F = _rows_struct(f, T, d, shape, _BF16, dev, "f") if f is not None else None
+    dr1 = None if dr is None else _rows(dr, shape, res, dev, "dr")
+    du1 = None if du is None else _rows(du, shape, _RES, dev, "du")
     shape = (T, 2)
-    s1, s2 = _maybe(stats_pre, shape, _F32, dev, "stats_pre"), _maybe(stats_post, shape, _F32, dev, "stats_post")
+    s1 = None if stats_pre is None else _rows(stats_pre, shape, _F32, dev, "stats_pre")
+    s2 = None if stats_post is None else _rows(stats_post, shape, _F32, dev, "stats_post")
     _call("moevie_residual_norm_backward", N, dr1, int(res is _F32), du1,
           int(du is not None and du.dtype is _F32), R, F, s1, s2, T, *results, at, ws.nbytes, _on(stream, dev))
     if T == 0:   # nothing was launched: sums over no rows
