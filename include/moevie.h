@@ -392,7 +392,8 @@ typedef struct moevie_norms {
     const float* gate;      /* fp32 [G, d] or NULL: 1 */
     const int32_t* seg;     /* int32 [G + 1], device: run g is rows [seg[g], seg[g + 1]); NULL: one run
                              * of all rows (G = 1).  Ascending within [0, T] (else MOEVIE_ERR_DEVICE in the
-                             * status); runs may be empty.  Rows in front of seg[0] and from seg[G] on are
+                             * status); runs may be empty.  Every warp reads them for itself: they must not
+                             * change while a call runs.  Rows in front of seg[0] and from seg[G] on are
                              * padding: never read, and left as they were in every output (moevie_moe_forward
                              * and moevie_moe_backward read all rows: clear them in what these get, once where
                              * the buffer is kept). */

@@ -10,8 +10,9 @@
 // gives the loss and ds.  p_t adds up to 1: with c_be = C_be - coef / T, formed from the whole number
 // E n_be - k T_b, nothing cancels where loads are nearly even:
 //   p.C = p.c + coef / T,   softmax: ds = p (c - p.c),   sigmoid: ds = p (1 - sigmoid(s)) (c - p.c).
-// HBM bounds it: s is read and ds written once, 8 T E bytes (65536 x 256, sigmoid: 32.4 us, 4.2 TB/s; about 7 of
-// them counting and starting, 21 the pass at 60% of the issue slots, 3 the last CTAs and the loss).  Where all ids together are few, every CTA
+// s is read and ds written once, 8 T E bytes; 65536 x 256, sigmoid: 32.7 us, 4.2 TB/s, about 7 of them counting and
+// starting, 21 the pass (instructions and their latency: 60% of the issue slots, DRAM 39% busy), 3 the last CTAs and
+// the loss.  Where ids are few, every CTA
 // of bal_main_kernel counts those of its runs by itself; otherwise bal_count_kernel first counts them in
 // parts, which bal_main_kernel adds up.
 #include <math.h>

@@ -3,13 +3,13 @@
 //
 //   r1 = alpha r + gate * N_post(f),   u = N_pre(r1)
 //
-// with N an RMS or layer norm over a row's d columns.  Every kernel here is bound by HBM: a row's
-// operands are read once, its results written once, and all arithmetic is fp32.  One thread owns 8
-// columns (16 bytes of bf16, 32 of fp32), ceil(d / 256) warps own a row, and a group of such warps
-// walks a contiguous range of rows, so that weights, the gate and the sums of the weights'
-// gradients stay on chip over the whole range.  Measured, bytes that have to move over the time: forward of
-// 65536 x 1664 in fp32 6.4 TB/s (95% of a plain copy's rate); of 8192 x 1024 in bf16 with two checkpoints
-// 3.7 TB/s (36 us; 60% of the issue slots, of which the codes take more than half).
+// with N an RMS or layer norm over a row's d columns.  A row's operands are read once, its results written
+// once, and all arithmetic is fp32.  One thread owns 8 columns (16 bytes of bf16, 32 of fp32), ceil(d / 256) warps
+// own a row, and a group of such warps walks a contiguous range of rows, so that weights, the gate and the sums of
+// the weights' gradients stay on chip over the whole range.  Measured, bytes that have to move over the time:
+// forward of 65536 x 1664 in fp32 6.4 TB/s, bound by HBM (95% of a plain copy's rate); of 8192 x 1024 in bf16 with
+// two checkpoints 3.7 TB/s (36 us), bound by the instructions, of which the codes are more than half, and their
+// latency: 60% of the issue slots at a third of the warps an SM could hold.
 #include "norm.cuh"
 
 namespace mv {
