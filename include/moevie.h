@@ -395,8 +395,8 @@ typedef struct moevie_norms {
                              * status); runs may be empty.  Every warp reads them for itself: they must not
                              * change while a call runs.  Rows in front of seg[0] and from seg[G] on are
                              * padding: never read, and left as they were in every output (moevie_moe_forward
-                             * and moevie_moe_backward read all rows: clear them in what these get, once where
-                             * the buffer is kept). */
+                             * and moevie_moe_backward read all rows: clear them in what these get, with
+                             * moevie_clear_padding, once where the buffer is kept). */
     int64_t G;
     float residual_scale;   /* finite */
     float eps;              /* > 0, finite */
@@ -462,6 +462,17 @@ moevie_status moevie_residual_norm_backward(const moevie_norms* n, const void* d
                                             const float* stats_pre, const float* stats_post, int64_t T, void* dr,
                                             void* df, float* dw_pre, float* db_pre, float* dw_post, float* db_post,
                                             float* dgate, void* ws, size_t ws_bytes, void* stream);
+
+/* Zeros in rows of padding, which the calls above and moevie_balance_loss leave as they were: of up to 16 buffers of
+ * T rows, row_bytes each (a multiple of 4; rows 4-byte aligned, one behind the other), the rows in front of seg[0]
+ * and from seg[G] on (seg as in moevie_norms; an end outside [0, T] counts as its nearest end).  T < 2^31, G <= 2^20;
+ * T == 0 launches nothing. */
+typedef struct moevie_buffer {
+    void* rows;
+    int64_t row_bytes;
+} moevie_buffer;
+moevie_status moevie_clear_padding(const moevie_buffer* buffers, int n_buffers, int64_t T, const int32_t* seg, int64_t G,
+                                   void* stream);
 
 /* ------------------------------------------------ balance loss
  *

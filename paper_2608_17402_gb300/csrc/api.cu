@@ -1362,6 +1362,24 @@ moevie_status moevie_residual_norm_backward(const moevie_norms* n, const void* d
     return cuda_status(launch_norm_backward(a, res_f32, du_f32, q, static_cast<cudaStream_t>(stream)));
 }
 
+moevie_status moevie_clear_padding(const moevie_buffer* buffers, int n_buffers, int64_t T, const int32_t* seg, int64_t G,
+                                   void* stream) {
+    if (T < 0 || G < 1 || n_buffers < 1) return MOEVIE_ERR_INVALID_ARG;
+    if (T >= (int64_t(1) << 31) || G > MAX_RUNS || n_buffers > MAX_PADDED_BUFFERS) return MOEVIE_ERR_UNSUPPORTED;
+    if (T == 0) return MOEVIE_OK;
+    if (!buffers || !seg || !a4(seg)) return MOEVIE_ERR_INVALID_ARG;
+    PaddedBuffers b = {};
+    b.n = n_buffers;
+    for (int i = 0; i < n_buffers; ++i) {
+        const int64_t bytes = buffers[i].row_bytes;
+        if (!buffers[i].rows || !a4(buffers[i].rows) || bytes <= 0 || bytes % 4 != 0 || bytes >= (int64_t(1) << 31))
+            return MOEVIE_ERR_INVALID_ARG;
+        b.rows[i] = buffers[i].rows;
+        b.row_bytes[i] = bytes;
+    }
+    return cuda_status(launch_clear_padding(b, T, seg, G, static_cast<cudaStream_t>(stream)));
+}
+
 moevie_status moevie_balance_workspace_size(int64_t T_max, int64_t E, int64_t k, int64_t G, size_t* bytes) {
     if (!bytes) return MOEVIE_ERR_INVALID_ARG;
     const moevie_status c = check_balance(T_max, E, k, G);

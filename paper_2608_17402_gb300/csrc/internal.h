@@ -473,6 +473,13 @@ cudaError_t launch_shared_rows(int64_t T, int64_t base, int S, int E, float lamb
 cudaError_t launch_combine(const __nv_bfloat16* rows, const int32_t* inv, const float* gate,
                            const __nv_bfloat16* shared, float lambda, int64_t T, int k, int d,
                            __nv_bfloat16* y, cudaStream_t s);
+constexpr int MAX_PADDED_BUFFERS = 16;
+struct PaddedBuffers {   // T rows of row_bytes each, both multiples of 4
+    void* rows[MAX_PADDED_BUFFERS];
+    int64_t row_bytes[MAX_PADDED_BUFFERS];
+    int n;
+};
+cudaError_t launch_clear_padding(const PaddedBuffers& b, int64_t T, const int32_t* seg, int64_t G, cudaStream_t s);
 cudaError_t launch_wait_probe(DevStatus* st, uint64_t limit_ns, cudaStream_t s);
 
 

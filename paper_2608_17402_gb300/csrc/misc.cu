@@ -3,7 +3,10 @@
 //   f32_to_bf16_kernel   y := bf16(y accumulator)  (32-byte loads, 16-byte stores)
 //   combine_kernel       Eq. (6) as a stand-alone gather-reduce over expert-major
 //                        rows: y[t] = sum_j gate[t, j] rows[inv[t*k + j]] + lambda * shared[t]
+//   clear_padding_kernel zeros in the rows of padding of up to 16 buffers
 //   wait_probe_kernel    bounded wait on a barrier nobody arrives at (error-path test)
+#include <algorithm>
+
 #include "internal.h"
 
 namespace mv {
@@ -16,6 +19,28 @@ __global__ void zero_f32_kernel(float4* __restrict__ p, int64_t n4) {
     for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < n4;
          i += (int64_t)gridDim.x * blockDim.x)
         p[i] = z;
+}
+
+// Zeros in [p, p + bytes), both multiples of 4, by the whole grid; 16 bytes at a time but for the ends.
+__device__ __forceinline__ void clear_bytes(char* p, int64_t bytes) {
+    const int64_t at = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x), step = (int64_t)gridDim.x * blockDim.x;
+    const int64_t head = min((int64_t)(-reinterpret_cast<uintptr_t>(p) & 15u), bytes), n16 = (bytes - head) / 16;
+    const int64_t tail = head + 16 * n16;
+    if (4 * at < head) *reinterpret_cast<uint32_t*>(p + 4 * at) = 0u;
+    for (int64_t i = at; i < n16; i += step) *reinterpret_cast<uint4*>(p + head + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
+    if (tail + 4 * at < bytes) *reinterpret_cast<uint32_t*>(p + tail + 4 * at) = 0u;
+}
+
+// Writes alone, and often none.  Residual norm of 65536 x 1664 in fp32, 63 runs, one call alone: 219 us on kept
+// buffers, 235 on fresh ones with this launch behind it, 349 with the fresh buffers zeroed whole in front.
+__global__ void __launch_bounds__(256) clear_padding_kernel(const PaddedBuffers b, int64_t T, const int32_t* seg, int64_t G) {
+    pdl_wait();
+    const int64_t lo = min(max((int64_t)seg[0], (int64_t)0), T), hi = min(max((int64_t)seg[G], lo), T);
+    for (int i = 0; i < b.n; ++i) {
+        char* rows = static_cast<char*>(b.rows[i]);
+        clear_bytes(rows, lo * b.row_bytes[i]);
+        clear_bytes(rows + hi * b.row_bytes[i], (T - hi) * b.row_bytes[i]);
+    }
 }
 
 // n8 groups of 8 values.
@@ -192,6 +217,15 @@ int grid_for(int64_t n, int threads) {
 }
 
 }  // namespace
+
+cudaError_t launch_clear_padding(const PaddedBuffers& b, int64_t T, const int32_t* seg, int64_t G, cudaStream_t s) {
+    int64_t most = 0;   // bytes of the largest buffer: 16 to a thread, up to two CTAs of 256 an SM
+    for (int i = 0; i < b.n; ++i) most = std::max(most, T * b.row_bytes[i]);
+    const int grid = (int)std::min<int64_t>((most + 16 * 256 - 1) / (16 * 256), 2 * GB300_SMS);
+    const cudaError_t e = launch_pdl(clear_padding_kernel, dim3(grid), dim3(256), 0, s, b, T, seg, G);
+    count_launches(1);
+    return e;
+}
 
 cudaError_t launch_zero_f32(float* p, int64_t n, cudaStream_t s) {
     const int64_t n4 = n / 4;   // callers pass multiples of 4

@@ -31,7 +31,8 @@ C_ENTRY_POINTS = ("moevie_status_string", "moevie_version", "moevie_workspace_si
                   "moevie_update_bias", "moevie_backward_workspace_size", "moevie_moe_backward",
                   "moevie_few_workspace_size", "moevie_moe_few",
                   "moevie_orthogonalize_workspace_size", "moevie_orthogonalize", "moevie_muon_update",
-                  "moevie_checkpoint_store", "moevie_checkpoint_load", "moevie_residual_norm_workspace_size",
+                  "moevie_checkpoint_store", "moevie_checkpoint_load", "moevie_clear_padding",
+                  "moevie_residual_norm_workspace_size",
                   "moevie_residual_norm", "moevie_residual_norm_backward", "moevie_balance_workspace_size",
                   "moevie_balance_loss", "moevie_router_logits", "moevie_moe_backward_balanced",
                   "moevie_test_route_logits",
@@ -109,6 +110,7 @@ def load():
                                ctypes.c_int),
         "moevie_checkpoint_store": ([P, ctypes.c_int, I64, I64, P, P, P], ctypes.c_int),
         "moevie_checkpoint_load": ([P, P, I64, I64, P, ctypes.c_int, P], ctypes.c_int),
+        "moevie_clear_padding": ([P, ctypes.c_int, I64, P, I64, P], ctypes.c_int),
         "moevie_residual_norm_workspace_size": ([I64] * 3 + [P], ctypes.c_int),
         "moevie_residual_norm": ([P, P, P, I64] + [P] * 9 + [SZ, P], ctypes.c_int),
         "moevie_residual_norm_backward": ([P, P, ctypes.c_int, P, ctypes.c_int, P, P, P, P, I64] + [P] * 8 + [SZ, P],
@@ -643,10 +645,21 @@ def _clear(stream, *tensors):
                 t.zero_()
 
 
-def _new(seg):
-    """How a call makes its buffers: the kernels leave rows outside the runs as they are, and what comes next (the
-    layer and its backward) reads every row."""
-    return torch.empty if seg is None else torch.zeros
+def moevie_clear_padding(seg, *buffers, stream=None):
+    """Zeros in the rows outside the runs ``seg`` (int32 [G + 1]) of contiguous tensors [T, ...] (None: passed over) on
+    the current device.  The calls that take runs leave these rows as they are, but for buffers that they make."""
+    dev, pairs, T = _device(), [], None
+    for t in buffers:
+        if t is None:
+            continue
+        if t.dim() < 1 or (T is not None and t.shape[0] != T):
+            raise ValueError(f"expected tensors of as many rows, got {tuple(t.shape)} beside {T} rows")
+        T = t.shape[0]
+        pairs += (_rows(t, None, t.dtype, dev, "buffer"), t.numel() // max(1, T) * t.element_size())
+    if T:
+        at = _rows(seg, (seg.numel(),), _I32, dev, "seg")
+        _call("moevie_clear_padding", struct.pack(f"@{len(pairs)}q", *pairs), len(pairs) // 2, T, at, seg.numel() - 1,
+              _on(stream, dev))
 
 
 @dataclass
@@ -657,9 +670,9 @@ class Checkpoint:
     scale: torch.Tensor   # fp32 [T, ceil(d / 128)]
 
     @classmethod
-    def empty(cls, T, d, device="cuda", new=torch.empty):
-        return cls(new((T, d), dtype=torch.int8, device=device),
-                   new((T, -(-d // Q8_BLOCK)), dtype=torch.float32, device=device))
+    def empty(cls, T, d, device="cuda"):
+        return cls(torch.empty((T, d), dtype=torch.int8, device=device),
+                   torch.empty((T, -(-d // Q8_BLOCK)), dtype=torch.float32, device=device))
 
     @property
     def shape(self):
@@ -771,18 +784,21 @@ class ResidualNormOut:
     save_f: Checkpoint | None = None
 
     @classmethod
-    def empty(cls, norms: ResidualNorm, T, dtype=torch.bfloat16, save=False, join=True, device="cuda", new=torch.empty):
-        """Buffers for T rows; rows outside norms' runs stay as ``new`` (torch.empty or torch.zeros) makes them."""
+    def empty(cls, norms: ResidualNorm, T, dtype=torch.bfloat16, save=False, join=True, device="cuda"):
+        """Buffers for T rows, of which nothing is written yet (rows outside norms' runs: moevie_clear_padding)."""
         d = norms.d
 
         def stats(kind):
-            return new((T, 2), dtype=torch.float32, device=device) if kind else None
+            return torch.empty((T, 2), dtype=torch.float32, device=device) if kind else None
 
-        return cls(new((T, d), dtype=dtype, device=device) if join else None,
-                   new((T, d), dtype=torch.bfloat16, device=device) if norms.pre else None,
+        return cls(torch.empty((T, d), dtype=dtype, device=device) if join else None,
+                   torch.empty((T, d), dtype=torch.bfloat16, device=device) if norms.pre else None,
                    stats(norms.pre), stats(norms.post if join else None),
-                   Checkpoint.empty(T, d, device, new) if save else None,
-                   Checkpoint.empty(T, d, device, new) if save and join else None)
+                   Checkpoint.empty(T, d, device) if save else None, Checkpoint.empty(T, d, device) if save and join else None)
+
+    def row_buffers(self):
+        kept = [t for ck in (self.save_r, self.save_f) if ck is not None for t in (ck.codes, ck.scale)]
+        return self.r, self.u, self.stats_pre, self.stats_post, *kept
 
     def addresses(self, T, d, dtype, join, dev):
         if join and self.r is None:
@@ -825,10 +841,13 @@ def moevie_residual_norm(norms: ResidualNorm, r, f, ws: ResidualNormWorkspace, o
     join = f is not None
     F = _rows(f, r.shape, _BF16, dev, "f") if join else None
     dtype = _BF16 if isinstance(r, Checkpoint) else r.dtype
-    if out is None:
-        out = _made(stream, ResidualNormOut.empty, norms, T, dtype, save, join, ws.buf.device, _new(norms.seg))
+    made = out is None
+    if made:
+        out = _made(stream, ResidualNormOut.empty, norms, T, dtype, save, join, ws.buf.device)
     _call("moevie_residual_norm", N, R, F, T, *out.addresses(T, d, dtype, join, dev), at,
           ws.nbytes, _on(stream, dev))
+    if made and norms.seg is not None:
+        moevie_clear_padding(norms.seg, *out.row_buffers(), stream=stream)
     return out
 
 
@@ -844,14 +863,14 @@ class ResidualNormGrads:
     dgate: torch.Tensor | None = None
 
     @classmethod
-    def empty(cls, norms: ResidualNorm, T, dtype=torch.bfloat16, join=True, device="cuda", new=torch.empty):
-        """Buffers for T rows; rows of dr and df outside norms' runs stay as ``new`` makes them."""
+    def empty(cls, norms: ResidualNorm, T, dtype=torch.bfloat16, join=True, device="cuda"):
+        """Buffers for T rows, of which nothing is written yet (rows outside norms' runs: moevie_clear_padding)."""
         def like(t):
             return None if t is None else torch.empty_like(t)
 
         post = join and norms.post
-        return cls(new((T, norms.d), dtype=dtype, device=device),
-                   new((T, norms.d), dtype=torch.bfloat16, device=device) if join else None,
+        return cls(torch.empty((T, norms.d), dtype=dtype, device=device),
+                   torch.empty((T, norms.d), dtype=torch.bfloat16, device=device) if join else None,
                    *(like(t) for t in ((norms.w_pre, norms.b_pre) if norms.pre else (None, None))),
                    *(like(t) for t in ((norms.w_post, norms.b_post) if post else (None, None))),
                    like(norms.gate if join else None))
@@ -883,9 +902,10 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
     if dr is None and du is None:
         raise ValueError("dr and du: one of them has to be given")
     T = _matrix(dr if dr is not None else du, d, "dr" if dr is not None else "du")
-    if out is None:
+    made = out is None
+    if made:
         dtype = dr.dtype if dr is not None else r.dtype if isinstance(r, torch.Tensor) else _BF16
-        out = _made(stream, ResidualNormGrads.empty, norms, T, dtype, f is not None, ws.buf.device, _new(norms.seg))
+        out = _made(stream, ResidualNormGrads.empty, norms, T, dtype, f is not None, ws.buf.device)
     results = out.addresses(T, d, norms.G, dev)
     res, shape = out.dr.dtype, (T, d)
     R = _rows_struct(r, T, d, shape, res, dev, "r") if r is not None else None
@@ -899,6 +919,8 @@ def moevie_residual_norm_backward(norms: ResidualNorm, dr, du, r, f, stats_pre, 
           int(du is not None and du.dtype is _F32), R, F, s1, s2, T, *results, at, ws.nbytes, _on(stream, dev))
     if T == 0:   # nothing was launched: sums over no rows
         _clear(stream, out.dw_pre, out.db_pre, out.dw_post, out.db_post, out.dgate)
+    elif made and norms.seg is not None:
+        moevie_clear_padding(norms.seg, out.dr, out.df, stream=stream)
     return out
 
 
@@ -946,11 +968,11 @@ class BalanceOut:
     ds: torch.Tensor | None       # fp32 [T, E], the gradient of the logits (None: not wanted)
 
     @classmethod
-    def empty(cls, T, E, G=1, grad=True, device="cuda", new=torch.empty):
-        """Buffers for T tokens; rows of ds outside the runs stay as ``new`` makes them."""
+    def empty(cls, T, E, G=1, grad=True, device="cuda"):
+        """Buffers for T tokens, of which nothing is written yet (rows of ds outside the runs: moevie_clear_padding)."""
         return cls(torch.empty(1, dtype=torch.float32, device=device),
                    torch.empty((G, E), dtype=torch.int32, device=device),
-                   new((T, E), dtype=torch.float32, device=device) if grad else None)
+                   torch.empty((T, E), dtype=torch.float32, device=device) if grad else None)
 
     def addresses(self, T, E, G, dev):
         """Of loss, counts and ds, and the stride of ds."""
@@ -985,10 +1007,13 @@ def moevie_balance_loss(s, idx, ws: BalanceWorkspace, coef=0.01, score="sigmoid"
     ids = _rows(idx, (T, k), _I32, dev, "idx")
     G = 1 if seg is None else seg.numel() - 1
     runs = None if seg is None else _rows(seg, (G + 1,), _I32, dev, "seg")
-    if out is None:
-        out = _made(stream, BalanceOut.empty, T, E, G, grad, s.device, _new(seg))
+    made = out is None
+    if made:
+        out = _made(stream, BalanceOut.empty, T, E, G, grad, s.device)
     _call("moevie_balance_loss", s.data_ptr(), ld, ids, T, E, k, runs, G, _SCORES[score], coef,
           *out.addresses(T, E, G, dev), at, ws.nbytes, _on(stream, dev))
+    if made and seg is not None:
+        moevie_clear_padding(seg, out.ds, stream=stream)
     return out
 
 

@@ -159,3 +159,59 @@ def test_columns_between_rows_of_logits_are_zeros(T, d, E):
     mine = torch.full((T, E32), float("nan"), device="cuda")
     moevie.moevie_router_logits(x, W.W_r, ws, s=mine)
     assert torch.equal(mine, whole)
+
+
+@pytest.mark.parametrize("T", [1, 2, 7, 300, 5000])
+def test_clear_padding(T):
+    """Rows of 4 to 6656 bytes at every address of 4 bytes; ends of runs outside the rows, or that do not ascend, stay
+    within the buffers."""
+    gen = torch.Generator()
+    gen.manual_seed(T)
+    for ends in ((0, T), (0, 0), (T, T), (T // 2, T), (0, T // 2), (T // 3, 2 * T // 3), (-5, T + 5), (T // 2, -1), (T + 3, T + 9)):
+        lo = min(max(ends[0], 0), T)
+        hi = min(max(ends[1], lo), T)
+        seg = torch.tensor([ends[0], (lo + hi) // 2, ends[1]], dtype=torch.int32, device="cuda")
+        whole, want, rows = [], [], []
+        for i, words in enumerate((1, 2, 3, 5, 8, 31, 33, 1664)):
+            off = i % 4
+            t = torch.randint(1, 1 << 30, (off + T * words + 9,), generator=gen, dtype=torch.int32).cuda()
+            w = t.clone()
+            part = w[off:off + T * words].view(T, words)
+            part[:lo] = 0
+            part[hi:] = 0
+            whole.append(t)
+            want.append(w)
+            rows.append(t[off:off + T * words].view(T, words))
+        moevie.moevie_clear_padding(seg, *rows)
+        for t, w in zip(whole, want):
+            assert torch.equal(t, w), ends
+
+
+def test_clear_padding_on_a_stream_and_in_a_graph():
+    seg = torch.tensor([10, 20], dtype=torch.int32, device="cuda")
+    x, y = torch.ones(50, 33, device="cuda"), torch.ones(50, 8, dtype=torch.int8, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(graph, stream=s):
+            moevie.moevie_clear_padding(seg, x, None, y)
+    torch.cuda.synchronize()
+    seg.copy_(torch.tensor([5, 50], dtype=torch.int32))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert not bool(x[:5].any()) and not bool(y[:5].any()) and bool((x[5:] == 1).all()) and bool((y[5:] == 1).all())
+    seg.copy_(torch.tensor([5, 48], dtype=torch.int32))
+    torch.cuda.synchronize()
+    moevie.moevie_clear_padding(seg, x, y, stream=s)
+    torch.cuda.synchronize()
+    assert not bool(x[48:].any()) and not bool(y[48:].any()) and bool((x[5:48] == 1).all()) and bool((y[5:48] == 1).all())
+
+
+def test_clear_padding_of_large_buffers():
+    """More than 2^31 bytes in front of the runs."""
+    T, words = (1 << 31) // 1664 + 2000, 1664
+    x = torch.ones(T, words, dtype=torch.int8, device="cuda")
+    seg = torch.tensor([T - 7, T - 3], dtype=torch.int32, device="cuda")
+    moevie.moevie_clear_padding(seg, x)
+    assert not bool(x[:T - 7].any()) and bool((x[T - 7:T - 3] == 1).all()) and not bool(x[T - 3:].any())
